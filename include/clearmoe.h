@@ -50,7 +50,11 @@ typedef enum {
     CLEARMOE_ETIMEOUT = -5      /* a bounded device-side wait ran out */
 } clearmoe_status;
 
-typedef enum { CLEARMOE_F32 = 0, CLEARMOE_BF16 = 1 } clearmoe_dtype;
+typedef enum {
+    CLEARMOE_F32 = 0,
+    CLEARMOE_BF16 = 1,
+    CLEARMOE_FP8 = 2 /* weights of clearmoe_ffn_weights only: 8-bit blocks (clearmoe_fp8) */
+} clearmoe_dtype;
 
 /* Capacity of a layer handle. d and hidden are fixed per handle; T, E and r are per call and
  * bounded by max_tokens, max_E and max_r. dtype selects the arithmetic:
@@ -88,7 +92,7 @@ typedef struct {
  * output layer and the argmax run in fp32 on the routing kernel, so the decision is taken on fp32
  * logits as for the linear router. hidden: a multiple of 16 (bf16) or 4 (fp32), at most H / 2
  * (bf16) or H (fp32): the hidden layer lives in the hidden-state workspace before fc1 runs. */
-typedef enum { CLEARMOE_ACT_RELU = 0, CLEARMOE_ACT_GELU = 1 } clearmoe_act;
+typedef enum { CLEARMOE_ACT_NONE = -1, CLEARMOE_ACT_RELU = 0, CLEARMOE_ACT_GELU = 1 } clearmoe_act;
 typedef struct {
     const void* W_in;
     const void* b_in;
@@ -336,6 +340,104 @@ int clearmoe_set_profile_events(clearmoe_layer* layer, void* const* events, int3
 int clearmoe_route_noalloc(const void* x, int64_t T, int32_t d, int32_t dtype,
                            const clearmoe_router* router, int32_t E, int32_t* idx, int32_t* counts,
                            int32_t* offsets, int32_t* perm, int32_t* status, void* stream);
+
+/* ---- 8-bit floating point with one scale per block of 128 ----
+ *
+ * A matrix [rows x cols] in e4m3 with power-of-two scales: value = e4m3(q) 2^(s - 127).
+ *   q      one byte per element, row-major, rows of cols rounded up to a multiple of 128 bytes; the bytes past
+ *          cols are zero (the quantising calls write them). 32-byte aligned.
+ *   scale  one byte s per block, row-major, rows of 4 ceil(cols / 512) bytes, of which the first
+ *          ceil(cols / 128) are used. 4-byte aligned. Blocks are 128 columns wide; those of activations one
+ *          row high (rows scale rows), those of weights 128 rows (ceil(rows / 128) scale rows).
+ * The quantising calls give each block the least s with max |value| <= 448 2^(s - 127) (448: e4m3's largest
+ * value; s = 0 at the least) and round value 2^(127 - s) to nearest even. A block with an infinity or a NaN
+ * gets s = 255, which stands for NaN: every value of the block, and every output that depends on it, is NaN.
+ * Scales are powers of two so that the tensor cores apply them inside the product, exactly.
+ * Both buffers are the caller's. rows <= 2^30, cols <= 2^24. */
+typedef struct {
+    void* q;
+    uint8_t* scale;
+    int64_t rows;
+    int64_t cols;
+} clearmoe_fp8;
+
+/* Activations x [out->rows x out->cols] (dtype CLEARMOE_F32 or CLEARMOE_BF16, rows ld elements apart, ld >=
+ * cols, any alignment of the element type) to 1 x 128 blocks. gather (nullable, int32 [out->rows], device): row
+ * i is x's row gather[i] instead. No handle; stream-ordered; x may be the preceding kernel's output. */
+int clearmoe_fp8_quantize_rows(const void* x, int32_t dtype, int64_t ld, const int32_t* gather, const clearmoe_fp8* out,
+                               void* stream);
+
+/* A weight matrix W [out->rows x out->cols] to 128 x 128 blocks; arguments as above. Once per weight set. */
+int clearmoe_fp8_quantize_weight(const void* W, int32_t dtype, int64_t ld, const clearmoe_fp8* out, void* stream);
+
+/* The values that a matrix stands for, rounded once to dtype: out [rows x cols], rows ld elements apart.
+ * block_rows: 1 for activations, 128 for weights. */
+int clearmoe_fp8_dequantize(const clearmoe_fp8* in, int32_t block_rows, void* out, int32_t dtype, int64_t ld, void* stream);
+
+/* What follows the product: + bias[n] (nullable, [N] of bias_dtype F32 or BF16, device), then the activation.
+ * status (nullable, int32, device): receives CLEARMOE_ETIMEOUT if a bounded device-side wait (1 s) runs out, in
+ * which case the outputs are undefined; the call does not clear it. */
+typedef struct {
+    const void* bias;
+    int32_t bias_dtype;
+    int32_t act; /* clearmoe_act */
+    int32_t* status;
+} clearmoe_fp8_epilogue;
+
+/* out = act(A W^T + bias): A [M x K] activations, W [N x K] weights (A->cols == W->cols), products of e4m3 values
+ * and the scales exact, sums in fp32, the result rounded once to out_dtype (F32 or BF16) and stored at
+ * out [M x N], rows ldo elements apart (ldo >= N, any alignment of the element type). epi may be NULL (no bias, no
+ * activation). N <= 2^24. No handle and no workspace; stream-ordered; out must not alias an input. */
+int clearmoe_fp8_gemm(const clearmoe_fp8* A, const clearmoe_fp8* W, const clearmoe_fp8_epilogue* epi, void* out,
+                      int32_t out_dtype, int64_t ldo, void* stream);
+
+/* The same with the fp32 result quantised as clearmoe_fp8_quantize_rows would: out [M x N] in 8-bit blocks, the
+ * next product's activations, without its intermediate in memory. */
+int clearmoe_fp8_gemm_fp8(const clearmoe_fp8* A, const clearmoe_fp8* W, const clearmoe_fp8_epilogue* epi,
+                          const clearmoe_fp8* out, void* stream);
+
+/* Grouped by expert: rows [offsets[e], offsets[e + 1]) of A (offsets: int32 [E + 1], device, ascending from 0 to
+ * A->rows; an expert may have none) times W[e]^T (host array of E matrices of the same shape); row i goes to
+ * row perm[i] of out (perm: nullable int32 [M], device; a permutation). 1 <= E <= 16. */
+int clearmoe_fp8_grouped_gemm(const clearmoe_fp8* A, const clearmoe_fp8* W, int32_t E, const int32_t* offsets,
+                              const int32_t* perm, const clearmoe_fp8_epilogue* epi, void* out, int32_t out_dtype,
+                              int64_t ldo, void* stream);
+
+/* The weights of a folded layer (clearmoe_fold_basis), bound once and passed to each of the two forwards below.
+ *  dtype            of W1, W_comb and W2: the layer's own, or CLEARMOE_FP8 (a bf16 layer's weights in 8-bit
+ *                   blocks). With the layer's own dtype only the q of each matrix is read, a dense row-major
+ *                   matrix (16-byte aligned); rows and cols must say its shape in any case.
+ *  W1 [H x d], W_comb[e] [d x H] for e < E; b1 [H] and the linear router in the layer's dtype.
+ *  b2, cls_stride, W2 ([d x H], read with cls_stride > 0 only), input_layernorm: as clearmoe_ffn_options. */
+typedef struct {
+    int32_t dtype;
+    int32_t E;
+    clearmoe_fp8 W1;
+    clearmoe_fp8 W2;
+    clearmoe_fp8 W_comb[16];
+    const void* b1;
+    const void* b2;
+    clearmoe_router router;
+    int64_t cls_stride;
+    int32_t input_layernorm;
+} clearmoe_ffn_weights;
+
+/* The whole folded layer for a few tokens, 1 <= T <= CLEARMOE_FEW_MAX: y_t = W_comb[a_t] GELU(W1 x_t + b1)
+ * (+ b2), a_t as clearmoe_route's, in two launches: one takes every token through the router and fc1, the other
+ * through its expert; only experts that have a token are read. Weights of the layer's dtype or 8-bit blocks
+ * (bf16 layers; the weights' values times unquantised activations). Sums in fp32; z is stored in the layer's
+ * dtype as in the other forwards; fp32 layers use three TF32 products per term (relative error near 2^-21). The
+ * routing can be read with clearmoe_get_routing. Errors as clearmoe_ffn_forward_folded_ex. */
+#define CLEARMOE_FEW_MAX 64
+int clearmoe_ffn_forward_few(clearmoe_layer* layer, const void* x, int64_t T, const clearmoe_ffn_weights* w, void* out,
+                             void* stream);
+
+/* The whole folded layer of a bf16 handle with both products in 8-bit blocks (w->dtype CLEARMOE_FP8): the
+ * tokens routed in bf16 as clearmoe_route, x (after the LayerNorm, with input_layernorm) quantised in expert
+ * order, z = GELU(W1 x + b1) quantised in fc1's epilogue, out = W_comb[a] z (+ b2) in bf16. 1 <= T <= max_tokens.
+ * Errors as clearmoe_ffn_forward_folded_ex; EUNSUPPORTED for fp32 handles and other weight types. */
+int clearmoe_ffn_forward_fp8(clearmoe_layer* layer, const void* x, int64_t T, const clearmoe_ffn_weights* w, void* out,
+                             void* stream);
 
 /* Static string for a status code. */
 const char* clearmoe_strerror(int status);

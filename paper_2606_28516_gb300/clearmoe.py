@@ -14,7 +14,7 @@ _LIB_PATH = pathlib.Path(__file__).resolve().parent / "libclearmoe.so"
 _lib = None
 
 OK, EINVAL, EUNSUPPORTED, ECUDA, ENOMEM, ETIMEOUT = 0, -1, -2, -3, -4, -5
-F32, BF16 = 0, 1
+F32, BF16, FP8 = 0, 1, 2
 
 
 class ClearMoEError(RuntimeError):
@@ -43,7 +43,23 @@ class clearmoe_ffn_options(ctypes.Structure):
                 ("router_in_fc1", ctypes.c_int32)]
 
 
-ACT_RELU, ACT_GELU = 0, 1
+class clearmoe_fp8(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64)]
+
+
+class clearmoe_fp8_epilogue(ctypes.Structure):
+    _fields_ = [("bias", ctypes.c_void_p), ("bias_dtype", ctypes.c_int32), ("act", ctypes.c_int32),
+                ("status", ctypes.c_void_p)]
+
+
+class clearmoe_ffn_weights(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("E", ctypes.c_int32), ("W1", clearmoe_fp8), ("W2", clearmoe_fp8),
+                ("W_comb", clearmoe_fp8 * 16), ("b1", ctypes.c_void_p), ("b2", ctypes.c_void_p),
+                ("router", clearmoe_router), ("cls_stride", ctypes.c_int64), ("input_layernorm", ctypes.c_int32)]
+
+
+ACT_NONE, ACT_RELU, ACT_GELU = -1, 0, 1
+FEW_MAX = 64
 
 
 def mlp_router(W_in, b_in, W_out, b_out, act: str = "relu") -> clearmoe_mlp_router:
@@ -88,6 +104,17 @@ _SIGS = {
                                     ctypes.POINTER(clearmoe_router), _I32, _P, _P],
     "clearmoe_route_noalloc": [_P, _I64, _I32, _I32, ctypes.POINTER(clearmoe_router), _I32, _P, _P,
                                _P, _P, _P, _P],
+    "clearmoe_fp8_quantize_rows": [_P, _I32, _I64, _P, ctypes.POINTER(clearmoe_fp8), _P],
+    "clearmoe_fp8_quantize_weight": [_P, _I32, _I64, ctypes.POINTER(clearmoe_fp8), _P],
+    "clearmoe_fp8_dequantize": [ctypes.POINTER(clearmoe_fp8), _I32, _P, _I32, _I64, _P],
+    "clearmoe_fp8_gemm": [ctypes.POINTER(clearmoe_fp8), ctypes.POINTER(clearmoe_fp8),
+                          ctypes.POINTER(clearmoe_fp8_epilogue), _P, _I32, _I64, _P],
+    "clearmoe_fp8_gemm_fp8": [ctypes.POINTER(clearmoe_fp8), ctypes.POINTER(clearmoe_fp8),
+                              ctypes.POINTER(clearmoe_fp8_epilogue), ctypes.POINTER(clearmoe_fp8), _P],
+    "clearmoe_fp8_grouped_gemm": [ctypes.POINTER(clearmoe_fp8), ctypes.POINTER(clearmoe_fp8), _I32, _P, _P,
+                                  ctypes.POINTER(clearmoe_fp8_epilogue), _P, _I32, _I64, _P],
+    "clearmoe_ffn_forward_few": [_P, _P, _I64, ctypes.POINTER(clearmoe_ffn_weights), _P, _P],
+    "clearmoe_ffn_forward_fp8": [_P, _P, _I64, ctypes.POINTER(clearmoe_ffn_weights), _P, _P],
     "clearmoe_strerror": [ctypes.c_int],
     "clearmoe_version": [],
 }
@@ -362,3 +389,178 @@ def clearmoe_route_noalloc(x, Wg, bg, idx, counts, offsets, perm, status=None,
                                         Wg.shape[0], _ptr(idx), _ptr(counts), _ptr(offsets),
                                         _ptr(perm), _ptr(status), _stream(stream)),
            "clearmoe_route_noalloc")
+
+
+# ---------------------------------------------------------------- 8-bit blocks with power-of-two scales
+class Fp8Matrix:
+    """A matrix [rows x cols] in 8-bit blocks (clearmoe_fp8): q, one byte per element in rows of cols rounded up
+    to 128 (float8_e4m3fn or uint8), and its scale bytes, rows of 4 ceil(cols / 512); 128-row blocks for weights,
+    1-row blocks otherwise. Keeps the tensors alive."""
+
+    def __init__(self, q, scale, rows: int, cols: int, weight: bool = False):
+        n_scale = -(-rows // 128) if weight else rows
+        for name, t, shape in (("q", q, (rows, fp8_pitch(cols))), ("scale", scale, (n_scale, fp8_scale_pitch(cols)))):
+            if tuple(t.shape) != shape or t.element_size() != 1:
+                raise ValueError(f"{name} of a {rows} x {cols} matrix in 8-bit blocks is one byte per element of {shape}, "
+                                 f"got {tuple(t.shape)} {t.dtype}")
+        self.q, self.scale, self.rows, self.cols, self.weight = q, scale, rows, cols, weight
+        self.c = clearmoe_fp8(_ptr(q), _ptr(scale), rows, cols)
+        self.ref = ctypes.pointer(self.c)
+
+
+def fp8_pitch(cols: int) -> int:
+    """Bytes from one row of q to the next."""
+    return -(-cols // 128) * 128
+
+
+def fp8_scale_pitch(cols: int) -> int:
+    """Bytes from one row of scales to the next."""
+    return -(-cols // 512) * 4
+
+
+def _fp8_empty(rows, cols, weight, device):
+    import torch
+    q = torch.empty(rows, fp8_pitch(cols), dtype=torch.float8_e4m3fn, device=device)
+    n = -(-rows // 128) if weight else rows
+    return Fp8Matrix(q, torch.empty(n, fp8_scale_pitch(cols), dtype=torch.uint8, device=device), rows, cols, weight)
+
+
+def fp8_rows(rows: int, cols: int, device="cuda") -> Fp8Matrix:
+    """Buffers for activations in 8-bit blocks, to be written by clearmoe_fp8_quantize_rows or a product."""
+    return _fp8_empty(rows, cols, False, device)
+
+
+def fp8_weight(rows: int, cols: int, device="cuda") -> Fp8Matrix:
+    """Buffers for a weight matrix in 8-bit blocks, to be written by clearmoe_fp8_quantize_weight."""
+    return _fp8_empty(rows, cols, True, device)
+
+
+def _matrix(t):
+    """Pointer, dtype and row pitch of a 2-D CUDA tensor whose rows are dense (any pitch)."""
+    name = str(t.dtype)
+    if not t.is_cuda or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("matrices passed to libclearmoe must be 2-D CUDA tensors with dense rows")
+    if name not in ("torch.bfloat16", "torch.float32"):
+        raise ValueError(f"matrices must be bfloat16 or float32, got {name}")
+    ld = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    return t.data_ptr(), BF16 if name == "torch.bfloat16" else F32, ld
+
+
+def _same_shape(t, rows, cols, what):
+    if tuple(t.shape) != (rows, cols):
+        raise ValueError(f"{what} must be [{rows} x {cols}], got {tuple(t.shape)}")
+
+
+def clearmoe_fp8_quantize_rows(x, out: Fp8Matrix, gather=None, stream=None) -> None:
+    """x [rows x cols] (bf16 or fp32, any row pitch) to out in 1 x 128 blocks; gather: int32 source rows."""
+    p, dt, ld = _matrix(x)
+    if gather is None:
+        _same_shape(x, out.rows, out.cols, "x")
+    elif x.shape[1] != out.cols or gather.numel() != out.rows:
+        raise ValueError("x must have out's columns and gather one entry per row of out")
+    _check(lib().clearmoe_fp8_quantize_rows(p, dt, ld, _ptr(gather), out.ref, _stream(stream)),
+           "clearmoe_fp8_quantize_rows")
+
+
+def clearmoe_fp8_quantize_weight(W, out: Fp8Matrix, stream=None) -> None:
+    """W [rows x cols] (bf16 or fp32, any row pitch) to out in 128 x 128 blocks."""
+    p, dt, ld = _matrix(W)
+    _same_shape(W, out.rows, out.cols, "W")
+    _check(lib().clearmoe_fp8_quantize_weight(p, dt, ld, out.ref, _stream(stream)), "clearmoe_fp8_quantize_weight")
+
+
+def clearmoe_fp8_dequantize(m: Fp8Matrix, out, stream=None) -> None:
+    """The values m stands for, rounded to out's dtype (bf16 or fp32)."""
+    p, dt, ld = _matrix(out)
+    _same_shape(out, m.rows, m.cols, "out")
+    _check(lib().clearmoe_fp8_dequantize(m.ref, 128 if m.weight else 1, p, dt, ld, _stream(stream)),
+           "clearmoe_fp8_dequantize")
+
+
+def _epilogue(bias, act, status, N):
+    if bias is None and act == ACT_NONE and status is None:
+        return None
+    if bias is not None and bias.numel() != N:
+        raise ValueError(f"bias must have {N} elements, got {bias.numel()}")
+    dt = BF16 if bias is not None and bias.element_size() == 2 else F32
+    return ctypes.byref(clearmoe_fp8_epilogue(_ptr(bias), dt, act, _ptr(status)))
+
+
+def clearmoe_fp8_gemm(A: Fp8Matrix, W: Fp8Matrix, out, bias=None, act: int = ACT_NONE, status=None, stream=None) -> None:
+    """out = act(A W^T + bias). out: a [M x N] bf16 or fp32 tensor of any row pitch, or an Fp8Matrix of rows (the
+    result quantised, clearmoe_fp8_gemm_fp8)."""
+    epi = _epilogue(bias, act, status, W.rows)
+    if isinstance(out, Fp8Matrix):
+        _check(lib().clearmoe_fp8_gemm_fp8(A.ref, W.ref, epi, out.ref, _stream(stream)), "clearmoe_fp8_gemm_fp8")
+        return
+    p, dt, ld = _matrix(out)
+    _same_shape(out, A.rows, W.rows, "out")
+    _check(lib().clearmoe_fp8_gemm(A.ref, W.ref, epi, p, dt, ld, _stream(stream)), "clearmoe_fp8_gemm")
+
+
+def clearmoe_fp8_grouped_gemm(A: Fp8Matrix, W, offsets, out, perm=None, bias=None, act: int = ACT_NONE, status=None,
+                              stream=None) -> None:
+    """Rows offsets[e] .. offsets[e + 1] of A times W[e]^T (W: a sequence of Fp8Matrix), row i to out[perm[i]]."""
+    if offsets.numel() != len(W) + 1 or (perm is not None and perm.numel() != A.rows):
+        raise ValueError("offsets must have one entry per matrix and one more, perm one per row of A")
+    p, dt, ld = _matrix(out)
+    _same_shape(out, A.rows, W[0].rows, "out")
+    arr = (clearmoe_fp8 * len(W))(*[m.c for m in W])
+    _check(lib().clearmoe_fp8_grouped_gemm(A.ref, arr, len(W), _ptr(offsets), _ptr(perm),
+                                           _epilogue(bias, act, status, W[0].rows), p, dt, ld, _stream(stream)),
+           "clearmoe_fp8_grouped_gemm")
+
+
+# ------------------------------------------------------------- a folded layer's weights and its forwards
+class FfnWeights:
+    """A folded layer's weights bound once (clearmoe_ffn_weights), with the tensors kept alive."""
+
+    def __init__(self, c, keep):
+        self.c, self.keep, self.ref = c, keep, ctypes.pointer(c)
+
+
+def ffn_weights(W1, b1, W_comb, Wg, bg, b2=None, W2=None, cls_stride: int = 0,
+                input_layernorm: bool = False) -> FfnWeights:
+    """W1 [H x d], W_comb (E matrices [d x H]) and W2 (class tokens' dense path) as tensors of the layer's dtype, or
+    all as Fp8Matrix weights; b1, b2, Wg, bg in the layer's dtype."""
+    E, d = Wg.shape
+    if len(W_comb) != E or E > 16:
+        raise ValueError(f"{E} experts (at most 16) need as many matrices, got {len(W_comb)}")
+    fp8 = isinstance(W1, Fp8Matrix)
+    H = W1.rows if fp8 else W1.shape[0]
+
+    def mat(W, rows, cols):
+        if isinstance(W, Fp8Matrix) != fp8 or (fp8 and not W.weight):
+            raise ValueError("W1, W_comb and W2 are all tensors or all Fp8Matrix weights")
+        if fp8:
+            return W.c
+        _same_shape(W, rows, cols, "a weight matrix")
+        return clearmoe_fp8(_ptr(W), None, rows, cols)
+
+    for name, t, n in (("b1", b1, H), ("bg", bg, E), ("b2", b2, d)):
+        if t is not None and t.numel() != n:
+            raise ValueError(f"{name} must have {n} elements, got {t.numel()}")
+    c = clearmoe_ffn_weights()
+    c.dtype = FP8 if fp8 else _matrix(W1)[1]
+    c.E = E
+    c.W1 = mat(W1, H, d)
+    for e in range(E):
+        c.W_comb[e] = mat(W_comb[e], d, H)
+    if W2 is not None:
+        c.W2 = mat(W2, d, H)
+    c.b1, c.b2 = _ptr(b1), _ptr(b2)
+    c.router = _router(Wg, bg)
+    c.cls_stride, c.input_layernorm = int(cls_stride), int(bool(input_layernorm))
+    return FfnWeights(c, (W1, b1, list(W_comb), Wg, bg, b2, W2))
+
+
+def clearmoe_ffn_forward_few(layer: int, x, w: FfnWeights, out, stream=None) -> None:
+    """The whole folded layer for 1 to FEW_MAX tokens."""
+    _check(lib().clearmoe_ffn_forward_few(layer, _ptr(x), x.shape[0], w.ref, _ptr(out), _stream(stream)),
+           "clearmoe_ffn_forward_few")
+
+
+def clearmoe_ffn_forward_fp8(layer: int, x, w: FfnWeights, out, stream=None) -> None:
+    """The whole folded layer with both products in 8-bit blocks."""
+    _check(lib().clearmoe_ffn_forward_fp8(layer, _ptr(x), x.shape[0], w.ref, _ptr(out), _stream(stream)),
+           "clearmoe_ffn_forward_fp8")

@@ -93,6 +93,41 @@ void free_ws(clearmoe_layer* L) {
         if (p) cudaFree(p);
 }
 
+// Bytes of T tokens in 8-bit blocks, x's and z's q and scales one after the other, each from a multiple of 256.
+struct Fp8Workspace {
+    clearmoe_fp8 x, z;
+    size_t bytes;
+};
+Fp8Workspace fp8_workspace_at(void* base, int64_t T, int64_t d, int64_t H) {
+    Fp8Workspace w;
+    size_t at = 0;
+    auto take = [&](size_t n) {
+        uint8_t* p = base ? static_cast<uint8_t*>(base) + at : nullptr;
+        at += (n + 255) / 256 * 256;
+        return p;
+    };
+    w.z.q = take((size_t)(T * cm::fp8_ldq(H)));
+    w.z.scale = take((size_t)(T * cm::fp8_lds(H)));
+    w.x.q = take((size_t)(T * cm::fp8_ldq(d)));
+    w.x.scale = take((size_t)(T * cm::fp8_lds(d)));
+    w.z.rows = w.x.rows = T;
+    w.z.cols = H;
+    w.x.cols = d;
+    w.bytes = at;
+    return w;
+}
+// In the hidden-state workspace, which is at least that large in bf16 layers.
+Fp8Workspace fp8_workspace(const clearmoe_layer* L, int64_t T) {
+    return fp8_workspace_at(L->z, T, L->desc.d, L->desc.hidden);
+}
+// Bytes of the hidden-state workspace: z in the layer's dtype, or (bf16 layers of narrow H, whose rows of 8-bit
+// blocks are padded to 128) x and z in 8-bit blocks where those take more.
+size_t z_bytes(const clearmoe_layer_desc& D, size_t esz) {
+    const size_t plain = (size_t)D.max_tokens * D.hidden * esz;
+    const size_t blocks = D.dtype == CLEARMOE_BF16 ? fp8_workspace_at(nullptr, D.max_tokens, D.d, D.hidden).bytes : 0;
+    return plain > blocks ? plain : blocks;
+}
+
 int check_common(const clearmoe_layer* L, const void* x, int64_t T) {
     if (!L || !x) return CLEARMOE_EINVAL;
     if (T < 1 || T > L->desc.max_tokens) return CLEARMOE_EINVAL;
@@ -323,7 +358,7 @@ int clearmoe_layer_create(const clearmoe_layer_desc* desc, clearmoe_layer** out)
     size_t ncta = (size_t)cm::route_max_ctas(L->num_sms, D.dtype, D.d, D.max_E);
     const size_t nfr = (T + cm::FR_RANGE - 1) / cm::FR_RANGE;
     if (nfr > ncta) ncta = nfr;
-    bool ok = cudaMalloc(&L->z, T * D.hidden * L->esz) == cudaSuccess &&
+    bool ok = cudaMalloc(&L->z, z_bytes(D, L->esz)) == cudaSuccess &&
               cudaMalloc(&L->t, T * D.max_r * L->esz) == cudaSuccess &&
               cudaMalloc((void**)&L->idx, T * 4) == cudaSuccess &&
               cudaMalloc((void**)&L->perm, T * 4) == cudaSuccess &&
@@ -1312,6 +1347,134 @@ int clearmoe_debug_set_wait(clearmoe_layer* L, int64_t wait_limit_ns, int32_t ph
     L->wait_limit_ns = wait_limit_ns;
     L->phantom = phantom_arrivals;
     return CLEARMOE_OK;
+}
+
+// The weights bound in w: what both of its forwards ask of them.
+static int check_ffn_weights(const clearmoe_layer* L, const clearmoe_ffn_weights* w) {
+    if (!w) return CLEARMOE_EINVAL;
+    const bool fp8 = w->dtype == CLEARMOE_FP8;
+    if (!fp8 && w->dtype != CLEARMOE_F32 && w->dtype != CLEARMOE_BF16) return CLEARMOE_EINVAL;
+    if (fp8 ? L->desc.dtype != CLEARMOE_BF16 : w->dtype != L->desc.dtype) return CLEARMOE_EUNSUPPORTED;
+    int rc = check_router(L, &w->router, w->E);
+    if (rc) return rc;
+    if (!w->b1 || misaligned(w->b1) || (w->b2 && misaligned(w->b2))) return CLEARMOE_EINVAL;
+    if (w->cls_stride < 0 || w->cls_stride > ((int64_t)1 << 30)) return CLEARMOE_EINVAL;
+    const int64_t d = L->desc.d, H = L->desc.hidden;
+    auto check = [&](const clearmoe_fp8& m, int64_t rows, int64_t cols) {
+        if (m.rows != rows || m.cols != cols) return (int)CLEARMOE_EINVAL;
+        if (fp8) return cm::check_fp8(&m);
+        return m.q && !misaligned(m.q) ? (int)CLEARMOE_OK : (int)CLEARMOE_EINVAL;
+    };
+    if ((rc = check(w->W1, H, d))) return rc;
+    for (int e = 0; e < w->E; ++e)
+        if ((rc = check(w->W_comb[e], d, H))) return rc;
+    if (w->cls_stride > 0) {
+        if ((rc = check(w->W2, d, H))) return rc;
+        if (w->E + 1 > CM_MAX_E) return CLEARMOE_EUNSUPPORTED;
+    }
+    return CLEARMOE_OK;
+}
+
+int clearmoe_ffn_forward_few(clearmoe_layer* L, const void* x, int64_t T, const clearmoe_ffn_weights* w, void* out,
+                             void* stream) {
+    int rc = check_common(L, x, T);
+    if (rc) return rc;
+    if (!out || misaligned(out)) return CLEARMOE_EINVAL;
+    if ((rc = check_ffn_weights(L, w))) return rc;
+    if (T > CLEARMOE_FEW_MAX) return CLEARMOE_EUNSUPPORTED;
+    cm::FewArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.x = x;
+    a.T = (int)T;
+    a.d = L->desc.d;
+    a.H = L->desc.hidden;
+    a.E = w->E;
+    a.G = w->E + (w->cls_stride > 0 ? 1 : 0);
+    a.f32 = L->desc.dtype == CLEARMOE_F32;
+    a.fp8 = w->dtype == CLEARMOE_FP8;
+    a.W1 = w->W1.q;
+    a.W1_s = w->W1.scale;
+    for (int e = 0; e < a.G; ++e) {
+        const clearmoe_fp8& m = e < w->E ? w->W_comb[e] : w->W2;
+        a.Wc[e] = m.q;
+        a.Wc_s[e] = m.scale;
+    }
+    a.b1 = w->b1;
+    a.b2 = w->b2;
+    a.Wg = w->router.W;
+    a.bg = w->router.b;
+    a.cls_stride = w->cls_stride;
+    a.ln = w->input_layernorm != 0;
+    a.z = L->z;
+    a.idx = L->idx;
+    a.counts = L->counts;
+    a.offsets = L->offsets;
+    a.perm = L->perm;
+    a.out = out;
+    L->last_T = T;
+    L->last_E = w->E;
+    L->last_groups = a.G;
+    return cuda_fail(cm::launch_few(a, L->num_sms, static_cast<cudaStream_t>(stream)));
+}
+
+// The layer in 8-bit blocks: routing and slots as the other forwards (with the LayerNorm's statistics ahead),
+// x quantised in expert order, fc1 with bias, GELU and the next quantisation in its epilogue, the grouped
+// product scattered back to token order.
+int clearmoe_ffn_forward_fp8(clearmoe_layer* L, const void* x, int64_t T, const clearmoe_ffn_weights* w, void* out,
+                             void* stream) {
+    int rc = check_common(L, x, T);
+    if (rc) return rc;
+    if (!out || misaligned(out)) return CLEARMOE_EINVAL;
+    if ((rc = check_ffn_weights(L, w))) return rc;
+    if (w->dtype != CLEARMOE_FP8) return CLEARMOE_EUNSUPPORTED;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const int d = L->desc.d, H = L->desc.hidden, G = w->E + (w->cls_stride > 0 ? 1 : 0);
+    const bool ln = w->input_layernorm != 0;
+    if (ln && (rc = ln_prep(L, x, T, nullptr, w->router.W, w->E, s))) return rc;
+    if ((rc = do_route(L, x, T, &w->router, nullptr, w->E, w->cls_stride, s, ln))) return rc;
+    if ((rc = do_finalize(L, s))) return rc;
+    const Fp8Workspace ws = fp8_workspace(L, T);
+    cm::QuantArgs q;
+    std::memset(&q, 0, sizeof(q));
+    q.x = x;
+    q.ld = d;
+    q.rows = T;
+    q.K = d;
+    q.kb = (d + 127) / 128;
+    q.gather = L->perm;
+    q.ln_stats = ln ? L->ln_stats : nullptr;
+    q.q = static_cast<uint8_t*>(ws.x.q);
+    q.scale = ws.x.scale;
+    q.ldq = cm::fp8_ldq(d);
+    q.lds = cm::fp8_lds(d);
+    if ((rc = cuda_fail(cm::launch_quantize_rows(q, CLEARMOE_BF16, L->num_sms, s)))) return rc;
+    cm::Fp8GemmArgs g;
+    std::memset(&g, 0, sizeof(g));
+    g.status = L->status;
+    g.wait_limit_ns = L->wait_limit_ns;
+    g.bias = w->b1;
+    g.bias_bf16 = 1;
+    g.act = CLEARMOE_ACT_GELU;
+    g.out_kind = cm::FP8_OUT_FP8;
+    g.out = ws.z.q;
+    g.ldo = cm::fp8_ldq(H);
+    g.out_scale = ws.z.scale;
+    g.ldos = cm::fp8_lds(H);
+    if ((rc = cm::run_fp8_gemm(g, &ws.x, &w->W1, 1, L->num_sms, s))) return rc;
+    clearmoe_fp8 experts[CM_MAX_E];
+    for (int e = 0; e < G; ++e) experts[e] = e < w->E ? w->W_comb[e] : w->W2;
+    std::memset(&g, 0, sizeof(g));
+    g.status = L->status;
+    g.wait_limit_ns = L->wait_limit_ns;
+    g.offsets = L->offsets;
+    g.rows = L->perm;
+    g.bias = w->b2;
+    g.bias_bf16 = 1;
+    g.act = CLEARMOE_ACT_NONE;
+    g.out_kind = cm::FP8_OUT_BF16;
+    g.out = out;
+    g.ldo = d;
+    return cm::run_fp8_gemm(g, &ws.z, experts, G, L->num_sms, s);
 }
 
 }  // extern "C"

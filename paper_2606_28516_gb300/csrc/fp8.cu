@@ -1,0 +1,280 @@
+// 8-bit blocks with power-of-two scales: quantisation of activations (1 x 128 blocks) and weights (128 x 128
+// blocks), and back. The product is in fp8_gemm.cu.
+#include <cstdint>
+
+#include "common.cuh"
+#include "fp8.cuh"
+#include "internal.h"
+
+namespace cm {
+
+namespace {
+
+// Eight consecutive elements of a row from column k on, zeros past K. VEC: the row's start and k are 16-byte
+// aligned and K is a multiple of 8, so that eight elements are all inside or all outside.
+template <typename T, bool VEC>
+__device__ __forceinline__ void load8(const T* row, int64_t k, int64_t K, float (&v)[8]) {
+    if (VEC) {
+        if (k >= K) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = 0.f;
+            return;
+        }
+        if (sizeof(T) == 2) {
+            const uint4 u = __ldcg(reinterpret_cast<const uint4*>(row + k));
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[2 * i] = bf16_lo(w[i]);
+                v[2 * i + 1] = bf16_hi(w[i]);
+            }
+        } else {
+            const float4 a = __ldcg(reinterpret_cast<const float4*>(row + k));
+            const float4 b = __ldcg(reinterpret_cast<const float4*>(row + k) + 1);
+            v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float f = 0.f;
+            if (k + i < K) {
+                if (sizeof(T) == 2)
+                    f = bf16_to_f32(__ldcg(reinterpret_cast<const uint16_t*>(row) + k + i));
+                else
+                    f = __ldcg(reinterpret_cast<const float*>(row) + k + i);
+            }
+            v[i] = f;
+        }
+    }
+}
+
+// Activations. A half warp takes a block of 128 columns, eight a lane (16 bytes of bf16 in, 8 bytes out): its
+// largest magnitude by one redux over the half warp, one store of the byte by the half's first lane. Bound by
+// HBM: each element is read once and written once as a byte.
+constexpr int Q_THREADS = 256;
+
+template <typename T, bool VEC, bool LN>
+__global__ void __launch_bounds__(Q_THREADS) quantize_rows_kernel(const QuantArgs a) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int half = (threadIdx.x >> 4) & 1, l16 = threadIdx.x & 15;
+    const uint32_t mask = half ? 0xFFFF0000u : 0x0000FFFFu;
+    const int64_t units = a.rows * a.kb;
+    const int64_t step = (int64_t)gridDim.x * (Q_THREADS / 16);
+    for (int64_t u = (int64_t)blockIdx.x * (Q_THREADS / 16) + (threadIdx.x >> 4); u < units; u += step) {
+        const int64_t row = u / a.kb;
+        const int kb = (int)(u - row * a.kb);
+        const int64_t src = a.gather ? (int64_t)__ldcg(a.gather + row) : row;
+        const int64_t k = (int64_t)kb * 128 + l16 * 8;
+        float v[8];
+        load8<T, VEC>(static_cast<const T*>(a.x) + src * a.ld, k, a.K, v);
+        if (LN) {
+            const float2 st = __ldcg(a.ln_stats + src);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = k + i < a.K ? (v[i] - st.x) * st.y : 0.f;
+        }
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, abs_bits(v[i]));
+        m = __reduce_max_sync(mask, m);
+        const uint32_t s = fp8_scale_byte(m);
+        const float inv = fp8_inverse_scale(s);
+        uint2 o;
+        o.x = fp8_pack4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+        o.y = fp8_pack4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
+        *reinterpret_cast<uint2*>(a.q + row * a.ldq + k) = o;
+        if (l16 == 0) a.scale[row * a.lds + kb] = (uint8_t)s;
+    }
+}
+
+// Weights: a block of 256 threads per 128 x 128 block, 8 columns of 8 rows a thread, read twice (the second
+// time from L1 / L2). Run once per weight set.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) quantize_weight_kernel(const QuantArgs a) {
+    __shared__ uint32_t s_max[8];
+    pdl_wait();
+    const int64_t nb = blockIdx.x / a.kb;
+    const int kb = (int)(blockIdx.x - nb * a.kb);
+    const int l16 = threadIdx.x & 15, r16 = threadIdx.x >> 4;
+    const int64_t k = (int64_t)kb * 128 + l16 * 8;
+    uint32_t m = 0;
+    for (int r = r16; r < 128; r += 16) {
+        const int64_t row = nb * 128 + r;
+        if (row >= a.rows) break;
+        float v[8];
+        load8<T, VEC>(static_cast<const T*>(a.x) + row * a.ld, k, a.K, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, abs_bits(v[i]));
+    }
+    m = __reduce_max_sync(0xFFFFFFFFu, m);
+    if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = m;
+    __syncthreads();
+    m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, s_max[i]);
+    const uint32_t s = fp8_scale_byte(m);
+    const float inv = fp8_inverse_scale(s);
+    for (int r = r16; r < 128; r += 16) {
+        const int64_t row = nb * 128 + r;
+        if (row >= a.rows) break;
+        float v[8];
+        load8<T, VEC>(static_cast<const T*>(a.x) + row * a.ld, k, a.K, v);
+        uint2 o;
+        o.x = fp8_pack4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+        o.y = fp8_pack4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
+        *reinterpret_cast<uint2*>(a.q + row * a.ldq + k) = o;
+    }
+    if (threadIdx.x == 0) a.scale[nb * a.lds + kb] = (uint8_t)s;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256)
+    dequantize_kernel(const uint8_t* q, const uint8_t* scale, int64_t rows, int64_t K, int64_t ldq, int64_t lds,
+                      int block_rows, T* out, int64_t ld) {
+    pdl_wait();
+    const int64_t n = rows * K;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / K, k = i - r * K;
+        const float v = fp8_unpack2(q[r * ldq + k]).x * fp8_scale(scale[r / block_rows * lds + k / 128]);
+        if (sizeof(T) == 2)
+            reinterpret_cast<uint16_t*>(out)[r * ld + k] = f32_to_bf16(v);
+        else
+            reinterpret_cast<float*>(out)[r * ld + k] = v;
+    }
+}
+
+template <typename K, typename... A>
+cudaError_t launch(K kernel, int64_t grid, int threads, cudaStream_t s, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(threads);
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+bool vec_ok(const QuantArgs& a, int esz) {
+    return (reinterpret_cast<uintptr_t>(a.x) & 15) == 0 && a.K % 8 == 0 && (a.ld * esz) % 16 == 0;
+}
+
+}  // namespace
+
+cudaError_t launch_quantize_rows(const QuantArgs& a, int dtype, int num_sms, cudaStream_t s) {
+    const int esz = dtype == CLEARMOE_BF16 ? 2 : 4;
+    const int64_t want = (a.rows * a.kb + Q_THREADS / 16 - 1) / (Q_THREADS / 16);
+    const int64_t grid = want < (int64_t)num_sms * 8 ? want : (int64_t)num_sms * 8;
+    const bool vec = vec_ok(a, esz);
+    if (dtype == CLEARMOE_BF16) {
+        if (a.ln_stats)
+            return vec ? launch(quantize_rows_kernel<uint16_t, true, true>, grid, Q_THREADS, s, a)
+                       : cudaErrorInvalidValue;  // the layer's rows are always aligned
+        return vec ? launch(quantize_rows_kernel<uint16_t, true, false>, grid, Q_THREADS, s, a)
+                   : launch(quantize_rows_kernel<uint16_t, false, false>, grid, Q_THREADS, s, a);
+    }
+    return vec ? launch(quantize_rows_kernel<float, true, false>, grid, Q_THREADS, s, a)
+               : launch(quantize_rows_kernel<float, false, false>, grid, Q_THREADS, s, a);
+}
+
+cudaError_t launch_quantize_weight(const QuantArgs& a, int dtype, cudaStream_t s) {
+    const int esz = dtype == CLEARMOE_BF16 ? 2 : 4;
+    const int64_t grid = (a.rows + 127) / 128 * a.kb;
+    const bool vec = vec_ok(a, esz);
+    if (dtype == CLEARMOE_BF16)
+        return vec ? launch(quantize_weight_kernel<uint16_t, true>, grid, 256, s, a)
+                   : launch(quantize_weight_kernel<uint16_t, false>, grid, 256, s, a);
+    return vec ? launch(quantize_weight_kernel<float, true>, grid, 256, s, a)
+               : launch(quantize_weight_kernel<float, false>, grid, 256, s, a);
+}
+
+}  // namespace cm
+
+namespace {
+
+using cm::fp8_ldq;
+using cm::fp8_lds;
+
+bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+int cuda_code(cudaError_t e) {
+    if (e == cudaSuccess) return CLEARMOE_OK;
+    (void)cudaGetLastError();
+    return CLEARMOE_ECUDA;
+}
+
+int check_pair(const void* x, int32_t dtype, int64_t ld, const clearmoe_fp8* m) {
+    const int rc = cm::check_fp8(m);
+    if (rc) return rc;
+    if (!x || (dtype != CLEARMOE_F32 && dtype != CLEARMOE_BF16) || ld < m->cols) return CLEARMOE_EINVAL;
+    if (ld > (int64_t)1 << 30) return CLEARMOE_EINVAL;
+    return aligned_to(x, dtype == CLEARMOE_BF16 ? 2 : 4) ? CLEARMOE_OK : CLEARMOE_EINVAL;
+}
+
+cm::QuantArgs quant_args(const void* x, int64_t ld, const clearmoe_fp8* m) {
+    cm::QuantArgs a = {};
+    a.x = x;
+    a.ld = ld;
+    a.rows = m->rows;
+    a.K = m->cols;
+    a.kb = (int)((m->cols + 127) / 128);
+    a.q = static_cast<uint8_t*>(m->q);
+    a.scale = m->scale;
+    a.ldq = fp8_ldq(m->cols);
+    a.lds = fp8_lds(m->cols);
+    return a;
+}
+
+}  // namespace
+
+namespace cm {
+
+int check_fp8(const clearmoe_fp8* m) {
+    if (!m || !m->q || !m->scale || m->rows < 1 || m->cols < 1) return CLEARMOE_EINVAL;
+    if (m->rows > (int64_t)1 << 30 || m->cols > (int64_t)1 << 24) return CLEARMOE_EINVAL;
+    return aligned_to(m->q, 32) && aligned_to(m->scale, 4) ? CLEARMOE_OK : CLEARMOE_EINVAL;
+}
+
+}  // namespace cm
+
+extern "C" {
+
+int clearmoe_fp8_quantize_rows(const void* x, int32_t dtype, int64_t ld, const int32_t* gather, const clearmoe_fp8* out,
+                               void* stream) {
+    const int rc = check_pair(x, dtype, ld, out);
+    if (rc) return rc;
+    if (gather && !aligned_to(gather, 4)) return CLEARMOE_EINVAL;
+    const int sms = cm::current_device_sms();
+    if (sms <= 0) return CLEARMOE_ECUDA;
+    cm::QuantArgs a = quant_args(x, ld, out);
+    a.gather = gather;
+    return cuda_code(cm::launch_quantize_rows(a, dtype, sms, static_cast<cudaStream_t>(stream)));
+}
+
+int clearmoe_fp8_quantize_weight(const void* W, int32_t dtype, int64_t ld, const clearmoe_fp8* out, void* stream) {
+    const int rc = check_pair(W, dtype, ld, out);
+    if (rc) return rc;
+    if ((out->rows + 127) / 128 * ((out->cols + 127) / 128) > 0x7FFFFFFF) return CLEARMOE_EUNSUPPORTED;
+    return cuda_code(cm::launch_quantize_weight(quant_args(W, ld, out), dtype, static_cast<cudaStream_t>(stream)));
+}
+
+int clearmoe_fp8_dequantize(const clearmoe_fp8* in, int32_t block_rows, void* out, int32_t dtype, int64_t ld, void* stream) {
+    const int rc = check_pair(out, dtype, ld, in);
+    if (rc) return rc;
+    if (block_rows != 1 && block_rows != 128) return CLEARMOE_EINVAL;
+    const int sms = cm::current_device_sms();
+    if (sms <= 0) return CLEARMOE_ECUDA;
+    const int64_t want = (in->rows * in->cols + 255) / 256, grid = want < (int64_t)sms * 8 ? want : (int64_t)sms * 8;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const uint8_t* q = static_cast<const uint8_t*>(in->q);
+    const int64_t ldq = fp8_ldq(in->cols), lds = fp8_lds(in->cols);
+    if (dtype == CLEARMOE_BF16)
+        return cuda_code(cm::launch(cm::dequantize_kernel<uint16_t>, grid, 256, s, q, (const uint8_t*)in->scale, in->rows,
+                                    in->cols, ldq, lds, (int)block_rows, static_cast<uint16_t*>(out), ld));
+    return cuda_code(cm::launch(cm::dequantize_kernel<float>, grid, 256, s, q, (const uint8_t*)in->scale, in->rows,
+                                in->cols, ldq, lds, (int)block_rows, static_cast<float*>(out), ld));
+}
+
+}  // extern "C"

@@ -1,0 +1,48 @@
+// 8-bit blocks: value = e4m3(q) 2^(s - 127), one scale byte s per block of 128 columns (activations: of one
+// row; weights: of 128 rows). Device helpers shared by the quantiser, the GEMM's epilogue and the few-token
+// kernels.
+#pragma once
+
+#include "common.cuh"
+
+namespace cm {
+
+// Scale byte of a block whose largest |value| has the fp32 bits `amax` (largest as an unsigned integer, so that
+// NaN > inf > every finite value): the least s with amax <= 448 2^(s - 127). 448 = 1.75 2^8 is e4m3's largest
+// value, so s is amax's biased exponent less 8, one more when its significand is above 1.75; held at 0 below
+// (2^-127), 255 (the scale format's NaN) for a block with an infinity or a NaN.
+__device__ __forceinline__ uint32_t fp8_scale_byte(uint32_t amax) {
+    if (amax >= 0x7F800000u) return 255u;
+    const int s = (int)(amax >> 23) - 8 + ((amax & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    return s < 0 ? 0u : (uint32_t)s;
+}
+// 2^(127 - s) of a scale byte that fp8_scale_byte gave (at most 247), NaN for 255.
+__device__ __forceinline__ float fp8_inverse_scale(uint32_t s) {
+    return s == 255u ? __uint_as_float(0x7FC00000u) : __uint_as_float((254u - s) << 23);
+}
+// 2^(s - 127) of any scale byte, NaN for 255.
+__device__ __forceinline__ float fp8_scale(uint32_t s) {
+    return s == 255u ? __uint_as_float(0x7FC00000u) : s == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(s << 23);
+}
+// Two values to e4m3, to nearest even; lo in the low byte. NaN becomes e4m3's NaN.
+__device__ __forceinline__ uint32_t fp8_pack2(float lo, float hi) {
+    uint16_t v;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(v) : "f"(hi), "f"(lo));
+    return v;
+}
+__device__ __forceinline__ uint32_t fp8_pack4(float a, float b, float c, float d) {
+    return fp8_pack2(a, b) | fp8_pack2(c, d) << 16;
+}
+// Two e4m3 values (the low byte first) as fp32, exactly.
+__device__ __forceinline__ float2 fp8_unpack2(uint32_t v) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)v));
+    float2 f;
+    asm("{\n\t.reg .b16 l, u;\n\tmov.b32 {l, u}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, u;\n\t}"
+        : "=f"(f.x), "=f"(f.y)
+        : "r"(h));
+    return f;
+}
+__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+}  // namespace cm

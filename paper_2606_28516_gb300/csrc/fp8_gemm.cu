@@ -1,0 +1,625 @@
+// Products of matrices in 8-bit blocks on the 5th-generation tensor cores (tcgen05, sm_103a):
+//
+//   C[m, n] = epilogue( sum_b 2^(sa[m, b] + sw[n / 128, b] - 254) sum_{k in block b} qa[m, k] qw[n, k] )
+//
+// kind::mxf8f6f4 with block scales takes one power-of-two scale per row and 32 values of K from tensor memory,
+// one byte each, and multiplies in the scale before the fp32 accumulation. A block of 128 is four such
+// 32-blocks with the same byte: the MMA of each K = 32 step names the same byte again. A 32-bit column of scale
+// memory holds four bytes of a row, so four consecutive blocks (512 of K) make one column for 32 rows, and the
+// rows of scales in global memory are padded to whole words: a scale warp moves words as they lie.
+//
+// One persistent, warp-specialised kernel per N tile width:
+//   warps 0-7    epilogue: warp w reads TMEM lane quarter w % 4 (its 32 rows) and column half w / 4;
+//   warps 8-11   scales: warp 8 + q loads the words of rows and of W's blocks and stores them to lane quarter q
+//                (each quarter needs a copy of all), four words of A and BN / 32 of W per 512 of K;
+//   warp 12      TMEM allocation, tcgen05.mma and commits (the whole warp in step, one elected lane issues);
+//   warp 13      TMA producer of the q tiles: 128 rows of A and BN of W, 128 bytes each, 128-byte swizzle.
+// Rings: q stages in shared memory (full: TMA bytes, empty: commit), scale slots in tensor memory (full: one
+// arrival per scale warp, empty: commit), two accumulators. Grouped products walk (group, row tile, column
+// tile) from the device-resident offsets; a row tile never crosses its group's end.
+// Every wait is bounded; a CTA that gives up records CLEARMOE_ETIMEOUT, lets its copies and MMAs in flight
+// finish, frees its tensor memory and returns.
+#include <cstdint>
+#include <cstring>
+
+#include "common.cuh"
+#include "fp8.cuh"
+#include "internal.h"
+
+namespace cm {
+
+namespace {
+
+constexpr int F8_NUM_EPI = 8;
+constexpr int F8_WARP_SCALE = 8, F8_WARP_MMA = 12, F8_WARP_TMA = 13;
+constexpr int F8_THREADS = 32 * 14;
+constexpr int F8_BM = 128;
+constexpr int F8_BK = 128;
+constexpr int F8_SLOTS = 4;        // scale slots, each 512 of K
+constexpr int F8_SLOT_COLS = 12;   // 4 columns of A's scales, up to 8 of W's
+
+template <int BN_>
+struct F8Cfg {
+    static constexpr int BN = BN_;
+    static constexpr int A_BYTES = F8_BM * F8_BK, B_BYTES = BN * F8_BK;
+    static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
+    static constexpr int STAGES = (200 * 1024 / STAGE_BYTES) < 8 ? (200 * 1024 / STAGE_BYTES) : 8;
+    static constexpr int HALF = BN / 2;                    // columns per epilogue warp
+    static constexpr int CW = HALF < 32 ? HALF : 32;       // columns per TMEM read
+    static constexpr int NBARS = 2 * STAGES + 2 * F8_SLOTS + 4 + 1 + 4;
+    static constexpr int SF_COL = 2 * BN;                  // first scale column
+    static constexpr int TMEM_USED = 2 * BN + F8_SLOTS * F8_SLOT_COLS;
+    static constexpr int TMEM_COLS = TMEM_USED <= 128 ? 128 : TMEM_USED <= 256 ? 256 : 512;
+    static_assert(TMEM_USED <= 512);
+    // bias of a chunk per epilogue warp, largest magnitudes of a row's halves, group prefixes
+    static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + F8_NUM_EPI * 32 * 4 + 2 * F8_NUM_EPI * 32 * 4 + NBARS * 8 + 16 +
+                                4 * (CM_MAX_E + 1);
+};
+
+// Instruction descriptor of kind::mxf8f6f4: e4m3 A and W, both K-major, UE8M0 scales; `byte` selects the byte of
+// each scale word.
+__device__ __forceinline__ uint32_t idesc_mxf8(int M, int N, int byte) {
+    return ((uint32_t)byte << 4) | ((uint32_t)(N >> 3) << 17) | (1u << 23) | ((uint32_t)(M >> 4) << 24) |
+           ((uint32_t)byte << 29);
+}
+__device__ __forceinline__ void umma_mxf8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sfa,
+                                          uint32_t sfb, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(
+            d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
+        : "memory");
+}
+#define CM_TMEM_ST_X4(taddr, r)                                                              \
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(taddr), \
+                 "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3])                                  \
+                 : "memory")
+#define CM_TMEM_LD_X32(taddr, r)                                                                                        \
+    asm volatile(                                                                                                       \
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19," \
+        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"                                                      \
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),   \
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),        \
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),       \
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])                     \
+        : "r"(taddr))
+
+struct F8Tile {
+    int64_t m0, hi;  // rows [m0, hi) of the group, of which the tile takes the first 128
+    int n0, e;
+};
+
+__device__ __forceinline__ int64_t f8_off(const Fp8GemmArgs& a, int e) {
+    return a.offsets ? (int64_t)__ldcg(a.offsets + e) : (e == 0 ? 0 : a.M);
+}
+
+__device__ __forceinline__ F8Tile f8_tile(const Fp8GemmArgs& a, int64_t tile, int n_tiles, int bn, const int* s_prefix) {
+    F8Tile t;
+    const int mt = (int)(tile / n_tiles);
+    t.n0 = (int)(tile - (int64_t)mt * n_tiles) * bn;
+    int e = 0;
+    while (e + 1 < a.E && s_prefix[e + 1] <= mt) ++e;
+    t.e = e;
+    t.m0 = f8_off(a, e) + (int64_t)(mt - s_prefix[e]) * F8_BM;
+    t.hi = f8_off(a, e + 1);
+    return t;
+}
+
+__device__ __forceinline__ void st_global_32(void* p, const uint32_t (&v)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+                 "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
+
+// CW accumulator columns + bias, activation; bias from the warp's shared-memory line.
+template <int CW, bool EXACT>
+__device__ __forceinline__ void f8_act(float (&v)[CW], const float* s_bias, bool has_bias, int act) {
+    if (has_bias) {
+#pragma unroll
+        for (int i = 0; i < CW; i += 4) {
+            const float4 b = *reinterpret_cast<const float4*>(s_bias + i);
+            v[i] += b.x, v[i + 1] += b.y, v[i + 2] += b.z, v[i + 3] += b.w;
+        }
+    }
+    if (act == CLEARMOE_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < CW; i += 2) {
+            const float2 u = make_float2(v[i], v[i + 1]);
+            const float2 g = EXACT ? gelu_pair_f32(u) : gelu_pair_bf16(u);
+            v[i] = g.x, v[i + 1] = g.y;
+        }
+    } else if (act == CLEARMOE_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < CW; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];  // NaN stays NaN
+    }
+}
+
+// KIND: Fp8Out.
+template <int BN_, int KIND>
+__global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_constant__ Fp8GemmArgs a) {
+    using C = F8Cfg<BN_>;
+    constexpr int BN = C::BN;
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    unsigned char* sm = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+    float* s_bias = reinterpret_cast<float*>(sm + C::STAGES * C::STAGE_BYTES);  // [epilogue warp][32]
+    uint32_t* s_amax = reinterpret_cast<uint32_t*>(s_bias + F8_NUM_EPI * 32);   // [2][epilogue warp][32]
+    uint64_t* bars = reinterpret_cast<uint64_t*>(s_amax + 2 * F8_NUM_EPI * 32);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::NBARS);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    int* s_prefix = reinterpret_cast<int*>(tmem_slot + 4);
+
+    pdl_launch_dependents();
+    const int warp = warp_uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const uint32_t bar0 = smem_u32(bars);
+    auto full_bar = [&](int s) { return bar0 + 8u * s; };
+    auto empty_bar = [&](int s) { return bar0 + 8u * (C::STAGES + s); };
+    auto sfull_bar = [&](int s) { return bar0 + 8u * (2 * C::STAGES + s); };
+    auto sempty_bar = [&](int s) { return bar0 + 8u * (2 * C::STAGES + F8_SLOTS + s); };
+    auto tfull_bar = [&](int i) { return bar0 + 8u * (2 * C::STAGES + 2 * F8_SLOTS + i); };
+    auto tempty_bar = [&](int i) { return bar0 + 8u * (2 * C::STAGES + 2 * F8_SLOTS + 2 + i); };
+    const uint32_t drain_bar = bar0 + 8u * (2 * C::STAGES + 2 * F8_SLOTS + 4);
+    auto pair_bar = [&](int q) { return bar0 + 8u * (2 * C::STAGES + 2 * F8_SLOTS + 5 + q); };
+    const uint64_t lim = (uint64_t)a.wait_limit_ns;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < C::STAGES; ++s) {
+            mbar_init(full_bar(s), 1);
+            mbar_init(empty_bar(s), 1);
+        }
+        for (int s = 0; s < F8_SLOTS; ++s) {
+            mbar_init(sfull_bar(s), 4);
+            mbar_init(sempty_bar(s), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(tfull_bar(i), 1);
+            mbar_init(tempty_bar(i), F8_NUM_EPI);
+        }
+        mbar_init(drain_bar, 1);
+        for (int q = 0; q < 4; ++q) mbar_init(pair_bar(q), 2);
+        *abort_flag = 0;
+        mbar_fence_init();
+    }
+    if (warp == F8_WARP_MMA) tmem_alloc(smem_u32(tmem_slot), C::TMEM_COLS);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    pdl_wait();  // everything below may read the previous kernel's results
+    if (threadIdx.x == 0) {
+        int acc = 0;
+        for (int e = 0; e < a.E; ++e) {
+            s_prefix[e] = acc;
+            acc += (int)((f8_off(a, e + 1) - f8_off(a, e) + F8_BM - 1) / F8_BM);
+        }
+        s_prefix[a.E] = acc;
+    }
+    __syncthreads();
+    const uint32_t tmem = warp_uniform(*tmem_slot);
+    const int n_tiles = (a.N + BN - 1) / BN;
+    const int64_t num_tiles = warp_uniform((long long)s_prefix[a.E] * n_tiles);
+    const int nkb = a.nkb;
+
+    if (warp == F8_WARP_TMA) {
+        // ------------------------------------------------ TMA producer
+        int stage = 0;
+        uint32_t ph = 0, issued = 0, par = 0;  // bit s: stage s has had a load; parity of its last
+        bool ok = true;
+        for (int64_t tile = blockIdx.x; tile < num_tiles && ok; tile += gridDim.x) {
+            F8Tile t = f8_tile(a, tile, n_tiles, BN, s_prefix);
+            const int e = warp_uniform(t.e), n0 = warp_uniform(t.n0), m0 = warp_uniform((int)t.m0);
+            for (int kb = 0; kb < nkb; ++kb) {
+                if (!mbar_wait_warp(empty_bar(stage), ph ^ 1, abort_flag, a.status, lim)) {
+                    ok = false;
+                    break;
+                }
+                const uint32_t sA = smem_u32(sm + stage * C::STAGE_BYTES);
+                mbar_arrive_expect_tx_warp(full_bar(stage), C::STAGE_BYTES);
+                // coordinates in the maps' 16-bit elements: two bytes each
+                tma_load_2d(sA, &a.tmA, kb * (F8_BK / 2), m0, full_bar(stage));
+                tma_load_2d(sA + C::A_BYTES, &a.tmB[e], kb * (F8_BK / 2), n0, full_bar(stage));
+                issued |= 1u << stage;
+                par = (par & ~(1u << stage)) | (ph << stage);
+                if (++stage == C::STAGES) {
+                    stage = 0;
+                    ph ^= 1;
+                }
+            }
+        }
+        // let every copy in flight land before the CTA retires, whoever gave up
+        for (int s = 0; s < C::STAGES; ++s)
+            if (issued & (1u << s)) mbar_wait_warp(full_bar(s), (par >> s) & 1, nullptr, a.status, lim + 10000000ull);
+    } else if (warp == F8_WARP_MMA) {
+        // ------------------------------------------------ MMA issuer
+        int stage = 0, slot = 0, acc = 0;
+        uint32_t ph = 0, sph = 0, aph = 0;
+        bool ok = true;
+        for (int64_t tile = blockIdx.x; tile < num_tiles && ok; tile += gridDim.x) {
+            if (!mbar_wait_warp(tempty_bar(acc), aph ^ 1, abort_flag, a.status, lim)) break;
+            tc_fence_after();
+            const uint32_t d = tmem + acc * BN;
+            for (int kb = 0; kb < nkb; ++kb) {
+                const int byte = kb & 3;
+                const uint32_t sf = tmem + C::SF_COL + slot * F8_SLOT_COLS;
+                if (byte == 0 && !mbar_wait_warp(sfull_bar(slot), sph, abort_flag, a.status, lim)) {
+                    ok = false;
+                    break;
+                }
+                if (!mbar_wait_warp(full_bar(stage), ph, abort_flag, a.status, lim)) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                const uint32_t sA = smem_u32(sm + stage * C::STAGE_BYTES);
+                const uint64_t ad = sdesc_kmajor_sw128(sA), bd = sdesc_kmajor_sw128(sA + C::A_BYTES);
+                const uint32_t id = idesc_mxf8(F8_BM, BN, byte);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)  // 32 of K: 32 bytes on in each row
+                    umma_mxf8(d, ad + 2 * k, bd + 2 * k, id, sf, sf + 4, (kb | k) != 0);
+                umma_commit(empty_bar(stage));
+                if (++stage == C::STAGES) {
+                    stage = 0;
+                    ph ^= 1;
+                }
+                if (byte == 3 || kb + 1 == nkb) {
+                    umma_commit(sempty_bar(slot));
+                    if (++slot == F8_SLOTS) {
+                        slot = 0;
+                        sph ^= 1;
+                    }
+                }
+            }
+            if (!ok) break;
+            umma_commit(tfull_bar(acc));
+            if (++acc == 2) {
+                acc = 0;
+                aph ^= 1;
+            }
+        }
+        umma_commit(drain_bar);  // every MMA issued above has completed once this fires
+        mbar_wait_warp(drain_bar, 0, nullptr, a.status, lim + 10000000ull);
+    } else if (warp >= F8_WARP_SCALE) {
+        // ------------------------------------------------ scales
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        int slot = 0;
+        uint32_t sph = 0;
+        bool ok = true;
+        const int nsb = (nkb + 3) / 4;
+        for (int64_t tile = blockIdx.x; tile < num_tiles && ok; tile += gridDim.x) {
+            const F8Tile t = f8_tile(a, tile, n_tiles, BN, s_prefix);
+            const uint32_t* pa[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {  // rows past the group's end: any row's scales will do
+                const int64_t r = min(t.m0 + 32 * j + lane, t.hi - 1);
+                pa[j] = reinterpret_cast<const uint32_t*>(a.sa + r * a.lds);
+            }
+            const uint8_t* sb = a.sb[t.e];
+            const int last_nb = (a.N - 1) / 128;
+            for (int c = 0; c < nsb; ++c) {
+                uint32_t wa[4], wb[8];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) wa[j] = __ldcg(pa[j] + c);
+#pragma unroll
+                for (int j = 0; j < (BN + 31) / 32; ++j)
+                    wb[j] = __ldg(reinterpret_cast<const uint32_t*>(sb + (int64_t)min((t.n0 + 32 * j) / 128, last_nb) * a.lds) + c);
+#pragma unroll
+                for (int j = (BN + 31) / 32; j < 8; ++j) wb[j] = 0;
+                if (!mbar_wait_warp(sempty_bar(slot), sph ^ 1, abort_flag, a.status, lim)) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();  // the slot's earlier MMAs read what is written below
+                const uint32_t sf = tmem + lanes + C::SF_COL + slot * F8_SLOT_COLS;
+                CM_TMEM_ST_X4(sf, wa);
+                CM_TMEM_ST_X4(sf + 4, wb);
+                if (BN > 128) CM_TMEM_ST_X4(sf + 8, (wb + 4));
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(sfull_bar(slot));
+                if (++slot == F8_SLOTS) {
+                    slot = 0;
+                    sph ^= 1;
+                }
+            }
+        }
+    } else {
+        // ------------------------------------------------ epilogue
+        constexpr int CW = C::CW, HALF = C::HALF;
+        const int quarter = warp & 3, half = warp >> 2;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        float* bias_line = s_bias + warp * 32;
+        const bool has_bias = a.bias != nullptr;
+        const int esz = KIND == FP8_OUT_BF16 ? 2 : 4;
+        // rows of the output in whole 32-byte pieces
+        const bool wide = KIND == FP8_OUT_FP8 ||
+                          ((reinterpret_cast<uintptr_t>(a.out) & 31) == 0 && (a.ldo * esz & 31) == 0);
+        int acc = 0;
+        uint32_t aph = 0, pph = 0;
+        for (int64_t tile = blockIdx.x; tile < num_tiles; tile += gridDim.x) {
+            const F8Tile t = f8_tile(a, tile, n_tiles, BN, s_prefix);
+            const int64_t m = t.m0 + quarter * 32 + lane;
+            const bool live = m < t.hi;
+            const int64_t orow = live ? (a.rows ? (int64_t)__ldcg(a.rows + m) : m) : 0;
+            if (!mbar_wait_warp(tfull_bar(acc), aph, abort_flag, a.status, lim)) break;
+            tc_fence_after();
+            const uint32_t d = tmem + lanes + acc * BN + half * HALF;
+            if constexpr (KIND == FP8_OUT_FP8) {
+                // The tile's 128 columns are one block: each of the quarter's two warps holds 64 of a row, and they
+                // exchange the row's largest magnitudes.
+                static_assert(KIND != FP8_OUT_FP8 || BN == 128);
+                float v[HALF];
+                uint32_t mx = 0;
+#pragma unroll
+                for (int c = 0; c < HALF / 32; ++c) {
+                    uint32_t r[32];
+                    CM_TMEM_LD_X32(d + c * 32, r);
+                    const int n = t.n0 + half * HALF + c * 32 + lane;
+                    __syncwarp();
+                    if (has_bias)
+                        bias_line[lane] = n >= a.N ? 0.f
+                                          : a.bias_bf16 ? bf16_to_f32(static_cast<const uint16_t*>(a.bias)[n])
+                                                        : static_cast<const float*>(a.bias)[n];
+                    __syncwarp();
+                    tmem_wait_ld();
+                    float f[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(r[i]);
+                    f8_act<32, false>(f, bias_line, has_bias, a.act);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        if (t.n0 + half * HALF + c * 32 + i >= a.N) f[i] = 0.f;
+                        v[c * 32 + i] = f[i];
+                        mx = max(mx, abs_bits(f[i]));
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(tempty_bar(acc));
+                // double-buffered by tile: a warp's read of one tile's value precedes its arrival for the next
+                // tile, and that the other warp's write two tiles on
+                uint32_t* ex = s_amax + acc * F8_NUM_EPI * 32;
+                ex[warp * 32 + lane] = mx;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(pair_bar(quarter));
+                if (!mbar_wait_warp(pair_bar(quarter), pph, abort_flag, a.status, lim)) break;
+                pph ^= 1;
+                mx = max(mx, ex[(warp ^ 4) * 32 + lane]);
+                const uint32_t s = fp8_scale_byte(mx);
+                const float inv = fp8_inverse_scale(s);
+                if (live) {
+                    uint8_t* q = static_cast<uint8_t*>(a.out) + orow * a.ldo + t.n0 + half * HALF;
+#pragma unroll
+                    for (int c = 0; c < HALF / 32; ++c) {
+                        uint32_t o[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            o[i] = fp8_pack4(v[c * 32 + 4 * i] * inv, v[c * 32 + 4 * i + 1] * inv, v[c * 32 + 4 * i + 2] * inv,
+                                             v[c * 32 + 4 * i + 3] * inv);
+                        st_global_32(q + c * 32, o);
+                    }
+                    if (half == 0) a.out_scale[orow * a.ldos + t.n0 / 128] = (uint8_t)s;
+                }
+            } else {
+#pragma unroll 1
+                for (int c = 0; c < HALF / CW; ++c) {
+                    uint32_t r[CW];
+                    __syncwarp();  // rows past the group's end skip the stores below
+                    if constexpr (CW == 32)
+                        CM_TMEM_LD_X32(d + c * CW, r);
+                    else
+                        CM_TMEM_LD_X16(d + c * CW, r);
+                    const int nc = t.n0 + half * HALF + c * CW;
+                    __syncwarp();
+                    if (has_bias && lane < CW)
+                        bias_line[lane] = nc + lane >= a.N ? 0.f
+                                          : a.bias_bf16 ? bf16_to_f32(static_cast<const uint16_t*>(a.bias)[nc + lane])
+                                                        : static_cast<const float*>(a.bias)[nc + lane];
+                    __syncwarp();
+                    tmem_wait_ld();
+                    if (c + 1 == HALF / CW) {  // the accumulator is read: the next tile's MMAs may start
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(tempty_bar(acc));
+                    }
+                    float v[CW];
+#pragma unroll
+                    for (int i = 0; i < CW; ++i) v[i] = __uint_as_float(r[i]);
+                    f8_act<CW, KIND == FP8_OUT_F32>(v, bias_line, has_bias, a.act);
+                    if (!live) continue;
+                    if constexpr (KIND == FP8_OUT_BF16) {
+                        uint16_t* o = static_cast<uint16_t*>(a.out) + orow * a.ldo + nc;
+                        if (wide && nc + CW <= a.N) {
+#pragma unroll
+                            for (int p = 0; p < CW / 16; ++p) {
+                                uint32_t w[8];
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) w[i] = pack_bf16(v[16 * p + 2 * i], v[16 * p + 2 * i + 1]);
+                                st_global_32(o + 16 * p, w);
+                            }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < CW; ++i)
+                                if (nc + i < a.N) o[i] = f32_to_bf16(v[i]);
+                        }
+                    } else {
+                        float* o = static_cast<float*>(a.out) + orow * a.ldo + nc;
+                        if (wide && nc + CW <= a.N) {
+#pragma unroll
+                            for (int p = 0; p < CW / 8; ++p) {
+                                uint32_t w[8];
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[8 * p + i]);
+                                st_global_32(o + 8 * p, w);
+                            }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < CW; ++i)
+                                if (nc + i < a.N) o[i] = v[i];
+                        }
+                    }
+                }
+            }
+            if (++acc == 2) {
+                acc = 0;
+                aph ^= 1;
+            }
+        }
+    }
+    __syncthreads();
+    if (warp == F8_WARP_MMA) tmem_dealloc(tmem, C::TMEM_COLS);
+}
+
+template <int BN, int KIND>
+cudaError_t launch_bn(const Fp8GemmArgs& a, int num_sms, cudaStream_t s) {
+    using C = F8Cfg<BN>;
+    const cudaError_t e = smem_attr_once((const void*)fp8_gemm_kernel<BN, KIND>, C::SMEM);
+    if (e != cudaSuccess) return e;
+    const int64_t m_tiles = (a.M + F8_BM - 1) / F8_BM + (a.offsets ? a.E - 1 : 0);
+    const int64_t tiles = m_tiles * ((a.N + BN - 1) / BN);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(tiles < num_sms ? tiles : num_sms));
+    cfg.blockDim = dim3(F8_THREADS);
+    cfg.dynamicSmemBytes = C::SMEM;
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, fp8_gemm_kernel<BN, KIND>, a);
+}
+
+template <int BN>
+cudaError_t launch_kind(const Fp8GemmArgs& a, int num_sms, cudaStream_t s) {
+    return a.out_kind == FP8_OUT_F32 ? launch_bn<BN, FP8_OUT_F32>(a, num_sms, s) : launch_bn<BN, FP8_OUT_BF16>(a, num_sms, s);
+}
+
+}  // namespace
+
+int fp8_pick_bn(int64_t M, int N, int out_kind, int groups, int num_sms) {
+    if (out_kind == FP8_OUT_FP8) return 128;  // one scale block
+    const int64_t mt = (M + F8_BM - 1) / F8_BM + groups - 1;
+    for (const int bn : {192, 128, 64})
+        if (mt * ((N + bn - 1) / bn) >= num_sms) return bn;
+    return 32;
+}
+
+cudaError_t launch_fp8_gemm(const Fp8GemmArgs& a, int bn, int num_sms, cudaStream_t s) {
+    if (a.out_kind == FP8_OUT_FP8) return launch_bn<128, FP8_OUT_FP8>(a, num_sms, s);
+    switch (bn) {
+        case 192: return launch_kind<192>(a, num_sms, s);
+        case 128: return launch_kind<128>(a, num_sms, s);
+        case 64: return launch_kind<64>(a, num_sms, s);
+        default: return launch_kind<32>(a, num_sms, s);
+    }
+}
+
+int run_fp8_gemm(Fp8GemmArgs& g, const clearmoe_fp8* A, const clearmoe_fp8* W, int E, int num_sms, cudaStream_t s) {
+    g.M = A->rows;
+    g.N = (int)W[0].rows;
+    g.nkb = (int)((A->cols + 127) / 128);
+    g.E = E;
+    g.lds = fp8_lds(A->cols);
+    g.sa = A->scale;
+    const int bn = fp8_pick_bn(g.M, g.N, g.out_kind, E, num_sms);
+    // rows of bytes as rows of half as many 16-bit elements: boxes of 64 of them are 128 bytes
+    const int64_t cols16 = fp8_ldq(A->cols) / 2;
+    if (encode_tmap_bf16(&g.tmA, A->q, A->rows, cols16, F8_BM)) return CLEARMOE_ECUDA;
+    for (int e = 0; e < E; ++e) {
+        g.sb[e] = W[e].scale;
+        if (encode_tmap_bf16(&g.tmB[e], W[e].q, W[e].rows, cols16, bn)) return CLEARMOE_ECUDA;
+    }
+    if (launch_fp8_gemm(g, bn, num_sms, s) == cudaSuccess) return CLEARMOE_OK;
+    (void)cudaGetLastError();
+    return CLEARMOE_ECUDA;
+}
+
+}  // namespace cm
+
+namespace {
+
+// Operands, epilogue and output of a product; fills g's epilogue fields.
+int check_gemm(const clearmoe_fp8* A, const clearmoe_fp8* W, int E, const clearmoe_fp8_epilogue* epi, cm::Fp8GemmArgs& g) {
+    std::memset(&g, 0, sizeof(g));
+    int rc = cm::check_fp8(A);
+    if (rc) return rc;
+    for (int e = 0; e < E; ++e) {
+        if ((rc = cm::check_fp8(W + e))) return rc;
+        if (W[e].cols != A->cols || W[e].rows != W[0].rows || W[e].rows > (int64_t)1 << 24) return CLEARMOE_EINVAL;
+    }
+    g.act = CLEARMOE_ACT_NONE;
+    g.wait_limit_ns = 1000000000LL;
+    if (epi) {
+        if (epi->act != CLEARMOE_ACT_NONE && epi->act != CLEARMOE_ACT_RELU && epi->act != CLEARMOE_ACT_GELU)
+            return CLEARMOE_EINVAL;
+        if (epi->bias) {
+            if (epi->bias_dtype != CLEARMOE_F32 && epi->bias_dtype != CLEARMOE_BF16) return CLEARMOE_EINVAL;
+            if (reinterpret_cast<uintptr_t>(epi->bias) & (epi->bias_dtype == CLEARMOE_BF16 ? 1 : 3)) return CLEARMOE_EINVAL;
+        }
+        if (reinterpret_cast<uintptr_t>(epi->status) & 3) return CLEARMOE_EINVAL;
+        g.bias = epi->bias;
+        g.bias_bf16 = epi->bias_dtype == CLEARMOE_BF16;
+        g.act = epi->act;
+        g.status = epi->status;
+    }
+    return CLEARMOE_OK;
+}
+
+int set_out(cm::Fp8GemmArgs& g, void* out, int32_t dtype, int64_t ldo, int64_t N) {
+    if (!out || (dtype != CLEARMOE_F32 && dtype != CLEARMOE_BF16) || ldo < N || ldo > (int64_t)1 << 30) return CLEARMOE_EINVAL;
+    if (reinterpret_cast<uintptr_t>(out) & (dtype == CLEARMOE_BF16 ? 1 : 3)) return CLEARMOE_EINVAL;
+    g.out = out;
+    g.out_kind = dtype == CLEARMOE_BF16 ? cm::FP8_OUT_BF16 : cm::FP8_OUT_F32;
+    g.ldo = ldo;
+    return CLEARMOE_OK;
+}
+
+int run(cm::Fp8GemmArgs& g, const clearmoe_fp8* A, const clearmoe_fp8* W, int E, void* stream) {
+    const int sms = cm::current_device_sms();
+    if (sms <= 0) return CLEARMOE_ECUDA;
+    return cm::run_fp8_gemm(g, A, W, E, sms, static_cast<cudaStream_t>(stream));
+}
+
+}  // namespace
+
+extern "C" {
+
+int clearmoe_fp8_gemm(const clearmoe_fp8* A, const clearmoe_fp8* W, const clearmoe_fp8_epilogue* epi, void* out,
+                      int32_t out_dtype, int64_t ldo, void* stream) {
+    cm::Fp8GemmArgs g;
+    int rc = check_gemm(A, W, 1, epi, g);
+    if (rc || (rc = set_out(g, out, out_dtype, ldo, W->rows))) return rc;
+    return run(g, A, W, 1, stream);
+}
+
+int clearmoe_fp8_gemm_fp8(const clearmoe_fp8* A, const clearmoe_fp8* W, const clearmoe_fp8_epilogue* epi,
+                          const clearmoe_fp8* out, void* stream) {
+    cm::Fp8GemmArgs g;
+    int rc = check_gemm(A, W, 1, epi, g);
+    if (rc || (rc = cm::check_fp8(out))) return rc;
+    if (out->rows != A->rows || out->cols != W->rows) return CLEARMOE_EINVAL;
+    g.out = out->q;
+    g.out_kind = cm::FP8_OUT_FP8;
+    g.ldo = cm::fp8_ldq(out->cols);
+    g.out_scale = out->scale;
+    g.ldos = cm::fp8_lds(out->cols);
+    return run(g, A, W, 1, stream);
+}
+
+int clearmoe_fp8_grouped_gemm(const clearmoe_fp8* A, const clearmoe_fp8* W, int32_t E, const int32_t* offsets,
+                              const int32_t* perm, const clearmoe_fp8_epilogue* epi, void* out, int32_t out_dtype,
+                              int64_t ldo, void* stream) {
+    if (E < 1 || E > CM_MAX_E || !W || !offsets || (reinterpret_cast<uintptr_t>(offsets) & 3) ||
+        (reinterpret_cast<uintptr_t>(perm) & 3))
+        return CLEARMOE_EINVAL;
+    cm::Fp8GemmArgs g;
+    int rc = check_gemm(A, W, E, epi, g);
+    if (rc || (rc = set_out(g, out, out_dtype, ldo, W->rows))) return rc;
+    g.offsets = offsets;
+    g.rows = perm;
+    return run(g, A, W, E, stream);
+}
+
+}  // extern "C"

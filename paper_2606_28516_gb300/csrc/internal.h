@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "../../include/clearmoe.h"
+
 namespace cm {
 
 struct RouteArgs {
@@ -291,6 +293,81 @@ __host__ __device__ inline int tc2_tail(int64_t tiles, int ncl, int half_pairs) 
 int tc2_dense_half_pairs(int64_t T, int N, int bn, int num_sms);
 cudaError_t launch_tc_gemm2(const TcGemmArgs& a, int num_sms, cudaStream_t s);
 cudaError_t launch_tc_gemm(const TcGemmArgs& a, int num_sms, cudaStream_t s);
+
+// ---- 8-bit blocks (clearmoe_fp8) ----
+// Row pitches in bytes of q and of the scales.
+__host__ __device__ inline int64_t fp8_ldq(int64_t cols) { return (cols + 127) / 128 * 128; }
+__host__ __device__ inline int64_t fp8_lds(int64_t cols) { return (cols + 511) / 512 * 4; }
+int check_fp8(const clearmoe_fp8* m);  // OK or EINVAL
+struct QuantArgs {
+    const void* x;
+    int64_t ld;  // elements
+    int64_t rows, K;
+    int kb;  // blocks of 128 columns per row
+    const int32_t* gather;  // source row of row i (nullable)
+    const float2* ln_stats;  // rows: (mean, rstd) per source row, applied first (nullable; bf16 rows)
+    uint8_t* q;
+    uint8_t* scale;
+    int64_t ldq, lds;
+};
+cudaError_t launch_quantize_rows(const QuantArgs& a, int dtype, int num_sms, cudaStream_t s);
+cudaError_t launch_quantize_weight(const QuantArgs& a, int dtype, cudaStream_t s);
+
+enum Fp8Out { FP8_OUT_F32 = 0, FP8_OUT_BF16 = 1, FP8_OUT_FP8 = 2 };
+struct Fp8GemmArgs {
+    CUtensorMap tmA;
+    CUtensorMap tmB[16];
+    const uint8_t* sa;  // scales of A, rows lds bytes apart
+    const uint8_t* sb[16];
+    int64_t lds;
+    int64_t M;
+    int N;
+    int nkb;  // K blocks of 128
+    int E;    // groups
+    const int32_t* offsets;  // [E + 1]; nullable: one group [0, M)
+    const int32_t* rows;     // output row of row i (nullable)
+    const void* bias;        // [N], fp32 or bf16 (nullable)
+    int bias_bf16;
+    int act;       // clearmoe_act
+    int out_kind;  // Fp8Out
+    void* out;
+    int64_t ldo;  // elements
+    uint8_t* out_scale;  // FP8_OUT_FP8
+    int64_t ldos;
+    int32_t* status;
+    int64_t wait_limit_ns;
+};
+// The N tile (rows of W per tensor-map box) of a product; then launch_fp8_gemm with the maps encoded for it.
+int fp8_pick_bn(int64_t M, int N, int out_kind, int groups, int num_sms);
+cudaError_t launch_fp8_gemm(const Fp8GemmArgs& a, int bn, int num_sms, cudaStream_t s);
+// Fills the operands of a product (maps, scales, sizes) and launches it; a clearmoe_status.
+int run_fp8_gemm(Fp8GemmArgs& g, const clearmoe_fp8* A, const clearmoe_fp8* W, int E, int num_sms, cudaStream_t s);
+
+// ---- a whole layer for a few tokens ----
+struct FewArgs {
+    const void* x;      // [T x d] layer dtype
+    int T, d, H, E;     // E routed experts
+    int G;              // groups: E, + 1 with class tokens
+    int f32;            // fp32 layer
+    int fp8;            // weights in 8-bit blocks
+    const void* W1;
+    const uint8_t* W1_s;
+    const void* Wc[16];   // experts, then the dense path
+    const uint8_t* Wc_s[16];
+    const void* b1;
+    const void* b2;  // nullable
+    const void* Wg;
+    const void* bg;
+    int64_t cls_stride;
+    int ln;
+    void* z;       // [T x H] layer dtype
+    int32_t* idx;  // [T]
+    int32_t* counts;
+    int32_t* offsets;
+    int32_t* perm;
+    void* out;  // [T x d]
+};
+cudaError_t launch_few(const FewArgs& a, int num_sms, cudaStream_t s);
 
 // cudaFuncSetAttribute(fn, MaxDynamicSharedMemorySize, bytes) once per (current device, fn): the
 // attribute belongs to a device, so a process that launches on several GPUs sets it on each.
