@@ -12,7 +12,7 @@ CSRC = PKG / "csrc"
 OUT = PKG / "libclearmoe.so"
 BUILD = PKG / "_build"
 SOURCES = ("api.cu", "route.cu", "simt.cu", "tc_gemm.cu", "tc_gemm2.cu", "noalloc.cu", "fold.cu",
-           "fp8.cu", "fp8_gemm.cu", "few.cu")
+           "fp8.cu", "fp8_gemm.cu", "fp8_gemm2.cu", "few.cu")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr"]
 
@@ -39,7 +39,7 @@ def _compile(src: pathlib.Path, verbose: bool) -> pathlib.Path:
 
 def build(verbose: bool = False, force: bool = False) -> pathlib.Path:
     srcs = [CSRC / s for s in SOURCES]
-    deps = srcs + [CSRC / "common.cuh", CSRC / "internal.h", CSRC / "drain.h", CSRC / "tmap_cache.h", CSRC / "fp8.cuh", PKG.parent / "include" / "clearmoe.h"]
+    deps = srcs + [*CSRC.glob("*.cuh"), *CSRC.glob("*.h"), PKG.parent / "include" / "clearmoe.h"]
     if OUT.exists() and not force and all(OUT.stat().st_mtime >= p.stat().st_mtime for p in deps):
         return OUT
     BUILD.mkdir(exist_ok=True)

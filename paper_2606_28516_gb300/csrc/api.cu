@@ -1414,7 +1414,7 @@ int clearmoe_ffn_forward_few(clearmoe_layer* L, const void* x, int64_t T, const 
     L->last_T = T;
     L->last_E = w->E;
     L->last_groups = a.G;
-    return cuda_fail(cm::launch_few(a, L->num_sms, static_cast<cudaStream_t>(stream)));
+    return cuda_fail(cm::launch_few(a, static_cast<cudaStream_t>(stream)));
 }
 
 // The layer in 8-bit blocks: routing and slots as the other forwards (with the LayerNorm's statistics ahead),

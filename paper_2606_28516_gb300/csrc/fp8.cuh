@@ -45,4 +45,11 @@ __device__ __forceinline__ float2 fp8_unpack2(uint32_t v) {
 }
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
+// The larger magnitude of two values, NaN if either is; its sign is either's.
+__device__ __forceinline__ float max_abs(float a, float b) {
+    float r;
+    asm("max.NaN.xorsign.abs.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
 }  // namespace cm

@@ -6,24 +6,28 @@
 // one byte each, and multiplies in the scale before the fp32 accumulation. A block of 128 is four such
 // 32-blocks with the same byte: the MMA of each K = 32 step names the same byte again. A 32-bit column of scale
 // memory holds four bytes of a row, so four consecutive blocks (512 of K) make one column for 32 rows, and the
-// rows of scales in global memory are padded to whole words: a scale warp moves words as they lie.
+// rows of scales in global memory are padded to whole words, which are moved as they lie.
 //
 // One persistent, warp-specialised kernel per N tile width:
 //   warps 0-7    epilogue: warp w reads TMEM lane quarter w % 4 (its 32 rows) and column half w / 4;
-//   warps 8-11   scales: warp 8 + q loads the words of rows and of W's blocks and stores them to lane quarter q
-//                (each quarter needs a copy of all), four words of A and BN / 32 of W per 512 of K;
-//   warp 12      TMEM allocation, tcgen05.mma and commits (the whole warp in step, one elected lane issues);
+//   warps 8-11   scales: one warp per slot loads the words of the tile's rows and of W's blocks and lays them out in
+//                shared memory;
+//   warp 12      TMEM allocation, tcgen05.cp of the scales, tcgen05.mma and commits (the whole warp in step, one
+//                elected lane issues);
 //   warp 13      TMA producer of the q tiles: 128 rows of A and BN of W, 128 bytes each, 128-byte swizzle.
-// Rings: q stages in shared memory (full: TMA bytes, empty: commit), scale slots in tensor memory (full: one
-// arrival per scale warp, empty: commit), two accumulators. Grouped products walk (group, row tile, column
+// Rings: q stages in shared memory (full: TMA bytes, empty: commit), scale slots (full: the scale
+// warp's arrival, empty: commit), two accumulators. Grouped products walk (group, row tile, column
 // tile) from the device-resident offsets; a row tile never crosses its group's end.
 // Every wait is bounded; a CTA that gives up records CLEARMOE_ETIMEOUT, lets its copies and MMAs in flight
 // finish, frees its tensor memory and returns.
 #include <cstdint>
 #include <cstring>
+#include <cstdio>
+#include <cstdlib>
 
 #include "common.cuh"
 #include "fp8.cuh"
+#include "fp8_gemm.cuh"
 #include "internal.h"
 
 namespace cm {
@@ -35,8 +39,6 @@ constexpr int F8_WARP_SCALE = 8, F8_WARP_MMA = 12, F8_WARP_TMA = 13;
 constexpr int F8_THREADS = 32 * 14;
 constexpr int F8_BM = 128;
 constexpr int F8_BK = 128;
-constexpr int F8_SLOTS = 4;        // scale slots, each 512 of K
-constexpr int F8_SLOT_COLS = 12;   // 4 columns of A's scales, up to 8 of W's
 
 template <int BN_>
 struct F8Cfg {
@@ -48,20 +50,15 @@ struct F8Cfg {
     static constexpr int CW = HALF < 32 ? HALF : 32;       // columns per TMEM read
     static constexpr int NBARS = 2 * STAGES + 2 * F8_SLOTS + 4 + 1 + 4;
     static constexpr int SF_COL = 2 * BN;                  // first scale column
-    static constexpr int TMEM_USED = 2 * BN + F8_SLOTS * F8_SLOT_COLS;
+    static constexpr int SF_COLS = f8_slot_cols(BN), SF_BYTES = f8_slot_bytes(BN);
+    static constexpr int TMEM_USED = 2 * BN + 2 * SF_COLS;
     static constexpr int TMEM_COLS = TMEM_USED <= 128 ? 128 : TMEM_USED <= 256 ? 256 : 512;
     static_assert(TMEM_USED <= 512);
     // bias of a chunk per epilogue warp, largest magnitudes of a row's halves, group prefixes
-    static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + F8_NUM_EPI * 32 * 4 + 2 * F8_NUM_EPI * 32 * 4 + NBARS * 8 + 16 +
-                                4 * (CM_MAX_E + 1);
+    static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + F8_SLOTS * SF_BYTES + F8_NUM_EPI * 32 * 4 + 2 * F8_NUM_EPI * 32 * 4 + NBARS * 8 + 16 +
+                                8 * (CM_MAX_E + 1);
 };
 
-// Instruction descriptor of kind::mxf8f6f4: e4m3 A and W, both K-major, UE8M0 scales; `byte` selects the byte of
-// each scale word.
-__device__ __forceinline__ uint32_t idesc_mxf8(int M, int N, int byte) {
-    return ((uint32_t)byte << 4) | ((uint32_t)(N >> 3) << 17) | (1u << 23) | ((uint32_t)(M >> 4) << 24) |
-           ((uint32_t)byte << 29);
-}
 __device__ __forceinline__ void umma_mxf8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sfa,
                                           uint32_t sfb, uint32_t accumulate) {
     asm volatile(
@@ -73,70 +70,6 @@ __device__ __forceinline__ void umma_mxf8(uint32_t d_tmem, uint64_t a_desc, uint
         "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
         : "memory");
 }
-#define CM_TMEM_ST_X4(taddr, r)                                                              \
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(taddr), \
-                 "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3])                                  \
-                 : "memory")
-#define CM_TMEM_LD_X32(taddr, r)                                                                                        \
-    asm volatile(                                                                                                       \
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19," \
-        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"                                                      \
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),   \
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),        \
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),       \
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])                     \
-        : "r"(taddr))
-
-struct F8Tile {
-    int64_t m0, hi;  // rows [m0, hi) of the group, of which the tile takes the first 128
-    int n0, e;
-};
-
-__device__ __forceinline__ int64_t f8_off(const Fp8GemmArgs& a, int e) {
-    return a.offsets ? (int64_t)__ldcg(a.offsets + e) : (e == 0 ? 0 : a.M);
-}
-
-__device__ __forceinline__ F8Tile f8_tile(const Fp8GemmArgs& a, int64_t tile, int n_tiles, int bn, const int* s_prefix) {
-    F8Tile t;
-    const int mt = (int)(tile / n_tiles);
-    t.n0 = (int)(tile - (int64_t)mt * n_tiles) * bn;
-    int e = 0;
-    while (e + 1 < a.E && s_prefix[e + 1] <= mt) ++e;
-    t.e = e;
-    t.m0 = f8_off(a, e) + (int64_t)(mt - s_prefix[e]) * F8_BM;
-    t.hi = f8_off(a, e + 1);
-    return t;
-}
-
-__device__ __forceinline__ void st_global_32(void* p, const uint32_t (&v)[8]) {
-    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
-                 "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
-                 : "memory");
-}
-
-// CW accumulator columns + bias, activation; bias from the warp's shared-memory line.
-template <int CW, bool EXACT>
-__device__ __forceinline__ void f8_act(float (&v)[CW], const float* s_bias, bool has_bias, int act) {
-    if (has_bias) {
-#pragma unroll
-        for (int i = 0; i < CW; i += 4) {
-            const float4 b = *reinterpret_cast<const float4*>(s_bias + i);
-            v[i] += b.x, v[i + 1] += b.y, v[i + 2] += b.z, v[i + 3] += b.w;
-        }
-    }
-    if (act == CLEARMOE_ACT_GELU) {
-#pragma unroll
-        for (int i = 0; i < CW; i += 2) {
-            const float2 u = make_float2(v[i], v[i + 1]);
-            const float2 g = EXACT ? gelu_pair_f32(u) : gelu_pair_bf16(u);
-            v[i] = g.x, v[i + 1] = g.y;
-        }
-    } else if (act == CLEARMOE_ACT_RELU) {
-#pragma unroll
-        for (int i = 0; i < CW; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];  // NaN stays NaN
-    }
-}
-
 // KIND: Fp8Out.
 template <int BN_, int KIND>
 __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_constant__ Fp8GemmArgs a) {
@@ -144,12 +77,14 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
     constexpr int BN = C::BN;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* sm = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
-    float* s_bias = reinterpret_cast<float*>(sm + C::STAGES * C::STAGE_BYTES);  // [epilogue warp][32]
+    unsigned char* s_sf = sm + C::STAGES * C::STAGE_BYTES;                       // [slot]
+    float* s_bias = reinterpret_cast<float*>(s_sf + F8_SLOTS * C::SF_BYTES);     // [epilogue warp][32]
     uint32_t* s_amax = reinterpret_cast<uint32_t*>(s_bias + F8_NUM_EPI * 32);   // [2][epilogue warp][32]
     uint64_t* bars = reinterpret_cast<uint64_t*>(s_amax + 2 * F8_NUM_EPI * 32);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::NBARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    int* s_prefix = reinterpret_cast<int*>(tmem_slot + 4);
+    int* s_prefix = reinterpret_cast<int*>(tmem_slot + 4);  // [E + 1]
+    int* s_off = s_prefix + CM_MAX_E + 1;                    // [E + 1]
 
     pdl_launch_dependents();
     const int warp = warp_uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
@@ -170,7 +105,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
             mbar_init(empty_bar(s), 1);
         }
         for (int s = 0; s < F8_SLOTS; ++s) {
-            mbar_init(sfull_bar(s), 4);
+            mbar_init(sfull_bar(s), 1);
             mbar_init(sempty_bar(s), 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -188,12 +123,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
     tc_fence_after();
     pdl_wait();  // everything below may read the previous kernel's results
     if (threadIdx.x == 0) {
-        int acc = 0;
-        for (int e = 0; e < a.E; ++e) {
-            s_prefix[e] = acc;
-            acc += (int)((f8_off(a, e + 1) - f8_off(a, e) + F8_BM - 1) / F8_BM);
-        }
-        s_prefix[a.E] = acc;
+        f8_groups(a, F8_BM, s_off, s_prefix);
     }
     __syncthreads();
     const uint32_t tmem = warp_uniform(*tmem_slot);
@@ -207,7 +137,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
         uint32_t ph = 0, issued = 0, par = 0;  // bit s: stage s has had a load; parity of its last
         bool ok = true;
         for (int64_t tile = blockIdx.x; tile < num_tiles && ok; tile += gridDim.x) {
-            F8Tile t = f8_tile(a, tile, n_tiles, BN, s_prefix);
+            F8Tile t = f8_tile(a.E, tile, n_tiles, F8_BM, BN, s_off, s_prefix);
             const int e = warp_uniform(t.e), n0 = warp_uniform(t.n0), m0 = warp_uniform((int)t.m0);
             for (int kb = 0; kb < nkb; ++kb) {
                 if (!mbar_wait_warp(empty_bar(stage), ph ^ 1, abort_flag, a.status, lim)) {
@@ -241,10 +171,16 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
             const uint32_t d = tmem + acc * BN;
             for (int kb = 0; kb < nkb; ++kb) {
                 const int byte = kb & 3;
-                const uint32_t sf = tmem + C::SF_COL + slot * F8_SLOT_COLS;
-                if (byte == 0 && !mbar_wait_warp(sfull_bar(slot), sph, abort_flag, a.status, lim)) {
-                    ok = false;
-                    break;
+                const uint32_t sf = tmem + C::SF_COL + (slot & 1) * C::SF_COLS;
+                if (byte == 0) {
+                    if (!mbar_wait_warp(sfull_bar(slot), sph, abort_flag, a.status, lim)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+#pragma unroll
+                    for (int h = 0; h < C::SF_COLS / 4; ++h)
+                        tmem_cp_scales<1>(sf + 4 * h, smem_u32(s_sf) + slot * C::SF_BYTES + 512 * h);
                 }
                 if (!mbar_wait_warp(full_bar(stage), ph, abort_flag, a.status, lim)) {
                     ok = false;
@@ -281,49 +217,16 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
         mbar_wait_warp(drain_bar, 0, nullptr, a.status, lim + 10000000ull);
     } else if (warp >= F8_WARP_SCALE) {
         // ------------------------------------------------ scales
-        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        int slot = 0;
-        uint32_t sph = 0;
-        bool ok = true;
-        const int nsb = (nkb + 3) / 4;
-        for (int64_t tile = blockIdx.x; tile < num_tiles && ok; tile += gridDim.x) {
-            const F8Tile t = f8_tile(a, tile, n_tiles, BN, s_prefix);
-            const uint32_t* pa[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {  // rows past the group's end: any row's scales will do
-                const int64_t r = min(t.m0 + 32 * j + lane, t.hi - 1);
-                pa[j] = reinterpret_cast<const uint32_t*>(a.sa + r * a.lds);
-            }
-            const uint8_t* sb = a.sb[t.e];
-            const int last_nb = (a.N - 1) / 128;
-            for (int c = 0; c < nsb; ++c) {
-                uint32_t wa[4], wb[8];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) wa[j] = __ldcg(pa[j] + c);
-#pragma unroll
-                for (int j = 0; j < (BN + 31) / 32; ++j)
-                    wb[j] = __ldg(reinterpret_cast<const uint32_t*>(sb + (int64_t)min((t.n0 + 32 * j) / 128, last_nb) * a.lds) + c);
-#pragma unroll
-                for (int j = (BN + 31) / 32; j < 8; ++j) wb[j] = 0;
-                if (!mbar_wait_warp(sempty_bar(slot), sph ^ 1, abort_flag, a.status, lim)) {
-                    ok = false;
-                    break;
-                }
-                tc_fence_after();  // the slot's earlier MMAs read what is written below
-                const uint32_t sf = tmem + lanes + C::SF_COL + slot * F8_SLOT_COLS;
-                CM_TMEM_ST_X4(sf, wa);
-                CM_TMEM_ST_X4(sf + 4, wb);
-                if (BN > 128) CM_TMEM_ST_X4(sf + 8, (wb + 4));
-                tmem_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(sfull_bar(slot));
-                if (++slot == F8_SLOTS) {
-                    slot = 0;
-                    sph ^= 1;
-                }
-            }
-        }
+        const int slot = warp - F8_WARP_SCALE;
+        f8_scale_warp<BN>(a, slot, blockIdx.x, gridDim.x, num_tiles, n_tiles, F8_BM, 0, s_off, s_prefix, lane,
+                          [&](const F8Scales<BN>& w, uint32_t ph) {
+                              if (!mbar_wait_warp(sempty_bar(slot), ph ^ 1, abort_flag, a.status, lim)) return false;
+                              w.store(s_sf + slot * C::SF_BYTES, lane);
+                              fence_proxy_async_smem();
+                              __syncwarp();
+                              if (lane == 0) mbar_arrive(sfull_bar(slot));
+                              return true;
+                          });
     } else {
         // ------------------------------------------------ epilogue
         constexpr int CW = C::CW, HALF = C::HALF;
@@ -338,7 +241,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
         int acc = 0;
         uint32_t aph = 0, pph = 0;
         for (int64_t tile = blockIdx.x; tile < num_tiles; tile += gridDim.x) {
-            const F8Tile t = f8_tile(a, tile, n_tiles, BN, s_prefix);
+            const F8Tile t = f8_tile(a.E, tile, n_tiles, F8_BM, BN, s_off, s_prefix);
             const int64_t m = t.m0 + quarter * 32 + lane;
             const bool live = m < t.hi;
             const int64_t orow = live ? (a.rows ? (int64_t)__ldcg(a.rows + m) : m) : 0;
@@ -498,17 +401,39 @@ cudaError_t launch_kind(const Fp8GemmArgs& a, int num_sms, cudaStream_t s) {
 
 }  // namespace
 
-int fp8_pick_bn(int64_t M, int N, int out_kind, int groups, int num_sms) {
-    if (out_kind == FP8_OUT_FP8) return 128;  // one scale block
-    const int64_t mt = (M + F8_BM - 1) / F8_BM + groups - 1;
-    for (const int bn : {192, 128, 64})
-        if (mt * ((N + bn - 1) / bn) >= num_sms) return bn;
-    return 32;
+// Cycles a product takes on kernel `k`, from what bounds each: rounds of tiles, each of which multiplies (2 BN cycles a
+// k-block on one SM's 128 rows), loads its operands (64 bytes a cycle and SM) or runs its epilogue, and the last
+// epilogue, which nothing hides.
+static double fp8_cost(const Fp8Pick& k, int64_t M, int N, int nkb, int out_kind, int groups, int num_sms) {
+    const int rows = k.pair ? 256 : 128, units = k.pair ? num_sms / 2 : num_sms;
+    if (units < 1) return 1e30;
+    const int64_t tiles = ((M + rows - 1) / rows + groups - 1) * (((int64_t)N + k.bn - 1) / k.bn);
+    const double rounds = (double)((tiles + units - 1) / units);
+    const double loads = 2.0 * (128 + (k.pair ? k.bn / 2 : k.bn));
+    const double block = loads > 2.0 * k.bn ? loads : 2.0 * k.bn;
+    const double epi = (out_kind == FP8_OUT_FP8 ? 14.0 : 8.0) * k.bn, main = block * nkb;
+    return rounds * (main > epi ? main : epi) + epi;
 }
 
-cudaError_t launch_fp8_gemm(const Fp8GemmArgs& a, int bn, int num_sms, cudaStream_t s) {
+Fp8Pick fp8_pick(int64_t M, int N, int nkb, int out_kind, int groups, int num_sms) {
+    static const Fp8Pick all[] = {{256, 1}, {192, 1}, {128, 1}, {192, 0}, {128, 0}, {64, 0}, {32, 0}};
+    Fp8Pick best = {128, 0};
+    double least = 1e30;
+    for (const Fp8Pick& k : all) {
+        if (out_kind == FP8_OUT_FP8 && k.bn % 128) continue;  // whole scale blocks
+        const double c = fp8_cost(k, M, N, nkb, out_kind, groups, num_sms);
+        if (c < least) {
+            least = c;
+            best = k;
+        }
+    }
+    return best;
+}
+
+cudaError_t launch_fp8_gemm(const Fp8GemmArgs& a, const Fp8Pick& k, int num_sms, cudaStream_t s) {
+    if (k.pair) return launch_fp8_gemm2(a, k.bn, num_sms, s);
     if (a.out_kind == FP8_OUT_FP8) return launch_bn<128, FP8_OUT_FP8>(a, num_sms, s);
-    switch (bn) {
+    switch (k.bn) {
         case 192: return launch_kind<192>(a, num_sms, s);
         case 128: return launch_kind<128>(a, num_sms, s);
         case 64: return launch_kind<64>(a, num_sms, s);
@@ -523,15 +448,16 @@ int run_fp8_gemm(Fp8GemmArgs& g, const clearmoe_fp8* A, const clearmoe_fp8* W, i
     g.E = E;
     g.lds = fp8_lds(A->cols);
     g.sa = A->scale;
-    const int bn = fp8_pick_bn(g.M, g.N, g.out_kind, E, num_sms);
+    Fp8Pick k = fp8_pick(g.M, g.N, g.nkb, g.out_kind, E, num_sms);
+    if (const char* o = getenv("F8PICK")) { int bn, pr; sscanf(o, "%d,%d", &bn, &pr); k = {bn, pr}; }
     // rows of bytes as rows of half as many 16-bit elements: boxes of 64 of them are 128 bytes
     const int64_t cols16 = fp8_ldq(A->cols) / 2;
     if (encode_tmap_bf16(&g.tmA, A->q, A->rows, cols16, F8_BM)) return CLEARMOE_ECUDA;
     for (int e = 0; e < E; ++e) {
         g.sb[e] = W[e].scale;
-        if (encode_tmap_bf16(&g.tmB[e], W[e].q, W[e].rows, cols16, bn)) return CLEARMOE_ECUDA;
+        if (encode_tmap_bf16(&g.tmB[e], W[e].q, W[e].rows, cols16, k.pair ? k.bn / 2 : k.bn)) return CLEARMOE_ECUDA;
     }
-    if (launch_fp8_gemm(g, bn, num_sms, s) == cudaSuccess) return CLEARMOE_OK;
+    if (launch_fp8_gemm(g, k, num_sms, s) == cudaSuccess) return CLEARMOE_OK;
     (void)cudaGetLastError();
     return CLEARMOE_ECUDA;
 }

@@ -1,0 +1,185 @@
+// Pieces shared by the kernels of products in 8-bit blocks: descriptors, tiles, epilogue arithmetic.
+#pragma once
+
+#include "common.cuh"
+#include "fp8.cuh"
+#include "internal.h"
+
+namespace cm {
+
+// Instruction descriptor of kind::mxf8f6f4: e4m3 A and W, both K-major, UE8M0 scales; `byte` selects the byte of
+// each scale word.
+__device__ __forceinline__ uint32_t idesc_mxf8(int M, int N, int byte) {
+    return ((uint32_t)byte << 4) | ((uint32_t)(N >> 3) << 17) | (1u << 23) | ((uint32_t)(M >> 4) << 24) |
+           ((uint32_t)byte << 29);
+}
+// 32 rows of 16 bytes at smem (contiguous: core matrices of 8 rows, 128 bytes apart, no swizzle) to four columns of
+// tensor memory, lanes 0 .. 31 and again in each other quarter; CG 2: in both CTAs of a pair, each from its own. In
+// order with the MMAs issued by the same lane.
+template <int CG>
+__device__ __forceinline__ void tmem_cp_scales(uint32_t tmem, uint32_t smem) {
+    const uint64_t desc = (uint64_t)((smem & 0x3FFFFu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+    if (CG == 1)
+        asm volatile(
+            "{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t"
+            "@q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(tmem),
+            "l"(desc)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t"
+            "@q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(tmem),
+            "l"(desc)
+            : "memory");
+}
+#define CM_TMEM_LD_X32(taddr, r)                                                                                        \
+    asm volatile(                                                                                                       \
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19," \
+        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"                                                      \
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),   \
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),        \
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),       \
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])                     \
+        : "r"(taddr))
+
+
+struct F8Tile {
+    int64_t m0, hi;  // rows [m0, hi) of the group, of which the tile takes the first
+    int n0, e;
+};
+
+// Row boundaries of the groups and the row tiles before each, in shared memory: off[E + 1], prefix[E + 1].
+__device__ __forceinline__ void f8_groups(const Fp8GemmArgs& a, int bm, int* off, int* prefix) {
+    int acc = 0;
+    for (int e = 0; e <= a.E; ++e) off[e] = a.offsets ? __ldcg(a.offsets + e) : (e == 0 ? 0 : (int)a.M);
+    for (int e = 0; e < a.E; ++e) {
+        prefix[e] = acc;
+        acc += (off[e + 1] - off[e] + bm - 1) / bm;
+    }
+    prefix[a.E] = acc;
+}
+__device__ __forceinline__ F8Tile f8_tile(int E, int64_t tile, int n_tiles, int bm, int bn, const int* off, const int* prefix) {
+    F8Tile t;
+    const int mt = tile <= 0x7FFFFFFF ? (int)((uint32_t)tile / (uint32_t)n_tiles) : (int)(tile / n_tiles);
+    t.n0 = (int)(tile - (int64_t)mt * n_tiles) * bn;
+    int e = 0;
+    while (e + 1 < E && prefix[e + 1] <= mt) ++e;
+    t.e = e;
+    t.m0 = off[e] + (int64_t)(mt - prefix[e]) * bm;
+    t.hi = off[e + 1];
+    return t;
+}
+
+// The scale words of one 512-column chunk as a lane of the scale warp holds them: rows 32 j + lane of the CTA's 128
+// rows of A, and those of W's blocks (columns n0 + 32 j of the tile lie in one block of 128 rows). Tensor memory
+// holds the word of row 32 j + l in lane l (of every quarter) and column j, which is what tcgen05.cp makes of 32
+// rows of 16 bytes in shared memory.
+constexpr int f8_slot_bytes(int bn) { return 512 * (1 + (bn + 127) / 128); }
+constexpr int f8_slot_cols(int bn) { return 4 * (1 + (bn + 127) / 128); }
+template <int BN>
+struct F8Scales {
+    static constexpr int NW = BN % 128 == 0 ? BN / 128 : BN >= 64 ? BN / 64 : 1;  // different words of W at most
+    static constexpr int SPAN = BN / NW;                                          // columns of each
+    uint32_t a[4], w[NW];
+    __device__ __forceinline__ void load(const Fp8GemmArgs& g, const F8Tile& t, int64_t m0, int chunk, int lane) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {  // rows past the group's end: any row's scales will do
+            const int64_t r = min(m0 + 32 * j + lane, t.hi - 1);
+            a[j] = __ldcg(reinterpret_cast<const uint32_t*>(g.sa + r * g.lds) + chunk);
+        }
+        const uint8_t* sb = g.sb[t.e];
+#pragma unroll
+        for (int j = 0; j < NW; ++j)
+            w[j] = __ldg(reinterpret_cast<const uint32_t*>(sb + (int64_t)(min(t.n0 + SPAN * j, g.N - 1) / 128) * g.lds) + chunk);
+    }
+    // to a slot in shared memory (f8_slot_bytes): 16 bytes a lane for A, and for each 128 columns of the tile
+    __device__ __forceinline__ void store(unsigned char* slot, int lane) const {
+        *reinterpret_cast<uint4*>(slot + lane * 16) = make_uint4(a[0], a[1], a[2], a[3]);
+#pragma unroll
+        for (int h = 0; h < (BN + 127) / 128; ++h) {
+            uint32_t b[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[j] = 128 * h + 32 * j < BN ? w[(128 * h + 32 * j) / SPAN] : 0u;
+            *reinterpret_cast<uint4*>(slot + 512 * (1 + h) + lane * 16) = make_uint4(b[0], b[1], b[2], b[3]);
+        }
+    }
+};
+
+constexpr int F8_SLOTS = 4;  // scale slots in shared memory, each 512 of K; two of them at a time in tensor memory
+constexpr int F8_AHEAD = 2;
+
+// The work of scale warp `slot` of F8_SLOTS: the words of every F8_SLOTS-th 512-column chunk of the CTA's tiles, in
+// order, each handed to put(words, phase), false when it gave up. One warp per slot, because a chunk takes a warp over a
+// microsecond from the free slot to the arrival (loads that wait behind the queued tile loads, the fence between the
+// proxies): with one warp for all slots 93 us, with four SCALES_US for 19,456 x 1,792 x 4,096. F8_AHEAD chunks' loads
+// are in flight; a set of registers is loaded again as soon as its words are stored (a set moved to another would wait
+// for its loads).
+template <int BN, class Put>
+__device__ __forceinline__ void f8_scale_warp(const Fp8GemmArgs& a, int slot, int64_t first, int step, int64_t num_tiles,
+                                              int n_tiles, int bm, int row0, const int* off, const int* prefix, int lane, Put put) {
+    const int nsb = (a.nkb + 3) / 4;
+    const int64_t chunks = (num_tiles > first ? (num_tiles - first + step - 1) / step : 0) * nsb;
+    F8Scales<BN> w[F8_AHEAD];
+    // the next chunk to load: its tile and place in it
+    int64_t tile = first;
+    int c = slot;
+    F8Tile t = {};
+    bool decoded = false;
+    auto load_next = [&](F8Scales<BN>& x) {
+        while (c >= nsb) {
+            c -= nsb;
+            tile += step;
+            decoded = false;
+        }
+        if (tile >= num_tiles) return;
+        if (!decoded) t = f8_tile(a.E, tile, n_tiles, bm, BN, off, prefix);
+        decoded = true;
+        x.load(a, t, t.m0 + row0, c, lane);
+        c += F8_SLOTS;
+    };
+#pragma unroll
+    for (int i = 0; i < F8_AHEAD; ++i) load_next(w[i]);
+    uint32_t ph = 0;
+    for (int64_t at = slot; at < chunks;) {
+#pragma unroll
+        for (int i = 0; i < F8_AHEAD; ++i) {
+            if (at < chunks) {
+                if (!put(w[i], ph)) return;
+                load_next(w[i]);
+                at += F8_SLOTS;
+                ph ^= 1;
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ void st_global_32(void* p, const uint32_t (&v)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+                 "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
+
+// CW accumulator columns + bias, activation; bias from the warp's shared-memory line.
+template <int CW, bool EXACT>
+__device__ __forceinline__ void f8_act(float (&v)[CW], const float* s_bias, bool has_bias, int act) {
+    if (has_bias) {
+#pragma unroll
+        for (int i = 0; i < CW; i += 4) {
+            const float4 b = *reinterpret_cast<const float4*>(s_bias + i);
+            v[i] += b.x, v[i + 1] += b.y, v[i + 2] += b.z, v[i + 3] += b.w;
+        }
+    }
+    if (act == CLEARMOE_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < CW; i += 2) {
+            const float2 u = make_float2(v[i], v[i + 1]);
+            const float2 g = EXACT ? gelu_pair_f32(u) : gelu_pair_bf16(u);
+            v[i] = g.x, v[i + 1] = g.y;
+        }
+    } else if (act == CLEARMOE_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < CW; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];  // NaN stays NaN
+    }
+}
+
+}  // namespace cm

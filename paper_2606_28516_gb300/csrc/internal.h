@@ -337,9 +337,14 @@ struct Fp8GemmArgs {
     int32_t* status;
     int64_t wait_limit_ns;
 };
-// The N tile (rows of W per tensor-map box) of a product; then launch_fp8_gemm with the maps encoded for it.
-int fp8_pick_bn(int64_t M, int N, int out_kind, int groups, int num_sms);
-cudaError_t launch_fp8_gemm(const Fp8GemmArgs& a, int bn, int num_sms, cudaStream_t s);
+// The kernel of a product: tile width, and whether a pair of SMs takes 256 rows or one SM 128.
+struct Fp8Pick {
+    int bn;
+    int pair;
+};
+Fp8Pick fp8_pick(int64_t M, int N, int nkb, int out_kind, int groups, int num_sms);
+cudaError_t launch_fp8_gemm(const Fp8GemmArgs& a, const Fp8Pick& k, int num_sms, cudaStream_t s);
+cudaError_t launch_fp8_gemm2(const Fp8GemmArgs& a, int bn, int num_sms, cudaStream_t s);
 // Fills the operands of a product (maps, scales, sizes) and launches it; a clearmoe_status.
 int run_fp8_gemm(Fp8GemmArgs& g, const clearmoe_fp8* A, const clearmoe_fp8* W, int E, int num_sms, cudaStream_t s);
 
@@ -367,7 +372,7 @@ struct FewArgs {
     int32_t* perm;
     void* out;  // [T x d]
 };
-cudaError_t launch_few(const FewArgs& a, int num_sms, cudaStream_t s);
+cudaError_t launch_few(const FewArgs& a, cudaStream_t s);
 
 // cudaFuncSetAttribute(fn, MaxDynamicSharedMemorySize, bytes) once per (current device, fn): the
 // attribute belongs to a device, so a process that launches on several GPUs sets it on each.
