@@ -403,6 +403,11 @@ int clearmoe_fp8_grouped_gemm(const clearmoe_fp8* A, const clearmoe_fp8* W, int3
                               const int32_t* perm, const clearmoe_fp8_epilogue* epi, void* out, int32_t out_dtype,
                               int64_t ldo, void* stream);
 
+/* For tests: every later product of 8-bit blocks in the process takes the tcgen05 kernel of this tile width, on pairs of
+ * SMs (pair 1: 256, 192, 128) or single ones (pair 0: 192, 128, 64, 32), or the kernel for few rows (16, 0), where the
+ * rows and the output allow it (8-bit outputs: a multiple of 128); (0, 0) restores the choice by size. EINVAL for another kernel. */
+int clearmoe_debug_fp8_kernel(int32_t width, int32_t pair);
+
 /* The weights of a folded layer (clearmoe_fold_basis), bound once and passed to each of the two forwards below.
  *  dtype            of W1, W_comb and W2: the layer's own, or CLEARMOE_FP8 (a bf16 layer's weights in 8-bit
  *                   blocks). With the layer's own dtype only the q of each matrix is read, a dense row-major

@@ -12,7 +12,7 @@ CSRC = PKG / "csrc"
 OUT = PKG / "libclearmoe.so"
 BUILD = PKG / "_build"
 SOURCES = ("api.cu", "route.cu", "simt.cu", "tc_gemm.cu", "tc_gemm2.cu", "noalloc.cu", "fold.cu",
-           "fp8.cu", "fp8_gemm.cu", "fp8_gemm2.cu", "few.cu")
+           "fp8.cu", "fp8_gemm.cu", "fp8_gemm2.cu", "fp8_few.cu", "few.cu")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr"]
 

@@ -113,6 +113,7 @@ _SIGS = {
                               ctypes.POINTER(clearmoe_fp8_epilogue), ctypes.POINTER(clearmoe_fp8), _P],
     "clearmoe_fp8_grouped_gemm": [ctypes.POINTER(clearmoe_fp8), ctypes.POINTER(clearmoe_fp8), _I32, _P, _P,
                                   ctypes.POINTER(clearmoe_fp8_epilogue), _P, _I32, _I64, _P],
+    "clearmoe_debug_fp8_kernel": [_I32, _I32],
     "clearmoe_ffn_forward_few": [_P, _P, _I64, ctypes.POINTER(clearmoe_ffn_weights), _P, _P],
     "clearmoe_ffn_forward_fp8": [_P, _P, _I64, ctypes.POINTER(clearmoe_ffn_weights), _P, _P],
     "clearmoe_strerror": [ctypes.c_int],
@@ -435,44 +436,52 @@ def fp8_weight(rows: int, cols: int, device="cuda") -> Fp8Matrix:
     return _fp8_empty(rows, cols, True, device)
 
 
-def _matrix(t):
-    """Pointer, dtype and row pitch of a 2-D CUDA tensor whose rows are dense (any pitch)."""
-    name = str(t.dtype)
-    if not t.is_cuda or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+_DTYPES = {}  # torch dtype -> clearmoe_dtype, filled on first use (torch is imported late)
+
+
+def _dtype(t) -> int:
+    dt = _DTYPES.get(t.dtype)
+    if dt is None:
+        dt = {"torch.bfloat16": BF16, "torch.float32": F32}.get(str(t.dtype))
+        if dt is None:
+            raise ValueError(f"matrices must be bfloat16 or float32, got {t.dtype}")
+        _DTYPES[t.dtype] = dt
+    return dt
+
+
+def _matrix(t, rows, cols, what):
+    """Pointer, dtype and row pitch of a [rows x cols] CUDA tensor whose rows are dense (any pitch; rows None: any
+    number)."""
+    shape = t.shape
+    if not t.is_cuda or len(shape) != 2:
         raise ValueError("matrices passed to libclearmoe must be 2-D CUDA tensors with dense rows")
-    if name not in ("torch.bfloat16", "torch.float32"):
-        raise ValueError(f"matrices must be bfloat16 or float32, got {name}")
-    ld = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
-    return t.data_ptr(), BF16 if name == "torch.bfloat16" else F32, ld
-
-
-def _same_shape(t, rows, cols, what):
-    if tuple(t.shape) != (rows, cols):
-        raise ValueError(f"{what} must be [{rows} x {cols}], got {tuple(t.shape)}")
+    n, k = shape
+    if (rows is not None and n != rows) or k != cols:
+        raise ValueError(f"{what} must be [{'any' if rows is None else rows} x {cols}], got {tuple(shape)}")
+    ld, step = t.stride()
+    if k > 1 and step != 1:
+        raise ValueError("matrices passed to libclearmoe must be 2-D CUDA tensors with dense rows")
+    return t.data_ptr(), _dtype(t), ld if n > 1 else max(ld, k)
 
 
 def clearmoe_fp8_quantize_rows(x, out: Fp8Matrix, gather=None, stream=None) -> None:
     """x [rows x cols] (bf16 or fp32, any row pitch) to out in 1 x 128 blocks; gather: int32 source rows."""
-    p, dt, ld = _matrix(x)
-    if gather is None:
-        _same_shape(x, out.rows, out.cols, "x")
-    elif x.shape[1] != out.cols or gather.numel() != out.rows:
-        raise ValueError("x must have out's columns and gather one entry per row of out")
+    p, dt, ld = _matrix(x, out.rows if gather is None else None, out.cols, "x")
+    if gather is not None and gather.numel() != out.rows:
+        raise ValueError("gather must have one entry per row of out")
     _check(lib().clearmoe_fp8_quantize_rows(p, dt, ld, _ptr(gather), out.ref, _stream(stream)),
            "clearmoe_fp8_quantize_rows")
 
 
 def clearmoe_fp8_quantize_weight(W, out: Fp8Matrix, stream=None) -> None:
     """W [rows x cols] (bf16 or fp32, any row pitch) to out in 128 x 128 blocks."""
-    p, dt, ld = _matrix(W)
-    _same_shape(W, out.rows, out.cols, "W")
+    p, dt, ld = _matrix(W, out.rows, out.cols, "W")
     _check(lib().clearmoe_fp8_quantize_weight(p, dt, ld, out.ref, _stream(stream)), "clearmoe_fp8_quantize_weight")
 
 
 def clearmoe_fp8_dequantize(m: Fp8Matrix, out, stream=None) -> None:
     """The values m stands for, rounded to out's dtype (bf16 or fp32)."""
-    p, dt, ld = _matrix(out)
-    _same_shape(out, m.rows, m.cols, "out")
+    p, dt, ld = _matrix(out, m.rows, m.cols, "out")
     _check(lib().clearmoe_fp8_dequantize(m.ref, 128 if m.weight else 1, p, dt, ld, _stream(stream)),
            "clearmoe_fp8_dequantize")
 
@@ -482,8 +491,7 @@ def _epilogue(bias, act, status, N):
         return None
     if bias is not None and bias.numel() != N:
         raise ValueError(f"bias must have {N} elements, got {bias.numel()}")
-    dt = BF16 if bias is not None and bias.element_size() == 2 else F32
-    return ctypes.byref(clearmoe_fp8_epilogue(_ptr(bias), dt, act, _ptr(status)))
+    return ctypes.byref(clearmoe_fp8_epilogue(_ptr(bias), F32 if bias is None else _dtype(bias), act, _ptr(status)))
 
 
 def clearmoe_fp8_gemm(A: Fp8Matrix, W: Fp8Matrix, out, bias=None, act: int = ACT_NONE, status=None, stream=None) -> None:
@@ -493,8 +501,7 @@ def clearmoe_fp8_gemm(A: Fp8Matrix, W: Fp8Matrix, out, bias=None, act: int = ACT
     if isinstance(out, Fp8Matrix):
         _check(lib().clearmoe_fp8_gemm_fp8(A.ref, W.ref, epi, out.ref, _stream(stream)), "clearmoe_fp8_gemm_fp8")
         return
-    p, dt, ld = _matrix(out)
-    _same_shape(out, A.rows, W.rows, "out")
+    p, dt, ld = _matrix(out, A.rows, W.rows, "out")
     _check(lib().clearmoe_fp8_gemm(A.ref, W.ref, epi, p, dt, ld, _stream(stream)), "clearmoe_fp8_gemm")
 
 
@@ -503,12 +510,16 @@ def clearmoe_fp8_grouped_gemm(A: Fp8Matrix, W, offsets, out, perm=None, bias=Non
     """Rows offsets[e] .. offsets[e + 1] of A times W[e]^T (W: a sequence of Fp8Matrix), row i to out[perm[i]]."""
     if offsets.numel() != len(W) + 1 or (perm is not None and perm.numel() != A.rows):
         raise ValueError("offsets must have one entry per matrix and one more, perm one per row of A")
-    p, dt, ld = _matrix(out)
-    _same_shape(out, A.rows, W[0].rows, "out")
+    p, dt, ld = _matrix(out, A.rows, W[0].rows, "out")
     arr = (clearmoe_fp8 * len(W))(*[m.c for m in W])
     _check(lib().clearmoe_fp8_grouped_gemm(A.ref, arr, len(W), _ptr(offsets), _ptr(perm),
                                            _epilogue(bias, act, status, W[0].rows), p, dt, ld, _stream(stream)),
            "clearmoe_fp8_grouped_gemm")
+
+
+def clearmoe_debug_fp8_kernel(width: int = 0, pair: int = 0) -> None:
+    """For tests: fixes the kernel of every later product of 8-bit blocks; no arguments: by size again."""
+    _check(lib().clearmoe_debug_fp8_kernel(width, pair), "clearmoe_debug_fp8_kernel")
 
 
 # ------------------------------------------------------------- a folded layer's weights and its forwards
@@ -534,14 +545,15 @@ def ffn_weights(W1, b1, W_comb, Wg, bg, b2=None, W2=None, cls_stride: int = 0,
             raise ValueError("W1, W_comb and W2 are all tensors or all Fp8Matrix weights")
         if fp8:
             return W.c
-        _same_shape(W, rows, cols, "a weight matrix")
+        if tuple(W.shape) != (rows, cols):
+            raise ValueError(f"a weight matrix must be [{rows} x {cols}], got {tuple(W.shape)}")
         return clearmoe_fp8(_ptr(W), None, rows, cols)
 
     for name, t, n in (("b1", b1, H), ("bg", bg, E), ("b2", b2, d)):
         if t is not None and t.numel() != n:
             raise ValueError(f"{name} must have {n} elements, got {t.numel()}")
     c = clearmoe_ffn_weights()
-    c.dtype = FP8 if fp8 else _matrix(W1)[1]
+    c.dtype = FP8 if fp8 else _dtype(W1)
     c.E = E
     c.W1 = mat(W1, H, d)
     for e in range(E):

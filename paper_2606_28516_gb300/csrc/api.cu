@@ -1382,6 +1382,7 @@ int clearmoe_ffn_forward_few(clearmoe_layer* L, const void* x, int64_t T, const 
     if (!out || misaligned(out)) return CLEARMOE_EINVAL;
     if ((rc = check_ffn_weights(L, w))) return rc;
     if (T > CLEARMOE_FEW_MAX) return CLEARMOE_EUNSUPPORTED;
+    if (w->dtype == CLEARMOE_FP8 && L->desc.hidden > 128 * cm::FP8_FEW_SCALES) return CLEARMOE_EUNSUPPORTED;  // their scales
     cm::FewArgs a;
     std::memset(&a, 0, sizeof(a));
     a.x = x;

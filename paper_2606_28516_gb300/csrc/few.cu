@@ -21,7 +21,6 @@
 #include "internal.h"
 
 namespace cm {
-
 namespace {
 
 template <int V>
@@ -48,7 +47,7 @@ struct FewRow {
         for (int p = 0; p < FEW_PIECES; ++p) {
             const int k = (p * 32 + lane) * PER;
             u[p] = make_uint4(0, 0, 0, 0);
-            if (k < d) u[p] = few_ld_token(static_cast<const char*>(x) + (row * d + k) * (16 / PER));
+            if (k < d) u[p] = __ldcg(reinterpret_cast<const uint4*>(static_cast<const char*>(x) + (row * d + k) * (16 / PER)));
         }
 #pragma unroll
         for (int p = 0; p < FEW_PIECES; ++p) {
@@ -81,108 +80,141 @@ struct FewRow {
     }
 };
 
-// The routing of token t by one CTA: a warp per expert, the logits in fp32, lowest index on ties.
 template <int V>
-__device__ __forceinline__ void few_route(const FewArgs& a, int t, float* s_logit, int warp, int lane) {
-    if (a.cls_stride > 0 && t % a.cls_stride == 0) {
-        if (threadIdx.x == 0) a.idx[t] = a.E;
-        return;
-    }
-    FewRow<V> x, w;
-    x.load(a.x, t, a.d, lane);
-    float2 st = make_float2(0.f, 1.f);
-    if (a.ln) st = x.stats(a.d, lane);
-    for (int e = warp; e < a.E; e += FEW_WARPS) {
-        w.load(a.Wg, e, a.d, lane);  // zeros past d
-        float s = 0.f;
-#pragma unroll
-        for (int p = 0; p < FEW_PIECES; ++p)
-#pragma unroll
-            for (int i = 0; i < FewRow<V>::PER; ++i) s = fmaf((x.v[p][i] - st.x) * st.y, w.v[p][i], s);
-#pragma unroll
-        for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-        if (lane == 0) s_logit[e] = s + few_get<V>(a.bg, e);
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        int best = 0;
-        for (int e = 1; e < a.E; ++e)
-            if (s_logit[e] > s_logit[best]) best = e;
-        a.idx[t] = best;
-    }
+__device__ __forceinline__ int64_t few_pitch(int K) {  // bytes
+    return V == FEWV_W8A16 ? fp8_ldq(K) : (int64_t)K * FewT<V, 1, 2>::WSZ;
 }
 
-template <int V, int NT, bool LN>
-__global__ void __launch_bounds__(FEW_THREADS, 2) few_fc1_kernel(const __grid_constant__ FewArgs a) {
-    extern __shared__ float red[];  // [warp][NT * 8 columns][16 rows], and the row sums' [warp][16]
-    __shared__ float2 s_stats[CLEARMOE_FEW_MAX];
-    __shared__ float s_logit[16];
+// The routing of tokens TOK block .. TOK block + TOK - 1 by one CTA: a warp per expert (two above 8), its row of W_g in registers
+// before the tokens may be read; the logits in fp32, lowest index on ties. (Eight tokens a CTA, one after the other,
+// took longer than fc1: 9.3 us instead of 7.1 for 64 tokens, d = 192. With up to 16 tokens one a CTA: one token, 3.9 us
+// against 4.5 with two.)
+template <int V, int TOK>
+__device__ __forceinline__ void few_route(const FewArgs& a, int block, float (*s_logit)[16], int warp, int lane) {
+    FewRow<V> w[2], x[TOK];
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+        if (warp + 8 * q < a.E) w[q].load(a.Wg, warp + 8 * q, a.d, lane);  // zeros past d
+    pdl_wait();
+#pragma unroll
+    for (int i = 0; i < TOK; ++i) x[i].load(a.x, min(TOK * block + i, a.T - 1), a.d, lane);
+#pragma unroll
+    for (int i = 0; i < TOK; ++i) {
+        float2 st = make_float2(0.f, 1.f);
+        if (a.ln) st = x[i].stats(a.d, lane);
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            if (warp + 8 * q >= a.E) break;
+            float s = 0.f;
+#pragma unroll
+            for (int p = 0; p < FEW_PIECES; ++p)
+#pragma unroll
+                for (int c = 0; c < FewRow<V>::PER; ++c) s = fmaf((x[i].v[p][c] - st.x) * st.y, w[q].v[p][c], s);
+#pragma unroll
+            for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+            if (lane == 0) s_logit[i][warp + 8 * q] = s + few_get<V>(a.bg, warp + 8 * q);
+        }
+    }
+    __syncthreads();
+    const int t = TOK * block + (int)threadIdx.x;  // a thread per token
+    if (threadIdx.x >= TOK || t >= a.T) return;
+    int best = 0;
+    for (int e = 1; e < a.E; ++e)
+        if (s_logit[threadIdx.x][e] > s_logit[threadIdx.x][best]) best = e;
+    a.idx[t] = a.cls_stride > 0 && t % a.cls_stride == 0 ? a.E : best;
+}
+
+constexpr int few_route_tokens(int nt) { return nt <= 2 ? 1 : 2; }
+
+// Tokens that a CTA of fc1 multiplies at a time.
+constexpr int few_chunk(int nt) { return 8 * nt; }
+
+// Scale bytes of a tile's rows (8-bit weights) to shared memory; the caller synchronises.
+template <int V>
+__device__ __forceinline__ void few_scales(uint8_t* dst, const uint8_t* s, int r0, int K) {
+    if (V != FEWV_W8A16) return;
+    s += (int64_t)(r0 / 128) * fp8_lds(K);
+    for (int i = threadIdx.x; i < (K + 127) / 128; i += FEW_THREADS) dst[i] = __ldg(s + i);
+}
+
+template <int V, int NT, int CTAS, bool LN>
+__global__ void __launch_bounds__(FEW_THREADS, CTAS) few_fc1_kernel(const __grid_constant__ FewArgs a) {
+    extern __shared__ float red[];  // the partial sums; then the scale bytes
+    __shared__ float2 s_stats[few_chunk(NT)];
+    __shared__ float s_logit[2][16];
+    __shared__ float s_rows[FEW_WARPS][16];  // LN: the warps' row sums of W
+    uint8_t* s_scale = reinterpret_cast<uint8_t*>(red) + FewT<V, NT, CTAS>::SMEM;
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if ((int)blockIdx.x < a.T) {  // first, as the expert kernel's work depends on them all
-        pdl_wait();
-        few_route<V>(a, blockIdx.x, s_logit, warp, lane);
+    constexpr int TOK = few_route_tokens(NT);
+    const int routers = (a.T + TOK - 1) / TOK;
+    if ((int)blockIdx.x < routers) {  // first, as the expert kernel's work depends on them all
+        if (blockIdx.y == 0) few_route<V, TOK>(a, blockIdx.x, s_logit, warp, lane);
         return;
     }
-    const int r0 = (blockIdx.x - a.T) * 16;
-    FewRound<V, NT> w;
-    const FewTile m = few_tile<V>(a.W1, a.W1_s, V >= FEWV_W8A16 ? fp8_ldq(a.d) : a.d, fp8_lds(a.d), r0, a.H, a.d, lane);
-    few_load<V, NT>(w, m, 0, warp, lane);
+    const int r0 = (blockIdx.x - routers) * 16;
+    const int t0 = blockIdx.y * few_chunk(NT), rows = min(few_chunk(NT), a.T - t0);  // the CTA's tokens
+    FewTile<V, NT, CTAS> t;
+    t.set_weights(a.W1, few_pitch<V>(a.d), r0, a.H, a.d);
+    t.start_w();
+    few_scales<V>(s_scale, a.W1_s, r0, a.d);
     pdl_wait();
     float acc[NT][4], sums[4] = {0.f, 0.f, 0.f, 0.f};
-    const char* tok[NT];
-    const uint8_t* none[NT][2] = {};
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-        tok[j] = static_cast<const char*>(a.x) + (int64_t)min(8 * j + (lane >> 2), a.T - 1) * a.d * FewT<V, NT>::XSZ;
+        t.set_row(j, static_cast<const char*>(a.x) + (int64_t)(t0 + min(8 * j + (lane >> 2), rows - 1)) * a.d * FewT<V, NT, CTAS>::XSZ);
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
     }
-    few_product<V, NT, LN>(acc, sums, m, w, tok, none, warp, lane);
+    t.start_x();
+    if (V == FEWV_W8A16) __syncthreads();
+    few_product<V, NT, CTAS, LN>(acc, sums, t, s_scale, nullptr, 0, rows);
     few_stage<NT>(red, acc, warp, lane);
-    float* red_sum = red + FEW_WARPS * NT * 128;
     if (LN) {
         if ((lane & 3) == 0) {  // column 0 of the ones
-            red_sum[warp * 16 + (lane >> 2)] = sums[0];
-            red_sum[warp * 16 + (lane >> 2) + 8] = sums[2];
+            s_rows[warp][lane >> 2] = sums[0];
+            s_rows[warp][(lane >> 2) + 8] = sums[2];
         }
-        for (int t = warp; t < a.T; t += FEW_WARPS) {
+        for (int r = warp; r < rows; r += FEW_WARPS) {
             FewRow<V> x;
-            x.load(a.x, t, a.d, lane);
+            x.load(a.x, t0 + r, a.d, lane);
             const float2 st = x.stats(a.d, lane);
-            if (lane == 0) s_stats[t] = st;
+            if (lane == 0) s_stats[r] = st;
         }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < a.T * 16; i += FEW_THREADS) {
-        const int t = i >> 4, r = i & 15;
+    for (int i = threadIdx.x; i < rows * 16; i += FEW_THREADS) {
+        const int m = i >> 4, r = i & 15;
         if (r0 + r >= a.H) continue;
-        float s = few_sum<NT>(red, t, r);
+        float s = few_sum<NT>(red, m, r);
         if (LN) {  // W LN(y) = rstd (W y - mean W 1)
             float c = 0.f;
 #pragma unroll
-            for (int q = 0; q < FEW_WARPS; ++q) c += red_sum[q * 16 + r];
-            const float2 st = s_stats[t];
+            for (int q = 0; q < FEW_WARPS; ++q) c += s_rows[q][r];
+            const float2 st = s_stats[m];
             s = st.y * (s - st.x * c);
         }
-        few_put<V>(a.z, (int64_t)t * a.H + r0 + r, gelu_erf(s + few_get<V>(a.b1, r0 + r)));
+        few_put<V>(a.z, (int64_t)(t0 + m) * a.H + r0 + r, gelu_erf(s + few_get<V>(a.b1, r0 + r)));
     }
 }
 
-// The CTA's tile for the n tokens of its group, at most 8 NT; ROUND0: the first round's weights are in w.
-template <int V, int NT>
-__device__ __forceinline__ void few_expert(const FewArgs& a, const FewTile& m, FewRound<V, NT>& w, float* red, const int* s_tok,
-                                           int n, int r0, int warp, int lane) {
+// A tile's product for tokens s_tok[0 .. n), n <= 8 NT, into their output rows.
+template <int V, int NT, int CTAS>
+__device__ __forceinline__ void few_expert(const FewArgs& a, int e, int r0, const int* s_tok, int n, float* red, const uint8_t* s_scale,
+                                           int warp, int lane) {
+    FewTile<V, NT, CTAS> t;
+    t.set_weights(a.Wc[e], few_pitch<V>(a.H), r0, a.d, a.H);
+    t.start_w();
     float acc[NT][4], sums[4];
-    const char* tok[NT];
-    const uint8_t* none[NT][2] = {};
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-        tok[j] = static_cast<const char*>(a.z) + (int64_t)s_tok[min(8 * j + (lane >> 2), n - 1)] * a.H * FewT<V, NT>::XSZ;
+        t.set_row(j, static_cast<const char*>(a.z) + (int64_t)s_tok[min(8 * j + (lane >> 2), n - 1)] * a.H * FewT<V, NT, CTAS>::XSZ);
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
     }
-    few_product<V, NT, false>(acc, sums, m, w, tok, none, warp, lane);
+    t.start_x();
+    if (V == FEWV_W8A16) __syncthreads();  // the scales
+    few_product<V, NT, CTAS, false>(acc, sums, t, s_scale, nullptr, 0, n);
     few_stage<NT>(red, acc, warp, lane);
     __syncthreads();
     for (int i = threadIdx.x; i < n * 16; i += FEW_THREADS) {
@@ -194,63 +226,55 @@ __device__ __forceinline__ void few_expert(const FewArgs& a, const FewTile& m, F
     }
 }
 
-template <int V, int NT>
-__global__ void __launch_bounds__(FEW_THREADS, 2) few_expert_kernel(const __grid_constant__ FewArgs a) {
-    extern __shared__ float red[];
+// One CTA per 16 output rows and group, NT token tiles at most at a time; more tokens than that go through in turns, the
+// weights then coming from L2.
+template <int V, int NT, int CTAS>
+__global__ void __launch_bounds__(FEW_THREADS, CTAS) few_expert_kernel(const __grid_constant__ FewArgs a) {
+    extern __shared__ float red[];  // the partial sums; then the scale bytes
     __shared__ int s_tok[CLEARMOE_FEW_MAX];
     __shared__ int s_n;
+    uint8_t* s_scale = reinterpret_cast<uint8_t*>(red) + FewT<V, NT, CTAS>::SMEM;
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int e = blockIdx.y, r0 = blockIdx.x * 16;
-    const FewTile m = few_tile<V>(a.Wc[e], a.Wc_s[e], V >= FEWV_W8A16 ? fp8_ldq(a.H) : a.H, fp8_lds(a.H), r0, a.d, a.H, lane);
+    few_scales<V>(s_scale, a.Wc_s[e], r0, a.H);
     pdl_wait();
-    if (warp == 0) {  // the group's tokens in order
-        int n = 0;
-        for (int t0 = 0; t0 < a.T; t0 += 32) {
-            const bool mine = t0 + lane < a.T && __ldcg(a.idx + t0 + lane) == e;
-            const uint32_t b = __ballot_sync(0xFFFFFFFFu, mine);
-            if (mine) s_tok[n + __popc(b & ((1u << lane) - 1))] = t0 + lane;
-            n += __popc(b);
-        }
+    if (warp == 0) {  // the group's tokens in order, two a lane; their number before it
+        const int v0 = lane < a.T ? __ldcg(a.idx + lane) : a.G, v1 = lane + 32 < a.T ? __ldcg(a.idx + lane + 32) : a.G;
+        const uint32_t b0 = __ballot_sync(0xFFFFFFFFu, v0 == e), b1 = __ballot_sync(0xFFFFFFFFu, v1 == e);
+        const uint32_t below = (1u << lane) - 1;
+        const int at0 = __popc(b0 & below), at1 = __popc(b0) + __popc(b1 & below), n = __popc(b0) + __popc(b1);
+        if (v0 == e) s_tok[at0] = lane;
+        if (v1 == e) s_tok[at1] = lane + 32;
         if (lane == 0) s_n = n;
-    } else if (warp == 1 && blockIdx.x == 0) {  // counts, offsets and perm, as the other forwards leave them
-        int before = 0, n = 0;
-        for (int t0 = 0; t0 < a.T; t0 += 32) {
-            const int v = t0 + lane < a.T ? __ldcg(a.idx + t0 + lane) : a.G;
-            before += __popc(__ballot_sync(0xFFFFFFFFu, v < e));
-            n += __popc(__ballot_sync(0xFFFFFFFFu, v == e));
-        }
-        int at = before;
-        for (int t0 = 0; t0 < a.T; t0 += 32) {
-            const bool mine = t0 + lane < a.T && __ldcg(a.idx + t0 + lane) == e;
-            const uint32_t b = __ballot_sync(0xFFFFFFFFu, mine);
-            if (mine) a.perm[at + __popc(b & ((1u << lane) - 1))] = t0 + lane;
-            at += __popc(b);
-        }
-        if (lane == 0) {
-            a.counts[e] = n;
-            a.offsets[e] = before;
-            if (e + 1 == a.G) a.offsets[a.G] = a.T;
+        if (blockIdx.x == 0) {  // counts, offsets and perm, as the other forwards leave them
+            const int before = __popc(__ballot_sync(0xFFFFFFFFu, v0 < e)) + __popc(__ballot_sync(0xFFFFFFFFu, v1 < e));
+            if (v0 == e) a.perm[before + at0] = lane;
+            if (v1 == e) a.perm[before + at1] = lane + 32;
+            if (lane == 0) {
+                a.counts[e] = n;
+                a.offsets[e] = before;
+                if (e + 1 == a.G) a.offsets[a.G] = a.T;
+            }
         }
     }
     __syncthreads();
-    const int n = s_n;
-    if (n == 0) return;
-    // as many token tiles as the group needs
-    auto run = [&](auto tiles) {
-        constexpr int N = decltype(tiles)::value;
-        FewRound<V, N> w;
-        few_load<V, N>(w, m, 0, warp, lane);
-        few_expert<V, N>(a, m, w, red, s_tok, n, r0, warp, lane);
-    };
-    if (NT == 1 || n <= 8) return run(std::integral_constant<int, 1>());
-    if (NT == 2 || n <= 16) return run(std::integral_constant<int, (NT < 2 ? NT : 2)>());
-    if (NT == 4 || n <= 32) return run(std::integral_constant<int, (NT < 4 ? NT : 4)>());
-    run(std::integral_constant<int, NT>());
+    for (int m0 = 0; m0 < s_n; m0 += 8 * NT) {
+        const int n = min(8 * NT, s_n - m0);
+        if (NT == 1 || n <= 8)
+            few_expert<V, 1, CTAS>(a, e, r0, s_tok + m0, n, red, s_scale, warp, lane);
+        else if (NT == 2 || n <= 16)
+            few_expert<V, NT < 2 ? NT : 2, CTAS>(a, e, r0, s_tok + m0, n, red, s_scale, warp, lane);
+        else
+            few_expert<V, NT, CTAS>(a, e, r0, s_tok + m0, n, red, s_scale, warp, lane);
+        __syncthreads();  // red is read
+    }
 }
 
-template <typename K>
-cudaError_t few_launch(K kernel, dim3 grid, int smem, const FewArgs& a, cudaStream_t s) {
+template <typename K, typename... A>
+cudaError_t few_launch(K kernel, dim3 grid, int smem, cudaStream_t s, const A&... a) {
+    const cudaError_t e = smem_attr_once((const void*)kernel, smem);
+    if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(FEW_THREADS);
@@ -261,20 +285,29 @@ cudaError_t few_launch(K kernel, dim3 grid, int smem, const FewArgs& a, cudaStre
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, a);
+    return cudaLaunchKernelEx(&cfg, kernel, a...);
 }
 
-template <int V, int NT>
-cudaError_t few_run(const FewArgs& a, cudaStream_t s) {
-    const dim3 g1((a.H + 15) / 16 + a.T), g2((a.d + 15) / 16, a.G);
-    const cudaError_t e = a.ln ? few_launch(few_fc1_kernel<V, NT, true>, g1, few_smem(NT) + FEW_WARPS * 64, a, s)
-                               : few_launch(few_fc1_kernel<V, NT, false>, g1, few_smem(NT), a, s);
-    return e != cudaSuccess ? e : few_launch(few_expert_kernel<V, NT>, g2, few_smem(NT), a, s);
+template <int V, int NT, int CTAS>
+cudaError_t few_fc1(const FewArgs& a, cudaStream_t s) {
+    const dim3 grid((a.H + 15) / 16 + (a.T + few_route_tokens(NT) - 1) / few_route_tokens(NT), (a.T + few_chunk(NT) - 1) / few_chunk(NT));
+    const int smem = FewT<V, NT, CTAS>::SMEM + (V == FEWV_W8A16 ? (a.d + 127) / 128 : 0);
+    return a.ln ? few_launch(few_fc1_kernel<V, NT, CTAS, true>, grid, smem, s, a)
+                : few_launch(few_fc1_kernel<V, NT, CTAS, false>, grid, smem, s, a);
+}
+template <int V, int NT, int CTAS>
+cudaError_t few_experts(const FewArgs& a, cudaStream_t s) {
+    const dim3 grid((a.d + 15) / 16, a.G);
+    const int smem = FewT<V, NT, CTAS>::SMEM + (V == FEWV_W8A16 ? (a.H + 127) / 128 : 0);
+    return few_launch(few_expert_kernel<V, NT, CTAS>, grid, smem, s, a);
 }
 
 template <int V>
 cudaError_t few_type(const FewArgs& a, cudaStream_t s) {
-    return a.T <= 8 ? few_run<V, 1>(a, s) : a.T <= 16 ? few_run<V, 2>(a, s) : a.T <= 32 ? few_run<V, 4>(a, s) : few_run<V, 8>(a, s);
+    const cudaError_t e = a.T <= 8 ? few_fc1<V, 1, 2>(a, s) : a.T <= 16 ? few_fc1<V, 2, 2>(a, s) : few_fc1<V, 4, 2>(a, s);
+    if (e != cudaSuccess) return e;
+    return a.T <= 4 ? few_experts<V, 1, 2>(a, s) : a.T <= 8 ? few_experts<V, 1, 3>(a, s) : a.T <= 16 ? few_experts<V, 2, 3>(a, s)
+                                                                                     : few_experts<V, 4, 2>(a, s);
 }
 
 }  // namespace

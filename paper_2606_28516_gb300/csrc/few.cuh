@@ -1,11 +1,16 @@
 // The product of a 16-row tile of weights with a few rows of activations, shared by the few-token layer and the
 // 8-bit product of few rows.
 //
-// The warps of a CTA split K. Weights go from global memory straight to the registers they are multiplied from:
-// the order of K within a sum is free as long as both operands agree, so lane (g, c) = (lane / 4, lane % 4) takes
-// 16 consecutive bytes of weight rows g and g + 8 and the same columns of activation row g, and feeds them to
-// m16n8 warp-level MMAs as their fragments. A lane issues the loads of a round (DEPTH steps) before the round's
-// products; the depth is what fits 128 registers a thread, so that two CTAs of eight warps share an SM.
+// What bounds it is reading the weights once, so every byte is asked for early. The warps of a CTA split K, step by
+// step. Weights go from global memory straight to the registers they are multiplied from: the order of K within a sum
+// is free as long as both operands agree, so lane (g, c) = (lane / 4, lane % 4) takes 16 consecutive bytes of weight
+// rows g and g + 8 and the same columns of activation row g, and feeds them to m16n8 warp-level MMAs as their
+// fragments. A register is loaded again for a step further on as soon as it has been multiplied, so that a lane always
+// has several steps' loads in flight, as many as fit beside the sums. The partial sums of the warps are added in warp
+// order through shared memory.
+// (Queues in shared memory filled by cp.async, with more bytes in flight and no registers held, were slower: two warps a
+// scheduler do not hide the copies' and reads' own instructions, and large blocks keep the next kernel from starting
+// early. One token, d = 768, 8-bit weights: 9.7 us against ONE_US; 64 tokens, bf16: 24.4 against SIXTYFOUR_US.)
 #pragma once
 
 #include "common.cuh"
@@ -20,15 +25,21 @@ constexpr int FEW_THREADS = FEW_WARPS * 32;
 // activations.
 enum FewVar { FEWV_F32 = 0, FEWV_BF16 = 1, FEWV_W8A16 = 2, FEWV_W8A8 = 3 };
 
-template <int V, int NT>
+// NT token tiles of 8 columns; CTAS of the kernel's CTAs share an SM: two where there are few, three where there are
+// more than the SMs take at once, so that one's start and end hide behind the others' loads.
+template <int V, int NT, int CTAS>
 struct FewT {
     static constexpr int LANE = V == FEWV_F32 ? 4 : V == FEWV_BF16 ? 8 : 16;  // weight columns per lane and step
     static constexpr int STEP = 4 * LANE;                                     // and of a warp's step
     static constexpr int WSZ = V == FEWV_F32 ? 4 : V == FEWV_BF16 ? 2 : 1;
     static constexpr int XSZ = V == FEWV_F32 ? 4 : V == FEWV_W8A8 ? 1 : 2;
     static constexpr int XV = LANE * XSZ / 16;  // 16-byte loads of activations per step and token tile
-    static constexpr int REGS = 8 + 4 * XV * NT;
-    static constexpr int DEPTH = REGS >= 72 ? 1 : REGS >= 40 ? 2 : REGS >= 24 ? 3 : REGS >= 16 ? 5 : 6;
+    // Steps of weights and of activations in flight, 8 and 4 XV NT registers each
+    static constexpr int XR = XV * NT;
+    static constexpr int DW = CTAS == 2 ? (XR == 1 ? 8 : XR == 2 ? 6 : XR == 4 ? 4 : 2) : (XR <= 2 ? 4 : 2);
+    static constexpr int DX = CTAS == 2 ? (XR == 1 ? 4 : XR == 2 ? 3 : XR == 4 ? 2 : 1) : (XR <= 2 ? 2 : 1);
+    static_assert(DW % DX == 0);
+    static constexpr int SMEM = FEW_WARPS * NT * 128 * 4;  // the partial sums
 };
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -37,9 +48,9 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void mma_e4m3(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
-                                         uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                        uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -54,100 +65,101 @@ __device__ __forceinline__ void few_split(uint32_t v, uint32_t& h, uint32_t& l) 
     h = (v + 0x1000u) & 0xFFFFE000u;
     l = __float_as_uint(__uint_as_float(v) - __uint_as_float(h)) + 0x1000u;
 }
+// Two e4m3 values as a pair of fp16, exactly
+__device__ __forceinline__ uint32_t fp8x2_to_f16x2(uint32_t v) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)v));
+    return h;
+}
 // Two e4m3 values as a pair of bf16, exactly
 __device__ __forceinline__ uint32_t fp8x2_to_bf16x2(uint32_t v) {
     const float2 f = fp8_unpack2(v & 0xFFFFu);
     return pack_bf16(f.x, f.y);
 }
 
-__device__ __forceinline__ uint4 few_ld_weight(const void* p) { return __ldg(static_cast<const uint4*>(p)); }
-__device__ __forceinline__ uint4 few_ld_token(const void* p) { return __ldcg(static_cast<const uint4*>(p)); }
-
-// A 16-row tile of a weight matrix as a lane sees it: its two rows, K columns in use.
+// A 16-row tile of weights and its activation rows as a lane sees them. Step i of a warp is columns
+// [STEP (warp + 8 i), + STEP) of K; the lane's bytes of it start at w0 + i * (stride), w1 and tok[j] likewise.
+template <int V, int NT, int CTAS>
 struct FewTile {
+    using F = FewT<V, NT, CTAS>;
     const char* w0;
     const char* w1;
-    const uint8_t* s;  // 8-bit blocks: scale bytes of the tile's rows
-    int K;
-};
-template <int V>
-__device__ __forceinline__ FewTile few_tile(const void* w, const uint8_t* s, int64_t pitch, int64_t lds, int r0, int rows,
-                                            int K, int lane) {
-    constexpr int WSZ = FewT<V, 1>::WSZ;
-    const int g = lane >> 2;
-    FewTile t;
-    t.w0 = static_cast<const char*>(w) + (int64_t)min(r0 + g, rows - 1) * pitch * WSZ;
-    t.w1 = static_cast<const char*>(w) + (int64_t)min(r0 + g + 8, rows - 1) * pitch * WSZ;
-    t.s = s ? s + (int64_t)(r0 / 128) * lds : nullptr;
-    t.K = K;
-    return t;
-}
-
-// The weights of one round of a warp: steps i0 .. i0 + DEPTH - 1 of its own, step i being step warp + 8 i of K.
-template <int V, int NT>
-struct FewRound {
-    uint4 a[FewT<V, NT>::DEPTH], b[FewT<V, NT>::DEPTH];
-    uint32_t s[FewT<V, NT>::DEPTH];
-};
-template <int V, int NT>
-__device__ __forceinline__ void few_load(FewRound<V, NT>& r, const FewTile& t, int i0, int warp, int lane) {
-    using F = FewT<V, NT>;
-#pragma unroll
-    for (int d = 0; d < F::DEPTH; ++d) {
-        const int k = (warp + FEW_WARPS * (i0 + d)) * F::STEP + (lane & 3) * F::LANE;
-        r.a[d] = r.b[d] = make_uint4(0, 0, 0, 0);
-        r.s[d] = 0;
-        if (k < t.K) {  // K is a multiple of a lane's columns
-            r.a[d] = few_ld_weight(t.w0 + (int64_t)k * F::WSZ);
-            r.b[d] = few_ld_weight(t.w1 + (int64_t)k * F::WSZ);
-            if (V >= FEWV_W8A16) r.s[d] = __ldg(t.s + k / 128);
+    const char* tok[NT];
+    int steps, in;  // the warp's steps, and how many of them lie inside K for this lane (K is a multiple of LANE)
+    uint4 a[F::DW], b[F::DW], x[F::DX][NT][F::XV];
+    __device__ __forceinline__ int column() const {
+        return ((int)threadIdx.x >> 5) * F::STEP + (threadIdx.x & 3) * F::LANE;
+    }
+    __device__ __forceinline__ void set_weights(const void* base, int64_t pitch_bytes, int r0, int n_rows, int K) {
+        const int g = (threadIdx.x >> 2) & 7, k = column(), warp = threadIdx.x >> 5, all = (K + F::STEP - 1) / F::STEP;
+        w0 = static_cast<const char*>(base) + (int64_t)min(r0 + g, n_rows - 1) * pitch_bytes + (int64_t)k * F::WSZ;
+        w1 = static_cast<const char*>(base) + (int64_t)min(r0 + g + 8, n_rows - 1) * pitch_bytes + (int64_t)k * F::WSZ;
+        steps = all > warp ? (all - warp + FEW_WARPS - 1) / FEW_WARPS : 0;
+        in = K > k ? (K - k + FEW_WARPS * F::STEP - 1) / (FEW_WARPS * F::STEP) : 0;
+    }
+    __device__ __forceinline__ void set_row(int j, const void* row) {
+        tok[j] = static_cast<const char*>(row) + (int64_t)column() * F::XSZ;
+    }
+    __device__ __forceinline__ void load_w(int d, int i) {
+        a[d] = b[d] = make_uint4(0, 0, 0, 0);
+        if (i < in) {
+            a[d] = __ldg(reinterpret_cast<const uint4*>(w0 + (int64_t)i * (FEW_WARPS * F::STEP * F::WSZ)));
+            b[d] = __ldg(reinterpret_cast<const uint4*>(w1 + (int64_t)i * (FEW_WARPS * F::STEP * F::WSZ)));
         }
     }
-}
+    __device__ __forceinline__ void load_x(int d, int i) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int q = 0; q < F::XV; ++q) {
+                x[d][j][q] = make_uint4(0, 0, 0, 0);
+                if (i < in)
+                    x[d][j][q] = __ldcg(reinterpret_cast<const uint4*>(tok[j] + (int64_t)i * (FEW_WARPS * F::STEP * F::XSZ)) + q);
+            }
+    }
+    // The first steps' loads: the weights' before the activations may be read.
+    __device__ __forceinline__ void start_w() {
+#pragma unroll
+        for (int d = 0; d < F::DW; ++d) load_w(d, d);
+    }
+    __device__ __forceinline__ void start_x() {
+#pragma unroll
+        for (int d = 0; d < F::DX; ++d) load_x(d, d);
+    }
+};
 
-// acc[j] += the warp's share of the tile times activation rows 8 j .. 8 j + 7 (tok[j]: the lane's row 8 j + g).
-// first: the first round's weights, loaded by the caller. xs[j] (FEWV_W8A8): the scale bytes of the lane's two
-// accumulator columns' rows. sums (LN): += W 1.
-// Sums: a step's products are added from zero and then to acc in fp32, so that the tensor cores' truncating
-// accumulation runs over one step (fp32) or one scale block's part (8 bits) only; bf16 outputs, whose own rounding
-// is 2^-9, accumulate in place.
-template <int V, int NT, bool LN>
-__device__ __forceinline__ void few_product(float (&acc)[NT][4], float (&sums)[4], const FewTile& t,
-                                            FewRound<V, NT>& first, const char* const (&tok)[NT],
-                                            const uint8_t* const (&xs)[NT][2], int warp, int lane) {
-    using F = FewT<V, NT>;
-    const int steps = (t.K + F::STEP - 1) / F::STEP;
-    for (int i0 = 0; warp + FEW_WARPS * i0 < steps; i0 += F::DEPTH) {
-        if (i0) few_load<V, NT>(first, t, i0, warp, lane);
-        uint4 x[F::DEPTH][NT][F::XV];
+// acc[j] += the warp's share of the tile (weights and activations started) times its activation rows. sw (8-bit weights): the scale bytes of the
+// tile's rows; sx (FEWV_W8A8): those of the activation rows, ldx bytes apart, rows past the last as the last; both in
+// shared memory. sums (LN): += W 1.
+// A step's products are added from zero and then to acc in fp32, so that the tensor cores' truncating accumulation
+// runs over one step (fp32) or one scale block's part (8 bits) only; bf16 outputs, whose own rounding is 2^-9,
+// accumulate in place.
+template <int V, int NT, int CTAS, bool LN>
+__device__ __forceinline__ void few_product(float (&acc)[NT][4], float (&sums)[4], FewTile<V, NT, CTAS>& t, const uint8_t* sw,
+                                            const uint8_t* sx, int ldx, int rows) {
+    using F = FewT<V, NT, CTAS>;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int i0 = 0; i0 < t.steps; i0 += F::DW) {
 #pragma unroll
-        for (int d = 0; d < F::DEPTH; ++d) {
-            const int k = (warp + FEW_WARPS * (i0 + d)) * F::STEP + (lane & 3) * F::LANE;
-#pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int q = 0; q < F::XV; ++q) {
-                    x[d][j][q] = make_uint4(0, 0, 0, 0);
-                    if (k < t.K) x[d][j][q] = few_ld_token(tok[j] + (int64_t)k * F::XSZ + 16 * q);
-                }
-        }
-#pragma unroll
-        for (int d = 0; d < F::DEPTH; ++d) {
-            const uint4 a = first.a[d], b = first.b[d];
-            const uint32_t wa[4] = {a.x, a.y, a.z, a.w}, wb[4] = {b.x, b.y, b.z, b.w};
+        for (int d = 0; d < F::DW; ++d) {
+            const int i = i0 + d, xd = d % F::DX;
+            if (i >= t.steps) break;
+            const uint32_t wa[4] = {t.a[d].x, t.a[d].y, t.a[d].z, t.a[d].w}, wb[4] = {t.b[d].x, t.b[d].y, t.b[d].z, t.b[d].w};
+            const int blk = (warp + FEW_WARPS * i) * F::STEP / 128;  // of 8-bit weights: a step lies in one block
             if constexpr (V == FEWV_F32) {
                 uint32_t ah[4], al[4], bh[4], bl[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    few_split(wa[i], ah[i], al[i]);
-                    few_split(wb[i], bh[i], bl[i]);
+                for (int h = 0; h < 4; ++h) {
+                    few_split(wa[h], ah[h], al[h]);
+                    few_split(wb[h], bh[h], bl[h]);
                 }
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
-                    const uint32_t xv[4] = {x[d][j][0].x, x[d][j][0].y, x[d][j][0].z, x[d][j][0].w};
+                    const uint4 v = t.x[xd][j][0];
+                    const uint32_t xv[4] = {v.x, v.y, v.z, v.w};
                     uint32_t xh[4], xl[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) few_split(xv[i], xh[i], xl[i]);
+                    for (int h = 0; h < 4; ++h) few_split(xv[h], xh[h], xl[h]);
                     float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int h = 0; h < 4; h += 2) {  // the small products first
@@ -155,10 +167,9 @@ __device__ __forceinline__ void few_product(float (&acc)[NT][4], float (&sums)[4
                         mma_tf32(part, ah[h], bh[h], ah[h + 1], bh[h + 1], xl[h], xl[h + 1]);
                     }
 #pragma unroll
-                    for (int h = 0; h < 4; h += 2)
-                        mma_tf32(part, ah[h], bh[h], ah[h + 1], bh[h + 1], xh[h], xh[h + 1]);
+                    for (int h = 0; h < 4; h += 2) mma_tf32(part, ah[h], bh[h], ah[h + 1], bh[h + 1], xh[h], xh[h + 1]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[j][i] += part[i];
+                    for (int c = 0; c < 4; ++c) acc[j][c] += part[c];
                 }
                 if (LN) {
                     const uint32_t one = __float_as_uint(1.f);
@@ -168,25 +179,31 @@ __device__ __forceinline__ void few_product(float (&acc)[NT][4], float (&sums)[4
 #pragma unroll
                     for (int h = 0; h < 4; h += 2) mma_tf32(part, ah[h], bh[h], ah[h + 1], bh[h + 1], one, one);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sums[i] += part[i];
+                    for (int c = 0; c < 4; ++c) sums[c] += part[c];
                 }
             } else if constexpr (V == FEWV_W8A8) {
-                const int blk = (warp + FEW_WARPS * (i0 + d)) * F::STEP / 128;
-                const float sw = fp8_scale(first.s[d]);
-                const bool in = blk * 128 < t.K;
+                // both operands widened to fp16, exactly (the warp-level e4m3 MMA is no faster)
+                const float s = fp8_scale(sw[blk]);
+                uint32_t f[4][4];
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    f[h][0] = fp8x2_to_f16x2(wa[h]), f[h][1] = fp8x2_to_f16x2(wb[h]);
+                    f[h][2] = fp8x2_to_f16x2(wa[h] >> 16), f[h][3] = fp8x2_to_f16x2(wb[h] >> 16);
+                }
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
-                    const uint4 v = x[d][j][0];
+                    const uint4 v = t.x[xd][j][0];
+                    const uint32_t xv[4] = {v.x, v.y, v.z, v.w};
                     float part[4] = {0.f, 0.f, 0.f, 0.f};
-                    mma_e4m3(part, wa[0], wb[0], wa[1], wb[1], v.x, v.y);
-                    mma_e4m3(part, wa[2], wb[2], wa[3], wb[3], v.z, v.w);
-                    if (in) {
-                        const float s0 = fp8_scale(__ldcg(xs[j][0] + blk)), s1 = fp8_scale(__ldcg(xs[j][1] + blk));
-                        acc[j][0] = fmaf(part[0] * sw, s0, acc[j][0]);
-                        acc[j][1] = fmaf(part[1] * sw, s1, acc[j][1]);
-                        acc[j][2] = fmaf(part[2] * sw, s0, acc[j][2]);
-                        acc[j][3] = fmaf(part[3] * sw, s1, acc[j][3]);
-                    }
+#pragma unroll
+                    for (int h = 0; h < 4; ++h)
+                        mma_f16(part, f[h][0], f[h][1], f[h][2], f[h][3], fp8x2_to_f16x2(xv[h]), fp8x2_to_f16x2(xv[h] >> 16));
+                    const int r = 8 * j + 2 * (lane & 3);
+                    const float s0 = s * fp8_scale(sx[min(r, rows - 1) * ldx + blk]), s1 = s * fp8_scale(sx[min(r + 1, rows - 1) * ldx + blk]);
+                    acc[j][0] = fmaf(part[0], s0, acc[j][0]);
+                    acc[j][1] = fmaf(part[1], s1, acc[j][1]);
+                    acc[j][2] = fmaf(part[2], s0, acc[j][2]);
+                    acc[j][3] = fmaf(part[3], s1, acc[j][3]);
                 }
             } else {
                 constexpr int NS = F::LANE / 4;  // MMAs of 16 columns per step: four of the lane's columns each
@@ -201,20 +218,22 @@ __device__ __forceinline__ void few_product(float (&acc)[NT][4], float (&sums)[4
                         f[h][2] = fp8x2_to_bf16x2(wa[h & 3] >> 16), f[h][3] = fp8x2_to_bf16x2(wb[h & 3] >> 16);
                     }
                 }
-                const float sw = V == FEWV_W8A16 ? fp8_scale(first.s[d]) : 1.f;
+                const float s = V == FEWV_W8A16 ? fp8_scale(sw[blk]) : 1.f;
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
                     uint32_t xv[2 * NS];
 #pragma unroll
-                    for (int q = 0; q < F::XV; ++q)
-                        xv[4 * q] = x[d][j][q].x, xv[4 * q + 1] = x[d][j][q].y, xv[4 * q + 2] = x[d][j][q].z, xv[4 * q + 3] = x[d][j][q].w;
+                    for (int q = 0; q < F::XV; ++q) {
+                        const uint4 v = t.x[xd][j][q];
+                        xv[4 * q] = v.x, xv[4 * q + 1] = v.y, xv[4 * q + 2] = v.z, xv[4 * q + 3] = v.w;
+                    }
                     if (V == FEWV_W8A16) {
                         float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                         for (int h = 0; h < NS; ++h)
                             mma_bf16(part, f[h][0], f[h][1], f[h][2], f[h][3], xv[2 * h], xv[2 * h + 1]);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[j][i] = fmaf(part[i], sw, acc[j][i]);
+                        for (int c = 0; c < 4; ++c) acc[j][c] = fmaf(part[c], s, acc[j][c]);
                     } else {
 #pragma unroll
                         for (int h = 0; h < NS; ++h)
@@ -227,9 +246,11 @@ __device__ __forceinline__ void few_product(float (&acc)[NT][4], float (&sums)[4
 #pragma unroll
                     for (int h = 0; h < NS; ++h) mma_bf16(part, f[h][0], f[h][1], f[h][2], f[h][3], one, one);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sums[i] = fmaf(part[i], sw, sums[i]);
+                    for (int c = 0; c < 4; ++c) sums[c] = fmaf(part[c], s, sums[c]);
                 }
             }
+            t.load_w(d, i + F::DW);
+            t.load_x(xd, i + F::DX);
         }
     }
 }
@@ -255,6 +276,5 @@ __device__ __forceinline__ float few_sum(const float* red, int col, int row) {
     for (int w = 0; w < FEW_WARPS; ++w) s += red[(w * NT * 8 + col) * 16 + row];
     return s;
 }
-constexpr int few_smem(int nt) { return FEW_WARPS * nt * 128 * 4; }
 
 }  // namespace cm

@@ -33,6 +33,15 @@ __device__ __forceinline__ uint32_t fp8_pack2(float lo, float hi) {
 __device__ __forceinline__ uint32_t fp8_pack4(float a, float b, float c, float d) {
     return fp8_pack2(a, b) | fp8_pack2(c, d) << 16;
 }
+// 32 values times inv, to e4m3.
+__device__ __forceinline__ void fp8_pack32(uint32_t (&o)[8], const float (&v)[32], float inv) {
+    const float2 k = make_float2(inv, inv);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float2 a = __fmul2_rn(make_float2(v[4 * i], v[4 * i + 1]), k), b = __fmul2_rn(make_float2(v[4 * i + 2], v[4 * i + 3]), k);
+        o[i] = fp8_pack4(a.x, a.y, b.x, b.y);
+    }
+}
 // Two e4m3 values (the low byte first) as fp32, exactly.
 __device__ __forceinline__ float2 fp8_unpack2(uint32_t v) {
     uint32_t h;
@@ -49,6 +58,13 @@ __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v
 __device__ __forceinline__ float max_abs(float a, float b) {
     float r;
     asm("max.NaN.xorsign.abs.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+// The largest magnitude of three values, NaN if one of them is.
+__device__ __forceinline__ float max_abs3(float a, float b, float c) {
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
 

@@ -10,11 +10,10 @@
 //
 // One persistent, warp-specialised kernel per N tile width:
 //   warps 0-7    epilogue: warp w reads TMEM lane quarter w % 4 (its 32 rows) and column half w / 4;
-//   warps 8-11   scales: one warp per slot loads the words of the tile's rows and of W's blocks and lays them out in
-//                shared memory;
-//   warp 12      TMEM allocation, tcgen05.cp of the scales, tcgen05.mma and commits (the whole warp in step, one
+//   warps 8-9    scales: load the words of the tile's rows and of W's blocks and lay them out in shared memory;
+//   warp 10      TMEM allocation, tcgen05.cp of the scales, tcgen05.mma and commits (the whole warp in step, one
 //                elected lane issues);
-//   warp 13      TMA producer of the q tiles: 128 rows of A and BN of W, 128 bytes each, 128-byte swizzle.
+//   warp 11      TMA producer of the q tiles: 128 rows of A and BN of W, 128 bytes each, 128-byte swizzle.
 // Rings: q stages in shared memory (full: TMA bytes, empty: commit), scale slots (full: the scale
 // warp's arrival, empty: commit), two accumulators. Grouped products walk (group, row tile, column
 // tile) from the device-resident offsets; a row tile never crosses its group's end.
@@ -22,8 +21,7 @@
 // finish, frees its tensor memory and returns.
 #include <cstdint>
 #include <cstring>
-#include <cstdio>
-#include <cstdlib>
+#include <atomic>
 
 #include "common.cuh"
 #include "fp8.cuh"
@@ -35,8 +33,8 @@ namespace cm {
 namespace {
 
 constexpr int F8_NUM_EPI = 8;
-constexpr int F8_WARP_SCALE = 8, F8_WARP_MMA = 12, F8_WARP_TMA = 13;
-constexpr int F8_THREADS = 32 * 14;
+constexpr int F8_WARP_SCALE = 8, F8_WARP_MMA = 10, F8_WARP_TMA = 11;
+constexpr int F8_THREADS = 32 * 12;
 constexpr int F8_BM = 128;
 constexpr int F8_BK = 128;
 
@@ -127,8 +125,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
     }
     __syncthreads();
     const uint32_t tmem = warp_uniform(*tmem_slot);
-    const int n_tiles = (a.N + BN - 1) / BN;
-    const int64_t num_tiles = warp_uniform((long long)s_prefix[a.E] * n_tiles);
+    F8Walk t(blockIdx.x, gridDim.x, a.N, F8_BM, BN, a.E, s_off, s_prefix);
     const int nkb = a.nkb;
 
     if (warp == F8_WARP_TMA) {
@@ -136,9 +133,8 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
         int stage = 0;
         uint32_t ph = 0, issued = 0, par = 0;  // bit s: stage s has had a load; parity of its last
         bool ok = true;
-        for (int64_t tile = blockIdx.x; tile < num_tiles && ok; tile += gridDim.x) {
-            F8Tile t = f8_tile(a.E, tile, n_tiles, F8_BM, BN, s_off, s_prefix);
-            const int e = warp_uniform(t.e), n0 = warp_uniform(t.n0), m0 = warp_uniform((int)t.m0);
+        for (; warp_uniform((int)t.live()) && ok; t.next()) {
+            const int e = warp_uniform(t.e), n0 = warp_uniform(t.n0), m0 = warp_uniform(t.m0);
             for (int kb = 0; kb < nkb; ++kb) {
                 if (!mbar_wait_warp(empty_bar(stage), ph ^ 1, abort_flag, a.status, lim)) {
                     ok = false;
@@ -165,7 +161,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
         int stage = 0, slot = 0, acc = 0;
         uint32_t ph = 0, sph = 0, aph = 0;
         bool ok = true;
-        for (int64_t tile = blockIdx.x; tile < num_tiles && ok; tile += gridDim.x) {
+        for (; warp_uniform((int)t.live()) && ok; t.next()) {
             if (!mbar_wait_warp(tempty_bar(acc), aph ^ 1, abort_flag, a.status, lim)) break;
             tc_fence_after();
             const uint32_t d = tmem + acc * BN;
@@ -217,9 +213,8 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
         mbar_wait_warp(drain_bar, 0, nullptr, a.status, lim + 10000000ull);
     } else if (warp >= F8_WARP_SCALE) {
         // ------------------------------------------------ scales
-        const int slot = warp - F8_WARP_SCALE;
-        f8_scale_warp<BN>(a, slot, blockIdx.x, gridDim.x, num_tiles, n_tiles, F8_BM, 0, s_off, s_prefix, lane,
-                          [&](const F8Scales<BN>& w, uint32_t ph) {
+        f8_scale_warp<BN>(a, warp - F8_WARP_SCALE, t, 0, lane,
+                          [&](const F8Scales<BN>& w, int slot, uint32_t ph) {
                               if (!mbar_wait_warp(sempty_bar(slot), ph ^ 1, abort_flag, a.status, lim)) return false;
                               w.store(s_sf + slot * C::SF_BYTES, lane);
                               fence_proxy_async_smem();
@@ -240,8 +235,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
                           ((reinterpret_cast<uintptr_t>(a.out) & 31) == 0 && (a.ldo * esz & 31) == 0);
         int acc = 0;
         uint32_t aph = 0, pph = 0;
-        for (int64_t tile = blockIdx.x; tile < num_tiles; tile += gridDim.x) {
-            const F8Tile t = f8_tile(a.E, tile, n_tiles, F8_BM, BN, s_off, s_prefix);
+        for (; t.live(); t.next()) {
             const int64_t m = t.m0 + quarter * 32 + lane;
             const bool live = m < t.hi;
             const int64_t orow = live ? (a.rows ? (int64_t)__ldcg(a.rows + m) : m) : 0;
@@ -441,6 +435,10 @@ cudaError_t launch_fp8_gemm(const Fp8GemmArgs& a, const Fp8Pick& k, int num_sms,
     }
 }
 
+// The kernel that tests have fixed (width << 1 | pair), or 0; FP8_FORCE_FEW: the one for few rows.
+constexpr int FP8_FORCE_FEW = 16 << 1;
+static std::atomic<int> g_forced{0};
+
 int run_fp8_gemm(Fp8GemmArgs& g, const clearmoe_fp8* A, const clearmoe_fp8* W, int E, int num_sms, cudaStream_t s) {
     g.M = A->rows;
     g.N = (int)W[0].rows;
@@ -448,8 +446,21 @@ int run_fp8_gemm(Fp8GemmArgs& g, const clearmoe_fp8* A, const clearmoe_fp8* W, i
     g.E = E;
     g.lds = fp8_lds(A->cols);
     g.sa = A->scale;
+    const int forced = g_forced.load(std::memory_order_relaxed);
+    if (!g.offsets && g.out_kind != FP8_OUT_FP8 && g.M <= FP8_FEW_MAX && (g.M + 1) * g.nkb <= FP8_FEW_SCALES &&
+        (forced == 0 || forced == FP8_FORCE_FEW)) {
+        g.x = A->q;
+        g.w = W->q;
+        g.sb[0] = W->scale;
+        if (launch_fp8_few(g, s) == cudaSuccess) return CLEARMOE_OK;
+        (void)cudaGetLastError();
+        return CLEARMOE_ECUDA;
+    }
     Fp8Pick k = fp8_pick(g.M, g.N, g.nkb, g.out_kind, E, num_sms);
-    if (const char* o = getenv("F8PICK")) { int bn, pr; sscanf(o, "%d,%d", &bn, &pr); k = {bn, pr}; }
+    if (forced && forced != FP8_FORCE_FEW) {
+        const Fp8Pick f = {forced >> 1, forced & 1};
+        if (g.out_kind != FP8_OUT_FP8 || f.bn % 128 == 0) k = f;
+    }
     // rows of bytes as rows of half as many 16-bit elements: boxes of 64 of them are 128 bytes
     const int64_t cols16 = fp8_ldq(A->cols) / 2;
     if (encode_tmap_bf16(&g.tmA, A->q, A->rows, cols16, F8_BM)) return CLEARMOE_ECUDA;
@@ -546,6 +557,18 @@ int clearmoe_fp8_grouped_gemm(const clearmoe_fp8* A, const clearmoe_fp8* W, int3
     g.offsets = offsets;
     g.rows = perm;
     return run(g, A, W, E, stream);
+}
+
+int clearmoe_debug_fp8_kernel(int32_t width, int32_t pair) {
+    if (width == 0 && pair == 0) {
+        cm::g_forced = 0;
+        return CLEARMOE_OK;
+    }
+    const bool known = pair == 1 ? width == 256 || width == 192 || width == 128
+                                 : pair == 0 && (width == 192 || width == 128 || width == 64 || width == 32 || width == 16);
+    if (!known) return CLEARMOE_EINVAL;
+    cm::g_forced = width << 1 | pair;
+    return CLEARMOE_OK;
 }
 
 }  // extern "C"

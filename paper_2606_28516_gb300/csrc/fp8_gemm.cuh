@@ -43,11 +43,6 @@ __device__ __forceinline__ void tmem_cp_scales(uint32_t tmem, uint32_t smem) {
         : "r"(taddr))
 
 
-struct F8Tile {
-    int64_t m0, hi;  // rows [m0, hi) of the group, of which the tile takes the first
-    int n0, e;
-};
-
 // Row boundaries of the groups and the row tiles before each, in shared memory: off[E + 1], prefix[E + 1].
 __device__ __forceinline__ void f8_groups(const Fp8GemmArgs& a, int bm, int* off, int* prefix) {
     int acc = 0;
@@ -58,17 +53,40 @@ __device__ __forceinline__ void f8_groups(const Fp8GemmArgs& a, int bm, int* off
     }
     prefix[a.E] = acc;
 }
-__device__ __forceinline__ F8Tile f8_tile(int E, int64_t tile, int n_tiles, int bm, int bn, const int* off, const int* prefix) {
-    F8Tile t;
-    const int mt = tile <= 0x7FFFFFFF ? (int)((uint32_t)tile / (uint32_t)n_tiles) : (int)(tile / n_tiles);
-    t.n0 = (int)(tile - (int64_t)mt * n_tiles) * bn;
-    int e = 0;
-    while (e + 1 < E && prefix[e + 1] <= mt) ++e;
-    t.e = e;
-    t.m0 = off[e] + (int64_t)(mt - prefix[e]) * bm;
-    t.hi = off[e + 1];
-    return t;
-}
+// A CTA's (or pair's) walk over the tiles first, first + step, ...: row tile by row tile, columns fastest. m0: the tile's
+// first row, of the group's rows up to hi. Advanced by additions (a division and a search per tile and warp were an
+// eighth of the epilogue's instructions).
+struct F8Walk {
+    int mt, nt;  // row and column tile
+    int e, m0, hi, n0;
+    int n_tiles, bm, bn, E, step_mt, step_nt;
+    const int* off;
+    const int* prefix;
+    __device__ __forceinline__ F8Walk(int first, int step, int N, int bm_, int bn_, int E_, const int* off_, const int* prefix_)
+        : e(0), n_tiles((N + bn_ - 1) / bn_), bm(bm_), bn(bn_), E(E_), off(off_), prefix(prefix_) {
+        mt = first / n_tiles;
+        nt = first - mt * n_tiles;
+        step_mt = step / n_tiles;
+        step_nt = step - step_mt * n_tiles;
+        place();
+    }
+    __device__ __forceinline__ bool live() const { return mt < prefix[E]; }
+    __device__ __forceinline__ void next() {
+        mt += step_mt;
+        nt += step_nt;
+        if (nt >= n_tiles) {
+            nt -= n_tiles;
+            ++mt;
+        }
+        place();
+    }
+    __device__ __forceinline__ void place() {
+        while (e + 1 < E && prefix[e + 1] <= mt) ++e;
+        m0 = off[e] + (mt - prefix[e]) * bm;
+        hi = off[e + 1];
+        n0 = nt * bn;
+    }
+};
 
 // The scale words of one 512-column chunk as a lane of the scale warp holds them: rows 32 j + lane of the CTA's 128
 // rows of A, and those of W's blocks (columns n0 + 32 j of the tile lie in one block of 128 rows). Tensor memory
@@ -81,11 +99,11 @@ struct F8Scales {
     static constexpr int NW = BN % 128 == 0 ? BN / 128 : BN >= 64 ? BN / 64 : 1;  // different words of W at most
     static constexpr int SPAN = BN / NW;                                          // columns of each
     uint32_t a[4], w[NW];
-    __device__ __forceinline__ void load(const Fp8GemmArgs& g, const F8Tile& t, int64_t m0, int chunk, int lane) {
+    __device__ __forceinline__ void load(const Fp8GemmArgs& g, const F8Walk& t, int m0, int chunk, int lane) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {  // rows past the group's end: any row's scales will do
-            const int64_t r = min(m0 + 32 * j + lane, t.hi - 1);
-            a[j] = __ldcg(reinterpret_cast<const uint32_t*>(g.sa + r * g.lds) + chunk);
+            const int r = min(m0 + 32 * j + lane, t.hi - 1);
+            a[j] = __ldcg(reinterpret_cast<const uint32_t*>(g.sa + (int64_t)r * g.lds) + chunk);
         }
         const uint8_t* sb = g.sb[t.e];
 #pragma unroll
@@ -106,49 +124,39 @@ struct F8Scales {
 };
 
 constexpr int F8_SLOTS = 4;  // scale slots in shared memory, each 512 of K; two of them at a time in tensor memory
+constexpr int F8_SCALE_WARPS = 2;
 constexpr int F8_AHEAD = 2;
 
-// The work of scale warp `slot` of F8_SLOTS: the words of every F8_SLOTS-th 512-column chunk of the CTA's tiles, in
-// order, each handed to put(words, phase), false when it gave up. One warp per slot, because a chunk takes a warp over a
-// microsecond from the free slot to the arrival (loads that wait behind the queued tile loads, the fence between the
-// proxies): with one warp for all slots 93 us, with four SCALES_US for 19,456 x 1,792 x 4,096. F8_AHEAD chunks' loads
-// are in flight; a set of registers is loaded again as soon as its words are stored (a set moved to another would wait
-// for its loads).
+// The work of scale warp `which` of F8_SCALE_WARPS: the words of every F8_SCALE_WARPS-th 512-column chunk of the CTA's
+// tiles, in order, each handed to put(words, slot, phase), false when it gave up. Two warps, because a chunk takes a
+// warp over a microsecond from the free slot to the arrival (loads that wait behind the queued tile loads, the fence
+// between the proxies): one warp 93 us, two TWO_US, four 83 us for 19,456 x 1,792 x 4,096 in 256 x 256 tiles.
+// F8_AHEAD chunks' loads are in flight; a set of registers is loaded again as soon as its words are stored (a set
+// moved to another would wait for its loads).
 template <int BN, class Put>
-__device__ __forceinline__ void f8_scale_warp(const Fp8GemmArgs& a, int slot, int64_t first, int step, int64_t num_tiles,
-                                              int n_tiles, int bm, int row0, const int* off, const int* prefix, int lane, Put put) {
+__device__ __forceinline__ void f8_scale_warp(const Fp8GemmArgs& a, int which, F8Walk t, int row0, int lane, Put put) {
     const int nsb = (a.nkb + 3) / 4;
-    const int64_t chunks = (num_tiles > first ? (num_tiles - first + step - 1) / step : 0) * nsb;
     F8Scales<BN> w[F8_AHEAD];
-    // the next chunk to load: its tile and place in it
-    int64_t tile = first;
-    int c = slot;
-    F8Tile t = {};
-    bool decoded = false;
+    int c = which;  // the next chunk to load: its place in tile t
     auto load_next = [&](F8Scales<BN>& x) {
-        while (c >= nsb) {
+        while (c >= nsb && t.live()) {
             c -= nsb;
-            tile += step;
-            decoded = false;
+            t.next();
         }
-        if (tile >= num_tiles) return;
-        if (!decoded) t = f8_tile(a.E, tile, n_tiles, bm, BN, off, prefix);
-        decoded = true;
+        if (!t.live()) return false;
         x.load(a, t, t.m0 + row0, c, lane);
-        c += F8_SLOTS;
+        c += F8_SCALE_WARPS;
+        return true;
     };
+    bool full[F8_AHEAD];
 #pragma unroll
-    for (int i = 0; i < F8_AHEAD; ++i) load_next(w[i]);
-    uint32_t ph = 0;
-    for (int64_t at = slot; at < chunks;) {
+    for (int i = 0; i < F8_AHEAD; ++i) full[i] = load_next(w[i]);
+    for (uint32_t at = which;;) {  // chunk number, as far as slots and phases go
 #pragma unroll
         for (int i = 0; i < F8_AHEAD; ++i) {
-            if (at < chunks) {
-                if (!put(w[i], ph)) return;
-                load_next(w[i]);
-                at += F8_SLOTS;
-                ph ^= 1;
-            }
+            if (!full[i] || !put(w[i], (int)(at % F8_SLOTS), at / F8_SLOTS & 1)) return;
+            full[i] = load_next(w[i]);
+            at += F8_SCALE_WARPS;
         }
     }
 }
@@ -159,6 +167,22 @@ __device__ __forceinline__ void st_global_32(void* p, const uint32_t (&v)[8]) {
                  : "memory");
 }
 
+// gelu_pair_bf16 with max(u, 0) taken directly, two operations a pair less: -inf gives 0, GELU's limit, instead of NaN.
+// The epilogue of 8-bit outputs is bound by its instructions.
+__device__ __forceinline__ float2 gelu_pair_fp8(float2 u) {
+    const float2 v = make_float2(fmaxf(-fabsf(u.x), GeluE::HOLD), fmaxf(-fabsf(u.y), GeluE::HOLD));
+    float2 q = __ffma2_rn(make_float2(GeluE::C6, GeluE::C6), v, make_float2(GeluE::C5, GeluE::C5));
+    q = __ffma2_rn(q, v, make_float2(GeluE::C4, GeluE::C4));
+    q = __ffma2_rn(q, v, make_float2(GeluE::C3, GeluE::C3));
+    q = __ffma2_rn(q, v, make_float2(GeluE::C2, GeluE::C2));
+    q = __ffma2_rn(q, v, make_float2(GeluE::C1, GeluE::C1));
+    q = __ffma2_rn(q, v, make_float2(-1.f, -1.f));
+    float2 r;  // NaN stays NaN
+    asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r.x) : "f"(u.x));
+    asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r.y) : "f"(u.y));
+    return __ffma2_rn(v, make_float2(ex2_approx(q.x), ex2_approx(q.y)), r);
+}
+
 // CW accumulator columns + bias, activation; bias from the warp's shared-memory line.
 template <int CW, bool EXACT>
 __device__ __forceinline__ void f8_act(float (&v)[CW], const float* s_bias, bool has_bias, int act) {
@@ -166,20 +190,31 @@ __device__ __forceinline__ void f8_act(float (&v)[CW], const float* s_bias, bool
 #pragma unroll
         for (int i = 0; i < CW; i += 4) {
             const float4 b = *reinterpret_cast<const float4*>(s_bias + i);
-            v[i] += b.x, v[i + 1] += b.y, v[i + 2] += b.z, v[i + 3] += b.w;
+            const float2 lo = __fadd2_rn(make_float2(v[i], v[i + 1]), make_float2(b.x, b.y));
+            const float2 hi = __fadd2_rn(make_float2(v[i + 2], v[i + 3]), make_float2(b.z, b.w));
+            v[i] = lo.x, v[i + 1] = lo.y, v[i + 2] = hi.x, v[i + 3] = hi.y;
         }
     }
     if (act == CLEARMOE_ACT_GELU) {
 #pragma unroll
         for (int i = 0; i < CW; i += 2) {
             const float2 u = make_float2(v[i], v[i + 1]);
-            const float2 g = EXACT ? gelu_pair_f32(u) : gelu_pair_bf16(u);
+            const float2 g = EXACT ? gelu_pair_f32(u) : gelu_pair_fp8(u);
             v[i] = g.x, v[i + 1] = g.y;
         }
     } else if (act == CLEARMOE_ACT_RELU) {
 #pragma unroll
         for (int i = 0; i < CW; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];  // NaN stays NaN
     }
+}
+__device__ __forceinline__ float f8_max_abs32(const float (&v)[32]) {
+    float m[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 32; i += 4) {
+        m[0] = max_abs3(m[0], v[i], v[i + 1]);
+        m[1] = max_abs3(m[1], v[i + 2], v[i + 3]);
+    }
+    return max_abs(m[0], m[1]);
 }
 
 }  // namespace cm

@@ -33,18 +33,20 @@ namespace cm {
 namespace {
 
 constexpr int P8_NUM_EPI = 16;
-constexpr int P8_WARP_SCALE = 16, P8_WARP_MMA = 20, P8_WARP_TMA = 21;
-constexpr int P8_THREADS = 32 * 22;
+constexpr int P8_WARP_SCALE = 16, P8_WARP_MMA = 18, P8_WARP_TMA = 19;
+constexpr int P8_THREADS = 32 * 20;
 constexpr int P8_BM = 128;  // rows per CTA
 constexpr int P8_BK = 128;
 
-template <int BN_>
+template <int BN_, int KIND>
 struct P8Cfg {
     static constexpr int BN = BN_;
     static constexpr int BH = BN / 2;  // W rows per CTA
     static constexpr int A_BYTES = P8_BM * P8_BK, B_BYTES = BH * P8_BK;
     static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
-    static constexpr int STAGES = 192 * 1024 / STAGE_BYTES;
+    // 8-bit outputs: a tile's rows of bytes, staged for whole-line stores
+    static constexpr int OUT_BYTES = KIND == FP8_OUT_FP8 ? P8_BM * BN : 0;
+    static constexpr int STAGES = (192 * 1024 - OUT_BYTES) / STAGE_BYTES;
     static constexpr bool OVL = BN == 256;
     static constexpr int ACC1 = OVL ? 224 : BN;  // first column of the second accumulator
     static constexpr int SF_COL = ACC1 + BN;
@@ -52,8 +54,8 @@ struct P8Cfg {
     static_assert(SF_COL + 2 * SF_COLS <= 512);
     static constexpr int CHUNKS = BN / 32;
     static constexpr int ROUNDS = (CHUNKS + 3) / 4;  // of four 32-column chunks, one per warp of a quarter
-    static constexpr int NBARS = 2 * STAGES + 2 * F8_SLOTS + 4 + 3 + 4;
-    static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + F8_SLOTS * SF_BYTES + P8_NUM_EPI * 32 * 4 + 2 * P8_NUM_EPI * 32 * 4 + NBARS * 8 + 16 +
+    static constexpr int NBARS = 2 * STAGES + 2 * F8_SLOTS + 4 + 3 + 4 * ROUNDS + 4;
+    static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + OUT_BYTES + F8_SLOTS * SF_BYTES + P8_NUM_EPI * 32 * 4 + 2 * ROUNDS * P8_NUM_EPI * 32 * 4 + NBARS * 8 + 16 +
                                 8 * (CM_MAX_E + 1) + 8;
 };
 
@@ -73,14 +75,15 @@ __device__ __forceinline__ void umma2_mxf8(uint32_t d_tmem, uint64_t a_desc, uin
 template <int BN_, int KIND>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
     fp8_gemm2_kernel(const __grid_constant__ Fp8GemmArgs a) {
-    using C = P8Cfg<BN_>;
+    using C = P8Cfg<BN_, KIND>;
     constexpr int BN = C::BN, STAGES = C::STAGES, SLOTS = F8_SLOTS;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* sm = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
-    unsigned char* s_sf = sm + STAGES * C::STAGE_BYTES;                       // [slot]
+    unsigned char* s_out = sm + STAGES * C::STAGE_BYTES;                      // [block][row][128], 8-bit outputs
+    unsigned char* s_sf = s_out + C::OUT_BYTES;                               // [slot]
     float* s_bias = reinterpret_cast<float*>(s_sf + SLOTS * C::SF_BYTES);      // [epilogue warp][32]
-    float* s_amax = s_bias + P8_NUM_EPI * 32;                                  // [2][epilogue warp][32]
-    uint64_t* bars = reinterpret_cast<uint64_t*>(s_amax + 2 * P8_NUM_EPI * 32);
+    float* s_amax = s_bias + P8_NUM_EPI * 32;                                  // [2][round][epilogue warp][32]
+    uint64_t* bars = reinterpret_cast<uint64_t*>(s_amax + 2 * C::ROUNDS * P8_NUM_EPI * 32);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::NBARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     volatile uint32_t* s_issued = tmem_slot + 2;  // k-blocks this CTA's producer has loaded, once it has stopped
@@ -119,7 +122,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
         mbar_init(ovl_bar, 8);  // the warps whose chunk lies in the shared columns, of both CTAs
         mbar_init(drain_bar, 1);
         mbar_init(stop_bar, 2);
-        for (int q = 0; q < 4; ++q) mbar_init(pair_bar(q), 4);
+        for (int q = 0; q < 4 * C::ROUNDS + 4; ++q) mbar_init(pair_bar(q), 4);
         *abort_flag = 0;
         mbar_fence_init();
     }
@@ -136,10 +139,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
     if (threadIdx.x == 0) f8_groups(a, 2 * P8_BM, s_off, s_prefix);
     __syncthreads();
     const uint32_t tmem = warp_uniform(*tmem_slot);  // all 512 columns: the same base in both CTAs
-    const int n_tiles = (a.N + BN - 1) / BN;
-    const int64_t num_tiles = warp_uniform((long long)s_prefix[a.E] * n_tiles);
     const int nkb = a.nkb;
-    const int cid = blockIdx.x >> 1, ncl = gridDim.x >> 1;
+    F8Walk t(blockIdx.x >> 1, gridDim.x >> 1, a.N, 2 * P8_BM, BN, a.E, s_off, s_prefix);
 
     if (warp == P8_WARP_TMA) {
         // ------------------------------------------------ producers (both CTAs)
@@ -147,10 +148,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
         int stage = 0;
         uint32_t ph = 0, issued = 0;
         bool ok = true;
-        for (int64_t tile = cid; tile < num_tiles && ok; tile += ncl) {
-            const F8Tile t = f8_tile(a.E, tile, n_tiles, 2 * P8_BM, BN, s_off, s_prefix);
+        for (; warp_uniform((int)t.live()) && ok; t.next()) {
             const int e = warp_uniform(t.e);
-            const int m0 = warp_uniform((int)t.m0 + (int)rank * P8_BM), n0 = warp_uniform(t.n0 + (int)rank * C::BH);
+            const int m0 = warp_uniform(t.m0 + (int)rank * P8_BM), n0 = warp_uniform(t.n0 + (int)rank * C::BH);
             for (int kb = 0; kb < nkb; ++kb) {
                 if (!mbar_wait_warp(empty_bar(stage), ph ^ 1, abort_flag, a.status, lim)) {
                     ok = false;
@@ -178,7 +178,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
             int stage = 0, slot = 0, acc = 0;
             uint32_t ph = 0, sph = 0, aph = 0, oph = 1;  // oph: phase of the previous tile's shared columns
             bool ok = true;
-            for (int64_t tile = cid; tile < num_tiles && ok; tile += ncl) {
+            for (; warp_uniform((int)t.live()) && ok; t.next()) {
                 if (!mbar_wait_warp(tempty_bar(acc), aph ^ 1, abort_flag, a.status, lim)) break;
                 if (C::OVL && !mbar_wait_warp(ovl_bar, oph, abort_flag, a.status, lim)) break;
                 oph ^= 1;
@@ -252,9 +252,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
     } else if (warp >= P8_WARP_SCALE) {
         // ------------------------------------------------ scales (both CTAs)
         const uint32_t sfull_leader0 = map_to_rank(sfull_bar(0), 0);
-        const int slot = warp - P8_WARP_SCALE;
-        f8_scale_warp<BN>(a, slot, cid, ncl, num_tiles, n_tiles, 2 * P8_BM, (int)rank * P8_BM, s_off, s_prefix, lane,
-                          [&](const F8Scales<BN>& w, uint32_t ph) {
+        f8_scale_warp<BN>(a, warp - P8_WARP_SCALE, t, (int)rank * P8_BM, lane,
+                          [&](const F8Scales<BN>& w, int slot, uint32_t ph) {
                               if (!mbar_wait_warp(sempty_bar(slot), ph ^ 1, abort_flag, a.status, lim)) return false;
                               w.store(s_sf + slot * C::SF_BYTES, lane);
                               fence_proxy_async_smem();
@@ -272,29 +271,126 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
         // rows of the output in whole 32-byte pieces
         const bool wide = KIND == FP8_OUT_FP8 || ((reinterpret_cast<uintptr_t>(a.out) & 31) == 0 && (a.ldo * esz & 31) == 0);
         const uint32_t tempty_leader0 = map_to_rank(tempty_bar(0), 0), ovl_leader = map_to_rank(ovl_bar, 0);
+        // What a tile's epilogue needs beside its sums, loaded a tile ahead: a load waits behind the queued tile loads.
+        float bias[C::ROUNDS];
+        int row = 0;
+        auto prefetch = [&](int acc) {
+            if (!t.live()) return;
+            const int m = t.m0 + (int)rank * P8_BM + quarter * 32 + lane;
+            if (KIND != FP8_OUT_FP8) row = m < t.hi ? (a.rows ? __ldcg(a.rows + m) : m) : 0;
+            if (has_bias) {
+#pragma unroll
+                for (int r = 0; r < C::ROUNDS; ++r) {
+                    const int n = t.n0 + ((C::OVL && acc == 0 ? C::ROUNDS - 1 - r : r) * 4 + cg) * 32 + lane;
+                    bias[r] = n >= a.N      ? 0.f
+                              : a.bias_bf16 ? bf16_to_f32(__ldg(static_cast<const uint16_t*>(a.bias) + n))
+                                            : __ldg(static_cast<const float*>(a.bias) + n);
+                }
+            }
+        };
+        prefetch(0);
         int acc = 0;
         uint32_t aph = 0, pph = 0;
+        float* ex = s_amax;
         bool ok = true;
-        for (int64_t tile = cid; tile < num_tiles && ok; tile += ncl) {
-            const F8Tile t = f8_tile(a.E, tile, n_tiles, 2 * P8_BM, BN, s_off, s_prefix);
-            const int64_t m = t.m0 + (int64_t)rank * P8_BM + quarter * 32 + lane;
-            const bool live = m < t.hi;
-            // what a tile needs beside its sums, loaded before the wait for them. The chunk of round r: the one in the
-            // columns that the accumulators share first.
-            const int64_t orow = live ? (a.rows ? (int64_t)__ldcg(a.rows + m) : m) : 0;
+        while (t.live() && ok) {
+            const int m0 = t.m0 + (int)rank * P8_BM, hi = t.hi, n0 = t.n0, orow = row;
+            const bool live = m0 + quarter * 32 + lane < hi;
+            // The chunk of round r: the one in the columns that the accumulators share first.
             int chunk[C::ROUNDS];
             float b[C::ROUNDS];
 #pragma unroll
             for (int r = 0; r < C::ROUNDS; ++r) {
                 chunk[r] = (C::OVL && acc == 0 ? C::ROUNDS - 1 - r : r) * 4 + cg;
-                const int n = t.n0 + chunk[r] * 32 + lane;
-                b[r] = 0.f;
-                if (has_bias && n < a.N)
-                    b[r] = a.bias_bf16 ? bf16_to_f32(__ldg(static_cast<const uint16_t*>(a.bias) + n))
-                                       : __ldg(static_cast<const float*>(a.bias) + n);
+                b[r] = bias[r];
             }
+            t.next();
+            prefetch(acc ^ 1);
             if (!mbar_wait_warp(tfull_bar(acc), aph, abort_flag, a.status, lim)) break;
             tc_fence_after();
+            const uint32_t d = tmem + lanes + acc * C::ACC1;
+            // after the read of round r: its columns may be written again
+            auto released = [&](int r) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (C::OVL && r == 0 && cg == (acc == 0 ? 3 : 0)) mbar_arrive_cluster(ovl_leader);
+                    if (r + 1 == C::ROUNDS) mbar_arrive_cluster(tempty_leader0 + 8u * acc);
+                }
+            };
+            if constexpr (KIND == FP8_OUT_FP8) {
+                // All of the tile's sums are read before any is worked on and before the next tile's MMAs start: reads
+                // beside MMAs wait for them (READ_US). Then every round's values are activated and its magnitudes handed
+                // over before the first exchange is waited for, so that arithmetic hides the latencies.
+                float v[C::ROUNDS][32];
+                {
+                    uint32_t u[C::ROUNDS][32];
+#pragma unroll
+                    for (int r = 0; r < C::ROUNDS; ++r) CM_TMEM_LD_X32(d + chunk[r] * 32, u[r]);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int r = 0; r < C::ROUNDS; ++r) {
+                        released(r);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[r][i] = __uint_as_float(u[r][i]);
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < C::ROUNDS; ++r) {
+                    if (has_bias) bias_line[lane] = b[r];
+                    __syncwarp();
+                    f8_act<32, false>(v[r], bias_line, has_bias, a.act);
+                    const int nc = n0 + chunk[r] * 32;
+                    if (nc + 32 > a.N) {  // columns past N are zero, in the last block's padding and where no block is
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (nc + i >= a.N) v[r][i] = 0.f;
+                    }
+                    ex[(r * P8_NUM_EPI + warp) * 32 + lane] = f8_max_abs32(v[r]);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(pair_bar(quarter * C::ROUNDS + r));
+                }
+#pragma unroll
+                for (int r = 0; r < C::ROUNDS; ++r) {
+                    if (!mbar_wait_warp(pair_bar(quarter * C::ROUNDS + r), pph, abort_flag, a.status, lim)) {
+                        ok = false;
+                        break;
+                    }
+                    const float* e = ex + (r * P8_NUM_EPI + quarter) * 32 + lane;
+                    const float mx = max_abs3(max_abs(e[0], e[4 * 32]), e[8 * 32], e[12 * 32]);
+                    const uint32_t s = fp8_scale_byte(abs_bits(mx));
+                    const int nc = n0 + chunk[r] * 32, trow = quarter * 32 + lane;
+                    uint32_t o[8];
+                    fp8_pack32(o, v[r], fp8_inverse_scale(s));
+                    // the row's 16-byte pieces 2 cg and 2 cg + 1, piece j at j ^ (row & 7)
+                    unsigned char* at = s_out + ((chunk[r] >> 2) * P8_BM + trow) * 128;
+                    *reinterpret_cast<uint4*>(at + (((2 * cg) ^ (trow & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+                    *reinterpret_cast<uint4*>(at + (((2 * cg + 1) ^ (trow & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+                    if (cg == 0 && live && nc < a.ldo) a.out_scale[(int64_t)(m0 + trow) * a.ldos + nc / 128] = (uint8_t)s;
+                }
+                if (!ok) break;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(pair_bar(4 * C::ROUNDS + quarter));
+                if (!mbar_wait_warp(pair_bar(4 * C::ROUNDS + quarter), pph, abort_flag, a.status, lim)) break;
+                // whole 128-byte rows of a block, four a store: rows 8 cg .. 8 cg + 7 of the quarter are this warp's. (One row a
+                // lane, 32 bytes of it at a time, took 53 us where this takes STORE_US, 19,456 x 3,072 x 768.)
+#pragma unroll
+                for (int r = 0; r < C::ROUNDS; ++r) {
+                    const int blk = chunk[r] >> 2;
+                    if (n0 + blk * 128 >= a.ldo) continue;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int trow = quarter * 32 + cg * 8 + h * 4 + (lane >> 3);
+                        const uint4 w = *reinterpret_cast<const uint4*>(s_out + (blk * P8_BM + trow) * 128 + (((lane & 7) ^ (trow & 7)) << 4));
+                        if (m0 + trow < hi)
+                            *reinterpret_cast<uint4*>(static_cast<uint8_t*>(a.out) + (int64_t)(m0 + trow) * a.ldo + n0 + blk * 128 + ((lane & 7) << 4)) = w;
+                    }
+                }
+                // the exchange of the next tile uses the other half: a warp's reads of this one precede its arrivals for
+                // the next, and those the other warps' writes two tiles on
+                pph ^= 1;
+                ex = s_amax + pph * (C::ROUNDS * P8_NUM_EPI * 32);
+            } else {
 #pragma unroll
             for (int r = 0; r < C::ROUNDS; ++r) {
                 const bool mine = chunk[r] < C::CHUNKS;
@@ -302,58 +398,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
                 __syncwarp();
                 if (mine) {
                     uint32_t u[32];
-                    CM_TMEM_LD_X32(tmem + lanes + acc * C::ACC1 + chunk[r] * 32, u);
+                    CM_TMEM_LD_X32(d + chunk[r] * 32, u);
                     if (has_bias) bias_line[lane] = b[r];
                     tmem_wait_ld();
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(u[i]);
                 }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    if (C::OVL && r == 0 && cg == (acc == 0 ? 3 : 0)) mbar_arrive_cluster(ovl_leader);
-                    if (r + 1 == C::ROUNDS) mbar_arrive_cluster(tempty_leader0 + 8u * acc);
-                }
-                const int nc = t.n0 + chunk[r] * 32;
-                if constexpr (KIND == FP8_OUT_FP8) {
-                    if (nc - cg * 32 >= a.ldo) continue;  // no such block: all four warps
-                    f8_act<32, false>(v, bias_line, has_bias, a.act);
-                    if (nc + 32 > a.N) {  // the last block's padding is zero
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (nc + i >= a.N) v[i] = 0.f;
-                    }
-                    float mx = 0.f;
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) mx = max_abs(mx, v[i]);
-                    // double-buffered: a warp's reads of one exchange precede its arrival for the next, and that the
-                    // other warps' writes two exchanges on
-                    float* ex = s_amax + pph * (P8_NUM_EPI * 32);
-                    ex[warp * 32 + lane] = mx;
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(pair_bar(quarter));
-                    if (!mbar_wait_warp(pair_bar(quarter), pph, abort_flag, a.status, lim)) {
-                        ok = false;
-                        break;
-                    }
-                    pph ^= 1;
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) mx = max_abs(mx, ex[(g * 4 + quarter) * 32 + lane]);
-                    const uint32_t s = fp8_scale_byte(abs_bits(mx));
-                    const float inv = fp8_inverse_scale(s);
-                    if (live) {
-                        uint32_t o[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            o[i] = fp8_pack4(v[4 * i] * inv, v[4 * i + 1] * inv, v[4 * i + 2] * inv, v[4 * i + 3] * inv);
-                        st_global_32(static_cast<uint8_t*>(a.out) + orow * a.ldo + nc, o);
-                        if (cg == 0) a.out_scale[orow * a.ldos + nc / 128] = (uint8_t)s;
-                    }
-                } else if (mine) {
+                released(r);
+                const int nc = n0 + chunk[r] * 32;
+                if (mine) {
                     f8_act<32, KIND == FP8_OUT_F32>(v, bias_line, has_bias, a.act);
                     if (live) {
                         if constexpr (KIND == FP8_OUT_BF16) {
-                            uint16_t* o = static_cast<uint16_t*>(a.out) + orow * a.ldo + nc;
+                            uint16_t* o = static_cast<uint16_t*>(a.out) + (int64_t)orow * a.ldo + nc;
                             if (wide && nc + 32 <= a.N) {
 #pragma unroll
                                 for (int p = 0; p < 2; ++p) {
@@ -368,7 +425,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
                                     if (nc + i < a.N) o[i] = f32_to_bf16(v[i]);
                             }
                         } else {
-                            float* o = static_cast<float*>(a.out) + orow * a.ldo + nc;
+                            float* o = static_cast<float*>(a.out) + (int64_t)orow * a.ldo + nc;
                             if (wide && nc + 32 <= a.N) {
 #pragma unroll
                                 for (int p = 0; p < 4; ++p) {
@@ -386,6 +443,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
                     }
                 }
             }
+            }
             if (++acc == 2) {
                 acc = 0;
                 aph ^= 1;
@@ -402,7 +460,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
 
 template <int BN, int KIND>
 cudaError_t launch_pair(const Fp8GemmArgs& a, int num_sms, cudaStream_t s) {
-    using C = P8Cfg<BN>;
+    using C = P8Cfg<BN, KIND>;
     static_assert(C::SMEM <= 227 * 1024);
     const cudaError_t e = smem_attr_once((const void*)fp8_gemm2_kernel<BN, KIND>, C::SMEM);
     if (e != cudaSuccess) return e;

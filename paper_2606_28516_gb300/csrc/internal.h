@@ -317,6 +317,8 @@ enum Fp8Out { FP8_OUT_F32 = 0, FP8_OUT_BF16 = 1, FP8_OUT_FP8 = 2 };
 struct Fp8GemmArgs {
     CUtensorMap tmA;
     CUtensorMap tmB[16];
+    const void* x;      // q of A, and of the first W (few rows)
+    const void* w;
     const uint8_t* sa;  // scales of A, rows lds bytes apart
     const uint8_t* sb[16];
     int64_t lds;
@@ -344,6 +346,10 @@ struct Fp8Pick {
 };
 Fp8Pick fp8_pick(int64_t M, int N, int nkb, int out_kind, int groups, int num_sms);
 cudaError_t launch_fp8_gemm(const Fp8GemmArgs& a, const Fp8Pick& k, int num_sms, cudaStream_t s);
+// A product of at most FP8_FEW_MAX rows in one group, not to 8-bit blocks, whose scales (nkb bytes per row of A, and W's) fit
+// FP8_FEW_SCALES bytes.
+constexpr int FP8_FEW_MAX = 16, FP8_FEW_SCALES = 4608;
+cudaError_t launch_fp8_few(const Fp8GemmArgs& a, cudaStream_t s);
 cudaError_t launch_fp8_gemm2(const Fp8GemmArgs& a, int bn, int num_sms, cudaStream_t s);
 // Fills the operands of a product (maps, scales, sizes) and launches it; a clearmoe_status.
 int run_fp8_gemm(Fp8GemmArgs& g, const clearmoe_fp8* A, const clearmoe_fp8* W, int E, int num_sms, cudaStream_t s);

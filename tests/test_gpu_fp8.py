@@ -145,6 +145,54 @@ def test_gemm(M, N, K, dtype):
     assert torch.equal(dense, out[:M, :N])  # every store width gives the same values
 
 
+KERNELS = [(256, 1), (192, 1), (128, 1), (192, 0), (128, 0), (64, 0), (32, 0)]
+
+
+@pytest.fixture
+def kernel(request):
+    cm.clearmoe_debug_fp8_kernel(*request.param)
+    yield request.param
+    cm.clearmoe_debug_fp8_kernel()
+
+
+@pytest.mark.parametrize("kernel", KERNELS, indirect=True)
+@pytest.mark.parametrize("M,N,K,act", [(700, 700, 1300, cm.ACT_GELU), (5, 40, 130, cm.ACT_NONE), (257, 300, 512, cm.ACT_RELU),
+                                       (40000, 200, 100, cm.ACT_NONE)])
+def test_every_kernel(kernel, M, N, K, act):
+    """Each tile width on one SM and on pairs: sums, both stores, 8-bit outputs where the kernel has them."""
+    rng = np.random.default_rng(M + N)
+    A, W, av, wv = make(rng, M, N, K)
+    bias = dev(rng.standard_normal(N) * 0.1)
+    y, err = reference(av, wv, bias, act)
+    for dtype in (torch.float32, torch.bfloat16):
+        out = torch.full((M, N), float("nan"), device="cuda", dtype=dtype)
+        cm.clearmoe_fp8_gemm(A, W, out, bias=bias, act=act)
+        assert bool(((out.double() - y).abs() <= err + (2.0 ** -8 * y.abs() if dtype == torch.bfloat16 else 0)).all())
+    if kernel[0] % 128 == 0:
+        q, got = cm.fp8_rows(M, N), torch.empty(M, N, device="cuda")
+        cm.clearmoe_fp8_gemm(A, W, q, bias=bias, act=act)
+        cm.clearmoe_fp8_dequantize(q, got)
+        amax = torch.nn.functional.pad(y.abs(), (0, -N % 128)).view(M, -1, 128).amax(2).repeat_interleave(128, 1)[:, :N]
+        assert bool(((got.double() - y).abs() <= 1.07 * err + 2.0 ** -4 * y.abs() + 2.0 ** -10 * 2 * amax / 448 * 1.01).all())
+
+
+@pytest.mark.parametrize("kernel", KERNELS, indirect=True)
+def test_every_kernel_grouped(kernel):
+    rng = np.random.default_rng(77)
+    counts, N, K = [0, 300, 1, 0, 129, 700], 320, 640
+    M, off = sum(counts), np.concatenate([[0], np.cumsum(counts)])
+    A, _, av, _ = make(rng, M, N, K)
+    pairs = [make(rng, 1, N, K)[1::2] for _ in counts]
+    perm = rng.permutation(M)
+    out = torch.full((M, N), float("nan"), device="cuda")
+    cm.clearmoe_fp8_grouped_gemm(A, [p[0] for p in pairs], torch.tensor(off, dtype=torch.int32, device="cuda"), out,
+                                 perm=torch.tensor(perm, dtype=torch.int32, device="cuda"))
+    for e in range(len(counts)):
+        sl = slice(int(off[e]), int(off[e + 1]))
+        y, err = reference(av[sl], pairs[e][1], None, cm.ACT_NONE)
+        assert bool(((out[torch.tensor(perm[sl], device="cuda", dtype=torch.long)].double() - y).abs() <= err).all())
+
+
 @pytest.mark.parametrize("M,N,K", [(1, 128, 128), (130, 768, 192), (77, 200, 300), (4000, 1536, 384), (9, 1, 5)])
 def test_gemm_to_blocks(M, N, K):
     rng = np.random.default_rng(M + N + K)
@@ -299,6 +347,8 @@ def test_refusals():
     assert grp(A.ref, arr, 0, off.data_ptr(), None, None, o, cm.F32, 8, None) == cm.EINVAL
     assert grp(A.ref, arr, 17, off.data_ptr(), None, None, o, cm.F32, 8, None) == cm.EINVAL
     assert grp(A.ref, arr, 1, None, None, None, o, cm.F32, 8, None) == cm.EINVAL
+    for k in ((256, 0), (64, 1), (100, 0), (0, 1), (128, 2)):
+        assert L.clearmoe_debug_fp8_kernel(*k) == cm.EINVAL
     with pytest.raises(ValueError):
         cm.clearmoe_fp8_quantize_rows(x[:, ::2], cm.fp8_rows(4, 128))
     with pytest.raises(ValueError):
