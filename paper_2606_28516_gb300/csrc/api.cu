@@ -1418,8 +1418,8 @@ int clearmoe_ffn_forward_few(clearmoe_layer* L, const void* x, int64_t T, const 
     return cuda_fail(cm::launch_few(a, static_cast<cudaStream_t>(stream)));
 }
 
-// The layer in 8-bit blocks: routing and slots as the other forwards (with the LayerNorm's statistics ahead),
-// x quantised in expert order, fc1 with bias, GELU and the next quantisation in its epilogue, the grouped
+// The layer in 8-bit blocks: routing as the other forwards (with the LayerNorm's statistics ahead), x quantised to the
+// slots in the kernel that forms them, fc1 with bias, GELU and the next quantisation in its epilogue, the grouped
 // product scattered back to token order.
 int clearmoe_ffn_forward_fp8(clearmoe_layer* L, const void* x, int64_t T, const clearmoe_ffn_weights* w, void* out,
                              void* stream) {
@@ -1433,7 +1433,6 @@ int clearmoe_ffn_forward_fp8(clearmoe_layer* L, const void* x, int64_t T, const 
     const bool ln = w->input_layernorm != 0;
     if (ln && (rc = ln_prep(L, x, T, nullptr, w->router.W, w->E, s))) return rc;
     if ((rc = do_route(L, x, T, &w->router, nullptr, w->E, w->cls_stride, s, ln))) return rc;
-    if ((rc = do_finalize(L, s))) return rc;
     const Fp8Workspace ws = fp8_workspace(L, T);
     cm::QuantArgs q;
     std::memset(&q, 0, sizeof(q));
@@ -1442,13 +1441,12 @@ int clearmoe_ffn_forward_fp8(clearmoe_layer* L, const void* x, int64_t T, const 
     q.rows = T;
     q.K = d;
     q.kb = (d + 127) / 128;
-    q.gather = L->perm;
     q.ln_stats = ln ? L->ln_stats : nullptr;
     q.q = static_cast<uint8_t*>(ws.x.q);
     q.scale = ws.x.scale;
     q.ldq = cm::fp8_ldq(d);
     q.lds = cm::fp8_lds(d);
-    if ((rc = cuda_fail(cm::launch_quantize_rows(q, CLEARMOE_BF16, L->num_sms, s)))) return rc;
+    if ((rc = cuda_fail(cm::launch_slots_quantize(L->rt, L->rt_grid, L->rt_chunk, q, L->num_sms, s)))) return rc;
     cm::Fp8GemmArgs g;
     std::memset(&g, 0, sizeof(g));
     g.status = L->status;

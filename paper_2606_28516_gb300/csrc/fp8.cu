@@ -56,18 +56,51 @@ __device__ __forceinline__ void load8(const T* row, int64_t k, int64_t K, float 
 constexpr int Q_THREADS = 256;
 constexpr int Q_UNITS = 2;
 constexpr int Q_CTA_BLOCKS = Q_THREADS / 8;
+constexpr int Q_PITCH = 132;
 
-template <typename T, bool VEC, bool LN>
+// A lane's 16 values of a block: through the LayerNorm (LN: st of its row), to e4m3 at q, the block's scale byte at scale.
+template <bool LN>
+__device__ __forceinline__ void quantize_block(float (&v)[2][8], float2 st, int64_t k, int64_t K, int l8, bool write, uint8_t* q,
+                                               uint8_t* scale) {
+    if (LN) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int c = 0; c < 8; ++c) v[h][c] = k + 8 * h + c < K ? (v[h][c] - st.x) * st.y : 0.f;
+    }
+    float m = 0.f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int c = 0; c < 8; c += 2) m = max_abs3(m, v[h][c], v[h][c + 1]);
+#pragma unroll
+    for (int o = 4; o; o >>= 1) m = max_abs(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+    const uint32_t s = fp8_scale_byte(abs_bits(m));
+    const float inv = fp8_inverse_scale(s);
+    uint32_t o[4];
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+        const float* f = v[h >> 1] + (h & 1) * 4;
+        o[h] = fp8_pack4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv);
+    }
+    if (write) {
+        *reinterpret_cast<uint4*>(q) = make_uint4(o[0], o[1], o[2], o[3]);
+        if (l8 == 0) *scale = (uint8_t)s;
+    }
+}
+
+template <typename T, bool VEC>
 __global__ void __launch_bounds__(Q_THREADS) quantize_rows_kernel(const QuantArgs a) {
+    // rows that are not 16-byte aligned go through shared memory, so that a load's lanes read consecutive elements
+    __shared__ __align__(16) float s_x[VEC ? 1 : Q_THREADS / 32][VEC ? 1 : 4 * Q_PITCH];
     pdl_launch_dependents();
-    const int l8 = threadIdx.x & 7;
+    const int l8 = threadIdx.x & 7, lane = threadIdx.x & 31;
     const int64_t blocks = a.rows * a.kb;
     const bool narrow = blocks <= 0xFFFFFFFFll;
     pdl_wait();
     for (int64_t b0 = (int64_t)blockIdx.x * (Q_CTA_BLOCKS * Q_UNITS) + (threadIdx.x >> 3);
          b0 - (int)(threadIdx.x >> 3) < blocks; b0 += (int64_t)gridDim.x * (Q_CTA_BLOCKS * Q_UNITS)) {
         float v[Q_UNITS][2][8];
-        float2 st[Q_UNITS];
         int64_t row[Q_UNITS];
         int kb[Q_UNITS];
 #pragma unroll
@@ -77,40 +110,150 @@ __global__ void __launch_bounds__(Q_THREADS) quantize_rows_kernel(const QuantArg
             kb[i] = (int)(b - row[i] * a.kb);
             const int64_t src = a.gather ? (int64_t)__ldcg(a.gather + row[i]) : row[i];
             const T* x = static_cast<const T*>(a.x) + src * a.ld;
-            load8<T, VEC>(x, (int64_t)kb[i] * 128 + l8 * 16, a.K, v[i][0]);
-            load8<T, VEC>(x, (int64_t)kb[i] * 128 + l8 * 16 + 8, a.K, v[i][1]);
-            if (LN) st[i] = __ldcg(a.ln_stats + src);
+            if (VEC) {
+                load8<T, VEC>(x, (int64_t)kb[i] * 128 + l8 * 16, a.K, v[i][0]);
+                load8<T, VEC>(x, (int64_t)kb[i] * 128 + l8 * 16 + 8, a.K, v[i][1]);
+            } else {
+                float* sx = s_x[VEC ? 0 : threadIdx.x >> 5];
+                float f[16];
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {  // the warp's four blocks
+                    const T* p = reinterpret_cast<const T*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(x), 8 * b));
+                    const int64_t k = (int64_t)__shfl_sync(0xFFFFFFFFu, kb[i], 8 * b) * 128 + lane;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        f[4 * b + c] = k + 32 * c >= a.K  ? 0.f
+                                       : sizeof(T) == 2 ? bf16_to_f32(__ldcg(reinterpret_cast<const uint16_t*>(p) + k + 32 * c))
+                                                        : __ldcg(reinterpret_cast<const float*>(p) + k + 32 * c);
+                }
+                __syncwarp();
+#pragma unroll
+                for (int c = 0; c < 16; ++c) sx[(c >> 2) * Q_PITCH + (c & 3) * 32 + lane] = f[c];
+                __syncwarp();
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const float4 q = *reinterpret_cast<const float4*>(sx + (lane >> 3) * Q_PITCH + l8 * 16 + 4 * c);
+                    float* o = v[i][c >> 1] + (c & 1) * 4;
+                    o[0] = q.x, o[1] = q.y, o[2] = q.z, o[3] = q.w;
+                }
+            }
         }
 #pragma unroll
         for (int i = 0; i < Q_UNITS; ++i) {
             const int64_t k = (int64_t)kb[i] * 128 + l8 * 16;
-            if (LN) {
+            quantize_block<false>(v[i], make_float2(0.f, 1.f), k, a.K, l8, b0 + i * Q_CTA_BLOCKS < blocks, a.q + row[i] * a.ldq + k,
+                               a.scale + row[i] * a.lds + kb[i]);
+        }
+    }
+}
+
+// The routing's slots and the tokens quantised to them in one launch (a token's row goes to its slot): CTA (c, part)
+// takes every SPLIT-th row of routing range c. As route_finalize_kernel it forms the ranges' prefix from their
+// histograms and writes counts, offsets and perm.
+constexpr int SQ_THREADS = 512;
+constexpr int SQ_ROWS = 256;  // rows at a time
+
+template <bool LN>
+__global__ void __launch_bounds__(SQ_THREADS) slots_quantize_kernel(const RouteArgs r, const int chunk, const int G, const QuantArgs a) {
+    __shared__ int s_before[SQ_THREADS / 32][CM_MAX_E], s_total[SQ_THREADS / 32][CM_MAX_E], s_base[CM_MAX_E];
+    __shared__ int s_slot[SQ_ROWS];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, E = r.E, split = gridDim.y;
+    const int64_t row0 = (int64_t)blockIdx.x * chunk;
+    const int64_t rows = max((int64_t)0, min((int64_t)chunk, r.T - row0));
+    const int64_t n_cls = n_class_tokens(r.T, r.cls_stride);
+    pdl_launch_dependents();
+    pdl_wait();  // everything below reads the routing kernel's output
+    int before[CM_MAX_E], total[CM_MAX_E];
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+    for (int e = 0; e < CM_MAX_E; ++e) before[e] = total[e] = 0;
+    for (int b = tid; b < G; b += SQ_THREADS) {
+        const int4* h = reinterpret_cast<const int4*>(r.cta_counts + (int64_t)b * CM_MAX_E);
 #pragma unroll
-                    for (int c = 0; c < 8; ++c)
-                        v[i][h][c] = k + 8 * h + c < a.K ? (v[i][h][c] - st[i].x) * st[i].y : 0.f;
-            }
-            float m = 0.f;
+        for (int q = 0; q < CM_MAX_E / 4; ++q) {
+            if (4 * q >= E) break;
+            const int4 v = __ldcg(h + q);
+            const int c[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int c = 0; c < 8; ++c) m = max_abs(m, v[i][h][c]);
-#pragma unroll
-            for (int o = 4; o; o >>= 1) m = max_abs(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-            const uint32_t s = fp8_scale_byte(abs_bits(m));
-            const float inv = fp8_inverse_scale(s);
-            uint32_t o[4];
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                const float* f = v[i][h >> 1] + (h & 1) * 4;
-                o[h] = fp8_pack4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv);
-            }
-            if (b0 + i * Q_CTA_BLOCKS < blocks) {
-                *reinterpret_cast<uint4*>(a.q + row[i] * a.ldq + k) = make_uint4(o[0], o[1], o[2], o[3]);
-                if (l8 == 0) a.scale[row[i] * a.lds + kb[i]] = (uint8_t)s;
+            for (int i = 0; i < 4; ++i) {
+                total[4 * q + i] += c[i];
+                if (b < (int)blockIdx.x) before[4 * q + i] += c[i];
             }
         }
+    }
+    if (warp * 32 < G) {
+#pragma unroll
+        for (int e = 0; e < CM_MAX_E; ++e) {
+            if (e >= E) break;
+            const int vb = __reduce_add_sync(0xFFFFFFFFu, before[e]), vt = __reduce_add_sync(0xFFFFFFFFu, total[e]);
+            if (lane == 0) s_before[warp][e] = vb, s_total[warp][e] = vt;
+        }
+    }
+    __syncthreads();
+    if (warp == 0) {
+        int b = 0, t = 0;
+        if (lane < E)
+            for (int w = 0; w * 32 < G && w < SQ_THREADS / 32; ++w) b += s_before[w][lane], t += s_total[w][lane];
+        int incl = t;  // over experts
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+            if (lane >= o) incl += v;
+        }
+        if (lane < E) {
+            s_base[lane] = incl - t + b;
+            if (blockIdx.x == 0 && blockIdx.y == 0) {
+                r.counts[lane] = t;
+                r.offsets[lane] = incl - t;
+                if (lane == E - 1) {
+                    r.offsets[E] = incl;
+                    if (n_cls > 0) r.counts[E] = (int32_t)n_cls, r.offsets[E + 1] = incl + (int32_t)n_cls;
+                }
+            }
+        }
+    }
+    __syncthreads();
+    const int l8 = tid & 7, per = SQ_THREADS / 8;  // blocks at a time
+    for (int64_t i0 = blockIdx.y; i0 < rows; i0 += (int64_t)SQ_ROWS * split) {  // rows i0, i0 + split, ..
+        const int n = (int)min((int64_t)SQ_ROWS, (rows - i0 + split - 1) / split);
+        for (int i = tid; i < n; i += SQ_THREADS) {
+            const int64_t tok = row0 + i0 + (int64_t)i * split;
+            int64_t slot;
+            if (r.cls_stride > 0 && tok % r.cls_stride == 0) {
+                slot = r.T - n_cls + tok / r.cls_stride;
+            } else {
+                const uint32_t w = (uint32_t)__ldcg(r.tinfo + tok);
+                const int e = (int)(w & 0xFFu);
+                slot = e < E ? (int64_t)s_base[e] + (int)(w >> 8) : -1;  // -1: only a routing that gave up leaves such words
+                if ((uint64_t)slot >= (uint64_t)r.T) slot = -1;
+            }
+            s_slot[i] = (int)slot;
+            if (slot >= 0) r.perm[slot] = (int32_t)tok;
+        }
+        __syncthreads();
+        const int blocks = n * a.kb;
+        for (int b0 = tid >> 3; b0 - (tid >> 3) < blocks; b0 += Q_UNITS * per) {
+            float v[Q_UNITS][2][8];
+            float2 st[Q_UNITS];
+            int row[Q_UNITS], kb[Q_UNITS];
+#pragma unroll
+            for (int i = 0; i < Q_UNITS; ++i) {
+                const int b = min(b0 + i * per, blocks - 1);  // past the end: the last block again
+                row[i] = (int)((uint32_t)b / (uint32_t)a.kb);
+                kb[i] = b - row[i] * a.kb;
+                const int64_t tok = row0 + i0 + (int64_t)row[i] * split;
+                const uint16_t* x = static_cast<const uint16_t*>(a.x) + tok * a.ld;
+                load8<uint16_t, true>(x, kb[i] * 128 + l8 * 16, a.K, v[i][0]);
+                load8<uint16_t, true>(x, kb[i] * 128 + l8 * 16 + 8, a.K, v[i][1]);
+                if (LN) st[i] = __ldcg(a.ln_stats + tok);
+            }
+#pragma unroll
+            for (int i = 0; i < Q_UNITS; ++i) {
+                const int k = kb[i] * 128 + l8 * 16, slot = s_slot[row[i]];
+                quantize_block<LN>(v[i], st[i], k, a.K, l8, b0 + i * per < blocks && slot >= 0, a.q + (int64_t)slot * a.ldq + k,
+                                   a.scale + (int64_t)slot * a.lds + kb[i]);
+            }
+        }
+        __syncthreads();
     }
 }
 
@@ -171,9 +314,9 @@ __global__ void __launch_bounds__(256)
 }
 
 template <typename K, typename... A>
-cudaError_t launch(K kernel, int64_t grid, int threads, cudaStream_t s, A... args) {
+cudaError_t launch(K kernel, dim3 grid, int threads, cudaStream_t s, A... args) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(threads);
     cfg.stream = s;
     cudaLaunchAttribute at[1];
@@ -196,14 +339,20 @@ cudaError_t launch_quantize_rows(const QuantArgs& a, int dtype, int num_sms, cud
     const int64_t grid = want < (int64_t)num_sms * 8 ? want : (int64_t)num_sms * 8;
     const bool vec = vec_ok(a, esz);
     if (dtype == CLEARMOE_BF16) {
-        if (a.ln_stats)
-            return vec ? launch(quantize_rows_kernel<uint16_t, true, true>, grid, Q_THREADS, s, a)
-                       : cudaErrorInvalidValue;  // the layer's rows are always aligned
-        return vec ? launch(quantize_rows_kernel<uint16_t, true, false>, grid, Q_THREADS, s, a)
-                   : launch(quantize_rows_kernel<uint16_t, false, false>, grid, Q_THREADS, s, a);
+        return vec ? launch(quantize_rows_kernel<uint16_t, true>, dim3((unsigned)grid), Q_THREADS, s, a)
+                   : launch(quantize_rows_kernel<uint16_t, false>, dim3((unsigned)grid), Q_THREADS, s, a);
     }
-    return vec ? launch(quantize_rows_kernel<float, true, false>, grid, Q_THREADS, s, a)
-               : launch(quantize_rows_kernel<float, false, false>, grid, Q_THREADS, s, a);
+    return vec ? launch(quantize_rows_kernel<float, true>, dim3((unsigned)grid), Q_THREADS, s, a)
+               : launch(quantize_rows_kernel<float, false>, dim3((unsigned)grid), Q_THREADS, s, a);
+}
+
+cudaError_t launch_slots_quantize(const RouteArgs& r, int grid, int chunk, const QuantArgs& a, int num_sms, cudaStream_t s) {
+    // as many CTAs as two an SM, while each keeps rows for its threads
+    int split = 1;
+    while (split < 8 && grid * split * 2 <= 2 * num_sms && chunk >= 2 * split * SQ_THREADS / 8 / a.kb) split *= 2;
+    const dim3 g(grid, split);
+    return a.ln_stats ? launch(slots_quantize_kernel<true>, g, SQ_THREADS, s, r, chunk, grid, a)
+                      : launch(slots_quantize_kernel<false>, g, SQ_THREADS, s, r, chunk, grid, a);
 }
 
 cudaError_t launch_quantize_weight(const QuantArgs& a, int dtype, cudaStream_t s) {
@@ -211,10 +360,10 @@ cudaError_t launch_quantize_weight(const QuantArgs& a, int dtype, cudaStream_t s
     const int64_t grid = (a.rows + 127) / 128 * a.kb;
     const bool vec = vec_ok(a, esz);
     if (dtype == CLEARMOE_BF16)
-        return vec ? launch(quantize_weight_kernel<uint16_t, true>, grid, 256, s, a)
-                   : launch(quantize_weight_kernel<uint16_t, false>, grid, 256, s, a);
-    return vec ? launch(quantize_weight_kernel<float, true>, grid, 256, s, a)
-               : launch(quantize_weight_kernel<float, false>, grid, 256, s, a);
+        return vec ? launch(quantize_weight_kernel<uint16_t, true>, dim3((unsigned)grid), 256, s, a)
+                   : launch(quantize_weight_kernel<uint16_t, false>, dim3((unsigned)grid), 256, s, a);
+    return vec ? launch(quantize_weight_kernel<float, true>, dim3((unsigned)grid), 256, s, a)
+               : launch(quantize_weight_kernel<float, false>, dim3((unsigned)grid), 256, s, a);
 }
 
 }  // namespace cm
@@ -298,9 +447,9 @@ int clearmoe_fp8_dequantize(const clearmoe_fp8* in, int32_t block_rows, void* ou
     const uint8_t* q = static_cast<const uint8_t*>(in->q);
     const int64_t ldq = fp8_ldq(in->cols), lds = fp8_lds(in->cols);
     if (dtype == CLEARMOE_BF16)
-        return cuda_code(cm::launch(cm::dequantize_kernel<uint16_t>, grid, 256, s, q, (const uint8_t*)in->scale, in->rows,
+        return cuda_code(cm::launch(cm::dequantize_kernel<uint16_t>, dim3((unsigned)grid), 256, s, q, (const uint8_t*)in->scale, in->rows,
                                     in->cols, ldq, lds, (int)block_rows, static_cast<uint16_t*>(out), ld));
-    return cuda_code(cm::launch(cm::dequantize_kernel<float>, grid, 256, s, q, (const uint8_t*)in->scale, in->rows,
+    return cuda_code(cm::launch(cm::dequantize_kernel<float>, dim3((unsigned)grid), 256, s, q, (const uint8_t*)in->scale, in->rows,
                                 in->cols, ldq, lds, (int)block_rows, static_cast<float*>(out), ld));
 }
 

@@ -9,7 +9,7 @@
 // rows of scales in global memory are padded to whole words, which are moved as they lie.
 //
 // One persistent, warp-specialised kernel per N tile width:
-//   warps 0-7    epilogue: warp w reads TMEM lane quarter w % 4 (its 32 rows) and column half w / 4;
+//   warps 0-7    epilogue: warp w reads TMEM lane quarter w % 4 (its 32 rows) and every other 32 columns;
 //   warps 8-9    scales: load the words of the tile's rows and of W's blocks and lay them out in shared memory;
 //   warp 10      TMEM allocation, tcgen05.cp of the scales, tcgen05.mma and commits (the whole warp in step, one
 //                elected lane issues);
@@ -44,15 +44,13 @@ struct F8Cfg {
     static constexpr int A_BYTES = F8_BM * F8_BK, B_BYTES = BN * F8_BK;
     static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
     static constexpr int STAGES = (200 * 1024 / STAGE_BYTES) < 8 ? (200 * 1024 / STAGE_BYTES) : 8;
-    static constexpr int HALF = BN / 2;                    // columns per epilogue warp
-    static constexpr int CW = HALF < 32 ? HALF : 32;       // columns per TMEM read
     static constexpr int NBARS = 2 * STAGES + 2 * F8_SLOTS + 4 + 1 + 4;
     static constexpr int SF_COL = 2 * BN;                  // first scale column
     static constexpr int SF_COLS = f8_slot_cols(BN), SF_BYTES = f8_slot_bytes(BN);
     static constexpr int TMEM_USED = 2 * BN + 2 * SF_COLS;
     static constexpr int TMEM_COLS = TMEM_USED <= 128 ? 128 : TMEM_USED <= 256 ? 256 : 512;
     static_assert(TMEM_USED <= 512);
-    // bias of a chunk per epilogue warp, largest magnitudes of a row's halves, group prefixes
+    // scales, bias of a chunk per epilogue warp, largest magnitudes of a row's halves, group prefixes
     static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + F8_SLOTS * SF_BYTES + F8_NUM_EPI * 32 * 4 + 2 * F8_NUM_EPI * 32 * 4 + NBARS * 8 + 16 +
                                 8 * (CM_MAX_E + 1);
 };
@@ -77,7 +75,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
     unsigned char* sm = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     unsigned char* s_sf = sm + C::STAGES * C::STAGE_BYTES;                       // [slot]
     float* s_bias = reinterpret_cast<float*>(s_sf + F8_SLOTS * C::SF_BYTES);     // [epilogue warp][32]
-    uint32_t* s_amax = reinterpret_cast<uint32_t*>(s_bias + F8_NUM_EPI * 32);   // [2][epilogue warp][32]
+    float* s_amax = s_bias + F8_NUM_EPI * 32;                                    // [2][epilogue warp][32]
     uint64_t* bars = reinterpret_cast<uint64_t*>(s_amax + 2 * F8_NUM_EPI * 32);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::NBARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -224,138 +222,88 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
                           });
     } else {
         // ------------------------------------------------ epilogue
-        constexpr int CW = C::CW, HALF = C::HALF;
+        // warp w takes 32-column chunks w / 4, w / 4 + 2, .. of the tile (a 32-wide tile's only chunk: warps 0-3)
+        constexpr int ROUNDS = (BN + 63) / 64;
         const int quarter = warp & 3, half = warp >> 2;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         float* bias_line = s_bias + warp * 32;
         const bool has_bias = a.bias != nullptr;
         const int esz = KIND == FP8_OUT_BF16 ? 2 : 4;
         // rows of the output in whole 32-byte pieces
-        const bool wide = KIND == FP8_OUT_FP8 ||
-                          ((reinterpret_cast<uintptr_t>(a.out) & 31) == 0 && (a.ldo * esz & 31) == 0);
+        const bool wide = (reinterpret_cast<uintptr_t>(a.out) & 31) == 0 && (a.ldo * esz & 31) == 0;
         int acc = 0;
         uint32_t aph = 0, pph = 0;
         for (; t.live(); t.next()) {
-            const int64_t m = t.m0 + quarter * 32 + lane;
+            const int m = t.m0 + quarter * 32 + lane;
             const bool live = m < t.hi;
-            const int64_t orow = live ? (a.rows ? (int64_t)__ldcg(a.rows + m) : m) : 0;
+            const int orow = live ? (a.rows ? __ldcg(a.rows + m) : m) : -1;
+            float b[ROUNDS];
+#pragma unroll
+            for (int r = 0; r < ROUNDS; ++r) {
+                const int n = t.n0 + (2 * r + half) * 32 + lane;
+                b[r] = 0.f;
+                if (has_bias && n < a.N)
+                    b[r] = a.bias_bf16 ? bf16_to_f32(__ldg(static_cast<const uint16_t*>(a.bias) + n))
+                                       : __ldg(static_cast<const float*>(a.bias) + n);
+            }
             if (!mbar_wait_warp(tfull_bar(acc), aph, abort_flag, a.status, lim)) break;
             tc_fence_after();
-            const uint32_t d = tmem + lanes + acc * BN + half * HALF;
-            if constexpr (KIND == FP8_OUT_FP8) {
-                // The tile's 128 columns are one block: each of the quarter's two warps holds 64 of a row, and they
-                // exchange the row's largest magnitudes.
-                static_assert(KIND != FP8_OUT_FP8 || BN == 128);
-                float v[HALF];
-                uint32_t mx = 0;
+            const uint32_t d = tmem + lanes + acc * BN;
+            float v[ROUNDS][32];
+            float mx = 0.f;
 #pragma unroll
-                for (int c = 0; c < HALF / 32; ++c) {
-                    uint32_t r[32];
-                    CM_TMEM_LD_X32(d + c * 32, r);
-                    const int n = t.n0 + half * HALF + c * 32 + lane;
-                    __syncwarp();
-                    if (has_bias)
-                        bias_line[lane] = n >= a.N ? 0.f
-                                          : a.bias_bf16 ? bf16_to_f32(static_cast<const uint16_t*>(a.bias)[n])
-                                                        : static_cast<const float*>(a.bias)[n];
-                    __syncwarp();
+            for (int r = 0; r < ROUNDS; ++r) {
+                const bool mine = (2 * r + half) * 32 < BN;
+                const int nc = t.n0 + (2 * r + half) * 32;
+                __syncwarp();  // the bias line is read, rows without a store have caught up
+                if (mine) {
+                    uint32_t u[32];
+                    CM_TMEM_LD_X32(d + (2 * r + half) * 32, u);
+                    if (has_bias) bias_line[lane] = b[r];
                     tmem_wait_ld();
-                    float f[32];
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(r[i]);
-                    f8_act<32, false>(f, bias_line, has_bias, a.act);
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        if (t.n0 + half * HALF + c * 32 + i >= a.N) f[i] = 0.f;
-                        v[c * 32 + i] = f[i];
-                        mx = max(mx, abs_bits(f[i]));
-                    }
+                    for (int i = 0; i < 32; ++i) v[r][i] = __uint_as_float(u[i]);
                 }
-                tc_fence_before();
+                if (r + 1 == ROUNDS) {  // the accumulator is read: the next tile's MMAs may start
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(tempty_bar(acc));
+                }
                 __syncwarp();
-                if (lane == 0) mbar_arrive(tempty_bar(acc));
-                // double-buffered by tile: a warp's read of one tile's value precedes its arrival for the next
-                // tile, and that the other warp's write two tiles on
-                uint32_t* ex = s_amax + acc * F8_NUM_EPI * 32;
+                if (!mine) continue;
+                f8_act<32, KIND == FP8_OUT_F32>(v[r], bias_line, has_bias, a.act);
+                if constexpr (KIND == FP8_OUT_FP8) {
+                    if (nc + 32 > a.N) {  // the last block's padding is zero
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (nc + i >= a.N) v[r][i] = 0.f;
+                    }
+                    mx = max_abs(mx, f8_max_abs32(v[r]));
+                } else {
+                    f8_store32<KIND>(a, v[r], orow, nc, wide, lane);
+                }
+            }
+            if constexpr (KIND == FP8_OUT_FP8) {
+                // The tile's 128 columns are one block: each of the quarter's two warps holds 64 of a row, and they exchange
+                // the row's largest magnitudes. Double-buffered by tile: a warp's read of one tile's value precedes its
+                // arrival for the next tile, and that the other warp's write two tiles on.
+                static_assert(BN == 128);
+                float* ex = s_amax + acc * F8_NUM_EPI * 32;
                 ex[warp * 32 + lane] = mx;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(pair_bar(quarter));
                 if (!mbar_wait_warp(pair_bar(quarter), pph, abort_flag, a.status, lim)) break;
                 pph ^= 1;
-                mx = max(mx, ex[(warp ^ 4) * 32 + lane]);
-                const uint32_t s = fp8_scale_byte(mx);
-                const float inv = fp8_inverse_scale(s);
+                const uint32_t s = fp8_scale_byte(abs_bits(max_abs(mx, ex[(warp ^ 4) * 32 + lane])));
                 if (live) {
-                    uint8_t* q = static_cast<uint8_t*>(a.out) + orow * a.ldo + t.n0 + half * HALF;
+                    uint8_t* q = static_cast<uint8_t*>(a.out) + (int64_t)orow * a.ldo + t.n0 + half * 32;
 #pragma unroll
-                    for (int c = 0; c < HALF / 32; ++c) {
+                    for (int r = 0; r < ROUNDS; ++r) {
                         uint32_t o[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            o[i] = fp8_pack4(v[c * 32 + 4 * i] * inv, v[c * 32 + 4 * i + 1] * inv, v[c * 32 + 4 * i + 2] * inv,
-                                             v[c * 32 + 4 * i + 3] * inv);
-                        st_global_32(q + c * 32, o);
+                        fp8_pack32(o, v[r], fp8_inverse_scale(s));
+                        st_global_32(q + 64 * r, o);
                     }
-                    if (half == 0) a.out_scale[orow * a.ldos + t.n0 / 128] = (uint8_t)s;
-                }
-            } else {
-#pragma unroll 1
-                for (int c = 0; c < HALF / CW; ++c) {
-                    uint32_t r[CW];
-                    __syncwarp();  // rows past the group's end skip the stores below
-                    if constexpr (CW == 32)
-                        CM_TMEM_LD_X32(d + c * CW, r);
-                    else
-                        CM_TMEM_LD_X16(d + c * CW, r);
-                    const int nc = t.n0 + half * HALF + c * CW;
-                    __syncwarp();
-                    if (has_bias && lane < CW)
-                        bias_line[lane] = nc + lane >= a.N ? 0.f
-                                          : a.bias_bf16 ? bf16_to_f32(static_cast<const uint16_t*>(a.bias)[nc + lane])
-                                                        : static_cast<const float*>(a.bias)[nc + lane];
-                    __syncwarp();
-                    tmem_wait_ld();
-                    if (c + 1 == HALF / CW) {  // the accumulator is read: the next tile's MMAs may start
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(tempty_bar(acc));
-                    }
-                    float v[CW];
-#pragma unroll
-                    for (int i = 0; i < CW; ++i) v[i] = __uint_as_float(r[i]);
-                    f8_act<CW, KIND == FP8_OUT_F32>(v, bias_line, has_bias, a.act);
-                    if (!live) continue;
-                    if constexpr (KIND == FP8_OUT_BF16) {
-                        uint16_t* o = static_cast<uint16_t*>(a.out) + orow * a.ldo + nc;
-                        if (wide && nc + CW <= a.N) {
-#pragma unroll
-                            for (int p = 0; p < CW / 16; ++p) {
-                                uint32_t w[8];
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) w[i] = pack_bf16(v[16 * p + 2 * i], v[16 * p + 2 * i + 1]);
-                                st_global_32(o + 16 * p, w);
-                            }
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < CW; ++i)
-                                if (nc + i < a.N) o[i] = f32_to_bf16(v[i]);
-                        }
-                    } else {
-                        float* o = static_cast<float*>(a.out) + orow * a.ldo + nc;
-                        if (wide && nc + CW <= a.N) {
-#pragma unroll
-                            for (int p = 0; p < CW / 8; ++p) {
-                                uint32_t w[8];
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[8 * p + i]);
-                                st_global_32(o + 8 * p, w);
-                            }
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < CW; ++i)
-                                if (nc + i < a.N) o[i] = v[i];
-                        }
-                    }
+                    if (half == 0) a.out_scale[(int64_t)orow * a.ldos + t.n0 / 128] = (uint8_t)s;
                 }
             }
             if (++acc == 2) {
@@ -395,30 +343,42 @@ cudaError_t launch_kind(const Fp8GemmArgs& a, int num_sms, cudaStream_t s) {
 
 }  // namespace
 
-// Cycles a product takes on kernel `k`, from what bounds each: rounds of tiles, each of which multiplies (2 BN cycles a
-// k-block on one SM's 128 rows), loads its operands (64 bytes a cycle and SM) or runs its epilogue, and the last
-// epilogue, which nothing hides.
-static double fp8_cost(const Fp8Pick& k, int64_t M, int N, int nkb, int out_kind, int groups, int num_sms) {
-    const int rows = k.pair ? 256 : 128, units = k.pair ? num_sms / 2 : num_sms;
-    if (units < 1) return 1e30;
-    const int64_t tiles = ((M + rows - 1) / rows + groups - 1) * (((int64_t)N + k.bn - 1) / k.bn);
-    const double rounds = (double)((tiles + units - 1) / units);
-    const double loads = 2.0 * (128 + (k.pair ? k.bn / 2 : k.bn));
-    const double block = loads > 2.0 * k.bn ? loads : 2.0 * k.bn;
-    const double epi = (out_kind == FP8_OUT_FP8 ? 14.0 : 8.0) * k.bn, main = block * nkb;
-    return rounds * (main > epi ? main : epi) + epi;
+// Cycles (at 1.9 GHz) a product takes on a kernel: its start, then rounds of tiles, each of which multiplies and loads its
+// k-blocks or, where that is longer, runs the epilogue of the tile before it, then the last epilogue. A k-block's cycles
+// grow from what the MMAs take (2 a column, 285 at the least) to what the path from L2 allows with every SM at work.
+// Fitted to measurements (us, the best two of seven kernels and this rule's choice, at M x N x K): 197 x 3,072 x 768
+// 3.9 (64 wide, one SM) and 4.5 (128), 3.9; 1,000 x 384 x 1,536 4.6 (32) and 4.8 (64), 4.6; 4,000 x 1,024 x 1,024 7.1
+// (128) and 8.4 (128, pair), 7.1; 9,973 x 384 x 1,536 9.0 (128) and 9.8 (128, pair), 9.0; 25,216 x 768 x 3,072 38.9
+// (256, pair) and 44.7 (192, pair), 38.9; 16,384 x 4,096 x 4,096 144 (256, pair) and 158 (192, pair), 144.
+struct Fp8Kernel {
+    Fp8Pick pick;
+    int block;     // cycles of a k-block with every SM at work
+    int epilogue;  // of a tile beside the next tile's MMAs: bf16 and fp32 outputs
+    int quantize;  // 8-bit outputs (0: none)
+};
+static double fp8_cost(const Fp8Kernel& k, int64_t M, int N, int nkb, int out_kind, int groups, int num_sms) {
+    const bool pair = k.pick.pair, q = out_kind == FP8_OUT_FP8;
+    const int bn = k.pick.bn, rows = pair ? 256 : 128, units = pair ? num_sms / 2 : num_sms;
+    if (units < 1 || (q && !k.quantize)) return 1e30;
+    const int64_t tiles = ((M + rows - 1) / rows + groups - 1) * (((int64_t)N + bn - 1) / bn);
+    const double rounds = (double)((tiles + units - 1) / units), busy = tiles < units ? (double)tiles / units : 1.0;
+    const double low = 2 * bn > 285 ? 2 * bn : 285, main = nkb * (low + (k.block - low) * busy * busy);
+    const double beside = q ? k.quantize : k.epilogue, between = bn == 256 ? 1500 : 0;  // 256: accumulators that overlap
+    const double next = main + between > beside ? main + between : beside;
+    return (pair ? 8800 : 4600) + main + (rounds - 1) * next + (q ? beside : 15.0 * bn);
 }
 
 Fp8Pick fp8_pick(int64_t M, int N, int nkb, int out_kind, int groups, int num_sms) {
-    static const Fp8Pick all[] = {{256, 1}, {192, 1}, {128, 1}, {192, 0}, {128, 0}, {64, 0}, {32, 0}};
-    Fp8Pick best = {128, 0};
+    static const Fp8Kernel all[] = {{{256, 1}, 540, 3072, 7900}, {{192, 1}, 550, 2304, 0}, {{128, 1}, 487, 1536, 4430},
+                                    {{192, 0}, 588, 2304, 0},    {{128, 0}, 445, 1536, 5070}, {{64, 0}, 350, 768, 0},
+                                    {{32, 0}, 285, 384, 0}};
+    Fp8Pick best = all[4].pick;
     double least = 1e30;
-    for (const Fp8Pick& k : all) {
-        if (out_kind == FP8_OUT_FP8 && k.bn % 128) continue;  // whole scale blocks
+    for (const Fp8Kernel& k : all) {
         const double c = fp8_cost(k, M, N, nkb, out_kind, groups, num_sms);
         if (c < least) {
             least = c;
-            best = k;
+            best = k.pick;
         }
     }
     return best;

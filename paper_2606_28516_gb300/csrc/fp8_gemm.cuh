@@ -167,6 +167,65 @@ __device__ __forceinline__ void st_global_32(void* p, const uint32_t (&v)[8]) {
                  : "memory");
 }
 
+// v[i] of lane r becomes v[r] of lane i: a 32 x 32 transposition across the warp.
+__device__ __forceinline__ void f8_transpose(float (&v)[32], int lane) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        const bool up = lane & o;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            if (i & o) continue;
+            const float send = up ? v[i] : v[i + o];
+            const float got = __shfl_xor_sync(0xFFFFFFFFu, send, o);
+            if (up)
+                v[i] = got;
+            else
+                v[i + o] = got;
+        }
+    }
+}
+
+// 32 rows' 32 columns [nc, nc + 32) (one row a lane: its output row, or -1) to out, fp32 or bf16. Rows in whole 32-byte
+// pieces (wide) are stored as each lane has them; others transposed first, so that a store's lanes write consecutive
+// columns of one row (an element a lane, rows apart, took 9.8 us for 1,001 x 777 x 1,131 where this takes ODD_US).
+template <int KIND>
+__device__ __forceinline__ void f8_store32(const Fp8GemmArgs& a, float (&v)[32], int row, int nc, bool wide, int lane) {
+    if (wide && nc + 32 <= a.N) {
+        if (row < 0) return;
+        if constexpr (KIND == FP8_OUT_BF16) {
+            uint16_t* o = static_cast<uint16_t*>(a.out) + (int64_t)row * a.ldo + nc;
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                uint32_t w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = pack_bf16(v[16 * p + 2 * i], v[16 * p + 2 * i + 1]);
+                st_global_32(o + 16 * p, w);
+            }
+        } else {
+            float* o = static_cast<float*>(a.out) + (int64_t)row * a.ldo + nc;
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                uint32_t w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[8 * p + i]);
+                st_global_32(o + 8 * p, w);
+            }
+        }
+        return;
+    }
+    __syncwarp();
+    f8_transpose(v, lane);
+#pragma unroll
+    for (int r = 0; r < 32; ++r) {
+        const int64_t orow = __shfl_sync(0xFFFFFFFFu, row, r);
+        if (orow < 0 || nc + lane >= a.N) continue;
+        if constexpr (KIND == FP8_OUT_BF16)
+            static_cast<uint16_t*>(a.out)[orow * a.ldo + nc + lane] = f32_to_bf16(v[r]);
+        else
+            static_cast<float*>(a.out)[orow * a.ldo + nc + lane] = v[r];
+    }
+}
+
 // gelu_pair_bf16 with max(u, 0) taken directly, two operations a pair less: -inf gives 0, GELU's limit, instead of NaN.
 // The epilogue of 8-bit outputs is bound by its instructions.
 __device__ __forceinline__ float2 gelu_pair_fp8(float2 u) {

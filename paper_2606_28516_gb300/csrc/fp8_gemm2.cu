@@ -408,39 +408,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
                 const int nc = n0 + chunk[r] * 32;
                 if (mine) {
                     f8_act<32, KIND == FP8_OUT_F32>(v, bias_line, has_bias, a.act);
-                    if (live) {
-                        if constexpr (KIND == FP8_OUT_BF16) {
-                            uint16_t* o = static_cast<uint16_t*>(a.out) + (int64_t)orow * a.ldo + nc;
-                            if (wide && nc + 32 <= a.N) {
-#pragma unroll
-                                for (int p = 0; p < 2; ++p) {
-                                    uint32_t w[8];
-#pragma unroll
-                                    for (int i = 0; i < 8; ++i) w[i] = pack_bf16(v[16 * p + 2 * i], v[16 * p + 2 * i + 1]);
-                                    st_global_32(o + 16 * p, w);
-                                }
-                            } else {
-#pragma unroll
-                                for (int i = 0; i < 32; ++i)
-                                    if (nc + i < a.N) o[i] = f32_to_bf16(v[i]);
-                            }
-                        } else {
-                            float* o = static_cast<float*>(a.out) + (int64_t)orow * a.ldo + nc;
-                            if (wide && nc + 32 <= a.N) {
-#pragma unroll
-                                for (int p = 0; p < 4; ++p) {
-                                    uint32_t w[8];
-#pragma unroll
-                                    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[8 * p + i]);
-                                    st_global_32(o + 8 * p, w);
-                                }
-                            } else {
-#pragma unroll
-                                for (int i = 0; i < 32; ++i)
-                                    if (nc + i < a.N) o[i] = v[i];
-                            }
-                        }
-                    }
+                    f8_store32<KIND>(a, v, live ? orow : -1, nc, wide, lane);
                 }
             }
             }

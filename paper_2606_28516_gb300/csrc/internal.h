@@ -305,12 +305,15 @@ struct QuantArgs {
     int64_t rows, K;
     int kb;  // blocks of 128 columns per row
     const int32_t* gather;  // source row of row i (nullable)
-    const float2* ln_stats;  // rows: (mean, rstd) per source row, applied first (nullable; bf16 rows)
+    const float2* ln_stats;  // launch_slots_quantize: (mean, rstd) per token, applied first (nullable)
     uint8_t* q;
     uint8_t* scale;
     int64_t ldq, lds;
 };
 cudaError_t launch_quantize_rows(const QuantArgs& a, int dtype, int num_sms, cudaStream_t s);
+// The slots of a routing launch (its grid and chunk; counts, offsets and perm as launch_route_finalize, not inv) and the
+// bf16 tokens quantised to them.
+cudaError_t launch_slots_quantize(const RouteArgs& r, int grid, int chunk, const QuantArgs& a, int num_sms, cudaStream_t s);
 cudaError_t launch_quantize_weight(const QuantArgs& a, int dtype, cudaStream_t s);
 
 enum Fp8Out { FP8_OUT_F32 = 0, FP8_OUT_BF16 = 1, FP8_OUT_FP8 = 2 };
