@@ -154,7 +154,7 @@ constexpr int SQ_THREADS = 512;
 constexpr int SQ_ROWS = 256;  // rows at a time
 
 template <bool LN>
-__global__ void __launch_bounds__(SQ_THREADS) slots_quantize_kernel(const RouteArgs r, const int chunk, const int G, const QuantArgs a) {
+__global__ void __launch_bounds__(SQ_THREADS, 2) slots_quantize_kernel(const RouteArgs r, const int chunk, const int G, const QuantArgs a) {
     __shared__ int s_before[SQ_THREADS / 32][CM_MAX_E], s_total[SQ_THREADS / 32][CM_MAX_E], s_base[CM_MAX_E];
     __shared__ int s_slot[SQ_ROWS];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, E = r.E, split = gridDim.y;

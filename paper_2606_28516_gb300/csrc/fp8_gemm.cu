@@ -424,6 +424,7 @@ int run_fp8_gemm(Fp8GemmArgs& g, const clearmoe_fp8* A, const clearmoe_fp8* W, i
     // rows of bytes as rows of half as many 16-bit elements: boxes of 64 of them are 128 bytes
     const int64_t cols16 = fp8_ldq(A->cols) / 2;
     if (encode_tmap_bf16(&g.tmA, A->q, A->rows, cols16, F8_BM)) return CLEARMOE_ECUDA;
+    if (g.out_kind == FP8_OUT_FP8 && k.pair && encode_tmap_bf16(&g.tmOut, g.out, g.M, g.ldo / 2, 32)) return CLEARMOE_ECUDA;
     for (int e = 0; e < E; ++e) {
         g.sb[e] = W[e].scale;
         if (encode_tmap_bf16(&g.tmB[e], W[e].q, W[e].rows, cols16, k.pair ? k.bn / 2 : k.bn)) return CLEARMOE_ECUDA;

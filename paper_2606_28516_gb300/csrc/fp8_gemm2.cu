@@ -347,6 +347,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
                             if (nc + i >= a.N) v[r][i] = 0.f;
                     }
                     ex[(r * P8_NUM_EPI + warp) * 32 + lane] = f8_max_abs32(v[r]);
+                    if (r == 0 && cg == 0) bulk_wait_read();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(pair_bar(quarter * C::ROUNDS + r));
                 }
@@ -369,22 +370,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
                     if (cg == 0 && live && nc < a.ldo) a.out_scale[(int64_t)(m0 + trow) * a.ldos + nc / 128] = (uint8_t)s;
                 }
                 if (!ok) break;
+                fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(pair_bar(4 * C::ROUNDS + quarter));
-                if (!mbar_wait_warp(pair_bar(4 * C::ROUNDS + quarter), pph, abort_flag, a.status, lim)) break;
-                // whole 128-byte rows of a block, four a store: rows 8 cg .. 8 cg + 7 of the quarter are this warp's. (One row a
-                // lane, 32 bytes of it at a time, took 53 us where this takes STORE_US, 19,456 x 3,072 x 768.)
+                // The quarter's rows as boxes of 32 rows x 128 bytes, by its first warp, which lets them be read before it
+                // arrives for the next tile's exchange, and so before any warp writes there again. (Copied out by the
+                // warps, whole lines or 32 bytes a lane, the stores cost 0.75 us a tile; so COPY_US.)
+                if (cg == 0) {
+                    if (!mbar_wait_warp(pair_bar(4 * C::ROUNDS + quarter), pph, abort_flag, a.status, lim)) break;
 #pragma unroll
-                for (int r = 0; r < C::ROUNDS; ++r) {
-                    const int blk = chunk[r] >> 2;
-                    if (n0 + blk * 128 >= a.ldo) continue;
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int trow = quarter * 32 + cg * 8 + h * 4 + (lane >> 3);
-                        const uint4 w = *reinterpret_cast<const uint4*>(s_out + (blk * P8_BM + trow) * 128 + (((lane & 7) ^ (trow & 7)) << 4));
-                        if (m0 + trow < hi)
-                            *reinterpret_cast<uint4*>(static_cast<uint8_t*>(a.out) + (int64_t)(m0 + trow) * a.ldo + n0 + blk * 128 + ((lane & 7) << 4)) = w;
-                    }
+                    for (int blk = 0; blk < C::ROUNDS; ++blk)
+                        if (n0 + blk * 128 < a.ldo)
+                            tma_store_2d(&a.tmOut, smem_u32(s_out + (blk * P8_BM + quarter * 32) * 128), (n0 + blk * 128) / 2,
+                                         m0 + quarter * 32);
+                    bulk_commit();
                 }
                 // the exchange of the next tile uses the other half: a warp's reads of this one precede its arrivals for
                 // the next, and those the other warps' writes two tiles on
@@ -418,6 +417,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
             }
         }
     }
+    if (KIND == FP8_OUT_FP8 && warp < 4) bulk_wait_all();  // the stores read this CTA's shared memory
     tc_fence_before();
     __syncthreads();
     cluster_sync();  // no copy, commit or remote arrival is left in flight towards either CTA
