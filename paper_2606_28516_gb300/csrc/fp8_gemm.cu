@@ -234,9 +234,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
         int acc = 0;
         uint32_t aph = 0, pph = 0;
         for (; t.live(); t.next()) {
-            const int m = t.m0 + quarter * 32 + lane;
-            const bool live = m < t.hi;
-            const int orow = live ? (a.rows ? __ldcg(a.rows + m) : m) : -1;
+            const int orow = f8_out_row(a, t.m0 + quarter * 32 + lane, t.hi);
             float b[ROUNDS];
 #pragma unroll
             for (int r = 0; r < ROUNDS; ++r) {
@@ -295,7 +293,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
                 if (!mbar_wait_warp(pair_bar(quarter), pph, abort_flag, a.status, lim)) break;
                 pph ^= 1;
                 const uint32_t s = fp8_scale_byte(abs_bits(max_abs(mx, ex[(warp ^ 4) * 32 + lane])));
-                if (live) {
+                if (orow >= 0) {
                     uint8_t* q = static_cast<uint8_t*>(a.out) + (int64_t)orow * a.ldo + t.n0 + half * 32;
 #pragma unroll
                     for (int r = 0; r < ROUNDS; ++r) {
@@ -312,7 +310,9 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
             }
         }
     }
+    tc_fence_before();
     __syncthreads();
+    tc_fence_after();
     if (warp == F8_WARP_MMA) tmem_dealloc(tmem, C::TMEM_COLS);
 }
 

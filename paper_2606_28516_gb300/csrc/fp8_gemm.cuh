@@ -43,10 +43,16 @@ __device__ __forceinline__ void tmem_cp_scales(uint32_t tmem, uint32_t smem) {
         : "r"(taddr))
 
 
-// Row boundaries of the groups and the row tiles before each, in shared memory: off[E + 1], prefix[E + 1].
+// Row boundaries of the groups and the row tiles before each, in shared memory: off[E + 1], prefix[E + 1]. Held to
+// ascend within the rows: after a routing that gave up they may be an earlier call's.
 __device__ __forceinline__ void f8_groups(const Fp8GemmArgs& a, int bm, int* off, int* prefix) {
     int acc = 0;
-    for (int e = 0; e <= a.E; ++e) off[e] = a.offsets ? __ldcg(a.offsets + e) : (e == 0 ? 0 : (int)a.M);
+    for (int e = 0; e <= a.E; ++e) {
+        const int v = a.offsets ? __ldcg(a.offsets + e) : (e == 0 ? 0 : (int)a.M);
+        off[e] = min(max(v, acc), (int)a.M);
+        acc = off[e];
+    }
+    acc = 0;
     for (int e = 0; e < a.E; ++e) {
         prefix[e] = acc;
         acc += (off[e + 1] - off[e] + bm - 1) / bm;
@@ -87,6 +93,14 @@ struct F8Walk {
         n0 = nt * bn;
     }
 };
+
+// The output row of row m of A (-1: none). An index outside the output, of a routing that gave up, is no row.
+__device__ __forceinline__ int f8_out_row(const Fp8GemmArgs& a, int m, int hi) {
+    if (m >= hi) return -1;
+    if (!a.rows) return m;
+    const int r = __ldcg(a.rows + m);
+    return (uint32_t)r < (uint32_t)a.M ? r : -1;
+}
 
 // The scale words of one 512-column chunk as a lane of the scale warp holds them: rows 32 j + lane of the CTA's 128
 // rows of A, and those of W's blocks (columns n0 + 32 j of the tile lie in one block of 128 rows). Tensor memory
@@ -130,7 +144,8 @@ constexpr int F8_AHEAD = 2;
 // The work of scale warp `which` of F8_SCALE_WARPS: the words of every F8_SCALE_WARPS-th 512-column chunk of the CTA's
 // tiles, in order, each handed to put(words, slot, phase), false when it gave up. Two warps, because a chunk takes a
 // warp over a microsecond from the free slot to the arrival (loads that wait behind the queued tile loads, the fence
-// between the proxies): one warp 93 us, two TWO_US, four 83 us for 19,456 x 1,792 x 4,096 in 256 x 256 tiles.
+// between the proxies): one warp 93 us, four 83, two
+// 83 for 19,456 x 1,792 x 4,096 in 256 x 256 tiles.
 // F8_AHEAD chunks' loads are in flight; a set of registers is loaded again as soon as its words are stored (a set
 // moved to another would wait for its loads).
 template <int BN, class Put>
@@ -187,7 +202,7 @@ __device__ __forceinline__ void f8_transpose(float (&v)[32], int lane) {
 
 // 32 rows' 32 columns [nc, nc + 32) (one row a lane: its output row, or -1) to out, fp32 or bf16. Rows in whole 32-byte
 // pieces (wide) are stored as each lane has them; others transposed first, so that a store's lanes write consecutive
-// columns of one row (an element a lane, rows apart, took 9.8 us for 1,001 x 777 x 1,131 where this takes ODD_US).
+// columns of one row (an element a lane, rows apart, took 9.8 us for 1,001 x 777 x 1,131 where this takes 5.7).
 template <int KIND>
 __device__ __forceinline__ void f8_store32(const Fp8GemmArgs& a, float (&v)[32], int row, int nc, bool wide, int lane) {
     if (wide && nc + 32 <= a.N) {
