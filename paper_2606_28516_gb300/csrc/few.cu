@@ -198,13 +198,21 @@ __global__ void __launch_bounds__(FEW_THREADS, CTAS) few_fc1_kernel(const __grid
     }
 }
 
-// A tile's product for tokens s_tok[0 .. n), n <= 8 NT, into their output rows.
-template <int V, int NT, int CTAS>
+// A tile's product for tokens s_tok[0 .. n), n <= 8 NT, into their output rows. early: the weights of its first steps,
+// already asked for (HAVE of them).
+constexpr int FEW_EARLY = 4;
+template <int V, int NT, int CTAS, int HAVE>
 __device__ __forceinline__ void few_expert(const FewArgs& a, int e, int r0, const int* s_tok, int n, float* red, const uint8_t* s_scale,
-                                           int warp, int lane) {
+                                           const uint4 (&early)[2][FEW_EARLY], int warp, int lane) {
     FewTile<V, NT, CTAS> t;
     t.set_weights(a.Wc[e], few_pitch<V>(a.H), r0, a.d, a.H);
-    t.start_w();
+#pragma unroll
+    for (int d = 0; d < FewT<V, NT, CTAS>::DW; ++d) {
+        if (d < HAVE)
+            t.a[d] = early[0][d], t.b[d] = early[1][d];
+        else
+            t.load_w(d, d);
+    }
     float acc[NT][4], sums[4];
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
@@ -227,8 +235,9 @@ __device__ __forceinline__ void few_expert(const FewArgs& a, int e, int r0, cons
 }
 
 // One CTA per 16 output rows and group, NT token tiles at most at a time; more tokens than that go through in turns, the
-// weights then coming from L2.
-template <int V, int NT, int CTAS>
+// weights then coming from L2. GUESS (as many tokens as groups or more): the first weights are asked for before the
+// routing is known, beside fc1, as if the group had tokens.
+template <int V, int NT, int CTAS, bool GUESS>
 __global__ void __launch_bounds__(FEW_THREADS, CTAS) few_expert_kernel(const __grid_constant__ FewArgs a) {
     extern __shared__ float red[];  // the partial sums; then the scale bytes
     __shared__ int s_tok[CLEARMOE_FEW_MAX];
@@ -237,6 +246,18 @@ __global__ void __launch_bounds__(FEW_THREADS, CTAS) few_expert_kernel(const __g
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int e = blockIdx.y, r0 = blockIdx.x * 16;
+    // the steps that every width of the product starts with
+    constexpr int HAVE = !GUESS ? 0 : FewT<V, NT, CTAS>::DW < FEW_EARLY ? FewT<V, NT, CTAS>::DW : FEW_EARLY;
+    uint4 early[2][FEW_EARLY];
+    if (GUESS) {
+        FewTile<V, 1, CTAS> t;
+        t.set_weights(a.Wc[e], few_pitch<V>(a.H), r0, a.d, a.H);
+#pragma unroll
+        for (int d = 0; d < HAVE; ++d) {
+            t.load_w(d, d);
+            early[0][d] = t.a[d], early[1][d] = t.b[d];
+        }
+    }
     few_scales<V>(s_scale, a.Wc_s[e], r0, a.H);
     pdl_wait();
     if (warp == 0) {  // the group's tokens in order, two a lane; their number before it
@@ -259,15 +280,18 @@ __global__ void __launch_bounds__(FEW_THREADS, CTAS) few_expert_kernel(const __g
         }
     }
     __syncthreads();
-    for (int m0 = 0; m0 < s_n; m0 += 8 * NT) {
-        const int n = min(8 * NT, s_n - m0);
-        if (NT == 1 || n <= 8)
-            few_expert<V, 1, CTAS>(a, e, r0, s_tok + m0, n, red, s_scale, warp, lane);
-        else if (NT == 2 || n <= 16)
-            few_expert<V, NT < 2 ? NT : 2, CTAS>(a, e, r0, s_tok + m0, n, red, s_scale, warp, lane);
-        else
-            few_expert<V, NT, CTAS>(a, e, r0, s_tok + m0, n, red, s_scale, warp, lane);
+    int n = min(8 * NT, s_n);
+    if (n == 0) return;
+    if (NT == 1 || n <= 8)
+        few_expert<V, 1, CTAS, HAVE>(a, e, r0, s_tok, n, red, s_scale, early, warp, lane);
+    else if (NT == 2 || n <= 16)
+        few_expert<V, NT < 2 ? NT : 2, CTAS, HAVE>(a, e, r0, s_tok, n, red, s_scale, early, warp, lane);
+    else
+        few_expert<V, NT, CTAS, HAVE>(a, e, r0, s_tok, n, red, s_scale, early, warp, lane);
+    for (int m0 = 8 * NT; m0 < s_n; m0 += 8 * NT) {
         __syncthreads();  // red is read
+        n = min(8 * NT, s_n - m0);
+        few_expert<V, NT, CTAS, 0>(a, e, r0, s_tok + m0, n, red, s_scale, early, warp, lane);
     }
 }
 
@@ -299,7 +323,8 @@ template <int V, int NT, int CTAS>
 cudaError_t few_experts(const FewArgs& a, cudaStream_t s) {
     const dim3 grid((a.d + 15) / 16, a.G);
     const int smem = FewT<V, NT, CTAS>::SMEM + (V == FEWV_W8A16 ? (a.H + 127) / 128 : 0);
-    return few_launch(few_expert_kernel<V, NT, CTAS>, grid, smem, s, a);
+    return a.T >= a.G ? few_launch(few_expert_kernel<V, NT, CTAS, true>, grid, smem, s, a)
+                      : few_launch(few_expert_kernel<V, NT, CTAS, false>, grid, smem, s, a);
 }
 
 template <int V>

@@ -9,11 +9,12 @@
 // rows of scales in global memory are padded to whole words, which are moved as they lie.
 //
 // One persistent, warp-specialised kernel per N tile width:
-//   warps 0-7    epilogue: warp w reads TMEM lane quarter w % 4 (its 32 rows) and every other 32 columns;
-//   warps 8-9    scales: load the words of the tile's rows and of W's blocks and lay them out in shared memory;
-//   warp 10      TMEM allocation, tcgen05.cp of the scales, tcgen05.mma and commits (the whole warp in step, one
+//   epilogue     8 warps, 16 for tiles of 128 columns or more: warp w reads TMEM lane quarter w % 4 (its 32 rows) and
+//                32 columns at a time;
+//   2 warps      scales: load the words of the tile's rows and of W's blocks and lay them out in shared memory;
+//   1 warp       TMEM allocation, tcgen05.cp of the scales, tcgen05.mma and commits (the whole warp in step, one
 //                elected lane issues);
-//   warp 11      TMA producer of the q tiles: 128 rows of A and BN of W, 128 bytes each, 128-byte swizzle.
+//   1 warp       TMA producer of the q tiles: 128 rows of A and BN of W, 128 bytes each, 128-byte swizzle.
 // Rings: q stages in shared memory (full: TMA bytes, empty: commit), scale slots (full: the scale
 // warp's arrival, empty: commit), two accumulators. Grouped products walk (group, row tile, column
 // tile) from the device-resident offsets; a row tile never crosses its group's end.
@@ -32,15 +33,15 @@ namespace cm {
 
 namespace {
 
-constexpr int F8_NUM_EPI = 8;
-constexpr int F8_WARP_SCALE = 8, F8_WARP_MMA = 10, F8_WARP_TMA = 11;
-constexpr int F8_THREADS = 32 * 12;
 constexpr int F8_BM = 128;
 constexpr int F8_BK = 128;
 
 template <int BN_>
 struct F8Cfg {
     static constexpr int BN = BN_;
+    static constexpr int NUM_EPI = BN >= 128 ? 16 : 8, SPAN = NUM_EPI / 4;  // warps per lane quarter
+    static constexpr int WARP_SCALE = NUM_EPI, WARP_MMA = NUM_EPI + 2, WARP_TMA = NUM_EPI + 3;
+    static constexpr int THREADS = 32 * (NUM_EPI + 4);
     static constexpr int A_BYTES = F8_BM * F8_BK, B_BYTES = BN * F8_BK;
     static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
     static constexpr int STAGES = (200 * 1024 / STAGE_BYTES) < 8 ? (200 * 1024 / STAGE_BYTES) : 8;
@@ -51,7 +52,7 @@ struct F8Cfg {
     static constexpr int TMEM_COLS = TMEM_USED <= 128 ? 128 : TMEM_USED <= 256 ? 256 : 512;
     static_assert(TMEM_USED <= 512);
     // scales, bias of a chunk per epilogue warp, largest magnitudes of a row's halves, group prefixes
-    static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + F8_SLOTS * SF_BYTES + F8_NUM_EPI * 32 * 4 + 2 * F8_NUM_EPI * 32 * 4 + NBARS * 8 + 16 +
+    static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + F8_SLOTS * SF_BYTES + NUM_EPI * 32 * 4 + 2 * NUM_EPI * 32 * 4 + NBARS * 8 + 16 +
                                 8 * (CM_MAX_E + 1);
 };
 
@@ -68,15 +69,15 @@ __device__ __forceinline__ void umma_mxf8(uint32_t d_tmem, uint64_t a_desc, uint
 }
 // KIND: Fp8Out.
 template <int BN_, int KIND>
-__global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_constant__ Fp8GemmArgs a) {
+__global__ void __launch_bounds__(F8Cfg<BN_>::THREADS, 1) fp8_gemm_kernel(const __grid_constant__ Fp8GemmArgs a) {
     using C = F8Cfg<BN_>;
     constexpr int BN = C::BN;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* sm = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     unsigned char* s_sf = sm + C::STAGES * C::STAGE_BYTES;                       // [slot]
     float* s_bias = reinterpret_cast<float*>(s_sf + F8_SLOTS * C::SF_BYTES);     // [epilogue warp][32]
-    float* s_amax = s_bias + F8_NUM_EPI * 32;                                    // [2][epilogue warp][32]
-    uint64_t* bars = reinterpret_cast<uint64_t*>(s_amax + 2 * F8_NUM_EPI * 32);
+    float* s_amax = s_bias + C::NUM_EPI * 32;                                    // [2][epilogue warp][32]
+    uint64_t* bars = reinterpret_cast<uint64_t*>(s_amax + 2 * C::NUM_EPI * 32);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::NBARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     int* s_prefix = reinterpret_cast<int*>(tmem_slot + 4);  // [E + 1]
@@ -106,14 +107,14 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(tfull_bar(i), 1);
-            mbar_init(tempty_bar(i), F8_NUM_EPI);
+            mbar_init(tempty_bar(i), C::NUM_EPI);
         }
         mbar_init(drain_bar, 1);
-        for (int q = 0; q < 4; ++q) mbar_init(pair_bar(q), 2);
+        for (int q = 0; q < 4; ++q) mbar_init(pair_bar(q), C::SPAN);
         *abort_flag = 0;
         mbar_fence_init();
     }
-    if (warp == F8_WARP_MMA) tmem_alloc(smem_u32(tmem_slot), C::TMEM_COLS);
+    if (warp == C::WARP_MMA) tmem_alloc(smem_u32(tmem_slot), C::TMEM_COLS);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -126,7 +127,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
     F8Walk t(blockIdx.x, gridDim.x, a.N, F8_BM, BN, a.E, s_off, s_prefix);
     const int nkb = a.nkb;
 
-    if (warp == F8_WARP_TMA) {
+    if (warp == C::WARP_TMA) {
         // ------------------------------------------------ TMA producer
         int stage = 0;
         uint32_t ph = 0, issued = 0, par = 0;  // bit s: stage s has had a load; parity of its last
@@ -154,7 +155,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
         // let every copy in flight land before the CTA retires, whoever gave up
         for (int s = 0; s < C::STAGES; ++s)
             if (issued & (1u << s)) mbar_wait_warp(full_bar(s), (par >> s) & 1, nullptr, a.status, lim + 10000000ull);
-    } else if (warp == F8_WARP_MMA) {
+    } else if (warp == C::WARP_MMA) {
         // ------------------------------------------------ MMA issuer
         int stage = 0, slot = 0, acc = 0;
         uint32_t ph = 0, sph = 0, aph = 0;
@@ -209,9 +210,9 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
         }
         umma_commit(drain_bar);  // every MMA issued above has completed once this fires
         mbar_wait_warp(drain_bar, 0, nullptr, a.status, lim + 10000000ull);
-    } else if (warp >= F8_WARP_SCALE) {
+    } else if (warp >= C::WARP_SCALE) {
         // ------------------------------------------------ scales
-        f8_scale_warp<BN>(a, warp - F8_WARP_SCALE, t, 0, lane,
+        f8_scale_warp<BN>(a, warp - C::WARP_SCALE, t, 0, lane,
                           [&](const F8Scales<BN>& w, int slot, uint32_t ph) {
                               if (!mbar_wait_warp(sempty_bar(slot), ph ^ 1, abort_flag, a.status, lim)) return false;
                               w.store(s_sf + slot * C::SF_BYTES, lane);
@@ -222,9 +223,9 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
                           });
     } else {
         // ------------------------------------------------ epilogue
-        // warp w takes 32-column chunks w / 4, w / 4 + 2, .. of the tile (a 32-wide tile's only chunk: warps 0-3)
-        constexpr int ROUNDS = (BN + 63) / 64;
-        const int quarter = warp & 3, half = warp >> 2;
+        // warp w takes 32-column chunks w / 4, w / 4 + SPAN, .. of the tile (a 32-wide tile's only chunk: warps 0-3)
+        constexpr int SPAN = C::SPAN, ROUNDS = (BN / 32 + SPAN - 1) / SPAN;
+        const int quarter = warp & 3, cg = warp >> 2;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         float* bias_line = s_bias + warp * 32;
         const bool has_bias = a.bias != nullptr;
@@ -238,7 +239,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
             float b[ROUNDS];
 #pragma unroll
             for (int r = 0; r < ROUNDS; ++r) {
-                const int n = t.n0 + (2 * r + half) * 32 + lane;
+                const int n = t.n0 + (SPAN * r + cg) * 32 + lane;
                 b[r] = 0.f;
                 if (has_bias && n < a.N)
                     b[r] = a.bias_bf16 ? bf16_to_f32(__ldg(static_cast<const uint16_t*>(a.bias) + n))
@@ -251,12 +252,12 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
             float mx = 0.f;
 #pragma unroll
             for (int r = 0; r < ROUNDS; ++r) {
-                const bool mine = (2 * r + half) * 32 < BN;
-                const int nc = t.n0 + (2 * r + half) * 32;
+                const bool mine = (SPAN * r + cg) * 32 < BN;
+                const int nc = t.n0 + (SPAN * r + cg) * 32;
                 __syncwarp();  // the bias line is read, rows without a store have caught up
                 if (mine) {
                     uint32_t u[32];
-                    CM_TMEM_LD_X32(d + (2 * r + half) * 32, u);
+                    CM_TMEM_LD_X32(d + (SPAN * r + cg) * 32, u);
                     if (has_bias) bias_line[lane] = b[r];
                     tmem_wait_ld();
 #pragma unroll
@@ -282,26 +283,23 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
                 }
             }
             if constexpr (KIND == FP8_OUT_FP8) {
-                // The tile's 128 columns are one block: each of the quarter's two warps holds 64 of a row, and they exchange
-                // the row's largest magnitudes. Double-buffered by tile: a warp's read of one tile's value precedes its
-                // arrival for the next tile, and that the other warp's write two tiles on.
-                static_assert(BN == 128);
-                float* ex = s_amax + acc * F8_NUM_EPI * 32;
+                // The tile's 128 columns are one block: each of the quarter's four warps holds 32 of a row, and they exchange
+                // the row's largest magnitudes. Double-buffered by tile: a warp's reads of one tile's values precede its
+                // arrival for the next tile, and that the other warps' writes two tiles on.
+                static_assert(BN == 128 && ROUNDS == 1);
+                float* ex = s_amax + acc * C::NUM_EPI * 32;
                 ex[warp * 32 + lane] = mx;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(pair_bar(quarter));
                 if (!mbar_wait_warp(pair_bar(quarter), pph, abort_flag, a.status, lim)) break;
                 pph ^= 1;
-                const uint32_t s = fp8_scale_byte(abs_bits(max_abs(mx, ex[(warp ^ 4) * 32 + lane])));
+                const float* e = ex + quarter * 32 + lane;
+                const uint32_t s = fp8_scale_byte(abs_bits(max_abs3(max_abs(e[0], e[4 * 32]), e[8 * 32], e[12 * 32])));
                 if (orow >= 0) {
-                    uint8_t* q = static_cast<uint8_t*>(a.out) + (int64_t)orow * a.ldo + t.n0 + half * 32;
-#pragma unroll
-                    for (int r = 0; r < ROUNDS; ++r) {
-                        uint32_t o[8];
-                        fp8_pack32(o, v[r], fp8_inverse_scale(s));
-                        st_global_32(q + 64 * r, o);
-                    }
-                    if (half == 0) a.out_scale[(int64_t)orow * a.ldos + t.n0 / 128] = (uint8_t)s;
+                    uint32_t o[8];
+                    fp8_pack32(o, v[0], fp8_inverse_scale(s));
+                    st_global_32(static_cast<uint8_t*>(a.out) + (int64_t)orow * a.ldo + t.n0 + cg * 32, o);
+                    if (cg == 0) a.out_scale[(int64_t)orow * a.ldos + t.n0 / 128] = (uint8_t)s;
                 }
             }
             if (++acc == 2) {
@@ -313,7 +311,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) fp8_gemm_kernel(const __grid_co
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == F8_WARP_MMA) tmem_dealloc(tmem, C::TMEM_COLS);
+    if (warp == C::WARP_MMA) tmem_dealloc(tmem, C::TMEM_COLS);
 }
 
 template <int BN, int KIND>
@@ -325,7 +323,7 @@ cudaError_t launch_bn(const Fp8GemmArgs& a, int num_sms, cudaStream_t s) {
     const int64_t tiles = m_tiles * ((a.N + BN - 1) / BN);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(tiles < num_sms ? tiles : num_sms));
-    cfg.blockDim = dim3(F8_THREADS);
+    cfg.blockDim = dim3(C::THREADS);
     cfg.dynamicSmemBytes = C::SMEM;
     cfg.stream = s;
     cudaLaunchAttribute at[1];
@@ -370,7 +368,7 @@ static double fp8_cost(const Fp8Kernel& k, int64_t M, int N, int nkb, int out_ki
 
 Fp8Pick fp8_pick(int64_t M, int N, int nkb, int out_kind, int groups, int num_sms) {
     static const Fp8Kernel all[] = {{{256, 1}, 540, 3072, 7900}, {{192, 1}, 550, 2304, 0}, {{128, 1}, 487, 1536, 4430},
-                                    {{192, 0}, 588, 2304, 0},    {{128, 0}, 445, 1536, 5070}, {{64, 0}, 350, 768, 0},
+                                    {{192, 0}, 588, 2304, 0},    {{128, 0}, 445, 1536, 4200}, {{64, 0}, 350, 768, 0},
                                     {{32, 0}, 285, 384, 0}};
     Fp8Pick best = all[4].pick;
     double least = 1e30;
