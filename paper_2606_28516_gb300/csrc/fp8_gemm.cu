@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(F8Cfg<BN_>::THREADS, 1) fp8_gemm_kernel(const 
                     break;
                 }
                 const uint32_t sA = smem_u32(sm + stage * C::STAGE_BYTES);
-                mbar_arrive_expect_tx_warp(full_bar(stage), C::STAGE_BYTES);
+                mbar_arrive_expect_tx_warp(full_bar(stage), a.box_rows * F8_BK + C::B_BYTES);
                 // coordinates in the maps' 16-bit elements: two bytes each
                 tma_load_2d(sA, &a.tmA, kb * (F8_BK / 2), m0, full_bar(stage));
                 tma_load_2d(sA + C::A_BYTES, &a.tmB[e], kb * (F8_BK / 2), n0, full_bar(stage));
@@ -405,8 +405,11 @@ int run_fp8_gemm(Fp8GemmArgs& g, const clearmoe_fp8* A, const clearmoe_fp8* W, i
     g.lds = fp8_lds(A->cols);
     g.sa = A->scale;
     const int forced = g_forced.load(std::memory_order_relaxed);
-    if (!g.offsets && g.out_kind != FP8_OUT_FP8 && g.M <= FP8_FEW_MAX && (g.M + 1) * g.nkb <= FP8_FEW_SCALES &&
-        (forced == 0 || forced == FP8_FORCE_FEW)) {
+    // Few rows, while the SMs take all CTAs of 16 columns at once: us against the best tcgen05 tile, 1 x 4,096 x 4,096 5.1 / 7.5,
+    // 12 x 4,096 x 4,096 7.1 / 7.6, 12 x 768 x 3,072 4.6 / 6.1; more CTAs than that: 12 x 8,192 x 1,024 5.7 / 4.0, 8 x 8,192 x
+    // 8,192 19.5 / 14.8.
+    const bool few_fits = !g.offsets && g.out_kind != FP8_OUT_FP8 && g.M <= FP8_FEW_MAX && (g.M + 1) * g.nkb <= FP8_FEW_SCALES;
+    if (few_fits && (forced == FP8_FORCE_FEW || (forced == 0 && (g.N + 15) / 16 <= 2 * num_sms))) {
         g.x = A->q;
         g.w = W->q;
         g.sb[0] = W->scale;
@@ -421,7 +424,11 @@ int run_fp8_gemm(Fp8GemmArgs& g, const clearmoe_fp8* A, const clearmoe_fp8* W, i
     }
     // rows of bytes as rows of half as many 16-bit elements: boxes of 64 of them are 128 bytes
     const int64_t cols16 = fp8_ldq(A->cols) / 2;
-    if (encode_tmap_bf16(&g.tmA, A->q, A->rows, cols16, F8_BM)) return CLEARMOE_ECUDA;
+    // One SM, fewer rows than a tile: a box of those alone. The copy engine takes longer over a row past the end, which it
+    // fills with zeros, than over one that it reads (24 x 4,096 x 4,096, 64 wide: 10.9 us, 8.0 so); what the others' sums are
+    // made of does not matter.
+    g.box_rows = !k.pair && g.M < F8_BM ? (int)(g.M + 7) / 8 * 8 : F8_BM;
+    if (encode_tmap_bf16(&g.tmA, A->q, A->rows, cols16, g.box_rows)) return CLEARMOE_ECUDA;
     if (g.out_kind == FP8_OUT_FP8 && k.pair && encode_tmap_bf16(&g.tmOut, g.out, g.M, g.ldo / 2, 32)) return CLEARMOE_ECUDA;
     for (int e = 0; e < E; ++e) {
         g.sb[e] = W[e].scale;

@@ -329,6 +329,7 @@ struct Fp8GemmArgs {
     int64_t M;
     int N;
     int nkb;  // K blocks of 128
+    int box_rows;  // rows of tmA's boxes
     int E;    // groups
     const int32_t* offsets;  // [E + 1]; nullable: one group [0, M)
     const int32_t* rows;     // output row of row i (nullable)
