@@ -176,6 +176,23 @@ def test_every_kernel(kernel, M, N, K, act):
         assert bool(((got.double() - y).abs() <= 1.07 * err + 2.0 ** -4 * y.abs() + 2.0 ** -10 * 2 * amax / 448 * 1.01).all())
 
 
+@pytest.mark.parametrize("kernel", [(16, 0)], indirect=True)
+@pytest.mark.parametrize("M,N,K,act", [(1, 1, 1, cm.ACT_NONE), (16, 40, 130, cm.ACT_GELU), (9, 5003, 257, cm.ACT_RELU),
+                                       (7, 12000, 512, cm.ACT_NONE), (3, 77, 9000, cm.ACT_GELU)])
+def test_kernel_for_few_rows(kernel, M, N, K, act):
+    """The kernel for up to 16 rows at widths that the library gives to the tiled ones, too; a call of more rows than it
+    takes is the tiled kernels' whatever was asked for."""
+    rng = np.random.default_rng(M + N + K)
+    A, W, av, wv = make(rng, M, N, K)
+    bias = dev(rng.standard_normal(N) * 0.1)
+    y, err = reference(av, wv, bias, act)
+    for dtype in (torch.float32, torch.bfloat16):
+        out = torch.full((M, N + 3), float("nan"), device="cuda", dtype=dtype)
+        cm.clearmoe_fp8_gemm(A, W, out[:, :N], bias=bias, act=act)
+        assert bool(((out[:, :N].double() - y).abs() <= err + (2.0 ** -8 * y.abs() if dtype == torch.bfloat16 else 0)).all())
+        assert bool(out[:, N:].isnan().all())
+
+
 @pytest.mark.parametrize("kernel", KERNELS, indirect=True)
 def test_every_kernel_grouped(kernel):
     rng = np.random.default_rng(77)
