@@ -4,6 +4,7 @@
 #include "common.cuh"
 #include "fp8.cuh"
 #include "internal.h"
+#include "pair.cuh"
 
 namespace cm {
 
@@ -241,20 +242,37 @@ __device__ __forceinline__ void f8_store32(const Fp8GemmArgs& a, float (&v)[32],
     }
 }
 
-// gelu_pair_bf16 with max(u, 0) taken directly, two operations a pair less: -inf gives 0, GELU's limit, instead of NaN.
-// The epilogue of 8-bit outputs is bound by its instructions.
-__device__ __forceinline__ float2 gelu_pair_fp8(float2 u) {
-    const float2 v = make_float2(fmaxf(-fabsf(u.x), GeluE::HOLD), fmaxf(-fabsf(u.y), GeluE::HOLD));
-    float2 q = __ffma2_rn(make_float2(GeluE::C6, GeluE::C6), v, make_float2(GeluE::C5, GeluE::C5));
-    q = __ffma2_rn(q, v, make_float2(GeluE::C4, GeluE::C4));
-    q = __ffma2_rn(q, v, make_float2(GeluE::C3, GeluE::C3));
-    q = __ffma2_rn(q, v, make_float2(GeluE::C2, GeluE::C2));
-    q = __ffma2_rn(q, v, make_float2(GeluE::C1, GeluE::C1));
-    q = __ffma2_rn(q, v, make_float2(-1.f, -1.f));
-    float2 r;  // NaN stays NaN
-    asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r.x) : "f"(u.x));
-    asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r.y) : "f"(u.y));
-    return __ffma2_rn(v, make_float2(ex2_approx(q.x), ex2_approx(q.y)), r);
+// gelu_pair_bf16 for P pairs at once, step by step, so that a step's latency passes under the other pairs' (50,432 x 3,072 x
+// 768 with 8-bit outputs, on pairs of SMs: one pair after another 122 us, two at a time 109, four 106, eight 106), and with
+// max(u, 0) taken directly, two operations a pair less: -inf gives 0, GELU's limit, instead of NaN.
+template <int P>
+__device__ __forceinline__ void gelu_pairs_fp8(float* u) {
+    float2 v[P], q[P];
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+        v[i] = make_float2(fmaxf(-fabsf(u[2 * i]), GeluE::HOLD), fmaxf(-fabsf(u[2 * i + 1]), GeluE::HOLD));
+#pragma unroll
+    for (int i = 0; i < P; ++i) q[i] = __ffma2_rn(make_float2(GeluE::C6, GeluE::C6), v[i], make_float2(GeluE::C5, GeluE::C5));
+#pragma unroll
+    for (int i = 0; i < P; ++i) q[i] = __ffma2_rn(q[i], v[i], make_float2(GeluE::C4, GeluE::C4));
+#pragma unroll
+    for (int i = 0; i < P; ++i) q[i] = __ffma2_rn(q[i], v[i], make_float2(GeluE::C3, GeluE::C3));
+#pragma unroll
+    for (int i = 0; i < P; ++i) q[i] = __ffma2_rn(q[i], v[i], make_float2(GeluE::C2, GeluE::C2));
+#pragma unroll
+    for (int i = 0; i < P; ++i) q[i] = __ffma2_rn(q[i], v[i], make_float2(GeluE::C1, GeluE::C1));
+#pragma unroll
+    for (int i = 0; i < P; ++i) q[i] = __ffma2_rn(q[i], v[i], make_float2(-1.f, -1.f));
+#pragma unroll
+    for (int i = 0; i < P; ++i) q[i] = make_float2(ex2_approx(q[i].x), ex2_approx(q[i].y));
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        float2 r;  // NaN stays NaN
+        asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r.x) : "f"(u[2 * i]));
+        asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r.y) : "f"(u[2 * i + 1]));
+        r = __ffma2_rn(v[i], q[i], r);
+        u[2 * i] = r.x, u[2 * i + 1] = r.y;
+    }
 }
 
 // CW accumulator columns + bias, activation; bias from the warp's shared-memory line.
@@ -270,11 +288,15 @@ __device__ __forceinline__ void f8_act(float (&v)[CW], const float* s_bias, bool
         }
     }
     if (act == CLEARMOE_ACT_GELU) {
+        if constexpr (EXACT) {
 #pragma unroll
-        for (int i = 0; i < CW; i += 2) {
-            const float2 u = make_float2(v[i], v[i + 1]);
-            const float2 g = EXACT ? gelu_pair_f32(u) : gelu_pair_fp8(u);
-            v[i] = g.x, v[i + 1] = g.y;
+            for (int i = 0; i < CW; i += 2) {
+                const float2 g = gelu_pair_f32(make_float2(v[i], v[i + 1]));
+                v[i] = g.x, v[i + 1] = g.y;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < CW; i += 8) gelu_pairs_fp8<4>(v + i);
         }
     } else if (act == CLEARMOE_ACT_RELU) {
 #pragma unroll
@@ -290,5 +312,87 @@ __device__ __forceinline__ float f8_max_abs32(const float (&v)[32]) {
     }
     return max_abs(m[0], m[1]);
 }
+
+// 8-bit outputs of an epilogue warp: a row a lane and 64 columns, half of a scale block, at a time. The warp with the same
+// rows' other half is its mate; they exchange the rows' largest magnitudes through shared memory, in two buffers by block:
+// a warp's read of one precedes its arrival for the next block, and that the mate's write two blocks on.
+constexpr int F8_STAGED = 32 * 64;  // bytes of a warp's staged half block
+struct F8Halves {
+    const Fp8GemmArgs& a;
+    float* line;            // [64] of the warp: the bias of its columns
+    float* amax;            // [2][32] of the warp; its mate's
+    const float* mate;
+    uint32_t bar;           // both warps arrive
+    unsigned char* staged;  // [32][64] of the warp
+    int lane;
+    uint32_t ph = 0;
+    uint32_t b[2];  // as loaded, bf16 or fp32: converted here, it would be waited for here
+    // The bias of columns [n, n + 64), a block ahead: a load waits behind the queued tile loads.
+    __device__ __forceinline__ void prefetch(int n) {
+        if (!a.bias) return;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int c = n + 32 * i + lane;
+            b[i] = 0;
+            if (c < a.N) {
+                b[i] = a.bias_bf16 ? __ldg(static_cast<const uint16_t*>(a.bias) + c) : __ldg(static_cast<const uint32_t*>(a.bias) + c);
+            }
+        }
+    }
+    // The sums of rows row0 .. row0 + 31 and columns [n, n + 64) to bytes and scales; next: the columns of the block after
+    // this one, or -1. The bytes leave by a bulk copy of 32 rows of 64 bytes, from shared memory where piece j of 16 bytes
+    // of row i lies at j ^ (i >> 1 & 3). False when the mate gave up.
+    template <class Wait>
+    __device__ __forceinline__ bool store(float (&v)[64], int row0, int n, int next, Wait wait) {
+        if (a.bias) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) line[32 * i + lane] = __uint_as_float(a.bias_bf16 ? b[i] << 16 : b[i]);
+            __syncwarp();
+        }
+        if (next >= 0) prefetch(next);
+        f8_act<64, false>(v, line, a.bias != nullptr, a.act);
+        if (n + 64 > a.N) {  // columns past N are zero, in the last block's padding and where no block is
+#pragma unroll
+            for (int i = 0; i < 64; ++i)
+                if (n + i >= a.N) v[i] = 0.f;
+        }
+        float m[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 64; i += 8)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) m[j] = max_abs3(m[j], v[i + 2 * j], v[i + 2 * j + 1]);
+        const float mine = max_abs3(max_abs(m[0], m[1]), m[2], m[3]);
+        amax[ph * 32 + lane] = mine;
+        bulk_wait_read();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar);
+        if (!wait(bar, ph)) return false;
+        const uint32_t s = fp8_scale_byte(abs_bits(max_abs(mine, mate[ph * 32 + lane])));
+        ph ^= 1;
+        const float inv = fp8_inverse_scale(s);
+        const float2 k = make_float2(inv, inv);
+        const uint32_t at = smem_u32(staged) + lane * 64;
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            uint32_t o[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float* w = v + 16 * p + 4 * i;
+                const float2 x = __fmul2_rn(make_float2(w[0], w[1]), k), y = __fmul2_rn(make_float2(w[2], w[3]), k);
+                o[i] = fp8_pack4(x.x, x.y, y.x, y.y);
+            }
+            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at + ((p ^ (lane >> 1 & 3)) << 4)), "r"(o[0]), "r"(o[1]),
+                         "r"(o[2]), "r"(o[3])
+                         : "memory");
+        }
+        if ((n & 64) == 0 && row0 + lane < a.M && n < a.ldo)
+            a.out_scale[(int64_t)(row0 + lane) * a.ldos + n / 128] = (uint8_t)s;
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (n < a.ldo && row0 < a.M) tma_store_2d(&a.tmOut, smem_u32(staged), n, row0);
+        bulk_commit();
+        return true;
+    }
+};
 
 }  // namespace cm

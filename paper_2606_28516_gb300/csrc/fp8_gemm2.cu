@@ -14,8 +14,12 @@
 // the accumulator traffic and bounded the kernel, 101 us against 93 for 19,456 x 1,792 x 4,096.
 //
 // Epilogue: 16 warps (four per lane quarter, so that each scheduler has four to hide the latencies of bias, GELU and
-// conversions), each 32 columns of a 128-column block at a time. For 8-bit outputs the block is one scale block: its
-// four warps exchange the row's largest magnitudes through shared memory.
+// conversions), each 32 columns of a 128-column block at a time. For 8-bit outputs, whose arithmetic takes longer than the
+// MMAs (of 64 values a lane: some 10 cycles each on the FMA pipe alone), two groups of eight take every other tile, one
+// accumulator each, so that one group's waits pass under the other's arithmetic; a warp has 64 columns of a 128-column
+// scale block and exchanges its rows' largest magnitudes with the warp that has the others. 50,432 x 3,072 x 768 with bias
+// and GELU: 106 us (2,250 TFLOP/s); all 16 warps on every tile, pair after pair of values, 121; eight warps with 128
+// columns a lane and no exchange 106, and 113 in 128-wide tiles against 105. Without bias and GELU 80.
 // Hand-offs and giving up as in tc_gemm2.cu: TMA bytes of both CTAs on the even CTA's full barriers, commits on
 // both CTAs' empty, sempty and tfull barriers, the scale warp and epilogue warps of both on the even CTA's sfull,
 // ovl and tempty; every wait is bounded, and the even CTA lets copies in flight land before the cluster retires.
@@ -32,9 +36,6 @@ namespace cm {
 
 namespace {
 
-constexpr int P8_NUM_EPI = 16;
-constexpr int P8_WARP_SCALE = 16, P8_WARP_MMA = 18, P8_WARP_TMA = 19;
-constexpr int P8_THREADS = 32 * 20;
 constexpr int P8_BM = 128;  // rows per CTA
 constexpr int P8_BK = 128;
 
@@ -42,10 +43,15 @@ template <int BN_, int KIND>
 struct P8Cfg {
     static constexpr int BN = BN_;
     static constexpr int BH = BN / 2;  // W rows per CTA
+    static constexpr bool Q = KIND == FP8_OUT_FP8;
+    static constexpr int NUM_EPI = 16;  // epilogue warps
+    static constexpr int WARP_SCALE = NUM_EPI, WARP_MMA = NUM_EPI + F8_SCALE_WARPS, WARP_TMA = WARP_MMA + 1;
+    static constexpr int THREADS = 32 * (WARP_TMA + 1);
+    static constexpr int TILE_WARPS = Q ? NUM_EPI / 2 : NUM_EPI;  // that share a tile's 128 rows
+    static constexpr int BIAS_LINE = Q ? 64 : 32;                 // floats per epilogue warp
     static constexpr int A_BYTES = P8_BM * P8_BK, B_BYTES = BH * P8_BK;
     static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
-    // 8-bit outputs: a tile's rows of bytes, staged for whole-line stores
-    static constexpr int OUT_BYTES = KIND == FP8_OUT_FP8 ? P8_BM * BN : 0;
+    static constexpr int OUT_BYTES = Q ? NUM_EPI * F8_STAGED : 0;
     static constexpr int STAGES = (192 * 1024 - OUT_BYTES) / STAGE_BYTES;
     static constexpr bool OVL = BN == 256;
     static constexpr int ACC1 = OVL ? 224 : BN;  // first column of the second accumulator
@@ -54,9 +60,9 @@ struct P8Cfg {
     static_assert(SF_COL + 2 * SF_COLS <= 512);
     static constexpr int CHUNKS = BN / 32;
     static constexpr int ROUNDS = (CHUNKS + 3) / 4;  // of four 32-column chunks, one per warp of a quarter
-    static constexpr int NBARS = 2 * STAGES + 2 * F8_SLOTS + 4 + 3 + 4 * ROUNDS + 4;
-    static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + OUT_BYTES + F8_SLOTS * SF_BYTES + P8_NUM_EPI * 32 * 4 + 2 * ROUNDS * P8_NUM_EPI * 32 * 4 + NBARS * 8 + 16 +
-                                8 * (CM_MAX_E + 1) + 8;
+    static constexpr int NBARS = 2 * STAGES + 2 * F8_SLOTS + 4 + 3 + (Q ? 8 : 0);
+    static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + OUT_BYTES + F8_SLOTS * SF_BYTES + NUM_EPI * BIAS_LINE * 4 +
+                                (Q ? NUM_EPI * 64 * 4 : 0) + NBARS * 8 + 16 + 8 * (CM_MAX_E + 1) + 8;
 };
 
 __device__ __forceinline__ void umma2_mxf8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sfa,
@@ -73,17 +79,17 @@ __device__ __forceinline__ void umma2_mxf8(uint32_t d_tmem, uint64_t a_desc, uin
 
 // KIND: Fp8Out.
 template <int BN_, int KIND>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8Cfg<BN_, KIND>::THREADS, 1)
     fp8_gemm2_kernel(const __grid_constant__ Fp8GemmArgs a) {
     using C = P8Cfg<BN_, KIND>;
     constexpr int BN = C::BN, STAGES = C::STAGES, SLOTS = F8_SLOTS;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* sm = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
-    unsigned char* s_out = sm + STAGES * C::STAGE_BYTES;                      // [block][row][128], 8-bit outputs
-    unsigned char* s_sf = s_out + C::OUT_BYTES;                               // [slot]
-    float* s_bias = reinterpret_cast<float*>(s_sf + SLOTS * C::SF_BYTES);      // [epilogue warp][32]
-    float* s_amax = s_bias + P8_NUM_EPI * 32;                                  // [2][round][epilogue warp][32]
-    uint64_t* bars = reinterpret_cast<uint64_t*>(s_amax + 2 * C::ROUNDS * P8_NUM_EPI * 32);
+    unsigned char* s_out = sm + STAGES * C::STAGE_BYTES;                   // [epilogue warp][32 rows][64], 8-bit outputs
+    unsigned char* s_sf = s_out + C::OUT_BYTES;                            // [slot]
+    float* s_bias = reinterpret_cast<float*>(s_sf + SLOTS * C::SF_BYTES);  // [epilogue warp][BIAS_LINE]
+    float* s_amax = s_bias + C::NUM_EPI * C::BIAS_LINE;                    // [epilogue warp][2][32], 8-bit outputs
+    uint64_t* bars = reinterpret_cast<uint64_t*>(s_amax + (C::Q ? C::NUM_EPI * 64 : 0));
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::NBARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     volatile uint32_t* s_issued = tmem_slot + 2;  // k-blocks this CTA's producer has loaded, once it has stopped
@@ -103,7 +109,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
     auto tempty_bar = [&](int i) { return bar0 + 8u * (2 * STAGES + 2 * SLOTS + 2 + i); };
     const uint32_t ovl_bar = bar0 + 8u * (2 * STAGES + 2 * SLOTS + 4);
     const uint32_t drain_bar = ovl_bar + 8, stop_bar = ovl_bar + 16;
-    auto pair_bar = [&](int q) { return ovl_bar + 24 + 8u * q; };
+    auto pair_bar = [&](int q) { return ovl_bar + 24 + 8u * q; };  // 8-bit outputs: two warps with the same rows
     const uint64_t lim = (uint64_t)a.wait_limit_ns;
 
     if (threadIdx.x == 0) {
@@ -117,16 +123,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(tfull_bar(i), 1);
-            mbar_init(tempty_bar(i), 2 * P8_NUM_EPI);  // epilogue warps of both CTAs
+            mbar_init(tempty_bar(i), 2 * C::TILE_WARPS);  // epilogue warps of both CTAs
         }
         mbar_init(ovl_bar, 8);  // the warps whose chunk lies in the shared columns, of both CTAs
         mbar_init(drain_bar, 1);
         mbar_init(stop_bar, 2);
-        for (int q = 0; q < 4 * C::ROUNDS + 4; ++q) mbar_init(pair_bar(q), 4);
+        if constexpr (C::Q)
+            for (int q = 0; q < 8; ++q) mbar_init(pair_bar(q), 2);
         *abort_flag = 0;
         mbar_fence_init();
     }
-    if (warp == P8_WARP_MMA) {
+    if (warp == C::WARP_MMA) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512)
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
@@ -142,125 +149,170 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
     const int nkb = a.nkb;
     F8Walk t(blockIdx.x >> 1, gridDim.x >> 1, a.N, 2 * P8_BM, BN, a.E, s_off, s_prefix);
 
-    if (warp == P8_WARP_TMA) {
-        // ------------------------------------------------ producers (both CTAs)
-        const uint32_t full_leader0 = map_to_rank(full_bar(0), 0);
-        int stage = 0;
-        uint32_t ph = 0, issued = 0;
-        bool ok = true;
-        for (; warp_uniform((int)t.live()) && ok; t.next()) {
-            const int e = warp_uniform(t.e);
-            const int m0 = warp_uniform(t.m0 + (int)rank * P8_BM), n0 = warp_uniform(t.n0 + (int)rank * C::BH);
-            for (int kb = 0; kb < nkb; ++kb) {
-                if (!mbar_wait_warp(empty_bar(stage), ph ^ 1, abort_flag, a.status, lim)) {
-                    ok = false;
-                    break;
-                }
-                const uint32_t sA = smem_u32(sm + stage * C::STAGE_BYTES);
-                const uint32_t fb = full_leader0 + 8u * stage;
-                if (leader) mbar_arrive_expect_tx_warp(full_bar(stage), 2 * C::STAGE_BYTES);
-                // coordinates in the maps' 16-bit elements: two bytes each
-                tma_load_2d_pair(sA, &a.tmA, kb * (P8_BK / 2), m0, fb);
-                tma_load_2d_pair(sA + C::A_BYTES, &a.tmB[e], kb * (P8_BK / 2), n0, fb);
-                ++issued;
-                if (++stage == STAGES) {
-                    stage = 0;
-                    ph ^= 1;
-                }
-            }
-        }
-        *s_issued = issued;
-        __syncwarp();
-        mbar_arrive_release_cluster_warp(map_to_rank(stop_bar, 0));
-    } else if (warp == P8_WARP_MMA) {
-        // ------------------------------------------------ MMA issuer (even CTA, the whole warp)
-        if (leader) {
-            int stage = 0, slot = 0, acc = 0;
-            uint32_t ph = 0, sph = 0, aph = 0, oph = 1;  // oph: phase of the previous tile's shared columns
+    if (warp >= C::NUM_EPI) {
+        if (warp == C::WARP_TMA) {
+            // ------------------------------------------------ producers (both CTAs)
+            const uint32_t full_leader0 = map_to_rank(full_bar(0), 0);
+            int stage = 0;
+            uint32_t ph = 0, issued = 0;
             bool ok = true;
             for (; warp_uniform((int)t.live()) && ok; t.next()) {
-                if (!mbar_wait_warp(tempty_bar(acc), aph ^ 1, abort_flag, a.status, lim)) break;
-                if (C::OVL && !mbar_wait_warp(ovl_bar, oph, abort_flag, a.status, lim)) break;
-                oph ^= 1;
-                tc_fence_after();
-                const uint32_t d = tmem + acc * C::ACC1;
+                const int e = warp_uniform(t.e);
+                const int m0 = warp_uniform(t.m0 + (int)rank * P8_BM), n0 = warp_uniform(t.n0 + (int)rank * C::BH);
                 for (int kb = 0; kb < nkb; ++kb) {
-                    const int byte = kb & 3;
-                    const uint32_t sf = tmem + C::SF_COL + (slot & 1) * C::SF_COLS;
-                    if (byte == 0) {
-                        if (!mbar_wait_warp(sfull_bar(slot), sph, abort_flag, a.status, lim)) {
-                            ok = false;
-                            break;
-                        }
-                        tc_fence_after();
-#pragma unroll
-                        for (int h = 0; h < C::SF_COLS / 4; ++h)
-                            tmem_cp_scales<2>(sf + 4 * h, smem_u32(s_sf) + slot * C::SF_BYTES + 512 * h);
-                    }
-                    if (!mbar_wait_warp(full_bar(stage), ph, abort_flag, a.status, lim)) {
+                    if (!mbar_wait_warp(empty_bar(stage), ph ^ 1, abort_flag, a.status, lim)) {
                         ok = false;
                         break;
                     }
-                    tc_fence_after();
                     const uint32_t sA = smem_u32(sm + stage * C::STAGE_BYTES);
-                    const uint64_t ad = sdesc_kmajor_sw128(sA), bd = sdesc_kmajor_sw128(sA + C::A_BYTES);
-                    const uint32_t id = idesc_mxf8(2 * P8_BM, BN, byte);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)  // 32 of K: 32 bytes on in each row
-                        umma2_mxf8(d, ad + 2 * k, bd + 2 * k, id, sf, sf + 4, (kb | k) != 0);
-                    umma2_commit_both(empty_bar(stage));
+                    const uint32_t fb = full_leader0 + 8u * stage;
+                    if (leader) mbar_arrive_expect_tx_warp(full_bar(stage), 2 * C::STAGE_BYTES);
+                    // coordinates in the maps' 16-bit elements: two bytes each
+                    tma_load_2d_pair(sA, &a.tmA, kb * (P8_BK / 2), m0, fb);
+                    tma_load_2d_pair(sA + C::A_BYTES, &a.tmB[e], kb * (P8_BK / 2), n0, fb);
+                    ++issued;
                     if (++stage == STAGES) {
                         stage = 0;
                         ph ^= 1;
                     }
-                    if (byte == 3 || kb + 1 == nkb) {
-                        umma2_commit_both(sempty_bar(slot));
-                        if (++slot == SLOTS) {
-                            slot = 0;
-                            sph ^= 1;
+                }
+            }
+            *s_issued = issued;
+            __syncwarp();
+            mbar_arrive_release_cluster_warp(map_to_rank(stop_bar, 0));
+        } else if (warp == C::WARP_MMA) {
+            // ------------------------------------------------ MMA issuer (even CTA, the whole warp)
+            if (leader) {
+                int stage = 0, slot = 0, acc = 0;
+                uint32_t ph = 0, sph = 0, aph = 0, oph = 1;  // oph: phase of the previous tile's shared columns
+                bool ok = true;
+                for (; warp_uniform((int)t.live()) && ok; t.next()) {
+                    if (!mbar_wait_warp(tempty_bar(acc), aph ^ 1, abort_flag, a.status, lim)) break;
+                    if (C::OVL && !mbar_wait_warp(ovl_bar, oph, abort_flag, a.status, lim)) break;
+                    oph ^= 1;
+                    tc_fence_after();
+                    const uint32_t d = tmem + acc * C::ACC1;
+                    for (int kb = 0; kb < nkb; ++kb) {
+                        const int byte = kb & 3;
+                        const uint32_t sf = tmem + C::SF_COL + (slot & 1) * C::SF_COLS;
+                        if (byte == 0) {
+                            if (!mbar_wait_warp(sfull_bar(slot), sph, abort_flag, a.status, lim)) {
+                                ok = false;
+                                break;
+                            }
+                            tc_fence_after();
+    #pragma unroll
+                            for (int h = 0; h < C::SF_COLS / 4; ++h)
+                                tmem_cp_scales<2>(sf + 4 * h, smem_u32(s_sf) + slot * C::SF_BYTES + 512 * h);
+                        }
+                        if (!mbar_wait_warp(full_bar(stage), ph, abort_flag, a.status, lim)) {
+                            ok = false;
+                            break;
+                        }
+                        tc_fence_after();
+                        const uint32_t sA = smem_u32(sm + stage * C::STAGE_BYTES);
+                        const uint64_t ad = sdesc_kmajor_sw128(sA), bd = sdesc_kmajor_sw128(sA + C::A_BYTES);
+                        const uint32_t id = idesc_mxf8(2 * P8_BM, BN, byte);
+    #pragma unroll
+                        for (int k = 0; k < 4; ++k)  // 32 of K: 32 bytes on in each row
+                            umma2_mxf8(d, ad + 2 * k, bd + 2 * k, id, sf, sf + 4, (kb | k) != 0);
+                        umma2_commit_both(empty_bar(stage));
+                        if (++stage == STAGES) {
+                            stage = 0;
+                            ph ^= 1;
+                        }
+                        if (byte == 3 || kb + 1 == nkb) {
+                            umma2_commit_both(sempty_bar(slot));
+                            if (++slot == SLOTS) {
+                                slot = 0;
+                                sph ^= 1;
+                            }
                         }
                     }
+                    if (!ok) break;
+                    umma2_commit_both(tfull_bar(acc));
+                    if (++acc == 2) {
+                        acc = 0;
+                        aph ^= 1;
+                    }
                 }
-                if (!ok) break;
-                umma2_commit_both(tfull_bar(acc));
-                if (++acc == 2) {
-                    acc = 0;
-                    aph ^= 1;
+                umma2_commit_one(drain_bar);  // every MMA issued above has completed once this fires
+                mbar_wait_warp(drain_bar, 0, nullptr, a.status, lim + 10000000ull);
+                // An issuer that ran all its tiles has seen every copy of both CTAs land. One that gave up waits, once
+                // both producers have stopped, for the last copies issued to each stage; a stage that only one producer
+                // reached gets the other's part of its barrier here.
+                if (warp_uniform((int)*abort_flag) && mbar_wait_warp(stop_bar, 0, nullptr, a.status, 2 * lim + 10000000ull)) {
+                    fence_cluster();
+                    const uint32_t at = smem_u32(tmem_slot + 2);
+                    const uint32_t n0 = ld_cluster_u32(map_to_rank(at, 0)), n1 = ld_cluster_u32(map_to_rank(at, 1)), n = max(n0, n1);
+    #pragma unroll 1
+                    for (uint32_t k = n > STAGES ? n - STAGES : 0; k < n; ++k) {
+                        const uint32_t s = k % STAGES;
+                        const DrainStep st = drain_step(k, n0, n1);
+                        // the odd CTA alone reached it: expect its bytes; the even CTA alone: count the odd one's as landed
+                        if (st.arrive) mbar_arrive_expect_tx_warp(full_bar(s), C::STAGE_BYTES);
+                        if (st.complete) mbar_complete_tx_warp(full_bar(s), C::STAGE_BYTES);
+                        mbar_wait_warp(full_bar(s), (k / STAGES) & 1, nullptr, a.status, 10000000ull);
+                    }
                 }
             }
-            umma2_commit_one(drain_bar);  // every MMA issued above has completed once this fires
-            mbar_wait_warp(drain_bar, 0, nullptr, a.status, lim + 10000000ull);
-            // An issuer that ran all its tiles has seen every copy of both CTAs land. One that gave up waits, once
-            // both producers have stopped, for the last copies issued to each stage; a stage that only one producer
-            // reached gets the other's part of its barrier here.
-            if (warp_uniform((int)*abort_flag) && mbar_wait_warp(stop_bar, 0, nullptr, a.status, 2 * lim + 10000000ull)) {
-                fence_cluster();
-                const uint32_t at = smem_u32(tmem_slot + 2);
-                const uint32_t n0 = ld_cluster_u32(map_to_rank(at, 0)), n1 = ld_cluster_u32(map_to_rank(at, 1)), n = max(n0, n1);
+            __syncwarp();
+        } else {
+            // ------------------------------------------------ scales (both CTAs)
+            const uint32_t sfull_leader0 = map_to_rank(sfull_bar(0), 0);
+            f8_scale_warp<BN>(a, warp - C::WARP_SCALE, t, (int)rank * P8_BM, lane,
+                              [&](const F8Scales<BN>& w, int slot, uint32_t ph) {
+                                  if (!mbar_wait_warp(sempty_bar(slot), ph ^ 1, abort_flag, a.status, lim)) return false;
+                                  w.store(s_sf + slot * C::SF_BYTES, lane);
+                                  fence_proxy_async_smem();
+                                  __syncwarp();
+                                  mbar_arrive_release_cluster_warp(sfull_leader0 + 8u * slot);
+                                  return true;
+                              });
+        }
+    } else if constexpr (KIND == FP8_OUT_FP8) {
+        // ------------------------------------------------ epilogue (both CTAs, own 128 rows): 8-bit outputs
+        const int acc = warp >> 3, half = warp >> 2 & 1, quarter = warp & 3;  // every other tile is its group's
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        const uint32_t tempty_leader = map_to_rank(tempty_bar(acc), 0), ovl_leader = map_to_rank(ovl_bar, 0);
+        F8Halves out{a, s_bias + warp * C::BIAS_LINE, s_amax + warp * 64, s_amax + (warp ^ 4) * 64, pair_bar(acc * 4 + quarter),
+                     s_out + warp * F8_STAGED, lane};
+        // first the block in the columns that the accumulators share
+        auto column = [&](int r) { return (C::OVL && acc == 0 ? C::ROUNDS - 1 - r : r) * 128 + half * 64; };
+        if (acc && t.live()) t.next();
+        if (t.live()) out.prefetch(t.n0 + column(0));
+        uint32_t ph = 0;
+        bool ok = true;
+        while (t.live() && ok) {
+            const int row0 = t.m0 + (int)rank * P8_BM + quarter * 32, n0 = t.n0;
+            t.next();
+            if (t.live()) t.next();
+            if (!mbar_wait_warp(tfull_bar(acc), ph, abort_flag, a.status, lim)) break;
+            tc_fence_after();
+            ph ^= 1;
 #pragma unroll 1
-                for (uint32_t k = n > STAGES ? n - STAGES : 0; k < n; ++k) {
-                    const uint32_t s = k % STAGES;
-                    const DrainStep st = drain_step(k, n0, n1);
-                    // the odd CTA alone reached it: expect its bytes; the even CTA alone: count the odd one's as landed
-                    if (st.arrive) mbar_arrive_expect_tx_warp(full_bar(s), C::STAGE_BYTES);
-                    if (st.complete) mbar_complete_tx_warp(full_bar(s), C::STAGE_BYTES);
-                    mbar_wait_warp(full_bar(s), (k / STAGES) & 1, nullptr, a.status, 10000000ull);
+            for (int r = 0; r < C::ROUNDS && ok; ++r) {
+                float v[64];
+                {
+                    uint32_t u[64];
+                    CM_TMEM_LD_X32(tmem + lanes + acc * C::ACC1 + column(r), u);
+                    CM_TMEM_LD_X32(tmem + lanes + acc * C::ACC1 + column(r) + 32, (u + 32));
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 64; ++i) v[i] = __uint_as_float(u[i]);
                 }
+                const bool last = r + 1 == C::ROUNDS;
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {  // these columns may be written again
+                    if (C::OVL && r == 0 && half == 1 - acc) mbar_arrive_cluster(ovl_leader);
+                    if (last) mbar_arrive_cluster(tempty_leader);
+                }
+                ok = out.store(v, row0, n0 + column(r), last ? (t.live() ? t.n0 + column(0) : -1) : n0 + column(r + 1),
+                               [&](uint32_t bar, uint32_t p) { return mbar_wait_warp(bar, p, abort_flag, a.status, lim); });
             }
         }
-        __syncwarp();
-    } else if (warp >= P8_WARP_SCALE) {
-        // ------------------------------------------------ scales (both CTAs)
-        const uint32_t sfull_leader0 = map_to_rank(sfull_bar(0), 0);
-        f8_scale_warp<BN>(a, warp - P8_WARP_SCALE, t, (int)rank * P8_BM, lane,
-                          [&](const F8Scales<BN>& w, int slot, uint32_t ph) {
-                              if (!mbar_wait_warp(sempty_bar(slot), ph ^ 1, abort_flag, a.status, lim)) return false;
-                              w.store(s_sf + slot * C::SF_BYTES, lane);
-                              fence_proxy_async_smem();
-                              __syncwarp();
-                              mbar_arrive_release_cluster_warp(sfull_leader0 + 8u * slot);
-                              return true;
-                          });
+        bulk_wait_all();  // the stores read this CTA's shared memory
     } else {
         // ------------------------------------------------ epilogue (both CTAs, own 128 rows)
         const int quarter = warp & 3, cg = warp >> 2;
@@ -269,14 +321,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
         const bool has_bias = a.bias != nullptr;
         const int esz = KIND == FP8_OUT_BF16 ? 2 : 4;
         // rows of the output in whole 32-byte pieces
-        const bool wide = KIND == FP8_OUT_FP8 || ((reinterpret_cast<uintptr_t>(a.out) & 31) == 0 && (a.ldo * esz & 31) == 0);
+        const bool wide = (reinterpret_cast<uintptr_t>(a.out) & 31) == 0 && (a.ldo * esz & 31) == 0;
         const uint32_t tempty_leader0 = map_to_rank(tempty_bar(0), 0), ovl_leader = map_to_rank(ovl_bar, 0);
         // What a tile's epilogue needs beside its sums, loaded a tile ahead: a load waits behind the queued tile loads.
         float bias[C::ROUNDS];
         int row = 0;
         auto prefetch = [&](int acc) {
             if (!t.live()) return;
-            if (KIND != FP8_OUT_FP8) row = f8_out_row(a, t.m0 + (int)rank * P8_BM + quarter * 32 + lane, t.hi);
+            row = f8_out_row(a, t.m0 + (int)rank * P8_BM + quarter * 32 + lane, t.hi);
             if (has_bias) {
 #pragma unroll
                 for (int r = 0; r < C::ROUNDS; ++r) {
@@ -289,11 +341,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
         };
         prefetch(0);
         int acc = 0;
-        uint32_t aph = 0, pph = 0;
-        float* ex = s_amax;
-        bool ok = true;
-        while (t.live() && ok) {
-            const int m0 = t.m0 + (int)rank * P8_BM, hi = t.hi, n0 = t.n0, orow = row;
+        uint32_t aph = 0;
+        while (t.live()) {
+            const int n0 = t.n0, orow = row;
             // The chunk of round r: the one in the columns that the accumulators share first.
             int chunk[C::ROUNDS];
             float b[C::ROUNDS];
@@ -316,79 +366,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
                     if (r + 1 == C::ROUNDS) mbar_arrive_cluster(tempty_leader0 + 8u * acc);
                 }
             };
-            if constexpr (KIND == FP8_OUT_FP8) {
-                // All of the tile's sums are read before any is worked on and before the next tile's MMAs start: reads
-                // beside MMAs wait for them (133 us against 128, 50,432 x 3,072 x 768). Then every round's values are activated and its magnitudes handed
-                // over before the first exchange is waited for, so that arithmetic hides the latencies.
-                float v[C::ROUNDS][32];
-                {
-                    uint32_t u[C::ROUNDS][32];
-#pragma unroll
-                    for (int r = 0; r < C::ROUNDS; ++r) CM_TMEM_LD_X32(d + chunk[r] * 32, u[r]);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int r = 0; r < C::ROUNDS; ++r) {
-                        released(r);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) v[r][i] = __uint_as_float(u[r][i]);
-                    }
-                }
-#pragma unroll
-                for (int r = 0; r < C::ROUNDS; ++r) {
-                    if (has_bias) bias_line[lane] = b[r];
-                    __syncwarp();
-                    f8_act<32, false>(v[r], bias_line, has_bias, a.act);
-                    const int nc = n0 + chunk[r] * 32;
-                    if (nc + 32 > a.N) {  // columns past N are zero, in the last block's padding and where no block is
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (nc + i >= a.N) v[r][i] = 0.f;
-                    }
-                    ex[(r * P8_NUM_EPI + warp) * 32 + lane] = f8_max_abs32(v[r]);
-                    if (r == 0 && cg == 0) bulk_wait_read();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(pair_bar(quarter * C::ROUNDS + r));
-                }
-#pragma unroll
-                for (int r = 0; r < C::ROUNDS; ++r) {
-                    if (!mbar_wait_warp(pair_bar(quarter * C::ROUNDS + r), pph, abort_flag, a.status, lim)) {
-                        ok = false;
-                        break;
-                    }
-                    const float* e = ex + (r * P8_NUM_EPI + quarter) * 32 + lane;
-                    const float mx = max_abs3(max_abs(e[0], e[4 * 32]), e[8 * 32], e[12 * 32]);
-                    const uint32_t s = fp8_scale_byte(abs_bits(mx));
-                    const int nc = n0 + chunk[r] * 32, trow = quarter * 32 + lane;
-                    uint32_t o[8];
-                    fp8_pack32(o, v[r], fp8_inverse_scale(s));
-                    // the row's 16-byte pieces 2 cg and 2 cg + 1, piece j at j ^ (row & 7)
-                    unsigned char* at = s_out + ((chunk[r] >> 2) * P8_BM + trow) * 128;
-                    *reinterpret_cast<uint4*>(at + (((2 * cg) ^ (trow & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
-                    *reinterpret_cast<uint4*>(at + (((2 * cg + 1) ^ (trow & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
-                    if (cg == 0 && m0 + trow < hi && nc < a.ldo) a.out_scale[(int64_t)(m0 + trow) * a.ldos + nc / 128] = (uint8_t)s;
-                }
-                if (!ok) break;
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(pair_bar(4 * C::ROUNDS + quarter));
-                // The quarter's rows as boxes of 32 rows x 128 bytes, by its first warp, which lets them be read before it
-                // arrives for the next tile's exchange, and so before any warp writes there again. (Copied out by the
-                // warps, whole lines or 32 bytes a lane, the stores cost 0.75 us a tile: 130 us
-                // against 114, 50,432 x 3,072 x 768.)
-                if (cg == 0) {
-                    if (!mbar_wait_warp(pair_bar(4 * C::ROUNDS + quarter), pph, abort_flag, a.status, lim)) break;
-#pragma unroll
-                    for (int blk = 0; blk < C::ROUNDS; ++blk)
-                        if (n0 + blk * 128 < a.ldo)
-                            tma_store_2d(&a.tmOut, smem_u32(s_out + (blk * P8_BM + quarter * 32) * 128), (n0 + blk * 128) / 2,
-                                         m0 + quarter * 32);
-                    bulk_commit();
-                }
-                // the exchange of the next tile uses the other half: a warp's reads of this one precede its arrivals for
-                // the next, and those the other warps' writes two tiles on
-                pph ^= 1;
-                ex = s_amax + pph * (C::ROUNDS * P8_NUM_EPI * 32);
-            } else {
 #pragma unroll
             for (int r = 0; r < C::ROUNDS; ++r) {
                 const bool mine = chunk[r] < C::CHUNKS;
@@ -409,19 +386,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
                     f8_store32<KIND>(a, v, orow, nc, wide, lane);
                 }
             }
-            }
             if (++acc == 2) {
                 acc = 0;
                 aph ^= 1;
             }
         }
     }
-    if (KIND == FP8_OUT_FP8 && warp < 4) bulk_wait_all();  // the stores read this CTA's shared memory
     tc_fence_before();
     __syncthreads();
     cluster_sync();  // no copy, commit or remote arrival is left in flight towards either CTA
     tc_fence_after();
-    if (warp == P8_WARP_MMA)
+    if (warp == C::WARP_MMA)
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
@@ -435,7 +410,7 @@ cudaError_t launch_pair(const Fp8GemmArgs& a, int num_sms, cudaStream_t s) {
     const int64_t tiles = m_tiles * ((a.N + BN - 1) / BN), pairs = num_sms / 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs)));
-    cfg.blockDim = dim3(P8_THREADS);
+    cfg.blockDim = dim3(C::THREADS);
     cfg.dynamicSmemBytes = C::SMEM;
     cfg.stream = s;
     cudaLaunchAttribute at[1];

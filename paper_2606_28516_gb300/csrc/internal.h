@@ -319,7 +319,7 @@ cudaError_t launch_quantize_weight(const QuantArgs& a, int dtype, cudaStream_t s
 enum Fp8Out { FP8_OUT_F32 = 0, FP8_OUT_BF16 = 1, FP8_OUT_FP8 = 2 };
 struct Fp8GemmArgs {
     CUtensorMap tmA;
-    CUtensorMap tmOut;  // FP8_OUT_FP8 on pairs: the output's bytes, boxes of 128 bytes x 32 rows
+    CUtensorMap tmOut;  // FP8_OUT_FP8: the output's bytes, boxes of 64 bytes x 32 rows
     CUtensorMap tmB[16];
     const void* x;      // q of A, and of the first W (few rows)
     const void* w;
@@ -403,5 +403,7 @@ int encode_tmap_bf16_chunks(CUtensorMap* map, const void* base, int64_t rows, in
 // Encode a 2-D fp32 row-major [rows x cols] tensor map (cols % 4 == 0), box {32, box_rows}
 // (128-byte rows), 128-byte swizzle.
 int encode_tmap_f32(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int box_rows);
+// The same of bytes (cols % 16 == 0), box {64, box_rows} (64-byte rows), 64-byte swizzle.
+int encode_tmap_bytes(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int box_rows);
 
 }  // namespace cm

@@ -1036,6 +1036,11 @@ int encode_tmap_f32(CUtensorMap* map, const void* base, int64_t rows, int64_t co
     return encode_tmap_cached(map, base, rows, cols, box_rows, 0, 4);
 }
 
+int encode_tmap_bytes(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int box_rows) {
+    if (cols % 16 != 0) return -2;  // the row pitch must be a multiple of 16 bytes
+    return encode_tmap_cached(map, base, rows, cols, box_rows, 0, 1);
+}
+
 static int encode_tmap_uncached(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int box_rows,
                                 int box_chunks, int elem) {
     static PFN_encodeTiled_t fn = nullptr;
@@ -1056,6 +1061,14 @@ static int encode_tmap_uncached(CUtensorMap* map, const void* base, int64_t rows
         const cuuint32_t es[2] = {1, 1};
         r = fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<void*>(base), gdim, gstride, box, es,
                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    } else if (elem == 1) {  // bytes [rows x cols]: boxes of 64 columns x box_rows rows
+        const cuuint64_t gdim[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+        const cuuint64_t gstride[1] = {(cuuint64_t)cols};
+        const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+        const cuuint32_t es[2] = {1, 1};
+        r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), gdim, gstride, box, es,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     } else if (box_chunks == 0) {  // [rows x cols]: boxes of 64 columns x box_rows rows
         const cuuint64_t gdim[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
