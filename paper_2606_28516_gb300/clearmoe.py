@@ -8,6 +8,8 @@ meaning, layout, ownership and errors, are in include/clearmoe.h.
 from __future__ import annotations
 
 import ctypes
+import importlib.machinery
+import importlib.util
 import pathlib
 
 _LIB_PATH = pathlib.Path(__file__).resolve().parent / "libclearmoe.so"
@@ -140,6 +142,26 @@ def lib() -> ctypes.CDLL:
     return _lib
 
 
+_calls = None
+
+
+def _bind_calls():
+    """Loads the compiled part of this binding (built in-tree with the library) and gives it the library's functions."""
+    global _calls
+    path = _LIB_PATH.with_name("_calls.so")
+    if not path.exists():
+        raise RuntimeError(f"{path} is not built; run paper_2606_28516_gb300.build.build()")
+    loader = importlib.machinery.ExtensionFileLoader("_calls", str(path))
+    m = importlib.util.module_from_spec(importlib.util.spec_from_loader("_calls", loader))
+    loader.exec_module(m)
+    L = lib()
+    m.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in
+             (L.clearmoe_fp8_quantize_rows, L.clearmoe_fp8_gemm, L.clearmoe_fp8_gemm_fp8, L.clearmoe_ffn_forward_few,
+              L.clearmoe_ffn_forward_fp8)))
+    _calls = m
+    return m
+
+
 def _check(code: int, where: str) -> None:
     if code != OK:
         raise ClearMoEError(code, where)
@@ -155,21 +177,25 @@ def _ptr(t) -> int | None:
 
 _torch = None
 _raw_stream = None  # device index -> handle of torch's current stream
+_device = None      # the current device's index, once CUDA is initialised
 
 
 def _stream(stream) -> int | None:
     """The given stream's handle, or that of torch's current stream. The handle is asked for directly:
     building torch's Stream object for it costs 3.2 us a call on the GB300's host, this 0.3 us."""
-    global _torch, _raw_stream
+    global _torch, _raw_stream, _device
     if stream is not None:
         return stream.cuda_stream
+    if _device is not None:
+        return _raw_stream(_device())
     if _torch is None:
         import torch
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         _torch = torch
     if _raw_stream is None or not _torch.cuda.is_initialized():
         return _torch.cuda.current_stream().cuda_stream
-    return _raw_stream(_torch._C._cuda_getDevice())
+    _device = _torch._C._cuda_getDevice
+    return _raw_stream(_device())
 
 
 def _ptrs(tensors, E: int):
@@ -406,7 +432,7 @@ class Fp8Matrix:
                                  f"got {tuple(t.shape)} {t.dtype}")
         self.q, self.scale, self.rows, self.cols, self.weight = q, scale, rows, cols, weight
         self.c = clearmoe_fp8(_ptr(q), _ptr(scale), rows, cols)
-        self.ref = ctypes.pointer(self.c)
+        self.ref, self.addr = ctypes.pointer(self.c), ctypes.addressof(self.c)
 
 
 def fp8_pitch(cols: int) -> int:
@@ -469,8 +495,9 @@ def clearmoe_fp8_quantize_rows(x, out: Fp8Matrix, gather=None, stream=None) -> N
     p, dt, ld = _matrix(x, out.rows if gather is None else None, out.cols, "x")
     if gather is not None and gather.numel() != out.rows:
         raise ValueError("gather must have one entry per row of out")
-    _check(lib().clearmoe_fp8_quantize_rows(p, dt, ld, _ptr(gather), out.ref, _stream(stream)),
-           "clearmoe_fp8_quantize_rows")
+    code = (_calls or _bind_calls()).quantize_rows(p, dt, ld, _ptr(gather), out.addr, _stream(stream))
+    if code:
+        raise ClearMoEError(code, "clearmoe_fp8_quantize_rows")
 
 
 def clearmoe_fp8_quantize_weight(W, out: Fp8Matrix, stream=None) -> None:
@@ -497,12 +524,21 @@ def _epilogue(bias, act, status, N):
 def clearmoe_fp8_gemm(A: Fp8Matrix, W: Fp8Matrix, out, bias=None, act: int = ACT_NONE, status=None, stream=None) -> None:
     """out = act(A W^T + bias). out: a [M x N] bf16 or fp32 tensor of any row pitch, or an Fp8Matrix of rows (the
     result quantised, clearmoe_fp8_gemm_fp8)."""
-    epi = _epilogue(bias, act, status, W.rows)
+    calls = _calls or _bind_calls()
+    bp, bdt = None, F32
+    if bias is not None:
+        if bias.numel() != W.rows:
+            raise ValueError(f"bias must have {W.rows} elements, got {bias.numel()}")
+        bp, bdt = _ptr(bias), _dtype(bias)
     if isinstance(out, Fp8Matrix):
-        _check(lib().clearmoe_fp8_gemm_fp8(A.ref, W.ref, epi, out.ref, _stream(stream)), "clearmoe_fp8_gemm_fp8")
+        code = calls.gemm_fp8(A.addr, W.addr, bp, bdt, act, _ptr(status), out.addr, _stream(stream))
+        if code:
+            raise ClearMoEError(code, "clearmoe_fp8_gemm_fp8")
         return
     p, dt, ld = _matrix(out, A.rows, W.rows, "out")
-    _check(lib().clearmoe_fp8_gemm(A.ref, W.ref, epi, p, dt, ld, _stream(stream)), "clearmoe_fp8_gemm")
+    code = calls.gemm(A.addr, W.addr, bp, bdt, act, _ptr(status), p, dt, ld, _stream(stream))
+    if code:
+        raise ClearMoEError(code, "clearmoe_fp8_gemm")
 
 
 def clearmoe_fp8_grouped_gemm(A: Fp8Matrix, W, offsets, out, perm=None, bias=None, act: int = ACT_NONE, status=None,
@@ -527,7 +563,8 @@ class FfnWeights:
     """A folded layer's weights bound once (clearmoe_ffn_weights), with the tensors kept alive."""
 
     def __init__(self, c, keep):
-        self.c, self.keep, self.ref = c, keep, ctypes.pointer(c)
+        self.c, self.keep = c, keep
+        self.ref, self.addr = ctypes.pointer(c), ctypes.addressof(c)
 
 
 def ffn_weights(W1, b1, W_comb, Wg, bg, b2=None, W2=None, cls_stride: int = 0,
@@ -568,11 +605,13 @@ def ffn_weights(W1, b1, W_comb, Wg, bg, b2=None, W2=None, cls_stride: int = 0,
 
 def clearmoe_ffn_forward_few(layer: int, x, w: FfnWeights, out, stream=None) -> None:
     """The whole folded layer for 1 to FEW_MAX tokens."""
-    _check(lib().clearmoe_ffn_forward_few(layer, _ptr(x), x.shape[0], w.ref, _ptr(out), _stream(stream)),
-           "clearmoe_ffn_forward_few")
+    code = (_calls or _bind_calls()).ffn_few(layer, _ptr(x), x.shape[0], w.addr, _ptr(out), _stream(stream))
+    if code:
+        raise ClearMoEError(code, "clearmoe_ffn_forward_few")
 
 
 def clearmoe_ffn_forward_fp8(layer: int, x, w: FfnWeights, out, stream=None) -> None:
     """The whole folded layer with both products in 8-bit blocks."""
-    _check(lib().clearmoe_ffn_forward_fp8(layer, _ptr(x), x.shape[0], w.ref, _ptr(out), _stream(stream)),
-           "clearmoe_ffn_forward_fp8")
+    code = (_calls or _bind_calls()).ffn_fp8(layer, _ptr(x), x.shape[0], w.addr, _ptr(out), _stream(stream))
+    if code:
+        raise ClearMoEError(code, "clearmoe_ffn_forward_fp8")
