@@ -430,9 +430,11 @@ typedef struct {
 /* The whole folded layer for a few tokens, 1 <= T <= CLEARMOE_FEW_MAX: y_t = W_comb[a_t] GELU(W1 x_t + b1)
  * (+ b2), a_t as clearmoe_route's, in two launches: one takes every token through the router and fc1, the other
  * through its expert; only experts that have a token are read. Weights of the layer's dtype or 8-bit blocks
- * (bf16 layers; the weights' values times unquantised activations). Sums in fp32; z is stored in the layer's
- * dtype as in the other forwards; fp32 layers use three TF32 products per term (relative error near 2^-21). The
- * routing can be read with clearmoe_get_routing. Errors as clearmoe_ffn_forward_folded_ex. */
+ * (bf16 layers; the weights' values times unquantised activations). Sums in fp32; z is stored in the layer's dtype
+ * as in the other forwards, of up to 16 tokens of bf16 layers in two bf16 parts (16 bits of significand); fp32 layers
+ * use three TF32 products per term (relative error near 2^-21, and NaN where an infinity's remainder is formed). The
+ * routing can be read with clearmoe_get_routing. Errors as clearmoe_ffn_forward_folded_ex; EUNSUPPORTED for more
+ * tokens, and for 8-bit weights with hidden > 589,824. */
 #define CLEARMOE_FEW_MAX 64
 int clearmoe_ffn_forward_few(clearmoe_layer* layer, const void* x, int64_t T, const clearmoe_ffn_weights* w, void* out,
                              void* stream);

@@ -120,12 +120,15 @@ Fp8Workspace fp8_workspace_at(void* base, int64_t T, int64_t d, int64_t H) {
 Fp8Workspace fp8_workspace(const clearmoe_layer* L, int64_t T) {
     return fp8_workspace_at(L->z, T, L->desc.d, L->desc.hidden);
 }
-// Bytes of the hidden-state workspace: z in the layer's dtype, or (bf16 layers of narrow H, whose rows of 8-bit
-// blocks are padded to 128) x and z in 8-bit blocks where those take more.
+// Bytes of the hidden-state workspace: z in the layer's dtype, or (bf16 layers) what takes more of x and z in 8-bit
+// blocks, whose rows are padded to 128, and a few tokens' z in two parts (16 at most are).
 size_t z_bytes(const clearmoe_layer_desc& D, size_t esz) {
-    const size_t plain = (size_t)D.max_tokens * D.hidden * esz;
-    const size_t blocks = D.dtype == CLEARMOE_BF16 ? fp8_workspace_at(nullptr, D.max_tokens, D.d, D.hidden).bytes : 0;
-    return plain > blocks ? plain : blocks;
+    size_t n = (size_t)D.max_tokens * D.hidden * esz;
+    if (D.dtype != CLEARMOE_BF16) return n;
+    const int64_t few = D.max_tokens < CLEARMOE_FEW_MAX ? D.max_tokens : CLEARMOE_FEW_MAX;
+    for (const size_t m : {fp8_workspace_at(nullptr, D.max_tokens, D.d, D.hidden).bytes, (size_t)(2 * few * D.hidden) * esz})
+        if (m > n) n = m;
+    return n;
 }
 
 int check_common(const clearmoe_layer* L, const void* x, int64_t T) {

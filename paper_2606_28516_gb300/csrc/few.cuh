@@ -268,12 +268,23 @@ __device__ __forceinline__ void few_stage(float* red, const float (&acc)[NT][4],
         p[16 + g + 8] = acc[j][3];
     }
 }
-// Their sum over the warps, in warp order.
+// The same where each pair of columns is one token's two parts: their sums, [warp][4 NT tokens][16 rows].
 template <int NT>
+__device__ __forceinline__ void few_stage_pairs(float* red, const float (&acc)[NT][4], int warp, int lane) {
+    const int g = lane >> 2, c = lane & 3;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        float* p = red + ((warp * NT + j) * 4 + c) * 16;
+        p[g] = acc[j][0] + acc[j][1];
+        p[g + 8] = acc[j][2] + acc[j][3];
+    }
+}
+// The sum over the warps of column col of COLS, in warp order.
+template <int COLS>
 __device__ __forceinline__ float few_sum(const float* red, int col, int row) {
     float s = 0.f;
 #pragma unroll
-    for (int w = 0; w < FEW_WARPS; ++w) s += red[(w * NT * 8 + col) * 16 + row];
+    for (int w = 0; w < FEW_WARPS; ++w) s += red[(w * COLS + col) * 16 + row];
     return s;
 }
 

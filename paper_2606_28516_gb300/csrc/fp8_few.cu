@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) fp8_few_kernel(const __grid_co
     for (int i = threadIdx.x; i < M * 16; i += FEW_THREADS) {
         const int m = i >> 4, n = r0 + (i & 15);
         if (n >= a.N) continue;
-        float s = few_sum<NT>(red, m, i & 15);
+        float s = few_sum<8 * NT>(red, m, i & 15);
         if (a.bias)
             s += a.bias_bf16 ? bf16_to_f32(__ldcg(static_cast<const uint16_t*>(a.bias) + n)) : __ldcg(static_cast<const float*>(a.bias) + n);
         if (a.act == CLEARMOE_ACT_GELU) s = gelu_erf(s);

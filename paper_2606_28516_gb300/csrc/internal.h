@@ -376,7 +376,7 @@ struct FewArgs {
     const void* bg;
     int64_t cls_stride;
     int ln;
-    void* z;       // [T x H] layer dtype
+    void* z;       // [T x H] layer dtype; up to 16 tokens, bf16: [2][T x H]
     int32_t* idx;  // [T]
     int32_t* counts;
     int32_t* offsets;

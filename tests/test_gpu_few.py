@@ -242,3 +242,32 @@ def test_refusals():
         cm.ffn_weights(Q.m[0], Q.b1, F.m[1:3], Q.Wg, Q.bg)
     F.close()
     Q.close()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+@pytest.mark.parametrize("T,E", [(1, 1), (1, 4), (4, 2), (5, 1), (9, 3), (16, 1), (16, 8)])
+def test_up_to_16_tokens_keep_z(kind, T, E):
+    """Two bf16 parts of z: against float64 with z as it is, each output within its own rounding (2^-8 of it at the most) and what
+    fp32 sums and 2^-17 of each z can do; z rounded to bf16 alone moves most of them further. The same from a handle for
+    exactly these tokens."""
+    d, H = 192, 768
+    outs = []
+    for T_max in (64, T):
+        L = Layer(kind, d, H, E, seed=T + E, b2=True, T=T_max)
+        x = L.tokens(T)
+        out = torch.full((T, d), float("nan"), device="cuda", dtype=L.tdt)
+        cm.clearmoe_ffn_forward_few(L.h, x, L.w, out)
+        outs.append(out)
+        a, _ = L.reference(x)
+        v, W1 = x.double(), L.m64[0]
+        u = v @ W1.T + L.b1.double()
+        z = 0.5 * u * torch.erfc(-u / np.sqrt(2.0))
+        du = (d / 16 + 16) * 2.0 ** -23 * (v.abs() @ W1.abs().T + L.b1.double().abs())
+        dz = 1.13 * du + 4e-7 + 4e-7 * z.abs() + 2.0 ** -17 * z.abs()
+        y = torch.stack([L.m64[1 + e] @ z[t] for t, e in enumerate(a.tolist())]) + L.b2.double()
+        mag = torch.stack([L.m64[1 + e].abs() @ (dz + (H / 16 + 16) * 2.0 ** -23 * z.abs())[t] for t, e in enumerate(a.tolist())])
+        assert bool(((out.double() - y).abs() <= 2.0 ** -8 * y.abs() + 1.01 * mag + 1e-6).all())
+        rounded = torch.stack([L.m64[1 + e] @ z.to(torch.bfloat16).double()[t] for t, e in enumerate(a.tolist())]) + L.b2.double()
+        assert bool(((rounded - y).abs() > mag).double().mean() > 0.5)
+        L.close()
+    assert torch.equal(*outs)
