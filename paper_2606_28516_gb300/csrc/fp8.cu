@@ -49,25 +49,18 @@ __device__ __forceinline__ void load8(const T* row, int64_t k, int64_t K, float 
 }
 
 // Activations. Eight lanes take a block of 128 columns, 16 consecutive ones a lane, so that a lane's conversions
-// share one scale and its largest magnitude takes three shuffles to become the block's; a lane has Q_UNITS blocks'
-// loads in flight. Bound by HBM: each element is read once and written once as a byte.
-// Measured (16,384 x 4,096 bf16, 202 MB): 50 us with a half warp per block, eight columns a lane, a masked redux
-// and integer magnitudes (19 instructions an element); 36 us with this.
+// share one scale and its largest magnitude takes three shuffles to become the block's. Bound by HBM: each element is read
+// once and written once as a byte; small blocks and many CTAs keep the loads coming. Measured (16,384 x 4,096 bf16, 202 MB):
+// 50 us with a half warp per block, eight columns a lane, a masked redux and integer magnitudes (19 instructions an
+// element); 37 us in fp32 with two blocks' loads a lane in flight and 8 CTAs an SM (12 instructions); 30 us (6.7 TB/s) with
+// the bf16 words taken two values at a time, a block a lane and 32 CTAs an SM (16: 31 us).
 constexpr int Q_THREADS = 256;
-constexpr int Q_UNITS = 2;
+constexpr int Q_CTAS = 32;  // an SM, at the most
 constexpr int Q_CTA_BLOCKS = Q_THREADS / 8;
 constexpr int Q_PITCH = 132;
 
-// A lane's 16 values of a block: through the LayerNorm (LN: st of its row), to e4m3 at q, the block's scale byte at scale.
-template <bool LN>
-__device__ __forceinline__ void quantize_block(float (&v)[2][8], float2 st, int64_t k, int64_t K, int l8, bool write, uint8_t* q,
-                                               uint8_t* scale) {
-    if (LN) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int c = 0; c < 8; ++c) v[h][c] = k + 8 * h + c < K ? (v[h][c] - st.x) * st.y : 0.f;
-    }
+// A lane's 16 values of a block to e4m3 at q, the block's scale byte at scale.
+__device__ __forceinline__ void quantize_block(float (&v)[2][8], int l8, bool write, uint8_t* q, uint8_t* scale) {
     float m = 0.f;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -89,7 +82,66 @@ __device__ __forceinline__ void quantize_block(float (&v)[2][8], float2 st, int6
     }
 }
 
-template <typename T, bool VEC>
+// Aligned bf16 rows as they are loaded, two values a word: 16 of a block a lane, zeros past K.
+__device__ __forceinline__ void load16_bf16(const uint16_t* row, int k, int64_t K, bool live, uint4 (&r)[2]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        r[h] = make_uint4(0, 0, 0, 0);
+        if (live && k + 8 * h < K) r[h] = __ldcg(reinterpret_cast<const uint4*>(row + k) + h);
+    }
+}
+__device__ __forceinline__ uint32_t max_abs_bf16x2(uint32_t a, uint32_t b) {  // each half's; NaN if either is
+    uint32_t r;
+    asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// quantize_block on such words: magnitudes and scaling two values an instruction, both exact in bf16 (the scale is a power
+// of two; what it takes below bf16's range is far below e4m3's), so that only the conversion takes them one by one.
+__device__ __forceinline__ void quantize_block_bf16(const uint4 (&r)[2], int l8, bool write, uint8_t* q, uint8_t* scale) {
+    const uint32_t w[8] = {r[0].x, r[0].y, r[0].z, r[0].w, r[1].x, r[1].y, r[1].z, r[1].w};
+    uint32_t m = max_abs_bf16x2(max_abs_bf16x2(max_abs_bf16x2(w[0], w[1]), max_abs_bf16x2(w[2], w[3])),
+                                max_abs_bf16x2(max_abs_bf16x2(w[4], w[5]), max_abs_bf16x2(w[6], w[7])));
+#pragma unroll
+    for (int o = 4; o; o >>= 1) m = max_abs_bf16x2(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+    const uint32_t s = fp8_scale_byte((max_abs_bf16x2(m, __byte_perm(m, m, 0x1032)) & 0x7FFFu) << 16);
+    const uint32_t inv = __byte_perm(__float_as_uint(fp8_inverse_scale(s)), 0, 0x3232);
+    uint32_t o[4];
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+        uint32_t a, b;
+        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(w[2 * h]), "r"(inv));
+        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(b) : "r"(w[2 * h + 1]), "r"(inv));
+        o[h] = fp8_pack4(bf16_lo(a), bf16_hi(a), bf16_lo(b), bf16_hi(b));
+    }
+    if (write) {
+        *reinterpret_cast<uint4*>(q) = make_uint4(o[0], o[1], o[2], o[3]);
+        if (l8 == 0) *scale = (uint8_t)s;
+    }
+}
+
+// Aligned bf16 rows.
+__global__ void __launch_bounds__(Q_THREADS) quantize_bf16_kernel(const QuantArgs a) {
+    pdl_launch_dependents();
+    const int l8 = threadIdx.x & 7;
+    const int64_t b0 = (int64_t)blockIdx.x * Q_CTA_BLOCKS + (threadIdx.x >> 3), step = (int64_t)gridDim.x * Q_CTA_BLOCKS;
+    int64_t row = b0 / a.kb;
+    int kb = (int)(b0 - row * a.kb);
+    const int64_t step_row = step / a.kb;
+    const int step_kb = (int)(step - step_row * a.kb);
+    pdl_wait();
+    while (__any_sync(0xFFFFFFFFu, row < a.rows)) {
+        const bool live = row < a.rows;
+        const int64_t src = a.gather && live ? (int64_t)__ldcg(a.gather + row) : row;
+        uint4 r[2];
+        load16_bf16(static_cast<const uint16_t*>(a.x) + src * a.ld, kb * 128 + l8 * 16, a.K, live, r);
+        quantize_block_bf16(r, l8, live, a.q + row * a.ldq + kb * 128 + l8 * 16, a.scale + row * a.lds + kb);
+        row += step_row;
+        kb += step_kb;
+        if (kb >= a.kb) kb -= a.kb, ++row;
+    }
+}
+
+template <typename T, bool VEC, int UNITS>
 __global__ void __launch_bounds__(Q_THREADS) quantize_rows_kernel(const QuantArgs a) {
     // rows that are not 16-byte aligned go through shared memory, so that a load's lanes read consecutive elements
     __shared__ __align__(16) float s_x[VEC ? 1 : Q_THREADS / 32][VEC ? 1 : 4 * Q_PITCH];
@@ -98,13 +150,13 @@ __global__ void __launch_bounds__(Q_THREADS) quantize_rows_kernel(const QuantArg
     const int64_t blocks = a.rows * a.kb;
     const bool narrow = blocks <= 0xFFFFFFFFll;
     pdl_wait();
-    for (int64_t b0 = (int64_t)blockIdx.x * (Q_CTA_BLOCKS * Q_UNITS) + (threadIdx.x >> 3);
-         b0 - (int)(threadIdx.x >> 3) < blocks; b0 += (int64_t)gridDim.x * (Q_CTA_BLOCKS * Q_UNITS)) {
-        float v[Q_UNITS][2][8];
-        int64_t row[Q_UNITS];
-        int kb[Q_UNITS];
+    for (int64_t b0 = (int64_t)blockIdx.x * (Q_CTA_BLOCKS * UNITS) + (threadIdx.x >> 3);
+         b0 - (int)(threadIdx.x >> 3) < blocks; b0 += (int64_t)gridDim.x * (Q_CTA_BLOCKS * UNITS)) {
+        float v[UNITS][2][8];
+        int64_t row[UNITS];
+        int kb[UNITS];
 #pragma unroll
-        for (int i = 0; i < Q_UNITS; ++i) {
+        for (int i = 0; i < UNITS; ++i) {
             const int64_t b = min(b0 + i * Q_CTA_BLOCKS, blocks - 1);  // past the end: the last block again
             row[i] = narrow ? (int64_t)((uint32_t)b / (uint32_t)a.kb) : b / a.kb;
             kb[i] = (int)(b - row[i] * a.kb);
@@ -139,10 +191,9 @@ __global__ void __launch_bounds__(Q_THREADS) quantize_rows_kernel(const QuantArg
             }
         }
 #pragma unroll
-        for (int i = 0; i < Q_UNITS; ++i) {
+        for (int i = 0; i < UNITS; ++i) {
             const int64_t k = (int64_t)kb[i] * 128 + l8 * 16;
-            quantize_block<false>(v[i], make_float2(0.f, 1.f), k, a.K, l8, b0 + i * Q_CTA_BLOCKS < blocks, a.q + row[i] * a.ldq + k,
-                               a.scale + row[i] * a.lds + kb[i]);
+            quantize_block(v[i], l8, b0 + i * Q_CTA_BLOCKS < blocks, a.q + row[i] * a.ldq + k, a.scale + row[i] * a.lds + kb[i]);
         }
     }
 }
@@ -231,26 +282,27 @@ __global__ void __launch_bounds__(SQ_THREADS, 2) slots_quantize_kernel(const Rou
         }
         __syncthreads();
         const int blocks = n * a.kb;
-        for (int b0 = tid >> 3; b0 - (tid >> 3) < blocks; b0 += Q_UNITS * per) {
-            float v[Q_UNITS][2][8];
-            float2 st[Q_UNITS];
-            int row[Q_UNITS], kb[Q_UNITS];
+        for (int b = tid >> 3; b - (tid >> 3) < blocks; b += per) {
+            const int row = (int)((uint32_t)b / (uint32_t)a.kb), kb = b - row * a.kb, k = kb * 128 + l8 * 16;
+            const bool live = row < n;
+            const int64_t tok = row0 + i0 + (int64_t)row * split;
+            const int slot = live ? s_slot[row] : -1;
+            uint4 w[2];
+            load16_bf16(static_cast<const uint16_t*>(a.x) + tok * a.ld, k, a.K, live, w);
+            uint8_t* q = a.q + (int64_t)slot * a.ldq + k;
+            uint8_t* scale = a.scale + (int64_t)slot * a.lds + kb;
+            if (LN) {
+                const float2 st = live ? __ldcg(a.ln_stats + tok) : make_float2(0.f, 0.f);
+                const uint32_t u[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w};
+                float v[2][8];
 #pragma unroll
-            for (int i = 0; i < Q_UNITS; ++i) {
-                const int b = min(b0 + i * per, blocks - 1);  // past the end: the last block again
-                row[i] = (int)((uint32_t)b / (uint32_t)a.kb);
-                kb[i] = b - row[i] * a.kb;
-                const int64_t tok = row0 + i0 + (int64_t)row[i] * split;
-                const uint16_t* x = static_cast<const uint16_t*>(a.x) + tok * a.ld;
-                load8<uint16_t, true>(x, kb[i] * 128 + l8 * 16, a.K, v[i][0]);
-                load8<uint16_t, true>(x, kb[i] * 128 + l8 * 16 + 8, a.K, v[i][1]);
-                if (LN) st[i] = __ldcg(a.ln_stats + tok);
-            }
-#pragma unroll
-            for (int i = 0; i < Q_UNITS; ++i) {
-                const int k = kb[i] * 128 + l8 * 16, slot = s_slot[row[i]];
-                quantize_block<LN>(v[i], st[i], k, a.K, l8, b0 + i * per < blocks && slot >= 0, a.q + (int64_t)slot * a.ldq + k,
-                                   a.scale + (int64_t)slot * a.lds + kb[i]);
+                for (int c = 0; c < 16; ++c) {
+                    const float f = c & 1 ? bf16_hi(u[c >> 1]) : bf16_lo(u[c >> 1]);
+                    v[c >> 3][c & 7] = k + c < a.K ? (f - st.x) * st.y : 0.f;
+                }
+                quantize_block(v, l8, slot >= 0, q, scale);
+            } else {
+                quantize_block_bf16(w, l8, slot >= 0, q, scale);
             }
         }
         __syncthreads();
@@ -334,16 +386,20 @@ bool vec_ok(const QuantArgs& a, int esz) {
 }  // namespace
 
 cudaError_t launch_quantize_rows(const QuantArgs& a, int dtype, int num_sms, cudaStream_t s) {
-    const int esz = dtype == CLEARMOE_BF16 ? 2 : 4;
-    const int64_t want = (a.rows * a.kb + Q_CTA_BLOCKS * Q_UNITS - 1) / (Q_CTA_BLOCKS * Q_UNITS);
-    const int64_t grid = want < (int64_t)num_sms * 8 ? want : (int64_t)num_sms * 8;
-    const bool vec = vec_ok(a, esz);
-    if (dtype == CLEARMOE_BF16) {
-        return vec ? launch(quantize_rows_kernel<uint16_t, true>, dim3((unsigned)grid), Q_THREADS, s, a)
-                   : launch(quantize_rows_kernel<uint16_t, false>, dim3((unsigned)grid), Q_THREADS, s, a);
-    }
-    return vec ? launch(quantize_rows_kernel<float, true>, dim3((unsigned)grid), Q_THREADS, s, a)
-               : launch(quantize_rows_kernel<float, false>, dim3((unsigned)grid), Q_THREADS, s, a);
+    const bool bf16 = dtype == CLEARMOE_BF16, vec = vec_ok(a, bf16 ? 2 : 4);
+    const int64_t one = (a.rows * a.kb + Q_CTA_BLOCKS - 1) / Q_CTA_BLOCKS, most = (int64_t)num_sms * Q_CTAS;
+    const dim3 grid((unsigned)(one < most ? one : most));
+    if (vec && bf16) return launch(quantize_bf16_kernel, grid, Q_THREADS, s, a);
+    if (vec) return launch(quantize_rows_kernel<float, true, 1>, grid, Q_THREADS, s, a);
+    // Unaligned rows, whose CTAs have shared memory: where two blocks a thread make them one an SM, the product that
+    // follows fits beside them and starts early (1,001 x 777 x 1,131 fp32 with its product 9.8 us against 10.3; alone 4.5
+    // against 3.8, and 8,192 x 4,095 bf16 39.6 against 33.6).
+    const int64_t two = (one + 1) / 2;
+    if (two <= num_sms)
+        return bf16 ? launch(quantize_rows_kernel<uint16_t, false, 2>, dim3((unsigned)two), Q_THREADS, s, a)
+                    : launch(quantize_rows_kernel<float, false, 2>, dim3((unsigned)two), Q_THREADS, s, a);
+    return bf16 ? launch(quantize_rows_kernel<uint16_t, false, 1>, grid, Q_THREADS, s, a)
+                : launch(quantize_rows_kernel<float, false, 1>, grid, Q_THREADS, s, a);
 }
 
 cudaError_t launch_slots_quantize(const RouteArgs& r, int grid, int chunk, const QuantArgs& a, int num_sms, cudaStream_t s) {
