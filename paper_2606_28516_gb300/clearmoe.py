@@ -158,6 +158,11 @@ def _bind_calls():
     m.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in
              (L.clearmoe_fp8_quantize_rows, L.clearmoe_fp8_gemm, L.clearmoe_fp8_gemm_fp8, L.clearmoe_ffn_forward_few,
               L.clearmoe_ffn_forward_fp8)))
+    try:
+        import torch
+        m.bind_torch(torch.bfloat16, torch.float32, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+    except (ImportError, AttributeError):  # a torch without CUDA: every call then goes by integers
+        pass
     _calls = m
     return m
 
@@ -492,10 +497,13 @@ def _matrix(t, rows, cols, what):
 
 def clearmoe_fp8_quantize_rows(x, out: Fp8Matrix, gather=None, stream=None) -> None:
     """x [rows x cols] (bf16 or fp32, any row pitch) to out in 1 x 128 blocks; gather: int32 source rows."""
-    p, dt, ld = _matrix(x, out.rows if gather is None else None, out.cols, "x")
-    if gather is not None and gather.numel() != out.rows:
-        raise ValueError("gather must have one entry per row of out")
-    code = (_calls or _bind_calls()).quantize_rows(p, dt, ld, _ptr(gather), out.addr, _stream(stream))
+    calls = _calls or _bind_calls()
+    code = calls.quantize_rows_t(x, out.rows, out.cols, out.addr, stream) if gather is None else None
+    if code is None:
+        p, dt, ld = _matrix(x, out.rows if gather is None else None, out.cols, "x")
+        if gather is not None and gather.numel() != out.rows:
+            raise ValueError("gather must have one entry per row of out")
+        code = calls.quantize_rows(p, dt, ld, _ptr(gather), out.addr, _stream(stream))
     if code:
         raise ClearMoEError(code, "clearmoe_fp8_quantize_rows")
 
@@ -525,12 +533,19 @@ def clearmoe_fp8_gemm(A: Fp8Matrix, W: Fp8Matrix, out, bias=None, act: int = ACT
     """out = act(A W^T + bias). out: a [M x N] bf16 or fp32 tensor of any row pitch, or an Fp8Matrix of rows (the
     result quantised, clearmoe_fp8_gemm_fp8)."""
     calls = _calls or _bind_calls()
+    blocks = isinstance(out, Fp8Matrix)
+    if not blocks:
+        code = calls.gemm_t(A.addr, W.addr, A.rows, W.rows, act, bias, status, out, stream)
+        if code is not None:
+            if code:
+                raise ClearMoEError(code, "clearmoe_fp8_gemm")
+            return
     bp, bdt = None, F32
     if bias is not None:
         if bias.numel() != W.rows:
             raise ValueError(f"bias must have {W.rows} elements, got {bias.numel()}")
         bp, bdt = _ptr(bias), _dtype(bias)
-    if isinstance(out, Fp8Matrix):
+    if blocks:
         code = calls.gemm_fp8(A.addr, W.addr, bp, bdt, act, _ptr(status), out.addr, _stream(stream))
         if code:
             raise ClearMoEError(code, "clearmoe_fp8_gemm_fp8")
@@ -605,13 +620,19 @@ def ffn_weights(W1, b1, W_comb, Wg, bg, b2=None, W2=None, cls_stride: int = 0,
 
 def clearmoe_ffn_forward_few(layer: int, x, w: FfnWeights, out, stream=None) -> None:
     """The whole folded layer for 1 to FEW_MAX tokens."""
-    code = (_calls or _bind_calls()).ffn_few(layer, _ptr(x), x.shape[0], w.addr, _ptr(out), _stream(stream))
+    calls, T = _calls or _bind_calls(), x.shape[0]
+    code = calls.ffn_few_t(layer, T, w.addr, x, out, stream)
+    if code is None:
+        code = calls.ffn_few(layer, _ptr(x), T, w.addr, _ptr(out), _stream(stream))
     if code:
         raise ClearMoEError(code, "clearmoe_ffn_forward_few")
 
 
 def clearmoe_ffn_forward_fp8(layer: int, x, w: FfnWeights, out, stream=None) -> None:
     """The whole folded layer with both products in 8-bit blocks."""
-    code = (_calls or _bind_calls()).ffn_fp8(layer, _ptr(x), x.shape[0], w.addr, _ptr(out), _stream(stream))
+    calls, T = _calls or _bind_calls(), x.shape[0]
+    code = calls.ffn_fp8_t(layer, T, w.addr, x, out, stream)
+    if code is None:
+        code = calls.ffn_fp8(layer, _ptr(x), T, w.addr, _ptr(out), _stream(stream))
     if code:
         raise ClearMoEError(code, "clearmoe_ffn_forward_fp8")

@@ -1,7 +1,11 @@
-/* The calls of the 8-bit and few-token operators whose time the host bounds, as Python functions of integers (addresses,
- * sizes, codes; None for a null pointer). ctypes took 0.6 us for the arguments of such a call and as much again for the
- * epilogue's structure, of 4 to 6 us for the whole call. The functions are libclearmoe's, by the addresses that bind()
- * got; each returns its clearmoe_status and runs without the interpreter's lock. */
+/* The calls of the 8-bit and few-token operators whose time the host bounds. ctypes took 0.6 us for the arguments of such a
+ * call and as much again for the epilogue's structure, and the looks at tensors in Python as much as that, of 4 to 6 us
+ * for the whole call.
+ *
+ * quantize_rows, gemm, gemm_fp8, ffn_few, ffn_fp8 take integers (addresses, sizes, codes; None for a null pointer); the
+ * same names with _t take the tensors and return None, having called nothing, for an argument that is not as it should
+ * be, which the Python side then looks at and refuses. Otherwise each returns the clearmoe_status of libclearmoe's
+ * function, got by bind(), and runs it without the interpreter's lock. */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -103,8 +107,158 @@ static PyObject* ffn_fp8(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     return ffn(args, n, g_fp8);
 }
 
+/* ---- from tensors ---- */
+static PyObject *s_is_cuda, *s_shape, *s_stride, *s_data_ptr, *s_dtype, *s_is_contiguous, *s_numel, *s_cuda_stream;
+static PyObject *g_bf16, *g_f32, *g_get_device, *g_raw_stream; /* torch's dtypes; the current device; its current stream */
+
+/* bfloat16, float32, a function giving the current device, one giving a device's current stream */
+static PyObject* bind_torch(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    PyObject** to[4] = {&g_bf16, &g_f32, &g_get_device, &g_raw_stream};
+    (void)self;
+    if (n != 4) return PyErr_Format(PyExc_TypeError, "4 arguments expected, got %zd", n);
+    for (int i = 0; i < 4; ++i) {
+        Py_INCREF(args[i]);
+        Py_XSETREF(*to[i], args[i]);
+    }
+    Py_RETURN_NONE;
+}
+
+/* Each of these: 0 for an argument that is not as it should be, with no exception left. */
+static int yes(PyObject* o) { /* takes the reference */
+    const int r = o == Py_True;
+    if (!o) PyErr_Clear();
+    Py_XDECREF(o);
+    return r;
+}
+static int integer(PyObject* o, int64_t* v) { /* takes the reference */
+    if (!o) {
+        PyErr_Clear();
+        return 0;
+    }
+    *v = (int64_t)PyLong_AsUnsignedLongLongMask(o);
+    Py_DECREF(o);
+    if (*v == -1 && PyErr_Occurred()) {
+        PyErr_Clear();
+        return 0;
+    }
+    return 1;
+}
+static int pair(PyObject* o, int64_t* v) { /* takes the reference */
+    int ok = o && PyTuple_Check(o) && PyTuple_GET_SIZE(o) == 2;
+    for (int i = 0; i < 2 && ok; ++i) {
+        Py_INCREF(PyTuple_GET_ITEM(o, i));
+        ok = integer(PyTuple_GET_ITEM(o, i), v + i);
+    }
+    if (!o) PyErr_Clear();
+    Py_XDECREF(o);
+    return ok;
+}
+static int dtype_of(PyObject* t, int32_t* dt) {
+    PyObject* o = PyObject_GetAttr(t, s_dtype);
+    const int ok = o && (o == g_bf16 || o == g_f32);
+    *dt = o == g_bf16 ? CLEARMOE_BF16 : CLEARMOE_F32;
+    if (!o) PyErr_Clear();
+    Py_XDECREF(o);
+    return ok;
+}
+/* A [rows x cols] matrix of any row pitch. */
+static int matrix(PyObject* t, int64_t rows, int64_t cols, int64_t* p, int32_t* dt, int64_t* ld) {
+    int64_t shape[2], stride[2];
+    if (!yes(PyObject_GetAttr(t, s_is_cuda)) || !pair(PyObject_GetAttr(t, s_shape), shape) || shape[0] != rows || shape[1] != cols ||
+        !pair(PyObject_CallMethodNoArgs(t, s_stride), stride) || (cols > 1 && stride[1] != 1) || !dtype_of(t, dt))
+        return 0;
+    *ld = rows > 1 || stride[0] > cols ? stride[0] : cols;
+    return integer(PyObject_CallMethodNoArgs(t, s_data_ptr), p);
+}
+/* A dense tensor, or None. */
+static int dense(PyObject* t, int64_t* p) {
+    *p = 0;
+    return t == Py_None || (yes(PyObject_GetAttr(t, s_is_cuda)) && yes(PyObject_CallMethodNoArgs(t, s_is_contiguous)) &&
+                            integer(PyObject_CallMethodNoArgs(t, s_data_ptr), p));
+}
+static int bias_of(PyObject* t, int64_t n, int64_t* p, int32_t* dt) {
+    int64_t numel;
+    *dt = CLEARMOE_F32;
+    if (t == Py_None) {
+        *p = 0;
+        return 1;
+    }
+    return integer(PyObject_CallMethodNoArgs(t, s_numel), &numel) && numel == n && dense(t, p) && dtype_of(t, dt);
+}
+static int stream_of(PyObject* stream, int64_t* s) {
+    if (!g_raw_stream) return 0;
+    if (stream != Py_None) return integer(PyObject_GetAttr(stream, s_cuda_stream), s);
+    PyObject* d = PyObject_CallNoArgs(g_get_device);
+    PyObject* r = d ? PyObject_CallOneArg(g_raw_stream, d) : NULL;
+    Py_XDECREF(d);
+    return integer(r, s);
+}
+#define AT(x) ((void*)(intptr_t)(x))
+
+/* x, rows, cols, out, stream */
+static PyObject* quantize_rows_t(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    int64_t v[3], x, ld, s;
+    int32_t dt;
+    int rc;
+    (void)self;
+    if (n != 5) return PyErr_Format(PyExc_TypeError, "5 arguments expected, got %zd", n);
+    if (!integers(args + 1, 3, 3, v)) return NULL;
+    if (!stream_of(args[4], &s) || !matrix(args[0], v[0], v[1], &x, &dt, &ld)) Py_RETURN_NONE;
+    Py_BEGIN_ALLOW_THREADS
+    rc = g_quantize_rows(AT(x), dt, ld, NULL, PTR(2), AT(s));
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+/* A, W, rows, cols, act, bias, status, out, stream */
+static PyObject* gemm_t(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    int64_t v[5], bias, status, out, ld, s;
+    int32_t bias_dt, dt;
+    int rc;
+    (void)self;
+    if (n != 9) return PyErr_Format(PyExc_TypeError, "9 arguments expected, got %zd", n);
+    if (!integers(args, 5, 5, v)) return NULL;
+    if (!stream_of(args[8], &s) || !bias_of(args[5], v[3], &bias, &bias_dt) || !dense(args[6], &status) ||
+        !matrix(args[7], v[2], v[3], &out, &dt, &ld))
+        Py_RETURN_NONE;
+    const clearmoe_fp8_epilogue epi = {AT(bias), bias_dt, (int32_t)v[4], AT(status)};
+    Py_BEGIN_ALLOW_THREADS
+    rc = g_gemm(PTR(0), PTR(1), &epi, AT(out), dt, ld, AT(s));
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+/* layer, T, weights, x, out, stream */
+static PyObject* ffn_t(PyObject* const* args, Py_ssize_t n,
+                       int (*fn)(clearmoe_layer*, const void*, int64_t, const clearmoe_ffn_weights*, void*, void*)) {
+    int64_t v[3], x, out, s;
+    int rc;
+    if (n != 6) return PyErr_Format(PyExc_TypeError, "6 arguments expected, got %zd", n);
+    if (!integers(args, 3, 3, v)) return NULL;
+    if (!stream_of(args[5], &s) || !dense(args[3], &x) || !dense(args[4], &out)) Py_RETURN_NONE;
+    Py_BEGIN_ALLOW_THREADS
+    rc = fn(PTR(0), AT(x), v[1], PTR(2), AT(out), AT(s));
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+static PyObject* ffn_few_t(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    (void)self;
+    return ffn_t(args, n, g_few);
+}
+static PyObject* ffn_fp8_t(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    (void)self;
+    return ffn_t(args, n, g_fp8);
+}
+
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, NULL}
-static PyMethodDef methods[] = {METHOD(bind),    METHOD(quantize_rows), METHOD(gemm), METHOD(gemm_fp8),
-                                METHOD(ffn_few), METHOD(ffn_fp8),       {NULL, NULL, 0, NULL}};
+static PyMethodDef methods[] = {METHOD(bind),      METHOD(bind_torch),      METHOD(quantize_rows), METHOD(gemm),
+                                METHOD(gemm_fp8),  METHOD(ffn_few),         METHOD(ffn_fp8),       METHOD(quantize_rows_t),
+                                METHOD(gemm_t),    METHOD(ffn_few_t),       METHOD(ffn_fp8_t),     {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", NULL, -1, methods, NULL, NULL, NULL, NULL};
-PyMODINIT_FUNC PyInit__calls(void) { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__calls(void) {
+    PyObject** names[] = {&s_is_cuda, &s_shape, &s_stride, &s_data_ptr, &s_dtype, &s_is_contiguous, &s_numel, &s_cuda_stream};
+    const char* text[] = {"is_cuda", "shape", "stride", "data_ptr", "dtype", "is_contiguous", "numel", "cuda_stream"};
+    for (int i = 0; i < 8; ++i)
+        if (!(*names[i] = PyUnicode_InternFromString(text[i]))) return NULL;
+    return PyModule_Create(&module);
+}
