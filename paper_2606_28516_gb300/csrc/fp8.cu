@@ -57,7 +57,6 @@ __device__ __forceinline__ void load8(const T* row, int64_t k, int64_t K, float 
 constexpr int Q_THREADS = 256;
 constexpr int Q_CTAS = 32;  // an SM, at the most
 constexpr int Q_CTA_BLOCKS = Q_THREADS / 8;
-constexpr int Q_PITCH = 132;
 
 // A lane's 16 values of a block to e4m3 at q, the block's scale byte at scale.
 __device__ __forceinline__ void quantize_block(float (&v)[2][8], int l8, bool write, uint8_t* q, uint8_t* scale) {
@@ -141,60 +140,62 @@ __global__ void __launch_bounds__(Q_THREADS) quantize_bf16_kernel(const QuantArg
     }
 }
 
-template <typename T, bool VEC, int UNITS>
+// Other rows: fp32, or not 16-byte aligned (VEC false).
+template <typename T, bool VEC>
 __global__ void __launch_bounds__(Q_THREADS) quantize_rows_kernel(const QuantArgs a) {
-    // rows that are not 16-byte aligned go through shared memory, so that a load's lanes read consecutive elements
-    __shared__ __align__(16) float s_x[VEC ? 1 : Q_THREADS / 32][VEC ? 1 : 4 * Q_PITCH];
+    // Unaligned rows go through shared memory, so that a load's lanes read consecutive elements: a block of the warp's four
+    // at a time, 16 columns a pitch of 20. (All four at once, 17 KB a CTA, kept the product that follows from starting
+    // beside it: 1,001 x 777 x 1,131 fp32 10.3 us for both.)
+    __shared__ __align__(16) float s_x[VEC ? 1 : Q_THREADS / 32][VEC ? 1 : 8 * 20];
     pdl_launch_dependents();
     const int l8 = threadIdx.x & 7, lane = threadIdx.x & 31;
-    const int64_t blocks = a.rows * a.kb;
-    const bool narrow = blocks <= 0xFFFFFFFFll;
+    const int64_t b0 = (int64_t)blockIdx.x * Q_CTA_BLOCKS + (threadIdx.x >> 3), step = (int64_t)gridDim.x * Q_CTA_BLOCKS;
+    int64_t row = b0 / a.kb;
+    int kb = (int)(b0 - row * a.kb);
+    const int64_t step_row = step / a.kb;
+    const int step_kb = (int)(step - step_row * a.kb);
     pdl_wait();
-    for (int64_t b0 = (int64_t)blockIdx.x * (Q_CTA_BLOCKS * UNITS) + (threadIdx.x >> 3);
-         b0 - (int)(threadIdx.x >> 3) < blocks; b0 += (int64_t)gridDim.x * (Q_CTA_BLOCKS * UNITS)) {
-        float v[UNITS][2][8];
-        int64_t row[UNITS];
-        int kb[UNITS];
+    while (__any_sync(0xFFFFFFFFu, row < a.rows)) {
+        const bool live = row < a.rows;
+        const int64_t src = a.gather && live ? (int64_t)__ldcg(a.gather + row) : row;
+        const T* x = static_cast<const T*>(a.x) + src * a.ld;
+        float v[2][8];
+        if (VEC) {
+            load8<T, VEC>(x, (int64_t)kb * 128 + l8 * 16, live ? a.K : 0, v[0]);
+            load8<T, VEC>(x, (int64_t)kb * 128 + l8 * 16 + 8, live ? a.K : 0, v[1]);
+        } else {
+            float* sx = s_x[VEC ? 0 : threadIdx.x >> 5];
+            float f[16];
 #pragma unroll
-        for (int i = 0; i < UNITS; ++i) {
-            const int64_t b = min(b0 + i * Q_CTA_BLOCKS, blocks - 1);  // past the end: the last block again
-            row[i] = narrow ? (int64_t)((uint32_t)b / (uint32_t)a.kb) : b / a.kb;
-            kb[i] = (int)(b - row[i] * a.kb);
-            const int64_t src = a.gather ? (int64_t)__ldcg(a.gather + row[i]) : row[i];
-            const T* x = static_cast<const T*>(a.x) + src * a.ld;
-            if (VEC) {
-                load8<T, VEC>(x, (int64_t)kb[i] * 128 + l8 * 16, a.K, v[i][0]);
-                load8<T, VEC>(x, (int64_t)kb[i] * 128 + l8 * 16 + 8, a.K, v[i][1]);
-            } else {
-                float* sx = s_x[VEC ? 0 : threadIdx.x >> 5];
-                float f[16];
+            for (int b = 0; b < 4; ++b) {  // the warp's four blocks
+                const T* p = reinterpret_cast<const T*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(x), 8 * b));
+                const int64_t k = (int64_t)__shfl_sync(0xFFFFFFFFu, live ? kb : a.kb, 8 * b) * 128 + lane;
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {  // the warp's four blocks
-                    const T* p = reinterpret_cast<const T*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(x), 8 * b));
-                    const int64_t k = (int64_t)__shfl_sync(0xFFFFFFFFu, kb[i], 8 * b) * 128 + lane;
+                for (int c = 0; c < 4; ++c)
+                    f[4 * b + c] = k + 32 * c >= a.K  ? 0.f
+                                   : sizeof(T) == 2 ? bf16_to_f32(__ldcg(reinterpret_cast<const uint16_t*>(p) + k + 32 * c))
+                                                    : __ldcg(reinterpret_cast<const float*>(p) + k + 32 * c);
+            }
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        f[4 * b + c] = k + 32 * c >= a.K  ? 0.f
-                                       : sizeof(T) == 2 ? bf16_to_f32(__ldcg(reinterpret_cast<const uint16_t*>(p) + k + 32 * c))
-                                                        : __ldcg(reinterpret_cast<const float*>(p) + k + 32 * c);
-                }
+            for (int b = 0; b < 4; ++b) {
                 __syncwarp();
 #pragma unroll
-                for (int c = 0; c < 16; ++c) sx[(c >> 2) * Q_PITCH + (c & 3) * 32 + lane] = f[c];
+                for (int c = 0; c < 4; ++c) sx[(2 * c + (lane >> 4)) * 20 + (lane & 15)] = f[4 * b + c];
                 __syncwarp();
+                if (lane >> 3 != b) continue;
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    const float4 q = *reinterpret_cast<const float4*>(sx + (lane >> 3) * Q_PITCH + l8 * 16 + 4 * c);
-                    float* o = v[i][c >> 1] + (c & 1) * 4;
+                    const float4 q = *reinterpret_cast<const float4*>(sx + l8 * 20 + 4 * c);
+                    float* o = v[c >> 1] + (c & 1) * 4;
                     o[0] = q.x, o[1] = q.y, o[2] = q.z, o[3] = q.w;
                 }
             }
+            __syncwarp();
         }
-#pragma unroll
-        for (int i = 0; i < UNITS; ++i) {
-            const int64_t k = (int64_t)kb[i] * 128 + l8 * 16;
-            quantize_block(v[i], l8, b0 + i * Q_CTA_BLOCKS < blocks, a.q + row[i] * a.ldq + k, a.scale + row[i] * a.lds + kb[i]);
-        }
+        quantize_block(v, l8, live, a.q + row * a.ldq + kb * 128 + l8 * 16, a.scale + row * a.lds + kb);
+        row += step_row;
+        kb += step_kb;
+        if (kb >= a.kb) kb -= a.kb, ++row;
     }
 }
 
@@ -390,16 +391,9 @@ cudaError_t launch_quantize_rows(const QuantArgs& a, int dtype, int num_sms, cud
     const int64_t one = (a.rows * a.kb + Q_CTA_BLOCKS - 1) / Q_CTA_BLOCKS, most = (int64_t)num_sms * Q_CTAS;
     const dim3 grid((unsigned)(one < most ? one : most));
     if (vec && bf16) return launch(quantize_bf16_kernel, grid, Q_THREADS, s, a);
-    if (vec) return launch(quantize_rows_kernel<float, true, 1>, grid, Q_THREADS, s, a);
-    // Unaligned rows, whose CTAs have shared memory: where two blocks a thread make them one an SM, the product that
-    // follows fits beside them and starts early (1,001 x 777 x 1,131 fp32 with its product 9.8 us against 10.3; alone 4.5
-    // against 3.8, and 8,192 x 4,095 bf16 39.6 against 33.6).
-    const int64_t two = (one + 1) / 2;
-    if (two <= num_sms)
-        return bf16 ? launch(quantize_rows_kernel<uint16_t, false, 2>, dim3((unsigned)two), Q_THREADS, s, a)
-                    : launch(quantize_rows_kernel<float, false, 2>, dim3((unsigned)two), Q_THREADS, s, a);
-    return bf16 ? launch(quantize_rows_kernel<uint16_t, false, 1>, grid, Q_THREADS, s, a)
-                : launch(quantize_rows_kernel<float, false, 1>, grid, Q_THREADS, s, a);
+    if (bf16) return launch(quantize_rows_kernel<uint16_t, false>, grid, Q_THREADS, s, a);
+    return vec ? launch(quantize_rows_kernel<float, true>, grid, Q_THREADS, s, a)
+               : launch(quantize_rows_kernel<float, false>, grid, Q_THREADS, s, a);
 }
 
 cudaError_t launch_slots_quantize(const RouteArgs& r, int grid, int chunk, const QuantArgs& a, int num_sms, cudaStream_t s) {
