@@ -1394,6 +1394,7 @@ int clearmoe_ffn_forward_few(clearmoe_layer* L, const void* x, int64_t T, const 
     a.H = L->desc.hidden;
     a.E = w->E;
     a.G = w->E + (w->cls_stride > 0 ? 1 : 0);
+    a.num_sms = L->num_sms;
     a.f32 = L->desc.dtype == CLEARMOE_F32;
     a.fp8 = w->dtype == CLEARMOE_FP8;
     a.W1 = w->W1.q;

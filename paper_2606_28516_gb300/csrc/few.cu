@@ -143,7 +143,7 @@ template <int V>
 __device__ __forceinline__ void few_scales(uint8_t* dst, const uint8_t* s, int r0, int K) {
     if (V != FEWV_W8A16) return;
     s += (int64_t)(r0 / 128) * fp8_lds(K);
-    for (int i = threadIdx.x; i < (K + 127) / 128; i += FEW_THREADS) dst[i] = __ldg(s + i);
+    for (int i = threadIdx.x; i < (K + 127) / 128; i += blockDim.x) dst[i] = __ldg(s + i);
 }
 
 template <int V, int NT, int CTAS, bool LN>
@@ -243,10 +243,10 @@ __device__ __forceinline__ void few_expert(const FewArgs& a, int e, int r0, cons
     else
         few_stage<NT>(red, acc, warp, lane);
     __syncthreads();
-    for (int i = threadIdx.x; i < n * 16; i += FEW_THREADS) {
+    for (int i = threadIdx.x; i < n * 16; i += FewT<V, NT, CTAS>::THREADS) {
         const int j = i >> 4, r = i & 15;
         if (r0 + r >= a.d) continue;
-        float s = few_sum<few_pass(PARTS, NT)>(red, j, r);
+        float s = few_sum<few_pass(PARTS, NT), FewT<V, NT, CTAS>::WARPS>(red, j, r);
         if (a.b2) s += few_get<V>(a.b2, r0 + r);
         few_put<V>(a.out, (int64_t)s_tok[j] * a.d + r0 + r, s);
     }
@@ -256,7 +256,7 @@ __device__ __forceinline__ void few_expert(const FewArgs& a, int e, int r0, cons
 // weights then coming from L2. GUESS (as many tokens as groups or more): the first weights are asked for before the
 // routing is known, beside fc1, as if the group had tokens.
 template <int V, int NT, int CTAS, bool GUESS>
-__global__ void __launch_bounds__(FEW_THREADS, CTAS) few_expert_kernel(const __grid_constant__ FewArgs a) {
+__global__ void __launch_bounds__(FewT<V, NT, CTAS>::THREADS, CTAS) few_expert_kernel(const __grid_constant__ FewArgs a) {
     extern __shared__ float red[];  // the partial sums; then the scale bytes
     __shared__ int s_tok[CLEARMOE_FEW_MAX];
     __shared__ int s_n;
@@ -315,12 +315,12 @@ __global__ void __launch_bounds__(FEW_THREADS, CTAS) few_expert_kernel(const __g
 }
 
 template <typename K, typename... A>
-cudaError_t few_launch(K kernel, dim3 grid, int smem, cudaStream_t s, const A&... a) {
+cudaError_t few_launch(K kernel, dim3 grid, int threads, int smem, cudaStream_t s, const A&... a) {
     const cudaError_t e = smem_attr_once((const void*)kernel, smem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
-    cfg.blockDim = dim3(FEW_THREADS);
+    cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute at[1];
@@ -335,15 +335,16 @@ template <int V, int NT, int CTAS>
 cudaError_t few_fc1(const FewArgs& a, cudaStream_t s) {
     const dim3 grid((a.H + 15) / 16 + (a.T + few_route_tokens(NT) - 1) / few_route_tokens(NT), (a.T + few_chunk(NT) - 1) / few_chunk(NT));
     const int smem = FewT<V, NT, CTAS>::SMEM + (V == FEWV_W8A16 ? (a.d + 127) / 128 : 0);
-    return a.ln ? few_launch(few_fc1_kernel<V, NT, CTAS, true>, grid, smem, s, a)
-                : few_launch(few_fc1_kernel<V, NT, CTAS, false>, grid, smem, s, a);
+    return a.ln ? few_launch(few_fc1_kernel<V, NT, CTAS, true>, grid, FEW_THREADS, smem, s, a)
+                : few_launch(few_fc1_kernel<V, NT, CTAS, false>, grid, FEW_THREADS, smem, s, a);
 }
 template <int V, int NT, int CTAS>
 cudaError_t few_experts(const FewArgs& a, cudaStream_t s) {
     const dim3 grid((a.d + 15) / 16, a.G);
     const int smem = FewT<V, NT, CTAS>::SMEM + (V == FEWV_W8A16 ? (a.H + 127) / 128 : 0);
-    return a.T >= a.G ? few_launch(few_expert_kernel<V, NT, CTAS, true>, grid, smem, s, a)
-                      : few_launch(few_expert_kernel<V, NT, CTAS, false>, grid, smem, s, a);
+    constexpr int threads = FewT<V, NT, CTAS>::THREADS;
+    return a.T >= a.G ? few_launch(few_expert_kernel<V, NT, CTAS, true>, grid, threads, smem, s, a)
+                      : few_launch(few_expert_kernel<V, NT, CTAS, false>, grid, threads, smem, s, a);
 }
 
 template <int V>
@@ -351,6 +352,8 @@ cudaError_t few_type(const FewArgs& a, cudaStream_t s) {
     const cudaError_t e = a.T <= 8 ? few_fc1<V, 1, 2>(a, s) : a.T <= 16 ? few_fc1<V, 2, 2>(a, s) : few_fc1<V, 4, 2>(a, s);
     if (e != cudaSuccess) return e;
     if (a.T <= 4) return few_experts<V, 1, 2>(a, s);
+    const bool lone = (int64_t)((a.d + 15) / 16) * (a.T < a.G ? a.T : a.G) <= a.num_sms;  // an SM for each CTA with work
+    if (lone) return a.T <= 16 ? few_experts<V, 2, 1>(a, s) : few_experts<V, 4, 1>(a, s);
     if (few_parts(V, 2) == 1 && a.T <= 8) return few_experts<V, 1, 3>(a, s);
     return a.T <= 16 ? few_experts<V, 2, 3>(a, s) : few_experts<V, 4, 2>(a, s);
 }

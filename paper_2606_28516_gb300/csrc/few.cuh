@@ -19,16 +19,18 @@
 namespace cm {
 
 constexpr int FEW_WARPS = 8;
-constexpr int FEW_THREADS = FEW_WARPS * 32;
+constexpr int FEW_THREADS = FEW_WARPS * 32;  // of kernels with two or three CTAs an SM
 
 // Kernel variants by element types: FEWV_W8A8 has 8-bit weights and activations, FEWV_W8A16 8-bit weights and bf16
 // activations.
 enum FewVar { FEWV_F32 = 0, FEWV_BF16 = 1, FEWV_W8A16 = 2, FEWV_W8A8 = 3 };
 
 // NT token tiles of 8 columns; CTAS of the kernel's CTAs share an SM: two where there are few, three where there are
-// more than the SMs take at once, so that one's start and end hide behind the others' loads.
+// more than the SMs take at once, so that one's start and end hide behind the others' loads; one of twice the warps where
+// the CTAs with work leave an SM to each.
 template <int V, int NT, int CTAS>
 struct FewT {
+    static constexpr int WARPS = CTAS == 1 ? 2 * FEW_WARPS : FEW_WARPS, THREADS = 32 * WARPS;
     static constexpr int LANE = V == FEWV_F32 ? 4 : V == FEWV_BF16 ? 8 : 16;  // weight columns per lane and step
     static constexpr int STEP = 4 * LANE;                                     // and of a warp's step
     static constexpr int WSZ = V == FEWV_F32 ? 4 : V == FEWV_BF16 ? 2 : 1;
@@ -36,10 +38,10 @@ struct FewT {
     static constexpr int XV = LANE * XSZ / 16;  // 16-byte loads of activations per step and token tile
     // Steps of weights and of activations in flight, 8 and 4 XV NT registers each
     static constexpr int XR = XV * NT;
-    static constexpr int DW = CTAS == 2 ? (XR == 1 ? 8 : XR == 2 ? 6 : XR == 4 ? 4 : 2) : (XR <= 2 ? 4 : 2);
-    static constexpr int DX = CTAS == 2 ? (XR == 1 ? 4 : XR == 2 ? 3 : XR == 4 ? 2 : 1) : (XR <= 2 ? 2 : 1);
+    static constexpr int DW = CTAS <= 2 ? (XR == 1 ? 8 : XR == 2 ? 6 : XR == 4 ? 4 : 2) : (XR <= 2 ? 4 : 2);
+    static constexpr int DX = CTAS <= 2 ? (XR == 1 ? 4 : XR == 2 ? 3 : XR == 4 ? 2 : 1) : (XR <= 2 ? 2 : 1);
     static_assert(DW % DX == 0);
-    static constexpr int SMEM = FEW_WARPS * NT * 128 * 4;  // the partial sums
+    static constexpr int SMEM = WARPS * NT * 128 * 4;  // the partial sums
 };
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -78,7 +80,7 @@ __device__ __forceinline__ uint32_t fp8x2_to_bf16x2(uint32_t v) {
 }
 
 // A 16-row tile of weights and its activation rows as a lane sees them. Step i of a warp is columns
-// [STEP (warp + 8 i), + STEP) of K; the lane's bytes of it start at w0 + i * (stride), w1 and tok[j] likewise.
+// [STEP (warp + WARPS i), + STEP) of K; the lane's bytes of it start at w0 + i * (stride), w1 and tok[j] likewise.
 template <int V, int NT, int CTAS>
 struct FewTile {
     using F = FewT<V, NT, CTAS>;
@@ -94,8 +96,8 @@ struct FewTile {
         const int g = (threadIdx.x >> 2) & 7, k = column(), warp = threadIdx.x >> 5, all = (K + F::STEP - 1) / F::STEP;
         w0 = static_cast<const char*>(base) + (int64_t)min(r0 + g, n_rows - 1) * pitch_bytes + (int64_t)k * F::WSZ;
         w1 = static_cast<const char*>(base) + (int64_t)min(r0 + g + 8, n_rows - 1) * pitch_bytes + (int64_t)k * F::WSZ;
-        steps = all > warp ? (all - warp + FEW_WARPS - 1) / FEW_WARPS : 0;
-        in = K > k ? (K - k + FEW_WARPS * F::STEP - 1) / (FEW_WARPS * F::STEP) : 0;
+        steps = all > warp ? (all - warp + F::WARPS - 1) / F::WARPS : 0;
+        in = K > k ? (K - k + F::WARPS * F::STEP - 1) / (F::WARPS * F::STEP) : 0;
     }
     __device__ __forceinline__ void set_row(int j, const void* row) {
         tok[j] = static_cast<const char*>(row) + (int64_t)column() * F::XSZ;
@@ -103,8 +105,8 @@ struct FewTile {
     __device__ __forceinline__ void load_w(int d, int i) {
         a[d] = b[d] = make_uint4(0, 0, 0, 0);
         if (i < in) {
-            a[d] = __ldg(reinterpret_cast<const uint4*>(w0 + (int64_t)i * (FEW_WARPS * F::STEP * F::WSZ)));
-            b[d] = __ldg(reinterpret_cast<const uint4*>(w1 + (int64_t)i * (FEW_WARPS * F::STEP * F::WSZ)));
+            a[d] = __ldg(reinterpret_cast<const uint4*>(w0 + (int64_t)i * (F::WARPS * F::STEP * F::WSZ)));
+            b[d] = __ldg(reinterpret_cast<const uint4*>(w1 + (int64_t)i * (F::WARPS * F::STEP * F::WSZ)));
         }
     }
     __device__ __forceinline__ void load_x(int d, int i) {
@@ -114,7 +116,7 @@ struct FewTile {
             for (int q = 0; q < F::XV; ++q) {
                 x[d][j][q] = make_uint4(0, 0, 0, 0);
                 if (i < in)
-                    x[d][j][q] = __ldcg(reinterpret_cast<const uint4*>(tok[j] + (int64_t)i * (FEW_WARPS * F::STEP * F::XSZ)) + q);
+                    x[d][j][q] = __ldcg(reinterpret_cast<const uint4*>(tok[j] + (int64_t)i * (F::WARPS * F::STEP * F::XSZ)) + q);
             }
     }
     // The first steps' loads: the weights' before the activations may be read.
@@ -145,7 +147,7 @@ __device__ __forceinline__ void few_product(float (&acc)[NT][4], float (&sums)[4
             const int i = i0 + d, xd = d % F::DX;
             if (i >= t.steps) break;
             const uint32_t wa[4] = {t.a[d].x, t.a[d].y, t.a[d].z, t.a[d].w}, wb[4] = {t.b[d].x, t.b[d].y, t.b[d].z, t.b[d].w};
-            const int blk = (warp + FEW_WARPS * i) * F::STEP / 128;  // of 8-bit weights: a step lies in one block
+            const int blk = (warp + F::WARPS * i) * F::STEP / 128;  // of 8-bit weights: a step lies in one block
             if constexpr (V == FEWV_F32) {
                 uint32_t ah[4], al[4], bh[4], bl[4];
 #pragma unroll
@@ -280,11 +282,11 @@ __device__ __forceinline__ void few_stage_pairs(float* red, const float (&acc)[N
     }
 }
 // The sum over the warps of column col of COLS, in warp order.
-template <int COLS>
+template <int COLS, int WARPS = FEW_WARPS>
 __device__ __forceinline__ float few_sum(const float* red, int col, int row) {
     float s = 0.f;
 #pragma unroll
-    for (int w = 0; w < FEW_WARPS; ++w) s += red[(w * COLS + col) * 16 + row];
+    for (int w = 0; w < WARPS; ++w) s += red[(w * COLS + col) * 16 + row];
     return s;
 }
 

@@ -364,6 +364,7 @@ struct FewArgs {
     const void* x;      // [T x d] layer dtype
     int T, d, H, E;     // E routed experts
     int G;              // groups: E, + 1 with class tokens
+    int num_sms;
     int f32;            // fp32 layer
     int fp8;            // weights in 8-bit blocks
     const void* W1;
