@@ -264,8 +264,10 @@ __global__ void __launch_bounds__(FewT<V, NT, CTAS>::THREADS, CTAS) few_expert_k
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int e = blockIdx.y, r0 = blockIdx.x * 16;
+    // z in two parts halves a pass; where the registers of one CTA an SM allow it, twice the tiles make up for it
+    constexpr int PARTS = few_parts(V, NT), WIDE = PARTS == 2 && NT == 2 && CTAS == 1 ? 4 : NT;
     // the steps that every width of the product starts with
-    constexpr int HAVE = !GUESS ? 0 : FewT<V, NT, CTAS>::DW < FEW_EARLY ? FewT<V, NT, CTAS>::DW : FEW_EARLY;
+    constexpr int HAVE = !GUESS ? 0 : FewT<V, WIDE, CTAS>::DW < FEW_EARLY ? FewT<V, WIDE, CTAS>::DW : FEW_EARLY;
     uint4 early[2][FEW_EARLY];
     if (GUESS) {
         FewTile<V, 1, CTAS> t;
@@ -298,19 +300,19 @@ __global__ void __launch_bounds__(FewT<V, NT, CTAS>::THREADS, CTAS) few_expert_k
         }
     }
     __syncthreads();
-    constexpr int PARTS = few_parts(V, NT), PASS = few_pass(PARTS, NT), P = few_pass(PARTS, 1);
+    constexpr int PASS = few_pass(PARTS, WIDE), P = few_pass(PARTS, 1);
     int n = min(PASS, s_n);
     if (n == 0) return;
     if (NT == 1 || n <= P)
         few_expert<V, 1, PARTS, CTAS, HAVE>(a, e, r0, s_tok, n, red, s_scale, early, warp, lane);
-    else if (NT == 2 || n <= 2 * P)
+    else if (WIDE == 2 || n <= 2 * P)
         few_expert<V, NT < 2 ? NT : 2, PARTS, CTAS, HAVE>(a, e, r0, s_tok, n, red, s_scale, early, warp, lane);
     else
-        few_expert<V, NT, PARTS, CTAS, HAVE>(a, e, r0, s_tok, n, red, s_scale, early, warp, lane);
+        few_expert<V, WIDE, PARTS, CTAS, HAVE>(a, e, r0, s_tok, n, red, s_scale, early, warp, lane);
     for (int m0 = PASS; m0 < s_n; m0 += PASS) {
         __syncthreads();  // red is read
         n = min(PASS, s_n - m0);
-        few_expert<V, NT, PARTS, CTAS, 0>(a, e, r0, s_tok + m0, n, red, s_scale, early, warp, lane);
+        few_expert<V, WIDE, PARTS, CTAS, 0>(a, e, r0, s_tok + m0, n, red, s_scale, early, warp, lane);
     }
 }
 
@@ -353,6 +355,8 @@ cudaError_t few_type(const FewArgs& a, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     if (a.T <= 4) return few_experts<V, 1, 2>(a, s);
     const bool lone = (int64_t)((a.d + 15) / 16) * (a.T < a.G ? a.T : a.G) <= a.num_sms;  // an SM for each CTA with work
+    // us, lone CTAs of 16 warps against two or three of 8 an SM: 8 tokens, d = 384, 4 experts, bf16 4.6 / 5.0; 24, d = 384, 6, fp32
+    // 9.6 / 10.7; 16, d = 768, 3, bf16 9.6 / 17.1; more CTAs than SMs: 13, d = 768, 9, bf16 18.9 / 14.6; 64, 8 19.8 / 18.4
     if (lone) return a.T <= 16 ? few_experts<V, 2, 1>(a, s) : few_experts<V, 4, 1>(a, s);
     if (few_parts(V, 2) == 1 && a.T <= 8) return few_experts<V, 1, 3>(a, s);
     return a.T <= 16 ? few_experts<V, 2, 3>(a, s) : few_experts<V, 4, 2>(a, s);
