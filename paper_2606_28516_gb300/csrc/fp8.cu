@@ -140,10 +140,11 @@ __global__ void __launch_bounds__(Q_THREADS) quantize_bf16_kernel(const QuantArg
     }
 }
 
-// Other rows: fp32, or not 16-byte aligned (VEC false). Six CTAs an SM, though it takes registers off the loads in flight:
-// 8,192 x 4,095 bf16 31.8 us, with four (57 registers) 36.8, with eight 41.4.
+// Other rows: fp32, or not 16-byte aligned (VEC false). Five CTAs an SM: 8,192 x 4,095 bf16 34.0 us, with four (57 registers)
+// 36.8, with six 31.8, which then leave the product that follows a later start: 1,001 x 777 x 1,131 fp32 9.0 us for both,
+// 8.9 with four, 9.9 with six.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(Q_THREADS, 6) quantize_rows_kernel(const QuantArgs a) {
+__global__ void __launch_bounds__(Q_THREADS, 5) quantize_rows_kernel(const QuantArgs a) {
     // Unaligned rows go through shared memory, so that a load's lanes read consecutive elements: a block of the warp's four
     // at a time, 16 columns a pitch of 20. (All four at once, 17 KB a CTA, kept the product that follows from starting
     // beside it: 1,001 x 777 x 1,131 fp32 10.3 us for both.)

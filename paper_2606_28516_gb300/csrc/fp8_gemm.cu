@@ -429,7 +429,7 @@ int run_fp8_gemm(Fp8GemmArgs& g, const clearmoe_fp8* A, const clearmoe_fp8* W, i
     // made of does not matter.
     g.box_rows = !k.pair && g.M < F8_BM ? (int)(g.M + 7) / 8 * 8 : F8_BM;
     if (encode_tmap_bf16(&g.tmA, A->q, A->rows, cols16, g.box_rows)) return CLEARMOE_ECUDA;
-    if (g.out_kind == FP8_OUT_FP8 && encode_tmap_bytes(&g.tmOut, g.out, g.M, g.ldo, 32)) return CLEARMOE_ECUDA;
+    if (g.out_kind == FP8_OUT_FP8 && k.pair && encode_tmap_bytes(&g.tmOut, g.out, g.M, g.ldo, 32)) return CLEARMOE_ECUDA;
     for (int e = 0; e < E; ++e) {
         g.sb[e] = W[e].scale;
         if (encode_tmap_bf16(&g.tmB[e], W[e].q, W[e].rows, cols16, k.pair ? k.bn / 2 : k.bn)) return CLEARMOE_ECUDA;

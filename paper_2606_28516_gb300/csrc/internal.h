@@ -319,7 +319,7 @@ cudaError_t launch_quantize_weight(const QuantArgs& a, int dtype, cudaStream_t s
 enum Fp8Out { FP8_OUT_F32 = 0, FP8_OUT_BF16 = 1, FP8_OUT_FP8 = 2 };
 struct Fp8GemmArgs {
     CUtensorMap tmA;
-    CUtensorMap tmOut;  // FP8_OUT_FP8: the output's bytes, boxes of 64 bytes x 32 rows
+    CUtensorMap tmOut;  // FP8_OUT_FP8 on pairs: the output's bytes, boxes of 64 bytes x 32 rows
     CUtensorMap tmB[16];
     const void* x;      // q of A, and of the first W (few rows)
     const void* w;
