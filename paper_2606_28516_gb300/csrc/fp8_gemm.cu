@@ -229,9 +229,7 @@ __global__ void __launch_bounds__(F8Cfg<BN_>::THREADS, 1) fp8_gemm_kernel(const 
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         float* bias_line = s_bias + warp * 32;
         const bool has_bias = a.bias != nullptr;
-        const int esz = KIND == FP8_OUT_BF16 ? 2 : 4;
-        // rows of the output in whole 32-byte pieces
-        const bool wide = (reinterpret_cast<uintptr_t>(a.out) & 31) == 0 && (a.ldo * esz & 31) == 0;
+        const bool wide = f8_wide(a);
         int acc = 0;
         uint32_t aph = 0, pph = 0;
         for (; t.live(); t.next()) {
@@ -351,29 +349,37 @@ cudaError_t launch_kind(const Fp8GemmArgs& a, int num_sms, cudaStream_t s) {
 struct Fp8Kernel {
     Fp8Pick pick;
     int block;     // cycles of a k-block with every SM at work
-    int epilogue;  // of a tile beside the next tile's MMAs: bf16 and fp32 outputs
-    int quantize;  // 8-bit outputs (0: none)
+    int epilogue[4];  // of a tile beside the next tile's MMAs, by Fp8Store
+    int quantize;     // 8-bit outputs (0: none)
 };
-static double fp8_cost(const Fp8Kernel& k, int64_t M, int N, int nkb, int out_kind, int groups, int num_sms) {
+// How outputs are stored: bf16 or fp32 rows in whole 32-byte pieces, or of any pitch. Cycles measured at 2,922 x 3,456 (3,453)
+// x 60, where the stores are all there is; us of the best kernel and of the one that a single figure had chosen: bf16 7.5 / 10.6,
+// fp32 11.6 / 14.7, any pitch 13.8 / 18.3 and 14.6 / 18.3.
+enum Fp8Store { FP8_STORE_BF16 = 0, FP8_STORE_F32 = 1, FP8_STORE_ODD = 2 };  // ODD: added to the type's
+static double fp8_cost(const Fp8Kernel& k, int64_t M, int N, int nkb, int out_kind, bool wide, int groups, int num_sms) {
     const bool pair = k.pick.pair, q = out_kind == FP8_OUT_FP8;
     const int bn = k.pick.bn, rows = pair ? 256 : 128, units = pair ? num_sms / 2 : num_sms;
     if (units < 1 || (q && !k.quantize)) return 1e30;
     const int64_t tiles = ((M + rows - 1) / rows + groups - 1) * (((int64_t)N + bn - 1) / bn);
     const double rounds = (double)((tiles + units - 1) / units), busy = tiles < units ? (double)tiles / units : 1.0;
     const double low = 2 * bn > 285 ? 2 * bn : 285, main = nkb * (low + (k.block - low) * busy * busy);
-    const double beside = q ? k.quantize : k.epilogue, between = bn == 256 ? 1500 : 0;  // 256: accumulators that overlap
+    const int store = (out_kind == FP8_OUT_BF16 ? FP8_STORE_BF16 : FP8_STORE_F32) + (wide ? 0 : FP8_STORE_ODD);
+    const double beside = q ? k.quantize : k.epilogue[store];
+    const double between = bn == 256 ? 1500 : 0;  // 256: accumulators that overlap
     const double next = main + between > beside ? main + between : beside;
     return (pair ? 8800 : 4600) + main + (rounds - 1) * next + (q ? beside : 15.0 * bn);
 }
 
-Fp8Pick fp8_pick(int64_t M, int N, int nkb, int out_kind, int groups, int num_sms) {
-    static const Fp8Kernel all[] = {{{256, 1}, 540, 3072, 5950}, {{192, 1}, 550, 2304, 0}, {{128, 1}, 487, 1536, 3000},
-                                    {{192, 0}, 588, 2304, 0},    {{128, 0}, 445, 1536, 4200}, {{64, 0}, 350, 768, 0},
-                                    {{32, 0}, 285, 384, 0}};
+Fp8Pick fp8_pick(int64_t M, int N, int nkb, int out_kind, bool wide, int groups, int num_sms) {
+    static const Fp8Kernel all[] = {
+        {{256, 1}, 540, {3160, 7200, 8450, 9150}, 5950}, {{192, 1}, 550, {2000, 5050, 7200, 8250}, 0},
+        {{128, 1}, 487, {1450, 3300, 4250, 4720}, 3000}, {{192, 0}, 588, {3040, 6960, 9060, 9800}, 0},
+        {{128, 0}, 445, {2180, 3960, 4800, 5260}, 4200}, {{64, 0}, 350, {1370, 2320, 2690, 2790}, 0},
+        {{32, 0}, 285, {920, 1400, 1840, 1840}, 0}};
     Fp8Pick best = all[4].pick;
     double least = 1e30;
     for (const Fp8Kernel& k : all) {
-        const double c = fp8_cost(k, M, N, nkb, out_kind, groups, num_sms);
+        const double c = fp8_cost(k, M, N, nkb, out_kind, wide, groups, num_sms);
         if (c < least) {
             least = c;
             best = k.pick;
@@ -417,7 +423,7 @@ int run_fp8_gemm(Fp8GemmArgs& g, const clearmoe_fp8* A, const clearmoe_fp8* W, i
         (void)cudaGetLastError();
         return CLEARMOE_ECUDA;
     }
-    Fp8Pick k = fp8_pick(g.M, g.N, g.nkb, g.out_kind, E, num_sms);
+    Fp8Pick k = fp8_pick(g.M, g.N, g.nkb, g.out_kind, f8_wide(g), E, num_sms);
     if (forced && forced != FP8_FORCE_FEW) {
         const Fp8Pick f = {forced >> 1, forced & 1};
         if (g.out_kind != FP8_OUT_FP8 || f.bn % 128 == 0) k = f;

@@ -1,6 +1,8 @@
 // Pieces shared by the kernels of products in 8-bit blocks: descriptors, tiles, epilogue arithmetic.
 #pragma once
 
+#include <type_traits>
+
 #include "common.cuh"
 #include "fp8.cuh"
 #include "internal.h"
@@ -201,9 +203,15 @@ __device__ __forceinline__ void f8_transpose(float (&v)[32], int lane) {
     }
 }
 
+// Rows of an fp32 or bf16 output in whole 32-byte pieces.
+__host__ __device__ __forceinline__ bool f8_wide(const Fp8GemmArgs& a) {
+    return (reinterpret_cast<uintptr_t>(a.out) & 31) == 0 && (a.ldo * (a.out_kind == FP8_OUT_BF16 ? 2 : 4) & 31) == 0;
+}
+
 // 32 rows' 32 columns [nc, nc + 32) (one row a lane: its output row, or -1) to out, fp32 or bf16. Rows in whole 32-byte
 // pieces (wide) are stored as each lane has them; others transposed first, so that a store's lanes write consecutive
-// columns of one row (an element a lane, rows apart, took 9.8 us for 1,001 x 777 x 1,131 where this takes 5.7).
+// columns of one row (an element a lane, rows apart, took 9.8 us for 1,001 x 777 x 1,131 where this takes 5.7; with each
+// row's number shuffled from its lane, 2,922 x 3,453 x 60 to bf16 took 18.5 us where this takes 13.8).
 template <int KIND>
 __device__ __forceinline__ void f8_store32(const Fp8GemmArgs& a, float (&v)[32], int row, int nc, bool wide, int lane) {
     if (wide && nc + 32 <= a.N) {
@@ -231,14 +239,32 @@ __device__ __forceinline__ void f8_store32(const Fp8GemmArgs& a, float (&v)[32],
     }
     __syncwarp();
     f8_transpose(v, lane);
+    const bool mine = nc + lane < a.N;
+    auto put = [&](int64_t at, float f) {
+        if constexpr (KIND == FP8_OUT_BF16)
+            static_cast<uint16_t*>(a.out)[at] = f32_to_bf16(f);
+        else
+            static_cast<float*>(a.out)[at] = f;
+    };
+    if (!a.rows) {  // consecutive rows from lane 0's on: without their shuffles a store waits for nothing
+        const int rows = __popc(__ballot_sync(0xFFFFFFFFu, row >= 0)), n = mine ? rows : 0;
+        using T = std::conditional_t<KIND == FP8_OUT_BF16, uint16_t, float>;
+        T* o = static_cast<T*>(a.out) + (int64_t)__shfl_sync(0xFFFFFFFFu, row, 0) * a.ldo + nc + lane;
+#pragma unroll
+        for (int r = 0; r < 32; ++r, o += a.ldo) {
+            if (r < n) {
+                if constexpr (KIND == FP8_OUT_BF16)
+                    *o = f32_to_bf16(v[r]);
+                else
+                    *o = v[r];
+            }
+        }
+        return;
+    }
 #pragma unroll
     for (int r = 0; r < 32; ++r) {
         const int64_t orow = __shfl_sync(0xFFFFFFFFu, row, r);
-        if (orow < 0 || nc + lane >= a.N) continue;
-        if constexpr (KIND == FP8_OUT_BF16)
-            static_cast<uint16_t*>(a.out)[orow * a.ldo + nc + lane] = f32_to_bf16(v[r]);
-        else
-            static_cast<float*>(a.out)[orow * a.ldo + nc + lane] = v[r];
+        if (orow >= 0 && mine) put(orow * a.ldo + nc + lane, v[r]);
     }
 }
 

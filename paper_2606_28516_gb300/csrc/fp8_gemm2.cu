@@ -319,9 +319,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8Cfg<BN_, KIND>::TH
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         float* bias_line = s_bias + warp * 32;
         const bool has_bias = a.bias != nullptr;
-        const int esz = KIND == FP8_OUT_BF16 ? 2 : 4;
-        // rows of the output in whole 32-byte pieces
-        const bool wide = (reinterpret_cast<uintptr_t>(a.out) & 31) == 0 && (a.ldo * esz & 31) == 0;
+        const bool wide = f8_wide(a);
         const uint32_t tempty_leader0 = map_to_rank(tempty_bar(0), 0), ovl_leader = map_to_rank(ovl_bar, 0);
         // What a tile's epilogue needs beside its sums, loaded a tile ahead: a load waits behind the queued tile loads.
         float bias[C::ROUNDS];

@@ -349,7 +349,7 @@ struct Fp8Pick {
     int bn;
     int pair;
 };
-Fp8Pick fp8_pick(int64_t M, int N, int nkb, int out_kind, int groups, int num_sms);
+Fp8Pick fp8_pick(int64_t M, int N, int nkb, int out_kind, bool wide, int groups, int num_sms);
 cudaError_t launch_fp8_gemm(const Fp8GemmArgs& a, const Fp8Pick& k, int num_sms, cudaStream_t s);
 // A product of at most FP8_FEW_MAX rows in one group, not to 8-bit blocks, whose scales (nkb bytes per row of A, and W's) fit
 // FP8_FEW_SCALES bytes.
