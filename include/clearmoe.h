@@ -432,7 +432,8 @@ typedef struct {
  * through its expert; only experts that have a token are read. Weights of the layer's dtype or 8-bit blocks
  * (bf16 layers; the weights' values times unquantised activations). Sums in fp32; z is stored in the layer's dtype
  * as in the other forwards, of up to 16 tokens of bf16 layers in two bf16 parts (16 bits of significand); fp32 layers
- * use three TF32 products per term (relative error near 2^-21, and NaN where an infinity's remainder is formed). The
+ * use three TF32 products per term (relative error near 2^-21; NaN for an infinity and for a magnitude past TF32's largest
+ * value, 3.4e38, whose remainder is not finite). The
  * routing can be read with clearmoe_get_routing. Errors as clearmoe_ffn_forward_folded_ex; EUNSUPPORTED for more
  * tokens, and for 8-bit weights with hidden > 589,824. */
 #define CLEARMOE_FEW_MAX 64

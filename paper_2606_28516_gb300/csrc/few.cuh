@@ -62,10 +62,13 @@ __device__ __forceinline__ void mma_tf32(float (&d)[4], uint32_t a0, uint32_t a1
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// v rounded to TF32 (to nearest, ties away from zero) and the remainder, rounded likewise
+// v rounded to TF32 (to nearest, ties away from zero) and the exact remainder, which the tensor cores cut to TF32: of at
+// most 13 bits, so that three of its last at 2^-24 of v are lost. Not rounded by integer arithmetic as v is: a NaN of
+// arithmetic has all its bits set, which makes h a zero, and only the remainder then is the NaN that the sum has to be. Of
+// an infinity, and past TF32's largest value (3.4e38), the remainder is a NaN or an infinity against h's, and the sum NaN.
 __device__ __forceinline__ void few_split(uint32_t v, uint32_t& h, uint32_t& l) {
     h = (v + 0x1000u) & 0xFFFFE000u;
-    l = __float_as_uint(__uint_as_float(v) - __uint_as_float(h)) + 0x1000u;
+    l = __float_as_uint(__uint_as_float(v) - __uint_as_float(h));
 }
 // Two e4m3 values as a pair of fp16, exactly
 __device__ __forceinline__ uint32_t fp8x2_to_f16x2(uint32_t v) {
