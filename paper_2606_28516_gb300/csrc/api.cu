@@ -1185,6 +1185,7 @@ static int dense_impl(clearmoe_layer* L, const void* x, int64_t T, const void* W
         g.bias = b1;
         g.C = L->z;
         g.ldc = H;
+        g.pdl_trigger_late = 1;  // the call's first kernel: what was written before its predecessor is complete for those after
         if ((rc = cuda_fail(cm::launch_tc_gemm(g, L->num_sms, s)))) return rc;
         mark(L, 1, s);
         cm::TcGemmArgs g2;
@@ -1261,6 +1262,7 @@ static int dense_impl(clearmoe_layer* L, const void* x, int64_t T, const void* W
     if (ln && pair1 && (rc = ln_fc1_aug(L, g, T, pair1))) return rc;  // 2-SM: the augmentation block
     g.bn = pair1;
     g.epi12 = pair1 == 256 && d <= cm::TC2_EPI12_MAX_K;  // short K: the GELU epilogue bounds a tile
+    g.pdl_trigger_late = 1;  // as above
     if ((rc = cuda_fail(pair1 ? cm::launch_tc_gemm2(g, L->num_sms, s) : cm::launch_tc_gemm(g, L->num_sms, s))))
         return rc;
     mark(L, 1, s);

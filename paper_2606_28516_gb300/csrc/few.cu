@@ -101,6 +101,7 @@ __device__ __forceinline__ void few_route(const FewArgs& a, int block, float (*s
     for (int q = 0; q < 2; ++q)
         if (warp + 8 * q < a.E) w[q].load(a.Wg, warp + 8 * q, a.d, lane);  // zeros past d
     pdl_wait();
+    pdl_launch_dependents();
 #pragma unroll
     for (int i = 0; i < TOK; ++i) x[i].load(a.x, min(TOK * block + i, a.T - 1), a.d, lane);
 #pragma unroll
@@ -153,7 +154,6 @@ __global__ void __launch_bounds__(FEW_THREADS, CTAS) few_fc1_kernel(const __grid
     __shared__ float s_logit[2][16];
     __shared__ float s_rows[FEW_WARPS][16];  // LN: the warps' row sums of W
     uint8_t* s_scale = reinterpret_cast<uint8_t*>(red) + FewT<V, NT, CTAS>::SMEM;
-    pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     constexpr int TOK = few_route_tokens(NT);
     const int routers = (a.T + TOK - 1) / TOK;
@@ -168,6 +168,8 @@ __global__ void __launch_bounds__(FEW_THREADS, CTAS) few_fc1_kernel(const __grid
     t.start_w();
     few_scales<V>(s_scale, a.W1_s, r0, a.d);
     pdl_wait();
+    // the expert kernel reads weights before its own wait: whatever wrote them before this call's predecessor has completed
+    pdl_launch_dependents();
     float acc[NT][4], sums[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < NT; ++j) {

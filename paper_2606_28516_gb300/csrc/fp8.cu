@@ -120,7 +120,6 @@ __device__ __forceinline__ void quantize_block_bf16(const uint4 (&r)[2], int l8,
 
 // Aligned bf16 rows.
 __global__ void __launch_bounds__(Q_THREADS) quantize_bf16_kernel(const QuantArgs a) {
-    pdl_launch_dependents();
     const int l8 = threadIdx.x & 7;
     const int64_t b0 = (int64_t)blockIdx.x * Q_CTA_BLOCKS + (threadIdx.x >> 3), step = (int64_t)gridDim.x * Q_CTA_BLOCKS;
     int64_t row = b0 / a.kb;
@@ -128,6 +127,7 @@ __global__ void __launch_bounds__(Q_THREADS) quantize_bf16_kernel(const QuantArg
     const int64_t step_row = step / a.kb;
     const int step_kb = (int)(step - step_row * a.kb);
     pdl_wait();
+    pdl_launch_dependents();  // after the wait: the next kernel may read weights that one before this has written
     while (__any_sync(0xFFFFFFFFu, row < a.rows)) {
         const bool live = row < a.rows;
         const int64_t src = a.gather && live ? (int64_t)__ldcg(a.gather + row) : row;
@@ -149,7 +149,6 @@ __global__ void __launch_bounds__(Q_THREADS, 5) quantize_rows_kernel(const Quant
     // at a time, 16 columns a pitch of 20. (All four at once, 17 KB a CTA, kept the product that follows from starting
     // beside it: 1,001 x 777 x 1,131 fp32 10.3 us for both.)
     __shared__ __align__(16) float s_x[VEC ? 1 : Q_THREADS / 32][VEC ? 1 : 8 * 20];
-    pdl_launch_dependents();
     const int l8 = threadIdx.x & 7, lane = threadIdx.x & 31;
     const int64_t b0 = (int64_t)blockIdx.x * Q_CTA_BLOCKS + (threadIdx.x >> 3), step = (int64_t)gridDim.x * Q_CTA_BLOCKS;
     int64_t row = b0 / a.kb;
@@ -157,6 +156,7 @@ __global__ void __launch_bounds__(Q_THREADS, 5) quantize_rows_kernel(const Quant
     const int64_t step_row = step / a.kb;
     const int step_kb = (int)(step - step_row * a.kb);
     pdl_wait();
+    pdl_launch_dependents();  // after the wait: the next kernel may read weights that one before this has written
     while (__any_sync(0xFFFFFFFFu, row < a.rows)) {
         const bool live = row < a.rows;
         const int64_t src = a.gather && live ? (int64_t)__ldcg(a.gather + row) : row;
@@ -215,8 +215,8 @@ __global__ void __launch_bounds__(SQ_THREADS, 2) slots_quantize_kernel(const Rou
     const int64_t row0 = (int64_t)blockIdx.x * chunk;
     const int64_t rows = max((int64_t)0, min((int64_t)chunk, r.T - row0));
     const int64_t n_cls = n_class_tokens(r.T, r.cls_stride);
-    pdl_launch_dependents();
     pdl_wait();  // everything below reads the routing kernel's output
+    pdl_launch_dependents();
     int before[CM_MAX_E], total[CM_MAX_E];
 #pragma unroll
     for (int e = 0; e < CM_MAX_E; ++e) before[e] = total[e] = 0;

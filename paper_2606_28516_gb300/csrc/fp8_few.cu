@@ -17,12 +17,12 @@ template <int NT>
 __global__ void __launch_bounds__(FEW_THREADS, 2) fp8_few_kernel(const __grid_constant__ Fp8GemmArgs a) {
     extern __shared__ float red[];  // the partial sums; then scale bytes: the tile's rows' [nkb], A's rows' [M][nkb]
     uint8_t* s_scale = reinterpret_cast<uint8_t*>(red) + FewT<FEWV_W8A8, NT, 2>::SMEM;
-    pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int r0 = blockIdx.x * 16, M = (int)a.M, ldq = a.nkb * 128;
     FewTile<FEWV_W8A8, NT, 2> t;
     t.set_weights(a.w, ldq, r0, a.N, ldq);
     pdl_wait();
+    pdl_launch_dependents();  // after the wait: the next kernel may read weights that one before this has written
     t.start_w();
     float acc[NT][4], sums[4];
 #pragma unroll

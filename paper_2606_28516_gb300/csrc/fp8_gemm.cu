@@ -83,7 +83,6 @@ __global__ void __launch_bounds__(F8Cfg<BN_>::THREADS, 1) fp8_gemm_kernel(const 
     int* s_prefix = reinterpret_cast<int*>(tmem_slot + 4);  // [E + 1]
     int* s_off = s_prefix + CM_MAX_E + 1;                    // [E + 1]
 
-    pdl_launch_dependents();
     const int warp = warp_uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
     const uint32_t bar0 = smem_u32(bars);
     auto full_bar = [&](int s) { return bar0 + 8u * s; };
@@ -119,6 +118,7 @@ __global__ void __launch_bounds__(F8Cfg<BN_>::THREADS, 1) fp8_gemm_kernel(const 
     __syncthreads();
     tc_fence_after();
     pdl_wait();  // everything below may read the previous kernel's results
+    pdl_launch_dependents();  // after the wait: the next kernel may read weights that one before this has written
     if (threadIdx.x == 0) {
         f8_groups(a, F8_BM, s_off, s_prefix);
     }

@@ -96,7 +96,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8Cfg<BN_, KIND>::TH
     int* s_prefix = reinterpret_cast<int*>(tmem_slot + 4);  // [E + 1]
     int* s_off = s_prefix + CM_MAX_E + 1;                   // [E + 1]
 
-    pdl_launch_dependents();
     const int warp = warp_uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     const bool leader = rank == 0;
@@ -143,6 +142,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8Cfg<BN_, KIND>::TH
     cluster_sync();  // barriers initialised and tensor memory allocated in both CTAs
     tc_fence_after();
     pdl_wait();  // everything below may read the previous kernel's results
+    pdl_launch_dependents();  // after the wait: the next kernel may read weights that one before this has written
     if (threadIdx.x == 0) f8_groups(a, 2 * P8_BM, s_off, s_prefix);
     __syncthreads();
     const uint32_t tmem = warp_uniform(*tmem_slot);  // all 512 columns: the same base in both CTAs

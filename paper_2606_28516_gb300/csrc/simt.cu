@@ -31,11 +31,11 @@ __global__ void __launch_bounds__(256) simt_gemm_kernel(const SimtGemmArgs a, co
     const int tid = threadIdx.x;
     const int nt = blockIdx.x % n_tiles_n;
     const int mt = blockIdx.x / n_tiles_n;
-    // Launched with programmatic dependent launch: the next kernel may be scheduled once every block
-    // of this one has started, and this one reads nothing (offsets, operands, the split-K workspace
-    // and counters) before the previous kernel has completed.
-    pdl_launch_dependents();
+    // Launched with programmatic dependent launch: this one reads nothing (offsets, operands, the split-K
+    // workspace and counters) before the previous kernel has completed, and only then releases the next,
+    // which may read weights that a kernel before this one has written.
     pdl_wait();
+    pdl_launch_dependents();
     int64_t m_lo, m_hi;
     int e = 0;
     if (a.offsets) {
