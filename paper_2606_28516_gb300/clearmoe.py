@@ -467,6 +467,11 @@ def fp8_weight(rows: int, cols: int, device="cuda") -> Fp8Matrix:
     return _fp8_empty(rows, cols, True, device)
 
 
+def _refuse_kind(what, weight):
+    raise ValueError(f"{what} must be a matrix in 8-bit blocks of {'weights (fp8_weight)' if weight else 'rows (fp8_rows)'}: its "
+                     f"scales have one row per {'128 rows' if weight else 'row'}")
+
+
 _DTYPES = {}  # torch dtype -> clearmoe_dtype, filled on first use (torch is imported late)
 
 
@@ -497,6 +502,8 @@ def _matrix(t, rows, cols, what):
 
 def clearmoe_fp8_quantize_rows(x, out: Fp8Matrix, gather=None, stream=None) -> None:
     """x [rows x cols] (bf16 or fp32, any row pitch) to out in 1 x 128 blocks; gather: int32 source rows."""
+    if getattr(out, "weight", False):
+        _refuse_kind("out", False)
     calls = _calls or _bind_calls()
     code = calls.quantize_rows_t(x, out.rows, out.cols, out.addr, stream) if gather is None else None
     if code is None:
@@ -510,6 +517,8 @@ def clearmoe_fp8_quantize_rows(x, out: Fp8Matrix, gather=None, stream=None) -> N
 
 def clearmoe_fp8_quantize_weight(W, out: Fp8Matrix, stream=None) -> None:
     """W [rows x cols] (bf16 or fp32, any row pitch) to out in 128 x 128 blocks."""
+    if not getattr(out, "weight", True):
+        _refuse_kind("out", True)
     p, dt, ld = _matrix(W, out.rows, out.cols, "W")
     _check(lib().clearmoe_fp8_quantize_weight(p, dt, ld, out.ref, _stream(stream)), "clearmoe_fp8_quantize_weight")
 
@@ -532,8 +541,14 @@ def _epilogue(bias, act, status, N):
 def clearmoe_fp8_gemm(A: Fp8Matrix, W: Fp8Matrix, out, bias=None, act: int = ACT_NONE, status=None, stream=None) -> None:
     """out = act(A W^T + bias). out: a [M x N] bf16 or fp32 tensor of any row pitch, or an Fp8Matrix of rows (the
     result quantised, clearmoe_fp8_gemm_fp8)."""
+    if getattr(A, "weight", False):
+        _refuse_kind("A", False)
+    if not getattr(W, "weight", True):
+        _refuse_kind("W", True)
     calls = _calls or _bind_calls()
     blocks = isinstance(out, Fp8Matrix)
+    if blocks and out.weight:
+        _refuse_kind("out", False)
     if not blocks:
         code = calls.gemm_t(A.addr, W.addr, A.rows, W.rows, act, bias, status, out, stream)
         if code is not None:
@@ -559,6 +574,10 @@ def clearmoe_fp8_gemm(A: Fp8Matrix, W: Fp8Matrix, out, bias=None, act: int = ACT
 def clearmoe_fp8_grouped_gemm(A: Fp8Matrix, W, offsets, out, perm=None, bias=None, act: int = ACT_NONE, status=None,
                               stream=None) -> None:
     """Rows offsets[e] .. offsets[e + 1] of A times W[e]^T (W: a sequence of Fp8Matrix), row i to out[perm[i]]."""
+    if getattr(A, "weight", False):
+        _refuse_kind("A", False)
+    if not all(getattr(m, "weight", True) for m in W):
+        _refuse_kind("every W", True)
     if offsets.numel() != len(W) + 1 or (perm is not None and perm.numel() != A.rows):
         raise ValueError("offsets must have one entry per matrix and one more, perm one per row of A")
     p, dt, ld = _matrix(out, A.rows, W[0].rows, "out")
