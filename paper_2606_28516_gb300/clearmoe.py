@@ -160,7 +160,7 @@ def _bind_calls():
               L.clearmoe_ffn_forward_fp8)))
     try:
         import torch
-        m.bind_torch(torch.bfloat16, torch.float32, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+        m.bind_torch(torch.bfloat16, torch.float32, torch.int32, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
     except (ImportError, AttributeError):  # a torch without CUDA: every call then goes by integers
         pass
     _calls = m
@@ -485,6 +485,15 @@ def _dtype(t) -> int:
     return dt
 
 
+def _int32(t, n, what):
+    """Pointer of n int32 values (n None: one or more) on the GPU, or None."""
+    if t is None:
+        return None
+    if str(t.dtype) != "torch.int32" or (t.numel() != n if n is not None else t.numel() < 1):
+        raise ValueError(f"{what} must be int32 with {n or 'at least one'} entries, got {t.numel()} of {t.dtype}")
+    return _ptr(t)
+
+
 def _matrix(t, rows, cols, what):
     """Pointer, dtype and row pitch of a [rows x cols] CUDA tensor whose rows are dense (any pitch; rows None: any
     number)."""
@@ -508,9 +517,7 @@ def clearmoe_fp8_quantize_rows(x, out: Fp8Matrix, gather=None, stream=None) -> N
     code = calls.quantize_rows_t(x, out.rows, out.cols, out.addr, stream) if gather is None else None
     if code is None:
         p, dt, ld = _matrix(x, out.rows if gather is None else None, out.cols, "x")
-        if gather is not None and gather.numel() != out.rows:
-            raise ValueError("gather must have one entry per row of out")
-        code = calls.quantize_rows(p, dt, ld, _ptr(gather), out.addr, _stream(stream))
+        code = calls.quantize_rows(p, dt, ld, _int32(gather, out.rows, "gather"), out.addr, _stream(stream))
     if code:
         raise ClearMoEError(code, "clearmoe_fp8_quantize_rows")
 
@@ -535,7 +542,8 @@ def _epilogue(bias, act, status, N):
         return None
     if bias is not None and bias.numel() != N:
         raise ValueError(f"bias must have {N} elements, got {bias.numel()}")
-    return ctypes.byref(clearmoe_fp8_epilogue(_ptr(bias), F32 if bias is None else _dtype(bias), act, _ptr(status)))
+    return ctypes.byref(clearmoe_fp8_epilogue(_ptr(bias), F32 if bias is None else _dtype(bias), act,
+                                              _int32(status, None, "status")))
 
 
 def clearmoe_fp8_gemm(A: Fp8Matrix, W: Fp8Matrix, out, bias=None, act: int = ACT_NONE, status=None, stream=None) -> None:
@@ -560,13 +568,14 @@ def clearmoe_fp8_gemm(A: Fp8Matrix, W: Fp8Matrix, out, bias=None, act: int = ACT
         if bias.numel() != W.rows:
             raise ValueError(f"bias must have {W.rows} elements, got {bias.numel()}")
         bp, bdt = _ptr(bias), _dtype(bias)
+    sp = _int32(status, None, "status")
     if blocks:
-        code = calls.gemm_fp8(A.addr, W.addr, bp, bdt, act, _ptr(status), out.addr, _stream(stream))
+        code = calls.gemm_fp8(A.addr, W.addr, bp, bdt, act, sp, out.addr, _stream(stream))
         if code:
             raise ClearMoEError(code, "clearmoe_fp8_gemm_fp8")
         return
     p, dt, ld = _matrix(out, A.rows, W.rows, "out")
-    code = calls.gemm(A.addr, W.addr, bp, bdt, act, _ptr(status), p, dt, ld, _stream(stream))
+    code = calls.gemm(A.addr, W.addr, bp, bdt, act, sp, p, dt, ld, _stream(stream))
     if code:
         raise ClearMoEError(code, "clearmoe_fp8_gemm")
 
@@ -578,11 +587,12 @@ def clearmoe_fp8_grouped_gemm(A: Fp8Matrix, W, offsets, out, perm=None, bias=Non
         _refuse_kind("A", False)
     if not all(getattr(m, "weight", True) for m in W):
         _refuse_kind("every W", True)
-    if offsets.numel() != len(W) + 1 or (perm is not None and perm.numel() != A.rows):
-        raise ValueError("offsets must have one entry per matrix and one more, perm one per row of A")
+    if not len(W) or offsets is None:
+        raise ValueError("a grouped product needs matrices and the offsets of their rows")
+    off, rows = _int32(offsets, len(W) + 1, "offsets"), _int32(perm, A.rows, "perm")
     p, dt, ld = _matrix(out, A.rows, W[0].rows, "out")
     arr = (clearmoe_fp8 * len(W))(*[m.c for m in W])
-    _check(lib().clearmoe_fp8_grouped_gemm(A.ref, arr, len(W), _ptr(offsets), _ptr(perm),
+    _check(lib().clearmoe_fp8_grouped_gemm(A.ref, arr, len(W), off, rows,
                                            _epilogue(bias, act, status, W[0].rows), p, dt, ld, _stream(stream)),
            "clearmoe_fp8_grouped_gemm")
 

@@ -109,14 +109,14 @@ static PyObject* ffn_fp8(PyObject* self, PyObject* const* args, Py_ssize_t n) {
 
 /* ---- from tensors ---- */
 static PyObject *s_is_cuda, *s_shape, *s_stride, *s_data_ptr, *s_dtype, *s_is_contiguous, *s_numel, *s_cuda_stream;
-static PyObject *g_bf16, *g_f32, *g_get_device, *g_raw_stream; /* torch's dtypes; the current device; its current stream */
+static PyObject *g_bf16, *g_f32, *g_i32, *g_get_device, *g_raw_stream; /* torch's dtypes; the current device; its current stream */
 
-/* bfloat16, float32, a function giving the current device, one giving a device's current stream */
+/* bfloat16, float32, int32, a function giving the current device, one giving a device's current stream */
 static PyObject* bind_torch(PyObject* self, PyObject* const* args, Py_ssize_t n) {
-    PyObject** to[4] = {&g_bf16, &g_f32, &g_get_device, &g_raw_stream};
+    PyObject** to[5] = {&g_bf16, &g_f32, &g_i32, &g_get_device, &g_raw_stream};
     (void)self;
-    if (n != 4) return PyErr_Format(PyExc_TypeError, "4 arguments expected, got %zd", n);
-    for (int i = 0; i < 4; ++i) {
+    if (n != 5) return PyErr_Format(PyExc_TypeError, "5 arguments expected, got %zd", n);
+    for (int i = 0; i < 5; ++i) {
         Py_INCREF(args[i]);
         Py_XSETREF(*to[i], args[i]);
     }
@@ -185,6 +185,17 @@ static int bias_of(PyObject* t, int64_t n, int64_t* p, int32_t* dt) {
     }
     return integer(PyObject_CallMethodNoArgs(t, s_numel), &numel) && numel == n && dense(t, p) && dtype_of(t, dt);
 }
+/* A status word, or None. */
+static int status_of(PyObject* t, int64_t* p) {
+    int64_t numel;
+    *p = 0;
+    if (t == Py_None) return 1;
+    PyObject* o = PyObject_GetAttr(t, s_dtype);
+    const int ok = o && o == g_i32;
+    if (!o) PyErr_Clear();
+    Py_XDECREF(o);
+    return ok && integer(PyObject_CallMethodNoArgs(t, s_numel), &numel) && numel >= 1 && dense(t, p);
+}
 static int stream_of(PyObject* stream, int64_t* s) {
     if (!g_raw_stream) return 0;
     if (stream != Py_None) return integer(PyObject_GetAttr(stream, s_cuda_stream), s);
@@ -218,7 +229,7 @@ static PyObject* gemm_t(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     (void)self;
     if (n != 9) return PyErr_Format(PyExc_TypeError, "9 arguments expected, got %zd", n);
     if (!integers(args, 5, 5, v)) return NULL;
-    if (!stream_of(args[8], &s) || !bias_of(args[5], v[3], &bias, &bias_dt) || !dense(args[6], &status) ||
+    if (!stream_of(args[8], &s) || !bias_of(args[5], v[3], &bias, &bias_dt) || !status_of(args[6], &status) ||
         !matrix(args[7], v[2], v[3], &out, &dt, &ld))
         Py_RETURN_NONE;
     const clearmoe_fp8_epilogue epi = {AT(bias), bias_dt, (int32_t)v[4], AT(status)};

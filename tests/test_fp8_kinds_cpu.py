@@ -23,10 +23,10 @@ def matrix(rows, cols, weight):
 
 
 class Dense:  # a CUDA tensor as far as the binding looks
-    is_cuda, dtype = True, "torch.float32"
+    is_cuda = True
 
-    def __init__(self, *shape):
-        self.shape = shape
+    def __init__(self, *shape, dtype="torch.float32"):
+        self.shape, self.dtype = shape, dtype
 
     def stride(self):
         return self.shape[1], 1
@@ -61,7 +61,8 @@ GOOD = [
     lambda: cm.clearmoe_fp8_quantize_weight(Dense(300, 64), weight(300, 64), stream=Stream()),
     lambda: cm.clearmoe_fp8_gemm(rows(300, 64), weight(200, 64), Dense(300, 200), stream=Stream()),
     lambda: cm.clearmoe_fp8_gemm(rows(300, 64), weight(200, 64), rows(300, 200), stream=Stream()),
-    lambda: cm.clearmoe_fp8_grouped_gemm(rows(300, 64), [weight(200, 64)] * 2, Dense(3, 1), Dense(300, 200), stream=Stream()),
+    lambda: cm.clearmoe_fp8_grouped_gemm(rows(300, 64), [weight(200, 64)] * 2, Dense(3, 1, dtype="torch.int32"),
+                                         Dense(300, 200), stream=Stream()),
 ]
 WRONG = [
     lambda: cm.clearmoe_fp8_quantize_rows(Dense(300, 64), weight(300, 64), stream=Stream()),
@@ -87,3 +88,30 @@ def test_the_right_kind_reaches_the_library(call):
 def test_the_wrong_kind_is_refused(call):
     with pytest.raises(ValueError, match="8-bit blocks of"):
         call()
+
+
+def indices(n, dtype="torch.int32"):
+    return Dense(n, 1, dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype,gather,offsets,perm,status", [
+    ("torch.int32", 301, 4, 299, 0), ("torch.int64", 300, 3, 300, 1), ("torch.int16", 300, 3, 300, 1), ("torch.float32", 300, 3, 300, 1)])
+def test_indices_of_another_type_or_number_are_refused(dtype, gather, offsets, perm, status):
+    """Kernels read them as int32: of a narrower type past their end, of a wider one other rows."""
+    A, W, out = rows(300, 64), weight(200, 64), Dense(300, 200)
+    fine = dict(offsets=indices(3), perm=indices(300))
+    for name, n in (("offsets", offsets), ("perm", perm)):
+        kw = {**fine, name: indices(n, dtype)}
+        with pytest.raises(ValueError, match=name + " must be int32"):
+            cm.clearmoe_fp8_grouped_gemm(A, [W] * 2, out=out, stream=Stream(), **kw)
+    with pytest.raises(ValueError, match="gather must be int32"):
+        cm.clearmoe_fp8_quantize_rows(Dense(1000, 64), A, gather=indices(gather, dtype), stream=Stream())
+    for o in (out, rows(300, 200)):
+        with pytest.raises(ValueError, match="status must be int32"):
+            cm.clearmoe_fp8_gemm(A, W, o, status=indices(status, dtype), stream=Stream())
+    with pytest.raises(ValueError, match="status must be int32"):
+        cm.clearmoe_fp8_grouped_gemm(A, [W] * 2, out=out, stream=Stream(), status=indices(status, dtype), **fine)
+    with pytest.raises(cm.ClearMoEError):  # these reach the library
+        cm.clearmoe_fp8_grouped_gemm(A, [W] * 2, out=out, stream=Stream(), status=indices(1), **fine)
+    with pytest.raises(ValueError):
+        cm.clearmoe_fp8_grouped_gemm(A, [], out=out, stream=Stream(), **fine)

@@ -1,0 +1,32 @@
+"""What the binding's quick path refuses on GPU tensors, and that a refused call has written nothing."""
+import pytest
+import torch
+
+from paper_2606_28516_gb300 import clearmoe as cm
+
+pytestmark = pytest.mark.gpu
+
+
+def test_status_and_indices():
+    A, W, out = cm.fp8_rows(4, 128), cm.fp8_weight(8, 128), torch.zeros(4, 8, device="cuda")
+    cm.clearmoe_fp8_quantize_rows(torch.ones(4, 128, device="cuda"), A)
+    cm.clearmoe_fp8_quantize_weight(torch.ones(8, 128, device="cuda"), W)
+    i = lambda *v, dtype=torch.int32: torch.tensor(v, dtype=dtype, device="cuda")  # noqa: E731
+    for bad in (i(0, dtype=torch.int64), i(0, dtype=torch.uint8), i(0, dtype=torch.float32), i(), i(0, 0, 0, 0)[::2]):
+        with pytest.raises(ValueError):
+            cm.clearmoe_fp8_gemm(A, W, out, status=bad)
+    for bad in (i(0, 4, dtype=torch.int64), i(0, 2, 4), i(0, 0, 4, 4)[::2]):
+        with pytest.raises(ValueError):
+            cm.clearmoe_fp8_grouped_gemm(A, [W], bad, out)
+    for bad in (i(0, 1, 2, 3, dtype=torch.int64), i(0, 1, 2)):
+        with pytest.raises(ValueError):
+            cm.clearmoe_fp8_grouped_gemm(A, [W], i(0, 4), out, perm=bad)
+        with pytest.raises(ValueError):
+            cm.clearmoe_fp8_quantize_rows(torch.ones(9, 128, device="cuda"), A, gather=bad)
+    torch.cuda.synchronize()
+    assert not out.any()
+    status = i(0)
+    cm.clearmoe_fp8_gemm(A, W, out, status=status)
+    assert bool((out == 128).all()) and status.item() == 0
+    cm.clearmoe_fp8_grouped_gemm(A, [W], i(0, 4), out.zero_(), perm=i(3, 2, 1, 0), status=status)
+    assert bool((out == 128).all()) and status.item() == 0
