@@ -363,9 +363,15 @@ typedef struct {
 
 /* Activations x [out->rows x out->cols] (dtype CLEARMOE_F32 or CLEARMOE_BF16, rows ld elements apart, ld >=
  * cols, any alignment of the element type) to 1 x 128 blocks. gather (nullable, int32 [out->rows], device): row
- * i is x's row gather[i] instead. No handle; stream-ordered; x may be the preceding kernel's output. */
+ * i is x's row gather[i] instead; every entry must be a row of x, which this call cannot check (the next one does).
+ * No handle; stream-ordered; x may be the preceding kernel's output. */
 int clearmoe_fp8_quantize_rows(const void* x, int32_t dtype, int64_t ld, const int32_t* gather, const clearmoe_fp8* out,
                                void* stream);
+
+/* The same with the number of x's rows: of an entry of gather outside [0, x_rows) nothing is read, and the row is NaN
+ * (s = 255). x_rows >= 1, and at least out->rows without gather. */
+int clearmoe_fp8_quantize_gathered(const void* x, int64_t x_rows, int32_t dtype, int64_t ld, const int32_t* gather,
+                                   const clearmoe_fp8* out, void* stream);
 
 /* A weight matrix W [out->rows x out->cols] to 128 x 128 blocks; arguments as above. Once per weight set. */
 int clearmoe_fp8_quantize_weight(const void* W, int32_t dtype, int64_t ld, const clearmoe_fp8* out, void* stream);

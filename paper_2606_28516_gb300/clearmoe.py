@@ -107,6 +107,7 @@ _SIGS = {
     "clearmoe_route_noalloc": [_P, _I64, _I32, _I32, ctypes.POINTER(clearmoe_router), _I32, _P, _P,
                                _P, _P, _P, _P],
     "clearmoe_fp8_quantize_rows": [_P, _I32, _I64, _P, ctypes.POINTER(clearmoe_fp8), _P],
+    "clearmoe_fp8_quantize_gathered": [_P, _I64, _I32, _I64, _P, ctypes.POINTER(clearmoe_fp8), _P],
     "clearmoe_fp8_quantize_weight": [_P, _I32, _I64, ctypes.POINTER(clearmoe_fp8), _P],
     "clearmoe_fp8_dequantize": [ctypes.POINTER(clearmoe_fp8), _I32, _P, _I32, _I64, _P],
     "clearmoe_fp8_gemm": [ctypes.POINTER(clearmoe_fp8), ctypes.POINTER(clearmoe_fp8),
@@ -510,14 +511,20 @@ def _matrix(t, rows, cols, what):
 
 
 def clearmoe_fp8_quantize_rows(x, out: Fp8Matrix, gather=None, stream=None) -> None:
-    """x [rows x cols] (bf16 or fp32, any row pitch) to out in 1 x 128 blocks; gather: int32 source rows."""
+    """x [rows x cols] (bf16 or fp32, any row pitch) to out in 1 x 128 blocks; gather: int32 source rows (one outside x
+    gives a row of NaN)."""
     if getattr(out, "weight", False):
         _refuse_kind("out", False)
     calls = _calls or _bind_calls()
-    code = calls.quantize_rows_t(x, out.rows, out.cols, out.addr, stream) if gather is None else None
+    if gather is not None:
+        p, dt, ld = _matrix(x, None, out.cols, "x")
+        _check(lib().clearmoe_fp8_quantize_gathered(p, x.shape[0], dt, ld, _int32(gather, out.rows, "gather"), out.ref,
+                                                    _stream(stream)), "clearmoe_fp8_quantize_gathered")
+        return
+    code = calls.quantize_rows_t(x, out.rows, out.cols, out.addr, stream)
     if code is None:
-        p, dt, ld = _matrix(x, out.rows if gather is None else None, out.cols, "x")
-        code = calls.quantize_rows(p, dt, ld, _int32(gather, out.rows, "gather"), out.addr, _stream(stream))
+        p, dt, ld = _matrix(x, out.rows, out.cols, "x")
+        code = calls.quantize_rows(p, dt, ld, None, out.addr, _stream(stream))
     if code:
         raise ClearMoEError(code, "clearmoe_fp8_quantize_rows")
 

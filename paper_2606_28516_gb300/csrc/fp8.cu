@@ -58,8 +58,15 @@ constexpr int Q_THREADS = 256;
 constexpr int Q_CTAS = 32;  // an SM, at the most
 constexpr int Q_CTA_BLOCKS = Q_THREADS / 8;
 
-// A lane's 16 values of a block to e4m3 at q, the block's scale byte at scale.
-__device__ __forceinline__ void quantize_block(float (&v)[2][8], int l8, bool write, uint8_t* q, uint8_t* scale) {
+// The row of x that row `row` is made from; `inside`: x has it (an index that gather may not have is not followed).
+__device__ __forceinline__ int64_t source_row(const QuantArgs& a, int64_t row, bool live, bool& inside) {
+    const int64_t src = a.gather && live ? (int64_t)__ldcg(a.gather + row) : row;
+    inside = !a.gather || (uint64_t)src < (uint64_t)a.src_rows;
+    return src;
+}
+
+// A lane's 16 values of a block to e4m3 at q, the block's scale byte at scale; none: NaN instead.
+__device__ __forceinline__ void quantize_block(float (&v)[2][8], int l8, bool write, uint8_t* q, uint8_t* scale, bool none = false) {
     float m = 0.f;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -67,7 +74,7 @@ __device__ __forceinline__ void quantize_block(float (&v)[2][8], int l8, bool wr
         for (int c = 0; c < 8; c += 2) m = max_abs3(m, v[h][c], v[h][c + 1]);
 #pragma unroll
     for (int o = 4; o; o >>= 1) m = max_abs(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-    const uint32_t s = fp8_scale_byte(abs_bits(m));
+    const uint32_t s = none ? 255u : fp8_scale_byte(abs_bits(m));
     const float inv = fp8_inverse_scale(s);
     uint32_t o[4];
 #pragma unroll
@@ -96,13 +103,13 @@ __device__ __forceinline__ uint32_t max_abs_bf16x2(uint32_t a, uint32_t b) {  //
 }
 // quantize_block on such words: magnitudes and scaling two values an instruction, both exact in bf16 (the scale is a power
 // of two; what it takes below bf16's range is far below e4m3's), so that only the conversion takes them one by one.
-__device__ __forceinline__ void quantize_block_bf16(const uint4 (&r)[2], int l8, bool write, uint8_t* q, uint8_t* scale) {
+__device__ __forceinline__ void quantize_block_bf16(const uint4 (&r)[2], int l8, bool write, uint8_t* q, uint8_t* scale, bool none = false) {
     const uint32_t w[8] = {r[0].x, r[0].y, r[0].z, r[0].w, r[1].x, r[1].y, r[1].z, r[1].w};
     uint32_t m = max_abs_bf16x2(max_abs_bf16x2(max_abs_bf16x2(w[0], w[1]), max_abs_bf16x2(w[2], w[3])),
                                 max_abs_bf16x2(max_abs_bf16x2(w[4], w[5]), max_abs_bf16x2(w[6], w[7])));
 #pragma unroll
     for (int o = 4; o; o >>= 1) m = max_abs_bf16x2(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-    const uint32_t s = fp8_scale_byte((max_abs_bf16x2(m, __byte_perm(m, m, 0x1032)) & 0x7FFFu) << 16);
+    const uint32_t s = none ? 255u : fp8_scale_byte((max_abs_bf16x2(m, __byte_perm(m, m, 0x1032)) & 0x7FFFu) << 16);
     const uint32_t inv = __byte_perm(__float_as_uint(fp8_inverse_scale(s)), 0, 0x3232);
     uint32_t o[4];
 #pragma unroll
@@ -130,10 +137,11 @@ __global__ void __launch_bounds__(Q_THREADS) quantize_bf16_kernel(const QuantArg
     pdl_launch_dependents();  // after the wait: the next kernel may read weights that one before this has written
     while (__any_sync(0xFFFFFFFFu, row < a.rows)) {
         const bool live = row < a.rows;
-        const int64_t src = a.gather && live ? (int64_t)__ldcg(a.gather + row) : row;
+        bool inside;
+        const int64_t src = source_row(a, row, live, inside);
         uint4 r[2];
-        load16_bf16(static_cast<const uint16_t*>(a.x) + src * a.ld, kb * 128 + l8 * 16, a.K, live, r);
-        quantize_block_bf16(r, l8, live, a.q + row * a.ldq + kb * 128 + l8 * 16, a.scale + row * a.lds + kb);
+        load16_bf16(static_cast<const uint16_t*>(a.x) + src * a.ld, kb * 128 + l8 * 16, a.K, live && inside, r);
+        quantize_block_bf16(r, l8, live, a.q + row * a.ldq + kb * 128 + l8 * 16, a.scale + row * a.lds + kb, !inside);
         row += step_row;
         kb += step_kb;
         if (kb >= a.kb) kb -= a.kb, ++row;
@@ -159,19 +167,21 @@ __global__ void __launch_bounds__(Q_THREADS, 5) quantize_rows_kernel(const Quant
     pdl_launch_dependents();  // after the wait: the next kernel may read weights that one before this has written
     while (__any_sync(0xFFFFFFFFu, row < a.rows)) {
         const bool live = row < a.rows;
-        const int64_t src = a.gather && live ? (int64_t)__ldcg(a.gather + row) : row;
+        bool inside;
+        const int64_t src = source_row(a, row, live, inside);
+        const bool reads = live && inside;
         const T* x = static_cast<const T*>(a.x) + src * a.ld;
         float v[2][8];
         if (VEC) {
-            load8<T, VEC>(x, (int64_t)kb * 128 + l8 * 16, live ? a.K : 0, v[0]);
-            load8<T, VEC>(x, (int64_t)kb * 128 + l8 * 16 + 8, live ? a.K : 0, v[1]);
+            load8<T, VEC>(x, (int64_t)kb * 128 + l8 * 16, reads ? a.K : 0, v[0]);
+            load8<T, VEC>(x, (int64_t)kb * 128 + l8 * 16 + 8, reads ? a.K : 0, v[1]);
         } else {
             float* sx = s_x[VEC ? 0 : threadIdx.x >> 5];
             float f[16];
 #pragma unroll
             for (int b = 0; b < 4; ++b) {  // the warp's four blocks
                 const T* p = reinterpret_cast<const T*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(x), 8 * b));
-                const int64_t k = (int64_t)__shfl_sync(0xFFFFFFFFu, live ? kb : a.kb, 8 * b) * 128 + lane;
+                const int64_t k = (int64_t)__shfl_sync(0xFFFFFFFFu, reads ? kb : a.kb, 8 * b) * 128 + lane;
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
                     f[4 * b + c] = k + 32 * c >= a.K  ? 0.f
@@ -194,7 +204,7 @@ __global__ void __launch_bounds__(Q_THREADS, 5) quantize_rows_kernel(const Quant
             }
             __syncwarp();
         }
-        quantize_block(v, l8, live, a.q + row * a.ldq + kb * 128 + l8 * 16, a.scale + row * a.lds + kb);
+        quantize_block(v, l8, live, a.q + row * a.ldq + kb * 128 + l8 * 16, a.scale + row * a.lds + kb, !inside);
         row += step_row;
         kb += step_kb;
         if (kb >= a.kb) kb -= a.kb, ++row;
@@ -471,13 +481,21 @@ extern "C" {
 
 int clearmoe_fp8_quantize_rows(const void* x, int32_t dtype, int64_t ld, const int32_t* gather, const clearmoe_fp8* out,
                                void* stream) {
+    // gathered rows without a count: 2^31, that is any index but a negative one
+    return clearmoe_fp8_quantize_gathered(x, (int64_t)1 << 31, dtype, ld, gather, out, stream);
+}
+
+int clearmoe_fp8_quantize_gathered(const void* x, int64_t x_rows, int32_t dtype, int64_t ld, const int32_t* gather,
+                                   const clearmoe_fp8* out, void* stream) {
     const int rc = check_pair(x, dtype, ld, out);
     if (rc) return rc;
+    if (x_rows < 1 || (!gather && x_rows < out->rows)) return CLEARMOE_EINVAL;
     if (gather && !aligned_to(gather, 4)) return CLEARMOE_EINVAL;
     const int sms = cm::current_device_sms();
     if (sms <= 0) return CLEARMOE_ECUDA;
     cm::QuantArgs a = quant_args(x, ld, out);
     a.gather = gather;
+    a.src_rows = x_rows;
     return cuda_code(cm::launch_quantize_rows(a, dtype, sms, static_cast<cudaStream_t>(stream)));
 }
 

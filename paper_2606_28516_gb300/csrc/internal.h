@@ -305,6 +305,7 @@ struct QuantArgs {
     int64_t rows, K;
     int kb;  // blocks of 128 columns per row
     const int32_t* gather;  // source row of row i (nullable)
+    int64_t src_rows;       // x's rows: a row gathered from outside them is NaN
     const float2* ln_stats;  // launch_slots_quantize: (mean, rstd) per token, applied first (nullable)
     uint8_t* q;
     uint8_t* scale;

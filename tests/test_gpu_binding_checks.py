@@ -30,3 +30,28 @@ def test_status_and_indices():
     assert bool((out == 128).all()) and status.item() == 0
     cm.clearmoe_fp8_grouped_gemm(A, [W], i(0, 4), out.zero_(), perm=i(3, 2, 1, 0), status=status)
     assert bool((out == 128).all()) and status.item() == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("K,pitch", [(256, 256), (200, 203)])
+def test_gathered_rows_outside_x_are_nan(dtype, K, pitch):
+    """Every load of the kernels: aligned bf16 and fp32 rows, unaligned ones."""
+    x = torch.randn(7, pitch, device="cuda").to(dtype)[:, :K]
+    at = [6, -1, 0, 7, 2 ** 31 - 1, -2 ** 31, 3, 3, 2000000]
+    g = cm.fp8_rows(len(at), K)
+    cm.clearmoe_fp8_quantize_rows(x, g, gather=torch.tensor(at, dtype=torch.int32, device="cuda"))
+    plain, got, want = cm.fp8_rows(7, K), torch.empty(len(at), K, device="cuda"), torch.empty(7, K, device="cuda")
+    cm.clearmoe_fp8_quantize_rows(x, plain)
+    cm.clearmoe_fp8_dequantize(g, got)
+    cm.clearmoe_fp8_dequantize(plain, want)
+    kb = -(-K // 128)
+    for i, r in enumerate(at):
+        if 0 <= r < 7:
+            assert torch.equal(got[i], want[r])
+            assert torch.equal(g.q.view(torch.uint8)[i], plain.q.view(torch.uint8)[r])
+        else:
+            assert bool(got[i].isnan().all()) and bool((g.scale[i, :kb] == 255).all())
+    L = cm.lib()
+    for rows in (0, -1):
+        assert L.clearmoe_fp8_quantize_gathered(x.data_ptr(), rows, cm.F32, 256, None, plain.ref, None) == cm.EINVAL
+    assert L.clearmoe_fp8_quantize_gathered(x.data_ptr(), 6, cm.F32, 256, None, plain.ref, None) == cm.EINVAL
