@@ -611,10 +611,11 @@ def clearmoe_debug_fp8_kernel(width: int = 0, pair: int = 0) -> None:
 
 # ------------------------------------------------------------- a folded layer's weights and its forwards
 class FfnWeights:
-    """A folded layer's weights bound once (clearmoe_ffn_weights), with the tensors kept alive."""
+    """A folded layer's weights bound once (clearmoe_ffn_weights), with the tensors kept alive; d and the layer's dtype, which
+    tokens have to be of."""
 
-    def __init__(self, c, keep):
-        self.c, self.keep = c, keep
+    def __init__(self, c, keep, d: int, dtype: int):
+        self.c, self.keep, self.d, self.dtype = c, keep, d, dtype
         self.ref, self.addr = ctypes.pointer(c), ctypes.addressof(c)
 
 
@@ -623,6 +624,7 @@ def ffn_weights(W1, b1, W_comb, Wg, bg, b2=None, W2=None, cls_stride: int = 0,
     """W1 [H x d], W_comb (E matrices [d x H]) and W2 (class tokens' dense path) as tensors of the layer's dtype, or
     all as Fp8Matrix weights; b1, b2, Wg, bg in the layer's dtype."""
     E, d = Wg.shape
+    layer = _dtype(Wg)
     if len(W_comb) != E or E > 16:
         raise ValueError(f"{E} experts (at most 16) need as many matrices, got {len(W_comb)}")
     fp8 = isinstance(W1, Fp8Matrix)
@@ -631,17 +633,22 @@ def ffn_weights(W1, b1, W_comb, Wg, bg, b2=None, W2=None, cls_stride: int = 0,
     def mat(W, rows, cols):
         if isinstance(W, Fp8Matrix) != fp8 or (fp8 and not W.weight):
             raise ValueError("W1, W_comb and W2 are all tensors or all Fp8Matrix weights")
+        shape = (W.rows, W.cols) if fp8 else tuple(W.shape)
+        if shape != (rows, cols):
+            raise ValueError(f"a weight matrix must be [{rows} x {cols}], got {shape}")
         if fp8:
             return W.c
-        if tuple(W.shape) != (rows, cols):
-            raise ValueError(f"a weight matrix must be [{rows} x {cols}], got {tuple(W.shape)}")
+        if _dtype(W) != layer:
+            raise ValueError(f"W1, W_comb and W2 must be of the router's dtype, got {W.dtype} and {Wg.dtype}")
         return clearmoe_fp8(_ptr(W), None, rows, cols)
 
     for name, t, n in (("b1", b1, H), ("bg", bg, E), ("b2", b2, d)):
-        if t is not None and t.numel() != n:
-            raise ValueError(f"{name} must have {n} elements, got {t.numel()}")
+        if t is not None and (t.numel() != n or _dtype(t) != layer):
+            raise ValueError(f"{name} must have {n} elements of the router's dtype, got {t.numel()} of {t.dtype}")
+    if fp8 and layer != BF16:
+        raise ValueError(f"8-bit weights are of bf16 layers: b1, b2, Wg and bg must be bfloat16, got {Wg.dtype}")
     c = clearmoe_ffn_weights()
-    c.dtype = FP8 if fp8 else _dtype(W1)
+    c.dtype = FP8 if fp8 else layer
     c.E = E
     c.W1 = mat(W1, H, d)
     for e in range(E):
@@ -651,24 +658,34 @@ def ffn_weights(W1, b1, W_comb, Wg, bg, b2=None, W2=None, cls_stride: int = 0,
     c.b1, c.b2 = _ptr(b1), _ptr(b2)
     c.router = _router(Wg, bg)
     c.cls_stride, c.input_layernorm = int(cls_stride), int(bool(input_layernorm))
-    return FfnWeights(c, (W1, b1, list(W_comb), Wg, bg, b2, W2))
+    return FfnWeights(c, (W1, b1, list(W_comb), Wg, bg, b2, W2), d, layer)
+
+
+def _tokens(x, out, w):
+    """Number of tokens and pointers of x and out, both [T x d] in the layer's dtype."""
+    for name, t in (("x", x), ("out", out)):
+        if len(t.shape) != 2 or t.shape[1] != w.d or t.shape[0] != x.shape[0] or _dtype(t) != w.dtype:
+            raise ValueError(f"{name} must be [T x {w.d}] in the layer's dtype, x and out of the same T; got {tuple(t.shape)} {t.dtype}")
+    return x.shape[0], _ptr(x), _ptr(out)
 
 
 def clearmoe_ffn_forward_few(layer: int, x, w: FfnWeights, out, stream=None) -> None:
     """The whole folded layer for 1 to FEW_MAX tokens."""
-    calls, T = _calls or _bind_calls(), x.shape[0]
-    code = calls.ffn_few_t(layer, T, w.addr, x, out, stream)
+    calls = _calls or _bind_calls()
+    code = calls.ffn_few_t(layer, w.addr, w.d, w.dtype, x, out, stream)
     if code is None:
-        code = calls.ffn_few(layer, _ptr(x), T, w.addr, _ptr(out), _stream(stream))
+        T, xp, op = _tokens(x, out, w)
+        code = calls.ffn_few(layer, xp, T, w.addr, op, _stream(stream))
     if code:
         raise ClearMoEError(code, "clearmoe_ffn_forward_few")
 
 
 def clearmoe_ffn_forward_fp8(layer: int, x, w: FfnWeights, out, stream=None) -> None:
     """The whole folded layer with both products in 8-bit blocks."""
-    calls, T = _calls or _bind_calls(), x.shape[0]
-    code = calls.ffn_fp8_t(layer, T, w.addr, x, out, stream)
+    calls = _calls or _bind_calls()
+    code = calls.ffn_fp8_t(layer, w.addr, w.d, w.dtype, x, out, stream)
     if code is None:
-        code = calls.ffn_fp8(layer, _ptr(x), T, w.addr, _ptr(out), _stream(stream))
+        T, xp, op = _tokens(x, out, w)
+        code = calls.ffn_fp8(layer, xp, T, w.addr, op, _stream(stream))
     if code:
         raise ClearMoEError(code, "clearmoe_ffn_forward_fp8")

@@ -239,16 +239,28 @@ static PyObject* gemm_t(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     return PyLong_FromLong(rc);
 }
 
-/* layer, T, weights, x, out, stream */
+/* A dense [rows x cols] matrix of one dtype; rows < 0: any number, which it gets. */
+static int tokens(PyObject* t, int64_t* rows, int64_t cols, int32_t dtype, int64_t* p) {
+    int64_t shape[2];
+    int32_t dt;
+    if (t == Py_None || !pair(PyObject_GetAttr(t, s_shape), shape) || shape[1] != cols || (*rows >= 0 && shape[0] != *rows) ||
+        !dtype_of(t, &dt) || dt != dtype)
+        return 0;
+    *rows = shape[0];
+    return dense(t, p);
+}
+
+/* layer, weights, d, dtype, x, out, stream */
 static PyObject* ffn_t(PyObject* const* args, Py_ssize_t n,
                        int (*fn)(clearmoe_layer*, const void*, int64_t, const clearmoe_ffn_weights*, void*, void*)) {
-    int64_t v[3], x, out, s;
+    int64_t v[4], T = -1, x, out, s;
     int rc;
-    if (n != 6) return PyErr_Format(PyExc_TypeError, "6 arguments expected, got %zd", n);
-    if (!integers(args, 3, 3, v)) return NULL;
-    if (!stream_of(args[5], &s) || !dense(args[3], &x) || !dense(args[4], &out)) Py_RETURN_NONE;
+    if (n != 7) return PyErr_Format(PyExc_TypeError, "7 arguments expected, got %zd", n);
+    if (!integers(args, 4, 4, v)) return NULL;
+    if (!stream_of(args[6], &s) || !tokens(args[4], &T, v[2], (int32_t)v[3], &x) || !tokens(args[5], &T, v[2], (int32_t)v[3], &out))
+        Py_RETURN_NONE;
     Py_BEGIN_ALLOW_THREADS
-    rc = fn(PTR(0), AT(x), v[1], PTR(2), AT(out), AT(s));
+    rc = fn(PTR(0), AT(x), T, PTR(1), AT(out), AT(s));
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(rc);
 }

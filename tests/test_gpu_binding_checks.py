@@ -55,3 +55,22 @@ def test_gathered_rows_outside_x_are_nan(dtype, K, pitch):
     for rows in (0, -1):
         assert L.clearmoe_fp8_quantize_gathered(x.data_ptr(), rows, cm.F32, 256, None, plain.ref, None) == cm.EINVAL
     assert L.clearmoe_fp8_quantize_gathered(x.data_ptr(), 6, cm.F32, 256, None, plain.ref, None) == cm.EINVAL
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_tokens_and_outputs_of_a_layer(dtype):
+    d, H, other = 64, 256, torch.float32 if dtype == torch.bfloat16 else torch.bfloat16
+    h = cm.clearmoe_layer_create(8, d, H, 2, 16, cm.BF16 if dtype == torch.bfloat16 else cm.F32)
+    g = lambda *s, t=dtype: torch.zeros(*s, device="cuda", dtype=t)  # noqa: E731
+    w = cm.ffn_weights(g(H, d), g(H), [g(d, H)] * 2, g(2, d), g(2), b2=torch.ones(d, device="cuda", dtype=dtype))
+    x, out = g(4, d), g(4, d)
+    for bad_x, bad_out in ((g(4, d, t=other), out), (x, g(4, d, t=other)), (x, g(3, d)), (x, g(4, d // 2)), (g(4, 2 * d), out),
+                           (g(2, 2, d), out), (g(4 * d), out), (x, g(4 * d))):
+        for call in (cm.clearmoe_ffn_forward_few, cm.clearmoe_ffn_forward_fp8):
+            with pytest.raises(ValueError):
+                call(h, bad_x, w, bad_out)
+    torch.cuda.synchronize()
+    assert not out.any()
+    cm.clearmoe_ffn_forward_few(h, x, w, out)
+    assert bool((out == 1).all())
+    cm.clearmoe_layer_destroy(h)
