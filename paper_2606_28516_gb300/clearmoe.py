@@ -672,7 +672,7 @@ def _tokens(x, out, w):
 def clearmoe_ffn_forward_few(layer: int, x, w: FfnWeights, out, stream=None) -> None:
     """The whole folded layer for 1 to FEW_MAX tokens."""
     calls = _calls or _bind_calls()
-    code = calls.ffn_few_t(layer, w.addr, w.d, w.dtype, x, out, stream)
+    code = calls.ffn_few_t(layer, w.addr, x, out, stream)
     if code is None:
         T, xp, op = _tokens(x, out, w)
         code = calls.ffn_few(layer, xp, T, w.addr, op, _stream(stream))
@@ -683,7 +683,7 @@ def clearmoe_ffn_forward_few(layer: int, x, w: FfnWeights, out, stream=None) -> 
 def clearmoe_ffn_forward_fp8(layer: int, x, w: FfnWeights, out, stream=None) -> None:
     """The whole folded layer with both products in 8-bit blocks."""
     calls = _calls or _bind_calls()
-    code = calls.ffn_fp8_t(layer, w.addr, w.d, w.dtype, x, out, stream)
+    code = calls.ffn_fp8_t(layer, w.addr, x, out, stream)
     if code is None:
         T, xp, op = _tokens(x, out, w)
         code = calls.ffn_fp8(layer, xp, T, w.addr, op, _stream(stream))

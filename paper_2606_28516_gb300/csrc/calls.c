@@ -250,17 +250,19 @@ static int tokens(PyObject* t, int64_t* rows, int64_t cols, int32_t dtype, int64
     return dense(t, p);
 }
 
-/* layer, weights, d, dtype, x, out, stream */
+/* layer, weights (not null), x, out, stream */
 static PyObject* ffn_t(PyObject* const* args, Py_ssize_t n,
                        int (*fn)(clearmoe_layer*, const void*, int64_t, const clearmoe_ffn_weights*, void*, void*)) {
-    int64_t v[4], T = -1, x, out, s;
+    int64_t v[2], T = -1, x, out, s;
     int rc;
-    if (n != 7) return PyErr_Format(PyExc_TypeError, "7 arguments expected, got %zd", n);
-    if (!integers(args, 4, 4, v)) return NULL;
-    if (!stream_of(args[6], &s) || !tokens(args[4], &T, v[2], (int32_t)v[3], &x) || !tokens(args[5], &T, v[2], (int32_t)v[3], &out))
+    if (n != 5) return PyErr_Format(PyExc_TypeError, "5 arguments expected, got %zd", n);
+    if (!integers(args, 2, 2, v)) return NULL;
+    const clearmoe_ffn_weights* w = PTR(1);
+    const int32_t dtype = w->dtype == CLEARMOE_F32 ? CLEARMOE_F32 : CLEARMOE_BF16; /* the layer's */
+    if (!stream_of(args[4], &s) || !tokens(args[2], &T, w->W1.cols, dtype, &x) || !tokens(args[3], &T, w->W1.cols, dtype, &out))
         Py_RETURN_NONE;
     Py_BEGIN_ALLOW_THREADS
-    rc = fn(PTR(0), AT(x), T, PTR(1), AT(out), AT(s));
+    rc = fn(PTR(0), AT(x), T, w, AT(out), AT(s));
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(rc);
 }
