@@ -135,7 +135,7 @@ struct FewTile {
 
 // acc[j] += the warp's share of the tile (weights and activations started) times its activation rows. sw (8-bit weights): the scale bytes of the
 // tile's rows; sx (FEWV_W8A8): those of the activation rows, ldx bytes apart, rows past the last as the last; both in
-// shared memory. sums (LN): += W 1.
+// shared memory (255 among them: the sums of its row or column mean nothing). sums (LN): += W 1.
 // A step's products are added from zero and then to acc in fp32, so that the tensor cores' truncating accumulation
 // runs over one step (fp32) or one scale block's part (8 bits) only; bf16 outputs, whose own rounding is 2^-9,
 // accumulate in place.
@@ -188,7 +188,7 @@ __device__ __forceinline__ void few_product(float (&acc)[NT][4], float (&sums)[4
                 }
             } else if constexpr (V == FEWV_W8A8) {
                 // both operands widened to fp16, exactly (the warp-level e4m3 MMA is no faster)
-                const float s = fp8_scale(sw[blk]);
+                const uint32_t s = sw[blk];
                 uint32_t f[4][4];
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {
@@ -204,11 +204,11 @@ __device__ __forceinline__ void few_product(float (&acc)[NT][4], float (&sums)[4
                     for (int h = 0; h < 4; ++h)
                         mma_f16(part, f[h][0], f[h][1], f[h][2], f[h][3], fp8x2_to_f16x2(xv[h]), fp8x2_to_f16x2(xv[h] >> 16));
                     const int r = 8 * j + 2 * (lane & 3);
-                    const float s0 = s * fp8_scale(sx[min(r, rows - 1) * ldx + blk]), s1 = s * fp8_scale(sx[min(r + 1, rows - 1) * ldx + blk]);
-                    acc[j][0] = fmaf(part[0], s0, acc[j][0]);
-                    acc[j][1] = fmaf(part[1], s1, acc[j][1]);
-                    acc[j][2] = fmaf(part[2], s0, acc[j][2]);
-                    acc[j][3] = fmaf(part[3], s1, acc[j][3]);
+                    const float2 s0 = fp8_scale_pair(s, sx[min(r, rows - 1) * ldx + blk]), s1 = fp8_scale_pair(s, sx[min(r + 1, rows - 1) * ldx + blk]);
+                    acc[j][0] = fmaf(part[0] * s0.x, s0.y, acc[j][0]);
+                    acc[j][1] = fmaf(part[1] * s1.x, s1.y, acc[j][1]);
+                    acc[j][2] = fmaf(part[2] * s0.x, s0.y, acc[j][2]);
+                    acc[j][3] = fmaf(part[3] * s1.x, s1.y, acc[j][3]);
                 }
             } else {
                 constexpr int NS = F::LANE / 4;  // MMAs of 16 columns per step: four of the lane's columns each

@@ -24,6 +24,14 @@ __device__ __forceinline__ float fp8_inverse_scale(uint32_t s) {
 __device__ __forceinline__ float fp8_scale(uint32_t s) {
     return s == 255u ? __uint_as_float(0x7FC00000u) : s == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(s << 23);
 }
+// Two factors that stand for 2^(a - 127) 2^(b - 127), for a sum of products of e4m3 values: the product itself may lie
+// outside fp32 where the scaled sum does not (a zero sum times an infinity is NaN). Each factor has half the exponent, so
+// that scaling by one after the other rounds or overflows only where the result does. A factor of 2^-127 is taken as 0: the
+// result, below 2^-220, is. Scale bytes of 255 are the caller's to look for.
+__device__ __forceinline__ float2 fp8_scale_pair(uint32_t a, uint32_t b) {
+    const uint32_t h = (a + b) >> 1;
+    return make_float2(__uint_as_float(h << 23), __uint_as_float((a + b - h) << 23));
+}
 // Two values to e4m3, to nearest even; lo in the low byte. NaN becomes e4m3's NaN.
 __device__ __forceinline__ uint32_t fp8_pack2(float lo, float hi) {
     uint16_t v;

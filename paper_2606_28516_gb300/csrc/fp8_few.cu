@@ -16,6 +16,7 @@ namespace {
 template <int NT>
 __global__ void __launch_bounds__(FEW_THREADS, 2) fp8_few_kernel(const __grid_constant__ Fp8GemmArgs a) {
     extern __shared__ float red[];  // the partial sums; then scale bytes: the tile's rows' [nkb], A's rows' [M][nkb]
+    __shared__ uint32_t s_nan[FEW_WARPS];  // bit 0: a NaN scale among the tile's rows', bit 1 + m: among those of A's row m
     uint8_t* s_scale = reinterpret_cast<uint8_t*>(red) + FewT<FEWV_W8A8, NT, 2>::SMEM;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int r0 = blockIdx.x * 16, M = (int)a.M, ldq = a.nkb * 128;
@@ -33,18 +34,27 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) fp8_few_kernel(const __grid_co
     }
     t.start_x();
     const uint8_t* sw = a.sb[0] + (int64_t)(r0 / 128) * a.lds;
+    uint32_t nan = 0;
     for (int i = threadIdx.x; i < (M + 1) * a.nkb; i += FEW_THREADS) {
         const int row = i / a.nkb, b = i - row * a.nkb;
-        s_scale[i] = row == 0 ? __ldcg(sw + b) : __ldcg(a.sa + (int64_t)(row - 1) * a.lds + b);
+        const uint8_t s = row == 0 ? __ldcg(sw + b) : __ldcg(a.sa + (int64_t)(row - 1) * a.lds + b);
+        s_scale[i] = s;
+        if (s == 255) nan |= 1u << row;
     }
+    nan = __reduce_or_sync(0xFFFFFFFFu, nan);
+    if (lane == 0) s_nan[warp] = nan;
     __syncthreads();
     few_product<FEWV_W8A8, NT, 2, false>(acc, sums, t, s_scale, s_scale + a.nkb, a.nkb, M);
     few_stage<NT>(red, acc, warp, lane);
     __syncthreads();
+    nan = 0;
+#pragma unroll
+    for (int w = 0; w < FEW_WARPS; ++w) nan |= s_nan[w];
     for (int i = threadIdx.x; i < M * 16; i += FEW_THREADS) {
         const int m = i >> 4, n = r0 + (i & 15);
         if (n >= a.N) continue;
         float s = few_sum<8 * NT>(red, m, i & 15);
+        if (nan & (1u | 2u << m)) s = __uint_as_float(0x7FC00000u);
         if (a.bias)
             s += a.bias_bf16 ? bf16_to_f32(__ldcg(static_cast<const uint16_t*>(a.bias) + n)) : __ldcg(static_cast<const float*>(a.bias) + n);
         if (a.act == CLEARMOE_ACT_GELU) s = gelu_erf(s);
