@@ -62,8 +62,10 @@ struct FewRow {
                 v[p][i] = V == FEWV_F32 ? __uint_as_float(w[i & 3]) : (i & 1) ? bf16_hi(w[(i >> 1) & 3]) : bf16_lo(w[(i >> 1) & 3]);
         }
     }
-    // (mean, 1 / sqrt(biased variance + 1e-6)), the variance from the differences to the mean
-    __device__ __forceinline__ float2 stats(int d, int lane) const {
+    // (mean, what it lacks, 1 / sqrt(biased variance + 1e-6)), the variance from the differences to the mean. fp32: the
+    // mean of those differences is what the rounded mean lacks, without which a mean of many deviations would be off by as
+    // many 2^-24 of them; bf16 tokens have no such means (0).
+    __device__ __forceinline__ float3 stats(int d, int lane) const {
         float s = 0.f;
 #pragma unroll
         for (int p = 0; p < FEW_PIECES; ++p)
@@ -72,16 +74,27 @@ struct FewRow {
 #pragma unroll
         for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
         const float mean = s / (float)d;
-        float q = 0.f;
+        float rest = 0.f, q = 0.f;
+        if (V == FEWV_F32) {
+#pragma unroll
+            for (int p = 0; p < FEW_PIECES; ++p)
+                if ((p * 32 + lane) * PER < d) {
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) rest += v[p][i] - mean;
+                }
+#pragma unroll
+            for (int o = 16; o; o >>= 1) rest += __shfl_xor_sync(0xFFFFFFFFu, rest, o);
+            rest /= (float)d;
+        }
 #pragma unroll
         for (int p = 0; p < FEW_PIECES; ++p)
             if ((p * 32 + lane) * PER < d) {
 #pragma unroll
-                for (int i = 0; i < PER; ++i) q = fmaf(v[p][i] - mean, v[p][i] - mean, q);
+                for (int i = 0; i < PER; ++i) q = fmaf(v[p][i] - mean - rest, v[p][i] - mean - rest, q);
             }
 #pragma unroll
         for (int o = 16; o; o >>= 1) q += __shfl_xor_sync(0xFFFFFFFFu, q, o);
-        return make_float2(mean, 1.f / sqrtf(q / (float)d + 1e-6f));
+        return make_float3(mean, rest, 1.f / sqrtf(q / (float)d + 1e-6f));
     }
 };
 
@@ -106,7 +119,7 @@ __device__ __forceinline__ void few_route(const FewArgs& a, int block, float (*s
     for (int i = 0; i < TOK; ++i) x[i].load(a.x, min(TOK * block + i, a.T - 1), a.d, lane);
 #pragma unroll
     for (int i = 0; i < TOK; ++i) {
-        float2 st = make_float2(0.f, 1.f);
+        float3 st = make_float3(0.f, 0.f, 1.f);
         if (a.ln) st = x[i].stats(a.d, lane);
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
@@ -115,7 +128,7 @@ __device__ __forceinline__ void few_route(const FewArgs& a, int block, float (*s
 #pragma unroll
             for (int p = 0; p < FEW_PIECES; ++p)
 #pragma unroll
-                for (int c = 0; c < FewRow<V>::PER; ++c) s = fmaf((x[i].v[p][c] - st.x) * st.y, w[q].v[p][c], s);
+                for (int c = 0; c < FewRow<V>::PER; ++c) s = fmaf((x[i].v[p][c] - st.x - st.y) * st.z, w[q].v[p][c], s);
 #pragma unroll
             for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
             if (lane == 0) s_logit[i][warp + 8 * q] = s + few_get<V>(a.bg, warp + 8 * q);
@@ -147,10 +160,24 @@ __device__ __forceinline__ void few_scales(uint8_t* dst, const uint8_t* s, int r
     for (int i = threadIdx.x; i < (K + 127) / 128; i += blockDim.x) dst[i] = __ldg(s + i);
 }
 
+// The LayerNorm's statistics of tokens t0 .. t0 + rows - 1, a warp a token.
+template <int V>
+__device__ __forceinline__ void few_stats(const FewArgs& a, float3* s_stats, int t0, int rows, int warp, int lane) {
+    for (int r = warp; r < rows; r += FEW_WARPS) {
+        FewRow<V> x;
+        x.load(a.x, t0 + r, a.d, lane);
+        const float3 st = x.stats(a.d, lane);
+        if (lane == 0) s_stats[r] = st;
+    }
+}
+
+// LN, 8-bit and bf16 weights: W LN(y) = rstd (W y - mean W 1), y as it is in bf16 and W 1 of the same products. fp32: W LN(y)
+// with each y normalised as it is split, because W y and mean W 1, with the TF32 products' error, would cancel (5 tokens,
+// d = 64, means 3,000 times the deviation: 4e-5 of the output's norm; 24 tokens, d = 384, 13.7 us so, 14.2 normalised).
 template <int V, int NT, int CTAS, bool LN>
 __global__ void __launch_bounds__(FEW_THREADS, CTAS) few_fc1_kernel(const __grid_constant__ FewArgs a) {
     extern __shared__ float red[];  // the partial sums; then the scale bytes
-    __shared__ float2 s_stats[few_chunk(NT)];
+    __shared__ float3 s_stats[few_chunk(NT)];
     __shared__ float s_logit[2][16];
     __shared__ float s_rows[FEW_WARPS][16];  // LN: the warps' row sums of W
     uint8_t* s_scale = reinterpret_cast<uint8_t*>(red) + FewT<V, NT, CTAS>::SMEM;
@@ -178,32 +205,33 @@ __global__ void __launch_bounds__(FEW_THREADS, CTAS) few_fc1_kernel(const __grid
         for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
     }
     t.start_x();
+    if (LN && V == FEWV_F32) {  // the statistics first, while the weights come
+        few_stats<V>(a, s_stats, t0, rows, warp, lane);
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < NT; ++j) t.norm[j] = s_stats[min(8 * j + (lane >> 2), rows - 1)];
+    }
     if (V == FEWV_W8A16) __syncthreads();
     few_product<V, NT, CTAS, LN>(acc, sums, t, s_scale, nullptr, 0, rows);
     few_stage<NT>(red, acc, warp, lane);
-    if (LN) {
+    if (LN && V != FEWV_F32) {
         if ((lane & 3) == 0) {  // column 0 of the ones
             s_rows[warp][lane >> 2] = sums[0];
             s_rows[warp][(lane >> 2) + 8] = sums[2];
         }
-        for (int r = warp; r < rows; r += FEW_WARPS) {
-            FewRow<V> x;
-            x.load(a.x, t0 + r, a.d, lane);
-            const float2 st = x.stats(a.d, lane);
-            if (lane == 0) s_stats[r] = st;
-        }
+        few_stats<V>(a, s_stats, t0, rows, warp, lane);
     }
     __syncthreads();
     for (int i = threadIdx.x; i < rows * 16; i += FEW_THREADS) {
         const int m = i >> 4, r = i & 15;
         if (r0 + r >= a.H) continue;
         float s = few_sum<8 * NT>(red, m, r);
-        if (LN) {  // W LN(y) = rstd (W y - mean W 1)
+        if (LN && V != FEWV_F32) {
             float c = 0.f;
 #pragma unroll
             for (int q = 0; q < FEW_WARPS; ++q) c += s_rows[q][r];
-            const float2 st = s_stats[m];
-            s = st.y * (s - st.x * c);
+            const float3 st = s_stats[m];
+            s = st.z * (s - st.x * c);
         }
         const float z = gelu_erf(s + few_get<V>(a.b1, r0 + r));
         few_put<V>(a.z, (int64_t)(t0 + m) * a.H + r0 + r, z);

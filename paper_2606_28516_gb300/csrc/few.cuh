@@ -92,6 +92,7 @@ struct FewTile {
     const char* tok[NT];
     int steps, in;  // the warp's steps, and how many of them lie inside K for this lane (K is a multiple of LANE)
     uint4 a[F::DW], b[F::DW], x[F::DX][NT][F::XV];
+    float3 norm[NT];  // fp32 with the LayerNorm: of the lane's activation rows, as FewRow::stats gives them
     __device__ __forceinline__ int column() const {
         return ((int)threadIdx.x >> 5) * F::STEP + (threadIdx.x & 3) * F::LANE;
     }
@@ -135,7 +136,8 @@ struct FewTile {
 
 // acc[j] += the warp's share of the tile (weights and activations started) times its activation rows. sw (8-bit weights): the scale bytes of the
 // tile's rows; sx (FEWV_W8A8): those of the activation rows, ldx bytes apart, rows past the last as the last; both in
-// shared memory (255 among them: the sums of its row or column mean nothing). sums (LN): += W 1.
+// shared memory (255 among them: the sums of its row or column mean nothing). LN: sums += W 1, or (fp32)
+// the activation rows are normalised on the way.
 // A step's products are added from zero and then to acc in fp32, so that the tensor cores' truncating accumulation
 // runs over one step (fp32) or one scale block's part (8 bits) only; bf16 outputs, whose own rounding is 2^-9,
 // accumulate in place.
@@ -164,7 +166,11 @@ __device__ __forceinline__ void few_product(float (&acc)[NT][4], float (&sums)[4
                     const uint32_t xv[4] = {v.x, v.y, v.z, v.w};
                     uint32_t xh[4], xl[4];
 #pragma unroll
-                    for (int h = 0; h < 4; ++h) few_split(xv[h], xh[h], xl[h]);
+                    for (int h = 0; h < 4; ++h) {
+                        // past K a lane's zeros become numbers, against weights that are zero
+                        const uint32_t y = LN ? __float_as_uint((__uint_as_float(xv[h]) - t.norm[j].x - t.norm[j].y) * t.norm[j].z) : xv[h];
+                        few_split(y, xh[h], xl[h]);
+                    }
                     float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int h = 0; h < 4; h += 2) {  // the small products first
@@ -175,16 +181,6 @@ __device__ __forceinline__ void few_product(float (&acc)[NT][4], float (&sums)[4
                     for (int h = 0; h < 4; h += 2) mma_tf32(part, ah[h], bh[h], ah[h + 1], bh[h + 1], xh[h], xh[h + 1]);
 #pragma unroll
                     for (int c = 0; c < 4; ++c) acc[j][c] += part[c];
-                }
-                if (LN) {
-                    const uint32_t one = __float_as_uint(1.f);
-                    float part[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int h = 0; h < 4; h += 2) mma_tf32(part, al[h], bl[h], al[h + 1], bl[h + 1], one, one);
-#pragma unroll
-                    for (int h = 0; h < 4; h += 2) mma_tf32(part, ah[h], bh[h], ah[h + 1], bh[h + 1], one, one);
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) sums[c] += part[c];
                 }
             } else if constexpr (V == FEWV_W8A8) {
                 // both operands widened to fp16, exactly (the warp-level e4m3 MMA is no faster)
