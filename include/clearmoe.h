@@ -409,7 +409,7 @@ int clearmoe_fp8_grouped_gemm(const clearmoe_fp8* A, const clearmoe_fp8* W, int3
                               const int32_t* perm, const clearmoe_fp8_epilogue* epi, void* out, int32_t out_dtype,
                               int64_t ldo, void* stream);
 
-/* For tests: every later product of 8-bit blocks in the process takes the tcgen05 kernel of this tile width, on pairs of
+/* For tests: every later product of 8-bit blocks that the calling thread asks for takes the tcgen05 kernel of this tile width, on pairs of
  * SMs (pair 1: 256, 192, 128) or single ones (pair 0: 192, 128, 64, 32), or the kernel for few rows (16, 0), where the
  * rows and the output allow it (8-bit outputs: a multiple of 128); (0, 0) restores the choice by size. EINVAL for another kernel. */
 int clearmoe_debug_fp8_kernel(int32_t width, int32_t pair);

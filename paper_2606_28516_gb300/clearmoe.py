@@ -605,7 +605,7 @@ def clearmoe_fp8_grouped_gemm(A: Fp8Matrix, W, offsets, out, perm=None, bias=Non
 
 
 def clearmoe_debug_fp8_kernel(width: int = 0, pair: int = 0) -> None:
-    """For tests: fixes the kernel of every later product of 8-bit blocks; no arguments: by size again."""
+    """For tests: fixes the kernel of the calling thread's later products of 8-bit blocks; no arguments: by size again."""
     _check(lib().clearmoe_debug_fp8_kernel(width, pair), "clearmoe_debug_fp8_kernel")
 
 

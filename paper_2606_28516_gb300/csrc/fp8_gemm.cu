@@ -22,7 +22,6 @@
 // finish, frees its tensor memory and returns.
 #include <cstdint>
 #include <cstring>
-#include <atomic>
 
 #include "common.cuh"
 #include "fp8.cuh"
@@ -399,9 +398,9 @@ cudaError_t launch_fp8_gemm(const Fp8GemmArgs& a, const Fp8Pick& k, int num_sms,
     }
 }
 
-// The kernel that tests have fixed (width << 1 | pair), or 0; FP8_FORCE_FEW: the one for few rows.
+// The kernel that tests have fixed for their thread's calls (width << 1 | pair), or 0; FP8_FORCE_FEW: the one for few rows.
 constexpr int FP8_FORCE_FEW = 16 << 1;
-static std::atomic<int> g_forced{0};
+static thread_local int g_forced = 0;
 
 int run_fp8_gemm(Fp8GemmArgs& g, const clearmoe_fp8* A, const clearmoe_fp8* W, int E, int num_sms, cudaStream_t s) {
     g.M = A->rows;
@@ -410,7 +409,7 @@ int run_fp8_gemm(Fp8GemmArgs& g, const clearmoe_fp8* A, const clearmoe_fp8* W, i
     g.E = E;
     g.lds = fp8_lds(A->cols);
     g.sa = A->scale;
-    const int forced = g_forced.load(std::memory_order_relaxed);
+    const int forced = g_forced;
     // Few rows, while the SMs take all CTAs of 16 columns at once: us against the best tcgen05 tile, 1 x 4,096 x 4,096 5.1 / 7.5,
     // 12 x 4,096 x 4,096 7.1 / 7.6, 12 x 768 x 3,072 4.6 / 6.1; more CTAs than that: 12 x 8,192 x 1,024 5.7 / 4.0, 8 x 8,192 x
     // 8,192 19.5 / 14.8.

@@ -57,3 +57,39 @@ def test_by_the_quantiser():
     out = torch.full((5, 64), float("nan"), device="cuda")
     cm.clearmoe_fp8_gemm(A, W, out)
     assert not out[:, ::2].any() and bool((out[:, 1::2] == float("inf")).all())
+
+
+def test_a_fixed_kernel_is_its_threads_alone():
+    """The kernel for few rows sums in another order than the tiled ones, which a width past its own choice gets: its bits
+    appear in the thread that fixed it, and in no other."""
+    import threading
+    g = torch.Generator(device="cuda").manual_seed(4)
+    A, W = cm.fp8_rows(5, 4096), cm.fp8_weight(12000, 4096)
+    cm.clearmoe_fp8_quantize_rows(torch.randn(5, 4096, generator=g, device="cuda"), A)
+    cm.clearmoe_fp8_quantize_weight(torch.randn(12000, 4096, generator=g, device="cuda"), W)
+
+    def product():
+        out = torch.empty(5, 12000, device="cuda")
+        cm.clearmoe_fp8_gemm(A, W, out)
+        torch.cuda.synchronize()
+        return out
+
+    by_size, fixed, ready, done = product(), [], threading.Event(), threading.Event()
+
+    def other():
+        cm.clearmoe_debug_fp8_kernel(16, 0)
+        fixed.append(product())
+        ready.set()
+        done.wait(60)
+        cm.clearmoe_debug_fp8_kernel()
+
+    t = threading.Thread(target=other)
+    t.start()
+    try:
+        assert ready.wait(60)
+        here = product()
+    finally:
+        done.set()
+        t.join()
+    assert not torch.equal(fixed[0], by_size)
+    assert torch.equal(here, by_size)
