@@ -375,8 +375,10 @@ cudaError_t few_experts(const FewArgs& a, cudaStream_t s) {
     const dim3 grid((a.d + 15) / 16, a.G);
     const int smem = FewT<V, NT, CTAS>::SMEM + (V == FEWV_W8A16 ? (a.H + 127) / 128 : 0);
     constexpr int threads = FewT<V, NT, CTAS>::THREADS;
-    return a.T >= a.G ? few_launch(few_expert_kernel<V, NT, CTAS, true>, grid, threads, smem, s, a)
-                      : few_launch(few_expert_kernel<V, NT, CTAS, false>, grid, threads, smem, s, a);
+    static_assert(CM_MAX_E <= 16);
+    if constexpr (NT < 4)  // four tiles: more than 16 tokens, as many as groups or more
+        if (a.T < a.G) return few_launch(few_expert_kernel<V, NT, CTAS, false>, grid, threads, smem, s, a);
+    return few_launch(few_expert_kernel<V, NT, CTAS, true>, grid, threads, smem, s, a);
 }
 
 template <int V>
@@ -388,7 +390,8 @@ cudaError_t few_type(const FewArgs& a, cudaStream_t s) {
     // us, lone CTAs of 16 warps against two or three of 8 an SM: 8 tokens, d = 384, 4 experts, bf16 4.6 / 5.0; 24, d = 384, 6, fp32
     // 9.6 / 10.7; 16, d = 768, 3, bf16 9.6 / 17.1; more CTAs than SMs: 13, d = 768, 9, bf16 18.9 / 14.6; 64, 8 19.8 / 18.4
     if (lone) return a.T <= 16 ? few_experts<V, 2, 1>(a, s) : few_experts<V, 4, 1>(a, s);
-    if (few_parts(V, 2) == 1 && a.T <= 8) return few_experts<V, 1, 3>(a, s);
+    if constexpr (few_parts(V, 2) == 1)
+        if (a.T <= 8) return few_experts<V, 1, 3>(a, s);
     return a.T <= 16 ? few_experts<V, 2, 3>(a, s) : few_experts<V, 4, 2>(a, s);
 }
 
