@@ -23,7 +23,9 @@
  *     and read the weights (every tensor argument except x), while the kernel enqueued just before it
  *     on the same stream is finishing; x is read only after that kernel has completed. So weights
  *     must not be written by the kernel immediately before the call (any later-enqueued work in
- *     between, or a synchronisation, is enough). clearmoe_route_noalloc reads nothing early.
+ *     between, or a synchronisation, is enough; of a kernel of the caller's own that work must not
+ *     let its successor start before it has waited for its predecessor). clearmoe_route_noalloc reads
+ *     nothing early, nor do the calls on 8-bit blocks that take no handle.
  *   - Arguments are validated on the host first; on a validation error (EINVAL, EUNSUPPORTED)
  *     nothing is enqueued and the outputs are untouched. CLEARMOE_ECUDA can also come from a
  *     launch after earlier kernels of the same call were enqueued; the outputs are then
@@ -105,7 +107,9 @@ typedef struct {
 typedef struct clearmoe_layer clearmoe_layer;
 
 /* Allocates the handle and its device workspace on the current device (hidden states
- * [max_tokens x hidden], basis coefficients [max_tokens x max_r], routing arrays, status word,
+ * [max_tokens x hidden], in bf16 layers no less than the tokens and hidden states in 8-bit blocks,
+ * max_tokens (ceil128(d) + ceil128(hidden)) bytes and their scales, nor than 4 hidden bytes for each
+ * of up to CLEARMOE_FEW_MAX tokens; basis coefficients [max_tokens x max_r], routing arrays, status word,
  * and for the folded LayerNorm 8 bytes per token of statistics, fp32 row sums [2 hidden + 16] and,
  * in bf16 layers, 128 bytes per token and per hidden unit of fc1's augmentation block).
  * Returns EINVAL for a null/invalid desc, EUNSUPPORTED per the tiling limits above, ENOMEM or
@@ -345,7 +349,8 @@ int clearmoe_route_noalloc(const void* x, int64_t T, int32_t d, int32_t dtype,
  *
  * A matrix [rows x cols] in e4m3 with power-of-two scales: value = e4m3(q) 2^(s - 127).
  *   q      one byte per element, row-major, rows of cols rounded up to a multiple of 128 bytes; the bytes past
- *          cols are zero (the quantising calls write them). 32-byte aligned.
+ *          cols are zero (the quantising calls write them; in a block that is NaN they may be anything). 32-byte
+ *          aligned.
  *   scale  one byte s per block, row-major, rows of 4 ceil(cols / 512) bytes, of which the first
  *          ceil(cols / 128) are used. 4-byte aligned. Blocks are 128 columns wide; those of activations one
  *          row high (rows scale rows), those of weights 128 rows (ceil(rows / 128) scale rows).
@@ -391,7 +396,7 @@ typedef struct {
 } clearmoe_fp8_epilogue;
 
 /* out = act(A W^T + bias): A [M x K] activations, W [N x K] weights (A->cols == W->cols), products of e4m3 values
- * and the scales exact, sums in fp32, the result rounded once to out_dtype (F32 or BF16) and stored at
+ * and the scales exact, sums in fp32 (the tensor cores cut where fp32 additions would round), the result rounded once to out_dtype (F32 or BF16) and stored at
  * out [M x N], rows ldo elements apart (ldo >= N, any alignment of the element type). epi may be NULL (no bias, no
  * activation). N <= 2^24. No handle and no workspace; stream-ordered; out must not alias an input. */
 int clearmoe_fp8_gemm(const clearmoe_fp8* A, const clearmoe_fp8* W, const clearmoe_fp8_epilogue* epi, void* out,
@@ -409,9 +414,10 @@ int clearmoe_fp8_grouped_gemm(const clearmoe_fp8* A, const clearmoe_fp8* W, int3
                               const int32_t* perm, const clearmoe_fp8_epilogue* epi, void* out, int32_t out_dtype,
                               int64_t ldo, void* stream);
 
-/* For tests: every later product of 8-bit blocks that the calling thread asks for takes the tcgen05 kernel of this tile width, on pairs of
- * SMs (pair 1: 256, 192, 128) or single ones (pair 0: 192, 128, 64, 32), or the kernel for few rows (16, 0), where the
- * rows and the output allow it (8-bit outputs: a multiple of 128); (0, 0) restores the choice by size. EINVAL for another kernel. */
+/* For tests: every later product of 8-bit blocks that the calling thread asks for takes the tcgen05 kernel of this
+ * tile width, on pairs of SMs (pair 1: 256, 192, 128) or single ones (pair 0: 192, 128, 64, 32), or the kernel for few
+ * rows (16, 0), where the rows and the output allow it (8-bit outputs: a multiple of 128); (0, 0) restores the choice
+ * by size. EINVAL for another kernel. */
 int clearmoe_debug_fp8_kernel(int32_t width, int32_t pair);
 
 /* The weights of a folded layer (clearmoe_fold_basis), bound once and passed to each of the two forwards below.
@@ -435,13 +441,14 @@ typedef struct {
 
 /* The whole folded layer for a few tokens, 1 <= T <= CLEARMOE_FEW_MAX: y_t = W_comb[a_t] GELU(W1 x_t + b1)
  * (+ b2), a_t as clearmoe_route's, in two launches: one takes every token through the router and fc1, the other
- * through its expert; only experts that have a token are read. Weights of the layer's dtype or 8-bit blocks
- * (bf16 layers; the weights' values times unquantised activations). Sums in fp32; z is stored in the layer's dtype
- * as in the other forwards, of up to 16 tokens of bf16 layers in two bf16 parts (16 bits of significand); fp32 layers
- * use three TF32 products per term (relative error near 2^-21; NaN for an infinity and for a magnitude past TF32's largest
- * value, 3.4e38, whose remainder is not finite). The
- * routing can be read with clearmoe_get_routing. Errors as clearmoe_ffn_forward_folded_ex; EUNSUPPORTED for more
- * tokens, and for 8-bit weights with hidden > 589,824. */
+ * through its expert. Of an expert without a token at most the first columns and the scales are read, asked for
+ * before the routing is known, so every matrix has to be readable. The linear router only. Weights of the layer's
+ * dtype or 8-bit blocks (bf16 layers; the weights' values times unquantised activations). Sums in fp32; z is stored in
+ * the layer's dtype as in the other forwards, of up to 16 tokens of bf16 layers in two bf16 parts (16 bits of
+ * significand); fp32 layers use three TF32 products per term (relative error near 2^-21; NaN for an infinity and for a
+ * magnitude past TF32's largest value, 3.4e38, whose remainder is not finite). The routing can be read with
+ * clearmoe_get_routing. Errors as clearmoe_ffn_forward_folded_ex; EUNSUPPORTED for more tokens, and for 8-bit weights
+ * with hidden > 589,824. */
 #define CLEARMOE_FEW_MAX 64
 int clearmoe_ffn_forward_few(clearmoe_layer* layer, const void* x, int64_t T, const clearmoe_ffn_weights* w, void* out,
                              void* stream);

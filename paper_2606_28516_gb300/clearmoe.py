@@ -670,7 +670,7 @@ def _tokens(x, out, w):
 
 
 def clearmoe_ffn_forward_few(layer: int, x, w: FfnWeights, out, stream=None) -> None:
-    """The whole folded layer for 1 to FEW_MAX tokens."""
+    """The whole folded layer for 1 to FEW_MAX tokens: x and out [T x d] in the layer's dtype."""
     calls = _calls or _bind_calls()
     code = calls.ffn_few_t(layer, w.addr, x, out, stream)
     if code is None:
@@ -681,7 +681,7 @@ def clearmoe_ffn_forward_few(layer: int, x, w: FfnWeights, out, stream=None) -> 
 
 
 def clearmoe_ffn_forward_fp8(layer: int, x, w: FfnWeights, out, stream=None) -> None:
-    """The whole folded layer with both products in 8-bit blocks."""
+    """The whole folded layer with both products in 8-bit blocks: x and out [T x d] bf16."""
     calls = _calls or _bind_calls()
     code = calls.ffn_fp8_t(layer, w.addr, x, out, stream)
     if code is None:

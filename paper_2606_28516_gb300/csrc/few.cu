@@ -2,7 +2,7 @@
 //
 //   fc1 kernel      one CTA per 16 rows of W1 for every token, and one CTA per token for its routing;
 //   expert kernel   one CTA per 16 output rows and group (expert, or the class tokens' dense path), for the
-//                   tokens of that group; a group without tokens is not read.
+//                   tokens of that group; of a group without tokens at most the first steps are.
 //
 // What bounds them is reading the weights once, W1 and the matrices of the experts that are taken, at these
 // sizes mostly the time until the first bytes come: so the first loads of weights are issued before the wait for
@@ -16,8 +16,8 @@
 // 16 tokens of bf16 layers as two bf16 matrices, z rounded and the remainder rounded (16 bits of significand): rounded to
 // bf16 alone it adds as much to the output's error as the output's own rounding (0.0024 instead of 0.0017 of its norm).
 // The parts are neighbouring columns of the expert's product, which has columns to spare there, and their sums are added
-// in fp32. (Beyond, they would double the columns and the reads of z: 64 tokens, d = 768, 18.3 us without, 21.0 with; 13
-// tokens 14.4 and 14.6.)
+// in fp32. (Beyond, they would double the columns and the reads of z: 64 tokens, d = 768, 18.2 us without, 21.1 with, on one
+// expert, d = 1,024, 19.1 and 27.0; 13 tokens 14.4 and 14.6.)
 #include <cstdint>
 #include <type_traits>
 
@@ -106,7 +106,7 @@ __device__ __forceinline__ int64_t few_pitch(int K) {  // bytes
 // The routing of tokens TOK block .. TOK block + TOK - 1 by one CTA: a warp per expert (two above 8), its row of W_g in registers
 // before the tokens may be read; the logits in fp32, lowest index on ties. (Eight tokens a CTA, one after the other,
 // took longer than fc1: 9.3 us instead of 7.1 for 64 tokens, d = 192. With up to 16 tokens one a CTA: one token, 3.9 us
-// against 4.5 with two.)
+// against 4.5 with two; now 3.7.)
 template <int V, int TOK>
 __device__ __forceinline__ void few_route(const FewArgs& a, int block, float (*s_logit)[16], int warp, int lane) {
     FewRow<V> w[2], x[TOK];
@@ -387,8 +387,8 @@ cudaError_t few_type(const FewArgs& a, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     if (a.T <= 4) return few_experts<V, 1, 2>(a, s);
     const bool lone = (int64_t)((a.d + 15) / 16) * (a.T < a.G ? a.T : a.G) <= a.num_sms;  // an SM for each CTA with work
-    // us, lone CTAs of 16 warps against two or three of 8 an SM: 8 tokens, d = 384, 4 experts, bf16 4.6 / 5.0; 24, d = 384, 6, fp32
-    // 9.6 / 10.7; 16, d = 768, 3, bf16 9.6 / 17.1; more CTAs than SMs: 13, d = 768, 9, bf16 18.9 / 14.6; 64, 8 19.8 / 18.4
+    // us, lone CTAs of 16 warps against two or three of 8 an SM: 8 tokens, d = 384, 4 experts, bf16 4.5 / 4.9; 24, d = 384, 6, fp32
+    // 9.3 / 10.2; 16, d = 768, 3, bf16 7.0 / 10.1; more CTAs than SMs: 13, d = 768, 9, bf16 16.5 / 12.8; 64, 8 19.8 / 18.4
     if (lone) return a.T <= 16 ? few_experts<V, 2, 1>(a, s) : few_experts<V, 4, 1>(a, s);
     if constexpr (few_parts(V, 2) == 1)
         if (a.T <= 8) return few_experts<V, 1, 3>(a, s);

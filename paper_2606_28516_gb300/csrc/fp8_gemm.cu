@@ -342,9 +342,11 @@ cudaError_t launch_kind(const Fp8GemmArgs& a, int num_sms, cudaStream_t s) {
 // k-blocks or, where that is longer, runs the epilogue of the tile before it, then the last epilogue. A k-block's cycles
 // grow from what the MMAs take (2 a column, 285 at the least) to what the path from L2 allows with every SM at work.
 // Fitted to measurements (us, the best two of seven kernels and this rule's choice, at M x N x K): 197 x 3,072 x 768
-// 3.9 (64 wide, one SM) and 4.5 (128), 3.9; 1,000 x 384 x 1,536 4.6 (32) and 4.8 (64), 4.6; 4,000 x 1,024 x 1,024 7.1
-// (128) and 8.4 (128, pair), 7.1; 9,973 x 384 x 1,536 9.0 (128) and 9.8 (128, pair), 9.0; 25,216 x 768 x 3,072 38.9
-// (256, pair) and 44.7 (192, pair), 38.9; 16,384 x 4,096 x 4,096 144 (256, pair) and 158 (192, pair), 144.
+// 3.9 (64 wide, one SM) and 4.5 (128), 3.9; 1,000 x 384 x 1,536 4.8 (32) and 4.8 (64), 4.7; 4,000 x 1,024 x 1,024 7.2
+// (128) and 8.3 (128, pair), 7.1; 9,973 x 384 x 1,536 9.2 (128) and 9.9 (128, pair), 9.1; 25,216 x 768 x 3,072 38.1
+// (256, pair) and 44.5 (192, pair), 38.2; 16,384 x 4,096 x 4,096 144 (256, pair) and 158 (192, pair), 143, all in runs
+// of a few milliseconds (at the power limit, after some more of them, 155 to 166). The quantising epilogue's cost is that
+// with bias and GELU; without them 50,432 x 3,072 x 768 takes 100 us in the 128-wide tiles that it chooses, 79 in 256.
 struct Fp8Kernel {
     Fp8Pick pick;
     int block;     // cycles of a k-block with every SM at work
@@ -352,8 +354,8 @@ struct Fp8Kernel {
     int quantize;     // 8-bit outputs (0: none)
 };
 // How outputs are stored: bf16 or fp32 rows in whole 32-byte pieces, or of any pitch. Cycles measured at 2,922 x 3,456 (3,453)
-// x 60, where the stores are all there is; us of the best kernel and of the one that a single figure had chosen: bf16 7.5 / 10.6,
-// fp32 11.6 / 14.7, any pitch 13.8 / 18.3 and 14.6 / 18.3.
+// x 60, where the stores are all there is; us of the best kernel and of the one that a single figure had chosen: bf16 7.4 / 10.5,
+// fp32 11.4 / 14.7, any pitch 13.8 / 18.5 and 14.6 / 18.3.
 enum Fp8Store { FP8_STORE_BF16 = 0, FP8_STORE_F32 = 1, FP8_STORE_ODD = 2 };  // ODD: added to the type's
 static double fp8_cost(const Fp8Kernel& k, int64_t M, int N, int nkb, int out_kind, bool wide, int groups, int num_sms) {
     const bool pair = k.pick.pair, q = out_kind == FP8_OUT_FP8;
@@ -410,9 +412,9 @@ int run_fp8_gemm(Fp8GemmArgs& g, const clearmoe_fp8* A, const clearmoe_fp8* W, i
     g.lds = fp8_lds(A->cols);
     g.sa = A->scale;
     const int forced = g_forced;
-    // Few rows, while the SMs take all CTAs of 16 columns at once: us against the best tcgen05 tile, 1 x 4,096 x 4,096 5.1 / 7.5,
-    // 12 x 4,096 x 4,096 7.1 / 7.6, 12 x 768 x 3,072 4.6 / 6.1; more CTAs than that: 12 x 8,192 x 1,024 5.7 / 4.0, 8 x 8,192 x
-    // 8,192 19.5 / 14.8.
+    // Few rows, while the SMs take all CTAs of 16 columns at once: us against the best tcgen05 tile, 1 x 4,096 x 4,096 4.6 / 7.4,
+    // 12 x 4,096 x 4,096 6.3 / 7.5, 12 x 768 x 3,072 3.6 / 5.9; more CTAs than that: 12 x 8,192 x 1,024 5.2 / 4.1, 8 x 8,192 x
+    // 8,192 18.2 / 14.8.
     const bool few_fits = !g.offsets && g.out_kind != FP8_OUT_FP8 && g.M <= FP8_FEW_MAX && (g.M + 1) * g.nkb <= FP8_FEW_SCALES;
     if (few_fits && (forced == FP8_FORCE_FEW || (forced == 0 && (g.N + 15) / 16 <= 2 * num_sms))) {
         g.x = A->q;
@@ -430,7 +432,7 @@ int run_fp8_gemm(Fp8GemmArgs& g, const clearmoe_fp8* A, const clearmoe_fp8* W, i
     // rows of bytes as rows of half as many 16-bit elements: boxes of 64 of them are 128 bytes
     const int64_t cols16 = fp8_ldq(A->cols) / 2;
     // One SM, fewer rows than a tile: a box of those alone. The copy engine takes longer over a row past the end, which it
-    // fills with zeros, than over one that it reads (24 x 4,096 x 4,096, 64 wide: 10.9 us, 8.0 so); what the others' sums are
+    // fills with zeros, than over one that it reads (24 x 4,096 x 4,096, 64 wide: 10.9 us, 7.7 so); what the others' sums are
     // made of does not matter.
     g.box_rows = !k.pair && g.M < F8_BM ? (int)(g.M + 7) / 8 * 8 : F8_BM;
     if (encode_tmap_bf16(&g.tmA, A->q, A->rows, cols16, g.box_rows)) return CLEARMOE_ECUDA;

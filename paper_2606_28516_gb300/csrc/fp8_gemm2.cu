@@ -14,12 +14,13 @@
 // the accumulator traffic and bounded the kernel, 101 us against 93 for 19,456 x 1,792 x 4,096.
 //
 // Epilogue: 16 warps (four per lane quarter, so that each scheduler has four to hide the latencies of bias, GELU and
-// conversions), each 32 columns of a 128-column block at a time. For 8-bit outputs, whose arithmetic takes longer than the
-// MMAs (of 64 values a lane: some 10 cycles each on the FMA pipe alone), two groups of eight take every other tile, one
-// accumulator each, so that one group's waits pass under the other's arithmetic; a warp has 64 columns of a 128-column
-// scale block and exchanges its rows' largest magnitudes with the warp that has the others. 50,432 x 3,072 x 768 with bias
-// and GELU: 106 us (2,250 TFLOP/s); all 16 warps on every tile, pair after pair of values, 121; eight warps with 128
-// columns a lane and no exchange 106, and 113 in 128-wide tiles against 105. Without bias and GELU 80.
+// conversions), each 32 columns of a 128-column block at a time. For 8-bit outputs, whose epilogue takes longer than the
+// MMAs (a 128 x 256 tile 5,850 cycles, of which the MMAs need 3,072 and the packed arithmetic of bias, GELU and scaling some
+// 2,500; tensor pipe 45 % busy, issue 56 %: no unit is full, its steps wait for one another), two groups of eight take every
+// other tile, one accumulator each, so that one group's waits pass under the other's arithmetic; a warp has 64 columns of a
+// 128-column scale block and exchanges its rows' largest magnitudes with the warp that has the others. 50,432 x 3,072 x 768
+// with bias and GELU: 106 us (2,250 TFLOP/s); all 16 warps on every tile, pair after pair of values, 121; eight warps with 128
+// columns a lane and no exchange 106, and 113 in 128-wide tiles against 105. Without bias and GELU 79.
 // Hand-offs and giving up as in tc_gemm2.cu: TMA bytes of both CTAs on the even CTA's full barriers, commits on
 // both CTAs' empty, sempty and tfull barriers, the scale warp and epilogue warps of both on the even CTA's sfull,
 // ovl and tempty; every wait is bounded, and the even CTA lets copies in flight land before the cluster retires.
