@@ -460,6 +460,94 @@ int clearmoe_ffn_forward_few(clearmoe_layer* layer, const void* x, int64_t T, co
 int clearmoe_ffn_forward_fp8(clearmoe_layer* layer, const void* x, int64_t T, const clearmoe_ffn_weights* w, void* out,
                              void* stream);
 
+/* ---- 4-bit floating point with one scale per 32 columns of a row ----
+ *
+ * A matrix [rows x cols] in e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) with power-of-two scales, activations
+ * and weights alike: value = e2m1(q) 2^(s - 127).
+ *   q      two codes a byte, the column of even number in the low half, row-major, rows of 32 ceil(cols / 64) bytes; the
+ *          codes past cols are zero (the quantising calls write them; in a block that is NaN they may be anything). 32-byte
+ *          aligned.
+ *   scale  one byte s per block of 32 columns of one row, in tiles of 128 rows x 128 columns: ceil(rows / 128) rows of
+ *          ceil(cols / 128) tiles, 512 bytes each, in which the byte of row r and block b (r < 128, b < 4 within the tile)
+ *          is byte 16 (r % 32) + 4 (r / 32) + b, as the tensor cores take them. 32-byte aligned. Bytes of rows past the
+ *          last and of blocks at or past 2 ceil(cols / 64) are not used and may be anything.
+ * The quantising calls give each block the least s with max |value| <= 6 2^(s - 127) (6: e2m1's largest value; s = 0 at
+ * the least) and round value 2^(127 - s) to nearest even. A block with an infinity or a NaN gets s = 255, which stands
+ * for NaN: every value of the block, and every output that depends on it, is NaN.
+ * Both buffers are the caller's. rows <= 2^30, cols <= 2^24. */
+typedef struct {
+    void* q;
+    uint8_t* scale;
+    int64_t rows;
+    int64_t cols;
+} clearmoe_fp4;
+
+/* x [x_rows x out->cols] (dtype CLEARMOE_F32 or CLEARMOE_BF16, rows ld elements apart, ld >= cols, any alignment of the
+ * element type) to 4-bit blocks: activations before a product, weights once per set. gather (nullable, int32
+ * [out->rows], device): row i is x's row gather[i] instead; of an entry outside [0, x_rows) nothing is read, and the row
+ * is NaN (s = 255). x_rows >= 1, and at least out->rows without gather. No handle; stream-ordered; x may be the preceding
+ * kernel's output. */
+int clearmoe_fp4_quantize(const void* x, int64_t x_rows, int32_t dtype, int64_t ld, const int32_t* gather,
+                          const clearmoe_fp4* out, void* stream);
+
+/* The values that a matrix stands for, rounded once to dtype: out [rows x cols], rows ld elements apart. */
+int clearmoe_fp4_dequantize(const clearmoe_fp4* in, void* out, int32_t dtype, int64_t ld, void* stream);
+
+/* out = act(A W^T + bias): A [M x K], W [N x K] (A->cols == W->cols), products of e2m1 values and the scales exact, sums in
+ * fp32 (the tensor cores cut where fp32 additions would round), the result rounded once to out_dtype (F32 or BF16) and
+ * stored at out [M x N], rows ldo elements apart (ldo >= N, any alignment of the element type). epi may be NULL (no bias,
+ * no activation); its status as in the 8-bit products. N <= 2^24. No handle and no workspace; stream-ordered; out must
+ * not alias an input. */
+int clearmoe_fp4_gemm(const clearmoe_fp4* A, const clearmoe_fp4* W, const clearmoe_fp8_epilogue* epi, void* out,
+                      int32_t out_dtype, int64_t ldo, void* stream);
+
+/* The same with the fp32 result quantised as clearmoe_fp4_quantize would: out [M x N] in 4-bit blocks, the next product's
+ * activations, without its intermediate in memory. */
+int clearmoe_fp4_gemm_fp4(const clearmoe_fp4* A, const clearmoe_fp4* W, const clearmoe_fp8_epilogue* epi,
+                          const clearmoe_fp4* out, void* stream);
+
+/* Grouped by expert: rows [offsets[e], offsets[e + 1]) of A (offsets: int32 [E + 1], device, ascending from 0 to
+ * A->rows; an expert may have none) times W[e]^T (host array of E matrices of the same shape); row i goes to
+ * row perm[i] of out (perm: nullable int32 [M], device; a permutation). 1 <= E <= 16. */
+int clearmoe_fp4_grouped_gemm(const clearmoe_fp4* A, const clearmoe_fp4* W, int32_t E, const int32_t* offsets,
+                              const int32_t* perm, const clearmoe_fp8_epilogue* epi, void* out, int32_t out_dtype,
+                              int64_t ldo, void* stream);
+
+/* For tests: every later product of 4-bit blocks that the calling thread asks for takes the tcgen05 kernel of this tile
+ * width on single SMs (pair 0: 128, 64); (0, 0) restores the choice by size. EINVAL for another kernel. */
+int clearmoe_debug_fp4_kernel(int32_t width, int32_t pair);
+
+/* ---- a residual's addition and the root-mean-square norm of the sum ----
+ *
+ * s = x + residual, rounded to dtype, is the stream as it goes on; its norm y = s weight / sqrt(mean(s^2) + eps) feeds the
+ * next sublayer. Sums and statistics in fp32 (a mean square past fp32's range makes the row zero), y rounded once.
+ *  x, residual (nullable: s = x), sum (nullable: s is not stored) [rows x cols] of dtype (F32 or BF16), rows ldx, ldr and
+ *  lds elements apart; weight (nullable: ones) [cols] of weight_dtype; eps >= 0.
+ * Every tensor may start anywhere that its element type allows. sum may be x or residual (with the same rows), out
+ * neither of the three unless it is x or residual and sum is not. 1 <= rows <= 2^30, 1 <= cols <= CLEARMOE_NORM_MAX
+ * (EUNSUPPORTED above). No handle; stream-ordered; reads nothing before the preceding kernel has completed. */
+#define CLEARMOE_NORM_MAX 32768
+typedef struct {
+    const void* x;
+    const void* residual;
+    void* sum;
+    const void* weight;
+    int64_t ldx, ldr, lds;
+    int64_t rows, cols;
+    int32_t dtype;
+    int32_t weight_dtype;
+    float eps;
+} clearmoe_norm;
+
+/* y to out [rows x cols] of out_dtype, rows ldo elements apart. */
+int clearmoe_rms_norm(const clearmoe_norm* n, void* out, int32_t out_dtype, int64_t ldo, void* stream);
+
+/* y to 8-bit blocks of activations, as clearmoe_fp8_quantize_rows would make them of the fp32 y. */
+int clearmoe_rms_norm_fp8(const clearmoe_norm* n, const clearmoe_fp8* out, void* stream);
+
+/* y to 4-bit blocks, as clearmoe_fp4_quantize would make them of the fp32 y. */
+int clearmoe_rms_norm_fp4(const clearmoe_norm* n, const clearmoe_fp4* out, void* stream);
+
 /* Static string for a status code. */
 const char* clearmoe_strerror(int status);
 

@@ -49,6 +49,16 @@ class clearmoe_fp8(ctypes.Structure):
     _fields_ = [("q", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64)]
 
 
+class clearmoe_fp4(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64)]
+
+
+class clearmoe_norm(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("sum", ctypes.c_void_p), ("weight", ctypes.c_void_p),
+                ("ldx", ctypes.c_int64), ("ldr", ctypes.c_int64), ("lds", ctypes.c_int64), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64), ("dtype", ctypes.c_int32), ("weight_dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
 class clearmoe_fp8_epilogue(ctypes.Structure):
     _fields_ = [("bias", ctypes.c_void_p), ("bias_dtype", ctypes.c_int32), ("act", ctypes.c_int32),
                 ("status", ctypes.c_void_p)]
@@ -62,6 +72,7 @@ class clearmoe_ffn_weights(ctypes.Structure):
 
 ACT_NONE, ACT_RELU, ACT_GELU = -1, 0, 1
 FEW_MAX = 64
+NORM_MAX = 32768  # columns of clearmoe_rms_norm
 
 
 def mlp_router(W_in, b_in, W_out, b_out, act: str = "relu") -> clearmoe_mlp_router:
@@ -119,6 +130,18 @@ _SIGS = {
     "clearmoe_debug_fp8_kernel": [_I32, _I32],
     "clearmoe_ffn_forward_few": [_P, _P, _I64, ctypes.POINTER(clearmoe_ffn_weights), _P, _P],
     "clearmoe_ffn_forward_fp8": [_P, _P, _I64, ctypes.POINTER(clearmoe_ffn_weights), _P, _P],
+    "clearmoe_fp4_quantize": [_P, _I64, _I32, _I64, _P, ctypes.POINTER(clearmoe_fp4), _P],
+    "clearmoe_fp4_dequantize": [ctypes.POINTER(clearmoe_fp4), _P, _I32, _I64, _P],
+    "clearmoe_fp4_gemm": [ctypes.POINTER(clearmoe_fp4), ctypes.POINTER(clearmoe_fp4),
+                          ctypes.POINTER(clearmoe_fp8_epilogue), _P, _I32, _I64, _P],
+    "clearmoe_fp4_gemm_fp4": [ctypes.POINTER(clearmoe_fp4), ctypes.POINTER(clearmoe_fp4),
+                              ctypes.POINTER(clearmoe_fp8_epilogue), ctypes.POINTER(clearmoe_fp4), _P],
+    "clearmoe_fp4_grouped_gemm": [ctypes.POINTER(clearmoe_fp4), ctypes.POINTER(clearmoe_fp4), _I32, _P, _P,
+                                  ctypes.POINTER(clearmoe_fp8_epilogue), _P, _I32, _I64, _P],
+    "clearmoe_debug_fp4_kernel": [_I32, _I32],
+    "clearmoe_rms_norm": [ctypes.POINTER(clearmoe_norm), _P, _I32, _I64, _P],
+    "clearmoe_rms_norm_fp8": [ctypes.POINTER(clearmoe_norm), ctypes.POINTER(clearmoe_fp8), _P],
+    "clearmoe_rms_norm_fp4": [ctypes.POINTER(clearmoe_norm), ctypes.POINTER(clearmoe_fp4), _P],
     "clearmoe_strerror": [ctypes.c_int],
     "clearmoe_version": [],
 }
@@ -607,6 +630,129 @@ def clearmoe_fp8_grouped_gemm(A: Fp8Matrix, W, offsets, out, perm=None, bias=Non
 def clearmoe_debug_fp8_kernel(width: int = 0, pair: int = 0) -> None:
     """For tests: fixes the kernel of the calling thread's later products of 8-bit blocks; no arguments: by size again."""
     _check(lib().clearmoe_debug_fp8_kernel(width, pair), "clearmoe_debug_fp8_kernel")
+
+
+# ---------------------------------------------------------------- 4-bit blocks with power-of-two scales
+class Fp4Matrix:
+    """A matrix [rows x cols] in 4-bit blocks (clearmoe_fp4), activations or weights: q, two values a byte in rows of cols
+    rounded up to 64 values (uint8), and its scale bytes, [ceil(rows / 128) x ceil(cols / 128) x 512] (uint8). Keeps the
+    tensors alive."""
+
+    def __init__(self, q, scale, rows: int, cols: int):
+        for name, t, shape in (("q", q, (rows, fp4_pitch(cols))), ("scale", scale, (-(-rows // 128), -(-cols // 128), 512))):
+            if tuple(t.shape) != shape or t.element_size() != 1:
+                raise ValueError(f"{name} of a {rows} x {cols} matrix in 4-bit blocks is bytes of {shape}, got {tuple(t.shape)} "
+                                 f"{t.dtype}")
+        self.q, self.scale, self.rows, self.cols = q, scale, rows, cols
+        self.c = clearmoe_fp4(_ptr(q), _ptr(scale), rows, cols)
+        self.ref, self.addr = ctypes.pointer(self.c), ctypes.addressof(self.c)
+
+    @property
+    def weight(self):
+        """What the calls on 8-bit blocks ask of a matrix first: this one is refused there."""
+        raise ValueError("a matrix in 8-bit blocks (fp8_rows, fp8_weight) is needed, got one in 4-bit blocks")
+
+
+def fp4_pitch(cols: int) -> int:
+    """Bytes from one row of q to the next."""
+    return -(-cols // 64) * 32
+
+
+def fp4_matrix(rows: int, cols: int, device="cuda") -> Fp4Matrix:
+    """Buffers for a matrix in 4-bit blocks, to be written by clearmoe_fp4_quantize, a product or a norm."""
+    import torch
+    q = torch.empty(rows, fp4_pitch(cols), dtype=torch.uint8, device=device)
+    return Fp4Matrix(q, torch.empty(-(-rows // 128), -(-cols // 128), 512, dtype=torch.uint8, device=device), rows, cols)
+
+
+def _fp4(m, what):
+    """The address of a matrix in 4-bit blocks: what the library sees of it does not tell it from one in 8-bit blocks."""
+    if not isinstance(m, Fp4Matrix):
+        raise ValueError(f"{what} must be a matrix in 4-bit blocks (fp4_matrix), got {type(m).__name__}")
+    return m.ref
+
+
+def clearmoe_fp4_quantize(x, out: Fp4Matrix, gather=None, stream=None) -> None:
+    """x [rows x cols] (bf16 or fp32, any row pitch) to out in 4-bit blocks, weights and activations alike; gather: int32
+    source rows (one outside x gives a row of NaN)."""
+    o = _fp4(out, "out")
+    p, dt, ld = _matrix(x, out.rows if gather is None else None, out.cols, "x")
+    _check(lib().clearmoe_fp4_quantize(p, x.shape[0], dt, ld, _int32(gather, out.rows, "gather"), o, _stream(stream)),
+           "clearmoe_fp4_quantize")
+
+
+def clearmoe_fp4_dequantize(m: Fp4Matrix, out, stream=None) -> None:
+    """The values m stands for, rounded to out's dtype (bf16 or fp32)."""
+    r = _fp4(m, "m")
+    p, dt, ld = _matrix(out, m.rows, m.cols, "out")
+    _check(lib().clearmoe_fp4_dequantize(r, p, dt, ld, _stream(stream)), "clearmoe_fp4_dequantize")
+
+
+def clearmoe_fp4_gemm(A: Fp4Matrix, W: Fp4Matrix, out, bias=None, act: int = ACT_NONE, status=None, stream=None) -> None:
+    """out = act(A W^T + bias). out: a [M x N] bf16 or fp32 tensor of any row pitch, or an Fp4Matrix (the result
+    quantised, clearmoe_fp4_gemm_fp4)."""
+    a, w = _fp4(A, "A"), _fp4(W, "W")
+    epi = _epilogue(bias, act, status, W.rows)
+    if isinstance(out, Fp4Matrix):
+        _check(lib().clearmoe_fp4_gemm_fp4(a, w, epi, out.ref, _stream(stream)), "clearmoe_fp4_gemm_fp4")
+        return
+    p, dt, ld = _matrix(out, A.rows, W.rows, "out")
+    _check(lib().clearmoe_fp4_gemm(a, w, epi, p, dt, ld, _stream(stream)), "clearmoe_fp4_gemm")
+
+
+def clearmoe_fp4_grouped_gemm(A: Fp4Matrix, W, offsets, out, perm=None, bias=None, act: int = ACT_NONE, status=None,
+                              stream=None) -> None:
+    """Rows offsets[e] .. offsets[e + 1] of A times W[e]^T (W: a sequence of Fp4Matrix), row i to out[perm[i]]."""
+    a = _fp4(A, "A")
+    if not len(W) or offsets is None:
+        raise ValueError("a grouped product needs matrices and the offsets of their rows")
+    for m in W:
+        _fp4(m, "every W")
+    off, rows = _int32(offsets, len(W) + 1, "offsets"), _int32(perm, A.rows, "perm")
+    p, dt, ld = _matrix(out, A.rows, W[0].rows, "out")
+    arr = (clearmoe_fp4 * len(W))(*[m.c for m in W])
+    _check(lib().clearmoe_fp4_grouped_gemm(a, arr, len(W), off, rows, _epilogue(bias, act, status, W[0].rows), p, dt, ld,
+                                           _stream(stream)), "clearmoe_fp4_grouped_gemm")
+
+
+def clearmoe_debug_fp4_kernel(width: int = 0, pair: int = 0) -> None:
+    """For tests: fixes the kernel of the calling thread's later products of 4-bit blocks; no arguments: by size again."""
+    _check(lib().clearmoe_debug_fp4_kernel(width, pair), "clearmoe_debug_fp4_kernel")
+
+
+# ------------------------------------------------------------------- residual addition and RMS norm
+def clearmoe_rms_norm(x, out, residual=None, sum_out=None, weight=None, eps: float = 1e-6, stream=None) -> None:
+    """s = x + residual, rounded to x's dtype, to sum_out; s weight / sqrt(mean(s^2) + eps) to out: a [rows x cols] bf16
+    or fp32 tensor, or an Fp8Matrix of rows or an Fp4Matrix (the norm quantised, clearmoe_rms_norm_fp8, _fp4). x,
+    residual and sum_out are of one dtype, of any row pitch; sum_out may be x or residual."""
+    if len(x.shape) != 2:
+        raise ValueError(f"x must be a matrix, got {tuple(x.shape)}")
+    rows, cols = x.shape
+    n = clearmoe_norm(rows=rows, cols=cols, eps=eps)
+    n.x, n.dtype, n.ldx = _matrix(x, rows, cols, "x")
+    for name, t in (("residual", residual), ("sum_out", sum_out)):
+        if t is not None:
+            p, dt, ld = _matrix(t, rows, cols, name)
+            if dt != n.dtype:
+                raise ValueError(f"{name} must be of x's dtype, got {t.dtype} and {x.dtype}")
+            if name == "residual":
+                n.residual, n.ldr = p, ld
+            else:
+                n.sum, n.lds = p, ld
+    if weight is not None:
+        if weight.numel() != cols:
+            raise ValueError(f"weight must have {cols} elements, got {weight.numel()}")
+        n.weight, n.weight_dtype = _ptr(weight), _dtype(weight)
+    ref = ctypes.byref(n)
+    if isinstance(out, Fp4Matrix):
+        _check(lib().clearmoe_rms_norm_fp4(ref, out.ref, _stream(stream)), "clearmoe_rms_norm_fp4")
+    elif isinstance(out, Fp8Matrix):
+        if out.weight:
+            _refuse_kind("out", False)
+        _check(lib().clearmoe_rms_norm_fp8(ref, out.ref, _stream(stream)), "clearmoe_rms_norm_fp8")
+    else:
+        p, dt, ld = _matrix(out, rows, cols, "out")
+        _check(lib().clearmoe_rms_norm(ref, p, dt, ld, _stream(stream)), "clearmoe_rms_norm")
 
 
 # ------------------------------------------------------------- a folded layer's weights and its forwards

@@ -1,0 +1,82 @@
+// 4-bit blocks: value = e2m1(q) 2^(s - 127), one scale byte s per 32 columns of a row, in tiles of 128 rows x 128
+// columns. Device helpers shared by the quantiser, the GEMMs' epilogue, the few-row kernel and the norm, and the
+// launchers.
+#pragma once
+
+#include "common.cuh"
+#include "fp8.cuh"
+#include "internal.h"
+
+namespace cm {
+
+// Bytes from one row of q to the next: whole K steps of the MMAs (64 columns).
+__host__ __device__ __forceinline__ int64_t fp4_ldq(int64_t cols) { return (cols + 63) / 64 * 32; }
+// Tiles of scales side by side; a tile has 512 bytes.
+__host__ __device__ __forceinline__ int64_t fp4_tiles(int64_t cols) { return (cols + 127) / 128; }
+// The four scale bytes of row `row` in tile column `tile` (of `tiles`), from the start of the scales.
+__host__ __device__ __forceinline__ int64_t fp4_scale_word(int64_t row, int64_t tile, int64_t tiles) {
+    return ((row >> 7) * tiles + tile) * 512 + (row & 31) * 16 + (row >> 5 & 3) * 4;
+}
+
+// Scale byte of a block whose largest |value| has the fp32 bits `amax` (largest as an unsigned integer, so that
+// NaN > inf > every finite value): the least s with amax <= 6 2^(s - 127). 6 = 1.5 2^2, so s is amax's biased exponent
+// less 2, one more when its significand is above 1.5; held at 0 below, 255 (the scale format's NaN) for a block with an
+// infinity or a NaN. At most 253 otherwise; its inverse is fp8_inverse_scale's.
+__device__ __forceinline__ uint32_t fp4_scale_byte(uint32_t amax) {
+    if (amax >= 0x7F800000u) return 255u;
+    const int s = (int)(amax >> 23) - 2 + ((amax & 0x7FFFFFu) > 0x400000u ? 1 : 0);
+    return s < 0 ? 0u : (uint32_t)s;
+}
+// Eight values to e2m1, to nearest even, the first in the lowest four bits. (NaN has no code.)
+__device__ __forceinline__ uint32_t fp4_pack8(float a, float b, float c, float d, float e, float f, float g, float h) {
+    uint32_t v;
+    asm("{\n\t.reg .b8 p, q, r, s;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 p, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 q, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 r, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 s, %8, %7;\n\t"
+        "mov.b32 %0, {p, q, r, s};\n\t}"
+        : "=r"(v)
+        : "f"(a), "f"(b), "f"(c), "f"(d), "f"(e), "f"(f), "f"(g), "f"(h));
+    return v;
+}
+// Eight values times k (a power of two), to e2m1.
+__device__ __forceinline__ uint32_t fp4_pack8_scaled(const float* v, float2 k) {
+    const float2 a = __fmul2_rn(make_float2(v[0], v[1]), k), b = __fmul2_rn(make_float2(v[2], v[3]), k);
+    const float2 c = __fmul2_rn(make_float2(v[4], v[5]), k), d = __fmul2_rn(make_float2(v[6], v[7]), k);
+    return fp4_pack8(a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y);
+}
+// The value of a code (its low four bits).
+__device__ __forceinline__ float fp4_value(uint32_t c) {
+    const uint32_t m = c & 7u;  // 0, .5, 1, 1.5, 2, 3, 4, 6
+    const float v = m < 4 ? 0.5f * (float)m : m < 6 ? (float)(m - 2) : (float)(2 * m - 8);
+    return c & 8u ? -v : v;
+}
+
+// ---- launchers ----
+struct Quant4Args {
+    const void* x;
+    int64_t ld;  // elements
+    int64_t rows, K;
+    int64_t src_rows;       // x's rows: a row gathered from outside them is NaN
+    const int32_t* gather;  // source row of row i (nullable)
+    uint8_t* q;
+    uint8_t* scale;
+    int64_t ldq;
+    int tiles;  // scale tiles side by side
+};
+cudaError_t launch_fp4_quantize(const Quant4Args& a, int dtype, int num_sms, cudaStream_t s);
+
+constexpr int FP4_OUT_FP4 = 3;  // of out_kind, beside FP8_OUT_F32 and FP8_OUT_BF16
+// tmA, tmB: bytes of q as half as many 16-bit elements, boxes of 128 bytes; nkb: stages of 256 columns; lds: scale tiles
+// side by side; 4-bit outputs: ldo bytes between rows of q, ldos scale tiles side by side.
+struct Fp4GemmArgs : Fp8GemmArgs {
+    CUtensorMap tmSA;  // scale tiles, boxes of two side by side (256 columns)
+    CUtensorMap tmSB[CM_MAX_E];
+    int ksteps;  // MMAs of 64 columns
+};
+int check_fp4(const clearmoe_fp4* m);
+// Scale tiles [tile_rows x tile_cols] of 512 bytes as a tensor map, boxes of two tiles side by side x box_rows.
+int encode_tmap_fp4_scales(CUtensorMap* map, const void* base, int64_t tile_rows, int64_t tile_cols, int box_rows);
+
+}  // namespace cm

@@ -1,0 +1,120 @@
+// Pieces shared by the kernels of products in 4-bit blocks: instruction descriptor, tiles, outputs. The epilogue's
+// arithmetic, the stores of fp32 and bf16 rows and the copy of scales to tensor memory are fp8_gemm.cuh's.
+#pragma once
+
+#include "fp4.cuh"
+#include "fp8_gemm.cuh"
+
+namespace cm {
+
+constexpr int F4_BK = 256;  // columns of a stage: 128 bytes of q, two scale tiles
+constexpr int F4_SF = 1024;  // bytes of a stage's scales for 128 rows
+
+// Instruction descriptor of kind::mxf4: e2m1 A and W, UE8M0 scales of 32 columns; `half` selects the two scale bytes of
+// each word that an MMA of 64 columns takes.
+__device__ __forceinline__ uint32_t idesc_mxf4(int M, int N, int half) {
+    return ((uint32_t)(2 * half) << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | (1u << 23) |
+           ((uint32_t)(M >> 4) << 24) | ((uint32_t)(2 * half) << 29);
+}
+
+// Row boundaries of the groups, off[E + 1], held to ascend within the rows (f8_groups), and the row tiles before each,
+// prefix[E + 1]. A group's tiles start at the scale tile that its first row lies in, so that scales come as they lie;
+// rows of another group in its first and last tile are computed and not stored.
+__device__ __forceinline__ void f4_groups(const Fp4GemmArgs& a, int bm, int* off, int* prefix) {
+    int acc = 0;
+    for (int e = 0; e <= a.E; ++e) {
+        const int v = a.offsets ? __ldcg(a.offsets + e) : (e == 0 ? 0 : (int)a.M);
+        off[e] = min(max(v, acc), (int)a.M);
+        acc = off[e];
+    }
+    acc = 0;
+    for (int e = 0; e < a.E; ++e) {
+        prefix[e] = acc;
+        if (off[e + 1] > off[e]) acc += (off[e + 1] - (off[e] & ~127) + bm - 1) / bm;
+    }
+    prefix[a.E] = acc;
+}
+// F8Walk over such tiles: rows [max(m0, lo), hi) of a tile are the group's.
+struct F4Walk {
+    int mt, nt;  // row and column tile
+    int e, m0, lo, hi, n0;
+    int n_tiles, bm, bn, E, step_mt, step_nt;
+    const int* off;
+    const int* prefix;
+    __device__ __forceinline__ F4Walk(int first, int step, int N, int bm_, int bn_, int E_, const int* off_, const int* prefix_)
+        : e(0), n_tiles((N + bn_ - 1) / bn_), bm(bm_), bn(bn_), E(E_), off(off_), prefix(prefix_) {
+        mt = first / n_tiles;
+        nt = first - mt * n_tiles;
+        step_mt = step / n_tiles;
+        step_nt = step - step_mt * n_tiles;
+        place();
+    }
+    __device__ __forceinline__ bool live() const { return mt < prefix[E]; }
+    __device__ __forceinline__ void next() {
+        mt += step_mt;
+        nt += step_nt;
+        if (nt >= n_tiles) {
+            nt -= n_tiles;
+            ++mt;
+        }
+        place();
+    }
+    __device__ __forceinline__ void place() {
+        while (e + 1 < E && prefix[e + 1] <= mt) ++e;
+        lo = off[e];
+        m0 = (lo & ~127) + (mt - prefix[e]) * bm;
+        hi = off[e + 1];
+        n0 = nt * bn;
+    }
+};
+
+// The output row of row m of A (-1: none).
+__device__ __forceinline__ int f4_out_row(const Fp4GemmArgs& a, int m, int lo, int hi) {
+    return m >= lo ? f8_out_row(a, m, hi) : -1;
+}
+
+// 32 rows' 32 columns [nc, nc + 32) (one row a lane: its output row, or -1) to out.
+template <int KIND>
+__device__ __forceinline__ void f4_store32(const Fp4GemmArgs& a, float (&v)[32], int row, int nc, bool wide, int lane) {
+    if constexpr (KIND == FP4_OUT_FP4) {
+        // a row's 32 columns are one block; zeros past N
+        if (nc + 32 > a.N) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (nc + i >= a.N) v[i] = 0.f;
+        }
+        const uint32_t s = fp4_scale_byte(abs_bits(f8_max_abs32(v)));
+        const float inv = fp8_inverse_scale(s);
+        uint32_t o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = fp4_pack8_scaled(v + 8 * i, make_float2(inv, inv));
+        if (row >= 0 && nc / 2 < a.ldo) {
+            *reinterpret_cast<uint4*>(static_cast<uint8_t*>(a.out) + (int64_t)row * a.ldo + nc / 2) = make_uint4(o[0], o[1], o[2], o[3]);
+            a.out_scale[fp4_scale_word(row, nc >> 7, a.ldos) + (nc >> 5 & 3)] = (uint8_t)s;
+        }
+    } else {
+        if (a.rows || (wide && nc + 32 <= a.N)) {
+            f8_store32<KIND>(a, v, row, nc, wide, lane);
+            return;
+        }
+        // rows of any pitch in order, of which a group's first tile may leave out the first ones
+        __syncwarp();
+        f8_transpose(v, lane);
+        const uint32_t live = __ballot_sync(0xFFFFFFFFu, row >= 0);
+        if (!live) return;
+        const int first = __ffs(live) - 1, end = nc + lane < a.N ? first + __popc(live) : 0;
+        using T = std::conditional_t<KIND == FP8_OUT_BF16, uint16_t, float>;
+        T* o = static_cast<T*>(a.out) + ((int64_t)__shfl_sync(0xFFFFFFFFu, row, first) - first) * a.ldo + nc + lane;
+#pragma unroll
+        for (int r = 0; r < 32; ++r, o += a.ldo) {
+            if (r >= first && r < end) {
+                if constexpr (KIND == FP8_OUT_BF16)
+                    *o = f32_to_bf16(v[r]);
+                else
+                    *o = v[r];
+            }
+        }
+    }
+}
+
+}  // namespace cm

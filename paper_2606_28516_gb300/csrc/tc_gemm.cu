@@ -45,6 +45,7 @@
 
 #include "common.cuh"
 #include "internal.h"
+#include "fp4.cuh"
 #include "tmap_cache.h"
 
 namespace cm {
@@ -1009,6 +1010,7 @@ typedef CUresult (*PFN_encodeTiled_t)(CUtensorMap*, CUtensorMapDataType, cuuint3
 
 namespace {
 TmapCache<CUtensorMap> g_tmaps;
+constexpr int TMAP_FP4_SCALES = 3;  // of TmapKey::elem, beside the element sizes
 }  // namespace
 
 static int encode_tmap_uncached(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int box_rows,
@@ -1041,6 +1043,10 @@ int encode_tmap_bytes(CUtensorMap* map, const void* base, int64_t rows, int64_t 
     return encode_tmap_cached(map, base, rows, cols, box_rows, 0, 1);
 }
 
+int encode_tmap_fp4_scales(CUtensorMap* map, const void* base, int64_t tile_rows, int64_t tile_cols, int box_rows) {
+    return encode_tmap_cached(map, base, tile_rows, tile_cols, box_rows, 0, TMAP_FP4_SCALES);
+}
+
 static int encode_tmap_uncached(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int box_rows,
                                 int box_chunks, int elem) {
     static PFN_encodeTiled_t fn = nullptr;
@@ -1061,6 +1067,14 @@ static int encode_tmap_uncached(CUtensorMap* map, const void* base, int64_t rows
         const cuuint32_t es[2] = {1, 1};
         r = fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<void*>(base), gdim, gstride, box, es,
                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    } else if (elem == TMAP_FP4_SCALES) {  // tiles of 512 bytes: boxes of two side by side x box_rows
+        const cuuint64_t gdim[2] = {(cuuint64_t)cols * 128, (cuuint64_t)rows};
+        const cuuint64_t gstride[1] = {(cuuint64_t)cols * 512};
+        const cuuint32_t box[2] = {256, (cuuint32_t)box_rows};
+        const cuuint32_t es[2] = {1, 1};
+        r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void*>(base), gdim, gstride, box, es,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     } else if (elem == 1) {  // bytes [rows x cols]: boxes of 64 columns x box_rows rows
         const cuuint64_t gdim[2] = {(cuuint64_t)cols, (cuuint64_t)rows};

@@ -1,0 +1,358 @@
+"""4-bit blocks on the GPU: quantisation against numpy bit for bit, products against float64.
+
+Error bounds, per element: products of e2m1 values and their scales are exact, so the fp32 sum over K terms is off by at
+most (K + 8) 2^-23 sum |a| |w| (2^-23: the tensor cores may cut instead of round); bias and activation add a few fp32
+roundings and the GELU's own 4e-7 (times 1.13, the largest slope, what came before); bf16 outputs half a bf16 step (2^-8
+relative, with what is before it); 4-bit outputs half an e2m1 step: at most 1/5 of the value (1.25, 2.5 and 5 lie half way)
+or, below 0.5, a quarter of the block's scale, which is less than a third of its largest magnitude."""
+import numpy as np
+import pytest
+import torch
+
+import fp4_ref as R
+from paper_2606_28516_gb300 import clearmoe as cm
+
+pytestmark = pytest.mark.gpu
+
+
+def dev(a, dtype=torch.float32):
+    with np.errstate(over="ignore"):
+        return torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to("cuda").to(dtype)
+
+
+def rows_of(rng, M, K, spread=4.0):
+    x = rng.standard_normal((M, K)) * np.exp(spread * rng.standard_normal((M, 1)))
+    x[:, rng.random(K) < 0.02] *= 50.0
+    return x.astype(np.float32)
+
+
+def f64(t):
+    return t.float().cpu().numpy().astype(np.float64)
+
+
+def check_quantized(m, x):
+    """Codes, their padding and scale bytes of m against numpy's of x; numpy's values."""
+    code, s, val = R.quantize(x)
+    assert np.array_equal(R.scale_bytes(m.scale.cpu().numpy(), m.rows, m.cols), s)
+    got, rest = R.unpack(m.q.cpu().numpy(), m.cols)
+    fine = np.repeat(s != 255, 32, 1)[:, :m.cols]
+    assert np.array_equal(np.where(fine, got, 0), np.where(fine, code, 0))
+    last = s[:, -1] != 255
+    assert not rest[last].any()
+    return val
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("M,K,pad", [(1, 1, 0), (1, 32, 0), (3, 31, 0), (5, 33, 0), (17, 512, 8), (130, 96, 0), (2, 1131, 3),
+                                     (300, 72, 0), (129, 200, 8)])
+def test_quantize(M, K, pad, dtype):
+    rng = np.random.default_rng(M * 1000 + K)
+    x = dev(rows_of(rng, M, K + pad), dtype)[:, :K]
+    m = cm.fp4_matrix(M, K)
+    m.q.fill_(0x5A)
+    m.scale.fill_(0x5A)
+    cm.clearmoe_fp4_quantize(x, m)
+    val = check_quantized(m, f64(x))
+    tiles = m.scale.cpu().numpy()  # rows past the last are left as they were
+    rest = np.concatenate([R.scale_bytes(tiles, tiles.shape[0] * 128, tiles.shape[1] * 128)[M:].ravel(), [0x5A]])
+    assert (rest == 0x5A).all()
+    out = torch.full((M, K), float("nan"), device="cuda")
+    cm.clearmoe_fp4_dequantize(m, out)
+    assert np.array_equal(f64(out), val)
+    wide = torch.full((M, K + 3), float("nan"), device="cuda", dtype=torch.bfloat16)
+    cm.clearmoe_fp4_dequantize(m, wide[:, :K])
+    assert np.array_equal(f64(wide[:, :K]), val) and bool(wide[:, K:].isnan().all())  # two significant bits: exact
+
+
+def test_quantize_ties_and_extremes():
+    x = np.zeros((12, 64), np.float32)
+    x[1, 3] = np.inf
+    x[2, 40] = np.nan
+    x[3] = 1e-45
+    x[4] = 3.4e38
+    x[5, :32] = 6.0
+    x[6, :32] = np.nextafter(np.float32(6.0), np.float32(7))
+    x[7] = -(2.0 ** -130)
+    x[8, 5] = 1.0
+    x[9, :17] = [6, .25, .75, 1.25, 1.75, 2.5, 3.5, 5, -.25, -.75, -1.25, -1.75, -2.5, -3.5, -5, -0.0, -6]
+    x[10, :17] = np.nextafter(x[9, :17], np.float32(0))
+    x[11, 32:49] = x[9, :17]
+    for dtype in (torch.float32, torch.bfloat16):
+        t = dev(x, dtype)
+        m = cm.fp4_matrix(12, 64)
+        cm.clearmoe_fp4_quantize(t, m)
+        val = check_quantized(m, f64(t))
+        out = torch.empty(12, 64, device="cuda")
+        cm.clearmoe_fp4_dequantize(m, out)
+        with np.errstate(over="ignore"):  # 3.4e38 rounds to 2^128, past fp32
+            assert np.array_equal(f64(out), val.astype(np.float32), equal_nan=True)
+
+
+@pytest.mark.parametrize("K", [256, 250])
+def test_quantize_gathered(K):
+    x = rows_of(np.random.default_rng(1), 9, K)
+    t = dev(x)
+    at = torch.tensor([8, 0, 8, 4, 5, -1, 9, 2 ** 31 - 1], dtype=torch.int32, device="cuda")
+    m = cm.fp4_matrix(8, K)
+    cm.clearmoe_fp4_quantize(t, m, gather=at)
+    val = np.full((8, K), np.nan)
+    val[:5] = x[at.cpu().numpy()[:5]]
+    check_quantized(m, val)
+
+
+def test_quantize_far_rows():
+    """Rows whose offsets pass 32 bits: two of a wide pitch."""
+    ld = 1 << 29
+    x = torch.zeros(5, ld, dtype=torch.bfloat16, device="cuda")
+    v = dev(rows_of(np.random.default_rng(2), 5, 100), torch.bfloat16)
+    x[:, 7:107] = v
+    m = cm.fp4_matrix(5, 100)
+    cm.clearmoe_fp4_quantize(x[:, 7:107], m)
+    check_quantized(m, f64(v))
+
+
+def make(rng, M, N, K, wscale=0.02):
+    A, W = cm.fp4_matrix(M, K), cm.fp4_matrix(N, K)
+    for m in (A, W):  # bytes of rows past the last may be anything
+        m.scale.fill_(255)
+    cm.clearmoe_fp4_quantize(dev(rows_of(rng, M, K, 1.0)), A)
+    cm.clearmoe_fp4_quantize(dev(rows_of(rng, N, K, 0.5) * wscale), W)
+    return A, W, values(A), values(W)
+
+
+def values(m):
+    out = torch.empty(m.rows, m.cols, device="cuda")
+    cm.clearmoe_fp4_dequantize(m, out)
+    return out.double()
+
+
+def reference(av, wv, bias, act):
+    """float64 result and the bound on the fp32 one's error."""
+    y, mag = av @ wv.T, av.abs() @ wv.abs().T
+    err = (av.shape[1] + 8) * 2.0 ** -23 * mag
+    if bias is not None:
+        y = y + bias.double()
+        err = err + 2.0 ** -23 * (y.abs() + bias.double().abs())
+    if act == cm.ACT_GELU:
+        y = 0.5 * y * torch.erfc(-y / np.sqrt(2.0))
+        err = 1.13 * err + 4e-7 + 4e-7 * y.abs()
+    elif act == cm.ACT_RELU:
+        y = y.clamp(min=0)
+    return y, err
+
+
+def within(out, y, err):
+    return bool(((out.double() - y).abs() <= err + (2.0 ** -8 * y.abs() if out.dtype == torch.bfloat16 else 0) + 1e-38).all())
+
+
+SHAPES = [(1, 1, 1), (1, 96, 16), (3, 130, 64), (128, 128, 128), (129, 200, 511), (197, 768, 192), (64, 33, 4099),
+          (1000, 777, 640), (5000, 512, 384), (20000, 192, 1024), (260, 2048, 768), (7, 5000, 65), (16, 64, 8192)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_gemm(M, N, K, dtype):
+    rng = np.random.default_rng(M + 7 * N + 13 * K)
+    A, W, av, wv = make(rng, M, N, K)
+    act = (cm.ACT_NONE, cm.ACT_GELU, cm.ACT_RELU)[(M + N + K) % 3]
+    bias = dev(rng.standard_normal(N), dtype) if (M + N) % 2 else None
+    out = torch.full((M + 1, N + 3), float("nan"), device="cuda", dtype=dtype)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    cm.clearmoe_fp4_gemm(A, W, out[:M, :N], bias=bias, act=act, status=status)
+    y, err = reference(av, wv, bias, act)
+    assert status.item() == 0
+    assert within(out[:M, :N], y, err)
+    assert bool(out[M].isnan().all()) and bool(out[:, N:].isnan().all())  # nothing past the output
+    dense = torch.empty(M, N, device="cuda", dtype=dtype)
+    cm.clearmoe_fp4_gemm(A, W, dense, bias=bias, act=act)
+    assert torch.equal(dense, out[:M, :N])  # every store width gives the same values
+
+
+KERNELS = [(128, 0), (64, 0)]
+
+
+@pytest.fixture
+def kernel(request):
+    cm.clearmoe_debug_fp4_kernel(*request.param)
+    yield request.param
+    cm.clearmoe_debug_fp4_kernel()
+
+
+def check_blocks(q, y, err):
+    """A matrix in 4-bit blocks against the float64 values that it was rounded from."""
+    M, N = y.shape
+    amax = torch.nn.functional.pad(y.abs(), (0, -N % 32)).view(M, -1, 32).amax(2).repeat_interleave(32, 1)[:, :N]
+    got = values(q)
+    assert bool(((got - y).abs() <= 1.2 * err + 0.2 * y.abs() + 0.25 * 1.01 * amax / 3 + 1e-38).all())
+    assert not R.unpack(q.q.cpu().numpy(), N)[1].any()
+    # the scale is the least that holds the block, to the error
+    s = R.scale_bytes(q.scale.cpu().numpy(), M, N).astype(np.float64)
+    s = torch.from_numpy(np.repeat(s, 32, 1)[:, :N]).cuda()
+    top = torch.nn.functional.pad(err, (0, -N % 32)).view(M, -1, 32).amax(2).repeat_interleave(32, 1)[:, :N]
+    assert bool(((amax <= 6 * torch.exp2(s - 127) + top) & ((amax > 3 * torch.exp2(s - 127) - top) | (s == 0))).all())
+
+
+@pytest.mark.parametrize("kernel", KERNELS, indirect=True)
+@pytest.mark.parametrize("M,N,K,act", [(700, 700, 1300, cm.ACT_GELU), (5, 40, 130, cm.ACT_NONE), (257, 300, 512, cm.ACT_RELU),
+                                       (40000, 200, 100, cm.ACT_NONE), (130, 129, 2000, cm.ACT_NONE)])
+def test_every_kernel(kernel, M, N, K, act):
+    """Each tile width on one SM and on pairs: sums, every kind of store, 4-bit outputs."""
+    rng = np.random.default_rng(M + N)
+    A, W, av, wv = make(rng, M, N, K)
+    bias = dev(rng.standard_normal(N) * 0.1)
+    y, err = reference(av, wv, bias, act)
+    for dtype in (torch.float32, torch.bfloat16):
+        out = torch.full((M, N), float("nan"), device="cuda", dtype=dtype)
+        cm.clearmoe_fp4_gemm(A, W, out, bias=bias, act=act)
+        assert within(out, y, err)
+    q = cm.fp4_matrix(M, N)
+    q.q.fill_(0x33)
+    cm.clearmoe_fp4_gemm(A, W, q, bias=bias, act=act)
+    check_blocks(q, y, err)
+
+
+@pytest.mark.parametrize("perm", [True, False])
+@pytest.mark.parametrize("counts", [[0, 300, 1, 0, 129, 700], [1130], [3, 2, 0, 1], [128, 128, 256], [127, 1, 129, 255, 0, 77, 500, 41],
+                                    [1] * 16])
+@pytest.mark.parametrize("kernel", KERNELS, indirect=True)
+def test_every_kernel_grouped(kernel, counts, perm):
+    rng = np.random.default_rng(77)
+    N, K = 320, 640
+    M, off = sum(counts), np.concatenate([[0], np.cumsum(counts)])
+    A, _, av, _ = make(rng, M, N, K)
+    pairs = [make(rng, 1, N, K)[1::2] for _ in counts]
+    at = rng.permutation(M) if perm else np.arange(M)
+    for pad, dtype in ((0, torch.float32), (3, torch.bfloat16), (3, torch.float32)):
+        out = torch.full((M + 1, N + pad), float("nan"), device="cuda", dtype=dtype)
+        cm.clearmoe_fp4_grouped_gemm(A, [p[0] for p in pairs], torch.tensor(off, dtype=torch.int32, device="cuda"), out[:M, :N],
+                                     perm=torch.tensor(at, dtype=torch.int32, device="cuda") if perm else None)
+        for e in range(len(counts)):
+            sl = slice(int(off[e]), int(off[e + 1]))
+            y, err = reference(av[sl], pairs[e][1], None, cm.ACT_NONE)
+            assert within(out[torch.tensor(at[sl], device="cuda", dtype=torch.long), :N], y, err)
+        assert bool(out[M].isnan().all()) and bool(out[:, N:].isnan().all())
+
+
+def test_grouped_rows_outside_the_offsets_are_left():
+    """Offsets that end before A does (a padded batch): the rows behind the last group stay as they were."""
+    rng = np.random.default_rng(3)
+    A, W, av, wv = make(rng, 300, 96, 128)
+    out = torch.full((300, 96), 7.0, device="cuda")
+    cm.clearmoe_fp4_grouped_gemm(A, [W, W], torch.tensor([5, 100, 201], dtype=torch.int32, device="cuda"), out)
+    y, err = reference(av, wv, None, cm.ACT_NONE)
+    assert within(out[5:201], y[5:201], err[5:201])
+    assert bool((out[:5] == 7).all()) and bool((out[201:] == 7).all())
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 128, 128), (130, 768, 192), (77, 200, 300), (4000, 1536, 384), (9, 1, 5), (3, 97, 64)])
+def test_gemm_to_blocks(M, N, K):
+    rng = np.random.default_rng(M + N + K)
+    A, W, av, wv = make(rng, M, N, K)
+    bias = dev(rng.standard_normal(N) * 0.1, torch.bfloat16)
+    out = cm.fp4_matrix(M, N)
+    out.q.fill_(0x33)
+    cm.clearmoe_fp4_gemm(A, W, out, bias=bias, act=cm.ACT_GELU)
+    check_blocks(out, *reference(av, wv, bias, cm.ACT_GELU))
+    assert out.rows == M
+
+
+@pytest.mark.parametrize("kernel", KERNELS + [(0, 0)], indirect=True)
+@pytest.mark.parametrize("M", [4, 257])
+def test_blocks_keep_their_scales(kernel, M):
+    """Every block of A and W in a scale of its own, over several stages, tiles and words: one byte read from the wrong
+    place is off by a power of two."""
+    N, K = 320, 1536 + 96
+    rng = np.random.default_rng(5)
+    a = rng.standard_normal((M, K)) * np.repeat(2.0 ** rng.integers(-20, 20, (M, K // 32)), 32, 1)
+    w = rng.standard_normal((N, K)) * np.repeat(2.0 ** rng.integers(-20, 20, (N, K // 32)), 32, 1)
+    A, W, out = cm.fp4_matrix(M, K), cm.fp4_matrix(N, K), torch.empty(M, N, device="cuda")
+    cm.clearmoe_fp4_quantize(dev(w), W)
+    wv = values(W)
+    for kb in [None, *range(K // 32)]:  # all, then each block alone
+        one = a if kb is None else np.where(np.arange(K) // 32 == kb, a, 0.0)
+        cm.clearmoe_fp4_quantize(dev(one), A)
+        cm.clearmoe_fp4_gemm(A, W, out)
+        assert within(out, *reference(values(A), wv, None, cm.ACT_NONE))
+
+
+@pytest.mark.parametrize("kernel", KERNELS + [(0, 0)], indirect=True)
+@pytest.mark.parametrize("M", [3, 200])
+def test_nan_stays_in_its_row_and_column(kernel, M):
+    rng = np.random.default_rng(11)
+    N, K = 200, 300
+    x, w = rows_of(rng, M, K, 1.0), rows_of(rng, N, K, 0.5)
+    x[1, 299], w[131, 5], w[7, 100] = np.inf, np.nan, -np.inf
+    A, W, out = cm.fp4_matrix(M, K), cm.fp4_matrix(N, K), torch.zeros(M, N, device="cuda")
+    cm.clearmoe_fp4_quantize(dev(x), A)
+    cm.clearmoe_fp4_quantize(dev(w), W)
+    for act in (cm.ACT_NONE, cm.ACT_RELU, cm.ACT_GELU):
+        cm.clearmoe_fp4_gemm(A, W, out, act=act)
+        want = torch.zeros(M, N, dtype=torch.bool, device="cuda")
+        want[1], want[:, 131], want[:, 7] = True, True, True
+        assert torch.equal(out.isnan(), want)
+        q = cm.fp4_matrix(M, N)
+        cm.clearmoe_fp4_gemm(A, W, q, act=act)
+        blocks = torch.nn.functional.pad(want, (0, -N % 32)).view(M, -1, 32).any(2).repeat_interleave(32, 1)[:, :N]
+        assert torch.equal(values(q).isnan(), blocks)
+
+
+@pytest.mark.parametrize("kernel", KERNELS + [(0, 0)], indirect=True)
+@pytest.mark.parametrize("M", [2, 130])
+def test_scales_at_the_ends_of_their_range(kernel, M):
+    """Values near fp32's ends, and past them as rounded, whose products are not: the scales are applied together. An input
+    past fp32 is an infinity: NaN."""
+    def values(m):  # in float64: 4 2^126 is past fp32
+        c = R.unpack(m.q.cpu().numpy(), m.cols)[0]
+        s = np.repeat(R.scale_bytes(m.scale.cpu().numpy(), m.rows, m.cols), 32, 1)[:, :m.cols].astype(np.float64)
+        return torch.from_numpy(np.where(s == 255, np.nan, R.e2m1_value(c) * 2.0 ** (s - 127))).cuda()
+
+    N, K = 70, 128
+    rng = np.random.default_rng(13)
+    a = rng.standard_normal((M, K))
+    w = rng.standard_normal((N, K))
+    for p, q in ((120, -118), (-120, 118), (100, -3), (-126, 126)):
+        A, W, out = cm.fp4_matrix(M, K), cm.fp4_matrix(N, K), torch.empty(M, N, device="cuda")
+        cm.clearmoe_fp4_quantize(dev(a * 2.0 ** p), A)
+        cm.clearmoe_fp4_quantize(dev(w * 2.0 ** q), W)
+        cm.clearmoe_fp4_gemm(A, W, out)
+        y, err = reference(values(A), values(W), None, cm.ACT_NONE)
+        fine = ~y.isnan()
+        assert torch.equal(~out.isnan(), fine) and float(fine.float().mean()) > 0.8
+        assert within(out[fine], y[fine], err[fine])
+
+
+def test_two_products_in_a_row():
+    """A whole FFN whose hidden state is in 4-bit blocks, on a stream of its own and then replayed from a graph."""
+    rng = np.random.default_rng(17)
+    T, d, H = 300, 192, 768
+    W1, W2 = (rows_of(rng, *s, 0.0) * 0.05 for s in ((H, d), (d, H)))
+    w1, w2, xq, zq = cm.fp4_matrix(H, d), cm.fp4_matrix(d, H), cm.fp4_matrix(T, d), cm.fp4_matrix(T, H)
+    x, b1, b2 = torch.empty(T, d, device="cuda"), dev(rng.standard_normal(H) * 0.1), dev(rng.standard_normal(d) * 0.1)
+    out = torch.empty(T, d, device="cuda")
+    cm.clearmoe_fp4_quantize(dev(W1), w1)
+    cm.clearmoe_fp4_quantize(dev(W2), w2)
+
+    def ffn():
+        cm.clearmoe_fp4_quantize(x, xq)
+        cm.clearmoe_fp4_gemm(xq, w1, zq, bias=b1, act=cm.ACT_GELU)
+        cm.clearmoe_fp4_gemm(zq, w2, out, bias=b2)
+
+    def check():
+        torch.cuda.synchronize()
+        check_blocks(zq, *reference(values(xq), values(w1), b1, cm.ACT_GELU))
+        assert within(out, *reference(values(zq), values(w2), b2, cm.ACT_NONE))
+
+    side = torch.cuda.Stream()
+    x.copy_(dev(rows_of(rng, T, d, 1.0)))
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        ffn()
+    check()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ffn()
+    for _ in range(2):
+        x.copy_(dev(rows_of(rng, T, d, 1.0)))
+        out.zero_()
+        graph.replay()
+        check()
