@@ -75,6 +75,7 @@ struct Fp4GemmArgs : Fp8GemmArgs {
     CUtensorMap tmSB[CM_MAX_E];
     int ksteps;  // MMAs of 64 columns
 };
+cudaError_t launch_fp4_gemm2(const Fp4GemmArgs& a, int bn, int num_sms, cudaStream_t s);
 int check_fp4(const clearmoe_fp4* m);
 // Scale tiles [tile_rows x tile_cols] of 512 bytes as a tensor map, boxes of two tiles side by side x box_rows.
 int encode_tmap_fp4_scales(CUtensorMap* map, const void* base, int64_t tile_rows, int64_t tile_cols, int box_rows);

@@ -269,6 +269,7 @@ struct Pick {
 };
 Pick pick(int64_t M, int N, int groups, int num_sms) {
     const int64_t m_tiles = (M + F4_BM - 1) / F4_BM + groups - 1;
+    if (m_tiles * ((N + 127) / 128) >= 2 * num_sms) return {256, 1};
     return {m_tiles * ((N + 127) / 128) >= num_sms ? 128 : 64, 0};
 }
 
@@ -321,16 +322,20 @@ int run(Fp4GemmArgs& g, const clearmoe_fp4* A, const clearmoe_fp4* W, int E, voi
     g.sa = A->scale;
     Pick k = pick(g.M, g.N, E, sms);
     if (g_forced) k = {g_forced >> 1, g_forced & 1};
+    const int wt = k.pair ? (k.bn + 127) / 128 : 1;  // scale tiles of a tile's columns
     const int64_t cols16 = fp4_ldq(A->cols) / 2;
     // Fewer rows than a tile: a box of those alone (the copy engine takes longer over a row past the end).
-    g.box_rows = g.M < F4_BM ? (int)(g.M + 7) / 8 * 8 : F4_BM;
+    g.box_rows = !k.pair && g.M < F4_BM ? (int)(g.M + 7) / 8 * 8 : F4_BM;
     if (encode_tmap_bf16(&g.tmA, A->q, A->rows, cols16, g.box_rows)) return CLEARMOE_ECUDA;
     if (encode_tmap_fp4_scales(&g.tmSA, A->scale, (A->rows + 127) / 128, g.lds, 1)) return CLEARMOE_ECUDA;
     for (int e = 0; e < E; ++e) {
-        if (encode_tmap_bf16(&g.tmB[e], W[e].q, W[e].rows, cols16, k.bn)) return CLEARMOE_ECUDA;
-        if (encode_tmap_fp4_scales(&g.tmSB[e], W[e].scale, (W[e].rows + 127) / 128, g.lds, 1)) return CLEARMOE_ECUDA;
+        if (encode_tmap_bf16(&g.tmB[e], W[e].q, W[e].rows, cols16, k.pair ? k.bn / 2 : k.bn)) return CLEARMOE_ECUDA;
+        if (encode_tmap_fp4_scales(&g.tmSB[e], W[e].scale, (W[e].rows + 127) / 128, g.lds, wt)) return CLEARMOE_ECUDA;
     }
-    if ((k.bn == 128 ? launch_kind<128>(g, sms, s) : launch_kind<64>(g, sms, s)) == cudaSuccess) return CLEARMOE_OK;
+    const cudaError_t e = k.pair        ? launch_fp4_gemm2(g, k.bn, sms, s)
+                          : k.bn == 128 ? launch_kind<128>(g, sms, s)
+                                        : launch_kind<64>(g, sms, s);
+    if (e == cudaSuccess) return CLEARMOE_OK;
     (void)cudaGetLastError();
     return CLEARMOE_ECUDA;
 }
@@ -382,7 +387,8 @@ int clearmoe_debug_fp4_kernel(int32_t width, int32_t pair) {
         cm::g_forced = 0;
         return CLEARMOE_OK;
     }
-    if (pair != 0 || (width != 128 && width != 64)) return CLEARMOE_EINVAL;
+    const bool known = pair == 1 ? width == 256 || width == 192 || width == 128 : pair == 0 && (width == 128 || width == 64);
+    if (!known) return CLEARMOE_EINVAL;
     cm::g_forced = width << 1 | pair;
     return CLEARMOE_OK;
 }

@@ -57,7 +57,7 @@ def test_library_refuses():
     arr = (cm.clearmoe_fp4 * 2)(good, fp4(rows=5))
     gg = lambda W=arr, E=1, off=A32, perm=None, ld=4: L.clearmoe_fp4_grouped_gemm(P(good), W, E, off, perm, None, A32, cm.F32, ld, None)  # noqa: E731
     assert gg(E=0) == gg(E=17) == gg(W=None) == gg(off=None) == gg(off=A32 + 2) == gg(perm=A32 + 2) == gg(E=2) == gg(ld=3) == cm.EINVAL
-    assert L.clearmoe_debug_fp4_kernel(100, 0) == L.clearmoe_debug_fp4_kernel(64, 1) == cm.EINVAL
+    assert L.clearmoe_debug_fp4_kernel(100, 0) == L.clearmoe_debug_fp4_kernel(64, 1) == L.clearmoe_debug_fp4_kernel(256, 0) == cm.EINVAL
     assert L.clearmoe_debug_fp4_kernel(0, 0) == cm.OK
 
 
@@ -199,7 +199,7 @@ def source(name):
     return re.sub(r"//[^\n]*", "", (CSRC / name).read_text())
 
 
-@pytest.mark.parametrize("name", ["fp4.cu", "fp4_gemm.cu", "norm.cu"])
+@pytest.mark.parametrize("name", ["fp4.cu", "fp4_gemm.cu", "fp4_gemm2.cu", "norm.cu"])
 def test_reads_and_releases_after_the_wait(name):
     """Every kernel waits for its predecessor before it releases its successor (a run cannot show that one does not)."""
     s = source(name)
@@ -216,6 +216,7 @@ def kernel(name):
 
 @pytest.mark.parametrize("name,drains,last", [
     ("fp4_gemm.cu", ["mbar_wait_warp(full_bar(s), (par >> s) & 1", "mbar_wait_warp(drain_bar, 0"], "tmem_dealloc(tmem"),
+    ("fp4_gemm2.cu", ["mbar_wait_warp(full_bar(s), (k / STAGES) & 1", "mbar_wait_warp(drain_bar, 0"], "tcgen05.dealloc"),
 ])
 def test_copies_and_mmas_end_before_tensor_memory_is_freed(name, drains, last):
     """Each role waits for what it started; then all meet; then the memory is freed, in no role's branch."""
@@ -224,10 +225,12 @@ def test_copies_and_mmas_end_before_tensor_memory_is_freed(name, drains, last):
     meet = s.rindex("__syncthreads();", 0, free)
     for d in drains:
         assert s.count(d) == 1 and s.index(d) < meet, d
-    assert "return;" not in s[:meet]
+    assert "return;" not in re.sub(r"auto \w+ = \[&\]\(int acc\) \{.*?\n        \};", "", s[:meet], flags=re.S)  # no thread leaves early
+    if name == "fp4_gemm2.cu":
+        assert meet < s.index("cluster_sync();", meet) < free
 
 
-@pytest.mark.parametrize("name", ["fp4_gemm.cu"])
+@pytest.mark.parametrize("name", ["fp4_gemm.cu", "fp4_gemm2.cu"])
 def test_tensor_memory_accesses_follow_a_fence(name):
     s = kernel(name)
     waits = [m.start() for m in re.finditer(r"\bmbar_wait_warp\(", s)]
