@@ -3,11 +3,13 @@
 // Bound by HBM: x and r are read, s and y written, once each.
 //
 // A warp takes 512 columns of a row at a time, 16 a lane; a row is 1 to 16 warps' and each has up to four such pieces.
-// Aligned rows: a lane has 16 consecutive columns, so that eight lanes have a block of 128 and two a block of 32, and
-// scales take three shuffles or one. Other rows: a lane has columns 32 apart, so that loads and stores are of consecutive
-// elements, and a block's scale takes five shuffles.
+// Aligned rows: a lane has pieces of 16 bytes, so that 16 (fp32: 32) lanes have a block of 128 columns and four (eight) one
+// of 32. Other rows: a lane has columns 32 apart, so that loads and stores are of consecutive elements, and values are
+// turned to such pieces in shared memory. CTAs stay and take every gridDim-th group of rows. Aligned rows of one piece a
+// warp come through shared memory, each lane's own elements a row ahead, so that loads on their way hold no registers.
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "common.cuh"
 #include "fp4.cuh"
@@ -18,7 +20,7 @@ namespace cm {
 
 namespace {
 
-enum NormOut { NORM_OUT_DTYPE = 0, NORM_OUT_FP8 = 1, NORM_OUT_FP4 = 2 };
+enum NormOut { NORM_OUT_F32 = 0, NORM_OUT_BF16 = 1, NORM_OUT_FP8 = 2, NORM_OUT_FP4 = 3 };
 
 struct NormArgs {
     const void* x;
@@ -30,7 +32,6 @@ struct NormArgs {
     int w_bf16;
     float eps;
     void* out;      // or q
-    int out_bf16;
     int64_t ldo;    // elements, or bytes between rows of q
     uint8_t* scale;
     int64_t ld_scale;  // 8 bits: bytes between rows of scales; 4 bits: scale tiles side by side
@@ -38,237 +39,339 @@ struct NormArgs {
     int w_vec;
 };
 
-template <typename T>
-__device__ __forceinline__ float load1(const void* p, int64_t at) {
-    return sizeof(T) == 2 ? bf16_to_f32(__ldcg(static_cast<const uint16_t*>(p) + at)) : __ldcg(static_cast<const float*>(p) + at);
+__device__ __forceinline__ uint4 pack8(const float2* v) {
+    return make_uint4(pack_bf16(v[0].x, v[0].y), pack_bf16(v[1].x, v[1].y), pack_bf16(v[2].x, v[2].y), pack_bf16(v[3].x, v[3].y));
 }
-__device__ __forceinline__ void unpack8(const uint4& u, float* v) {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+// x + r as stored. In bf16 one rounding of the exact sum, which that of the fp32 sum equals: a term whose last bit fp32
+// drops is below 2^-16 of the other, and the nearest half way point 2^-10 away.
+__device__ __forceinline__ uint32_t add_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
+// A lane's 16 elements of a row. VEC: pieces of 16 bytes, P columns each, 32 P columns apart, so that a load's lanes read
+// consecutive bytes; otherwise single ones, 32 apart.
+template <typename T, bool VEC>
+struct Lane16 {
+    static constexpr bool BF16 = sizeof(T) == 2;
+    static constexpr int P = VEC ? (BF16 ? 8 : 4) : 1, N = 16 / P;
+    using Piece = std::conditional_t<VEC, uint4, T>;
+    Piece u[N];
+    __device__ __forceinline__ static constexpr int at(int h) { return 32 * P * h; }  // piece h's column, from the first on
+
+    // p: the first element's place; left: columns from there to the row's end
+    __device__ __forceinline__ void load(const T* p, int left) {
+        if (VEC || left > at(N - 1)) {  // whole warps of single elements without a test each
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[2 * i] = bf16_lo(w[i]), v[2 * i + 1] = bf16_hi(w[i]);
-}
-// Eight elements from an aligned place on.
-template <typename T>
-__device__ __forceinline__ void load8(const void* p, int64_t at, float* v) {
-    if (sizeof(T) == 2) {
-        unpack8(__ldcg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + at)), v);
-    } else {
-        const float4* f = reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
-        const float4 a = __ldcg(f), b = __ldcg(f + 1);
-        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+            for (int h = 0; h < N; ++h) {
+                if (VEC) u[h] = Piece{};
+                if (!VEC || at(h) < left) u[h] = __ldcg(reinterpret_cast<const Piece*>(p + at(h)));
+            }
+        } else {
+#pragma unroll
+            for (int h = 0; h < N; ++h) u[h] = at(h) < left ? __ldcg(reinterpret_cast<const Piece*>(p + at(h))) : Piece{};
+        }
     }
-}
-__device__ __forceinline__ uint4 pack8(const float* v) {
-    return make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-}
-__device__ __forceinline__ void store8(void* p, bool bf16, int64_t at, const float* v) {
-    if (bf16) {
-        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + at) = pack8(v);
-    } else {
-        float4* f = reinterpret_cast<float4*>(static_cast<float*>(p) + at);
-        f[0] = make_float4(v[0], v[1], v[2], v[3]);
-        f[1] = make_float4(v[4], v[5], v[6], v[7]);
+    // The same by way of shared memory (VEC), a thread's pieces `pitch` apart.
+    __device__ __forceinline__ static void ask(uint32_t to, uint32_t pitch, const T* p, int left) {
+#pragma unroll
+        for (int h = 0; h < N; ++h)
+            if (at(h) < left) cp_async_16(to + h * pitch, p + at(h));
     }
+    __device__ __forceinline__ void take(uint32_t from, uint32_t pitch, int left) {
+        if constexpr (VEC) {
+#pragma unroll
+            for (int h = 0; h < N; ++h) {
+                u[h] = make_uint4(0, 0, 0, 0);
+                if (at(h) < left)
+                    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];"
+                                 : "=r"(u[h].x), "=r"(u[h].y), "=r"(u[h].z), "=r"(u[h].w)
+                                 : "r"(from + h * pitch)
+                                 : "memory");
+            }
+        }
+    }
+    __device__ __forceinline__ void add(const Lane16& r) {
+#pragma unroll
+        for (int h = 0; h < N; ++h) {
+            if constexpr (VEC && BF16) {
+                u[h].x = add_bf16x2(u[h].x, r.u[h].x), u[h].y = add_bf16x2(u[h].y, r.u[h].y);
+                u[h].z = add_bf16x2(u[h].z, r.u[h].z), u[h].w = add_bf16x2(u[h].w, r.u[h].w);
+            } else if constexpr (VEC) {
+                float2 p = __fadd2_rn(make_float2(__uint_as_float(u[h].x), __uint_as_float(u[h].y)),
+                                      make_float2(__uint_as_float(r.u[h].x), __uint_as_float(r.u[h].y)));
+                float2 q = __fadd2_rn(make_float2(__uint_as_float(u[h].z), __uint_as_float(u[h].w)),
+                                      make_float2(__uint_as_float(r.u[h].z), __uint_as_float(r.u[h].w)));
+                u[h] = make_uint4(__float_as_uint(p.x), __float_as_uint(p.y), __float_as_uint(q.x), __float_as_uint(q.y));
+            } else if constexpr (BF16) {
+                u[h] = (T)add_bf16x2(u[h], r.u[h]);
+            } else {
+                u[h] += r.u[h];
+            }
+        }
+    }
+    __device__ __forceinline__ void store(T* p, int left) const {
+#pragma unroll
+        for (int h = 0; h < N; ++h)
+            if (at(h) < left) *reinterpret_cast<Piece*>(p + at(h)) = u[h];
+    }
+    __device__ __forceinline__ void values(float2 (&v)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (!VEC && BF16)
+                v[i] = make_float2(bf16_to_f32(u[2 * i]), bf16_to_f32(u[2 * i + 1]));
+            else if constexpr (!VEC)
+                v[i] = make_float2(u[2 * i], u[2 * i + 1]);
+            else if constexpr (BF16) {
+                const uint4& p = u[i >> 2];
+                const uint32_t w = (i & 3) == 0 ? p.x : (i & 3) == 1 ? p.y : (i & 3) == 2 ? p.z : p.w;
+                v[i] = make_float2(bf16_lo(w), bf16_hi(w));
+            } else {
+                const uint4& p = u[i >> 1];
+                v[i] = i & 1 ? make_float2(__uint_as_float(p.z), __uint_as_float(p.w)) : make_float2(__uint_as_float(p.x), __uint_as_float(p.y));
+            }
+        }
+    }
+};
+
+// The weights of a lane's 16 columns (as Lane16's) from k on.
+template <int P>
+__device__ __forceinline__ void weights(const NormArgs& a, int k, float2 (&w)[8]) {
+    float f[16];
+#pragma unroll
+    for (int h = 0; h < 16 / P; ++h) {
+        const int n = k + 32 * P * h;
+        float* v = f + P * h;
+#pragma unroll
+        for (int i = 0; i < P; ++i) v[i] = 0.f;
+        if (!a.w || n >= a.cols) continue;
+        if (P > 1 && a.w_vec) {  // whole pieces
+            if (!a.w_bf16) {
+#pragma unroll
+                for (int i = 0; i < P; i += 4) {
+                    const float4 q = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(a.w) + n + i));
+                    v[i] = q.x, v[i + 1] = q.y, v[i + 2] = q.z, v[i + 3] = q.w;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < P; i += 4) {
+                    const uint2 q = __ldg(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(a.w) + n + i));
+                    v[i] = bf16_lo(q.x), v[i + 1] = bf16_hi(q.x), v[i + 2] = bf16_lo(q.y), v[i + 3] = bf16_hi(q.y);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < P; ++i)
+                v[i] = a.w_bf16 ? bf16_to_f32(__ldg(static_cast<const uint16_t*>(a.w) + n + i)) : __ldg(static_cast<const float*>(a.w) + n + i);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = make_float2(f[2 * i], f[2 * i + 1]);
 }
-__device__ __forceinline__ void store1(void* p, bool bf16, int64_t at, float v) {
-    if (bf16)
-        static_cast<uint16_t*>(p)[at] = f32_to_bf16(v);
-    else
-        static_cast<float*>(p)[at] = v;
-}
-__device__ __forceinline__ float weight1(const NormArgs& a, int k) {
-    return a.w_bf16 ? bf16_to_f32(__ldg(static_cast<const uint16_t*>(a.w) + k)) : __ldg(static_cast<const float*>(a.w) + k);
+
+constexpr int NO_ROW = -(1 << 30);  // `left` where there is no row
+
+// A lane's 16 values (as Lane16's) to row `row`, columns k on, `left` to the row's end.
+template <int OUT, int P>
+__device__ __forceinline__ void put(const NormArgs& a, int64_t row, int k, int left, float2 (&y)[8], int lane) {
+    if constexpr (OUT == NORM_OUT_F32 || OUT == NORM_OUT_BF16) {
+        constexpr bool BF16 = OUT == NORM_OUT_BF16;
+        uint16_t* b = static_cast<uint16_t*>(a.out) + row * a.ldo + k;
+        float* f = static_cast<float*>(a.out) + row * a.ldo + k;
+#pragma unroll
+        for (int h = 0; h < 16 / P; ++h) {
+            const int c = 32 * P * h;
+            if (c >= left) continue;
+            if (P > 1 && a.out_vec) {
+                const float2* v = y + P / 2 * h;
+                if constexpr (P == 8 && BF16) {
+                    *reinterpret_cast<uint4*>(b + c) = pack8(v);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < P / 2; i += 2) {
+                        if constexpr (BF16)
+                            *reinterpret_cast<uint2*>(b + c + 2 * i) = make_uint2(pack_bf16(v[i].x, v[i].y), pack_bf16(v[i + 1].x, v[i + 1].y));
+                        else
+                            *reinterpret_cast<float4*>(f + c + 2 * i) = make_float4(v[i].x, v[i].y, v[i + 1].x, v[i + 1].y);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    const float2 p = y[(P * h + i) >> 1];
+                    const float v = (P * h + i) & 1 ? p.y : p.x;
+                    if constexpr (BF16)
+                        b[c + i] = f32_to_bf16(v);
+                    else
+                        f[c + i] = v;
+                }
+            }
+        }
+    } else if constexpr (P > 1) {
+        // lanes of rows past the last take part in the shuffles and store nothing
+        constexpr bool Q8 = OUT == NORM_OUT_FP8;
+        constexpr int L128 = 128 / P, LB = Q8 ? L128 : 32 / P;  // lanes of 128 columns, of a block
+        uint8_t* q = static_cast<uint8_t*>(a.out) + row * a.ldo + (Q8 ? k : k / 2);
+        uint8_t* scale = a.scale + (Q8 ? row * a.ld_scale + k / 128 : fp4_scale_word(row, k >> 7, a.ld_scale));
+        const int pad = (int)a.ldo * (Q8 ? 1 : 2) - a.cols;  // columns of zeros after the last
+#pragma unroll
+        for (int h = 0; h < 16 / P; ++h) {
+            const int c = 32 * P * h;
+            float2* f = y + P / 2 * h;
+            if (c >= left) {
+#pragma unroll
+                for (int i = 0; i < P / 2; ++i) f[i] = make_float2(0.f, 0.f);  // (0 times an infinite rstd is NaN)
+            }
+            float m = max_abs3(max_abs(f[0].x, f[0].y), f[1].x, f[1].y);
+            if constexpr (P == 8) m = max_abs3(max_abs3(m, f[2].x, f[2].y), f[3].x, f[3].y);
+#pragma unroll
+            for (int o = LB / 2; o; o >>= 1) m = max_abs(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+            const uint32_t s = Q8 ? fp8_scale_byte(abs_bits(m)) : fp4_scale_byte(abs_bits(m));
+            const float inv = fp8_inverse_scale(s);
+#pragma unroll
+            for (int i = 0; i < P / 2; ++i) f[i] = __fmul2_rn(f[i], make_float2(inv, inv));
+            const bool stores = c < left + pad && left != NO_ROW;
+            if constexpr (Q8) {
+                if (stores) {
+                    const uint32_t lo = fp8_pack4(f[0].x, f[0].y, f[1].x, f[1].y);
+                    if constexpr (P == 8)
+                        *reinterpret_cast<uint2*>(q + c) = make_uint2(lo, fp8_pack4(f[2].x, f[2].y, f[3].x, f[3].y));
+                    else
+                        *reinterpret_cast<uint32_t*>(q + c) = lo;
+                    if (lane % L128 == 0) scale[c / 128] = (uint8_t)s;
+                }
+            } else {
+                uint32_t w = s << (8 * (lane / LB & 3));
+                w |= __shfl_xor_sync(0xFFFFFFFFu, w, LB);
+                w |= __shfl_xor_sync(0xFFFFFFFFu, w, 2 * LB);
+                if (stores) {
+                    if constexpr (P == 8)
+                        *reinterpret_cast<uint32_t*>(q + c / 2) = fp4_pack8(f[0].x, f[0].y, f[1].x, f[1].y, f[2].x, f[2].y, f[3].x, f[3].y);
+                    else
+                        *reinterpret_cast<uint16_t*>(q + c / 2) = (uint16_t)fp4_pack8(f[0].x, f[0].y, f[1].x, f[1].y, 0.f, 0.f, 0.f, 0.f);
+                    if (lane % L128 == 0) *reinterpret_cast<uint32_t*>(scale + c * 4) = w;
+                }
+            }
+        }
+    }
 }
 
 // CH pieces of 512 columns a warp; wpr warps a row (blockDim / 32 a multiple of it).
 template <typename T, int OUT, bool VEC, int CH>
-__global__ void __launch_bounds__(512) rms_norm_kernel(const NormArgs a, const int wpr) {
-    __shared__ float s_part[16];
-    constexpr bool BF16 = sizeof(T) == 2;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % wpr;
-    const int64_t row = (int64_t)blockIdx.x * (blockDim.x / 32 / wpr) + warp / wpr;
-    const bool live = row < a.rows;
+__global__ void __launch_bounds__(512, CH == 1 ? 2 : 1) rms_norm_kernel(const NormArgs a, const int wpr) {
+    constexpr bool AHEAD = VEC && CH == 1;  // elements by cp.async, a row ahead
+    constexpr bool TURN = !VEC && (OUT == NORM_OUT_FP8 || OUT == NORM_OUT_FP4);  // values to aligned pieces for their blocks
+    __shared__ float s_part[2][16];
+    extern __shared__ uint4 s_mem[];  // AHEAD: [x, r][piece][thread]; TURN: [thread][16] values
+    using Lane = Lane16<T, VEC>;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % wpr, per = (int)(blockDim.x >> 5) / wpr;
+    auto first = [&](int c) { return (c * wpr + part) * 512 + lane * Lane::P; };
     pdl_wait();
     pdl_launch_dependents();  // after the wait: the next kernel may read weights that one before this has written
-    // column of element i of piece c
-    auto column = [&](int c, int i) { return (c * wpr + part) * 512 + (VEC ? lane * 16 + i : i * 32 + lane); };
-    float v[CH][16];
-    float sq = 0.f;
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        if constexpr (VEC) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int k = column(c, 8 * h);
-                float* o = v[c] + 8 * h;
-                if (live && k < a.cols) {
-                    load8<T>(a.x, row * a.ldx + k, o);
-                    if (a.r) {
-                        float r[8];
-                        load8<T>(a.r, row * a.ldr + k, r);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) o[i] += r[i];
-                    }
-                    if constexpr (BF16) unpack8(pack8(o), o);  // the sum as it is stored
-                    if (a.sum) store8(a.sum, BF16, row * a.lds + k, o);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) o[i] = 0.f;
-                }
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int k = column(c, i);
-                float s = 0.f;
-                if (live && k < a.cols) {
-                    s = load1<T>(a.x, row * a.ldx + k);
-                    if (a.r) s += load1<T>(a.r, row * a.ldr + k);
-                    if constexpr (BF16) s = bf16_to_f32(f32_to_bf16(s));
-                    if (a.sum) store1(a.sum, BF16, row * a.lds + k, s);
-                }
-                v[c][i] = s;
-            }
+    const uint32_t pitch = 16 * blockDim.x, tensor = Lane::N * pitch, own = smem_u32(s_mem) + 16 * threadIdx.x;
+    const int64_t step = (int64_t)gridDim.x * per, row0 = (int64_t)blockIdx.x * per + warp / wpr;
+    // columns from k to the end of row `row`; none for a row that is not there
+    auto left_of = [&](int64_t row, int k) { return row < a.rows ? a.cols - k : NO_ROW; };
+    auto ask = [&](int64_t row) {
+        if constexpr (AHEAD) {
+            const int left = left_of(row, first(0));
+            Lane::ask(own, pitch, static_cast<const T*>(a.x) + row * a.ldx + first(0), left);
+            if (a.r) Lane::ask(own + tensor, pitch, static_cast<const T*>(a.r) + row * a.ldr + first(0), left);
+            cp_async_commit();
         }
+    };
+    float2 w[8];
+    ask(row0);
+    if constexpr (CH == 1) weights<Lane::P>(a, first(0), w);
+    int turn = 0;
+    for (int64_t row = row0; row - warp / wpr < a.rows; row += step, turn ^= 1) {
+        float2 v[CH][8], sq = make_float2(0.f, 0.f);
+        if constexpr (AHEAD) cp_async_wait<0>();
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sq = fmaf(v[c][i], v[c][i], sq);
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) sq += __shfl_xor_sync(0xFFFFFFFFu, sq, o);
-    if (wpr > 1) {
-        if (lane == 0) s_part[warp] = sq;
-        __syncthreads();
-        sq = 0.f;
-        for (int i = warp - part; i < warp - part + wpr; ++i) sq += s_part[i];
-    }
-    const float rstd = 1.f / sqrtf(sq / (float)a.cols + a.eps);
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        float y[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) y[i] = v[c][i] * rstd;
-        if (a.w) {
-            if (VEC && a.w_vec) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int k = column(c, 8 * h);
-                    if (k >= a.cols) continue;
-                    float w[8];
-                    if (a.w_bf16)
-                        load8<uint16_t>(a.w, k, w);
-                    else
-                        load8<float>(a.w, k, w);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) y[8 * h + i] *= w[i];
-                }
+        for (int c = 0; c < CH; ++c) {
+            const int left = left_of(row, first(c));
+            Lane x, r;
+            if constexpr (AHEAD) {
+                x.take(own, pitch, a.cols - first(0));
+                if (a.r) r.take(own + tensor, pitch, a.cols - first(0));
             } else {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int k = column(c, i);
-                    if (k < a.cols) y[i] *= weight1(a, k);
-                }
+                x.load(static_cast<const T*>(a.x) + row * a.ldx + first(c), left);
+                if (a.r) r.load(static_cast<const T*>(a.r) + row * a.ldr + first(c), left);
             }
+            if (a.r) x.add(r);
+            ask(row + step);
+            if (a.sum) x.store(static_cast<T*>(a.sum) + row * a.lds + first(c), left);
+            x.values(v[c]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sq = __ffma2_rn(v[c][i], v[c][i], sq);
         }
-        // rows past the last and columns past cols: nothing, or zeros in a block's padding (0 times an infinite rstd: NaN)
-        if (!(VEC && OUT == NORM_OUT_DTYPE)) {
+        float ss = sq.x + sq.y;
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (column(c, i) >= a.cols) y[i] = 0.f;
+        for (int o = 16; o; o >>= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
+        if (wpr > 1) {  // in two buffers by turn: a warp's reads of one precede its next barrier
+            if (lane == 0) s_part[turn][warp] = ss;
+            __syncthreads();
+            ss = 0.f;
+            for (int i = warp - part; i < warp - part + wpr; ++i) ss += s_part[turn][i];
         }
-        if constexpr (OUT == NORM_OUT_DTYPE) {
-            if (!live) continue;
-            if (VEC && a.out_vec) {
+        const float rstd = 1.f / sqrtf(ss / (float)a.cols + a.eps);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int k = column(c, 8 * h);
-                    if (k < a.cols) store8(a.out, a.out_bf16, row * a.ldo + k, y + 8 * h);
-                }
-            } else {
+        for (int c = 0; c < CH; ++c) {
+            if constexpr (CH > 1) weights<Lane::P>(a, first(c), w);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int k = column(c, i);
-                    if (k < a.cols) store1(a.out, a.out_bf16, row * a.ldo + k, y[i]);
-                }
+            for (int i = 0; i < 8; ++i) {
+                v[c][i] = __fmul2_rn(v[c][i], make_float2(rstd, rstd));
+                if (a.w) v[c][i] = __fmul2_rn(v[c][i], w[i]);
             }
-        } else if constexpr (VEC) {
-            const int k = column(c, 0);  // of 16
-            float m = 0.f;
+            if constexpr (TURN) {  // element i of lane l is column 32 i + l; lane l then has eight from 8 l and from 256 + 8 l on
+                float* t = reinterpret_cast<float*>(s_mem) + warp * 512;
+                const int k = first(c) - lane + 8 * lane;
+                __syncwarp();
 #pragma unroll
-            for (int i = 0; i < 16; i += 2) m = max_abs3(m, y[i], y[i + 1]);
+                for (int i = 0; i < 16; ++i) t[32 * i + lane] = first(c) + 32 * i < a.cols ? (i & 1 ? v[c][i >> 1].y : v[c][i >> 1].x) : 0.f;
+                __syncwarp();
 #pragma unroll
-            for (int o = OUT == NORM_OUT_FP8 ? 4 : 1; o; o >>= 1) m = max_abs(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-            const uint32_t s = OUT == NORM_OUT_FP8 ? fp8_scale_byte(abs_bits(m)) : fp4_scale_byte(abs_bits(m));
-            const float inv = fp8_inverse_scale(s);
-            if constexpr (OUT == NORM_OUT_FP8) {
-                uint32_t o[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] = fp8_pack4(y[4 * i] * inv, y[4 * i + 1] * inv, y[4 * i + 2] * inv, y[4 * i + 3] * inv);
-                if (live && k < a.ldo) {
-                    *reinterpret_cast<uint4*>(static_cast<uint8_t*>(a.out) + row * a.ldo + k) = make_uint4(o[0], o[1], o[2], o[3]);
-                    if ((lane & 7) == 0) a.scale[row * a.ld_scale + k / 128] = (uint8_t)s;
+                for (int i = 0; i < 4; ++i) {
+                    const float4 q = *reinterpret_cast<const float4*>(t + 256 * (i >> 1) + 8 * lane + 4 * (i & 1));
+                    v[c][2 * i] = make_float2(q.x, q.y), v[c][2 * i + 1] = make_float2(q.z, q.w);
                 }
+                put<OUT, 8>(a, row, k, left_of(row, k), v[c], lane);
             } else {
-                const uint32_t lo = fp4_pack8_scaled(y, make_float2(inv, inv)), hi = fp4_pack8_scaled(y + 8, make_float2(inv, inv));
-                uint32_t w = s << (8 * (lane >> 1 & 3));
-                w |= __shfl_xor_sync(0xFFFFFFFFu, w, 2);
-                w |= __shfl_xor_sync(0xFFFFFFFFu, w, 4);
-                if (live && k / 2 < a.ldo) {
-                    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.out) + row * a.ldo + k / 2) = make_uint2(lo, hi);
-                    if ((lane & 7) == 0) *reinterpret_cast<uint32_t*>(a.scale + fp4_scale_word(row, k >> 7, a.ld_scale)) = w;
-                }
-            }
-        } else {
-#pragma unroll
-            for (int b = 0; b < 4; ++b) {  // 128 columns: four elements a lane
-                const int k = column(c, 4 * b);
-                uint32_t m[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) m[i] = abs_bits(y[4 * b + i]);
-                if constexpr (OUT == NORM_OUT_FP8) {
-                    const uint32_t s = fp8_scale_byte(__reduce_max_sync(0xFFFFFFFFu, max(max(m[0], m[1]), max(m[2], m[3]))));
-                    const float inv = fp8_inverse_scale(s);
-                    if (live && k - lane < a.cols) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            static_cast<uint8_t*>(a.out)[row * a.ldo + k + 32 * i] = (uint8_t)fp8_pack2(y[4 * b + i] * inv, 0.f);
-                        if (lane == 0) a.scale[row * a.ld_scale + (k - lane) / 128] = (uint8_t)s;
-                    }
-                } else {
-                    uint32_t word = 0;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t s = fp4_scale_byte(__reduce_max_sync(0xFFFFFFFFu, m[i]));
-                        word |= s << (8 * i);
-                        const float f = y[4 * b + i] * fp8_inverse_scale(s), g = __shfl_down_sync(0xFFFFFFFFu, f, 1);
-                        const int at = (k + 32 * i) / 2;
-                        if (live && (lane & 1) == 0 && at < a.ldo)
-                            static_cast<uint8_t*>(a.out)[row * a.ldo + at] = (uint8_t)fp4_pack8(f, g, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f);
-                    }
-                    if (live && lane == 0 && k < a.cols) *reinterpret_cast<uint32_t*>(a.scale + fp4_scale_word(row, k >> 7, a.ld_scale)) = word;
-                }
+                put<OUT, Lane::P>(a, row, first(c), left_of(row, first(c)), v[c], lane);
             }
         }
     }
 }
 
-template <typename T, int OUT, bool VEC>
-cudaError_t launch_ch(const NormArgs& a, cudaStream_t s) {
-    int wpr = 1, ch = 1;
-    while (wpr < 16 && wpr * 512 < a.cols) wpr *= 2;
-    while (wpr * ch * 512 < a.cols) ch *= 2;
-    const int warps = wpr < 8 ? 8 : wpr, rows = warps / wpr;
+constexpr int NORM_THREADS = 1024;  // an SM
+
+template <typename T, int OUT, bool VEC, int CH>
+cudaError_t launch_ch(const NormArgs& a, int wpr, int num_sms, cudaStream_t s) {
+    const int per = wpr <= 8 ? 8 / wpr : 1, threads = 32 * wpr * per;  // rows at a time
+    int ctas = NORM_THREADS / threads;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((a.rows + rows - 1) / rows));
-    cfg.blockDim = dim3(32 * warps);
+    const bool ahead = VEC && CH == 1, turn = !VEC && (OUT == NORM_OUT_FP8 || OUT == NORM_OUT_FP4);
+    if (ahead || turn) {
+        cfg.dynamicSmemBytes = threads * (turn ? 64 : (a.r ? 32 : 16) * (int)sizeof(T));
+        const cudaError_t e = smem_attr_once((const void*)rms_norm_kernel<T, OUT, VEC, CH>, 512 * (turn ? 64 : 32 * (int)sizeof(T)));
+        if (e != cudaSuccess) return e;
+    }
+    const int64_t want = (a.rows + per - 1) / per, most = (int64_t)num_sms * (ctas < 1 ? 1 : ctas);
+    cfg.gridDim = dim3((unsigned)(want < most ? want : most));
+    cfg.blockDim = dim3(threads);
     cfg.stream = s;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    return ch == 1   ? cudaLaunchKernelEx(&cfg, rms_norm_kernel<T, OUT, VEC, 1>, a, wpr)
-           : ch == 2 ? cudaLaunchKernelEx(&cfg, rms_norm_kernel<T, OUT, VEC, 2>, a, wpr)
-                     : cudaLaunchKernelEx(&cfg, rms_norm_kernel<T, OUT, VEC, 4>, a, wpr);
+    return cudaLaunchKernelEx(&cfg, rms_norm_kernel<T, OUT, VEC, CH>, a, wpr);
+}
+template <typename T, int OUT, bool VEC>
+cudaError_t launch_norm(const NormArgs& a, int num_sms, cudaStream_t s) {
+    const int pieces = (a.cols + 511) / 512;
+    return pieces <= 16 ? launch_ch<T, OUT, VEC, 1>(a, pieces, num_sms, s) : launch_ch<T, OUT, VEC, 4>(a, (pieces + 3) / 4, num_sms, s);
 }
 
 bool rows_vec(const void* p, int64_t ld, int esz) { return !p || ((reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * esz % 16 == 0); }
@@ -305,9 +408,11 @@ template <int OUT>
 int run(const clearmoe_norm* n, const NormArgs& a, void* stream) {
     const int esz = n->dtype == CLEARMOE_BF16 ? 2 : 4;
     const bool vec = n->cols % 8 == 0 && rows_vec(n->x, n->ldx, esz) && rows_vec(n->residual, n->ldr, esz) && rows_vec(n->sum, n->lds, esz);
+    const int sms = current_device_sms();
+    if (sms <= 0) return CLEARMOE_ECUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = esz == 2 ? (vec ? launch_ch<uint16_t, OUT, true>(a, s) : launch_ch<uint16_t, OUT, false>(a, s))
-                                   : (vec ? launch_ch<float, OUT, true>(a, s) : launch_ch<float, OUT, false>(a, s));
+    const cudaError_t e = esz == 2 ? (vec ? launch_norm<uint16_t, OUT, true>(a, sms, s) : launch_norm<uint16_t, OUT, false>(a, sms, s))
+                                   : (vec ? launch_norm<float, OUT, true>(a, sms, s) : launch_norm<float, OUT, false>(a, sms, s));
     if (e == cudaSuccess) return CLEARMOE_OK;
     (void)cudaGetLastError();
     return CLEARMOE_ECUDA;
@@ -328,10 +433,9 @@ int clearmoe_rms_norm(const clearmoe_norm* n, void* out, int32_t out_dtype, int6
     if ((out == n->x && (out_dtype != n->dtype || ldo != n->ldx)) || (out == n->residual && (out_dtype != n->dtype || ldo != n->ldr)))
         return CLEARMOE_EINVAL;
     a.out = out;
-    a.out_bf16 = out_dtype == CLEARMOE_BF16;
     a.ldo = ldo;
-    a.out_vec = cm::rows_vec(out, ldo, a.out_bf16 ? 2 : 4);
-    return cm::run<cm::NORM_OUT_DTYPE>(n, a, stream);
+    a.out_vec = cm::rows_vec(out, ldo, out_dtype == CLEARMOE_BF16 ? 2 : 4);
+    return out_dtype == CLEARMOE_BF16 ? cm::run<cm::NORM_OUT_BF16>(n, a, stream) : cm::run<cm::NORM_OUT_F32>(n, a, stream);
 }
 
 int clearmoe_rms_norm_fp8(const clearmoe_norm* n, const clearmoe_fp8* out, void* stream) {
