@@ -182,6 +182,9 @@ def _bind_calls():
     m.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in
              (L.clearmoe_fp8_quantize_rows, L.clearmoe_fp8_gemm, L.clearmoe_fp8_gemm_fp8, L.clearmoe_ffn_forward_few,
               L.clearmoe_ffn_forward_fp8)))
+    m.bind_fp4(*(ctypes.cast(f, ctypes.c_void_p).value for f in
+                 (L.clearmoe_fp4_quantize, L.clearmoe_fp4_gemm, L.clearmoe_fp4_gemm_fp4, L.clearmoe_rms_norm, L.clearmoe_rms_norm_fp8,
+                  L.clearmoe_rms_norm_fp4)))
     try:
         import torch
         m.bind_torch(torch.bfloat16, torch.float32, torch.int32, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
@@ -676,6 +679,12 @@ def clearmoe_fp4_quantize(x, out: Fp4Matrix, gather=None, stream=None) -> None:
     """x [rows x cols] (bf16 or fp32, any row pitch) to out in 4-bit blocks, weights and activations alike; gather: int32
     source rows (one outside x gives a row of NaN)."""
     o = _fp4(out, "out")
+    if gather is None:
+        code = (_calls or _bind_calls()).fp4_quantize_t(x, out.rows, out.cols, out.addr, stream)
+        if code is not None:
+            if code:
+                raise ClearMoEError(code, "clearmoe_fp4_quantize")
+            return
     p, dt, ld = _matrix(x, out.rows if gather is None else None, out.cols, "x")
     _check(lib().clearmoe_fp4_quantize(p, x.shape[0], dt, ld, _int32(gather, out.rows, "gather"), o, _stream(stream)),
            "clearmoe_fp4_quantize")
@@ -691,9 +700,14 @@ def clearmoe_fp4_dequantize(m: Fp4Matrix, out, stream=None) -> None:
 def clearmoe_fp4_gemm(A: Fp4Matrix, W: Fp4Matrix, out, bias=None, act: int = ACT_NONE, status=None, stream=None) -> None:
     """out = act(A W^T + bias). out: a [M x N] bf16 or fp32 tensor of any row pitch, or an Fp4Matrix (the result
     quantised, clearmoe_fp4_gemm_fp4)."""
-    a, w = _fp4(A, "A"), _fp4(W, "W")
+    a, w, blocks = _fp4(A, "A"), _fp4(W, "W"), isinstance(out, Fp4Matrix)
+    code = (_calls or _bind_calls()).fp4_gemm_t(A.addr, W.addr, A.rows, W.rows, act, bias, status, out.addr if blocks else out, stream)
+    if code is not None:
+        if code:
+            raise ClearMoEError(code, "clearmoe_fp4_gemm_fp4" if blocks else "clearmoe_fp4_gemm")
+        return
     epi = _epilogue(bias, act, status, W.rows)
-    if isinstance(out, Fp4Matrix):
+    if blocks:
         _check(lib().clearmoe_fp4_gemm_fp4(a, w, epi, out.ref, _stream(stream)), "clearmoe_fp4_gemm_fp4")
         return
     p, dt, ld = _matrix(out, A.rows, W.rows, "out")
@@ -725,6 +739,14 @@ def clearmoe_rms_norm(x, out, residual=None, sum_out=None, weight=None, eps: flo
     """s = x + residual, rounded to x's dtype, to sum_out; s weight / sqrt(mean(s^2) + eps) to out: a [rows x cols] bf16
     or fp32 tensor, or an Fp8Matrix of rows or an Fp4Matrix (the norm quantised, clearmoe_rms_norm_fp8, _fp4). x,
     residual and sum_out are of one dtype, of any row pitch; sum_out may be x or residual."""
+    bits = 4 if isinstance(out, Fp4Matrix) else 8 if isinstance(out, Fp8Matrix) else 0
+    if bits == 8 and out.weight:
+        _refuse_kind("out", False)
+    code = (_calls or _bind_calls()).rms_norm_t(x, residual, sum_out, weight, eps, bits, out.addr if bits else out, stream)
+    if code is not None:
+        if code:
+            raise ClearMoEError(code, "clearmoe_rms_norm" + ("", "_fp4", "_fp8")[bits // 4])
+        return
     if len(x.shape) != 2:
         raise ValueError(f"x must be a matrix, got {tuple(x.shape)}")
     rows, cols = x.shape
@@ -744,11 +766,9 @@ def clearmoe_rms_norm(x, out, residual=None, sum_out=None, weight=None, eps: flo
             raise ValueError(f"weight must have {cols} elements, got {weight.numel()}")
         n.weight, n.weight_dtype = _ptr(weight), _dtype(weight)
     ref = ctypes.byref(n)
-    if isinstance(out, Fp4Matrix):
+    if bits == 4:
         _check(lib().clearmoe_rms_norm_fp4(ref, out.ref, _stream(stream)), "clearmoe_rms_norm_fp4")
-    elif isinstance(out, Fp8Matrix):
-        if out.weight:
-            _refuse_kind("out", False)
+    elif bits == 8:
         _check(lib().clearmoe_rms_norm_fp8(ref, out.ref, _stream(stream)), "clearmoe_rms_norm_fp8")
     else:
         p, dt, ld = _matrix(out, rows, cols, "out")

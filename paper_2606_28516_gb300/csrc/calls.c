@@ -1,4 +1,4 @@
-/* The calls of the 8-bit and few-token operators whose time the host bounds. ctypes took 0.6 us for the arguments of such a
+/* The calls of the 4-bit, 8-bit, norm and few-token operators whose time the host bounds. ctypes took 0.6 us for the arguments of such a
  * call and as much again for the epilogue's structure, and the looks at tensors in Python as much as that, of 4 to 6 us
  * for the whole call.
  *
@@ -275,10 +275,104 @@ static PyObject* ffn_fp8_t(PyObject* self, PyObject* const* args, Py_ssize_t n) 
     return ffn_t(args, n, g_fp8);
 }
 
+/* ---- 4-bit blocks and the norm ---- */
+static int (*g_fp4_quantize)(const void*, int64_t, int32_t, int64_t, const int32_t*, const clearmoe_fp4*, void*);
+static int (*g_fp4_gemm)(const clearmoe_fp4*, const clearmoe_fp4*, const clearmoe_fp8_epilogue*, void*, int32_t, int64_t, void*);
+static int (*g_fp4_gemm_fp4)(const clearmoe_fp4*, const clearmoe_fp4*, const clearmoe_fp8_epilogue*, const clearmoe_fp4*, void*);
+static int (*g_norm)(const clearmoe_norm*, void*, int32_t, int64_t, void*);
+static int (*g_norm_fp8)(const clearmoe_norm*, const clearmoe_fp8*, void*);
+static int (*g_norm_fp4)(const clearmoe_norm*, const clearmoe_fp4*, void*);
+
+static PyObject* bind_fp4(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    int64_t v[6];
+    (void)self;
+    if (!integers(args, n, 6, v)) return NULL;
+    *(void**)&g_fp4_quantize = PTR(0);
+    *(void**)&g_fp4_gemm = PTR(1);
+    *(void**)&g_fp4_gemm_fp4 = PTR(2);
+    *(void**)&g_norm = PTR(3);
+    *(void**)&g_norm_fp8 = PTR(4);
+    *(void**)&g_norm_fp4 = PTR(5);
+    Py_RETURN_NONE;
+}
+
+/* x, rows, cols, out, stream */
+static PyObject* fp4_quantize_t(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    int64_t v[3], x, ld, s;
+    int32_t dt;
+    int rc;
+    (void)self;
+    if (n != 5) return PyErr_Format(PyExc_TypeError, "5 arguments expected, got %zd", n);
+    if (!integers(args + 1, 3, 3, v)) return NULL;
+    if (!stream_of(args[4], &s) || !matrix(args[0], v[0], v[1], &x, &dt, &ld)) Py_RETURN_NONE;
+    Py_BEGIN_ALLOW_THREADS
+    rc = g_fp4_quantize(AT(x), v[0], dt, ld, NULL, PTR(2), AT(s));
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+/* A, W, rows, cols, act, bias, status, out (a tensor, or the address of 4-bit blocks), stream */
+static PyObject* fp4_gemm_t(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    int64_t v[5], bias, status, out, ld, s;
+    int32_t bias_dt, dt;
+    int rc;
+    (void)self;
+    if (n != 9) return PyErr_Format(PyExc_TypeError, "9 arguments expected, got %zd", n);
+    if (!integers(args, 5, 5, v)) return NULL;
+    if (!stream_of(args[8], &s) || !bias_of(args[5], v[3], &bias, &bias_dt) || !status_of(args[6], &status)) Py_RETURN_NONE;
+    const clearmoe_fp8_epilogue epi = {AT(bias), bias_dt, (int32_t)v[4], AT(status)};
+    const int blocks = PyLong_Check(args[7]);
+    if (blocks ? !integers(args + 7, 1, 1, &out) : !matrix(args[7], v[2], v[3], &out, &dt, &ld)) {
+        if (blocks) return NULL;
+        Py_RETURN_NONE;
+    }
+    Py_BEGIN_ALLOW_THREADS
+    rc = blocks ? g_fp4_gemm_fp4(PTR(0), PTR(1), &epi, AT(out), AT(s)) : g_fp4_gemm(PTR(0), PTR(1), &epi, AT(out), dt, ld, AT(s));
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+/* x, residual, sum, weight (tensors or None), eps, bits (0: a tensor, 8 or 4: the address of blocks), out, stream */
+static PyObject* rms_norm_t(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    int64_t shape[2], x, r = 0, sum = 0, w, out, ldo, s;
+    int64_t bits;
+    int32_t dt, other, out_dt;
+    clearmoe_norm a = {0};
+    int rc;
+    (void)self;
+    if (n != 8) return PyErr_Format(PyExc_TypeError, "8 arguments expected, got %zd", n);
+    if (!integers(args + 5, 1, 1, &bits)) return NULL;
+    a.eps = (float)PyFloat_AsDouble(args[4]);
+    if (PyErr_Occurred()) return NULL;
+    if (!stream_of(args[7], &s) || !pair(PyObject_GetAttr(args[0], s_shape), shape) || !matrix(args[0], shape[0], shape[1], &x, &dt, &a.ldx) ||
+        (args[1] != Py_None && (!matrix(args[1], shape[0], shape[1], &r, &other, &a.ldr) || other != dt)) ||
+        (args[2] != Py_None && (!matrix(args[2], shape[0], shape[1], &sum, &other, &a.lds) || other != dt)) ||
+        !bias_of(args[3], shape[1], &w, &a.weight_dtype))
+        Py_RETURN_NONE;
+    if (bits) {
+        if (!integers(args + 6, 1, 1, &out)) return NULL;
+    } else if (!matrix(args[6], shape[0], shape[1], &out, &out_dt, &ldo)) {
+        Py_RETURN_NONE;
+    }
+    a.x = AT(x);
+    a.residual = AT(r);
+    a.sum = AT(sum);
+    a.weight = AT(w);
+    a.rows = shape[0];
+    a.cols = shape[1];
+    a.dtype = dt;
+    Py_BEGIN_ALLOW_THREADS
+    rc = bits == 8 ? g_norm_fp8(&a, AT(out), AT(s)) : bits == 4 ? g_norm_fp4(&a, AT(out), AT(s)) : g_norm(&a, AT(out), out_dt, ldo, AT(s));
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {METHOD(bind),      METHOD(bind_torch),      METHOD(quantize_rows), METHOD(gemm),
                                 METHOD(gemm_fp8),  METHOD(ffn_few),         METHOD(ffn_fp8),       METHOD(quantize_rows_t),
-                                METHOD(gemm_t),    METHOD(ffn_few_t),       METHOD(ffn_fp8_t),     {NULL, NULL, 0, NULL}};
+                                METHOD(gemm_t),    METHOD(ffn_few_t),       METHOD(ffn_fp8_t),
+                                METHOD(bind_fp4),  METHOD(fp4_quantize_t),  METHOD(fp4_gemm_t),    METHOD(rms_norm_t),
+                                {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", NULL, -1, methods, NULL, NULL, NULL, NULL};
 PyMODINIT_FUNC PyInit__calls(void) {
     PyObject** names[] = {&s_is_cuda, &s_shape, &s_stride, &s_data_ptr, &s_dtype, &s_is_contiguous, &s_numel, &s_cuda_stream};

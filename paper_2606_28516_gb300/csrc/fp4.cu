@@ -4,84 +4,130 @@
 #include "common.cuh"
 #include "fp4.cuh"
 #include "internal.h"
+#include "lane16.cuh"
 
 namespace cm {
 
 namespace {
 
-// Eight lanes take 128 columns of a row (a word of four scale bytes), 16 consecutive ones a lane, so that a block is two
-// lanes'. A warp's four groups of lanes take rows 32 apart, whose words lie side by side, and a CTA's eight warps eight
-// consecutive rows of each: 128 consecutive bytes of scales a CTA.
+// Eight lanes take 128 columns of a row (a word of four scale bytes), 16 a lane. A warp's four groups of lanes take rows 32
+// apart, whose words lie side by side, and a CTA's eight warps eight consecutive rows of each: 128 consecutive bytes of
+// scales a CTA. Bound by HBM: each element is read once and written once as half a byte. Aligned rows come through shared
+// memory, each lane's next elements on their way while it converts these: what is on its way to registers lies in L1
+// meanwhile, and beside a product, whose shared memory leaves L1 28 KB, that held the loads back (16,384 x 4,096 bf16 and
+// its product: 123 us where the two take 105). Other rows: a warp reads 32 consecutive elements at a time, and turns them to
+// the same order in shared memory.
 constexpr int Q4_THREADS = 256;
 constexpr int Q4_CTAS = 32;  // an SM, at the most
 
-template <typename T, bool VEC>
-__device__ __forceinline__ void load16(const T* row, int64_t k, int64_t K, bool live, float (&v)[16]) {
-    if (VEC) {
+// A lane's 16 values (as Lane16's of P columns, eight lanes a row) from column k of row `row` on to codes and scales. live:
+// there is such a row; inside: it is one of x's.
+template <int P>
+__device__ __forceinline__ void quantize16(const Quant4Args& a, float2 (&v)[8], int64_t row, int tile, int l8, bool live, bool inside) {
+    uint8_t* q = a.q + row * a.ldq + (int64_t)tile * 64 + l8 * (P / 2);
+    const int64_t bytes = a.ldq - (int64_t)tile * 64 - l8 * (P / 2);  // to the row's end
+    uint32_t word = 0;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const bool in = live && k + 8 * h < K;
-            if (sizeof(T) == 2) {
-                uint4 u = make_uint4(0, 0, 0, 0);
-                if (in) u = __ldcg(reinterpret_cast<const uint4*>(row + k) + h);
-                const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    for (int h = 0; h < 16 / P; ++h) {
+        float2* f = v + P / 2 * h;
+        float m = max_abs3(max_abs(f[0].x, f[0].y), f[1].x, f[1].y);
+        if constexpr (P == 8) m = max_abs3(max_abs3(m, f[2].x, f[2].y), f[3].x, f[3].y);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[8 * h + 2 * i] = bf16_lo(w[i]), v[8 * h + 2 * i + 1] = bf16_hi(w[i]);
-            } else {
-                float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
-                if (in) {
-                    a = __ldcg(reinterpret_cast<const float4*>(row + k) + 2 * h);
-                    b = __ldcg(reinterpret_cast<const float4*>(row + k) + 2 * h + 1);
-                }
-                float* o = v + 8 * h;
-                o[0] = a.x, o[1] = a.y, o[2] = a.z, o[3] = a.w, o[4] = b.x, o[5] = b.y, o[6] = b.z, o[7] = b.w;
-            }
-        }
-    } else {
+        for (int o = 16 / P; o; o >>= 1) m = max_abs(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+        const uint32_t s = inside ? fp4_scale_byte(abs_bits(m)) : 255u;
+        const float inv = fp8_inverse_scale(s);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            v[i] = 0.f;
-            if (live && k + i < K)
-                v[i] = sizeof(T) == 2 ? bf16_to_f32(__ldg(reinterpret_cast<const uint16_t*>(row) + k + i))
-                                      : __ldg(reinterpret_cast<const float*>(row) + k + i);
+        for (int i = 0; i < P / 2; ++i) f[i] = __fmul2_rn(f[i], make_float2(inv, inv));
+        word |= s << (P == 8 ? 16 * h + 8 * (l8 >> 2) : 8 * h);
+        if (live && 4 * P * h < bytes) {
+            if constexpr (P == 8)
+                *reinterpret_cast<uint32_t*>(q + 4 * P * h) = fp4_pack8(f[0].x, f[0].y, f[1].x, f[1].y, f[2].x, f[2].y, f[3].x, f[3].y);
+            else
+                *reinterpret_cast<uint16_t*>(q + 4 * P * h) = (uint16_t)fp4_pack8(f[0].x, f[0].y, f[1].x, f[1].y, 0.f, 0.f, 0.f, 0.f);
         }
     }
+    if constexpr (P == 8) word |= __shfl_xor_sync(0xFFFFFFFFu, word, 4);
+    if (live && l8 == 0) *reinterpret_cast<uint32_t*>(a.scale + fp4_scale_word(row, tile, a.tiles)) = word;
 }
 
 template <typename T, bool VEC, bool GATHER>
 __global__ void __launch_bounds__(Q4_THREADS) fp4_quantize_kernel(const Quant4Args a) {
+    using Lane = Lane16<T, VEC, 8>;
+    __shared__ __align__(16) unsigned char s_mem[VEC ? Lane::N * 16 * Q4_THREADS : Q4_THREADS / 32 * 4 * 132 * 4];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l8 = lane & 7;
-    const int64_t groups = (a.rows + 127) / 128 * 4;  // of 8 rows and those 32, 64 and 96 after them
+    const int64_t items = (a.rows + 127) / 128 * 4 * a.tiles;  // 8 rows and those 32, 64 and 96 after them, 128 columns
+    const uint32_t own = smem_u32(s_mem) + 16 * threadIdx.x, pitch = 16 * Q4_THREADS;
     pdl_wait();
     pdl_launch_dependents();  // after the wait: the next kernel may read weights that one before this has written
-    for (int64_t i = blockIdx.x; i < groups * a.tiles; i += gridDim.x) {
+    int64_t row = 0, src = 0;
+    int tile = 0;
+    bool live = false, inside = true;
+    auto place = [&](int64_t i) {
         const int64_t group = i / a.tiles;
-        const int tile = (int)(i - group * a.tiles);
-        const int64_t row = (group >> 2) * 128 + (lane >> 3) * 32 + (group & 3) * 8 + warp;
-        const bool live = row < a.rows;
-        int64_t src = row;
-        bool inside = true;
+        tile = (int)(i - group * a.tiles);
+        row = (group >> 2) * 128 + (lane >> 3) * 32 + (group & 3) * 8 + warp;
+        live = i < items && row < a.rows;
+        src = row;
+        inside = true;
         if (GATHER && live) {
             src = __ldcg(a.gather + row);
             inside = (uint64_t)src < (uint64_t)a.src_rows;
         }
-        const int64_t k = (int64_t)tile * 128 + l8 * 16;
-        float v[16];
-        load16<T, VEC>(static_cast<const T*>(a.x) + src * a.ld, k, a.K, live && inside, v);
-        float m = 0.f;
+    };
+    // columns from the lane's first one to the end of its row; none for one that is not there
+    auto left = [&]() { return live && inside ? (int)(a.K - (int64_t)tile * 128 - l8 * Lane::P) : -(1 << 30); };
+    auto ask = [&]() {
+        if constexpr (VEC) {
+            Lane::ask(own, pitch, static_cast<const T*>(a.x) + src * a.ld + (int64_t)tile * 128 + l8 * Lane::P, left());
+            cp_async_commit();
+        }
+    };
+    int64_t i = blockIdx.x;
+    place(i);
+    ask();
+    for (; i < items; i += gridDim.x) {
+        float2 v[8];
+        const int64_t r = row;
+        const int t = tile;
+        const bool l = live, in = inside;
+        if constexpr (VEC) {
+            Lane x;
+            cp_async_wait<0>();
+            x.take(own, pitch, left());
+            x.values(v);
+            place(i + gridDim.x);
+            ask();
+            quantize16<Lane::P>(a, v, r, t, l8, l, in);
+        } else {
+            float* s = reinterpret_cast<float*>(s_mem) + warp * 4 * 132;  // [row of the warp's four][column]
+            const T* p = static_cast<const T*>(a.x) + src * a.ld + (int64_t)tile * 128 + lane;
+            const int n = live && inside ? (int)min((int64_t)128, a.K - (int64_t)tile * 128) : 0;
+            T e[4][4];
 #pragma unroll
-        for (int c = 0; c < 16; c += 2) m = max_abs3(m, v[c], v[c + 1]);
-        m = max_abs(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-        const uint32_t s = inside ? fp4_scale_byte(abs_bits(m)) : 255u;
-        const float inv = fp8_inverse_scale(s);
-        const uint32_t lo = fp4_pack8_scaled(v, make_float2(inv, inv)), hi = fp4_pack8_scaled(v + 8, make_float2(inv, inv));
-        uint32_t w = s << (8 * (l8 >> 1));  // the word of four blocks
-        w |= __shfl_xor_sync(0xFFFFFFFFu, w, 2);
-        w |= __shfl_xor_sync(0xFFFFFFFFu, w, 4);
-        if (live) {
-            if ((int64_t)tile * 64 + l8 * 8 < a.ldq)
-                *reinterpret_cast<uint2*>(a.q + row * a.ldq + (int64_t)tile * 64 + l8 * 8) = make_uint2(lo, hi);
-            if (l8 == 0) *reinterpret_cast<uint32_t*>(a.scale + fp4_scale_word(row, tile, a.tiles)) = w;
+            for (int j = 0; j < 4; ++j) {
+                const T* pj = reinterpret_cast<const T*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(p - lane), 8 * j)) + lane;
+                const int nj = __shfl_sync(0xFFFFFFFFu, n, 8 * j);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) e[j][c] = lane + 32 * c < nj ? __ldcg(pj + 32 * c) : T(0);
+            }
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    if constexpr (sizeof(T) == 2)
+                        s[132 * j + 32 * c + lane] = bf16_to_f32(e[j][c]);
+                    else
+                        s[132 * j + 32 * c + lane] = e[j][c];
+                }
+            __syncwarp();
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                const float4 f = *reinterpret_cast<const float4*>(s + 132 * (lane >> 3) + 64 * (h >> 1) + 8 * l8 + 4 * (h & 1));
+                v[2 * h] = make_float2(f.x, f.y), v[2 * h + 1] = make_float2(f.z, f.w);
+            }
+            place(i + gridDim.x);
+            quantize16<8>(a, v, r, t, l8, l, in);
         }
     }
 }

@@ -68,16 +68,25 @@ struct Quant4Args {
 cudaError_t launch_fp4_quantize(const Quant4Args& a, int dtype, int num_sms, cudaStream_t s);
 
 constexpr int FP4_OUT_FP4 = 3;  // of out_kind, beside FP8_OUT_F32 and FP8_OUT_BF16
+constexpr int FP4_OUT_BF16_BULK = 4;  // a kernel's: bf16 by bulk copies
 // tmA, tmB: bytes of q as half as many 16-bit elements, boxes of 128 bytes; nkb: stages of 256 columns; lds: scale tiles
 // side by side; 4-bit outputs: ldo bytes between rows of q, ldos scale tiles side by side.
 struct Fp4GemmArgs : Fp8GemmArgs {
     CUtensorMap tmSA;  // scale tiles, boxes of two side by side (256 columns)
     CUtensorMap tmSB[CM_MAX_E];
     int ksteps;  // MMAs of 64 columns
+    int tma_out;  // bf16 outputs on pairs leave by tmOut
 };
 cudaError_t launch_fp4_gemm2(const Fp4GemmArgs& a, int bn, int num_sms, cudaStream_t s);
+// A product of at most FP4_FEW_MAX rows in one group: tmA in boxes of fp4_few_rows(M) rows, tmB of 128.
+constexpr int FP4_FEW_MAX = 32;
+int fp4_few_rows(int64_t M);
+cudaError_t launch_fp4_few(const Fp4GemmArgs& a, int num_sms, cudaStream_t s);
 int check_fp4(const clearmoe_fp4* m);
 // Scale tiles [tile_rows x tile_cols] of 512 bytes as a tensor map, boxes of two tiles side by side x box_rows.
 int encode_tmap_fp4_scales(CUtensorMap* map, const void* base, int64_t tile_rows, int64_t tile_cols, int box_rows);
+// Bytes [rows x bytes], rows `pitch` apart (a multiple of 16), as a tensor map for stores, boxes of 64 bytes x 32 rows with
+// 64-byte swizzle.
+int encode_tmap_out_bytes(CUtensorMap* map, const void* base, int64_t rows, int64_t bytes, int64_t pitch);
 
 }  // namespace cm

@@ -261,14 +261,18 @@ cudaError_t launch_kind(const Fp4GemmArgs& a, int num_sms, cudaStream_t s) {
                                         : launch_bn<BN, FP8_OUT_F32>(a, num_sms, s);
 }
 
+constexpr int BULK_NKB = 8;
+
 // The kernel that tests have fixed for their thread's calls (width << 1 | pair), or 0.
 thread_local int g_forced = 0;
 
+constexpr int FEW_WIDTH = 16;  // stands for the kernel for few rows
 struct Pick {
     int bn, pair;
 };
 Pick pick(int64_t M, int N, int groups, int num_sms) {
     const int64_t m_tiles = (M + F4_BM - 1) / F4_BM + groups - 1;
+    if (M <= FP4_FEW_MAX && groups == 1) return {FEW_WIDTH, 0};
     if (m_tiles * ((N + 127) / 128) >= 2 * num_sms) return {256, 1};
     return {m_tiles * ((N + 127) / 128) >= num_sms ? 128 : 64, 0};
 }
@@ -322,17 +326,26 @@ int run(Fp4GemmArgs& g, const clearmoe_fp4* A, const clearmoe_fp4* W, int E, voi
     g.sa = A->scale;
     Pick k = pick(g.M, g.N, E, sms);
     if (g_forced) k = {g_forced >> 1, g_forced & 1};
+    const bool few = k.bn == FEW_WIDTH && !g.offsets && g.M <= FP4_FEW_MAX;
+    if (k.bn == FEW_WIDTH) k.bn = few ? 128 : 64;
     const int wt = k.pair ? (k.bn + 127) / 128 : 1;  // scale tiles of a tile's columns
     const int64_t cols16 = fp4_ldq(A->cols) / 2;
     // Fewer rows than a tile: a box of those alone (the copy engine takes longer over a row past the end).
-    g.box_rows = !k.pair && g.M < F4_BM ? (int)(g.M + 7) / 8 * 8 : F4_BM;
+    g.box_rows = few ? fp4_few_rows(g.M) : !k.pair && g.M < F4_BM ? (int)(g.M + 7) / 8 * 8 : F4_BM;
     if (encode_tmap_bf16(&g.tmA, A->q, A->rows, cols16, g.box_rows)) return CLEARMOE_ECUDA;
     if (encode_tmap_fp4_scales(&g.tmSA, A->scale, (A->rows + 127) / 128, g.lds, 1)) return CLEARMOE_ECUDA;
+    // bf16 rows in order, in whole 16-byte pieces, leave by bulk copies where the epilogue is what takes time
+    const int64_t pitch = g.ldo * 2;
+    if (k.pair && g.nkb <= BULK_NKB && g.out_kind == FP8_OUT_BF16 && !g.offsets && pitch % 16 == 0 && (reinterpret_cast<uintptr_t>(g.out) & 15) == 0) {
+        if (encode_tmap_out_bytes(&g.tmOut, g.out, g.M, (int64_t)g.N * 2, pitch)) return CLEARMOE_ECUDA;
+        g.tma_out = 1;
+    }
     for (int e = 0; e < E; ++e) {
         if (encode_tmap_bf16(&g.tmB[e], W[e].q, W[e].rows, cols16, k.pair ? k.bn / 2 : k.bn)) return CLEARMOE_ECUDA;
         if (encode_tmap_fp4_scales(&g.tmSB[e], W[e].scale, (W[e].rows + 127) / 128, g.lds, wt)) return CLEARMOE_ECUDA;
     }
-    const cudaError_t e = k.pair        ? launch_fp4_gemm2(g, k.bn, sms, s)
+    const cudaError_t e = few           ? launch_fp4_few(g, sms, s)
+                          : k.pair      ? launch_fp4_gemm2(g, k.bn, sms, s)
                           : k.bn == 128 ? launch_kind<128>(g, sms, s)
                                         : launch_kind<64>(g, sms, s);
     if (e == cudaSuccess) return CLEARMOE_OK;
@@ -387,7 +400,7 @@ int clearmoe_debug_fp4_kernel(int32_t width, int32_t pair) {
         cm::g_forced = 0;
         return CLEARMOE_OK;
     }
-    const bool known = pair == 1 ? width == 256 || width == 192 || width == 128 : pair == 0 && (width == 128 || width == 64);
+    const bool known = pair == 1 ? width == 256 || width == 192 || width == 128 : pair == 0 && (width == 128 || width == 64 || width == cm::FEW_WIDTH);
     if (!known) return CLEARMOE_EINVAL;
     cm::g_forced = width << 1 | pair;
     return CLEARMOE_OK;

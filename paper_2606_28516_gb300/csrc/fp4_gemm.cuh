@@ -73,25 +73,44 @@ __device__ __forceinline__ int f4_out_row(const Fp4GemmArgs& a, int m, int lo, i
     return m >= lo ? f8_out_row(a, m, hi) : -1;
 }
 
+// A row's 32 columns [nc, nc + 32) to a block, zeros past N.
+__device__ __forceinline__ uint4 f4_block(const Fp4GemmArgs& a, float (&v)[32], int nc, uint32_t& scale) {
+    if (nc + 32 > a.N) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (nc + i >= a.N) v[i] = 0.f;
+    }
+    scale = fp4_scale_byte(abs_bits(f8_max_abs32(v)));
+    const float inv = fp8_inverse_scale(scale);
+    uint32_t o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = fp4_pack8_scaled(v + 8 * i, make_float2(inv, inv));
+    return make_uint4(o[0], o[1], o[2], o[3]);
+}
+// B blocks side by side of output row `row` (-1: none), from column nc on (B == 2: a multiple of 64, as rows of q are long).
+template <int B>
+__device__ __forceinline__ void f4_store_blocks(const Fp4GemmArgs& a, const uint4* block, const uint32_t* scale, int row, int nc) {
+    if (row < 0 || nc / 2 >= a.ldo) return;
+    uint8_t* q = static_cast<uint8_t*>(a.out) + (int64_t)row * a.ldo + nc / 2;
+    uint8_t* s = a.out_scale + fp4_scale_word(row, nc >> 7, a.ldos) + (nc >> 5 & 3);
+    if constexpr (B == 2) {
+        const uint32_t w[8] = {block[0].x, block[0].y, block[0].z, block[0].w, block[1].x, block[1].y, block[1].z, block[1].w};
+        st_global_32(q, w);
+        *reinterpret_cast<uint16_t*>(s) = (uint16_t)(scale[0] | scale[1] << 8);
+    } else {
+        *reinterpret_cast<uint4*>(q) = block[0];
+        *s = (uint8_t)scale[0];
+    }
+}
+
 // 32 rows' 32 columns [nc, nc + 32) (one row a lane: its output row, or -1) to out.
 template <int KIND>
 __device__ __forceinline__ void f4_store32(const Fp4GemmArgs& a, float (&v)[32], int row, int nc, bool wide, int lane) {
     if constexpr (KIND == FP4_OUT_FP4) {
-        // a row's 32 columns are one block; zeros past N
-        if (nc + 32 > a.N) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (nc + i >= a.N) v[i] = 0.f;
-        }
-        const uint32_t s = fp4_scale_byte(abs_bits(f8_max_abs32(v)));
-        const float inv = fp8_inverse_scale(s);
-        uint32_t o[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = fp4_pack8_scaled(v + 8 * i, make_float2(inv, inv));
-        if (row >= 0 && nc / 2 < a.ldo) {
-            *reinterpret_cast<uint4*>(static_cast<uint8_t*>(a.out) + (int64_t)row * a.ldo + nc / 2) = make_uint4(o[0], o[1], o[2], o[3]);
-            a.out_scale[fp4_scale_word(row, nc >> 7, a.ldos) + (nc >> 5 & 3)] = (uint8_t)s;
-        }
+        uint4 block[1];
+        uint32_t scale[1];
+        block[0] = f4_block(a, v, nc, scale[0]);
+        f4_store_blocks<1>(a, block, scale, row, nc);
     } else {
         if (a.rows || (wide && nc + 32 <= a.N)) {
             f8_store32<KIND>(a, v, row, nc, wide, lane);

@@ -8,7 +8,10 @@
 // (ovl_bar), and the next tile's MMAs start then rather than when the whole accumulator is read. Columns 480 .. 503 hold
 // the scales of two times 128 of K, in turn.
 //
-// Epilogue: 16 warps (four per lane quarter), each 32 columns at a time: one block of a 4-bit output.
+// Epilogue: 16 warps (four per lane quarter), each 32 columns at a time (one block of a 4-bit output), two times side by
+// side. What bounds it is the path of loads and stores (TMEM, shared and global memory): a store whose lanes write 32 rows
+// apart takes it 32 cycles whatever its width, so bf16 rows leave by bulk copies from shared memory and 4-bit rows 32
+// bytes at a time.
 // Hand-offs and giving up as in fp8_gemm2.cu: TMA bytes of both CTAs on the even CTA's full barriers, commits on both
 // CTAs' empty and tfull barriers, the epilogue warps of both on the even CTA's ovl and tempty; every wait is bounded, and
 // the even CTA lets copies in flight land before the cluster retires.
@@ -26,8 +29,9 @@ namespace cm {
 namespace {
 
 constexpr int P4_BM = 128;  // rows per CTA
+constexpr int P4_STAGED = 32 * 64;  // bytes of a warp's 32 rows and columns of bf16
 
-template <int BN_>
+template <int BN_, int KIND>
 struct P4Cfg {
     static constexpr int BN = BN_;
     static constexpr int BH = BN / 2;  // W rows per CTA
@@ -37,16 +41,17 @@ struct P4Cfg {
     static constexpr int A_BYTES = P4_BM * 128, B_BYTES = BH * 128;
     static constexpr int NF = (BN + 127) / 128;  // scale tiles of a tile's columns
     static constexpr int STAGE_BYTES = A_BYTES + B_BYTES + (1 + NF) * F4_SF;
-    static constexpr int STAGES = 220 * 1024 / STAGE_BYTES < 8 ? 220 * 1024 / STAGE_BYTES : 8;
+    static constexpr int OUT_BYTES = KIND == FP4_OUT_BF16_BULK ? NUM_EPI * P4_STAGED : 0;
+    static constexpr int ROOM = 220 * 1024 - OUT_BYTES, STAGES = ROOM / STAGE_BYTES < 8 ? ROOM / STAGE_BYTES : 8;
     static constexpr bool OVL = BN == 256;
     static constexpr int ACC1 = OVL ? 224 : BN;  // first column of the second accumulator
     static constexpr int SF_COL = ACC1 + BN, SF_COLS = 4 * (1 + NF);
     static_assert(SF_COL + 2 * SF_COLS <= 512);
     static constexpr int CHUNKS = BN / 32;
-    static constexpr int ROUNDS = (CHUNKS + 3) / 4;  // of four 32-column chunks, one per warp of a quarter
+    static constexpr int ROUNDS = (CHUNKS + 3) / 4;  // a warp of a quarter has ROUNDS chunks of 32 columns side by side
     static constexpr int NBARS = 2 * STAGES + 4 + 3;
-    static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + NUM_EPI * 32 * 4 + NBARS * 8 + 16 + 8 * (CM_MAX_E + 1) + 8;
-    static_assert(STAGE_BYTES % 1024 == 0);
+    static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + OUT_BYTES + NUM_EPI * ROUNDS * 32 * 4 + NBARS * 8 + 16 + 8 * (CM_MAX_E + 1) + 8;
+    static_assert(STAGE_BYTES % 1024 == 0 && CHUNKS % ROUNDS == 0);
 };
 
 __device__ __forceinline__ void umma2_mxf4(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sfa,
@@ -61,16 +66,33 @@ __device__ __forceinline__ void umma2_mxf4(uint32_t d_tmem, uint64_t a_desc, uin
         : "memory");
 }
 
-// KIND: FP8_OUT_F32, FP8_OUT_BF16 or FP4_OUT_FP4.
+// 32 rows' 32 columns (a row a lane) to a warp's shared memory as bf16, where the copy engine takes them from: piece j of
+// 16 bytes of row i lies at j ^ (i >> 1 & 3). The engine has read what was there before.
+__device__ __forceinline__ void stage_bf16(const float (&v)[32], uint32_t staged, int lane) {
+    bulk_wait_read();
+    __syncwarp();
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const float* w = v + 8 * p;
+        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(staged + lane * 64 + ((p ^ (lane >> 1 & 3)) << 4)),
+                     "r"(pack_bf16(w[0], w[1])), "r"(pack_bf16(w[2], w[3])), "r"(pack_bf16(w[4], w[5])), "r"(pack_bf16(w[6], w[7]))
+                     : "memory");
+    }
+    fence_proxy_async_smem();
+    __syncwarp();
+}
+
+// KIND: FP8_OUT_F32, FP8_OUT_BF16, FP4_OUT_FP4 or FP4_OUT_BF16_BULK.
 template <int BN_, int KIND>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_>::THREADS, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::THREADS, 1)
     fp4_gemm2_kernel(const __grid_constant__ Fp4GemmArgs a) {
-    using C = P4Cfg<BN_>;
+    using C = P4Cfg<BN_, KIND>;
     constexpr int BN = C::BN, STAGES = C::STAGES;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* sm = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
-    float* s_bias = reinterpret_cast<float*>(sm + STAGES * C::STAGE_BYTES);  // [epilogue warp][32]
-    uint64_t* bars = reinterpret_cast<uint64_t*>(s_bias + C::NUM_EPI * 32);
+    unsigned char* s_out = sm + STAGES * C::STAGE_BYTES;               // [epilogue warp][32 rows][64], bf16 outputs
+    float* s_bias = reinterpret_cast<float*>(s_out + C::OUT_BYTES);    // [epilogue warp][ROUNDS][32]
+    uint64_t* bars = reinterpret_cast<uint64_t*>(s_bias + C::NUM_EPI * C::ROUNDS * 32);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::NBARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     volatile uint32_t* s_issued = tmem_slot + 2;  // k-blocks this CTA's producer has loaded, once it has stopped
@@ -228,78 +250,89 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_>::THREADS,
         // ------------------------------------------------ epilogue (both CTAs, own 128 rows)
         const int quarter = warp & 3, cg = warp >> 2;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-        float* bias_line = s_bias + warp * 32;
+        float* bias_line = s_bias + warp * C::ROUNDS * 32;
         const bool has_bias = a.bias != nullptr;
-        const bool wide = f8_wide(a);
+        const bool wide = f8_wide(a), mine = cg * C::ROUNDS < C::CHUNKS;
+        unsigned char* staged = s_out + warp * P4_STAGED;
         const uint32_t tempty_leader0 = map_to_rank(tempty_bar(0), 0), ovl_leader = map_to_rank(ovl_bar, 0);
         // What a tile's epilogue needs beside its sums, loaded a tile ahead: a load waits behind the queued tile loads.
         float bias[C::ROUNDS];
         int row = 0;
-        auto prefetch = [&](int acc) {
+        auto prefetch = [&]() {
             if (!t.live()) return;
             row = f4_out_row(a, t.m0 + (int)rank * P4_BM + quarter * 32 + lane, t.lo, t.hi);
             if (has_bias) {
 #pragma unroll
                 for (int r = 0; r < C::ROUNDS; ++r) {
-                    const int n = t.n0 + ((C::OVL && acc == 0 ? C::ROUNDS - 1 - r : r) * 4 + cg) * 32 + lane;
+                    const int n = t.n0 + (cg * C::ROUNDS + r) * 32 + lane;
                     bias[r] = n >= a.N      ? 0.f
                               : a.bias_bf16 ? bf16_to_f32(__ldg(static_cast<const uint16_t*>(a.bias) + n))
                                             : __ldg(static_cast<const float*>(a.bias) + n);
                 }
             }
         };
-        prefetch(0);
+        prefetch();
         int acc = 0;
         uint32_t aph = 0;
         while (t.live()) {
             const int n0 = t.n0, orow = row;
-            // The chunk of round r: the one in the columns that the accumulators share first.
-            int chunk[C::ROUNDS];
             float b[C::ROUNDS];
 #pragma unroll
-            for (int r = 0; r < C::ROUNDS; ++r) {
-                chunk[r] = (C::OVL && acc == 0 ? C::ROUNDS - 1 - r : r) * 4 + cg;
-                b[r] = bias[r];
-            }
+            for (int r = 0; r < C::ROUNDS; ++r) b[r] = bias[r];
+            const int row0 = t.m0 + (int)rank * P4_BM + quarter * 32, nc = n0 + cg * C::ROUNDS * 32;
             t.next();
-            prefetch(acc ^ 1);
+            prefetch();
             if (!mbar_wait_warp(tfull_bar(acc), aph, abort_flag, a.status, lim)) break;
             tc_fence_after();
-            const uint32_t d = tmem + lanes + acc * C::ACC1;
-            // after the read of round r: its columns may be written again
-            auto released = [&](int r) {
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    if (C::OVL && r == 0 && cg == (acc == 0 ? 3 : 0)) mbar_arrive_cluster(ovl_leader);
-                    if (r + 1 == C::ROUNDS) mbar_arrive_cluster(tempty_leader0 + 8u * acc);
-                }
-            };
+            const uint32_t d = tmem + lanes + acc * C::ACC1 + cg * C::ROUNDS * 32;
+            // All of the warp's columns at once: the accumulator is free the sooner, and one chunk's arithmetic passes under
+            // the other's.
+            float v[C::ROUNDS][32];
+            if (mine) {
+                uint32_t u[C::ROUNDS][32];
 #pragma unroll
-            for (int r = 0; r < C::ROUNDS; ++r) {
-                const bool mine = chunk[r] < C::CHUNKS;
-                float v[32];
+                for (int r = 0; r < C::ROUNDS; ++r) CM_TMEM_LD_X32(d + 32 * r, u[r]);
                 __syncwarp();
-                if (mine) {
-                    uint32_t u[32];
-                    CM_TMEM_LD_X32(d + chunk[r] * 32, u);
-                    if (has_bias) bias_line[lane] = b[r];
-                    tmem_wait_ld();
+                if (has_bias) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(u[i]);
+                    for (int r = 0; r < C::ROUNDS; ++r) bias_line[32 * r + lane] = b[r];
                 }
-                released(r);
-                const int nc = n0 + chunk[r] * 32;
-                if (mine) {
-                    f8_act<32, KIND == FP8_OUT_F32>(v, bias_line, has_bias, a.act);
-                    f4_store32<KIND>(a, v, orow, nc, wide, lane);
+                tmem_wait_ld();
+#pragma unroll
+                for (int r = 0; r < C::ROUNDS; ++r)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[r][i] = __uint_as_float(u[r][i]);
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {  // the columns may be written again
+                if (C::OVL && cg == (acc == 0 ? 3 : 0)) mbar_arrive_cluster(ovl_leader);
+                mbar_arrive_cluster(tempty_leader0 + 8u * acc);
+            }
+            if (mine) {
+                uint4 blocks[C::ROUNDS];
+                uint32_t scales[C::ROUNDS];
+#pragma unroll
+                for (int r = 0; r < C::ROUNDS; ++r) {
+                    f8_act<32, KIND == FP8_OUT_F32>(v[r], bias_line + 32 * r, has_bias, a.act);
+                    if constexpr (KIND == FP4_OUT_FP4) {
+                        blocks[r] = f4_block(a, v[r], nc + 32 * r, scales[r]);
+                    } else if constexpr (KIND == FP4_OUT_BF16_BULK) {
+                        stage_bf16(v[r], smem_u32(staged), lane);
+                        if (row0 < a.M && nc + 32 * r < a.N) tma_store_2d(&a.tmOut, smem_u32(staged), (nc + 32 * r) * 2, row0);
+                        bulk_commit();
+                    } else {
+                        f4_store32<KIND>(a, v[r], orow, nc + 32 * r, wide, lane);
+                    }
                 }
+                if constexpr (KIND == FP4_OUT_FP4) f4_store_blocks<C::ROUNDS>(a, blocks, scales, orow, nc);
             }
             if (++acc == 2) {
                 acc = 0;
                 aph ^= 1;
             }
         }
+        if (KIND == FP4_OUT_BF16_BULK) bulk_wait_all();  // the stores read this CTA's shared memory
     }
     tc_fence_before();
     __syncthreads();
@@ -311,7 +344,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_>::THREADS,
 
 template <int BN, int KIND>
 cudaError_t launch_pair(const Fp4GemmArgs& a, int num_sms, cudaStream_t s) {
-    using C = P4Cfg<BN>;
+    using C = P4Cfg<BN, KIND>;
     static_assert(C::SMEM <= 227 * 1024);
     const cudaError_t e = smem_attr_once((const void*)fp4_gemm2_kernel<BN, KIND>, C::SMEM);
     if (e != cudaSuccess) return e;
@@ -341,6 +374,7 @@ cudaError_t launch_kind2(const Fp4GemmArgs& a, int bn, int num_sms, cudaStream_t
 
 cudaError_t launch_fp4_gemm2(const Fp4GemmArgs& a, int bn, int num_sms, cudaStream_t s) {
     return a.out_kind == FP4_OUT_FP4    ? launch_kind2<FP4_OUT_FP4>(a, bn, num_sms, s)
+           : a.tma_out                  ? launch_kind2<FP4_OUT_BF16_BULK>(a, bn, num_sms, s)
            : a.out_kind == FP8_OUT_BF16 ? launch_kind2<FP8_OUT_BF16>(a, bn, num_sms, s)
                                         : launch_kind2<FP8_OUT_F32>(a, bn, num_sms, s);
 }

@@ -1010,7 +1010,7 @@ typedef CUresult (*PFN_encodeTiled_t)(CUtensorMap*, CUtensorMapDataType, cuuint3
 
 namespace {
 TmapCache<CUtensorMap> g_tmaps;
-constexpr int TMAP_FP4_SCALES = 3;  // of TmapKey::elem, beside the element sizes
+constexpr int TMAP_FP4_SCALES = 3, TMAP_OUT_BYTES = 5;  // of TmapKey::elem, beside the element sizes
 }  // namespace
 
 static int encode_tmap_uncached(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int box_rows,
@@ -1047,6 +1047,11 @@ int encode_tmap_fp4_scales(CUtensorMap* map, const void* base, int64_t tile_rows
     return encode_tmap_cached(map, base, tile_rows, tile_cols, box_rows, 0, TMAP_FP4_SCALES);
 }
 
+int encode_tmap_out_bytes(CUtensorMap* map, const void* base, int64_t rows, int64_t bytes, int64_t pitch) {
+    if (pitch % 16 != 0) return -2;
+    return encode_tmap_cached(map, base, rows, bytes, 32, (int)(pitch / 16), TMAP_OUT_BYTES);
+}
+
 static int encode_tmap_uncached(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int box_rows,
                                 int box_chunks, int elem) {
     static PFN_encodeTiled_t fn = nullptr;
@@ -1075,6 +1080,14 @@ static int encode_tmap_uncached(CUtensorMap* map, const void* base, int64_t rows
         const cuuint32_t es[2] = {1, 1};
         r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void*>(base), gdim, gstride, box, es,
                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    } else if (elem == TMAP_OUT_BYTES) {  // bytes [rows x cols], rows 16 box_chunks apart: boxes of 64 columns x box_rows rows
+        const cuuint64_t gdim[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+        const cuuint64_t gstride[1] = {(cuuint64_t)box_chunks * 16};
+        const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+        const cuuint32_t es[2] = {1, 1};
+        r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), gdim, gstride, box, es,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     } else if (elem == 1) {  // bytes [rows x cols]: boxes of 64 columns x box_rows rows
         const cuuint64_t gdim[2] = {(cuuint64_t)cols, (cuuint64_t)rows};

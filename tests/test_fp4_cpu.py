@@ -199,7 +199,7 @@ def source(name):
     return re.sub(r"//[^\n]*", "", (CSRC / name).read_text())
 
 
-@pytest.mark.parametrize("name", ["fp4.cu", "fp4_gemm.cu", "fp4_gemm2.cu", "norm.cu"])
+@pytest.mark.parametrize("name", ["fp4.cu", "fp4_gemm.cu", "fp4_gemm2.cu", "fp4_few.cu", "norm.cu"])
 def test_reads_and_releases_after_the_wait(name):
     """Every kernel waits for its predecessor before it releases its successor (a run cannot show that one does not)."""
     s = source(name)
@@ -216,6 +216,7 @@ def kernel(name):
 
 @pytest.mark.parametrize("name,drains,last", [
     ("fp4_gemm.cu", ["mbar_wait_warp(full_bar(s), (par >> s) & 1", "mbar_wait_warp(drain_bar, 0"], "tmem_dealloc(tmem"),
+    ("fp4_few.cu", ["mbar_wait_warp(full_bar(s), (par >> s) & 1", "mbar_wait_warp(done_bar, 0"], "tmem_dealloc(tmem"),
     ("fp4_gemm2.cu", ["mbar_wait_warp(full_bar(s), (k / STAGES) & 1", "mbar_wait_warp(drain_bar, 0"], "tcgen05.dealloc"),
 ])
 def test_copies_and_mmas_end_before_tensor_memory_is_freed(name, drains, last):
@@ -225,16 +226,16 @@ def test_copies_and_mmas_end_before_tensor_memory_is_freed(name, drains, last):
     meet = s.rindex("__syncthreads();", 0, free)
     for d in drains:
         assert s.count(d) == 1 and s.index(d) < meet, d
-    assert "return;" not in re.sub(r"auto \w+ = \[&\]\(int acc\) \{.*?\n        \};", "", s[:meet], flags=re.S)  # no thread leaves early
+    assert "return;" not in re.sub(r"auto prefetch = .*?\n        };", "", s[:meet], flags=re.S)  # no thread leaves early
     if name == "fp4_gemm2.cu":
         assert meet < s.index("cluster_sync();", meet) < free
 
 
-@pytest.mark.parametrize("name", ["fp4_gemm.cu", "fp4_gemm2.cu"])
+@pytest.mark.parametrize("name", ["fp4_gemm.cu", "fp4_gemm2.cu", "fp4_few.cu"])
 def test_tensor_memory_accesses_follow_a_fence(name):
     s = kernel(name)
     waits = [m.start() for m in re.finditer(r"\bmbar_wait_warp\(", s)]
-    uses = [m for m in re.finditer(r"\b(CM_TMEM_LD_X\d+|umma2?_mxf4|tmem_cp_scales<\d>)\(", s)]
+    uses = [m for m in re.finditer(r"\b(CM_TMEM_LD_X\d+|umma2?_mxf4|umma_few|tmem_cp_scales<\d>)\(", s)]
     assert uses and not re.search(r"\bmbar_wait\(", s)
     for m in uses:
         last = max(w for w in waits if w < m.start())

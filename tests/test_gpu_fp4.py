@@ -168,7 +168,7 @@ def test_gemm(M, N, K, dtype):
     assert torch.equal(dense, out[:M, :N])  # every store width gives the same values
 
 
-KERNELS = [(256, 1), (192, 1), (128, 1), (128, 0), (64, 0)]
+KERNELS = [(256, 1), (192, 1), (128, 1), (128, 0), (64, 0), (16, 0)]
 
 
 @pytest.fixture
@@ -209,6 +209,33 @@ def test_every_kernel(kernel, M, N, K, act):
     q.q.fill_(0x33)
     cm.clearmoe_fp4_gemm(A, W, q, bias=bias, act=act)
     check_blocks(q, y, err)
+
+
+@pytest.mark.parametrize("M,N,K,act", [(1, 1, 1, cm.ACT_NONE), (16, 40, 130, cm.ACT_GELU), (17, 5003, 257, cm.ACT_RELU),
+                                       (32, 700, 2048, cm.ACT_GELU), (32, 96, 9000, cm.ACT_NONE), (7, 40000, 512, cm.ACT_NONE),
+                                       (3, 128, 1792, cm.ACT_GELU), (29, 20000, 64, cm.ACT_RELU), (33, 300, 300, cm.ACT_NONE)])
+def test_kernel_for_few_rows(M, N, K, act):
+    """K split over one to eight CTAs, one to many tiles, each number of rows; the same bits each time."""
+    rng = np.random.default_rng(M + N + K)
+    A, W, av, wv = make(rng, M, N, K)
+    bias = dev(rng.standard_normal(N) * 0.1)
+    y, err = reference(av, wv, bias, act)
+    cm.clearmoe_debug_fp4_kernel(16, 0)
+    try:
+        for dtype in (torch.float32, torch.bfloat16):
+            out = torch.full((M + 1, N + 3), float("nan"), device="cuda", dtype=dtype)
+            cm.clearmoe_fp4_gemm(A, W, out[:M, :N], bias=bias, act=act)
+            assert within(out[:M, :N], y, err)
+            assert bool(out[M].isnan().all()) and bool(out[:, N:].isnan().all())
+            again = torch.empty(M, N, device="cuda", dtype=dtype)
+            cm.clearmoe_fp4_gemm(A, W, again, bias=bias, act=act)
+            assert torch.equal(again, out[:M, :N])
+        q = cm.fp4_matrix(M, N)
+        q.q.fill_(0x33)
+        cm.clearmoe_fp4_gemm(A, W, q, bias=bias, act=act)
+        check_blocks(q, y, err)
+    finally:
+        cm.clearmoe_debug_fp4_kernel()
 
 
 @pytest.mark.parametrize("perm", [True, False])
