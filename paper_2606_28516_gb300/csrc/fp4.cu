@@ -18,7 +18,7 @@ namespace {
 // its product: 123 us where the two take 105). Other rows: a warp reads 32 consecutive elements at a time, and turns them to
 // the same order in shared memory.
 constexpr int Q4_THREADS = 256;
-constexpr int Q4_CTAS = 32;  // an SM, at the most
+constexpr int Q4_CTAS = 8;  // an SM, at the most
 
 // A lane's 16 values (as Lane16's of P columns, eight lanes a row) from column k of row `row` on to codes and scales. live:
 // there is such a row; inside: it is one of x's.
@@ -50,23 +50,27 @@ __device__ __forceinline__ void quantize16(const Quant4Args& a, float2 (&v)[8], 
     if (live && l8 == 0) *reinterpret_cast<uint32_t*>(a.scale + fp4_scale_word(row, tile, a.tiles)) = word;
 }
 
-template <typename T, bool VEC, bool GATHER>
+// U: tiles of 128 columns side by side that a lane has at a time, so that more is on its way: 16,384 x 4,096 bf16 26.5 us with
+// two, 32.7 with one, 29.9 with four; 9,973 x 4,096 gathered 21.1, 25.6, 21.8. Fewer than four items a CTA are better off
+// with one: 197 x 384 1.5 us, two 1.6, four 2.1.
+template <typename T, bool VEC, bool GATHER, int U>
 __global__ void __launch_bounds__(Q4_THREADS) fp4_quantize_kernel(const Quant4Args a) {
     using Lane = Lane16<T, VEC, 8>;
-    __shared__ __align__(16) unsigned char s_mem[VEC ? Lane::N * 16 * Q4_THREADS : Q4_THREADS / 32 * 4 * 132 * 4];
+    __shared__ __align__(16) unsigned char s_mem[VEC ? U * Lane::N * 16 * Q4_THREADS : Q4_THREADS / 32 * 4 * 132 * 4];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l8 = lane & 7;
-    const int64_t items = (a.rows + 127) / 128 * 4 * a.tiles;  // 8 rows and those 32, 64 and 96 after them, 128 columns
     const uint32_t own = smem_u32(s_mem) + 16 * threadIdx.x, pitch = 16 * Q4_THREADS;
     pdl_wait();
     pdl_launch_dependents();  // after the wait: the next kernel may read weights that one before this has written
-    int64_t row = 0, src = 0;
-    int tile = 0;
+    // items: groups of 8 rows and those 32, 64 and 96 after them, U tiles of each
+    const int cols = (a.tiles + U - 1) / U;
+    const int64_t groups = (a.rows + 127) / 128 * 4, step_group = gridDim.x / cols;
+    const int step_col = (int)(gridDim.x - step_group * cols);
+    int64_t group = blockIdx.x / cols, row = 0, src = 0;
+    int col = (int)(blockIdx.x - group * cols);
     bool live = false, inside = true;
-    auto place = [&](int64_t i) {
-        const int64_t group = i / a.tiles;
-        tile = (int)(i - group * a.tiles);
+    auto place = [&]() {
         row = (group >> 2) * 128 + (lane >> 3) * 32 + (group & 3) * 8 + warp;
-        live = i < items && row < a.rows;
+        live = group < groups && row < a.rows;
         src = row;
         inside = true;
         if (GATHER && live) {
@@ -74,38 +78,50 @@ __global__ void __launch_bounds__(Q4_THREADS) fp4_quantize_kernel(const Quant4Ar
             inside = (uint64_t)src < (uint64_t)a.src_rows;
         }
     };
-    // columns from the lane's first one to the end of its row; none for one that is not there
-    auto left = [&]() { return live && inside ? (int)(a.K - (int64_t)tile * 128 - l8 * Lane::P) : -(1 << 30); };
+    // columns from the lane's first one of unit u to the end of its row; none for one that is not there
+    auto left = [&](int u) { return live && inside ? (int)(a.K - ((int64_t)col * U + u) * 128 - l8 * Lane::P) : -(1 << 30); };
     auto ask = [&]() {
         if constexpr (VEC) {
-            Lane::ask(own, pitch, static_cast<const T*>(a.x) + src * a.ld + (int64_t)tile * 128 + l8 * Lane::P, left());
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                Lane::ask(own + u * Lane::N * pitch, pitch, static_cast<const T*>(a.x) + src * a.ld + ((int64_t)col * U + u) * 128 + l8 * Lane::P, left(u));
             cp_async_commit();
         }
     };
-    int64_t i = blockIdx.x;
-    place(i);
+    auto next = [&]() {
+        group += step_group;
+        col += step_col;
+        if (col >= cols) col -= cols, ++group;
+        place();
+    };
+    place();
     ask();
-    for (; i < items; i += gridDim.x) {
-        float2 v[8];
+    while (group < groups) {
         const int64_t r = row;
-        const int t = tile;
+        const int t = col * U;
         const bool l = live, in = inside;
         if constexpr (VEC) {
-            Lane x;
+            Lane x[U];
             cp_async_wait<0>();
-            x.take(own, pitch, left());
-            x.values(v);
-            place(i + gridDim.x);
+#pragma unroll
+            for (int u = 0; u < U; ++u) x[u].take(own + u * Lane::N * pitch, pitch, left(u));
+            next();
             ask();
-            quantize16<Lane::P>(a, v, r, t, l8, l, in);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (t + u >= a.tiles) break;
+                float2 v[8];
+                x[u].values(v);
+                quantize16<Lane::P>(a, v, r, t + u, l8, l, in);
+            }
         } else {
             float* s = reinterpret_cast<float*>(s_mem) + warp * 4 * 132;  // [row of the warp's four][column]
-            const T* p = static_cast<const T*>(a.x) + src * a.ld + (int64_t)tile * 128 + lane;
-            const int n = live && inside ? (int)min((int64_t)128, a.K - (int64_t)tile * 128) : 0;
+            const T* p = static_cast<const T*>(a.x) + src * a.ld + (int64_t)t * 128;
+            const int n = l && in ? (int)min((int64_t)128, a.K - (int64_t)t * 128) : 0;
             T e[4][4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const T* pj = reinterpret_cast<const T*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(p - lane), 8 * j)) + lane;
+                const T* pj = reinterpret_cast<const T*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(p), 8 * j)) + lane;
                 const int nj = __shfl_sync(0xFFFFFFFFu, n, 8 * j);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) e[j][c] = lane + 32 * c < nj ? __ldcg(pj + 32 * c) : T(0);
@@ -121,12 +137,13 @@ __global__ void __launch_bounds__(Q4_THREADS) fp4_quantize_kernel(const Quant4Ar
                         s[132 * j + 32 * c + lane] = e[j][c];
                 }
             __syncwarp();
+            float2 v[8];
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
                 const float4 f = *reinterpret_cast<const float4*>(s + 132 * (lane >> 3) + 64 * (h >> 1) + 8 * l8 + 4 * (h & 1));
                 v[2 * h] = make_float2(f.x, f.y), v[2 * h + 1] = make_float2(f.z, f.w);
             }
-            place(i + gridDim.x);
+            next();
             quantize16<8>(a, v, r, t, l8, l, in);
         }
     }
@@ -161,9 +178,10 @@ cudaError_t launch(K kernel, int64_t grid, cudaStream_t s, A... args) {
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-template <typename T, bool VEC>
-cudaError_t launch_rows(const Quant4Args& a, int64_t grid, cudaStream_t s) {
-    return a.gather ? launch(fp4_quantize_kernel<T, VEC, true>, grid, s, a) : launch(fp4_quantize_kernel<T, VEC, false>, grid, s, a);
+template <typename T, bool VEC, int U>
+cudaError_t launch_rows(const Quant4Args& a, int64_t most, cudaStream_t s) {
+    const int64_t items = (a.rows + 127) / 128 * 4 * ((a.tiles + U - 1) / U), grid = items < most ? items : most;
+    return a.gather ? launch(fp4_quantize_kernel<T, VEC, true, U>, grid, s, a) : launch(fp4_quantize_kernel<T, VEC, false, U>, grid, s, a);
 }
 
 }  // namespace
@@ -171,10 +189,11 @@ cudaError_t launch_rows(const Quant4Args& a, int64_t grid, cudaStream_t s) {
 cudaError_t launch_fp4_quantize(const Quant4Args& a, int dtype, int num_sms, cudaStream_t s) {
     const bool bf16 = dtype == CLEARMOE_BF16;
     const bool vec = (reinterpret_cast<uintptr_t>(a.x) & 15) == 0 && a.K % 8 == 0 && (a.ld * (bf16 ? 2 : 4)) % 16 == 0;
-    const int64_t one = (a.rows + 127) / 128 * 4 * a.tiles, most = (int64_t)num_sms * Q4_CTAS;
-    const int64_t grid = one < most ? one : most;
-    if (bf16) return vec ? launch_rows<uint16_t, true>(a, grid, s) : launch_rows<uint16_t, false>(a, grid, s);
-    return vec ? launch_rows<float, true>(a, grid, s) : launch_rows<float, false>(a, grid, s);
+    const int64_t most = (int64_t)num_sms * Q4_CTAS;
+    const bool two = (a.rows + 127) / 128 * 4 * a.tiles >= 4 * most;
+    if (!vec) return bf16 ? launch_rows<uint16_t, false, 1>(a, most, s) : launch_rows<float, false, 1>(a, most, s);
+    if (bf16) return two ? launch_rows<uint16_t, true, 2>(a, most, s) : launch_rows<uint16_t, true, 1>(a, most, s);
+    return two ? launch_rows<float, true, 2>(a, most, s) : launch_rows<float, true, 1>(a, most, s);
 }
 
 int check_fp4(const clearmoe_fp4* m) {

@@ -270,11 +270,50 @@ constexpr int FEW_WIDTH = 16;  // stands for the kernel for few rows
 struct Pick {
     int bn, pair;
 };
-Pick pick(int64_t M, int N, int groups, int num_sms) {
-    const int64_t m_tiles = (M + F4_BM - 1) / F4_BM + groups - 1;
-    if (M <= FP4_FEW_MAX && groups == 1) return {FEW_WIDTH, 0};
-    if (m_tiles * ((N + 127) / 128) >= 2 * num_sms) return {256, 1};
-    return {m_tiles * ((N + 127) / 128) >= num_sms ? 128 : 64, 0};
+// Cycles (at 1.9 GHz) a product takes on a kernel: its start; rounds of tiles, each of which multiplies its stages or, where
+// that is longer, runs the epilogue of the tile before it; and a part of the last epilogue. A stage's cycles grow from what
+// the MMAs and their scales take to what the path from L2 allows with every SM at work. Fitted to 57 products of 32 to
+// 16,384 rows; what the rule chooses is 0.5 % slower than the best kernel in the mean, 10 % at the most. In us, (64, 0),
+// (128, 0), (128, 1), (256, 1) at M x N x K: 197 x 1,536 x 384 with bias and GELU 3.5, 4.5, 4.4, 5.7; 788 x 768 x 2,048 4.4,
+// 5.0, 5.0, 6.5; 1,970 x 2,304 x 768 6.3, 6.1, 6.0, 6.3; 6,000 x 384 x 1,536 5.8, 5.3, 6.0, 6.7; 2,048 x 4,096 x 4,096 24.7,
+// 19.7, 17.4, 15.9; 16,384 x 4,096 x 4,096 162, 116, 99, 76. (Tiles of 192 columns on pairs were nowhere the best by more
+// than 1 %.)
+struct Fp4Kernel {
+    Pick pick;
+    int start, low, block, between;  // low, block: a stage's cycles on an idle GPU and with every SM at work
+    int gelu;                        // bias and GELU, of a tile
+    double last;                     // the part of the last epilogue that nothing runs beside
+    int epilogue[4];                 // of a tile by the kind of its stores: bf16 and fp32 in whole 32-byte pieces, rows of any pitch, 4-bit
+};
+double cost(const Fp4Kernel& k, int64_t M, int N, int nkb, int store, bool gelu, int groups, int num_sms) {
+    const int rows = k.pick.pair ? 256 : 128, units = k.pick.pair ? num_sms / 2 : num_sms;
+    if (units < 1) return 1e30;
+    const int64_t tiles = ((M + rows - 1) / rows + groups - 1) * (((int64_t)N + k.pick.bn - 1) / k.pick.bn);
+    const double rounds = (double)((tiles + units - 1) / units), busy = tiles < units ? (double)tiles / units : 1.0;
+    const double main = nkb * (k.low + (k.block - k.low) * busy * busy), beside = k.epilogue[store] + (gelu ? k.gelu : 0);
+    const double next = main + k.between > beside ? main + k.between : beside;
+    return k.start + main + (rounds - 1) * next + k.last * beside;
+}
+Pick pick(const Fp4GemmArgs& g, int num_sms) {
+    static const Fp4Kernel all[] = {{{64, 0}, 4770, 323, 392, 490, 1350, 0.44, {1560, 3050, 2880, 1160}},
+                                    {{128, 0}, 3090, 373, 602, 0, 930, 1.14, {3000, 4360, 4750, 2430}},
+                                    {{128, 1}, 6230, 264, 499, 293, 1050, 0.72, {1670, 3920, 4570, 2120}},
+                                    {{256, 1}, 5620, 516, 850, 16, 2040, 0.87, {3150, 6970, 8730, 3190}}};
+    // Few rows, while at least two CTAs share a tile's K: 16 x 1,024 x 4,096 3.2 us against 5.2 (64, 0), 3 x 8,192 x 8,192 8.5
+    // against 9.9, 32 x 4,096 x 4,096 5.1 against 5.6; otherwise 16 x 32,768 x 1,024 8.9 against 6.6, and with 32 rows of few
+    // stages 32 x 768 x 768 4.5 against 2.9.
+    if (g.M <= FP4_FEW_MAX && !g.offsets && 2 * ((g.N + 127) / 128) <= num_sms && (g.M <= 16 || g.nkb >= 8)) return {FEW_WIDTH, 0};
+    const int store = g.out_kind == FP4_OUT_FP4 ? 3 : !f8_wide(g) ? 2 : g.out_kind == FP8_OUT_F32 ? 1 : 0;
+    Pick best = all[0].pick;
+    double least = 1e30;
+    for (const Fp4Kernel& k : all) {
+        const double c = cost(k, g.M, g.N, g.nkb, store, g.act == CLEARMOE_ACT_GELU, g.E, num_sms);
+        if (c < least) {
+            least = c;
+            best = k.pick;
+        }
+    }
+    return best;
 }
 
 // Operands, epilogue and output of a product; fills g's epilogue fields.
@@ -324,7 +363,7 @@ int run(Fp4GemmArgs& g, const clearmoe_fp4* A, const clearmoe_fp4* W, int E, voi
     g.E = E;
     g.lds = fp4_tiles(A->cols);
     g.sa = A->scale;
-    Pick k = pick(g.M, g.N, E, sms);
+    Pick k = pick(g, sms);
     if (g_forced) k = {g_forced >> 1, g_forced & 1};
     const bool few = k.bn == FEW_WIDTH && !g.offsets && g.M <= FP4_FEW_MAX;
     if (k.bn == FEW_WIDTH) k.bn = few ? 128 : 64;
@@ -400,7 +439,7 @@ int clearmoe_debug_fp4_kernel(int32_t width, int32_t pair) {
         cm::g_forced = 0;
         return CLEARMOE_OK;
     }
-    const bool known = pair == 1 ? width == 256 || width == 192 || width == 128 : pair == 0 && (width == 128 || width == 64 || width == cm::FEW_WIDTH);
+    const bool known = pair == 1 ? width == 256 || width == 128 : pair == 0 && (width == 128 || width == 64 || width == cm::FEW_WIDTH);
     if (!known) return CLEARMOE_EINVAL;
     cm::g_forced = width << 1 | pair;
     return CLEARMOE_OK;

@@ -39,7 +39,7 @@ struct P4Cfg {
     static constexpr int WARP_MMA = NUM_EPI, WARP_TMA = NUM_EPI + 1;
     static constexpr int THREADS = 32 * (WARP_TMA + 1);
     static constexpr int A_BYTES = P4_BM * 128, B_BYTES = BH * 128;
-    static constexpr int NF = (BN + 127) / 128;  // scale tiles of a tile's columns
+    static constexpr int NF = BN / 128;  // scale tiles of a tile's columns
     static constexpr int STAGE_BYTES = A_BYTES + B_BYTES + (1 + NF) * F4_SF;
     static constexpr int OUT_BYTES = KIND == FP4_OUT_BF16_BULK ? NUM_EPI * P4_STAGED : 0;
     static constexpr int ROOM = 220 * 1024 - OUT_BYTES, STAGES = ROOM / STAGE_BYTES < 8 ? ROOM / STAGE_BYTES : 8;
@@ -47,11 +47,10 @@ struct P4Cfg {
     static constexpr int ACC1 = OVL ? 224 : BN;  // first column of the second accumulator
     static constexpr int SF_COL = ACC1 + BN, SF_COLS = 4 * (1 + NF);
     static_assert(SF_COL + 2 * SF_COLS <= 512);
-    static constexpr int CHUNKS = BN / 32;
-    static constexpr int ROUNDS = (CHUNKS + 3) / 4;  // a warp of a quarter has ROUNDS chunks of 32 columns side by side
+    static constexpr int ROUNDS = BN / 128;  // a warp of a quarter has ROUNDS chunks of 32 columns side by side
     static constexpr int NBARS = 2 * STAGES + 4 + 3;
     static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + OUT_BYTES + NUM_EPI * ROUNDS * 32 * 4 + NBARS * 8 + 16 + 8 * (CM_MAX_E + 1) + 8;
-    static_assert(STAGE_BYTES % 1024 == 0 && CHUNKS % ROUNDS == 0);
+    static_assert(STAGE_BYTES % 1024 == 0);
 };
 
 __device__ __forceinline__ void umma2_mxf4(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sfa,
@@ -188,7 +187,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::TH
                     oph ^= 1;
                     tc_fence_after();
                     const uint32_t d = tmem + acc * C::ACC1;
-                    const int at = warp_uniform(t.n0 >> 5 & 3);  // W's first column of scales in its tile of 128 rows
                     for (int kb = 0; kb < nkb; ++kb) {
                         if (!mbar_wait_warp(full_bar(stage), ph, abort_flag, a.status, lim)) {
                             ok = false;
@@ -208,7 +206,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::TH
                             for (int j = 0; j < 2; ++j) {  // 64 columns: 32 bytes on in each row
                                 const int k = 2 * h + j;
                                 if (4 * kb + k < a.ksteps)
-                                    umma2_mxf4(d, ad + 2 * k, bd + 2 * k, idesc_mxf4(2 * P4_BM, BN, j), sf, sf + 4 + at, (kb | k) != 0);
+                                    umma2_mxf4(d, ad + 2 * k, bd + 2 * k, idesc_mxf4(2 * P4_BM, BN, j), sf, sf + 4, (kb | k) != 0);
                             }
                         }
                         umma2_commit_both(empty_bar(stage));
@@ -252,7 +250,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::TH
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         float* bias_line = s_bias + warp * C::ROUNDS * 32;
         const bool has_bias = a.bias != nullptr;
-        const bool wide = f8_wide(a), mine = cg * C::ROUNDS < C::CHUNKS;
+        const bool wide = f8_wide(a);
         unsigned char* staged = s_out + warp * P4_STAGED;
         const uint32_t tempty_leader0 = map_to_rank(tempty_bar(0), 0), ovl_leader = map_to_rank(ovl_bar, 0);
         // What a tile's epilogue needs beside its sums, loaded a tile ahead: a load waits behind the queued tile loads.
@@ -288,7 +286,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::TH
             // All of the warp's columns at once: the accumulator is free the sooner, and one chunk's arithmetic passes under
             // the other's.
             float v[C::ROUNDS][32];
-            if (mine) {
+            {
                 uint32_t u[C::ROUNDS][32];
 #pragma unroll
                 for (int r = 0; r < C::ROUNDS; ++r) CM_TMEM_LD_X32(d + 32 * r, u[r]);
@@ -309,7 +307,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::TH
                 if (C::OVL && cg == (acc == 0 ? 3 : 0)) mbar_arrive_cluster(ovl_leader);
                 mbar_arrive_cluster(tempty_leader0 + 8u * acc);
             }
-            if (mine) {
+            {
                 uint4 blocks[C::ROUNDS];
                 uint32_t scales[C::ROUNDS];
 #pragma unroll
@@ -365,9 +363,7 @@ cudaError_t launch_pair(const Fp4GemmArgs& a, int num_sms, cudaStream_t s) {
 
 template <int KIND>
 cudaError_t launch_kind2(const Fp4GemmArgs& a, int bn, int num_sms, cudaStream_t s) {
-    return bn == 256   ? launch_pair<256, KIND>(a, num_sms, s)
-           : bn == 192 ? launch_pair<192, KIND>(a, num_sms, s)
-                       : launch_pair<128, KIND>(a, num_sms, s);
+    return bn == 256 ? launch_pair<256, KIND>(a, num_sms, s) : launch_pair<128, KIND>(a, num_sms, s);
 }
 
 }  // namespace

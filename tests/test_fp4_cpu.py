@@ -57,7 +57,7 @@ def test_library_refuses():
     arr = (cm.clearmoe_fp4 * 2)(good, fp4(rows=5))
     gg = lambda W=arr, E=1, off=A32, perm=None, ld=4: L.clearmoe_fp4_grouped_gemm(P(good), W, E, off, perm, None, A32, cm.F32, ld, None)  # noqa: E731
     assert gg(E=0) == gg(E=17) == gg(W=None) == gg(off=None) == gg(off=A32 + 2) == gg(perm=A32 + 2) == gg(E=2) == gg(ld=3) == cm.EINVAL
-    assert L.clearmoe_debug_fp4_kernel(100, 0) == L.clearmoe_debug_fp4_kernel(64, 1) == L.clearmoe_debug_fp4_kernel(256, 0) == cm.EINVAL
+    assert L.clearmoe_debug_fp4_kernel(100, 0) == L.clearmoe_debug_fp4_kernel(192, 1) == L.clearmoe_debug_fp4_kernel(256, 0) == cm.EINVAL
     assert L.clearmoe_debug_fp4_kernel(0, 0) == cm.OK
 
 

@@ -168,7 +168,7 @@ def test_gemm(M, N, K, dtype):
     assert torch.equal(dense, out[:M, :N])  # every store width gives the same values
 
 
-KERNELS = [(256, 1), (192, 1), (128, 1), (128, 0), (64, 0), (16, 0)]
+KERNELS = [(256, 1), (128, 1), (128, 0), (64, 0), (16, 0)]
 
 
 @pytest.fixture
