@@ -518,6 +518,10 @@ int clearmoe_fp4_grouped_gemm(const clearmoe_fp4* A, const clearmoe_fp4* W, int3
  * where the product is not grouped; (0, 0) restores the choice by size. EINVAL for another kernel. */
 int clearmoe_debug_fp4_kernel(int32_t width, int32_t pair);
 
+/* For tests of the bounded waits: those of the calling thread's later products of 4-bit blocks run out after
+ * wait_limit_ns nanoseconds; 0 restores 1 s. EINVAL below 0 and above 1 s. */
+int clearmoe_debug_fp4_wait(int64_t wait_limit_ns);
+
 /* ---- a residual's addition and the root-mean-square norm of the sum ----
  *
  * s = x + residual, rounded to dtype, is the stream as it goes on; its norm y = s weight / sqrt(mean(s^2) + eps) feeds the

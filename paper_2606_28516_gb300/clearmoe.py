@@ -139,6 +139,7 @@ _SIGS = {
     "clearmoe_fp4_grouped_gemm": [ctypes.POINTER(clearmoe_fp4), ctypes.POINTER(clearmoe_fp4), _I32, _P, _P,
                                   ctypes.POINTER(clearmoe_fp8_epilogue), _P, _I32, _I64, _P],
     "clearmoe_debug_fp4_kernel": [_I32, _I32],
+    "clearmoe_debug_fp4_wait": [_I64],
     "clearmoe_rms_norm": [ctypes.POINTER(clearmoe_norm), _P, _I32, _I64, _P],
     "clearmoe_rms_norm_fp8": [ctypes.POINTER(clearmoe_norm), ctypes.POINTER(clearmoe_fp8), _P],
     "clearmoe_rms_norm_fp4": [ctypes.POINTER(clearmoe_norm), ctypes.POINTER(clearmoe_fp4), _P],
@@ -732,6 +733,11 @@ def clearmoe_fp4_grouped_gemm(A: Fp4Matrix, W, offsets, out, perm=None, bias=Non
 def clearmoe_debug_fp4_kernel(width: int = 0, pair: int = 0) -> None:
     """For tests: fixes the kernel of the calling thread's later products of 4-bit blocks; no arguments: by size again."""
     _check(lib().clearmoe_debug_fp4_kernel(width, pair), "clearmoe_debug_fp4_kernel")
+
+
+def clearmoe_debug_fp4_wait(wait_limit_ns: int = 0) -> None:
+    """For tests: the limit of the waits in the calling thread's later products of 4-bit blocks; no argument: 1 s again."""
+    _check(lib().clearmoe_debug_fp4_wait(wait_limit_ns), "clearmoe_debug_fp4_wait")
 
 
 # ------------------------------------------------------------------- residual addition and RMS norm

@@ -68,15 +68,17 @@ __global__ void __launch_bounds__(Q4_THREADS) fp4_quantize_kernel(const Quant4Ar
     int64_t group = blockIdx.x / cols, row = 0, src = 0;
     int col = (int)(blockIdx.x - group * cols);
     bool live = false, inside = true;
+    auto row_of = [&](int64_t g) { return (g >> 2) * 128 + (lane >> 3) * 32 + (g & 3) * 8 + warp; };
+    int index = 0;  // of the next item's row, on its way a turn ahead
+    auto ask_index = [&](int64_t g) {
+        if (GATHER && row_of(g) < a.rows) index = __ldcg(a.gather + row_of(g));
+    };
     auto place = [&]() {
-        row = (group >> 2) * 128 + (lane >> 3) * 32 + (group & 3) * 8 + warp;
+        row = row_of(group);
         live = group < groups && row < a.rows;
-        src = row;
-        inside = true;
-        if (GATHER && live) {
-            src = __ldcg(a.gather + row);
-            inside = (uint64_t)src < (uint64_t)a.src_rows;
-        }
+        src = GATHER ? index : row;
+        inside = !GATHER || (uint64_t)src < (uint64_t)a.src_rows;
+        ask_index(group + step_group + (col + step_col >= cols ? 1 : 0));
     };
     // columns from the lane's first one of unit u to the end of its row; none for one that is not there
     auto left = [&](int u) { return live && inside ? (int)(a.K - ((int64_t)col * U + u) * 128 - l8 * Lane::P) : -(1 << 30); };
@@ -94,6 +96,7 @@ __global__ void __launch_bounds__(Q4_THREADS) fp4_quantize_kernel(const Quant4Ar
         if (col >= cols) col -= cols, ++group;
         place();
     };
+    ask_index(group);
     place();
     ask();
     while (group < groups) {

@@ -102,6 +102,7 @@ __global__ void __launch_bounds__(FewCfg<NT_>::THREADS, 2) fp4_few_kernel(const 
         *abort_flag = 0;
         mbar_fence_init();
     }
+    if (warp == 4 && lane == 0) f4_prefetch_maps(a);
     if (warp == 5) tmem_alloc(smem_u32(tmem_slot), C::TMEM_COLS);
     tc_fence_before();
     __syncthreads();

@@ -91,13 +91,14 @@ __global__ void __launch_bounds__(F4Cfg<BN_>::THREADS, 1) fp4_gemm_kernel(const 
         *abort_flag = 0;
         mbar_fence_init();
     }
+    if (warp == C::WARP_TMA && lane == 0) f4_prefetch_maps(a);
     if (warp == C::WARP_MMA) tmem_alloc(smem_u32(tmem_slot), C::TMEM_COLS);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     pdl_wait();  // everything below may read the previous kernel's results
     pdl_launch_dependents();  // after the wait: the next kernel may read weights that one before this has written
-    if (threadIdx.x == 0) f4_groups(a, F4_BM, s_off, s_prefix);
+    if (warp == 0) f4_groups(a, F4_BM, s_off, s_prefix, lane);
     __syncthreads();
     const uint32_t tmem = warp_uniform(*tmem_slot);
     F4Walk t(blockIdx.x, gridDim.x, a.N, F4_BM, BN, a.E, s_off, s_prefix);
@@ -265,6 +266,8 @@ constexpr int BULK_NKB = 8;
 
 // The kernel that tests have fixed for their thread's calls (width << 1 | pair), or 0.
 thread_local int g_forced = 0;
+constexpr int64_t WAIT_LIMIT_NS = 1000000000LL;
+thread_local int64_t g_wait = WAIT_LIMIT_NS;  // of their waits
 
 constexpr int FEW_WIDTH = 16;  // stands for the kernel for few rows
 struct Pick {
@@ -326,7 +329,7 @@ int check_gemm(const clearmoe_fp4* A, const clearmoe_fp4* W, int E, const clearm
         if (W[e].cols != A->cols || W[e].rows != W[0].rows || W[e].rows > (int64_t)1 << 24) return CLEARMOE_EINVAL;
     }
     g.act = CLEARMOE_ACT_NONE;
-    g.wait_limit_ns = 1000000000LL;
+    g.wait_limit_ns = g_wait;
     if (epi) {
         if (epi->act != CLEARMOE_ACT_NONE && epi->act != CLEARMOE_ACT_RELU && epi->act != CLEARMOE_ACT_GELU)
             return CLEARMOE_EINVAL;
@@ -442,6 +445,12 @@ int clearmoe_debug_fp4_kernel(int32_t width, int32_t pair) {
     const bool known = pair == 1 ? width == 256 || width == 128 : pair == 0 && (width == 128 || width == 64 || width == cm::FEW_WIDTH);
     if (!known) return CLEARMOE_EINVAL;
     cm::g_forced = width << 1 | pair;
+    return CLEARMOE_OK;
+}
+
+int clearmoe_debug_fp4_wait(int64_t wait_limit_ns) {
+    if (wait_limit_ns < 0 || wait_limit_ns > cm::WAIT_LIMIT_NS) return CLEARMOE_EINVAL;
+    cm::g_wait = wait_limit_ns ? wait_limit_ns : cm::WAIT_LIMIT_NS;
     return CLEARMOE_OK;
 }
 

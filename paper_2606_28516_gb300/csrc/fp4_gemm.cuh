@@ -20,19 +20,35 @@ __device__ __forceinline__ uint32_t idesc_mxf4(int M, int N, int half) {
 // Row boundaries of the groups, off[E + 1], held to ascend within the rows (f8_groups), and the row tiles before each,
 // prefix[E + 1]. A group's tiles start at the scale tile that its first row lies in, so that scales come as they lie;
 // rows of another group in its first and last tile are computed and not stored.
-__device__ __forceinline__ void f4_groups(const Fp4GemmArgs& a, int bm, int* off, int* prefix) {
-    int acc = 0;
-    for (int e = 0; e <= a.E; ++e) {
-        const int v = a.offsets ? __ldcg(a.offsets + e) : (e == 0 ? 0 : (int)a.M);
-        off[e] = min(max(v, acc), (int)a.M);
-        acc = off[e];
+// By one warp, a group a lane: E + 1 loads one after the other took 2 us.
+__device__ __forceinline__ void f4_groups(const Fp4GemmArgs& a, int bm, int* off, int* prefix, int lane) {
+    int v = lane == 0 && !a.offsets ? 0 : (int)a.M;
+    if (a.offsets && lane <= a.E) v = __ldcg(a.offsets + lane);
+    v = max(v, 0);
+#pragma unroll
+    for (int o = 1; o <= CM_MAX_E; o <<= 1) {
+        const int u = __shfl_up_sync(0xFFFFFFFFu, v, o);
+        if (lane >= o) v = max(v, u);
     }
-    acc = 0;
-    for (int e = 0; e < a.E; ++e) {
-        prefix[e] = acc;
-        if (off[e + 1] > off[e]) acc += (off[e + 1] - (off[e] & ~127) + bm - 1) / bm;
+    v = min(v, (int)a.M);
+    const int end = __shfl_down_sync(0xFFFFFFFFu, v, 1);
+    const int n = lane < a.E && end > v ? (end - (v & ~127) + bm - 1) / bm : 0;
+    int sum = n;  // of the groups up to this one
+#pragma unroll
+    for (int o = 1; o <= CM_MAX_E; o <<= 1) {
+        const int u = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+        if (lane >= o) sum += u;
     }
-    prefix[a.E] = acc;
+    if (lane <= a.E) {
+        off[lane] = v;
+        prefix[lane] = sum - n;
+    }
+}
+// The maps of group 0's tiles, of a product with its kernel's parameters, on their way.
+__device__ __forceinline__ void f4_prefetch_maps(const Fp4GemmArgs& a) {
+    const CUtensorMap* m[4] = {&a.tmA, &a.tmB[0], &a.tmSA, &a.tmSB[0]};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m[i])) : "memory");
 }
 // F8Walk over such tiles: rows [max(m0, lo), hi) of a tile are the group's.
 struct F4Walk {

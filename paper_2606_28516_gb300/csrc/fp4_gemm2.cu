@@ -125,6 +125,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::TH
         *abort_flag = 0;
         mbar_fence_init();
     }
+    if (warp == C::WARP_TMA && lane == 0) f4_prefetch_maps(a);
     if (warp == C::WARP_MMA) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512)
                      : "memory");
@@ -136,7 +137,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::TH
     tc_fence_after();
     pdl_wait();  // everything below may read the previous kernel's results
     pdl_launch_dependents();  // after the wait: the next kernel may read weights that one before this has written
-    if (threadIdx.x == 0) f4_groups(a, 2 * P4_BM, s_off, s_prefix);
+    if (warp == 0) f4_groups(a, 2 * P4_BM, s_off, s_prefix, lane);
     __syncthreads();
     const uint32_t tmem = warp_uniform(*tmem_slot);  // all 512 columns: the same base in both CTAs
     const int nkb = a.nkb;

@@ -59,6 +59,8 @@ def test_library_refuses():
     assert gg(E=0) == gg(E=17) == gg(W=None) == gg(off=None) == gg(off=A32 + 2) == gg(perm=A32 + 2) == gg(E=2) == gg(ld=3) == cm.EINVAL
     assert L.clearmoe_debug_fp4_kernel(100, 0) == L.clearmoe_debug_fp4_kernel(192, 1) == L.clearmoe_debug_fp4_kernel(256, 0) == cm.EINVAL
     assert L.clearmoe_debug_fp4_kernel(0, 0) == cm.OK
+    assert L.clearmoe_debug_fp4_wait(-1) == L.clearmoe_debug_fp4_wait(1_000_000_001) == cm.EINVAL
+    assert L.clearmoe_debug_fp4_wait(0) == cm.OK
 
 
 def norm(**kw):

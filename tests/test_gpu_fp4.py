@@ -238,6 +238,17 @@ def test_kernel_for_few_rows(M, N, K, act):
         cm.clearmoe_debug_fp4_kernel()
 
 
+@pytest.mark.parametrize("kernel", [(256, 1), (128, 1)], indirect=True)
+@pytest.mark.parametrize("M,N,K,pitch", [(300, 777, 64, 784), (257, 131, 500, 136), (1000, 8, 1024, 8), (513, 33, 2048, 64)])
+def test_bf16_rows_by_bulk_copies(kernel, M, N, K, pitch):
+    """Rows in whole 16-byte pieces whose last columns are not: nothing is written past them."""
+    A, W, av, wv = make(np.random.default_rng(M), M, N, K)
+    out = torch.full((M + 300, pitch), float("nan"), device="cuda", dtype=torch.bfloat16)
+    cm.clearmoe_fp4_gemm(A, W, out[:M, :N], act=cm.ACT_RELU)
+    assert within(out[:M, :N], *reference(av, wv, None, cm.ACT_RELU))
+    assert bool(out[M:].isnan().all()) and bool(out[:, N:].isnan().all())
+
+
 @pytest.mark.parametrize("perm", [True, False])
 @pytest.mark.parametrize("counts", [[0, 300, 1, 0, 129, 700], [1130], [3, 2, 0, 1], [128, 128, 256], [127, 1, 129, 255, 0, 77, 500, 41],
                                     [1] * 16])
@@ -383,3 +394,65 @@ def test_two_products_in_a_row():
         out.zero_()
         graph.replay()
         check()
+
+
+def test_two_streams_and_two_graphs():
+    """Calls share nothing: products of two streams at once, and two graphs replayed side by side."""
+    rng = np.random.default_rng(23)
+    sets = []
+    for M, N, K in ((500, 640, 1024), (20, 640, 1024), (500, 640, 1024), (20, 640, 1024)):
+        A, W, av, wv = make(rng, M, N, K)
+        sets.append((A, W, torch.zeros(M, N, device="cuda"), reference(av, wv, None, cm.ACT_NONE)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    for _ in range(20):
+        for s, (A, W, out, _) in zip(streams, sets):
+            with torch.cuda.stream(s):
+                cm.clearmoe_fp4_gemm(A, W, out)
+    torch.cuda.synchronize()
+    for _, _, out, ref in sets:
+        assert within(out, *ref)
+        out.zero_()
+    graphs = []
+    for A, W, out, _ in sets:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            cm.clearmoe_fp4_gemm(A, W, out)
+    for _ in range(20):
+        for s, g in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    for _, _, out, ref in sets:
+        assert within(out, *ref)
+
+
+@pytest.mark.parametrize("kernel", KERNELS, indirect=True)
+@pytest.mark.parametrize("blocks", [False, True])
+def test_waits_that_run_out(kernel, blocks):
+    """Under limits of 1 to 200 microseconds the kernels give up between their copies, let what is in flight land, and
+    return; the call reports CLEARMOE_ETIMEOUT or completes, and the next call with the usual limit gives the same bits."""
+    M = 32 if kernel[0] == 16 else 3000
+    A, W, av, wv = make(np.random.default_rng(29), M, 1024, 16384)
+    out = cm.fp4_matrix(M, 1024) if blocks else torch.empty(M, 1024, device="cuda", dtype=torch.bfloat16)
+    bits = out.q if blocks else out
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    cm.clearmoe_fp4_gemm(A, W, out, status=status)
+    want, gave_up = bits.clone(), []
+    try:
+        for limit in (1_000, 4_000, 16_000, 50_000, 200_000):
+            for _ in range(4):
+                cm.clearmoe_debug_fp4_wait(limit)
+                cm.clearmoe_fp4_gemm(A, W, out, status=status)
+                cm.clearmoe_fp4_gemm(A, W, out, status=status)
+                st = status.item()
+                assert st in (0, cm.ETIMEOUT)
+                gave_up.append(st == cm.ETIMEOUT)
+                status.zero_()
+                cm.clearmoe_debug_fp4_wait()
+                bits.zero_()
+                cm.clearmoe_fp4_gemm(A, W, out, status=status)
+                assert torch.equal(bits, want) and status.item() == 0
+    finally:
+        cm.clearmoe_debug_fp4_wait()
+    assert kernel[0] == 16 or any(gave_up)
