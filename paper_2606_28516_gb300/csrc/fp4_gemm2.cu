@@ -47,9 +47,12 @@ struct P4Cfg {
     static constexpr int ACC1 = OVL ? 224 : BN;  // first column of the second accumulator
     static constexpr int SF_COL = ACC1 + BN, SF_COLS = 4 * (1 + NF);
     static_assert(SF_COL + 2 * SF_COLS <= 512);
-    static constexpr int ROUNDS = BN / 128;  // a warp of a quarter has ROUNDS chunks of 32 columns side by side
+    // Epilogue warps in GROUPS that take every GROUPS-th tile (two: one accumulator each); a warp has PASSES times CH chunks
+    // of 32 columns side by side.
+    static constexpr int GROUPS = KIND == FP4_OUT_FP4 ? 2 : 1, TILE_WARPS = NUM_EPI / GROUPS;
+    static constexpr int PASSES = GROUPS == 2 ? BN / 128 : 1, CH = GROUPS == 2 ? 2 : BN / 128, WIDTH = 32 * PASSES * CH;
     static constexpr int NBARS = 2 * STAGES + 4 + 3;
-    static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + OUT_BYTES + NUM_EPI * ROUNDS * 32 * 4 + NBARS * 8 + 16 + 8 * (CM_MAX_E + 1) + 8;
+    static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + OUT_BYTES + NUM_EPI * CH * 32 * 4 + NBARS * 8 + 16 + 8 * (CM_MAX_E + 1) + 8;
     static_assert(STAGE_BYTES % 1024 == 0);
 };
 
@@ -90,8 +93,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::TH
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* sm = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     unsigned char* s_out = sm + STAGES * C::STAGE_BYTES;               // [epilogue warp][32 rows][64], bf16 outputs
-    float* s_bias = reinterpret_cast<float*>(s_out + C::OUT_BYTES);    // [epilogue warp][ROUNDS][32]
-    uint64_t* bars = reinterpret_cast<uint64_t*>(s_bias + C::NUM_EPI * C::ROUNDS * 32);
+    float* s_bias = reinterpret_cast<float*>(s_out + C::OUT_BYTES);    // [epilogue warp][CH][32]
+    uint64_t* bars = reinterpret_cast<uint64_t*>(s_bias + C::NUM_EPI * C::CH * 32);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::NBARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     volatile uint32_t* s_issued = tmem_slot + 2;  // k-blocks this CTA's producer has loaded, once it has stopped
@@ -117,7 +120,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::TH
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(tfull_bar(i), 1);
-            mbar_init(tempty_bar(i), 2 * C::NUM_EPI);  // epilogue warps of both CTAs
+            mbar_init(tempty_bar(i), 2 * C::TILE_WARPS);  // epilogue warps of both CTAs
         }
         mbar_init(ovl_bar, 8);  // the warps whose chunk lies in the shared columns, of both CTAs
         mbar_init(drain_bar, 1);
@@ -247,72 +250,86 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::TH
         }
     } else {
         // ------------------------------------------------ epilogue (both CTAs, own 128 rows)
-        const int quarter = warp & 3, cg = warp >> 2;
+        const int quarter = warp & 3, cg = warp % C::TILE_WARPS >> 2, group = warp / C::TILE_WARPS;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-        float* bias_line = s_bias + warp * C::ROUNDS * 32;
+        float* bias_line = s_bias + warp * C::CH * 32;
         const bool has_bias = a.bias != nullptr;
         const bool wide = f8_wide(a);
         unsigned char* staged = s_out + warp * P4_STAGED;
         const uint32_t tempty_leader0 = map_to_rank(tempty_bar(0), 0), ovl_leader = map_to_rank(ovl_bar, 0);
+        int acc = group;
+        // The warp's first column in pass p: the pass with the columns that the accumulators share first.
+        auto column = [&](int p) { return cg * C::WIDTH + (C::OVL && acc == 0 ? C::PASSES - 1 - p : p) * C::CH * 32; };
         // What a tile's epilogue needs beside its sums, loaded a tile ahead: a load waits behind the queued tile loads.
-        float bias[C::ROUNDS];
+        float bias[C::PASSES][C::CH];
         int row = 0;
         auto prefetch = [&]() {
             if (!t.live()) return;
             row = f4_out_row(a, t.m0 + (int)rank * P4_BM + quarter * 32 + lane, t.lo, t.hi);
             if (has_bias) {
 #pragma unroll
-                for (int r = 0; r < C::ROUNDS; ++r) {
-                    const int n = t.n0 + (cg * C::ROUNDS + r) * 32 + lane;
-                    bias[r] = n >= a.N      ? 0.f
-                              : a.bias_bf16 ? bf16_to_f32(__ldg(static_cast<const uint16_t*>(a.bias) + n))
-                                            : __ldg(static_cast<const float*>(a.bias) + n);
-                }
+                for (int p = 0; p < C::PASSES; ++p)
+#pragma unroll
+                    for (int r = 0; r < C::CH; ++r) {
+                        const int n = t.n0 + column(p) + 32 * r + lane;
+                        bias[p][r] = n >= a.N      ? 0.f
+                                     : a.bias_bf16 ? bf16_to_f32(__ldg(static_cast<const uint16_t*>(a.bias) + n))
+                                                   : __ldg(static_cast<const float*>(a.bias) + n);
+                    }
             }
         };
+        if (group && t.live()) t.next();
         prefetch();
-        int acc = 0;
         uint32_t aph = 0;
         while (t.live()) {
-            const int n0 = t.n0, orow = row;
-            float b[C::ROUNDS];
+            const int n0 = t.n0, orow = row, row0 = t.m0 + (int)rank * P4_BM + quarter * 32;
+            int col[C::PASSES];
+            float b[C::PASSES][C::CH];
 #pragma unroll
-            for (int r = 0; r < C::ROUNDS; ++r) b[r] = bias[r];
-            const int row0 = t.m0 + (int)rank * P4_BM + quarter * 32, nc = n0 + cg * C::ROUNDS * 32;
+            for (int p = 0; p < C::PASSES; ++p) {
+                col[p] = column(p);
+#pragma unroll
+                for (int r = 0; r < C::CH; ++r) b[p][r] = bias[p][r];
+            }
+            const int now = acc;
+            if (C::GROUPS == 1) acc ^= 1;
             t.next();
+            if (C::GROUPS == 2 && t.live()) t.next();
             prefetch();
-            if (!mbar_wait_warp(tfull_bar(acc), aph, abort_flag, a.status, lim)) break;
+            if (!mbar_wait_warp(tfull_bar(now), aph, abort_flag, a.status, lim)) break;
             tc_fence_after();
-            const uint32_t d = tmem + lanes + acc * C::ACC1 + cg * C::ROUNDS * 32;
-            // All of the warp's columns at once: the accumulator is free the sooner, and one chunk's arithmetic passes under
-            // the other's.
-            float v[C::ROUNDS][32];
-            {
-                uint32_t u[C::ROUNDS][32];
+            const uint32_t d = tmem + lanes + now * C::ACC1;
 #pragma unroll
-                for (int r = 0; r < C::ROUNDS; ++r) CM_TMEM_LD_X32(d + 32 * r, u[r]);
-                __syncwarp();
-                if (has_bias) {
+            for (int p = 0; p < C::PASSES; ++p) {
+                // All of a pass's columns at once: the accumulator is free the sooner, and one chunk's arithmetic passes under
+                // the other's.
+                float v[C::CH][32];
+                {
+                    uint32_t u[C::CH][32];
 #pragma unroll
-                    for (int r = 0; r < C::ROUNDS; ++r) bias_line[32 * r + lane] = b[r];
+                    for (int r = 0; r < C::CH; ++r) CM_TMEM_LD_X32(d + col[p] + 32 * r, u[r]);
+                    __syncwarp();
+                    if (has_bias) {
+#pragma unroll
+                        for (int r = 0; r < C::CH; ++r) bias_line[32 * r + lane] = b[p][r];
+                    }
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int r = 0; r < C::CH; ++r)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[r][i] = __uint_as_float(u[r][i]);
                 }
-                tmem_wait_ld();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {  // the columns may be written again
+                    if (C::OVL && p == 0 && cg == (now == 0 ? C::TILE_WARPS / 4 - 1 : 0)) mbar_arrive_cluster(ovl_leader);
+                    if (p + 1 == C::PASSES) mbar_arrive_cluster(tempty_leader0 + 8u * now);
+                }
+                const int nc = n0 + col[p];
+                uint4 blocks[C::CH];
+                uint32_t scales[C::CH];
 #pragma unroll
-                for (int r = 0; r < C::ROUNDS; ++r)
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[r][i] = __uint_as_float(u[r][i]);
-            }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) {  // the columns may be written again
-                if (C::OVL && cg == (acc == 0 ? 3 : 0)) mbar_arrive_cluster(ovl_leader);
-                mbar_arrive_cluster(tempty_leader0 + 8u * acc);
-            }
-            {
-                uint4 blocks[C::ROUNDS];
-                uint32_t scales[C::ROUNDS];
-#pragma unroll
-                for (int r = 0; r < C::ROUNDS; ++r) {
+                for (int r = 0; r < C::CH; ++r) {
                     f8_act<32, KIND == FP8_OUT_F32>(v[r], bias_line + 32 * r, has_bias, a.act);
                     if constexpr (KIND == FP4_OUT_FP4) {
                         blocks[r] = f4_block(a, v[r], nc + 32 * r, scales[r]);
@@ -324,12 +341,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::TH
                         f4_store32<KIND>(a, v[r], orow, nc + 32 * r, wide, lane);
                     }
                 }
-                if constexpr (KIND == FP4_OUT_FP4) f4_store_blocks<C::ROUNDS>(a, blocks, scales, orow, nc);
+                if constexpr (KIND == FP4_OUT_FP4) f4_store_blocks<C::CH>(a, blocks, scales, orow, nc);
             }
-            if (++acc == 2) {
-                acc = 0;
-                aph ^= 1;
-            }
+            if (C::GROUPS == 2 || now == 1) aph ^= 1;
         }
         if (KIND == FP4_OUT_BF16_BULK) bulk_wait_all();  // the stores read this CTA's shared memory
     }
