@@ -96,9 +96,25 @@ __global__ void __launch_bounds__(Q4_THREADS) fp4_quantize_kernel(const Quant4Ar
         if (col >= cols) col -= cols, ++group;
         place();
     };
+    // Other rows: 32 consecutive elements of each of the warp's four rows at a time.
+    T e[VEC ? 1 : 4][VEC ? 1 : 4];
+    auto load = [&]() {
+        if constexpr (!VEC) {
+            const T* p = static_cast<const T*>(a.x) + src * a.ld + (int64_t)col * 128;
+            const int n = live && inside ? (int)min((int64_t)128, a.K - (int64_t)col * 128) : 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const T* pj = reinterpret_cast<const T*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(p), 8 * j)) + lane;
+                const int nj = __shfl_sync(0xFFFFFFFFu, n, 8 * j);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) e[j][c] = lane + 32 * c < nj ? __ldcg(pj + 32 * c) : T(0);
+            }
+        }
+    };
     ask_index(group);
     place();
     ask();
+    load();
     while (group < groups) {
         const int64_t r = row;
         const int t = col * U;
@@ -119,16 +135,6 @@ __global__ void __launch_bounds__(Q4_THREADS) fp4_quantize_kernel(const Quant4Ar
             }
         } else {
             float* s = reinterpret_cast<float*>(s_mem) + warp * 4 * 132;  // [row of the warp's four][column]
-            const T* p = static_cast<const T*>(a.x) + src * a.ld + (int64_t)t * 128;
-            const int n = l && in ? (int)min((int64_t)128, a.K - (int64_t)t * 128) : 0;
-            T e[4][4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const T* pj = reinterpret_cast<const T*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(p), 8 * j)) + lane;
-                const int nj = __shfl_sync(0xFFFFFFFFu, n, 8 * j);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) e[j][c] = lane + 32 * c < nj ? __ldcg(pj + 32 * c) : T(0);
-            }
             __syncwarp();
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -147,6 +153,7 @@ __global__ void __launch_bounds__(Q4_THREADS) fp4_quantize_kernel(const Quant4Ar
                 v[2 * h] = make_float2(f.x, f.y), v[2 * h + 1] = make_float2(f.z, f.w);
             }
             next();
+            load();
             quantize16<8>(a, v, r, t, l8, l, in);
         }
     }

@@ -275,8 +275,8 @@ struct Pick {
 };
 // Cycles (at 1.9 GHz) a product takes on a kernel: its start; rounds of tiles, each of which multiplies its stages or, where
 // that is longer, runs the epilogue of the tile before it; and a part of the last epilogue. A stage's cycles grow from what
-// the MMAs and their scales take to what the path from L2 allows with every SM at work. Fitted to 57 products of 32 to
-// 16,384 rows; what the rule chooses is 0.5 % slower than the best kernel in the mean, 10 % at the most. In us, (64, 0),
+// the MMAs and their scales take to what the path from L2 allows with every SM at work. Fitted to 90 products of 8 to
+// 16,384 rows; what the rule chooses is 0.6 % slower than the best kernel in the mean, 9 % at the most. In us, (64, 0),
 // (128, 0), (128, 1), (256, 1) at M x N x K: 197 x 1,536 x 384 with bias and GELU 3.5, 4.5, 4.4, 5.7; 788 x 768 x 2,048 4.4,
 // 5.0, 5.0, 6.5; 1,970 x 2,304 x 768 6.3, 6.1, 6.0, 6.3; 6,000 x 384 x 1,536 5.8, 5.3, 6.0, 6.7; 2,048 x 4,096 x 4,096 24.7,
 // 19.7, 17.4, 15.9; 16,384 x 4,096 x 4,096 162, 116, 99, 76. (Tiles of 192 columns on pairs were nowhere the best by more
@@ -298,10 +298,10 @@ double cost(const Fp4Kernel& k, int64_t M, int N, int nkb, int store, bool gelu,
     return k.start + main + (rounds - 1) * next + k.last * beside;
 }
 Pick pick(const Fp4GemmArgs& g, int num_sms) {
-    static const Fp4Kernel all[] = {{{64, 0}, 4770, 323, 392, 490, 1350, 0.44, {1560, 3050, 2880, 1160}},
-                                    {{128, 0}, 3090, 373, 602, 0, 930, 1.14, {3000, 4360, 4750, 2430}},
-                                    {{128, 1}, 6230, 264, 499, 293, 1050, 0.72, {1670, 3920, 4570, 2120}},
-                                    {{256, 1}, 5620, 516, 850, 16, 2040, 0.87, {3150, 6970, 8730, 3190}}};
+    static const Fp4Kernel all[] = {{{64, 0}, 4690, 319, 386, 367, 1290, 0.49, {1600, 3010, 2840, 1180}},
+                                    {{128, 0}, 3550, 370, 564, 0, 970, 1.06, {2910, 4400, 4730, 2250}},
+                                    {{128, 1}, 5960, 267, 473, 394, 1140, 0.84, {1630, 3780, 4370, 1470}},
+                                    {{256, 1}, 5890, 516, 788, 144, 2420, 0.86, {2870, 6850, 8560, 2830}}};
     // Few rows, while at least two CTAs share a tile's K: 16 x 1,024 x 4,096 3.2 us against 5.2 (64, 0), 3 x 8,192 x 8,192 8.5
     // against 9.9, 32 x 4,096 x 4,096 5.1 against 5.6; otherwise 16 x 32,768 x 1,024 8.9 against 6.6, and with 32 rows of few
     // stages 32 x 768 x 768 4.5 against 2.9.
