@@ -50,6 +50,16 @@ __device__ __forceinline__ void f4_prefetch_maps(const Fp4GemmArgs& a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m[i])) : "memory");
 }
+// A box on its way to L2, by the elected lane of a converged warp. Weights are asked for so before the kernel waits for its
+// predecessor: nothing of them is read before that, and a write of the predecessor's goes to the same L2.
+__device__ __forceinline__ void l2_prefetch_2d(const CUtensorMap* map, int32_t c0, int32_t c1) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t"
+        "@q cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];\n\t}" ::"l"(reinterpret_cast<uint64_t>(map)),
+        "r"(c0), "r"(c1)
+        : "memory");
+}
+
 // F8Walk over such tiles: rows [max(m0, lo), hi) of a tile are the group's.
 struct F4Walk {
     int mt, nt;  // row and column tile
