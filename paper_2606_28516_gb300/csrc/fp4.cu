@@ -159,25 +159,47 @@ __global__ void __launch_bounds__(Q4_THREADS) fp4_quantize_kernel(const Quant4Ar
     }
 }
 
+// Eight columns a thread (a quarter of a block: four bytes of codes, one scale), blocks of 2,048 columns, every gridDim.y-th
+// row. vec: rows of out in whole 16-byte pieces.
 template <typename T>
 __global__ void __launch_bounds__(256)
-    fp4_dequantize_kernel(const uint8_t* q, const uint8_t* scale, int64_t rows, int64_t K, int64_t ldq, int tiles, T* out, int64_t ld) {
+    fp4_dequantize_kernel(const uint8_t* q, const uint8_t* scale, int64_t rows, int64_t K, int64_t ldq, int tiles, T* out, int64_t ld, int vec) {
     pdl_wait();
-    const int64_t n = rows * K;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / K, k = i - r * K;
-        const float v = fp4_value(q[r * ldq + k / 2] >> (k & 1) * 4) * fp8_scale(scale[fp4_scale_word(r, k / 128, tiles) + k / 32 % 4]);
-        if (sizeof(T) == 2)
-            reinterpret_cast<uint16_t*>(out)[r * ld + k] = f32_to_bf16(v);
-        else
-            reinterpret_cast<float*>(out)[r * ld + k] = v;
+    pdl_launch_dependents();  // after the wait: the next kernel may read weights that one before this has written
+    const int64_t k = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (k >= K) return;
+    for (int64_t r = blockIdx.y; r < rows; r += gridDim.y) {
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(q + r * ldq + k / 2);
+        const float f = fp8_scale(scale[fp4_scale_word(r, k >> 7, tiles) + (k >> 5 & 3)]);
+        float v[8];
+        fp4_unpack8(w, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= f;
+        T* o = out + r * ld + k;
+        if (vec) {
+            if constexpr (sizeof(T) == 2) {
+                *reinterpret_cast<uint4*>(o) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+            } else {
+                *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
+                *(reinterpret_cast<float4*>(o) + 1) = make_float4(v[4], v[5], v[6], v[7]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (k + i >= K) break;
+                if constexpr (sizeof(T) == 2)
+                    o[i] = f32_to_bf16(v[i]);
+                else
+                    o[i] = v[i];
+            }
+        }
     }
 }
 
 template <typename K, typename... A>
-cudaError_t launch(K kernel, int64_t grid, cudaStream_t s, A... args) {
+cudaError_t launch(K kernel, dim3 grid, cudaStream_t s, A... args) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(256);
     cfg.stream = s;
     cudaLaunchAttribute at[1];
@@ -191,7 +213,7 @@ cudaError_t launch(K kernel, int64_t grid, cudaStream_t s, A... args) {
 template <typename T, bool VEC, int U>
 cudaError_t launch_rows(const Quant4Args& a, int64_t most, cudaStream_t s) {
     const int64_t items = (a.rows + 127) / 128 * 4 * ((a.tiles + U - 1) / U), grid = items < most ? items : most;
-    return a.gather ? launch(fp4_quantize_kernel<T, VEC, true, U>, grid, s, a) : launch(fp4_quantize_kernel<T, VEC, false, U>, grid, s, a);
+    return a.gather ? launch(fp4_quantize_kernel<T, VEC, true, U>, dim3((unsigned)grid), s, a) : launch(fp4_quantize_kernel<T, VEC, false, U>, dim3((unsigned)grid), s, a);
 }
 
 }  // namespace
@@ -259,16 +281,18 @@ int clearmoe_fp4_dequantize(const clearmoe_fp4* in, void* out, int32_t dtype, in
     if (rc) return rc;
     const int sms = cm::current_device_sms();
     if (sms <= 0) return CLEARMOE_ECUDA;
-    const int64_t want = (in->rows * in->cols + 255) / 256, grid = want < (int64_t)sms * 8 ? want : (int64_t)sms * 8;
+    const int64_t wide = (in->cols + 2047) / 2048, most = (int64_t)sms * 32 / wide + 1;
+    const dim3 grid((unsigned)wide, (unsigned)(in->rows < most ? in->rows : most));
+    const int vec = in->cols % 8 == 0 && (reinterpret_cast<uintptr_t>(out) & 15) == 0 && ld * (dtype == CLEARMOE_BF16 ? 2 : 4) % 16 == 0;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const uint8_t *q = static_cast<const uint8_t*>(in->q), *scale = in->scale;
     const int64_t ldq = cm::fp4_ldq(in->cols);
     const int tiles = (int)cm::fp4_tiles(in->cols);
     if (dtype == CLEARMOE_BF16)
         return cuda_code(cm::launch(cm::fp4_dequantize_kernel<uint16_t>, grid, s, q, scale, in->rows, in->cols, ldq, tiles,
-                                    static_cast<uint16_t*>(out), ld));
+                                    static_cast<uint16_t*>(out), ld, vec));
     return cuda_code(cm::launch(cm::fp4_dequantize_kernel<float>, grid, s, q, scale, in->rows, in->cols, ldq, tiles,
-                                static_cast<float*>(out), ld));
+                                static_cast<float*>(out), ld, vec));
 }
 
 }  // extern "C"

@@ -46,11 +46,22 @@ __device__ __forceinline__ uint32_t fp4_pack8_scaled(const float* v, float2 k) {
     const float2 c = __fmul2_rn(make_float2(v[4], v[5]), k), d = __fmul2_rn(make_float2(v[6], v[7]), k);
     return fp4_pack8(a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y);
 }
-// The value of a code (its low four bits).
-__device__ __forceinline__ float fp4_value(uint32_t c) {
-    const uint32_t m = c & 7u;  // 0, .5, 1, 1.5, 2, 3, 4, 6
-    const float v = m < 4 ? 0.5f * (float)m : m < 6 ? (float)(m - 2) : (float)(2 * m - 8);
-    return c & 8u ? -v : v;
+// The values of eight codes, the first in the lowest four bits, exactly (by way of fp16).
+__device__ __forceinline__ void fp4_unpack8(uint32_t w, float (&v)[8]) {
+    uint32_t h[4];
+    asm("{\n\t.reg .b8 p, q, r, s;\n\t"
+        "mov.b32 {p, q, r, s}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, p;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %1, q;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, r;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %3, s;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+        : "r"(w));
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        asm("{\n\t.reg .b16 l, u;\n\tmov.b32 {l, u}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, u;\n\t}"
+            : "=f"(v[2 * i]), "=f"(v[2 * i + 1])
+            : "r"(h[i]));
 }
 
 // ---- launchers ----
