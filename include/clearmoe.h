@@ -25,7 +25,7 @@
  *     must not be written by the kernel immediately before the call (any later-enqueued work in
  *     between, or a synchronisation, is enough; of a kernel of the caller's own that work must not
  *     let its successor start before it has waited for its predecessor). clearmoe_route_noalloc reads
- *     nothing early, nor do the calls on 8-bit blocks that take no handle.
+ *     nothing early, nor do the calls that take no handle: those on 8-bit and 4-bit blocks, and the norm.
  *   - Arguments are validated on the host first; on a validation error (EINVAL, EUNSUPPORTED)
  *     nothing is enqueued and the outputs are untouched. CLEARMOE_ECUDA can also come from a
  *     launch after earlier kernels of the same call were enqueued; the outputs are then
@@ -470,7 +470,8 @@ int clearmoe_ffn_forward_fp8(clearmoe_layer* layer, const void* x, int64_t T, co
  *   scale  one byte s per block of 32 columns of one row, in tiles of 128 rows x 128 columns: ceil(rows / 128) rows of
  *          ceil(cols / 128) tiles, 512 bytes each, in which the byte of row r and block b (r < 128, b < 4 within the tile)
  *          is byte 16 (r % 32) + 4 (r / 32) + b, as the tensor cores take them. 32-byte aligned. Bytes of rows past the
- *          last and of blocks at or past 2 ceil(cols / 64) are not used and may be anything.
+ *          last and of blocks at or past 2 ceil(cols / 64) are not used and may be anything; that of a block past cols
+ *          before there may be any but 255 (the quantising calls write 0).
  * The quantising calls give each block the least s with max |value| <= 6 2^(s - 127) (6: e2m1's largest value; s = 0 at
  * the least) and round value 2^(127 - s) to nearest even. A block with an infinity or a NaN gets s = 255, which stands
  * for NaN: every value of the block, and every output that depends on it, is NaN.
@@ -528,8 +529,8 @@ int clearmoe_debug_fp4_wait(int64_t wait_limit_ns);
  * next sublayer. Sums and statistics in fp32 (a mean square past fp32's range makes the row zero), y rounded once.
  *  x, residual (nullable: s = x), sum (nullable: s is not stored) [rows x cols] of dtype (F32 or BF16), rows ldx, ldr and
  *  lds elements apart; weight (nullable: ones) [cols] of weight_dtype; eps >= 0.
- * Every tensor may start anywhere that its element type allows. sum may be x or residual (with the same rows), out
- * neither of the three unless it is x or residual and sum is not. 1 <= rows <= 2^30, 1 <= cols <= CLEARMOE_NORM_MAX
+ * Every tensor may start anywhere that its element type allows. sum may be x or residual (with the same pitch), and out
+ * may be x or residual (of the same dtype and pitch) where sum is not; they must not overlap otherwise. 1 <= rows <= 2^30, 1 <= cols <= CLEARMOE_NORM_MAX
  * (EUNSUPPORTED above). No handle; stream-ordered; reads nothing before the preceding kernel has completed. */
 #define CLEARMOE_NORM_MAX 32768
 typedef struct {

@@ -456,3 +456,70 @@ def test_waits_that_run_out(kernel, blocks):
     finally:
         cm.clearmoe_debug_fp4_wait()
     assert kernel[0] == 16 or any(gave_up)
+
+
+@pytest.mark.parametrize("M,N,K", [(3, 2048, 16384), (300, 512, 1024)])
+def test_weights_and_rows_just_written(M, N, K):
+    """Weights and rows quantised by the kernels right before the product, new ones each time: what is asked for into L2
+    before they are written is not what the product reads."""
+    rng = np.random.default_rng(31)
+    xs, ws = [dev(rows_of(rng, M, K, 1.0)) for _ in range(2)], [dev(rows_of(rng, N, K, 0.5)) for _ in range(2)]
+    A, W, want = cm.fp4_matrix(M, K), cm.fp4_matrix(N, K), []
+    for x, w in zip(xs, ws):
+        cm.clearmoe_fp4_quantize(x, A)
+        cm.clearmoe_fp4_quantize(w, W)
+        torch.cuda.synchronize()
+        want.append(torch.empty(M, N, device="cuda"))
+        cm.clearmoe_fp4_gemm(A, W, want[-1])
+        torch.cuda.synchronize()
+        assert within(want[-1], *reference(values(A), values(W), None, cm.ACT_NONE))
+    outs = [torch.empty(M, N, device="cuda") for _ in range(40)]
+    for i, out in enumerate(outs):
+        cm.clearmoe_fp4_quantize(xs[i & 1], A)
+        cm.clearmoe_fp4_quantize(ws[i & 1], W)
+        cm.clearmoe_fp4_gemm(A, W, out)
+    assert all(torch.equal(out, want[i & 1]) for i, out in enumerate(outs))
+
+
+@pytest.mark.parametrize("kernel", KERNELS[:-1], indirect=True)
+def test_offsets_of_a_routing_that_gave_up(kernel):
+    """Offsets that descend or lie outside the rows, and rows outside the output, are held to the buffers: each row stored
+    is its expert's or stays."""
+    rng = np.random.default_rng(37)
+    M, N, K = 700, 96, 128
+    A, W, av, wv = make(rng, M, N, K)
+    y, err = reference(av, wv, None, cm.ACT_NONE)
+    for off in ([0, -5, 2 ** 31 - 1, 3, 9], [500, 20, 300, 650, -1], [2 ** 31 - 1] * 5, [-2 ** 31] * 5):
+        out = torch.full((M + 1, N), 7.0, device="cuda")
+        cm.clearmoe_fp4_grouped_gemm(A, [W] * 4, torch.tensor(off, dtype=torch.int32, device="cuda"), out[:M])
+        lo = min(max(off[0], 0), M)
+        hi = min(max(max(off), 0), M)
+        assert within(out[lo:hi], y[lo:hi], err[lo:hi])
+        assert bool((out[:lo] == 7).all()) and bool((out[hi:] == 7).all())
+    perm = torch.arange(M, dtype=torch.int32, device="cuda")
+    perm[::3] = -1
+    perm[1::3] = M
+    out = torch.full((M + 1, N), 7.0, device="cuda")
+    cm.clearmoe_fp4_grouped_gemm(A, [W], torch.tensor([0, M], dtype=torch.int32, device="cuda"), out[:M], perm=perm)
+    assert within(out[2:M:3], y[2::3], err[2::3])
+    assert bool((out[0::3] == 7).all()) and bool((out[1::3] == 7).all())
+
+
+def test_long_sums():
+    """K of 300,007 columns: exact values (integers of few bits) in sums that fp32 holds exactly."""
+    rng = np.random.default_rng(41)
+    for M, N in ((1, 40), (40, 130)):
+        K = 300_007
+        a, w = rng.integers(-1, 2, (M, K)).astype(np.float32), rng.integers(-1, 2, (N, K)).astype(np.float32)
+        A, W, out = cm.fp4_matrix(M, K), cm.fp4_matrix(N, K), torch.empty(M, N, device="cuda")
+        cm.clearmoe_fp4_quantize(dev(a), A)
+        cm.clearmoe_fp4_quantize(dev(w), W)
+        cm.clearmoe_fp4_gemm(A, W, out)
+        assert np.array_equal(f64(out), a.astype(np.float64) @ w.T.astype(np.float64))
+
+
+def test_empty_matrices_are_refused():
+    with pytest.raises(cm.ClearMoEError):
+        cm.clearmoe_fp4_quantize(torch.empty(0, 64, device="cuda"), cm.fp4_matrix(0, 64))
+    with pytest.raises(cm.ClearMoEError):
+        cm.clearmoe_rms_norm(torch.empty(0, 64, device="cuda"), torch.empty(0, 64, device="cuda"))

@@ -212,3 +212,51 @@ def test_a_sublayer(blocks):
         x0, h0 = x.clone(), hid.clone()
         graph.replay()
         check(x0, h0)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("odd", ["x", "residual", "sum", "weight", "out"])
+def test_each_tensor_anywhere(odd, dtype):
+    """One tensor that starts and runs off 16 bytes while the others do not."""
+    rng = np.random.default_rng(9)
+    T, d = 37, 776
+
+    def place(name, *shape, dt=dtype):
+        pitch = shape[-1] + (3 if name == odd else 8)
+        t = torch.full((*shape[:-1], pitch), float("nan"), device="cuda", dtype=dt)
+        return t[..., 1:1 + shape[-1]] if name == odd else t[..., :shape[-1]]
+
+    x, r, s, w = place("x", T, d), place("residual", T, d), place("sum", T, d), place("weight", d)
+    x.copy_(stream(rng, T, d, 0, dtype))
+    r.copy_(stream(rng, T, d, 0, dtype))
+    w.copy_(stream(rng, 1, d, 0, dtype)[0])
+    want = (x.float() + r.float()).to(dtype)
+    y, err = reference(want, w, 1e-6)
+    for out_dtype in (torch.bfloat16, torch.float32):
+        out = place("out", T, d, dt=out_dtype)
+        cm.clearmoe_rms_norm(x, out, residual=r, sum_out=s, weight=w)
+        assert torch.equal(s, want)
+        assert bool(((out.double() - y).abs() <= err + (2.0 ** -8 * y.abs() if out_dtype == torch.bfloat16 else 0)).all())
+        for t in (s, out):
+            assert int(t._base.isnan().sum()) == t._base.numel() - t.numel()
+    a = cm.fp4_matrix(T, d)
+    cm.clearmoe_rms_norm(x, a, residual=r, weight=w)
+    got = torch.empty(T, d, device="cuda")
+    cm.clearmoe_fp4_dequantize(a, got)
+    amax = torch.nn.functional.pad(y.abs(), (0, -d % 32)).view(T, -1, 32).amax(2).repeat_interleave(32, 1)[:, :d]
+    assert bool(((got.double() - y).abs() <= 1.2 * err + 0.2 * y.abs() + 0.25 * 1.01 * amax / 3).all())
+
+
+def test_two_streams():
+    xs = [torch.randn(4000, 512, device="cuda", dtype=torch.bfloat16) for _ in range(4)]
+    outs, want = [torch.empty_like(x) for x in xs], []
+    for x in xs:
+        want.append(torch.empty_like(x))
+        cm.clearmoe_rms_norm(x, want[-1])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+    for _ in range(10):
+        for s, x, o in zip(streams, xs, outs):
+            cm.clearmoe_rms_norm(x, o, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
