@@ -189,6 +189,7 @@ def _bind_calls():
     try:
         import torch
         m.bind_torch(torch.bfloat16, torch.float32, torch.int32, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+        m.bind_dlpack(torch._C._to_dlpack)
     except (ImportError, AttributeError):  # a torch without CUDA: every call then goes by integers
         pass
     _calls = m
@@ -676,16 +677,30 @@ def _fp4(m, what):
     return m.ref
 
 
+def _here(stream, *tensors):
+    """Tensors on another GPU than the stream's are refused: the kernels would read them across, or fault."""
+    if stream is not None:
+        here = getattr(stream, "device_index", None)
+    else:
+        import torch
+        here = torch.cuda.current_device() if torch.cuda.is_initialized() else None
+    for t in tensors:
+        at = t.get_device() if hasattr(t, "get_device") else here
+        if here is not None and at >= 0 and at != here:
+            raise ValueError(f"a tensor on GPU {at} was passed to a call on a stream of GPU {here}")
+
+
 def clearmoe_fp4_quantize(x, out: Fp4Matrix, gather=None, stream=None) -> None:
     """x [rows x cols] (bf16 or fp32, any row pitch) to out in 4-bit blocks, weights and activations alike; gather: int32
     source rows (one outside x gives a row of NaN)."""
     o = _fp4(out, "out")
     if gather is None:
-        code = (_calls or _bind_calls()).fp4_quantize_t(x, out.rows, out.cols, out.addr, stream)
+        code = (_calls or _bind_calls()).fp4_quantize_t(x, out.addr, stream)
         if code is not None:
             if code:
                 raise ClearMoEError(code, "clearmoe_fp4_quantize")
             return
+    _here(stream, x, gather)
     p, dt, ld = _matrix(x, out.rows if gather is None else None, out.cols, "x")
     _check(lib().clearmoe_fp4_quantize(p, x.shape[0], dt, ld, _int32(gather, out.rows, "gather"), o, _stream(stream)),
            "clearmoe_fp4_quantize")
@@ -694,6 +709,7 @@ def clearmoe_fp4_quantize(x, out: Fp4Matrix, gather=None, stream=None) -> None:
 def clearmoe_fp4_dequantize(m: Fp4Matrix, out, stream=None) -> None:
     """The values m stands for, rounded to out's dtype (bf16 or fp32)."""
     r = _fp4(m, "m")
+    _here(stream, out)
     p, dt, ld = _matrix(out, m.rows, m.cols, "out")
     _check(lib().clearmoe_fp4_dequantize(r, p, dt, ld, _stream(stream)), "clearmoe_fp4_dequantize")
 
@@ -701,12 +717,15 @@ def clearmoe_fp4_dequantize(m: Fp4Matrix, out, stream=None) -> None:
 def clearmoe_fp4_gemm(A: Fp4Matrix, W: Fp4Matrix, out, bias=None, act: int = ACT_NONE, status=None, stream=None) -> None:
     """out = act(A W^T + bias). out: a [M x N] bf16 or fp32 tensor of any row pitch, or an Fp4Matrix (the result
     quantised, clearmoe_fp4_gemm_fp4)."""
-    a, w, blocks = _fp4(A, "A"), _fp4(W, "W"), isinstance(out, Fp4Matrix)
-    code = (_calls or _bind_calls()).fp4_gemm_t(A.addr, W.addr, A.rows, W.rows, act, bias, status, out.addr if blocks else out, stream)
-    if code is not None:
-        if code:
-            raise ClearMoEError(code, "clearmoe_fp4_gemm_fp4" if blocks else "clearmoe_fp4_gemm")
-        return
+    blocks = isinstance(out, Fp4Matrix)
+    if isinstance(A, Fp4Matrix) and isinstance(W, Fp4Matrix):
+        code = (_calls or _bind_calls()).fp4_gemm_t(A.addr, W.addr, act, bias, status, out.addr if blocks else out, stream)
+        if code is not None:
+            if code:
+                raise ClearMoEError(code, "clearmoe_fp4_gemm_fp4" if blocks else "clearmoe_fp4_gemm")
+            return
+    a, w = _fp4(A, "A"), _fp4(W, "W")
+    _here(stream, bias, status, None if blocks else out)
     epi = _epilogue(bias, act, status, W.rows)
     if blocks:
         _check(lib().clearmoe_fp4_gemm_fp4(a, w, epi, out.ref, _stream(stream)), "clearmoe_fp4_gemm_fp4")
@@ -723,6 +742,7 @@ def clearmoe_fp4_grouped_gemm(A: Fp4Matrix, W, offsets, out, perm=None, bias=Non
         raise ValueError("a grouped product needs matrices and the offsets of their rows")
     for m in W:
         _fp4(m, "every W")
+    _here(stream, offsets, out, perm, bias, status)
     off, rows = _int32(offsets, len(W) + 1, "offsets"), _int32(perm, A.rows, "perm")
     p, dt, ld = _matrix(out, A.rows, W[0].rows, "out")
     arr = (clearmoe_fp4 * len(W))(*[m.c for m in W])
@@ -753,6 +773,7 @@ def clearmoe_rms_norm(x, out, residual=None, sum_out=None, weight=None, eps: flo
         if code:
             raise ClearMoEError(code, "clearmoe_rms_norm" + ("", "_fp4", "_fp8")[bits // 4])
         return
+    _here(stream, x, residual, sum_out, weight, None if bits else out)
     if len(x.shape) != 2:
         raise ValueError(f"x must be a matrix, got {tuple(x.shape)}")
     rows, cols = x.shape

@@ -108,7 +108,7 @@ static PyObject* ffn_fp8(PyObject* self, PyObject* const* args, Py_ssize_t n) {
 }
 
 /* ---- from tensors ---- */
-static PyObject *s_is_cuda, *s_shape, *s_stride, *s_data_ptr, *s_dtype, *s_is_contiguous, *s_numel, *s_cuda_stream;
+static PyObject *s_is_cuda, *s_shape, *s_stride, *s_data_ptr, *s_dtype, *s_is_contiguous, *s_numel, *s_cuda_stream, *s_device_index;
 static PyObject *g_bf16, *g_f32, *g_i32, *g_get_device, *g_raw_stream; /* torch's dtypes; the current device; its current stream */
 
 /* bfloat16, float32, int32, a function giving the current device, one giving a device's current stream */
@@ -161,6 +161,40 @@ static int dtype_of(PyObject* t, int32_t* dt) {
     Py_XDECREF(o);
     return ok;
 }
+/* A tensor as its exchange capsule describes it (DLPack's structure, a public format): one call of torch's where its
+ * attributes are five. */
+struct exchanged {
+    void* data;
+    int32_t device_type, device_id, ndim;
+    uint8_t code, bits;
+    uint16_t lanes;
+    int64_t* shape;
+    int64_t* strides;
+    uint64_t byte_offset;
+};
+enum { ON_CUDA = 2, CODE_FLOAT = 2, CODE_BFLOAT = 4 };
+static PyObject* g_to_dlpack; /* torch's function, or NULL */
+
+/* t as [rows x cols] (rows < 0: any number) on GPU `device` (negative: any): its shape, address, dtype and row pitch. 0 for
+ * anything else, with no exception left. */
+static int matrix_at(PyObject* t, int64_t rows, int64_t cols, int device, int64_t* shape, int64_t* p, int32_t* dt, int64_t* ld) {
+    PyObject* capsule = g_to_dlpack ? PyObject_CallOneArg(g_to_dlpack, t) : NULL;
+    const struct exchanged* x = capsule ? PyCapsule_GetPointer(capsule, "dltensor") : NULL;
+    int ok = x && x->device_type == ON_CUDA && (device < 0 || x->device_id == device) && x->ndim == 2 && x->strides && x->lanes == 1 &&
+             (rows < 0 || x->shape[0] == rows) && (cols < 0 || x->shape[1] == cols) && (x->shape[1] < 2 || x->strides[1] == 1) &&
+             ((x->code == CODE_FLOAT && x->bits == 32) || (x->code == CODE_BFLOAT && x->bits == 16));
+    if (ok) {
+        shape[0] = x->shape[0];
+        shape[1] = x->shape[1];
+        *p = (int64_t)(intptr_t)x->data + (int64_t)x->byte_offset;
+        *dt = x->bits == 16 ? CLEARMOE_BF16 : CLEARMOE_F32;
+        *ld = shape[0] > 1 ? x->strides[0] : shape[1];
+    }
+    if (!x) PyErr_Clear();
+    Py_XDECREF(capsule);
+    return ok;
+}
+
 /* A [rows x cols] matrix of any row pitch. */
 static int matrix(PyObject* t, int64_t rows, int64_t cols, int64_t* p, int32_t* dt, int64_t* ld) {
     int64_t shape[2], stride[2];
@@ -296,70 +330,98 @@ static PyObject* bind_fp4(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
-/* x, rows, cols, out, stream */
-static PyObject* fp4_quantize_t(PyObject* self, PyObject* const* args, Py_ssize_t n) {
-    int64_t v[3], x, ld, s;
-    int32_t dt;
-    int rc;
+/* The stream's handle and its device (-1: not known). */
+static int stream_and_device(PyObject* stream, int64_t* s, int* device) {
+    int64_t d = -1;
+    if (!g_raw_stream) return 0;
+    if (stream != Py_None) {
+        if (!integer(PyObject_GetAttr(stream, s_device_index), &d)) d = -1;
+        *device = (int)d;
+        return integer(PyObject_GetAttr(stream, s_cuda_stream), s);
+    }
+    PyObject* o = PyObject_CallNoArgs(g_get_device);
+    PyObject* r = o ? PyObject_CallOneArg(g_raw_stream, o) : NULL;
+    const int ok = integer(r, s) && integer(o, &d);
+    if (!ok) PyErr_Clear();
+    *device = (int)d;
+    return ok;
+}
+
+/* torch's function that makes exchange capsules */
+static PyObject* bind_dlpack(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     (void)self;
-    if (n != 5) return PyErr_Format(PyExc_TypeError, "5 arguments expected, got %zd", n);
-    if (!integers(args + 1, 3, 3, v)) return NULL;
-    if (!stream_of(args[4], &s) || !matrix(args[0], v[0], v[1], &x, &dt, &ld)) Py_RETURN_NONE;
+    if (n != 1) return PyErr_Format(PyExc_TypeError, "1 argument expected, got %zd", n);
+    Py_INCREF(args[0]);
+    Py_XSETREF(g_to_dlpack, args[0]);
+    Py_RETURN_NONE;
+}
+
+/* x, out, stream */
+static PyObject* fp4_quantize_t(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    int64_t v[1], shape[2], x, ld, s;
+    int32_t dt;
+    int rc, device;
+    (void)self;
+    if (n != 3) return PyErr_Format(PyExc_TypeError, "3 arguments expected, got %zd", n);
+    if (!integers(args + 1, 1, 1, v)) return NULL;
+    const clearmoe_fp4* out = PTR(0);
+    if (!stream_and_device(args[2], &s, &device) || !matrix_at(args[0], out->rows, out->cols, device, shape, &x, &dt, &ld)) Py_RETURN_NONE;
     Py_BEGIN_ALLOW_THREADS
-    rc = g_fp4_quantize(AT(x), v[0], dt, ld, NULL, PTR(2), AT(s));
+    rc = g_fp4_quantize(AT(x), shape[0], dt, ld, NULL, out, AT(s));
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(rc);
 }
 
-/* A, W, rows, cols, act, bias, status, out (a tensor, or the address of 4-bit blocks), stream */
+/* A, W, act, bias, status, out (a tensor, or the address of 4-bit blocks), stream */
 static PyObject* fp4_gemm_t(PyObject* self, PyObject* const* args, Py_ssize_t n) {
-    int64_t v[5], bias, status, out, ld, s;
-    int32_t bias_dt, dt;
-    int rc;
+    int64_t v[3], shape[2], bias, status, out, ld = 0, s;
+    int32_t bias_dt, dt = CLEARMOE_F32;
+    int rc, device;
     (void)self;
-    if (n != 9) return PyErr_Format(PyExc_TypeError, "9 arguments expected, got %zd", n);
-    if (!integers(args, 5, 5, v)) return NULL;
-    if (!stream_of(args[8], &s) || !bias_of(args[5], v[3], &bias, &bias_dt) || !status_of(args[6], &status)) Py_RETURN_NONE;
-    const clearmoe_fp8_epilogue epi = {AT(bias), bias_dt, (int32_t)v[4], AT(status)};
-    const int blocks = PyLong_Check(args[7]);
-    if (blocks ? !integers(args + 7, 1, 1, &out) : !matrix(args[7], v[2], v[3], &out, &dt, &ld)) {
-        if (blocks) return NULL;
+    if (n != 7) return PyErr_Format(PyExc_TypeError, "7 arguments expected, got %zd", n);
+    if (!integers(args, 3, 3, v)) return NULL;
+    const clearmoe_fp4 *A = PTR(0), *W = PTR(1);
+    if (!stream_and_device(args[6], &s, &device) || !bias_of(args[3], W->rows, &bias, &bias_dt) || !status_of(args[4], &status)) Py_RETURN_NONE;
+    const clearmoe_fp8_epilogue epi = {AT(bias), bias_dt, (int32_t)v[2], AT(status)};
+    const int blocks = PyLong_Check(args[5]);
+    if (blocks) {
+        if (!integers(args + 5, 1, 1, &out)) return NULL;
+    } else if (!matrix_at(args[5], A->rows, W->rows, device, shape, &out, &dt, &ld)) {
         Py_RETURN_NONE;
     }
     Py_BEGIN_ALLOW_THREADS
-    rc = blocks ? g_fp4_gemm_fp4(PTR(0), PTR(1), &epi, AT(out), AT(s)) : g_fp4_gemm(PTR(0), PTR(1), &epi, AT(out), dt, ld, AT(s));
+    rc = blocks ? g_fp4_gemm_fp4(A, W, &epi, AT(out), AT(s)) : g_fp4_gemm(A, W, &epi, AT(out), dt, ld, AT(s));
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(rc);
 }
 
 /* x, residual, sum, weight (tensors or None), eps, bits (0: a tensor, 8 or 4: the address of blocks), out, stream */
 static PyObject* rms_norm_t(PyObject* self, PyObject* const* args, Py_ssize_t n) {
-    int64_t shape[2], x, r = 0, sum = 0, w, out, ldo, s;
-    int64_t bits;
-    int32_t dt, other, out_dt;
+    int64_t shape[2], x, r = 0, sum = 0, w, out, ldo = 0, s, bits;
+    int32_t dt, other, out_dt = CLEARMOE_F32;
     clearmoe_norm a = {0};
-    int rc;
+    int rc, device;
     (void)self;
     if (n != 8) return PyErr_Format(PyExc_TypeError, "8 arguments expected, got %zd", n);
     if (!integers(args + 5, 1, 1, &bits)) return NULL;
     a.eps = (float)PyFloat_AsDouble(args[4]);
     if (PyErr_Occurred()) return NULL;
-    if (!stream_of(args[7], &s) || !pair(PyObject_GetAttr(args[0], s_shape), shape) || !matrix(args[0], shape[0], shape[1], &x, &dt, &a.ldx) ||
-        (args[1] != Py_None && (!matrix(args[1], shape[0], shape[1], &r, &other, &a.ldr) || other != dt)) ||
-        (args[2] != Py_None && (!matrix(args[2], shape[0], shape[1], &sum, &other, &a.lds) || other != dt)) ||
-        !bias_of(args[3], shape[1], &w, &a.weight_dtype))
+    if (!stream_and_device(args[7], &s, &device) || !matrix_at(args[0], -1, -1, device, shape, &x, &dt, &a.ldx)) Py_RETURN_NONE;
+    a.rows = shape[0];
+    a.cols = shape[1];
+    if ((args[1] != Py_None && (!matrix_at(args[1], a.rows, a.cols, device, shape, &r, &other, &a.ldr) || other != dt)) ||
+        (args[2] != Py_None && (!matrix_at(args[2], a.rows, a.cols, device, shape, &sum, &other, &a.lds) || other != dt)) ||
+        !bias_of(args[3], a.cols, &w, &a.weight_dtype))
         Py_RETURN_NONE;
     if (bits) {
         if (!integers(args + 6, 1, 1, &out)) return NULL;
-    } else if (!matrix(args[6], shape[0], shape[1], &out, &out_dt, &ldo)) {
+    } else if (!matrix_at(args[6], a.rows, a.cols, device, shape, &out, &out_dt, &ldo)) {
         Py_RETURN_NONE;
     }
     a.x = AT(x);
     a.residual = AT(r);
     a.sum = AT(sum);
     a.weight = AT(w);
-    a.rows = shape[0];
-    a.cols = shape[1];
     a.dtype = dt;
     Py_BEGIN_ALLOW_THREADS
     rc = bits == 8 ? g_norm_fp8(&a, AT(out), AT(s)) : bits == 4 ? g_norm_fp4(&a, AT(out), AT(s)) : g_norm(&a, AT(out), out_dt, ldo, AT(s));
@@ -372,12 +434,14 @@ static PyMethodDef methods[] = {METHOD(bind),      METHOD(bind_torch),      METH
                                 METHOD(gemm_fp8),  METHOD(ffn_few),         METHOD(ffn_fp8),       METHOD(quantize_rows_t),
                                 METHOD(gemm_t),    METHOD(ffn_few_t),       METHOD(ffn_fp8_t),
                                 METHOD(bind_fp4),  METHOD(fp4_quantize_t),  METHOD(fp4_gemm_t),    METHOD(rms_norm_t),
+                                METHOD(bind_dlpack),
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", NULL, -1, methods, NULL, NULL, NULL, NULL};
 PyMODINIT_FUNC PyInit__calls(void) {
-    PyObject** names[] = {&s_is_cuda, &s_shape, &s_stride, &s_data_ptr, &s_dtype, &s_is_contiguous, &s_numel, &s_cuda_stream};
-    const char* text[] = {"is_cuda", "shape", "stride", "data_ptr", "dtype", "is_contiguous", "numel", "cuda_stream"};
-    for (int i = 0; i < 8; ++i)
+    PyObject** names[] = {&s_is_cuda, &s_shape, &s_stride, &s_data_ptr, &s_dtype, &s_is_contiguous, &s_numel, &s_cuda_stream,
+                          &s_device_index};
+    const char* text[] = {"is_cuda", "shape", "stride", "data_ptr", "dtype", "is_contiguous", "numel", "cuda_stream", "device_index"};
+    for (int i = 0; i < 9; ++i)
         if (!(*names[i] = PyUnicode_InternFromString(text[i]))) return NULL;
     return PyModule_Create(&module);
 }
