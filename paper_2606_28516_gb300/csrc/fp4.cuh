@@ -80,19 +80,40 @@ cudaError_t launch_fp4_quantize(const Quant4Args& a, int dtype, int num_sms, cud
 
 constexpr int FP4_OUT_FP4 = 3;  // of out_kind, beside FP8_OUT_F32 and FP8_OUT_BF16
 constexpr int FP4_OUT_BF16_BULK = 4;  // a kernel's: bf16 by bulk copies
-// tmA, tmB: bytes of q as half as many 16-bit elements, boxes of 128 bytes; nkb: stages of 256 columns; lds: scale tiles
-// side by side; 4-bit outputs: ldo bytes between rows of q, ldos scale tiles side by side.
-struct Fp4GemmArgs : Fp8GemmArgs {
-    CUtensorMap tmSA;  // scale tiles, boxes of two side by side (256 columns)
-    CUtensorMap tmSB[CM_MAX_E];
-    int ksteps;  // MMAs of 64 columns
-    int tma_out;  // bf16 outputs on pairs leave by tmOut
+// A product of NE matrices of weights: one, or CM_MAX_E of a grouped product (a launch copies its arguments: 0.2 us of host
+// time for those of sixteen).
+template <int NE>
+struct Fp4GemmArgs {
+    static constexpr bool GROUPED = NE > 1;
+    CUtensorMap tmA, tmSA;          // bytes of q as half as many 16-bit elements, boxes of 128 bytes; scale tiles, boxes of two side by side
+    CUtensorMap tmB[NE], tmSB[NE];  // the same of W
+    CUtensorMap tmOut;              // FP4_OUT_BF16_BULK
+    int64_t M;
+    int N;
+    int nkb;       // stages of 256 columns
+    int ksteps;    // MMAs of 64 columns
+    int box_rows;  // rows of tmA's boxes
+    int E;         // groups
+    const int32_t* offsets;  // [E + 1]; a grouped product's
+    const int32_t* rows;     // output row of row i (nullable); a grouped product's
+    const void* bias;        // [N], fp32 or bf16 (nullable)
+    int bias_bf16;
+    int act;       // clearmoe_act
+    int out_kind;  // FP8_OUT_F32, FP8_OUT_BF16 or FP4_OUT_FP4
+    int tma_out;   // bf16 outputs on pairs leave by tmOut
+    void* out;
+    int64_t ldo;         // elements; 4-bit outputs: bytes between rows of q
+    uint8_t* out_scale;  // FP4_OUT_FP4
+    int64_t ldos;        // scale tiles side by side
+    int32_t* status;
+    int64_t wait_limit_ns;
 };
-cudaError_t launch_fp4_gemm2(const Fp4GemmArgs& a, int bn, int num_sms, cudaStream_t s);
+template <int NE>
+cudaError_t launch_fp4_gemm2(const Fp4GemmArgs<NE>& a, int bn, int num_sms, cudaStream_t s);
 // A product of at most FP4_FEW_MAX rows in one group: tmA in boxes of fp4_few_rows(M) rows, tmB of 128.
 constexpr int FP4_FEW_MAX = 32;
 int fp4_few_rows(int64_t M);
-cudaError_t launch_fp4_few(const Fp4GemmArgs& a, int num_sms, cudaStream_t s);
+cudaError_t launch_fp4_few(const Fp4GemmArgs<1>& a, int num_sms, cudaStream_t s);
 int check_fp4(const clearmoe_fp4* m);
 // Scale tiles [tile_rows x tile_cols] of 512 bytes as a tensor map, boxes of two tiles side by side x box_rows.
 int encode_tmap_fp4_scales(CUtensorMap* map, const void* base, int64_t tile_rows, int64_t tile_cols, int box_rows);

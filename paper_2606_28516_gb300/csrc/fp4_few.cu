@@ -55,7 +55,7 @@ __device__ __forceinline__ float ld_cluster_f32(uint32_t addr_cluster) {
 
 // The sum of row m and column n, a column a lane, to the output.
 template <int KIND>
-__device__ __forceinline__ void finish(const Fp4GemmArgs& a, float v, int m, int n, int lane) {
+__device__ __forceinline__ void finish(const Fp4GemmArgs<1>& a, float v, int m, int n, int lane) {
     if (a.act == CLEARMOE_ACT_GELU) v = gelu_pair_f32(make_float2(v, v)).x;
     if (a.act == CLEARMOE_ACT_RELU) v = v < 0.f ? 0.f : v;  // NaN stays NaN
     if constexpr (KIND == FP4_OUT_FP4) {  // the warp's 32 columns are a block
@@ -76,7 +76,7 @@ __device__ __forceinline__ void finish(const Fp4GemmArgs& a, float v, int m, int
 }
 
 template <int NT_, int KIND>
-__global__ void __launch_bounds__(FewCfg<NT_>::THREADS, 2) fp4_few_kernel(const __grid_constant__ Fp4GemmArgs a, const int split) {
+__global__ void __launch_bounds__(FewCfg<NT_>::THREADS, 2) fp4_few_kernel(const __grid_constant__ Fp4GemmArgs<1> a, const int split) {
     using C = FewCfg<NT_>;
     constexpr int NT = C::NT, STAGES = C::STAGES;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(FewCfg<NT_>::THREADS, 2) fp4_few_kernel(const 
 }
 
 template <int NT, int KIND>
-cudaError_t launch_kind(const Fp4GemmArgs& a, int split, cudaStream_t s) {
+cudaError_t launch_kind(const Fp4GemmArgs<1>& a, int split, cudaStream_t s) {
     using C = FewCfg<NT>;
     const cudaError_t e = smem_attr_once((const void*)fp4_few_kernel<NT, KIND>, C::SMEM);
     if (e != cudaSuccess) return e;
@@ -243,7 +243,7 @@ cudaError_t launch_kind(const Fp4GemmArgs& a, int split, cudaStream_t s) {
     return cudaLaunchKernelEx(&cfg, fp4_few_kernel<NT, KIND>, a, split);
 }
 template <int NT>
-cudaError_t launch_nt(const Fp4GemmArgs& a, int split, cudaStream_t s) {
+cudaError_t launch_nt(const Fp4GemmArgs<1>& a, int split, cudaStream_t s) {
     return a.out_kind == FP4_OUT_FP4    ? launch_kind<NT, FP4_OUT_FP4>(a, split, s)
            : a.out_kind == FP8_OUT_BF16 ? launch_kind<NT, FP8_OUT_BF16>(a, split, s)
                                         : launch_kind<NT, FP8_OUT_F32>(a, split, s);
@@ -265,7 +265,7 @@ static int few_split(int tiles, int nkb, int num_sms) {
     return split < 1 ? 1 : split;
 }
 
-cudaError_t launch_fp4_few(const Fp4GemmArgs& a, int num_sms, cudaStream_t s) {
+cudaError_t launch_fp4_few(const Fp4GemmArgs<1>& a, int num_sms, cudaStream_t s) {
     const int split = few_split((a.N + 127) / 128, a.nkb, num_sms);
     return fp4_few_rows(a.M) == 16 ? launch_nt<16>(a, split, s) : launch_nt<32>(a, split, s);
 }

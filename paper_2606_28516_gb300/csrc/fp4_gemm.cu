@@ -56,8 +56,8 @@ __device__ __forceinline__ void umma_mxf4(uint32_t d_tmem, uint64_t a_desc, uint
         : "memory");
 }
 // KIND: FP8_OUT_F32, FP8_OUT_BF16 or FP4_OUT_FP4.
-template <int BN_, int KIND>
-__global__ void __launch_bounds__(F4Cfg<BN_>::THREADS, 1) fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs a) {
+template <int BN_, int KIND, int NE>
+__global__ void __launch_bounds__(F4Cfg<BN_>::THREADS, 1) fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs<NE> a) {
     using C = F4Cfg<BN_>;
     constexpr int BN = C::BN;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
@@ -234,13 +234,13 @@ __global__ void __launch_bounds__(F4Cfg<BN_>::THREADS, 1) fp4_gemm_kernel(const 
     if (warp == C::WARP_MMA) tmem_dealloc(tmem, C::TMEM_COLS);
 }
 
-template <int BN, int KIND>
-cudaError_t launch_bn(const Fp4GemmArgs& a, int num_sms, cudaStream_t s) {
+template <int BN, int KIND, int NE>
+cudaError_t launch_bn(const Fp4GemmArgs<NE>& a, int num_sms, cudaStream_t s) {
     using C = F4Cfg<BN>;
     static_assert(C::SMEM <= 227 * 1024);
-    const cudaError_t e = smem_attr_once((const void*)fp4_gemm_kernel<BN, KIND>, C::SMEM);
+    const cudaError_t e = smem_attr_once((const void*)fp4_gemm_kernel<BN, KIND, NE>, C::SMEM);
     if (e != cudaSuccess) return e;
-    const int64_t m_tiles = (a.M + F4_BM - 1) / F4_BM + (a.offsets ? a.E - 1 : 0);
+    const int64_t m_tiles = (a.M + F4_BM - 1) / F4_BM + a.E - 1;
     const int64_t tiles = m_tiles * ((a.N + BN - 1) / BN);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(tiles < num_sms ? tiles : num_sms));
@@ -252,14 +252,15 @@ cudaError_t launch_bn(const Fp4GemmArgs& a, int num_sms, cudaStream_t s) {
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, fp4_gemm_kernel<BN, KIND>, a);
+    return cudaLaunchKernelEx(&cfg, fp4_gemm_kernel<BN, KIND, NE>, a);
 }
 
-template <int BN>
-cudaError_t launch_kind(const Fp4GemmArgs& a, int num_sms, cudaStream_t s) {
-    return a.out_kind == FP4_OUT_FP4    ? launch_bn<BN, FP4_OUT_FP4>(a, num_sms, s)
-           : a.out_kind == FP8_OUT_BF16 ? launch_bn<BN, FP8_OUT_BF16>(a, num_sms, s)
-                                        : launch_bn<BN, FP8_OUT_F32>(a, num_sms, s);
+template <int BN, int NE>
+cudaError_t launch_kind(const Fp4GemmArgs<NE>& a, int num_sms, cudaStream_t s) {
+    if constexpr (NE == 1) {
+        if (a.out_kind == FP4_OUT_FP4) return launch_bn<BN, FP4_OUT_FP4>(a, num_sms, s);
+    }
+    return a.out_kind == FP8_OUT_BF16 ? launch_bn<BN, FP8_OUT_BF16>(a, num_sms, s) : launch_bn<BN, FP8_OUT_F32>(a, num_sms, s);
 }
 
 constexpr int BULK_NKB = 8;
@@ -297,7 +298,8 @@ double cost(const Fp4Kernel& k, int64_t M, int N, int nkb, int store, bool gelu,
     const double next = main + k.between > beside ? main + k.between : beside;
     return k.start + main + (rounds - 1) * next + k.last * beside;
 }
-Pick pick(const Fp4GemmArgs& g, int num_sms) {
+template <int NE>
+Pick pick(const Fp4GemmArgs<NE>& g, int num_sms) {
     static const Fp4Kernel all[] = {{{64, 0}, 4690, 319, 386, 367, 1290, 0.49, {1600, 3010, 2840, 1180}},
                                     {{128, 0}, 3550, 370, 564, 0, 970, 1.06, {2910, 4400, 4730, 2250}},
                                     {{128, 1}, 5960, 267, 473, 394, 1140, 0.84, {1630, 3780, 4370, 1470}},
@@ -305,7 +307,7 @@ Pick pick(const Fp4GemmArgs& g, int num_sms) {
     // Few rows, while at least two CTAs share a tile's K: 16 x 1,024 x 4,096 3.2 us against 5.2 (64, 0), 3 x 8,192 x 8,192 8.5
     // against 9.9, 32 x 4,096 x 4,096 5.1 against 5.6; otherwise 16 x 32,768 x 1,024 8.9 against 6.6, and with 32 rows of few
     // stages 32 x 768 x 768 4.5 against 2.9.
-    if (g.M <= FP4_FEW_MAX && !g.offsets && 2 * ((g.N + 127) / 128) <= num_sms && (g.M <= 16 || g.nkb >= 8)) return {FEW_WIDTH, 0};
+    if (NE == 1 && g.M <= FP4_FEW_MAX && 2 * ((g.N + 127) / 128) <= num_sms && (g.M <= 16 || g.nkb >= 8)) return {FEW_WIDTH, 0};
     const int store = g.out_kind == FP4_OUT_FP4 ? 3 : !f8_wide(g) ? 2 : g.out_kind == FP8_OUT_F32 ? 1 : 0;
     Pick best = all[0].pick;
     double least = 1e30;
@@ -320,7 +322,8 @@ Pick pick(const Fp4GemmArgs& g, int num_sms) {
 }
 
 // Operands, epilogue and output of a product; fills g's epilogue fields.
-int check_gemm(const clearmoe_fp4* A, const clearmoe_fp4* W, int E, const clearmoe_fp8_epilogue* epi, Fp4GemmArgs& g) {
+template <int NE>
+int check_gemm(const clearmoe_fp4* A, const clearmoe_fp4* W, int E, const clearmoe_fp8_epilogue* epi, Fp4GemmArgs<NE>& g) {
     std::memset(&g, 0, sizeof(g));
     int rc = check_fp4(A);
     if (rc) return rc;
@@ -346,7 +349,8 @@ int check_gemm(const clearmoe_fp4* A, const clearmoe_fp4* W, int E, const clearm
     return CLEARMOE_OK;
 }
 
-int set_out(Fp4GemmArgs& g, void* out, int32_t dtype, int64_t ldo, int64_t N) {
+template <int NE>
+int set_out(Fp4GemmArgs<NE>& g, void* out, int32_t dtype, int64_t ldo, int64_t N) {
     if (!out || (dtype != CLEARMOE_F32 && dtype != CLEARMOE_BF16) || ldo < N || ldo > (int64_t)1 << 30) return CLEARMOE_EINVAL;
     if (reinterpret_cast<uintptr_t>(out) & (dtype == CLEARMOE_BF16 ? 1 : 3)) return CLEARMOE_EINVAL;
     g.out = out;
@@ -355,7 +359,8 @@ int set_out(Fp4GemmArgs& g, void* out, int32_t dtype, int64_t ldo, int64_t N) {
     return CLEARMOE_OK;
 }
 
-int run(Fp4GemmArgs& g, const clearmoe_fp4* A, const clearmoe_fp4* W, int E, void* stream) {
+template <int NE>
+int run(Fp4GemmArgs<NE>& g, const clearmoe_fp4* A, const clearmoe_fp4* W, int E, void* stream) {
     const int sms = current_device_sms();
     if (sms <= 0) return CLEARMOE_ECUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -364,32 +369,33 @@ int run(Fp4GemmArgs& g, const clearmoe_fp4* A, const clearmoe_fp4* W, int E, voi
     g.ksteps = (int)((A->cols + 63) / 64);
     g.nkb = (g.ksteps + 3) / 4;
     g.E = E;
-    g.lds = fp4_tiles(A->cols);
-    g.sa = A->scale;
+    const int64_t tiles = fp4_tiles(A->cols);
     Pick k = pick(g, sms);
     if (g_forced) k = {g_forced >> 1, g_forced & 1};
-    const bool few = k.bn == FEW_WIDTH && !g.offsets && g.M <= FP4_FEW_MAX;
+    const bool few = NE == 1 && k.bn == FEW_WIDTH && g.M <= FP4_FEW_MAX;
     if (k.bn == FEW_WIDTH) k.bn = few ? 128 : 64;
     const int wt = k.pair ? (k.bn + 127) / 128 : 1;  // scale tiles of a tile's columns
     const int64_t cols16 = fp4_ldq(A->cols) / 2;
     // Fewer rows than a tile: a box of those alone (the copy engine takes longer over a row past the end).
     g.box_rows = few ? fp4_few_rows(g.M) : !k.pair && g.M < F4_BM ? (int)(g.M + 7) / 8 * 8 : F4_BM;
     if (encode_tmap_bf16(&g.tmA, A->q, A->rows, cols16, g.box_rows)) return CLEARMOE_ECUDA;
-    if (encode_tmap_fp4_scales(&g.tmSA, A->scale, (A->rows + 127) / 128, g.lds, 1)) return CLEARMOE_ECUDA;
+    if (encode_tmap_fp4_scales(&g.tmSA, A->scale, (A->rows + 127) / 128, tiles, 1)) return CLEARMOE_ECUDA;
     // bf16 rows in order, in whole 16-byte pieces, leave by bulk copies where the epilogue is what takes time
     const int64_t pitch = g.ldo * 2;
-    if (k.pair && g.nkb <= BULK_NKB && g.out_kind == FP8_OUT_BF16 && !g.offsets && pitch % 16 == 0 && (reinterpret_cast<uintptr_t>(g.out) & 15) == 0) {
+    if (NE == 1 && k.pair && g.nkb <= BULK_NKB && g.out_kind == FP8_OUT_BF16 && pitch % 16 == 0 && (reinterpret_cast<uintptr_t>(g.out) & 15) == 0) {
         if (encode_tmap_out_bytes(&g.tmOut, g.out, g.M, (int64_t)g.N * 2, pitch)) return CLEARMOE_ECUDA;
         g.tma_out = 1;
     }
     for (int e = 0; e < E; ++e) {
         if (encode_tmap_bf16(&g.tmB[e], W[e].q, W[e].rows, cols16, k.pair ? k.bn / 2 : k.bn)) return CLEARMOE_ECUDA;
-        if (encode_tmap_fp4_scales(&g.tmSB[e], W[e].scale, (W[e].rows + 127) / 128, g.lds, wt)) return CLEARMOE_ECUDA;
+        if (encode_tmap_fp4_scales(&g.tmSB[e], W[e].scale, (W[e].rows + 127) / 128, tiles, wt)) return CLEARMOE_ECUDA;
     }
-    const cudaError_t e = few           ? launch_fp4_few(g, sms, s)
-                          : k.pair      ? launch_fp4_gemm2(g, k.bn, sms, s)
-                          : k.bn == 128 ? launch_kind<128>(g, sms, s)
-                                        : launch_kind<64>(g, sms, s);
+    cudaError_t e;
+    if constexpr (NE == 1) {
+        e = few ? launch_fp4_few(g, sms, s) : k.pair ? launch_fp4_gemm2(g, k.bn, sms, s) : k.bn == 128 ? launch_kind<128>(g, sms, s) : launch_kind<64>(g, sms, s);
+    } else {
+        e = k.pair ? launch_fp4_gemm2(g, k.bn, sms, s) : k.bn == 128 ? launch_kind<128>(g, sms, s) : launch_kind<64>(g, sms, s);
+    }
     if (e == cudaSuccess) return CLEARMOE_OK;
     (void)cudaGetLastError();
     return CLEARMOE_ECUDA;
@@ -403,7 +409,7 @@ extern "C" {
 
 int clearmoe_fp4_gemm(const clearmoe_fp4* A, const clearmoe_fp4* W, const clearmoe_fp8_epilogue* epi, void* out,
                       int32_t out_dtype, int64_t ldo, void* stream) {
-    cm::Fp4GemmArgs g;
+    cm::Fp4GemmArgs<1> g;
     int rc = cm::check_gemm(A, W, 1, epi, g);
     if (rc || (rc = cm::set_out(g, out, out_dtype, ldo, W->rows))) return rc;
     return cm::run(g, A, W, 1, stream);
@@ -411,7 +417,7 @@ int clearmoe_fp4_gemm(const clearmoe_fp4* A, const clearmoe_fp4* W, const clearm
 
 int clearmoe_fp4_gemm_fp4(const clearmoe_fp4* A, const clearmoe_fp4* W, const clearmoe_fp8_epilogue* epi,
                           const clearmoe_fp4* out, void* stream) {
-    cm::Fp4GemmArgs g;
+    cm::Fp4GemmArgs<1> g;
     int rc = cm::check_gemm(A, W, 1, epi, g);
     if (rc || (rc = cm::check_fp4(out))) return rc;
     if (out->rows != A->rows || out->cols != W->rows) return CLEARMOE_EINVAL;
@@ -429,7 +435,7 @@ int clearmoe_fp4_grouped_gemm(const clearmoe_fp4* A, const clearmoe_fp4* W, int3
     if (E < 1 || E > CM_MAX_E || !W || !offsets || (reinterpret_cast<uintptr_t>(offsets) & 3) ||
         (reinterpret_cast<uintptr_t>(perm) & 3))
         return CLEARMOE_EINVAL;
-    cm::Fp4GemmArgs g;
+    cm::Fp4GemmArgs<CM_MAX_E> g;
     int rc = cm::check_gemm(A, W, E, epi, g);
     if (rc || (rc = cm::set_out(g, out, out_dtype, ldo, W->rows))) return rc;
     g.offsets = offsets;

@@ -21,9 +21,10 @@ __device__ __forceinline__ uint32_t idesc_mxf4(int M, int N, int half) {
 // prefix[E + 1]. A group's tiles start at the scale tile that its first row lies in, so that scales come as they lie;
 // rows of another group in its first and last tile are computed and not stored.
 // By one warp, a group a lane: E + 1 loads one after the other took 2 us.
-__device__ __forceinline__ void f4_groups(const Fp4GemmArgs& a, int bm, int* off, int* prefix, int lane) {
-    int v = lane == 0 && !a.offsets ? 0 : (int)a.M;
-    if (a.offsets && lane <= a.E) v = __ldcg(a.offsets + lane);
+template <class Args>
+__device__ __forceinline__ void f4_groups(const Args& a, int bm, int* off, int* prefix, int lane) {
+    int v = lane == 0 && !Args::GROUPED ? 0 : (int)a.M;
+    if (Args::GROUPED && lane <= a.E) v = __ldcg(a.offsets + lane);
     v = max(v, 0);
 #pragma unroll
     for (int o = 1; o <= CM_MAX_E; o <<= 1) {
@@ -45,7 +46,8 @@ __device__ __forceinline__ void f4_groups(const Fp4GemmArgs& a, int bm, int* off
     }
 }
 // The maps of group 0's tiles, of a product with its kernel's parameters, on their way.
-__device__ __forceinline__ void f4_prefetch_maps(const Fp4GemmArgs& a) {
+template <class Args>
+__device__ __forceinline__ void f4_prefetch_maps(const Args& a) {
     const CUtensorMap* m[4] = {&a.tmA, &a.tmB[0], &a.tmSA, &a.tmSB[0]};
 #pragma unroll
     for (int i = 0; i < 4; ++i) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m[i])) : "memory");
@@ -95,12 +97,14 @@ struct F4Walk {
 };
 
 // The output row of row m of A (-1: none).
-__device__ __forceinline__ int f4_out_row(const Fp4GemmArgs& a, int m, int lo, int hi) {
+template <class Args>
+__device__ __forceinline__ int f4_out_row(const Args& a, int m, int lo, int hi) {
     return m >= lo ? f8_out_row(a, m, hi) : -1;
 }
 
 // A row's 32 columns [nc, nc + 32) to a block, zeros past N.
-__device__ __forceinline__ uint4 f4_block(const Fp4GemmArgs& a, float (&v)[32], int nc, uint32_t& scale) {
+template <class Args>
+__device__ __forceinline__ uint4 f4_block(const Args& a, float (&v)[32], int nc, uint32_t& scale) {
     if (nc + 32 > a.N) {
 #pragma unroll
         for (int i = 0; i < 32; ++i)
@@ -114,8 +118,8 @@ __device__ __forceinline__ uint4 f4_block(const Fp4GemmArgs& a, float (&v)[32], 
     return make_uint4(o[0], o[1], o[2], o[3]);
 }
 // B blocks side by side of output row `row` (-1: none), from column nc on (B == 2: a multiple of 64, as rows of q are long).
-template <int B>
-__device__ __forceinline__ void f4_store_blocks(const Fp4GemmArgs& a, const uint4* block, const uint32_t* scale, int row, int nc) {
+template <int B, class Args>
+__device__ __forceinline__ void f4_store_blocks(const Args& a, const uint4* block, const uint32_t* scale, int row, int nc) {
     if (row < 0 || nc / 2 >= a.ldo) return;
     uint8_t* q = static_cast<uint8_t*>(a.out) + (int64_t)row * a.ldo + nc / 2;
     uint8_t* s = a.out_scale + fp4_scale_word(row, nc >> 7, a.ldos) + (nc >> 5 & 3);
@@ -130,15 +134,15 @@ __device__ __forceinline__ void f4_store_blocks(const Fp4GemmArgs& a, const uint
 }
 
 // 32 rows' 32 columns [nc, nc + 32) (one row a lane: its output row, or -1) to out.
-template <int KIND>
-__device__ __forceinline__ void f4_store32(const Fp4GemmArgs& a, float (&v)[32], int row, int nc, bool wide, int lane) {
+template <int KIND, class Args>
+__device__ __forceinline__ void f4_store32(const Args& a, float (&v)[32], int row, int nc, bool wide, int lane) {
     if constexpr (KIND == FP4_OUT_FP4) {
         uint4 block[1];
         uint32_t scale[1];
         block[0] = f4_block(a, v, nc, scale[0]);
         f4_store_blocks<1>(a, block, scale, row, nc);
     } else {
-        if (a.rows || (wide && nc + 32 <= a.N)) {
+        if ((Args::GROUPED && a.rows) || (wide && nc + 32 <= a.N)) {
             f8_store32<KIND>(a, v, row, nc, wide, lane);
             return;
         }

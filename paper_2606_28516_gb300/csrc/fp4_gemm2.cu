@@ -85,9 +85,9 @@ __device__ __forceinline__ void stage_bf16(const float (&v)[32], uint32_t staged
 }
 
 // KIND: FP8_OUT_F32, FP8_OUT_BF16, FP4_OUT_FP4 or FP4_OUT_BF16_BULK.
-template <int BN_, int KIND>
+template <int BN_, int KIND, int NE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::THREADS, 1)
-    fp4_gemm2_kernel(const __grid_constant__ Fp4GemmArgs a) {
+    fp4_gemm2_kernel(const __grid_constant__ Fp4GemmArgs<NE> a) {
     using C = P4Cfg<BN_, KIND>;
     constexpr int BN = C::BN, STAGES = C::STAGES;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
@@ -355,13 +355,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::TH
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
-template <int BN, int KIND>
-cudaError_t launch_pair(const Fp4GemmArgs& a, int num_sms, cudaStream_t s) {
+template <int BN, int KIND, int NE>
+cudaError_t launch_pair(const Fp4GemmArgs<NE>& a, int num_sms, cudaStream_t s) {
     using C = P4Cfg<BN, KIND>;
     static_assert(C::SMEM <= 227 * 1024);
-    const cudaError_t e = smem_attr_once((const void*)fp4_gemm2_kernel<BN, KIND>, C::SMEM);
+    const cudaError_t e = smem_attr_once((const void*)fp4_gemm2_kernel<BN, KIND, NE>, C::SMEM);
     if (e != cudaSuccess) return e;
-    const int64_t m_tiles = (a.M + 2 * P4_BM - 1) / (2 * P4_BM) + (a.offsets ? a.E - 1 : 0);
+    const int64_t m_tiles = (a.M + 2 * P4_BM - 1) / (2 * P4_BM) + a.E - 1;
     const int64_t tiles = m_tiles * ((a.N + BN - 1) / BN), pairs = num_sms / 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs)));
@@ -373,21 +373,25 @@ cudaError_t launch_pair(const Fp4GemmArgs& a, int num_sms, cudaStream_t s) {
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, fp4_gemm2_kernel<BN, KIND>, a);
+    return cudaLaunchKernelEx(&cfg, fp4_gemm2_kernel<BN, KIND, NE>, a);
 }
 
-template <int KIND>
-cudaError_t launch_kind2(const Fp4GemmArgs& a, int bn, int num_sms, cudaStream_t s) {
+template <int KIND, int NE>
+cudaError_t launch_kind2(const Fp4GemmArgs<NE>& a, int bn, int num_sms, cudaStream_t s) {
     return bn == 256 ? launch_pair<256, KIND>(a, num_sms, s) : launch_pair<128, KIND>(a, num_sms, s);
 }
 
 }  // namespace
 
-cudaError_t launch_fp4_gemm2(const Fp4GemmArgs& a, int bn, int num_sms, cudaStream_t s) {
-    return a.out_kind == FP4_OUT_FP4    ? launch_kind2<FP4_OUT_FP4>(a, bn, num_sms, s)
-           : a.tma_out                  ? launch_kind2<FP4_OUT_BF16_BULK>(a, bn, num_sms, s)
-           : a.out_kind == FP8_OUT_BF16 ? launch_kind2<FP8_OUT_BF16>(a, bn, num_sms, s)
-                                        : launch_kind2<FP8_OUT_F32>(a, bn, num_sms, s);
+template <int NE>
+cudaError_t launch_fp4_gemm2(const Fp4GemmArgs<NE>& a, int bn, int num_sms, cudaStream_t s) {
+    if constexpr (NE == 1) {
+        if (a.out_kind == FP4_OUT_FP4) return launch_kind2<FP4_OUT_FP4>(a, bn, num_sms, s);
+        if (a.tma_out) return launch_kind2<FP4_OUT_BF16_BULK>(a, bn, num_sms, s);
+    }
+    return a.out_kind == FP8_OUT_BF16 ? launch_kind2<FP8_OUT_BF16>(a, bn, num_sms, s) : launch_kind2<FP8_OUT_F32>(a, bn, num_sms, s);
 }
+template cudaError_t launch_fp4_gemm2<1>(const Fp4GemmArgs<1>&, int, int, cudaStream_t);
+template cudaError_t launch_fp4_gemm2<CM_MAX_E>(const Fp4GemmArgs<CM_MAX_E>&, int, int, cudaStream_t);
 
 }  // namespace cm

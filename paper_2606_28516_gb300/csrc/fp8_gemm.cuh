@@ -98,7 +98,8 @@ struct F8Walk {
 };
 
 // The output row of row m of A (-1: none). An index outside the output, of a routing that gave up, is no row.
-__device__ __forceinline__ int f8_out_row(const Fp8GemmArgs& a, int m, int hi) {
+template <class Args>
+__device__ __forceinline__ int f8_out_row(const Args& a, int m, int hi) {
     if (m >= hi) return -1;
     if (!a.rows) return m;
     const int r = __ldcg(a.rows + m);
@@ -204,7 +205,8 @@ __device__ __forceinline__ void f8_transpose(float (&v)[32], int lane) {
 }
 
 // Rows of an fp32 or bf16 output in whole 32-byte pieces.
-__host__ __device__ __forceinline__ bool f8_wide(const Fp8GemmArgs& a) {
+template <class Args>
+__host__ __device__ __forceinline__ bool f8_wide(const Args& a) {
     return (reinterpret_cast<uintptr_t>(a.out) & 31) == 0 && (a.ldo * (a.out_kind == FP8_OUT_BF16 ? 2 : 4) & 31) == 0;
 }
 
@@ -212,8 +214,8 @@ __host__ __device__ __forceinline__ bool f8_wide(const Fp8GemmArgs& a) {
 // pieces (wide) are stored as each lane has them; others transposed first, so that a store's lanes write consecutive
 // columns of one row (an element a lane, rows apart, took 9.8 us for 1,001 x 777 x 1,131 where this takes 5.7; with each
 // row's number shuffled from its lane, 2,922 x 3,453 x 60 to bf16 took 18.5 us where this takes 13.8).
-template <int KIND>
-__device__ __forceinline__ void f8_store32(const Fp8GemmArgs& a, float (&v)[32], int row, int nc, bool wide, int lane) {
+template <int KIND, class Args>
+__device__ __forceinline__ void f8_store32(const Args& a, float (&v)[32], int row, int nc, bool wide, int lane) {
     if (wide && nc + 32 <= a.N) {
         if (row < 0) return;
         if constexpr (KIND == FP8_OUT_BF16) {
