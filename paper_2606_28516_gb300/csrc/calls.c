@@ -195,6 +195,26 @@ static int matrix_at(PyObject* t, int64_t rows, int64_t cols, int device, int64_
     return ok;
 }
 
+/* n elements in a row on GPU `device` (negative: any), or None: their address and dtype. 0 for anything else, with no
+ * exception left. */
+static int row_at(PyObject* t, int64_t n, int device, int64_t* p, int32_t* dt) {
+    *p = 0;
+    *dt = CLEARMOE_F32;
+    if (t == Py_None) return 1;
+    PyObject* capsule = g_to_dlpack ? PyObject_CallOneArg(g_to_dlpack, t) : NULL;
+    const struct exchanged* x = capsule ? PyCapsule_GetPointer(capsule, "dltensor") : NULL;
+    const int ok = x && x->device_type == ON_CUDA && (device < 0 || x->device_id == device) && x->ndim == 1 && x->strides && x->lanes == 1 &&
+                   x->shape[0] == n && (n < 2 || x->strides[0] == 1) &&
+                   ((x->code == CODE_FLOAT && x->bits == 32) || (x->code == CODE_BFLOAT && x->bits == 16));
+    if (ok) {
+        *p = (int64_t)(intptr_t)x->data + (int64_t)x->byte_offset;
+        *dt = x->bits == 16 ? CLEARMOE_BF16 : CLEARMOE_F32;
+    }
+    if (!x) PyErr_Clear();
+    Py_XDECREF(capsule);
+    return ok;
+}
+
 /* A [rows x cols] matrix of any row pitch. */
 static int matrix(PyObject* t, int64_t rows, int64_t cols, int64_t* p, int32_t* dt, int64_t* ld) {
     int64_t shape[2], stride[2];
@@ -381,7 +401,7 @@ static PyObject* fp4_gemm_t(PyObject* self, PyObject* const* args, Py_ssize_t n)
     if (n != 7) return PyErr_Format(PyExc_TypeError, "7 arguments expected, got %zd", n);
     if (!integers(args, 3, 3, v)) return NULL;
     const clearmoe_fp4 *A = PTR(0), *W = PTR(1);
-    if (!stream_and_device(args[6], &s, &device) || !bias_of(args[3], W->rows, &bias, &bias_dt) || !status_of(args[4], &status)) Py_RETURN_NONE;
+    if (!stream_and_device(args[6], &s, &device) || !row_at(args[3], W->rows, device, &bias, &bias_dt) || !status_of(args[4], &status)) Py_RETURN_NONE;
     const clearmoe_fp8_epilogue epi = {AT(bias), bias_dt, (int32_t)v[2], AT(status)};
     const int blocks = PyLong_Check(args[5]);
     if (blocks) {
@@ -411,7 +431,7 @@ static PyObject* rms_norm_t(PyObject* self, PyObject* const* args, Py_ssize_t n)
     a.cols = shape[1];
     if ((args[1] != Py_None && (!matrix_at(args[1], a.rows, a.cols, device, shape, &r, &other, &a.ldr) || other != dt)) ||
         (args[2] != Py_None && (!matrix_at(args[2], a.rows, a.cols, device, shape, &sum, &other, &a.lds) || other != dt)) ||
-        !bias_of(args[3], a.cols, &w, &a.weight_dtype))
+        !row_at(args[3], a.cols, device, &w, &a.weight_dtype))
         Py_RETURN_NONE;
     if (bits) {
         if (!integers(args + 6, 1, 1, &out)) return NULL;

@@ -197,6 +197,27 @@ def test_calls_that_the_binding_refuses(call):
         call()
 
 
+class Elsewhere(Dense):
+    def get_device(self):
+        return 1
+
+
+class Stream0(Stream):
+    device_index = 0
+
+
+@pytest.mark.parametrize("call", [
+    lambda: cm.clearmoe_fp4_quantize(Elsewhere(4, 64), matrix4(4, 64), stream=Stream0()),
+    lambda: cm.clearmoe_fp4_dequantize(matrix4(4, 64), Elsewhere(4, 64), stream=Stream0()),
+    lambda: cm.clearmoe_fp4_gemm(matrix4(4, 64), matrix4(9, 64), Dense(4, 9), bias=Elsewhere(9), stream=Stream0()),
+    lambda: cm.clearmoe_fp4_grouped_gemm(matrix4(4, 64), [matrix4(9, 64)], Elsewhere(2, dtype=I32), Dense(4, 9), stream=Stream0()),
+    lambda: cm.clearmoe_rms_norm(Dense(4, 64), Dense(4, 64), residual=Elsewhere(4, 64), stream=Stream0()),
+])
+def test_tensors_of_another_gpu_are_refused(call):
+    with pytest.raises(ValueError, match="GPU 1"):
+        call()
+
+
 def source(name):
     return re.sub(r"//[^\n]*", "", (CSRC / name).read_text())
 
