@@ -515,7 +515,7 @@ int clearmoe_fp4_grouped_gemm(const clearmoe_fp4* A, const clearmoe_fp4* W, int3
                               int64_t ldo, void* stream);
 
 /* For tests: every later product of 4-bit blocks that the calling thread asks for takes the tcgen05 kernel of this tile
- * width on pairs of SMs (pair 1: 256, 128) or single ones (pair 0: 128, 64), or the kernel for up to 32 rows (16, 0)
+ * width on pairs of SMs (pair 1: 256, 128) or single ones (pair 0: 128, 64), or the kernel for up to 128 rows (16, 0)
  * where the product is not grouped; (0, 0) restores the choice by size. EINVAL for another kernel. */
 int clearmoe_debug_fp4_kernel(int32_t width, int32_t pair);
 

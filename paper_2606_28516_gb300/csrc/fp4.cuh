@@ -111,8 +111,9 @@ struct Fp4GemmArgs {
 template <int NE>
 cudaError_t launch_fp4_gemm2(const Fp4GemmArgs<NE>& a, int bn, int num_sms, cudaStream_t s);
 // A product of at most FP4_FEW_MAX rows in one group: tmA in boxes of fp4_few_rows(M) rows, tmB of 128.
-constexpr int FP4_FEW_MAX = 32;
+constexpr int FP4_FEW_MAX = 128;
 int fp4_few_rows(int64_t M);
+bool fp4_few_pays(int64_t M, int N, int nkb, int num_sms);
 cudaError_t launch_fp4_few(const Fp4GemmArgs<1>& a, int num_sms, cudaStream_t s);
 int check_fp4(const clearmoe_fp4* m);
 // Scale tiles [tile_rows x tile_cols] of 512 bytes as a tensor map, boxes of two tiles side by side x box_rows.

@@ -4,7 +4,8 @@
 // stages it has room for at once; its sums go to shared memory, and CTA r of the cluster adds the parts of every KS-th row
 // of A in CTA order (the result does not depend on which comes first) and finishes it.
 //
-//   4 warps      epilogue: TMEM lane quarters (32 columns of the output each) to shared memory, then the sums over the cluster
+//   4 warps      epilogue: TMEM lane quarters (32 columns of the output each) to shared memory, then the sums over the cluster,
+//                a row a warp, four columns a lane
 //   1 warp       TMEM allocation, tcgen05.cp of the scales, tcgen05.mma and commits
 //   1 warp       TMA producer
 // Waits are bounded as in fp4_gemm.cu; a CTA that gave up still takes part in the cluster's two barriers.
@@ -30,7 +31,7 @@ struct FewCfg {
     static constexpr int STAGE_BYTES = W_BYTES + X_BYTES + 2 * F4_SF;
     static constexpr int STAGES = 108 * 1024 / STAGE_BYTES;  // two CTAs an SM
     static constexpr int SF_COL = NT;
-    static constexpr int TMEM_COLS = NT + 16 <= 32 ? 32 : 64;
+    static constexpr int TMEM_COLS = NT + 16 <= 32 ? 32 : NT + 16 <= 64 ? 64 : NT + 16 <= 128 ? 128 : 256;
     static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + 8 * (2 * STAGES + 1) + 16;
     static_assert(128 * NT * 4 <= STAGES * STAGE_BYTES);  // the sums, once the stages are read
     static_assert(SMEM <= 113 * 1024);
@@ -47,31 +48,55 @@ __device__ __forceinline__ void umma_few(uint32_t d_tmem, uint64_t a_desc, uint6
         "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
         : "memory");
 }
-__device__ __forceinline__ float ld_cluster_f32(uint32_t addr_cluster) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr_cluster) : "memory");
+__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t addr_cluster) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr_cluster) : "memory");
     return v;
 }
 
-// The sum of row m and column n, a column a lane, to the output.
+// The sums of row m and columns n .. n + 3, four a lane, to the output; vec: its rows are in whole pieces of four.
 template <int KIND>
-__device__ __forceinline__ void finish(const Fp4GemmArgs<1>& a, float v, int m, int n, int lane) {
-    if (a.act == CLEARMOE_ACT_GELU) v = gelu_pair_f32(make_float2(v, v)).x;
-    if (a.act == CLEARMOE_ACT_RELU) v = v < 0.f ? 0.f : v;  // NaN stays NaN
-    if constexpr (KIND == FP4_OUT_FP4) {  // the warp's 32 columns are a block
-        if (n >= a.N) v = 0.f;
-        const uint32_t s = fp4_scale_byte(__reduce_max_sync(0xFFFFFFFFu, abs_bits(v)));
-        const uint32_t code = fp4_pack8(v * fp8_inverse_scale(s), 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f) & 15u;
-        uint32_t w = code << (4 * (lane & 7));
+__device__ __forceinline__ void finish(const Fp4GemmArgs<1>& a, float4 s, const float4& bias, int m, int n, bool vec, int lane) {
+    float v[4] = {s.x + bias.x, s.y + bias.y, s.z + bias.z, s.w + bias.w};
+    if (a.act == CLEARMOE_ACT_GELU) {
+        const float2 p = gelu_pair_f32(make_float2(v[0], v[1])), q = gelu_pair_f32(make_float2(v[2], v[3]));
+        v[0] = p.x, v[1] = p.y, v[2] = q.x, v[3] = q.y;
+    } else if (a.act == CLEARMOE_ACT_RELU) {
 #pragma unroll
-        for (int o = 1; o < 8; o <<= 1) w |= __shfl_xor_sync(0xFFFFFFFFu, w, o);
-        if ((lane & 7) == 0 && n / 2 < a.ldo) *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.out) + (int64_t)m * a.ldo + n / 2) = w;
-        if (lane == 0 && n / 2 < a.ldo) a.out_scale[fp4_scale_word(m, n >> 7, a.ldos) + (n >> 5 & 3)] = (uint8_t)s;
-    } else if (n < a.N) {
-        if constexpr (KIND == FP8_OUT_BF16)
-            static_cast<uint16_t*>(a.out)[(int64_t)m * a.ldo + n] = f32_to_bf16(v);
-        else
-            static_cast<float*>(a.out)[(int64_t)m * a.ldo + n] = v;
+        for (int i = 0; i < 4; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];  // NaN stays NaN
+    }
+    if constexpr (KIND == FP4_OUT_FP4) {  // eight lanes' columns are a block
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (n + i >= a.N) v[i] = 0.f;
+        float top = max_abs3(max_abs(v[0], v[1]), v[2], v[3]);
+#pragma unroll
+        for (int o = 4; o; o >>= 1) top = max_abs(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        const uint32_t scale = fp4_scale_byte(abs_bits(top));
+        const float inv = fp8_inverse_scale(scale);
+        if (n / 2 >= a.ldo) return;
+        *reinterpret_cast<uint16_t*>(static_cast<uint8_t*>(a.out) + (int64_t)m * a.ldo + n / 2) =
+            (uint16_t)fp4_pack8(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv, 0.f, 0.f, 0.f, 0.f);
+        if ((lane & 7) == 0) a.out_scale[fp4_scale_word(m, n >> 7, a.ldos) + (n >> 5 & 3)] = (uint8_t)scale;
+    } else {
+        constexpr bool BF16 = KIND == FP8_OUT_BF16;
+        uint16_t* b = static_cast<uint16_t*>(a.out) + (int64_t)m * a.ldo + n;
+        float* f = static_cast<float*>(a.out) + (int64_t)m * a.ldo + n;
+        if (vec && n + 4 <= a.N) {
+            if constexpr (BF16)
+                *reinterpret_cast<uint2*>(b) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+            else
+                *reinterpret_cast<float4*>(f) = make_float4(v[0], v[1], v[2], v[3]);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (n + i >= a.N) break;
+            if constexpr (BF16)
+                b[i] = f32_to_bf16(v[i]);
+            else
+                f[i] = v[i];
+        }
     }
 }
 
@@ -188,33 +213,42 @@ __global__ void __launch_bounds__(FewCfg<NT_>::THREADS, 2) fp4_few_kernel(const 
     cluster_sync();  // every CTA's sums are in its shared memory
     tc_fence_after();
     if (warp < 4) {
-        const int n = n0 + warp * 32 + lane;
-        const uint32_t own = smem_u32(s_sum + warp * 32 + lane);
-        float bias = 0.f;
-        if (a.bias && n < a.N)
-            bias = a.bias_bf16 ? bf16_to_f32(__ldcg(static_cast<const uint16_t*>(a.bias) + n)) : __ldcg(static_cast<const float*>(a.bias) + n);
-        // two rows at a time, every CTA's part of both asked for before the first is added
-        for (int m0 = rank; m0 < (int)a.M; m0 += 2 * split) {
-            float part[2][8];
+        // Row rank + split j is warp j % 4's, four columns a lane; every CTA's part of it is asked for before the first is added.
+        const int n = n0 + 4 * lane;
+        float4 bias = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (a.bias) {
+            float b[4];
 #pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                const uint32_t at = r < split ? map_to_rank(own, r) : 0;
+            for (int i = 0; i < 4; ++i)
+                b[i] = n + i >= a.N  ? 0.f
+                       : a.bias_bf16 ? bf16_to_f32(__ldcg(static_cast<const uint16_t*>(a.bias) + n + i))
+                                     : __ldcg(static_cast<const float*>(a.bias) + n + i);
+            bias = make_float4(b[0], b[1], b[2], b[3]);
+        }
+        const int piece = KIND == FP8_OUT_BF16 ? 8 : 16;
+        const bool vec = (reinterpret_cast<uintptr_t>(a.out) & (piece - 1)) == 0 && a.ldo % 4 == 0;
+        uint32_t part[8];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int m = m0 + i * split;
-                    part[i][r] = r < split && m < (int)a.M ? ld_cluster_f32(at + m * 512) : 0.f;
-                }
+        for (int r = 0; r < 8; ++r) part[r] = map_to_rank(smem_u32(s_sum + 4 * lane), r < split ? r : 0);
+        constexpr int R = NT == 16 ? 1 : 2;  // rows of a warp at a time
+        for (int m0 = rank + split * warp; m0 < (int)a.M; m0 += 4 * R * split) {
+            float4 p[R][8];
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const int m = min(m0 + 4 * i * split, (int)a.M - 1);
+#pragma unroll
+                for (int r = 0; r < 8; ++r)
+                    if (r < split) p[i][r] = ld_cluster_f32x4(part[r] + m * 512);
             }
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int m = m0 + i * split;
+            for (int i = 0; i < R; ++i) {
+                const int m = m0 + 4 * i * split;
                 if (m >= (int)a.M) break;
-                float v = part[i][0];
+                float4 v = p[i][0];
 #pragma unroll
                 for (int r = 1; r < 8; ++r)
-                    if (r < split) v += part[i][r];
-                v += bias;
-                finish<KIND>(a, v, m, n, lane);
+                    if (r < split) v = make_float4(v.x + p[i][r].x, v.y + p[i][r].y, v.z + p[i][r].z, v.w + p[i][r].w);
+                finish<KIND>(a, v, bias, m, n, vec, lane);
             }
         }
     }
@@ -251,23 +285,39 @@ cudaError_t launch_nt(const Fp4GemmArgs<1>& a, int split, cudaStream_t s) {
 
 }  // namespace
 
-int fp4_few_rows(int64_t M) { return M <= 16 ? 16 : 32; }
+int fp4_few_rows(int64_t M) { return M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128; }
 
-// CTAs that share a tile's K: as many as leave each an SM; where the stages a CTA asks for at once are then less than its
-// part, two CTAs an SM. 4 x 4,096 x 4,096: four CTAs of four stages 3.8 us, eight of two 4.2, two 4.4; 16 x 1,024 x 4,096:
-// eight 3.3, four 3.6; 3 x 8,192 x 8,192: four CTAs, two an SM, 8.5, two 9.0.
-static int few_split(int tiles, int nkb, int num_sms) {
-    const int stages = FewCfg<16>::STAGES;
+// CTAs that share a tile's K: as many as leave each an SM and two stages; where the stages a CTA asks for at once are then
+// less than its part, two CTAs an SM. 4 x 4,096 x 4,096: four CTAs of four stages 3.8 us, eight of two 4.2, two 4.4; 16 x
+// 1,024 x 4,096: eight 3.3, four 3.6; 3 x 8,192 x 8,192: four CTAs, two an SM, 8.5, two 9.0; 32 x 2,048 x 2,048: four of two
+// stages 3.2, eight of one 4.8.
+static int few_split(int N, int nkb, int num_sms) {
+    const int tiles = (N + 127) / 128, stages = FewCfg<16>::STAGES;
     int split = num_sms / tiles;
     if (split < 1 || nkb > split * stages) split = 2 * num_sms / tiles;
     split = split > 8 ? 8 : split;
-    split = split > nkb ? nkb : split;
+    split = split > nkb / 2 ? nkb / 2 : split;
     return split < 1 ? 1 : split;
 }
 
+// Whether the kernel is the better one: of the 0.17 us that a stage of K takes a tile of 64 columns and 128 rows, the
+// cluster saves all but its split's part, and a row takes it 0.025 us to add and store. Us, this kernel and that one: 1 x 1,024 x
+// 4,096 3.1, 5.1; 16 x 4,096 x 4,096 3.8, 5.1; 32 x 2,048 x 2,048 3.2, 3.8; 64 x 4,096 x 4,096 5.0, 5.5; 128 x 512 x 8,192
+// 5.7, 8.2; otherwise 1 x 768 x 768 2.9, 2.7; 32 x 4,096 x 1,024 3.3, 3.1; 128 x 4,096 x 4,096 6.7, 6.1.
+bool fp4_few_pays(int64_t M, int N, int nkb, int num_sms) {
+    const int64_t split = few_split(N, nkb, num_sms);
+    // with two CTAs an SM the weights are what takes time: 32 x 8,192 x 8,192 9.4 us against 10.1, 100 x 8,192 x 8,192 12.0 against 10.5
+    if (M > ((N + 127) / 128 * split > num_sms ? 32 : FP4_FEW_MAX)) return false;
+    return 7 * nkb * (split - 1) > M * split;
+}
+
 cudaError_t launch_fp4_few(const Fp4GemmArgs<1>& a, int num_sms, cudaStream_t s) {
-    const int split = few_split((a.N + 127) / 128, a.nkb, num_sms);
-    return fp4_few_rows(a.M) == 16 ? launch_nt<16>(a, split, s) : launch_nt<32>(a, split, s);
+    const int split = few_split(a.N, a.nkb, num_sms);
+    const int nt = fp4_few_rows(a.M);
+    return nt == 16   ? launch_nt<16>(a, split, s)
+           : nt == 32 ? launch_nt<32>(a, split, s)
+           : nt == 64 ? launch_nt<64>(a, split, s)
+                      : launch_nt<128>(a, split, s);
 }
 
 }  // namespace cm

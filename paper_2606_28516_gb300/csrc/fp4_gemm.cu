@@ -304,10 +304,7 @@ Pick pick(const Fp4GemmArgs<NE>& g, int num_sms) {
                                     {{128, 0}, 3550, 370, 564, 0, 970, 1.06, {2910, 4400, 4730, 2250}},
                                     {{128, 1}, 5960, 267, 473, 394, 1140, 0.84, {1630, 3780, 4370, 1470}},
                                     {{256, 1}, 5890, 516, 788, 144, 2420, 0.86, {2870, 6850, 8560, 2830}}};
-    // Few rows, while at least two CTAs share a tile's K: 16 x 1,024 x 4,096 3.2 us against 5.2 (64, 0), 3 x 8,192 x 8,192 8.5
-    // against 9.9, 32 x 4,096 x 4,096 5.1 against 5.6; otherwise 16 x 32,768 x 1,024 8.9 against 6.6, and with 32 rows of few
-    // stages 32 x 768 x 768 4.5 against 2.9.
-    if (NE == 1 && g.M <= FP4_FEW_MAX && 2 * ((g.N + 127) / 128) <= num_sms && (g.M <= 16 || g.nkb >= 8)) return {FEW_WIDTH, 0};
+    if (NE == 1 && fp4_few_pays(g.M, g.N, g.nkb, num_sms)) return {FEW_WIDTH, 0};
     const int store = g.out_kind == FP4_OUT_FP4 ? 3 : !f8_wide(g) ? 2 : g.out_kind == FP8_OUT_F32 ? 1 : 0;
     Pick best = all[0].pick;
     double least = 1e30;

@@ -213,7 +213,9 @@ def test_every_kernel(kernel, M, N, K, act):
 
 @pytest.mark.parametrize("M,N,K,act", [(1, 1, 1, cm.ACT_NONE), (16, 40, 130, cm.ACT_GELU), (17, 5003, 257, cm.ACT_RELU),
                                        (32, 700, 2048, cm.ACT_GELU), (32, 96, 9000, cm.ACT_NONE), (7, 40000, 512, cm.ACT_NONE),
-                                       (3, 128, 1792, cm.ACT_GELU), (29, 20000, 64, cm.ACT_RELU), (33, 300, 300, cm.ACT_NONE)])
+                                       (3, 128, 1792, cm.ACT_GELU), (29, 20000, 64, cm.ACT_RELU), (33, 300, 300, cm.ACT_NONE),
+                                       (64, 1024, 4096, cm.ACT_GELU), (128, 130, 2048, cm.ACT_RELU), (99, 515, 9000, cm.ACT_NONE),
+                                       (129, 64, 512, cm.ACT_NONE)])
 def test_kernel_for_few_rows(M, N, K, act):
     """K split over one to eight CTAs, one to many tiles, each number of rows; the same bits each time."""
     rng = np.random.default_rng(M + N + K)
@@ -432,7 +434,7 @@ def test_two_streams_and_two_graphs():
 def test_waits_that_run_out(kernel, blocks):
     """Under limits of 1 to 200 microseconds the kernels give up between their copies, let what is in flight land, and
     return; the call reports CLEARMOE_ETIMEOUT or completes, and the next call with the usual limit gives the same bits."""
-    M = 32 if kernel[0] == 16 else 3000
+    M = 100 if kernel[0] == 16 else 3000
     A, W, av, wv = make(np.random.default_rng(29), M, 1024, 16384)
     out = cm.fp4_matrix(M, 1024) if blocks else torch.empty(M, 1024, device="cuda", dtype=torch.bfloat16)
     bits = out.q if blocks else out
