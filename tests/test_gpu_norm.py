@@ -260,3 +260,21 @@ def test_two_streams():
             cm.clearmoe_rms_norm(x, o, stream=s)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+@pytest.mark.parametrize("pad", [0, 3])
+def test_sums_of_every_bf16_value(pad):
+    """Every value of bf16 (subnormal, infinite and NaN ones too) plus others: the sum that is stored is the rounded fp32 sum."""
+    bits = torch.arange(65536, dtype=torch.int32, device="cuda")
+    g = torch.Generator("cuda").manual_seed(3)
+    x = bits.to(torch.int16).view(torch.bfloat16).view(1024, 64)
+    for k in range(16):
+        order = torch.randperm(65536, device="cuda", generator=g) if k < 12 else (bits + (k - 13) * 129) % 65536  # and its neighbours
+        r = bits[order.long()].to(torch.int16).view(torch.bfloat16).view(1024, 64)
+        a, b, s, out = (torch.zeros(1024, 64 + pad, device="cuda", dtype=torch.bfloat16)[:, :64] for _ in range(4))
+        a.copy_(x)
+        b.copy_(r)
+        cm.clearmoe_rms_norm(a, out, residual=b, sum_out=s)
+        want = (x.float() + r.float()).to(torch.bfloat16)
+        assert torch.equal(s.isnan(), want.isnan())
+        assert torch.equal(s[~s.isnan()], want[~want.isnan()])
