@@ -57,20 +57,20 @@ __device__ __forceinline__ void weights(const NormArgs& a, int k, float2 (&w)[8]
             if (!a.w_bf16) {
 #pragma unroll
                 for (int i = 0; i < P; i += 4) {
-                    const float4 q = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(a.w) + n + i));
+                    const float4 q = __ldcg(reinterpret_cast<const float4*>(static_cast<const float*>(a.w) + n + i));
                     v[i] = q.x, v[i + 1] = q.y, v[i + 2] = q.z, v[i + 3] = q.w;
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < P; i += 4) {
-                    const uint2 q = __ldg(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(a.w) + n + i));
+                    const uint2 q = __ldcg(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(a.w) + n + i));
                     v[i] = bf16_lo(q.x), v[i + 1] = bf16_hi(q.x), v[i + 2] = bf16_lo(q.y), v[i + 3] = bf16_hi(q.y);
                 }
             }
         } else {
 #pragma unroll
             for (int i = 0; i < P; ++i)
-                v[i] = a.w_bf16 ? bf16_to_f32(__ldg(static_cast<const uint16_t*>(a.w) + n + i)) : __ldg(static_cast<const float*>(a.w) + n + i);
+                v[i] = a.w_bf16 ? bf16_to_f32(__ldcg(static_cast<const uint16_t*>(a.w) + n + i)) : __ldcg(static_cast<const float*>(a.w) + n + i);
         }
     }
 #pragma unroll

@@ -232,6 +232,12 @@ def test_reads_and_releases_after_the_wait(name):
         assert "pdl_launch_dependents();" not in body[:wait]
 
 
+@pytest.mark.parametrize("name", ["fp4.cu", "fp4_gemm.cuh", "fp4_gemm.cu", "fp4_gemm2.cu", "fp4_few.cu", "norm.cu", "lane16.cuh"])
+def test_no_loads_for_data_that_never_changes(name):
+    """A kernel that starts beside its predecessor lives while that one still writes: what ld.global.nc must not read."""
+    assert "__ldg(" not in source(name) and ".nc" not in source(name) and "__restrict__" not in source(name)
+
+
 def kernel(name):
     s = source(name)
     return s[s.index("__global__ void"):s.index("cudaError_t launch")]

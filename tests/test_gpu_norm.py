@@ -278,3 +278,20 @@ def test_sums_of_every_bf16_value(pad):
         want = (x.float() + r.float()).to(torch.bfloat16)
         assert torch.equal(s.isnan(), want.isnan())
         assert torch.equal(s[~s.isnan()], want[~want.isnan()])
+
+
+def test_weights_and_bias_just_written():
+    """A norm's weights and a product's bias that the kernel right before wrote, new ones each time."""
+    x, W = torch.randn(300, 256, device="cuda"), cm.fp4_matrix(384, 256)
+    w, b, q = torch.empty(256, device="cuda"), torch.empty(384, device="cuda"), cm.fp4_matrix(300, 256)
+    cm.clearmoe_fp4_quantize(torch.randn(384, 256, device="cuda"), W)
+    outs = []
+    for i in range(60):
+        w.fill_(float(2 ** (i % 5)))
+        cm.clearmoe_rms_norm(x, q, weight=w)
+        b.fill_(float(i % 7))
+        outs.append(torch.empty(300, 384, device="cuda"))
+        cm.clearmoe_fp4_gemm(q, W, outs[-1], bias=b)
+    base = outs[0]
+    for i, out in enumerate(outs):  # powers of two scale every sum exactly; the bias is added with one rounding
+        assert torch.equal(out, base * 2.0 ** (i % 5) + float(i % 7))
