@@ -53,6 +53,14 @@ class clearmoe_fp4(ctypes.Structure):
     _fields_ = [("q", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64)]
 
 
+class _PlacedFp8(clearmoe_fp8):  # and the GPU it lies on (-1: not known), for the calls that look
+    _fields_ = [("device", ctypes.c_int32)]
+
+
+class _PlacedFp4(clearmoe_fp4):
+    _fields_ = [("device", ctypes.c_int32)]
+
+
 class clearmoe_norm(ctypes.Structure):
     _fields_ = [("x", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("sum", ctypes.c_void_p), ("weight", ctypes.c_void_p),
                 ("ldx", ctypes.c_int64), ("ldr", ctypes.c_int64), ("lds", ctypes.c_int64), ("rows", ctypes.c_int64),
@@ -453,6 +461,14 @@ def clearmoe_route_noalloc(x, Wg, bg, idx, counts, offsets, perm, status=None,
 
 
 # ---------------------------------------------------------------- 8-bit blocks with power-of-two scales
+def _device_of(q, scale) -> int:
+    """The GPU that both parts of a matrix in blocks lie on, -1 where they do not say."""
+    at = [t.get_device() if hasattr(t, "get_device") else -1 for t in (q, scale)]
+    if at[0] != at[1]:
+        raise ValueError(f"q and scale of one matrix lie on GPU {at[0]} and GPU {at[1]}")
+    return at[0]
+
+
 class Fp8Matrix:
     """A matrix [rows x cols] in 8-bit blocks (clearmoe_fp8): q, one byte per element in rows of cols rounded up
     to 128 (float8_e4m3fn or uint8), and its scale bytes, rows of 4 ceil(cols / 512); 128-row blocks for weights,
@@ -465,8 +481,11 @@ class Fp8Matrix:
                 raise ValueError(f"{name} of a {rows} x {cols} matrix in 8-bit blocks is one byte per element of {shape}, "
                                  f"got {tuple(t.shape)} {t.dtype}")
         self.q, self.scale, self.rows, self.cols, self.weight = q, scale, rows, cols, weight
-        self.c = clearmoe_fp8(_ptr(q), _ptr(scale), rows, cols)
-        self.ref, self.addr = ctypes.pointer(self.c), ctypes.addressof(self.c)
+        self.c = _PlacedFp8(_ptr(q), _ptr(scale), rows, cols, _device_of(q, scale))
+        self.ref, self.addr = ctypes.cast(ctypes.pointer(self.c), ctypes.POINTER(clearmoe_fp8)), ctypes.addressof(self.c)
+
+    def get_device(self) -> int:
+        return self.c.device
 
 
 def fp8_pitch(cols: int) -> int:
@@ -649,8 +668,11 @@ class Fp4Matrix:
                 raise ValueError(f"{name} of a {rows} x {cols} matrix in 4-bit blocks is bytes of {shape}, got {tuple(t.shape)} "
                                  f"{t.dtype}")
         self.q, self.scale, self.rows, self.cols = q, scale, rows, cols
-        self.c = clearmoe_fp4(_ptr(q), _ptr(scale), rows, cols)
-        self.ref, self.addr = ctypes.pointer(self.c), ctypes.addressof(self.c)
+        self.c = _PlacedFp4(_ptr(q), _ptr(scale), rows, cols, _device_of(q, scale))
+        self.ref, self.addr = ctypes.cast(ctypes.pointer(self.c), ctypes.POINTER(clearmoe_fp4)), ctypes.addressof(self.c)
+
+    def get_device(self) -> int:
+        return self.c.device
 
     @property
     def weight(self):
@@ -700,7 +722,7 @@ def clearmoe_fp4_quantize(x, out: Fp4Matrix, gather=None, stream=None) -> None:
             if code:
                 raise ClearMoEError(code, "clearmoe_fp4_quantize")
             return
-    _here(stream, x, gather)
+    _here(stream, x, gather, out)
     p, dt, ld = _matrix(x, out.rows if gather is None else None, out.cols, "x")
     _check(lib().clearmoe_fp4_quantize(p, x.shape[0], dt, ld, _int32(gather, out.rows, "gather"), o, _stream(stream)),
            "clearmoe_fp4_quantize")
@@ -709,7 +731,7 @@ def clearmoe_fp4_quantize(x, out: Fp4Matrix, gather=None, stream=None) -> None:
 def clearmoe_fp4_dequantize(m: Fp4Matrix, out, stream=None) -> None:
     """The values m stands for, rounded to out's dtype (bf16 or fp32)."""
     r = _fp4(m, "m")
-    _here(stream, out)
+    _here(stream, m, out)
     p, dt, ld = _matrix(out, m.rows, m.cols, "out")
     _check(lib().clearmoe_fp4_dequantize(r, p, dt, ld, _stream(stream)), "clearmoe_fp4_dequantize")
 
@@ -725,7 +747,7 @@ def clearmoe_fp4_gemm(A: Fp4Matrix, W: Fp4Matrix, out, bias=None, act: int = ACT
                 raise ClearMoEError(code, "clearmoe_fp4_gemm_fp4" if blocks else "clearmoe_fp4_gemm")
             return
     a, w = _fp4(A, "A"), _fp4(W, "W")
-    _here(stream, bias, status, None if blocks else out)
+    _here(stream, A, W, bias, status, out)
     epi = _epilogue(bias, act, status, W.rows)
     if blocks:
         _check(lib().clearmoe_fp4_gemm_fp4(a, w, epi, out.ref, _stream(stream)), "clearmoe_fp4_gemm_fp4")
@@ -742,7 +764,7 @@ def clearmoe_fp4_grouped_gemm(A: Fp4Matrix, W, offsets, out, perm=None, bias=Non
         raise ValueError("a grouped product needs matrices and the offsets of their rows")
     for m in W:
         _fp4(m, "every W")
-    _here(stream, offsets, out, perm, bias, status)
+    _here(stream, A, *W, offsets, out, perm, bias, status)
     off, rows = _int32(offsets, len(W) + 1, "offsets"), _int32(perm, A.rows, "perm")
     p, dt, ld = _matrix(out, A.rows, W[0].rows, "out")
     arr = (clearmoe_fp4 * len(W))(*[m.c for m in W])
@@ -773,7 +795,7 @@ def clearmoe_rms_norm(x, out, residual=None, sum_out=None, weight=None, eps: flo
         if code:
             raise ClearMoEError(code, "clearmoe_rms_norm" + ("", "_fp4", "_fp8")[bits // 4])
         return
-    _here(stream, x, residual, sum_out, weight, None if bits else out)
+    _here(stream, x, residual, sum_out, weight, out)
     if len(x.shape) != 2:
         raise ValueError(f"x must be a matrix, got {tuple(x.shape)}")
     rows, cols = x.shape

@@ -330,6 +330,18 @@ static PyObject* ffn_fp8_t(PyObject* self, PyObject* const* args, Py_ssize_t n) 
 }
 
 /* ---- 4-bit blocks and the norm ---- */
+/* Matrices in blocks as the binding hands them over: the library's structure and, behind it, their GPU (-1: not known). */
+struct placed_fp4 {
+    clearmoe_fp4 m;
+    int32_t device;
+};
+struct placed_fp8 {
+    clearmoe_fp8 m;
+    int32_t device;
+};
+static int here(int32_t at, int device) { return at < 0 || device < 0 || at == device; }
+#define HERE4(p) here(((const struct placed_fp4*)(p))->device, device)
+#define HERE8(p) here(((const struct placed_fp8*)(p))->device, device)
 static int (*g_fp4_quantize)(const void*, int64_t, int32_t, int64_t, const int32_t*, const clearmoe_fp4*, void*);
 static int (*g_fp4_gemm)(const clearmoe_fp4*, const clearmoe_fp4*, const clearmoe_fp8_epilogue*, void*, int32_t, int64_t, void*);
 static int (*g_fp4_gemm_fp4)(const clearmoe_fp4*, const clearmoe_fp4*, const clearmoe_fp8_epilogue*, const clearmoe_fp4*, void*);
@@ -385,7 +397,7 @@ static PyObject* fp4_quantize_t(PyObject* self, PyObject* const* args, Py_ssize_
     if (n != 3) return PyErr_Format(PyExc_TypeError, "3 arguments expected, got %zd", n);
     if (!integers(args + 1, 1, 1, v)) return NULL;
     const clearmoe_fp4* out = PTR(0);
-    if (!stream_and_device(args[2], &s, &device) || !matrix_at(args[0], out->rows, out->cols, device, shape, &x, &dt, &ld)) Py_RETURN_NONE;
+    if (!stream_and_device(args[2], &s, &device) || !HERE4(out) || !matrix_at(args[0], out->rows, out->cols, device, shape, &x, &dt, &ld)) Py_RETURN_NONE;
     Py_BEGIN_ALLOW_THREADS
     rc = g_fp4_quantize(AT(x), shape[0], dt, ld, NULL, out, AT(s));
     Py_END_ALLOW_THREADS
@@ -401,11 +413,12 @@ static PyObject* fp4_gemm_t(PyObject* self, PyObject* const* args, Py_ssize_t n)
     if (n != 7) return PyErr_Format(PyExc_TypeError, "7 arguments expected, got %zd", n);
     if (!integers(args, 3, 3, v)) return NULL;
     const clearmoe_fp4 *A = PTR(0), *W = PTR(1);
-    if (!stream_and_device(args[6], &s, &device) || !row_at(args[3], W->rows, device, &bias, &bias_dt) || !status_of(args[4], &status)) Py_RETURN_NONE;
+    if (!stream_and_device(args[6], &s, &device) || !HERE4(A) || !HERE4(W) || !row_at(args[3], W->rows, device, &bias, &bias_dt) || !status_of(args[4], &status)) Py_RETURN_NONE;
     const clearmoe_fp8_epilogue epi = {AT(bias), bias_dt, (int32_t)v[2], AT(status)};
     const int blocks = PyLong_Check(args[5]);
     if (blocks) {
         if (!integers(args + 5, 1, 1, &out)) return NULL;
+        if (!HERE4(AT(out))) Py_RETURN_NONE;
     } else if (!matrix_at(args[5], A->rows, W->rows, device, shape, &out, &dt, &ld)) {
         Py_RETURN_NONE;
     }
@@ -435,6 +448,7 @@ static PyObject* rms_norm_t(PyObject* self, PyObject* const* args, Py_ssize_t n)
         Py_RETURN_NONE;
     if (bits) {
         if (!integers(args + 6, 1, 1, &out)) return NULL;
+        if (!(bits == 8 ? HERE8(AT(out)) : HERE4(AT(out)))) Py_RETURN_NONE;
     } else if (!matrix_at(args[6], a.rows, a.cols, device, shape, &out, &out_dt, &ldo)) {
         Py_RETURN_NONE;
     }

@@ -206,12 +206,31 @@ class Stream0(Stream):
     device_index = 0
 
 
+def matrix4_elsewhere(rows, cols):
+    return cm.Fp4Matrix(Elsewhere(rows, cm.fp4_pitch(cols)), Elsewhere(-(-rows // 128), -(-cols // 128), 512), rows, cols)
+
+
+def matrix8_elsewhere(rows, cols):
+    return cm.Fp8Matrix(Elsewhere(rows, cm.fp8_pitch(cols)), Elsewhere(rows, cm.fp8_scale_pitch(cols)), rows, cols)
+
+
 @pytest.mark.parametrize("call", [
     lambda: cm.clearmoe_fp4_quantize(Elsewhere(4, 64), matrix4(4, 64), stream=Stream0()),
     lambda: cm.clearmoe_fp4_dequantize(matrix4(4, 64), Elsewhere(4, 64), stream=Stream0()),
     lambda: cm.clearmoe_fp4_gemm(matrix4(4, 64), matrix4(9, 64), Dense(4, 9), bias=Elsewhere(9), stream=Stream0()),
     lambda: cm.clearmoe_fp4_grouped_gemm(matrix4(4, 64), [matrix4(9, 64)], Elsewhere(2, dtype=I32), Dense(4, 9), stream=Stream0()),
     lambda: cm.clearmoe_rms_norm(Dense(4, 64), Dense(4, 64), residual=Elsewhere(4, 64), stream=Stream0()),
+    lambda: cm.clearmoe_fp4_quantize(Dense(4, 64), matrix4_elsewhere(4, 64), stream=Stream0()),
+    lambda: cm.clearmoe_fp4_quantize(Dense(9, 64), matrix4_elsewhere(4, 64), gather=Dense(4, dtype=I32), stream=Stream0()),
+    lambda: cm.clearmoe_fp4_dequantize(matrix4_elsewhere(4, 64), Dense(4, 64), stream=Stream0()),
+    lambda: cm.clearmoe_fp4_gemm(matrix4_elsewhere(4, 64), matrix4(9, 64), Dense(4, 9), stream=Stream0()),
+    lambda: cm.clearmoe_fp4_gemm(matrix4(4, 64), matrix4_elsewhere(9, 64), matrix4(4, 9), stream=Stream0()),
+    lambda: cm.clearmoe_fp4_gemm(matrix4(4, 64), matrix4(9, 64), matrix4_elsewhere(4, 9), stream=Stream0()),
+    lambda: cm.clearmoe_fp4_grouped_gemm(matrix4(4, 64), [matrix4(9, 64), matrix4_elsewhere(9, 64)], Dense(3, dtype=I32), Dense(4, 9),
+                                         stream=Stream0()),
+    lambda: cm.clearmoe_rms_norm(Dense(4, 64), matrix4_elsewhere(4, 64), stream=Stream0()),
+    lambda: cm.clearmoe_rms_norm(Dense(4, 64), matrix8_elsewhere(4, 64), stream=Stream0()),
+    lambda: cm.Fp4Matrix(Elsewhere(4, 32), Dense(1, 1, 512), 4, 64),
 ])
 def test_tensors_of_another_gpu_are_refused(call):
     with pytest.raises(ValueError, match="GPU 1"):

@@ -525,3 +525,17 @@ def test_empty_matrices_are_refused():
         cm.clearmoe_fp4_quantize(torch.empty(0, 64, device="cuda"), cm.fp4_matrix(0, 64))
     with pytest.raises(cm.ClearMoEError):
         cm.clearmoe_rms_norm(torch.empty(0, 64, device="cuda"), torch.empty(0, 64, device="cuda"))
+
+
+def test_matrices_of_another_gpu_are_refused():
+    x, A, W, q = torch.randn(5, 64, device="cuda"), cm.fp4_matrix(5, 64), cm.fp4_matrix(9, 64), cm.fp4_matrix(5, 9)
+    out, e = torch.empty(5, 9, device="cuda"), cm.fp8_rows(5, 64)
+    for m in (A, W, q, e):
+        assert m.get_device() == 0
+        m.c.device = 1  # as if it lay there
+        for call in (lambda: cm.clearmoe_fp4_quantize(x, A), lambda: cm.clearmoe_fp4_gemm(A, W, q), lambda: cm.clearmoe_fp4_gemm(A, W, out),
+                     lambda: cm.clearmoe_rms_norm(x, A), lambda: cm.clearmoe_rms_norm(x, e), lambda: cm.clearmoe_fp4_dequantize(A, x)):
+            if any(c.cell_contents is m for c in call.__closure__):
+                with pytest.raises(ValueError, match="GPU 1"):
+                    call()
+        m.c.device = 0
