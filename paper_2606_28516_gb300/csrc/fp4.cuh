@@ -87,6 +87,7 @@ struct Fp4GemmArgs {
     static constexpr bool GROUPED = NE > 1;
     CUtensorMap tmA, tmSA;          // bytes of q as half as many 16-bit elements, boxes of 128 bytes; scale tiles, boxes of two side by side
     CUtensorMap tmB[NE], tmSB[NE];  // the same of W
+    CUtensorMap tmH[NE];            // W's q in boxes of half as many rows, for halves of tiles
     CUtensorMap tmOut;              // FP4_OUT_BF16_BULK
     int64_t M;
     int N;
@@ -94,6 +95,7 @@ struct Fp4GemmArgs {
     int ksteps;    // MMAs of 64 columns
     int box_rows;  // rows of tmA's boxes
     int E;         // groups
+    int whole, rest;  // of a product of one matrix on pairs: rounds of tiles that every pair has one of, tiles after them
     const int32_t* offsets;  // [E + 1]; a grouped product's
     const int32_t* rows;     // output row of row i (nullable); a grouped product's
     const void* bias;        // [N], fp32 or bf16 (nullable)
@@ -109,7 +111,7 @@ struct Fp4GemmArgs {
     int64_t wait_limit_ns;
 };
 template <int NE>
-cudaError_t launch_fp4_gemm2(const Fp4GemmArgs<NE>& a, int bn, int num_sms, cudaStream_t s);
+cudaError_t launch_fp4_gemm2(Fp4GemmArgs<NE>& a, int bn, int num_sms, cudaStream_t s);
 // A product of at most FP4_FEW_MAX rows in one group: tmA in boxes of fp4_few_rows(M) rows, tmB of 128.
 constexpr int FP4_FEW_MAX = 128;
 int fp4_few_rows(int64_t M);

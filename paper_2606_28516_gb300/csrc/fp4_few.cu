@@ -301,14 +301,14 @@ static int few_split(int N, int nkb, int num_sms) {
 }
 
 // Whether the kernel is the better one: of the 0.17 us that a stage of K takes a tile of 64 columns and 128 rows, the
-// cluster saves all but its split's part, and a row takes it 0.025 us to add and store. Us, this kernel and that one: 1 x 1,024 x
-// 4,096 3.1, 5.1; 16 x 4,096 x 4,096 3.8, 5.1; 32 x 2,048 x 2,048 3.2, 3.8; 64 x 4,096 x 4,096 5.0, 5.5; 128 x 512 x 8,192
-// 5.7, 8.2; otherwise 1 x 768 x 768 2.9, 2.7; 32 x 4,096 x 1,024 3.3, 3.1; 128 x 4,096 x 4,096 6.7, 6.1.
+// cluster saves all but its split's part; joining its sums takes 0.35 us, and 0.025 a row. Us, this kernel and that one:
+// 1 x 1,024 x 4,096 3.1, 4.8; 16 x 4,096 x 4,096 3.8, 4.8; 64 x 1,024 x 4,096 4.1, 4.9; 100 x 512 x 8,192 5.7, 7.6; otherwise
+// 1 x 768 x 768 2.9, 2.3; 16 x 8,192 x 2,048 4.0, 3.7; 64 x 2,048 x 2,048 4.1, 3.5; 100 x 4,096 x 4,096 6.3, 5.6.
 bool fp4_few_pays(int64_t M, int N, int nkb, int num_sms) {
     const int64_t split = few_split(N, nkb, num_sms);
-    // with two CTAs an SM the weights are what takes time: 32 x 8,192 x 8,192 9.4 us against 10.1, 100 x 8,192 x 8,192 12.0 against 10.5
+    // with two CTAs an SM the weights are what takes time: 32 x 8,192 x 8,192 9.5 us against 9.6, 64 x 8,192 x 8,192 10.4 against 9.8
     if (M > ((N + 127) / 128 * split > num_sms ? 32 : FP4_FEW_MAX)) return false;
-    return 7 * nkb * (split - 1) > M * split;
+    return 7 * nkb * (split - 1) > (M + 14) * split;
 }
 
 cudaError_t launch_fp4_few(const Fp4GemmArgs<1>& a, int num_sms, cudaStream_t s) {

@@ -96,12 +96,19 @@ __global__ void __launch_bounds__(F4Cfg<BN_>::THREADS, 1) fp4_gemm_kernel(const 
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    pdl_wait();  // everything below may read the previous kernel's results
-    pdl_launch_dependents();  // after the wait: the next kernel may read weights that one before this has written
-    if (warp == 0) f4_groups(a, F4_BM, s_off, s_prefix, lane);
-    __syncthreads();
+    constexpr bool GROUPED = Fp4GemmArgs<NE>::GROUPED;
+    auto begin = [&]() {
+        pdl_wait();  // everything below may read the previous kernel's results
+        pdl_launch_dependents();  // after the wait: the next kernel may read weights that one before this has written
+    };
+    if constexpr (GROUPED) {
+        begin();
+        if (warp == 0) f4_groups(a, F4_BM, s_off, s_prefix, lane);
+        __syncthreads();
+    }
     const uint32_t tmem = warp_uniform(*tmem_slot);
-    F4Walk t(blockIdx.x, gridDim.x, a.N, F4_BM, BN, a.E, s_off, s_prefix);
+    F4Walk<GROUPED> t(blockIdx.x, gridDim.x, a, F4_BM, BN, s_off, s_prefix);
+    if constexpr (!GROUPED) begin();
     const int nkb = a.nkb;
 
     if (warp == C::WARP_TMA) {
@@ -275,13 +282,13 @@ struct Pick {
     int bn, pair;
 };
 // Cycles (at 1.9 GHz) a product takes on a kernel: its start; rounds of tiles, each of which multiplies its stages or, where
-// that is longer, runs the epilogue of the tile before it; and a part of the last epilogue. A stage's cycles grow from what
-// the MMAs and their scales take to what the path from L2 allows with every SM at work. Fitted to 90 products of 8 to
-// 16,384 rows; what the rule chooses is 0.6 % slower than the best kernel in the mean, 9 % at the most. In us, (64, 0),
-// (128, 0), (128, 1), (256, 1) at M x N x K: 197 x 1,536 x 384 with bias and GELU 3.5, 4.5, 4.4, 5.7; 788 x 768 x 2,048 4.4,
-// 5.0, 5.0, 6.5; 1,970 x 2,304 x 768 6.3, 6.1, 6.0, 6.3; 6,000 x 384 x 1,536 5.8, 5.3, 6.0, 6.7; 2,048 x 4,096 x 4,096 24.7,
-// 19.7, 17.4, 15.9; 16,384 x 4,096 x 4,096 162, 116, 99, 76. (Tiles of 192 columns on pairs were nowhere the best by more
-// than 1 %.)
+// that is longer, runs the epilogue of the tile before it; and a part of the last epilogue. A round of halves of tiles
+// (256 columns on pairs) counts 0.6. A stage's cycles grow from what the MMAs and their scales take to what the path from L2
+// allows with every SM at work. Fitted to 99 products of 8 to 16,384 rows; what the rule chooses is 0.5 % slower than the
+// best kernel in the mean, 7 % at the most. In us, (64, 0), (128, 0), (128, 1), (256, 1) at M x N x K: 197 x 1,536 x 384 with
+// bias and GELU 3.0, 4.0, 3.9, 5.2; 788 x 768 x 2,048 3.7, 4.5, 4.6, 6.1; 1,970 x 2,304 x 768 5.5, 5.1, 5.5, 5.8; 6,000 x
+// 384 x 1,536 5.2, 4.7, 5.5, 6.3; 2,048 x 4,096 x 4,096 24.4, 18.7, 16.5, 15.2; 4,096 x 4,096 x 4,096 45.3, 30.3, 25.9, 23.3.
+// (Tiles of 192 columns on pairs were nowhere the best by more than 1 %.)
 struct Fp4Kernel {
     Pick pick;
     int start, low, block, between;  // low, block: a stage's cycles on an idle GPU and with every SM at work
@@ -293,17 +300,19 @@ double cost(const Fp4Kernel& k, int64_t M, int N, int nkb, int store, bool gelu,
     const int rows = k.pick.pair ? 256 : 128, units = k.pick.pair ? num_sms / 2 : num_sms;
     if (units < 1) return 1e30;
     const int64_t tiles = ((M + rows - 1) / rows + groups - 1) * (((int64_t)N + k.pick.bn - 1) / k.pick.bn);
-    const double rounds = (double)((tiles + units - 1) / units), busy = tiles < units ? (double)tiles / units : 1.0;
+    const int64_t walkers = tiles < units ? tiles : units, rest = tiles % walkers;
+    const double last = !rest ? 0.0 : k.pick.bn == 256 && 2 * rest <= walkers ? 0.6 : 1.0;  // of halves of tiles
+    const double rounds = (double)(tiles / walkers) + last, busy = (double)walkers / units;
     const double main = nkb * (k.low + (k.block - k.low) * busy * busy), beside = k.epilogue[store] + (gelu ? k.gelu : 0);
     const double next = main + k.between > beside ? main + k.between : beside;
     return k.start + main + (rounds - 1) * next + k.last * beside;
 }
 template <int NE>
 Pick pick(const Fp4GemmArgs<NE>& g, int num_sms) {
-    static const Fp4Kernel all[] = {{{64, 0}, 4690, 319, 386, 367, 1290, 0.49, {1600, 3010, 2840, 1180}},
-                                    {{128, 0}, 3550, 370, 564, 0, 970, 1.06, {2910, 4400, 4730, 2250}},
-                                    {{128, 1}, 5960, 267, 473, 394, 1140, 0.84, {1630, 3780, 4370, 1470}},
-                                    {{256, 1}, 5890, 516, 788, 144, 2420, 0.86, {2870, 6850, 8560, 2830}}};
+    static const Fp4Kernel all[] = {{{64, 0}, 3550, 326, 390, 321, 1140, 0.57, {1270, 2490, 2710, 1240}},
+                                    {{128, 0}, 3090, 380, 546, 0, 1200, 0.96, {2440, 4040, 4560, 1930}},
+                                    {{128, 1}, 5160, 273, 454, 387, 1160, 0.82, {1620, 3650, 4240, 1340}},
+                                    {{256, 1}, 4920, 509, 747, 598, 2360, 0.90, {3030, 6870, 8690, 3050}}};
     if (NE == 1 && fp4_few_pays(g.M, g.N, g.nkb, num_sms)) return {FEW_WIDTH, 0};
     const int store = g.out_kind == FP4_OUT_FP4 ? 3 : !f8_wide(g) ? 2 : g.out_kind == FP8_OUT_F32 ? 1 : 0;
     Pick best = all[0].pick;
@@ -385,6 +394,7 @@ int run(Fp4GemmArgs<NE>& g, const clearmoe_fp4* A, const clearmoe_fp4* W, int E,
     }
     for (int e = 0; e < E; ++e) {
         if (encode_tmap_bf16(&g.tmB[e], W[e].q, W[e].rows, cols16, k.pair ? k.bn / 2 : k.bn)) return CLEARMOE_ECUDA;
+        if (k.pair && k.bn == 256 && encode_tmap_bf16(&g.tmH[e], W[e].q, W[e].rows, cols16, k.bn / 4)) return CLEARMOE_ECUDA;
         if (encode_tmap_fp4_scales(&g.tmSB[e], W[e].scale, (W[e].rows + 127) / 128, tiles, wt)) return CLEARMOE_ECUDA;
     }
     cudaError_t e;

@@ -23,8 +23,7 @@ __device__ __forceinline__ uint32_t idesc_mxf4(int M, int N, int half) {
 // By one warp, a group a lane: E + 1 loads one after the other took 2 us.
 template <class Args>
 __device__ __forceinline__ void f4_groups(const Args& a, int bm, int* off, int* prefix, int lane) {
-    int v = lane == 0 && !Args::GROUPED ? 0 : (int)a.M;
-    if (Args::GROUPED && lane <= a.E) v = __ldcg(a.offsets + lane);
+    int v = lane <= a.E ? __ldcg(a.offsets + lane) : (int)a.M;
     v = max(v, 0);
 #pragma unroll
     for (int o = 1; o <= CM_MAX_E; o <<= 1) {
@@ -62,22 +61,25 @@ __device__ __forceinline__ void l2_prefetch_2d(const CUtensorMap* map, int32_t c
         : "memory");
 }
 
-// F8Walk over such tiles: rows [max(m0, lo), hi) of a tile are the group's.
+// F8Walk over such tiles: rows [max(m0, lo), hi) of a tile are the group's. Without groups nothing is read of off and prefix.
+template <bool GROUPED>
 struct F4Walk {
     int mt, nt;  // row and column tile
     int e, m0, lo, hi, n0;
-    int n_tiles, bm, bn, E, step_mt, step_nt;
+    int m_tiles, n_tiles, bm, bn, E, step_mt, step_nt;
     const int* off;
     const int* prefix;
-    __device__ __forceinline__ F4Walk(int first, int step, int N, int bm_, int bn_, int E_, const int* off_, const int* prefix_)
-        : e(0), n_tiles((N + bn_ - 1) / bn_), bm(bm_), bn(bn_), E(E_), off(off_), prefix(prefix_) {
+    template <class Args>
+    __device__ __forceinline__ F4Walk(int first, int step, const Args& a, int bm_, int bn_, const int* off_, const int* prefix_)
+        : e(0), lo(0), hi((int)a.M), n_tiles((a.N + bn_ - 1) / bn_), bm(bm_), bn(bn_), E(a.E), off(off_), prefix(prefix_) {
+        m_tiles = GROUPED ? prefix[E] : ((int)a.M + bm - 1) / bm;
         mt = first / n_tiles;
         nt = first - mt * n_tiles;
         step_mt = step / n_tiles;
         step_nt = step - step_mt * n_tiles;
         place();
     }
-    __device__ __forceinline__ bool live() const { return mt < prefix[E]; }
+    __device__ __forceinline__ bool live() const { return mt < m_tiles; }
     __device__ __forceinline__ void next() {
         mt += step_mt;
         nt += step_nt;
@@ -88,11 +90,57 @@ struct F4Walk {
         place();
     }
     __device__ __forceinline__ void place() {
-        while (e + 1 < E && prefix[e + 1] <= mt) ++e;
-        lo = off[e];
-        m0 = (lo & ~127) + (mt - prefix[e]) * bm;
-        hi = off[e + 1];
         n0 = nt * bn;
+        if constexpr (GROUPED) {
+            while (e + 1 < E && prefix[e + 1] <= mt) ++e;
+            lo = off[e];
+            m0 = (lo & ~127) + (mt - prefix[e]) * bm;
+            hi = off[e + 1];
+        } else {
+            m0 = mt * bm;
+        }
+    }
+};
+
+// The tiles of one of `units` walkers: rounds in which each has one, then `rest` tiles. Where those are for half of the
+// walkers at the most, each is two of half the width (HALVES).
+template <bool GROUPED, bool HALVES>
+struct F4PairWalk : F4Walk<GROUPED> {
+    using Walk = F4Walk<GROUPED>;
+    int left;     // tiles of this walker to go
+    bool halved;  // the last one is a half
+    template <class Args>
+    __device__ __forceinline__ F4PairWalk(int unit, int units, const Args& a, int bm_, int bn_, const int* off_, const int* prefix_)
+        : Walk(unit, units, a, bm_, bn_, off_, prefix_) {
+        int rest = a.rest;
+        left = whole(a, units, rest);
+        halved = HALVES && 2 * rest <= units;
+        const bool more = unit < (halved ? 2 * rest : rest);
+        halved = halved && more;
+        if (more) ++left;
+        if (GROUPED && half()) turn(unit);
+    }
+    // Rounds in which each walker has a whole tile.
+    template <class Args>
+    __device__ __forceinline__ int whole(const Args& a, int units, int& rest) const {
+        if constexpr (!GROUPED) return a.whole;
+        const int tiles = this->m_tiles * this->n_tiles, rounds = tiles / units;
+        rest = tiles - rounds * units;
+        return rounds;
+    }
+    __device__ __forceinline__ bool live() const { return left > 0; }
+    __device__ __forceinline__ bool half() const { return HALVES && left == 1 && halved; }
+    __device__ __forceinline__ void next(int unit) {
+        --left;
+        Walk::next();
+        if (half()) turn(unit);
+    }
+    // From the tile that would be the walker's in the last round to the one it has half of: walkers 2 i and 2 i + 1 have tile i.
+    __device__ __forceinline__ void turn(int unit) {
+        for (this->nt -= (unit + 1) >> 1; this->nt < 0; this->nt += this->n_tiles) --this->mt;
+        this->e = 0;
+        this->place();
+        if (unit & 1) this->n0 += this->bn / 2;
     }
 };
 

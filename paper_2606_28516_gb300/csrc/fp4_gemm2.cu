@@ -8,6 +8,9 @@
 // (ovl_bar), and the next tile's MMAs start then rather than when the whole accumulator is read. Columns 480 .. 503 hold
 // the scales of two times 128 of K, in turn.
 //
+// A last round with tiles for half of the pairs at the most has them in halves of 128 columns, one a pair (9,973 x 1,024 x
+// 4,096 in eight groups 20.7 -> 19.3 us, 2,560 x 2,048 x 4,096 14.8 -> 12.3, 10,240 x 1,024 x 4,096 20.1 -> 18.0).
+//
 // Epilogue: 16 warps (four per lane quarter), each 32 columns at a time (one block of a 4-bit output), two times side by
 // side. What bounds it is the path of loads and stores (TMEM, shared and global memory): a store whose lanes write 32 rows
 // apart takes it 32 cycles whatever its width, so bf16 rows leave by bulk copies from shared memory and 4-bit rows 32
@@ -44,6 +47,8 @@ struct P4Cfg {
     static constexpr int OUT_BYTES = KIND == FP4_OUT_BF16_BULK ? NUM_EPI * P4_STAGED : 0;
     static constexpr int ROOM = 220 * 1024 - OUT_BYTES, STAGES = ROOM / STAGE_BYTES < 8 ? ROOM / STAGE_BYTES : 8;
     static constexpr bool OVL = BN == 256;
+    static constexpr bool HALVES = BN == 256;  // of tiles of the last round
+    static constexpr int HALF_BYTES = STAGE_BYTES - (HALVES ? B_BYTES / 2 : 0);  // of a stage of theirs
     static constexpr int ACC1 = OVL ? 224 : BN;  // first column of the second accumulator
     static constexpr int SF_COL = ACC1 + BN, SF_COLS = 4 * (1 + NF);
     static_assert(SF_COL + 2 * SF_COLS <= 512);
@@ -90,6 +95,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::TH
     fp4_gemm2_kernel(const __grid_constant__ Fp4GemmArgs<NE> a) {
     using C = P4Cfg<BN_, KIND>;
     constexpr int BN = C::BN, STAGES = C::STAGES;
+    constexpr bool GROUPED = Fp4GemmArgs<NE>::GROUPED;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* sm = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     unsigned char* s_out = sm + STAGES * C::STAGE_BYTES;               // [epilogue warp][32 rows][64], bf16 outputs
@@ -138,13 +144,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::TH
     __syncthreads();
     cluster_sync();  // barriers initialised and tensor memory allocated in both CTAs
     tc_fence_after();
-    pdl_wait();  // everything below may read the previous kernel's results
-    pdl_launch_dependents();  // after the wait: the next kernel may read weights that one before this has written
-    if (warp == 0) f4_groups(a, 2 * P4_BM, s_off, s_prefix, lane);
-    __syncthreads();
+    auto begin = [&]() {
+        pdl_wait();  // everything below may read the previous kernel's results
+        pdl_launch_dependents();  // after the wait: the next kernel may read weights that one before this has written
+    };
+    if constexpr (GROUPED) {
+        begin();
+        if (warp == 0) f4_groups(a, 2 * P4_BM, s_off, s_prefix, lane);
+        __syncthreads();
+    }
     const uint32_t tmem = warp_uniform(*tmem_slot);  // all 512 columns: the same base in both CTAs
     const int nkb = a.nkb;
-    F4Walk t(blockIdx.x >> 1, gridDim.x >> 1, a.N, 2 * P4_BM, BN, a.E, s_off, s_prefix);
+    const int unit = (int)blockIdx.x >> 1;
+    F4PairWalk<GROUPED, C::HALVES> t(unit, gridDim.x >> 1, a, 2 * P4_BM, BN, s_off, s_prefix);
+    if constexpr (!GROUPED) begin();
 
     if (warp >= C::NUM_EPI) {
         if (warp == C::WARP_TMA) {
@@ -153,9 +166,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::TH
             int stage = 0;
             uint32_t ph = 0, issued = 0;
             bool ok = true;
-            for (; warp_uniform((int)t.live()) && ok; t.next()) {
+            for (; warp_uniform((int)t.live()) && ok; t.next(unit)) {
                 const int e = warp_uniform(t.e);
                 const int m0 = warp_uniform(t.m0 + (int)rank * P4_BM), n0 = warp_uniform(t.n0);
+                const bool half = warp_uniform((int)t.half());
+                const int w0 = n0 + (int)rank * (half ? C::BH / 2 : C::BH);
                 for (int kb = 0; kb < nkb; ++kb) {
                     if (!mbar_wait_warp(empty_bar(stage), ph ^ 1, abort_flag, a.status, lim)) {
                         ok = false;
@@ -163,10 +178,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::TH
                     }
                     const uint32_t sA = smem_u32(sm + stage * C::STAGE_BYTES), sB = sA + C::A_BYTES, sF = sB + C::B_BYTES;
                     const uint32_t fb = full_leader0 + 8u * stage;
-                    if (leader) mbar_arrive_expect_tx_warp(full_bar(stage), 2 * C::STAGE_BYTES);
+                    if (leader) mbar_arrive_expect_tx_warp(full_bar(stage), 2 * (half ? C::HALF_BYTES : C::STAGE_BYTES));
                     // coordinates in the maps' elements: 16-bit ones of four columns, 32-bit ones of four scales
                     tma_load_2d_pair(sA, &a.tmA, kb * 64, m0, fb);
-                    tma_load_2d_pair(sB, &a.tmB[e], kb * 64, n0 + (int)rank * C::BH, fb);
+                    tma_load_2d_pair(sB, half ? &a.tmH[e] : &a.tmB[e], kb * 64, w0, fb);
                     tma_load_2d_pair(sF, &a.tmSA, kb * 256, m0 >> 7, fb);
                     tma_load_2d_pair(sF + F4_SF, &a.tmSB[e], kb * 256, n0 >> 7, fb);
                     ++issued;
@@ -185,12 +200,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::TH
                 int stage = 0, acc = 0;
                 uint32_t ph = 0, aph = 0, oph = 1;  // oph: phase of the previous tile's shared columns
                 bool ok = true;
-                for (; warp_uniform((int)t.live()) && ok; t.next()) {
+                for (; warp_uniform((int)t.live()) && ok; t.next(unit)) {
                     if (!mbar_wait_warp(tempty_bar(acc), aph ^ 1, abort_flag, a.status, lim)) break;
                     if (C::OVL && !mbar_wait_warp(ovl_bar, oph, abort_flag, a.status, lim)) break;
                     oph ^= 1;
                     tc_fence_after();
                     const uint32_t d = tmem + acc * C::ACC1;
+                    const int width = warp_uniform(t.half() ? BN / 2 : BN);
                     for (int kb = 0; kb < nkb; ++kb) {
                         if (!mbar_wait_warp(full_bar(stage), ph, abort_flag, a.status, lim)) {
                             ok = false;
@@ -210,7 +226,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::TH
                             for (int j = 0; j < 2; ++j) {  // 64 columns: 32 bytes on in each row
                                 const int k = 2 * h + j;
                                 if (4 * kb + k < a.ksteps)
-                                    umma2_mxf4(d, ad + 2 * k, bd + 2 * k, idesc_mxf4(2 * P4_BM, BN, j), sf, sf + 4, (kb | k) != 0);
+                                    umma2_mxf4(d, ad + 2 * k, bd + 2 * k, idesc_mxf4(2 * P4_BM, width, j), sf, sf + 4, (kb | k) != 0);
                             }
                         }
                         umma2_commit_both(empty_bar(stage));
@@ -233,15 +249,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::TH
                 // reached gets the other's part of its barrier here.
                 if (warp_uniform((int)*abort_flag) && mbar_wait_warp(stop_bar, 0, nullptr, a.status, 2 * lim + 10000000ull)) {
                     fence_cluster();
+                    int rest;
+                    const uint32_t halves = (uint32_t)(t.whole(a, (int)gridDim.x >> 1, rest) * nkb);  // k-blocks before a half's
                     const uint32_t at = smem_u32(tmem_slot + 2);
                     const uint32_t n0 = ld_cluster_u32(map_to_rank(at, 0)), n1 = ld_cluster_u32(map_to_rank(at, 1)), n = max(n0, n1);
     #pragma unroll 1
                     for (uint32_t k = n > STAGES ? n - STAGES : 0; k < n; ++k) {
                         const uint32_t s = k % STAGES;
                         const DrainStep st = drain_step(k, n0, n1);
+                        const uint32_t bytes = t.halved && k >= halves ? C::HALF_BYTES : C::STAGE_BYTES;
                         // the odd CTA alone reached it: expect its bytes; the even CTA alone: count the odd one's as landed
-                        if (st.arrive) mbar_arrive_expect_tx_warp(full_bar(s), C::STAGE_BYTES);
-                        if (st.complete) mbar_complete_tx_warp(full_bar(s), C::STAGE_BYTES);
+                        if (st.arrive) mbar_arrive_expect_tx_warp(full_bar(s), bytes);
+                        if (st.complete) mbar_complete_tx_warp(full_bar(s), bytes);
                         mbar_wait_warp(full_bar(s), (k / STAGES) & 1, nullptr, a.status, 10000000ull);
                     }
                 }
@@ -278,7 +297,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::TH
                     }
             }
         };
-        if (group && t.live()) t.next();
+        if (group && t.live()) t.next(unit);
         prefetch();
         uint32_t aph = 0;
         while (t.live()) {
@@ -291,10 +310,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::TH
 #pragma unroll
                 for (int r = 0; r < C::CH; ++r) b[p][r] = bias[p][r];
             }
+            // A half tile is the walker's last one: nobody waits for its accumulator to be read.
+            if (t.half() && cg * C::WIDTH >= BN / 2) break;
             const int now = acc;
             if (C::GROUPS == 1) acc ^= 1;
-            t.next();
-            if (C::GROUPS == 2 && t.live()) t.next();
+            t.next(unit);
+            if (C::GROUPS == 2 && t.live()) t.next(unit);
             prefetch();
             if (!mbar_wait_warp(tfull_bar(now), aph, abort_flag, a.status, lim)) break;
             tc_fence_after();
@@ -356,15 +377,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::TH
 }
 
 template <int BN, int KIND, int NE>
-cudaError_t launch_pair(const Fp4GemmArgs<NE>& a, int num_sms, cudaStream_t s) {
+cudaError_t launch_pair(Fp4GemmArgs<NE>& a, int num_sms, cudaStream_t s) {
     using C = P4Cfg<BN, KIND>;
     static_assert(C::SMEM <= 227 * 1024);
     const cudaError_t e = smem_attr_once((const void*)fp4_gemm2_kernel<BN, KIND, NE>, C::SMEM);
     if (e != cudaSuccess) return e;
     const int64_t m_tiles = (a.M + 2 * P4_BM - 1) / (2 * P4_BM) + a.E - 1;
-    const int64_t tiles = m_tiles * ((a.N + BN - 1) / BN), pairs = num_sms / 2;
+    const int64_t tiles = m_tiles * ((a.N + BN - 1) / BN), pairs = num_sms / 2, units = tiles < pairs ? tiles : pairs;
+    a.whole = (int)(tiles / units);
+    a.rest = (int)(tiles % units);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs)));
+    cfg.gridDim = dim3((unsigned)(2 * units));
     cfg.blockDim = dim3(C::THREADS);
     cfg.dynamicSmemBytes = C::SMEM;
     cfg.stream = s;
@@ -377,21 +400,21 @@ cudaError_t launch_pair(const Fp4GemmArgs<NE>& a, int num_sms, cudaStream_t s) {
 }
 
 template <int KIND, int NE>
-cudaError_t launch_kind2(const Fp4GemmArgs<NE>& a, int bn, int num_sms, cudaStream_t s) {
+cudaError_t launch_kind2(Fp4GemmArgs<NE>& a, int bn, int num_sms, cudaStream_t s) {
     return bn == 256 ? launch_pair<256, KIND>(a, num_sms, s) : launch_pair<128, KIND>(a, num_sms, s);
 }
 
 }  // namespace
 
 template <int NE>
-cudaError_t launch_fp4_gemm2(const Fp4GemmArgs<NE>& a, int bn, int num_sms, cudaStream_t s) {
+cudaError_t launch_fp4_gemm2(Fp4GemmArgs<NE>& a, int bn, int num_sms, cudaStream_t s) {
     if constexpr (NE == 1) {
         if (a.out_kind == FP4_OUT_FP4) return launch_kind2<FP4_OUT_FP4>(a, bn, num_sms, s);
         if (a.tma_out) return launch_kind2<FP4_OUT_BF16_BULK>(a, bn, num_sms, s);
     }
     return a.out_kind == FP8_OUT_BF16 ? launch_kind2<FP8_OUT_BF16>(a, bn, num_sms, s) : launch_kind2<FP8_OUT_F32>(a, bn, num_sms, s);
 }
-template cudaError_t launch_fp4_gemm2<1>(const Fp4GemmArgs<1>&, int, int, cudaStream_t);
-template cudaError_t launch_fp4_gemm2<CM_MAX_E>(const Fp4GemmArgs<CM_MAX_E>&, int, int, cudaStream_t);
+template cudaError_t launch_fp4_gemm2<1>(Fp4GemmArgs<1>&, int, int, cudaStream_t);
+template cudaError_t launch_fp4_gemm2<CM_MAX_E>(Fp4GemmArgs<CM_MAX_E>&, int, int, cudaStream_t);
 
 }  // namespace cm

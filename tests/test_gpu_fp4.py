@@ -211,6 +211,47 @@ def test_every_kernel(kernel, M, N, K, act):
     check_blocks(q, y, err)
 
 
+@pytest.mark.parametrize("kernel", [(256, 1), (128, 1)], indirect=True)
+@pytest.mark.parametrize("M,N,K,act", [(2500, 2000, 300, cm.ACT_GELU), (2500, 1900, 700, cm.ACT_NONE), (20000, 256, 100, cm.ACT_RELU),
+                                       (4864, 1536, 1100, cm.ACT_NONE), (5120, 1290, 257, cm.ACT_GELU), (300, 20000, 64, cm.ACT_NONE)])
+def test_rounds_that_end_in_few_tiles(kernel, M, N, K, act):
+    """Last rounds of two to 38 tiles for 76 pairs, each of them in halves; those past the matrix among them."""
+    rng = np.random.default_rng(M + N)
+    A, W, av, wv = make(rng, M, N, K)
+    bias = dev(rng.standard_normal(N) * 0.1)
+    y, err = reference(av, wv, bias, act)
+    for pad, dtype in ((0, torch.float32), (-N % 8, torch.bfloat16), (-N % 8 + 1, torch.bfloat16), (1, torch.float32)):
+        out = torch.full((M + 1, N + pad), float("nan"), device="cuda", dtype=dtype)
+        cm.clearmoe_fp4_gemm(A, W, out[:M, :N], bias=bias, act=act)
+        assert within(out[:M, :N], y, err)
+        assert bool(out[M].isnan().all()) and bool(out[:, N:].isnan().all())
+    q = cm.fp4_matrix(M, N)
+    q.q.fill_(0x33)
+    cm.clearmoe_fp4_gemm(A, W, q, bias=bias, act=act)
+    check_blocks(q, y, err)
+
+
+@pytest.mark.parametrize("kernel", [(256, 1)], indirect=True)
+@pytest.mark.parametrize("counts", [[200, 0, 0, 0], [0, 0, 0, 0, 300], [3000, 1, 0, 5000, 2500, 777], [0, 9000, 0, 1300]])
+def test_grouped_rounds_that_end_in_few_tiles(kernel, counts):
+    """Halves of tiles in the first round, for half of the pairs that the grid has at the most, and in the second."""
+    rng = np.random.default_rng(78)
+    N, K = 500, 320
+    M, off = sum(counts), np.concatenate([[0], np.cumsum(counts)])
+    A, _, av, _ = make(rng, M, N, K)
+    pairs = [make(rng, 1, N, K)[1::2] for _ in counts]
+    at = rng.permutation(M)
+    for dtype in (torch.float32, torch.bfloat16):
+        out = torch.full((M + 1, N + 4), float("nan"), device="cuda", dtype=dtype)
+        cm.clearmoe_fp4_grouped_gemm(A, [p[0] for p in pairs], torch.tensor(off, dtype=torch.int32, device="cuda"), out[:M, :N],
+                                     perm=torch.tensor(at, dtype=torch.int32, device="cuda"))
+        for e in range(len(counts)):
+            sl = slice(int(off[e]), int(off[e + 1]))
+            y, err = reference(av[sl], pairs[e][1], None, cm.ACT_NONE)
+            assert within(out[torch.tensor(at[sl], device="cuda", dtype=torch.long), :N], y, err)
+        assert bool(out[M].isnan().all()) and bool(out[:, N:].isnan().all())
+
+
 @pytest.mark.parametrize("M,N,K,act", [(1, 1, 1, cm.ACT_NONE), (16, 40, 130, cm.ACT_GELU), (17, 5003, 257, cm.ACT_RELU),
                                        (32, 700, 2048, cm.ACT_GELU), (32, 96, 9000, cm.ACT_NONE), (7, 40000, 512, cm.ACT_NONE),
                                        (3, 128, 1792, cm.ACT_GELU), (29, 20000, 64, cm.ACT_RELU), (33, 300, 300, cm.ACT_NONE),
