@@ -292,6 +292,26 @@ def test_bf16_rows_by_bulk_copies(kernel, M, N, K, pitch):
     assert bool(out[M:].isnan().all()) and bool(out[:, N:].isnan().all())
 
 
+@pytest.mark.parametrize("kernel", KERNELS, indirect=True)
+@pytest.mark.parametrize("M,N,pitch", [(100, 32, 40), (300, 100, 101), (77, 33, 36), (130, 1, 3), (65, 287, 290), (260, 64, 65), (1, 95, 97)])
+@pytest.mark.parametrize("start", [0, 1, 2])
+def test_bf16_rows_that_start_anywhere(kernel, M, N, pitch, start):
+    """Rows at whole words, between them and by turns; nothing beside them is written."""
+    A, W, av, wv = make(np.random.default_rng(M), M, N, 200)
+    flat = torch.full((start + (M + 1) * pitch,), float("nan"), device="cuda", dtype=torch.bfloat16)
+    out = flat[start:].view(M + 1, pitch)
+    cm.clearmoe_fp4_gemm(A, W, out[:M, :N], act=cm.ACT_RELU)
+    assert within(out[:M, :N], *reference(av, wv, None, cm.ACT_RELU))
+    assert bool(out[M].isnan().all()) and bool(out[:, N:].isnan().all()) and bool(flat[:start].isnan().all())
+    if kernel != (16, 0):
+        flat.fill_(float("nan"))
+        at = torch.randperm(M, device="cuda").to(torch.int32)
+        cm.clearmoe_fp4_grouped_gemm(A, [W] * 3, torch.tensor([0, M // 3, M // 2, M], dtype=torch.int32, device="cuda"), out[:M, :N], perm=at,
+                                     act=cm.ACT_RELU)
+        assert within(out[:M, :N][at.long()], *reference(av, wv, None, cm.ACT_RELU))
+        assert bool(out[M].isnan().all()) and bool(out[:, N:].isnan().all()) and bool(flat[:start].isnan().all())
+
+
 @pytest.mark.parametrize("perm", [True, False])
 @pytest.mark.parametrize("counts", [[0, 300, 1, 0, 129, 700], [1130], [3, 2, 0, 1], [128, 128, 256], [127, 1, 129, 255, 0, 77, 500, 41],
                                     [1] * 16])
