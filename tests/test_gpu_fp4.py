@@ -100,6 +100,22 @@ def test_quantize_gathered(K):
     check_quantized(m, val)
 
 
+@pytest.mark.parametrize("gather", [False, True])
+@pytest.mark.parametrize("start,pad", [(0, 1), (1, 0), (1, 1), (2, 2)])
+@pytest.mark.parametrize("K", [1, 2, 31, 127, 128, 129, 255, 256, 301, 1131])
+def test_quantize_rows_that_start_anywhere(K, start, pad, gather):
+    """bf16 rows at whole words, between them and by turns, NaN around each."""
+    rng, M = np.random.default_rng(K), 37
+    pitch = K + pad + 1
+    flat = torch.full((start + M * pitch,), float("nan"), device="cuda", dtype=torch.bfloat16)
+    x = flat[start:].view(M, pitch)[:, :K]
+    x.copy_(dev(rows_of(rng, M, K), torch.bfloat16))
+    m = cm.fp4_matrix(M, K)
+    at = rng.permutation(M) if gather else np.arange(M)
+    cm.clearmoe_fp4_quantize(x, m, gather=torch.tensor(at, dtype=torch.int32, device="cuda") if gather else None)
+    check_quantized(m, f64(x)[at])
+
+
 def test_quantize_far_rows():
     """Rows whose offsets pass 32 bits: two of a wide pitch."""
     ld = 1 << 29
