@@ -530,8 +530,9 @@ int clearmoe_debug_fp4_wait(int64_t wait_limit_ns);
  *  x, residual (nullable: s = x), sum (nullable: s is not stored) [rows x cols] of dtype (F32 or BF16), rows ldx, ldr and
  *  lds elements apart; weight (nullable: ones) [cols] of weight_dtype; eps >= 0.
  * Every tensor may start anywhere that its element type allows. sum may be x or residual (with the same pitch), and out
- * may be x or residual (of the same dtype and pitch) where sum is not; they must not overlap otherwise. 1 <= rows <= 2^30, 1 <= cols <= CLEARMOE_NORM_MAX
- * (EUNSUPPORTED above). No handle; stream-ordered; reads nothing before the preceding kernel has completed. */
+ * may be x or residual (of the same dtype and pitch) where sum is not; they must not overlap otherwise. 1 <= rows <= 2^30,
+ * 1 <= cols <= CLEARMOE_NORM_MAX (EUNSUPPORTED above). No handle; stream-ordered; reads nothing before the preceding kernel
+ * has completed. */
 #define CLEARMOE_NORM_MAX 32768
 typedef struct {
     const void* x;

@@ -537,6 +537,32 @@ def test_waits_that_run_out(kernel, blocks):
     assert kernel[0] == 16 or any(gave_up)
 
 
+@pytest.mark.parametrize("kernel", [(256, 1)], indirect=True)
+@pytest.mark.parametrize("counts,N", [([200, 0, 0, 0], 512), ([3000, 2120], 1280)])
+def test_waits_that_run_out_in_halves_of_tiles(kernel, counts, N):
+    """The same of tiles in halves, the first and the last that a pair has."""
+    M, E = sum(counts), len(counts)
+    A, W, *_ = make(np.random.default_rng(30), M, N, 8192)
+    off = torch.tensor(np.concatenate([[0], np.cumsum(counts)]), dtype=torch.int32, device="cuda")
+    out, status = torch.empty(M, N, device="cuda", dtype=torch.bfloat16), torch.zeros(1, dtype=torch.int32, device="cuda")
+    cm.clearmoe_fp4_grouped_gemm(A, [W] * E, off, out, status=status)
+    want = out.clone()
+    try:
+        for limit in (200, 1_000, 4_000, 12_000, 16_000, 24_000):
+            for _ in range(4):
+                cm.clearmoe_debug_fp4_wait(limit)
+                cm.clearmoe_fp4_grouped_gemm(A, [W] * E, off, out, status=status)
+                cm.clearmoe_fp4_grouped_gemm(A, [W] * E, off, out, status=status)
+                assert status.item() in (0, cm.ETIMEOUT)
+                status.zero_()
+                cm.clearmoe_debug_fp4_wait()
+                out.zero_()
+                cm.clearmoe_fp4_grouped_gemm(A, [W] * E, off, out, status=status)
+                assert torch.equal(out, want) and status.item() == 0
+    finally:
+        cm.clearmoe_debug_fp4_wait()
+
+
 @pytest.mark.parametrize("M,N,K", [(3, 2048, 16384), (300, 512, 1024)])
 def test_weights_and_rows_just_written(M, N, K):
     """Weights and rows quantised by the kernels right before the product, new ones each time: what is asked for into L2
