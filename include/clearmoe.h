@@ -497,13 +497,15 @@ int clearmoe_fp4_dequantize(const clearmoe_fp4* in, void* out, int32_t dtype, in
 /* out = act(A W^T + bias): A [M x K], W [N x K] (A->cols == W->cols), products of e2m1 values and the scales exact, sums in
  * fp32 (the tensor cores cut where fp32 additions would round), the result rounded once to out_dtype (F32 or BF16) and
  * stored at out [M x N], rows ldo elements apart (ldo >= N, any alignment of the element type). epi may be NULL (no bias,
- * no activation); its status as in the 8-bit products. N <= 2^24. No handle and no workspace; stream-ordered; out must
- * not alias an input. */
+ * no activation); its status as in the 8-bit products. The GELU is a kind of output's own, the same at every size:
+ * before the rounding within 2.5e-7 of the exact one to fp32 and within 3.2e-7 to bf16 and 4-bit blocks, or half a step of
+ * fp32 where that is more; NaN and -inf give NaN, as u (1 + erf(u / sqrt 2)) / 2 does, and inf gives inf. N <= 2^24. No
+ * handle and no workspace; stream-ordered; out must not alias an input. */
 int clearmoe_fp4_gemm(const clearmoe_fp4* A, const clearmoe_fp4* W, const clearmoe_fp8_epilogue* epi, void* out,
                       int32_t out_dtype, int64_t ldo, void* stream);
 
-/* The same with the fp32 result quantised as clearmoe_fp4_quantize would: out [M x N] in 4-bit blocks, the next product's
- * activations, without its intermediate in memory. */
+/* The same with the fp32 result (the GELU as said) quantised as clearmoe_fp4_quantize would: out [M x N] in 4-bit blocks,
+ * the next product's activations, without its intermediate in memory. */
 int clearmoe_fp4_gemm_fp4(const clearmoe_fp4* A, const clearmoe_fp4* W, const clearmoe_fp8_epilogue* epi,
                           const clearmoe_fp4* out, void* stream);
 

@@ -59,8 +59,12 @@ template <int KIND>
 __device__ __forceinline__ void finish(const Fp4GemmArgs<1>& a, float4 s, const float4& bias, int m, int n, bool vec, int lane) {
     float v[4] = {s.x + bias.x, s.y + bias.y, s.z + bias.z, s.w + bias.w};
     if (a.act == CLEARMOE_ACT_GELU) {
-        const float2 p = gelu_pair_f32(make_float2(v[0], v[1])), q = gelu_pair_f32(make_float2(v[2], v[3]));
-        v[0] = p.x, v[1] = p.y, v[2] = q.x, v[3] = q.y;
+        if constexpr (KIND == FP8_OUT_F32) {  // f8_act's of the tiles' epilogues
+            const float2 p = gelu_pair_f32(make_float2(v[0], v[1])), q = gelu_pair_f32(make_float2(v[2], v[3]));
+            v[0] = p.x, v[1] = p.y, v[2] = q.x, v[3] = q.y;
+        } else {
+            gelu_pairs_bf16<2>(v);
+        }
     } else if (a.act == CLEARMOE_ACT_RELU) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];  // NaN stays NaN

@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(F4Cfg<BN_>::THREADS, 1) fp4_gemm_kernel(const 
                 if (r + 1 == ROUNDS) tc_fence_before();
                 __syncwarp();
                 if (r + 1 == ROUNDS && lane == 0) mbar_arrive(tempty_bar(acc));  // the accumulator is read
-                f8_act<32, KIND == FP8_OUT_F32>(v, bias_line, has_bias, a.act);
+                f8_act<32, KIND == FP8_OUT_F32 ? GELU_F32 : GELU_BF16>(v, bias_line, has_bias, a.act);
                 f4_store32<KIND>(a, v, orow, nc, wide, lane);
             }
             if (++acc == 2) {

@@ -351,7 +351,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::TH
                 uint32_t scales[C::CH];
 #pragma unroll
                 for (int r = 0; r < C::CH; ++r) {
-                    f8_act<32, KIND == FP8_OUT_F32>(v[r], bias_line + 32 * r, has_bias, a.act);
+                    f8_act<32, KIND == FP8_OUT_F32 ? GELU_F32 : GELU_BF16>(v[r], bias_line + 32 * r, has_bias, a.act);
                     if constexpr (KIND == FP4_OUT_FP4) {
                         blocks[r] = f4_block(a, v[r], nc + 32 * r, scales[r]);
                     } else if constexpr (KIND == FP4_OUT_BF16_BULK) {

@@ -267,7 +267,7 @@ __global__ void __launch_bounds__(F8Cfg<BN_>::THREADS, 1) fp8_gemm_kernel(const 
                 }
                 __syncwarp();
                 if (!mine) continue;
-                f8_act<32, KIND == FP8_OUT_F32>(v[r], bias_line, has_bias, a.act);
+                f8_act<32, KIND == FP8_OUT_F32 ? GELU_F32 : GELU_8BIT>(v[r], bias_line, has_bias, a.act);
                 if constexpr (KIND == FP8_OUT_FP8) {
                     if (nc + 32 > a.N) {  // the last block's padding is zero
 #pragma unroll

@@ -303,8 +303,35 @@ __device__ __forceinline__ void gelu_pairs_fp8(float* u) {
     }
 }
 
+// gelu_pair_bf16 for P pairs at once in the same way, of products in 4-bit blocks whichever kernel they take: NaN for -inf as
+// for NaN, by max(u, 0) = u - min(u, 0), which is exact. It costs an operation a value (8,192 x 4,096 x 1,024 to 4-bit blocks
+// 22.7 us with -inf to 0, 23.7 so; 25.6 with the difference packed, whose register pairs spilled).
+template <int P>
+__device__ __forceinline__ void gelu_pairs_bf16(float* u) {
+    float2 v[P], q[P];
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+        v[i] = make_float2(fmaxf(-fabsf(u[2 * i]), GeluE::HOLD), fmaxf(-fabsf(u[2 * i + 1]), GeluE::HOLD));
+#pragma unroll
+    for (int i = 0; i < P; ++i) q[i] = __ffma2_rn(make_float2(GeluE::C6, GeluE::C6), v[i], make_float2(GeluE::C5, GeluE::C5));
+    constexpr float C[5] = {GeluE::C4, GeluE::C3, GeluE::C2, GeluE::C1, -1.f};
+#pragma unroll
+    for (int k = 0; k < 5; ++k)
+#pragma unroll
+        for (int i = 0; i < P; ++i) q[i] = __ffma2_rn(q[i], v[i], make_float2(C[k], C[k]));
+#pragma unroll
+    for (int i = 0; i < P; ++i) q[i] = make_float2(ex2_approx(q[i].x), ex2_approx(q[i].y));
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        const float2 relu = make_float2(u[2 * i] - fminf(u[2 * i], 0.f), u[2 * i + 1] - fminf(u[2 * i + 1], 0.f));
+        const float2 r = __ffma2_rn(v[i], q[i], relu);
+        u[2 * i] = r.x, u[2 * i + 1] = r.y;
+    }
+}
+
+enum F8Gelu { GELU_8BIT = 0, GELU_F32 = 1, GELU_BF16 = 2 };  // by gelu_pairs_fp8, gelu_pair_f32, gelu_pairs_bf16
 // CW accumulator columns + bias, activation; bias from the warp's shared-memory line.
-template <int CW, bool EXACT>
+template <int CW, int GELU>
 __device__ __forceinline__ void f8_act(float (&v)[CW], const float* s_bias, bool has_bias, int act) {
     if (has_bias) {
 #pragma unroll
@@ -316,12 +343,15 @@ __device__ __forceinline__ void f8_act(float (&v)[CW], const float* s_bias, bool
         }
     }
     if (act == CLEARMOE_ACT_GELU) {
-        if constexpr (EXACT) {
+        if constexpr (GELU == GELU_F32) {
 #pragma unroll
             for (int i = 0; i < CW; i += 2) {
                 const float2 g = gelu_pair_f32(make_float2(v[i], v[i + 1]));
                 v[i] = g.x, v[i + 1] = g.y;
             }
+        } else if constexpr (GELU == GELU_BF16) {
+#pragma unroll
+            for (int i = 0; i < CW; i += 8) gelu_pairs_bf16<4>(v + i);
         } else {
 #pragma unroll
             for (int i = 0; i < CW; i += 8) gelu_pairs_fp8<4>(v + i);
@@ -378,7 +408,7 @@ struct F8Halves {
             __syncwarp();
         }
         if (next >= 0) prefetch(next);
-        f8_act<64, false>(v, line, a.bias != nullptr, a.act);
+        f8_act<64, GELU_8BIT>(v, line, a.bias != nullptr, a.act);
         if (n + 64 > a.N) {  // columns past N are zero, in the last block's padding and where no block is
 #pragma unroll
             for (int i = 0; i < 64; ++i)

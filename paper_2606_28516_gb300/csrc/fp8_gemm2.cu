@@ -381,7 +381,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8Cfg<BN_, KIND>::TH
                 released(r);
                 const int nc = n0 + chunk[r] * 32;
                 if (mine) {
-                    f8_act<32, KIND == FP8_OUT_F32>(v, bias_line, has_bias, a.act);
+                    f8_act<32, KIND == FP8_OUT_F32 ? GELU_F32 : GELU_8BIT>(v, bias_line, has_bias, a.act);
                     f8_store32<KIND>(a, v, orow, nc, wide, lane);
                 }
             }
