@@ -107,11 +107,16 @@ struct FewTile {
     __device__ __forceinline__ void set_row(int j, const void* row) {
         tok[j] = static_cast<const char*>(row) + (int64_t)column() * F::XSZ;
     }
+    // A product's weights may be the preceding kernel's, beside which this one may have started: not what ld.global.nc may read.
+    // A layer's are older (the rule for weights).
+    __device__ __forceinline__ static uint4 weights(const char* p) {
+        return V == FEWV_W8A8 ? __ldcg(reinterpret_cast<const uint4*>(p)) : __ldg(reinterpret_cast<const uint4*>(p));
+    }
     __device__ __forceinline__ void load_w(int d, int i) {
         a[d] = b[d] = make_uint4(0, 0, 0, 0);
         if (i < in) {
-            a[d] = __ldg(reinterpret_cast<const uint4*>(w0 + (int64_t)i * (F::WARPS * F::STEP * F::WSZ)));
-            b[d] = __ldg(reinterpret_cast<const uint4*>(w1 + (int64_t)i * (F::WARPS * F::STEP * F::WSZ)));
+            a[d] = weights(w0 + (int64_t)i * (F::WARPS * F::STEP * F::WSZ));
+            b[d] = weights(w1 + (int64_t)i * (F::WARPS * F::STEP * F::WSZ));
         }
     }
     __device__ __forceinline__ void load_x(int d, int i) {

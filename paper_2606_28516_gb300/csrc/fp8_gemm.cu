@@ -239,8 +239,8 @@ __global__ void __launch_bounds__(F8Cfg<BN_>::THREADS, 1) fp8_gemm_kernel(const 
                 const int n = t.n0 + (SPAN * r + cg) * 32 + lane;
                 b[r] = 0.f;
                 if (has_bias && n < a.N)
-                    b[r] = a.bias_bf16 ? bf16_to_f32(__ldg(static_cast<const uint16_t*>(a.bias) + n))
-                                       : __ldg(static_cast<const float*>(a.bias) + n);
+                    b[r] = a.bias_bf16 ? bf16_to_f32(__ldcg(static_cast<const uint16_t*>(a.bias) + n))
+                                       : __ldcg(static_cast<const float*>(a.bias) + n);
             }
             if (!mbar_wait_warp(tfull_bar(acc), aph, abort_flag, a.status, lim)) break;
             tc_fence_after();

@@ -126,7 +126,7 @@ struct F8Scales {
         const uint8_t* sb = g.sb[t.e];
 #pragma unroll
         for (int j = 0; j < NW; ++j)
-            w[j] = __ldg(reinterpret_cast<const uint32_t*>(sb + (int64_t)(min(t.n0 + SPAN * j, g.N - 1) / 128) * g.lds) + chunk);
+            w[j] = __ldcg(reinterpret_cast<const uint32_t*>(sb + (int64_t)(min(t.n0 + SPAN * j, g.N - 1) / 128) * g.lds) + chunk);
     }
     // to a slot in shared memory (f8_slot_bytes): 16 bytes a lane for A, and for each 128 columns of the tile
     __device__ __forceinline__ void store(unsigned char* slot, int lane) const {
@@ -393,7 +393,7 @@ struct F8Halves {
             const int c = n + 32 * i + lane;
             b[i] = 0;
             if (c < a.N) {
-                b[i] = a.bias_bf16 ? __ldg(static_cast<const uint16_t*>(a.bias) + c) : __ldg(static_cast<const uint32_t*>(a.bias) + c);
+                b[i] = a.bias_bf16 ? __ldcg(static_cast<const uint16_t*>(a.bias) + c) : __ldcg(static_cast<const uint32_t*>(a.bias) + c);
             }
         }
     }

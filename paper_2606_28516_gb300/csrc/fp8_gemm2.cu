@@ -333,8 +333,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8Cfg<BN_, KIND>::TH
                 for (int r = 0; r < C::ROUNDS; ++r) {
                     const int n = t.n0 + ((C::OVL && acc == 0 ? C::ROUNDS - 1 - r : r) * 4 + cg) * 32 + lane;
                     bias[r] = n >= a.N      ? 0.f
-                              : a.bias_bf16 ? bf16_to_f32(__ldg(static_cast<const uint16_t*>(a.bias) + n))
-                                            : __ldg(static_cast<const float*>(a.bias) + n);
+                              : a.bias_bf16 ? bf16_to_f32(__ldcg(static_cast<const uint16_t*>(a.bias) + n))
+                                            : __ldcg(static_cast<const float*>(a.bias) + n);
                 }
             }
         };
