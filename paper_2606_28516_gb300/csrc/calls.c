@@ -172,7 +172,7 @@ struct exchanged {
     int64_t* strides;
     uint64_t byte_offset;
 };
-enum { ON_CUDA = 2, CODE_FLOAT = 2, CODE_BFLOAT = 4 };
+enum { ON_CUDA = 2, CODE_INT = 0, CODE_FLOAT = 2, CODE_BFLOAT = 4 };
 static PyObject* g_to_dlpack; /* torch's function, or NULL */
 
 /* t as [rows x cols] (rows < 0: any number) on GPU `device` (negative: any): its shape, address, dtype and row pitch. 0 for
@@ -210,6 +210,26 @@ static int row_at(PyObject* t, int64_t n, int device, int64_t* p, int32_t* dt) {
         *p = (int64_t)(intptr_t)x->data + (int64_t)x->byte_offset;
         *dt = x->bits == 16 ? CLEARMOE_BF16 : CLEARMOE_F32;
     }
+    if (!x) PyErr_Clear();
+    Py_XDECREF(capsule);
+    return ok;
+}
+
+/* A status word (dense int32, its first element) on GPU `device` (negative: any), or None: its address. 0 for anything else,
+ * with no exception left. */
+static int status_at(PyObject* t, int device, int64_t* p) {
+    *p = 0;
+    if (t == Py_None) return 1;
+    PyObject* capsule = g_to_dlpack ? PyObject_CallOneArg(g_to_dlpack, t) : NULL;
+    const struct exchanged* x = capsule ? PyCapsule_GetPointer(capsule, "dltensor") : NULL;
+    int ok = x && x->device_type == ON_CUDA && (device < 0 || x->device_id == device) && x->code == CODE_INT && x->bits == 32 &&
+             x->lanes == 1 && (x->ndim == 0 || x->strides);
+    int64_t step = 1;
+    for (int i = ok ? x->ndim - 1 : -1; i >= 0; --i) {
+        ok = ok && x->shape[i] > 0 && (x->shape[i] == 1 || x->strides[i] == step);
+        step *= x->shape[i];
+    }
+    if (ok) *p = (int64_t)(intptr_t)x->data + (int64_t)x->byte_offset;
     if (!x) PyErr_Clear();
     Py_XDECREF(capsule);
     return ok;
@@ -413,7 +433,9 @@ static PyObject* fp4_gemm_t(PyObject* self, PyObject* const* args, Py_ssize_t n)
     if (n != 7) return PyErr_Format(PyExc_TypeError, "7 arguments expected, got %zd", n);
     if (!integers(args, 3, 3, v)) return NULL;
     const clearmoe_fp4 *A = PTR(0), *W = PTR(1);
-    if (!stream_and_device(args[6], &s, &device) || !HERE4(A) || !HERE4(W) || !row_at(args[3], W->rows, device, &bias, &bias_dt) || !status_of(args[4], &status)) Py_RETURN_NONE;
+    if (!stream_and_device(args[6], &s, &device) || !HERE4(A) || !HERE4(W) || !row_at(args[3], W->rows, device, &bias, &bias_dt) ||
+        !status_at(args[4], device, &status))
+        Py_RETURN_NONE;
     const clearmoe_fp8_epilogue epi = {AT(bias), bias_dt, (int32_t)v[2], AT(status)};
     const int blocks = PyLong_Check(args[5]);
     if (blocks) {
