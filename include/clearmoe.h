@@ -528,7 +528,8 @@ int clearmoe_debug_fp4_wait(int64_t wait_limit_ns);
 /* ---- a residual's addition and the root-mean-square norm of the sum ----
  *
  * s = x + residual, rounded to dtype, is the stream as it goes on; its norm y = s weight / sqrt(mean(s^2) + eps) feeds the
- * next sublayer. Sums and statistics in fp32 (a mean square past fp32's range makes the row zero), y rounded once.
+ * next sublayer. Sums and statistics in fp32, y rounded once. Squares and their sum may leave fp32's range where s and the mean
+ * square do not: a row is zero where its mean square is past the range, and with eps 0 NaN where it is all zeros, no others.
  *  x, residual (nullable: s = x), sum (nullable: s is not stored) [rows x cols] of dtype (F32 or BF16), rows ldx, ldr and
  *  lds elements apart; weight (nullable: ones) [cols] of weight_dtype; eps >= 0.
  * Every tensor may start anywhere that its element type allows. sum may be x or residual (with the same pitch), and out
