@@ -22,4 +22,10 @@ CM_HD inline DrainStep drain_step(uint32_t k, uint32_t n_even, uint32_t n_odd) {
     return DrainStep{k >= n_even && k < n_odd, k < n_even && k >= n_odd};
 }
 
+// The bytes of one CTA's boxes in the k-th stage of a walk whose last tile is a half (`halved`), k_half stages into it: `half`
+// of them from there on, `whole` before.
+CM_HD inline uint32_t drain_bytes(uint32_t k, bool halved, uint32_t k_half, uint32_t whole, uint32_t half) {
+    return halved && k >= k_half ? half : whole;
+}
+
 }  // namespace cm

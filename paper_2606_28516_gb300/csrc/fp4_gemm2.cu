@@ -250,14 +250,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P4Cfg<BN_, KIND>::TH
                 if (warp_uniform((int)*abort_flag) && mbar_wait_warp(stop_bar, 0, nullptr, a.status, 2 * lim + 10000000ull)) {
                     fence_cluster();
                     int rest;
-                    const uint32_t halves = (uint32_t)(t.whole(a, (int)gridDim.x >> 1, rest) * nkb);  // k-blocks before a half's
+                    const uint32_t k_half = (uint32_t)(t.whole(a, (int)gridDim.x >> 1, rest) * nkb);
                     const uint32_t at = smem_u32(tmem_slot + 2);
                     const uint32_t n0 = ld_cluster_u32(map_to_rank(at, 0)), n1 = ld_cluster_u32(map_to_rank(at, 1)), n = max(n0, n1);
     #pragma unroll 1
                     for (uint32_t k = n > STAGES ? n - STAGES : 0; k < n; ++k) {
                         const uint32_t s = k % STAGES;
                         const DrainStep st = drain_step(k, n0, n1);
-                        const uint32_t bytes = t.halved && k >= halves ? C::HALF_BYTES : C::STAGE_BYTES;
+                        const uint32_t bytes = drain_bytes(k, t.halved, k_half, C::STAGE_BYTES, C::HALF_BYTES);
                         // the odd CTA alone reached it: expect its bytes; the even CTA alone: count the odd one's as landed
                         if (st.arrive) mbar_arrive_expect_tx_warp(full_bar(s), bytes);
                         if (st.complete) mbar_complete_tx_warp(full_bar(s), bytes);
