@@ -288,7 +288,7 @@ struct Pick {
 // (256 columns on pairs) counts 0.6. A stage's cycles grow from what the MMAs and their scales take to what the path from L2
 // allows with every SM at work. Fitted to 99 products of 8 to 16,384 rows; what the rule chooses is 0.5 % slower than the
 // best kernel in the mean, 7 % at the most. In us, (64, 0), (128, 0), (128, 1), (256, 1) at M x N x K: 197 x 1,536 x 384 with
-// bias and GELU 3.0, 4.0, 3.9, 5.2; 788 x 768 x 2,048 3.7, 4.5, 4.6, 6.1; 1,970 x 2,304 x 768 5.5, 5.1, 5.5, 5.8; 6,000 x
+// bias and GELU 3.0, 3.9, 3.9, 5.4; 788 x 768 x 2,048 3.7, 4.5, 4.6, 6.1; 1,970 x 2,304 x 768 5.5, 5.1, 5.5, 5.8; 6,000 x
 // 384 x 1,536 5.2, 4.7, 5.5, 6.3; 2,048 x 4,096 x 4,096 24.4, 18.7, 16.5, 15.2; 4,096 x 4,096 x 4,096 45.3, 30.3, 25.9, 23.3.
 // (Tiles of 192 columns on pairs were nowhere the best by more than 1 %.)
 struct Fp4Kernel {

@@ -9,7 +9,7 @@
 // the scales of two times 128 of K, in turn.
 //
 // A last round with tiles for half of the pairs at the most has them in halves of 128 columns, one a pair (9,973 x 1,024 x
-// 4,096 in eight groups 20.7 -> 19.3 us, 2,560 x 2,048 x 4,096 14.8 -> 12.3, 10,240 x 1,024 x 4,096 20.1 -> 18.0).
+// 4,096 in eight groups 21.3 -> 19.9 us, 2,560 x 2,048 x 4,096 15.1 -> 12.4, 10,240 x 1,024 x 4,096 20.4 -> 18.1).
 //
 // Epilogue: 16 warps (four per lane quarter), each 32 columns at a time (one block of a 4-bit output), two times side by
 // side. What bounds it is the path of loads and stores (TMEM, shared and global memory): a store whose lanes write 32 rows

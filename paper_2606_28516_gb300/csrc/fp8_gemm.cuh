@@ -305,7 +305,7 @@ __device__ __forceinline__ void gelu_pairs_fp8(float* u) {
 
 // gelu_pair_bf16 for P pairs at once in the same way, of products in 4-bit blocks whichever kernel they take: NaN for -inf as
 // for NaN, by max(u, 0) = u - min(u, 0), which is exact. It costs an operation a value (8,192 x 4,096 x 1,024 to 4-bit blocks
-// 22.7 us with -inf to 0, 23.7 so; 25.6 with the difference packed, whose register pairs spilled).
+// 22.5 us with -inf to 0, 23.6 so; 25.6 with the difference packed, whose register pairs spilled; 29.1 with gelu_pair_f32).
 template <int P>
 __device__ __forceinline__ void gelu_pairs_bf16(float* u) {
     float2 v[P], q[P];
